@@ -346,6 +346,107 @@ estp_status estp_misalignment(estp_ctx* ctx, const float* entropy, const float* 
                               const int32_t* cu_seqlens, int32_t B, int64_t sumT, int32_t pct,
                               int32_t* counts_out, estp_stream_t stream);
 
+/* ------------------------------------------------------------------ (e)
+ * A paged KV cache that keeps, for every slot, the attention weight its token has received,
+ * so that decoding goes on with the importance the prefill measured (Eq. 2-0) and the cache
+ * can be held to a budget by it.  The paper stops at the prompt: these calls carry its
+ * importance into serving.
+ *
+ * A cache holds one layer.  Slot s of sequence b lies on page page_table[b, s / page_size], at
+ * s % page_size; the first length[b] slots are in use.  The order of the slots means nothing:
+ * after an eviction the KV heads of a slot may hold different tokens, each with a weight and a
+ * position of its own.
+ *   k, v       : [n_pages, page_size, Hkv, head_dim] in any order of the strides (elements, the
+ *                same for both; head_dim contiguous; 16-byte aligned, multiples of 16 bytes).
+ *                Unused slots may hold anything.
+ *   weight     : fp32 [n_pages, Hkv, page_size], or NULL (attention without accumulation only)
+ *   position   : int32 [n_pages, Hkv, page_size], or NULL (not needed by the attention)
+ *   page_table : int32 [B, max_pages]; entries past a sequence's slots are not read.  Sequences
+ *                may share pages for reading; calls that write (append, evict, accumulate)
+ *                need every page in one sequence only.
+ *   page_size  : a power of two, 8 .. 2^20
+ * The struct is a HOST pointer, its arrays caller-owned device memory.  Per sequence a program
+ * also holds length int32 [B] (slots in use) and seen int32 [B] (tokens so far: the position of
+ * the next one).  A length past the table, or a table entry outside the pool, records
+ * ESTP_ERR_INVALID_ARG in the status word; nothing outside the pool is touched. */
+typedef struct {
+    void* k;
+    void* v;
+    float* weight;
+    int32_t* position;
+    const int32_t* page_table;
+    int64_t page_stride, slot_stride, head_stride;
+    int64_t n_pages;
+    int32_t max_pages;
+    int32_t page_size;
+    int32_t Hkv;
+    int32_t head_dim;   /* 64 or 128 */
+    estp_dtype dtype;
+} estp_kv_cache;
+
+/* Rows enter the cache.  Entry e of cu_rows[b] .. cu_rows[b+1]-1 goes to slot
+ * length[b] + (e - cu_rows[b]) of sequence b, with position seen[b] + (e - cu_rows[b]); the new
+ * lengths and counts go to length_out and seen_out, which may be length and seen.
+ *   length, seen   : int32 [B], or both NULL: every sequence starts empty (its old rows are dropped)
+ *   k_new, v_new   : [n_new, Hkv, head_dim] of the cache's type, row stride ld_new elements
+ *   weight_new     : fp32 [n_new, Hkv], the rows' weights so far (the prefill's importance, or
+ *                    estp_cache_attention's weight_new_out), or NULL for 0
+ *   rows           : int32 [n_rows], the row of k_new that entry e takes (accepted drafts, for
+ *                    instance), or NULL: row e
+ *   cu_rows        : int32 [B + 1], cu_rows[0] = 0; n_rows is at least cu_rows[B] (a bound: entries
+ *                    past cu_rows[B] are ignored)
+ * A sequence whose entries do not fit its table keeps its length and records
+ * ESTP_ERR_INVALID_ARG. */
+estp_status estp_cache_append(estp_ctx* ctx, const estp_kv_cache* cache, const int32_t* length,
+                              const int32_t* seen, int32_t* length_out, int32_t* seen_out, int32_t B,
+                              const void* k_new, const void* v_new, int64_t ld_new, int64_t n_new,
+                              const float* weight_new, const int32_t* rows, const int32_t* cu_rows,
+                              int64_t n_rows, estp_stream_t stream);
+
+/* Attention of a step's rows over the cache, and the attention weight they give:
+ *   s_ij = softmax_scale * q_i . k_j,  lse_i = ln sum_j exp(s_ij),
+ *   out_i = sum_j exp(s_ij - lse_i) v_j,
+ *   weight_j += sum_{i, h of the KV head} row_weight_i exp(s_ij - lse_i)     (accumulate != 0)
+ * for the rows i = cu_rows[b] .. cu_rows[b+1]-1 of sequence b (a single token, or drafts that are
+ * not in the cache yet) over j = the sequence's cached slots and those of its rows that i sees.
+ * Query head h reads KV head h / (Hq / Hkv).  A row that sees nothing, or scores of -inf only,
+ * gives zeros and lse = -inf.
+ *   max_slots      : a bound of the sum of the lengths (it sizes the workspace; more slots on
+ *                    the device record ESTP_ERR_INVALID_ARG)
+ *   Q              : [n_rows, Hq, head_dim] of the cache's type, row stride ldq elements
+ *   k_new, v_new   : [n_rows, Hkv, head_dim], row stride ld_new, the rows' own K and V, or both
+ *                    NULL: rows see cached slots only
+ *   cu_rows        : int32 [B + 1], from 0 to n_rows; a sequence may have no row
+ *   max_rows       : at least every sequence's rows; <= 128, and max_rows * Hq / Hkv <= 1024
+ *                    (else ESTP_ERR_UNSUPPORTED)
+ *   tree_mask      : uint64 [n_rows, mask_words]: bit j of row i is set where i sees the
+ *                    sequence's j-th row (its own bit included); NULL: row i sees rows j <= i.
+ *                    What a hidden row holds, NaN among it, reaches no other row.
+ *   row_weight     : fp32 [n_rows] factor of a row's attention in the weights (a draft's
+ *                    probability, for instance; a row of factor 0 does not count), NULL for 1
+ *   out            : [n_rows, Hq, head_dim] of the cache's type
+ *   lse_out        : fp32 [Hq, n_rows], or NULL
+ *   weight_new_out : fp32 [n_rows, Hkv], what the rows' own keys received, or NULL
+ * fp32 accumulation.
+ * Repeated calls give identical outputs; the sums have one order for given lengths. */
+estp_status estp_cache_attention(estp_ctx* ctx, const estp_kv_cache* cache, const int32_t* length, int32_t B,
+                                 int64_t max_slots, const void* Q, int64_t ldq, int32_t Hq, const void* k_new,
+                                 const void* v_new, int64_t ld_new, const int32_t* cu_rows, int64_t n_rows,
+                                 int32_t max_rows, float softmax_scale, const uint64_t* tree_mask,
+                                 int32_t mask_words, const float* row_weight, int accumulate, void* out,
+                                 float* lse_out, float* weight_new_out, estp_stream_t stream);
+
+/* Cuts every sequence to at most `budget` slots.  Each KV head of a longer sequence keeps, in
+ * this order: tokens of the last `recent` positions and of the first `sinks` ones, then those of
+ * the greatest weight (NaN below everything), the lower slot first among equals.  Kept rows from
+ * slots at or past `budget`, in order, move into the slots below it that were freed, in order,
+ * with their weights and positions; other rows stay where they are.  length_out[b] =
+ * min(length[b], budget) (may be length).  The pages past it are the caller's again.
+ * recent + sinks <= budget. */
+estp_status estp_cache_evict(estp_ctx* ctx, const estp_kv_cache* cache, const int32_t* length,
+                             const int32_t* seen, int32_t* length_out, int32_t B, int32_t budget,
+                             int32_t recent, int32_t sinks, estp_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -41,7 +41,8 @@ EXPORTS = ("estp_create", "estp_destroy", "estp_last_error", "estp_sync_status",
            "estp_attn_importance_finalize", "estp_pool", "estp_token_entropy_noalloc",
            "estp_head_loss", "estp_misalignment", "estp_lm_head_entropy",
            "estp_mlp_head_predict", "estp_mlp_head_loss", "estp_attn_forward_importance",
-           "estp_set_wait_limit")
+           "estp_set_wait_limit", "estp_cache_append", "estp_cache_attention",
+           "estp_cache_evict")
 
 
 class EstpError(RuntimeError):
@@ -70,6 +71,15 @@ class _MlpHead(ctypes.Structure):
 class _MlpGrads(ctypes.Structure):
     _fields_ = [("W1", ctypes.c_void_p), ("b1", ctypes.c_void_p), ("W2", ctypes.c_void_p),
                 ("b2", ctypes.c_void_p), ("pooled", ctypes.c_void_p)]
+
+
+class _KVCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("position", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+                ("max_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int)]
 
 
 def load_library(path: str = LIB_PATH):
@@ -107,6 +117,10 @@ def load_library(path: str = LIB_PATH):
                                 ctypes.POINTER(_MlpGrads), P], ctypes.c_int),
         "estp_lm_head_entropy": ([P, P, I64, P, I64, ctypes.c_int, I64, I64, I64, P, P],
                                  ctypes.c_int),
+        "estp_cache_append": ([P, P, P, P, P, P, I32, P, P, I64, I64, P, P, P, I64, P], ctypes.c_int),
+        "estp_cache_attention": ([P, P, P, I32, I64, P, I64, I32, P, P, I64, P, I64, I32, F, P, I32, P,
+                                  ctypes.c_int, P, P, P, P], ctypes.c_int),
+        "estp_cache_evict": ([P, P, P, P, P, I32, I32, I32, I32, P], ctypes.c_int),
     }
     for name, (args, res) in sigs.items():
         fn = getattr(lib, name)
@@ -163,6 +177,56 @@ class MlpHead:
     W2: "object"
     b2: "object"
     centers: "object"
+
+
+def _like(t, dtype, shape, name):
+    """A dense tensor of this type and shape (None passes)."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError(f"{name} is a contiguous {dtype} tensor of shape {tuple(shape)}")
+
+
+class KVCache:
+    """A paged KV cache of one layer (estp_kv_cache) over tensors that the caller owns.
+
+    k, v       [n_pages, page_size, Hkv, d] bf16 or fp32, in any order of strides (a permuted
+               view of head-major pages, for instance), d contiguous
+    page_table int32 [B, max_pages];  length, seen: int32 [B], updated in place
+    weight     fp32 [n_pages, Hkv, page_size], position: int32 of that shape, or None
+    max_slots  a bound of the slots in use over all sequences (default: what the page table can
+               hold; with weights, which need every page in one sequence only, at most the pool's)
+    """
+
+    def __init__(self, k, v, page_table, length, seen, weight=None, position=None, max_slots=None):
+        import torch
+        n_pages, page, Hkv, d = k.shape
+        if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype or (k.numel() and k.stride(3) != 1):
+            raise ValueError("k and v share their type, shape and strides, with contiguous rows")
+        B, per = page_table.shape
+        _like(page_table, torch.int32, (B, per), "page_table")
+        _like(length, torch.int32, (B,), "length")
+        _like(seen, torch.int32, (B,), "seen")
+        _like(weight, torch.float32, (n_pages, Hkv, page), "weight")
+        _like(position, torch.int32, (n_pages, Hkv, page), "position")
+        self.k, self.v, self.page_table, self.length, self.seen = k, v, page_table, length, seen
+        self.weight, self.position = weight, position
+        self.B = B
+        self.Hkv, self.head_dim, self.dtype = Hkv, d, k.dtype
+        bound = B * per * page
+        if weight is not None:
+            bound = min(bound, n_pages * page)
+        self.max_slots = bound if max_slots is None else int(max_slots)
+        self._c = _KVCache(_ptr(k), _ptr(v), _ptr(weight), _ptr(position), _ptr(page_table), k.stride(0),
+                           k.stride(1), k.stride(2), n_pages, per, page, Hkv, d, _dtype(k))
+        self._ref = ctypes.addressof(self._c)
+
+    def _rows(self, t, heads, name):
+        """Row stride of a [rows, heads, d] tensor of the cache's type."""
+        if t.dtype != self.dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim:
+            raise ValueError(f"{name} is a {self.dtype} tensor [rows, {heads}, {self.head_dim}]")
+        rows, s0, s1, s2 = t.shape[0], *t.stride()
+        if rows and (s2 != 1 or (heads > 1 and s1 != self.head_dim)):
+            raise ValueError(f"{name}: a row's heads are contiguous")
+        return s0 if rows > 1 else heads * self.head_dim
 
 
 class Context:
@@ -391,3 +455,71 @@ class Context:
                              _ptr(pooled), _ptr(pred) if head is not None else None,
                              _stream(stream)))
         return pooled, (pred if head is not None else None)
+
+    # ------------------------------------------------------------------ (e)
+    def cache_append(self, cache: KVCache, k_new, v_new, cu_rows, weight=None, rows=None,
+                     fresh: bool = False, stream=None):
+        """estp_cache_append: rows of k_new, v_new [n, Hkv, d] enter the cache, cu_rows[b] ..
+        cu_rows[b+1]-1 into sequence b; `rows` (int32) picks rows of k_new, `weight` [n, Hkv]
+        gives their attention weights so far.  fresh: the sequences start empty.  cache.length
+        and cache.seen are updated in place."""
+        import torch
+        n = k_new.shape[0]
+        ld = cache._rows(k_new, cache.Hkv, "k_new")
+        if cache._rows(v_new, cache.Hkv, "v_new") != ld or v_new.shape[0] != n:
+            raise ValueError("k_new and v_new share their shape and row stride")
+        if weight is not None:
+            _like(weight, torch.float32, (n, cache.Hkv), "weight")
+        _like(cu_rows, torch.int32, (cache.B + 1,), "cu_rows")
+        if rows is not None:
+            _like(rows, torch.int32, (rows.numel(),), "rows")
+        length, seen = cache.length.data_ptr(), cache.seen.data_ptr()
+        self._check(self._lib.estp_cache_append(
+            self._h, cache._ref, None if fresh else length, None if fresh else seen, length, seen, cache.B,
+            k_new.data_ptr(), v_new.data_ptr(), ld, n, _ptr(weight), _ptr(rows), cu_rows.data_ptr(),
+            n if rows is None else rows.numel(), _stream(stream)))
+
+    def cache_attention(self, cache: KVCache, Q, k_new, v_new, cu_rows, max_rows: int,
+                        scale: float | None = None, tree_mask=None, row_weight=None,
+                        accumulate: bool = False, details: bool = False, out=None, stream=None):
+        """estp_cache_attention: Q [n, Hq, d] over the cache and the rows' own k_new, v_new
+        [n, Hkv, d] (None: the cache alone); returns out [n, Hq, d], with details (out,
+        lse [Hq, n], weight_new [n, Hkv] or None).  tree_mask: int64 or uint64 [n, words], bit j
+        of a row set where it sees the sequence's j-th row.  accumulate adds the attention the
+        slots receive, times row_weight [n], to cache.weight."""
+        import torch
+        n, Hq, d = Q.shape
+        ldq = cache._rows(Q, Hq, "Q")
+        ld = 0
+        if k_new is not None:
+            ld = cache._rows(k_new, cache.Hkv, "k_new")
+            if cache._rows(v_new, cache.Hkv, "v_new") != ld or k_new.shape[0] != n or v_new.shape[0] != n:
+                raise ValueError("k_new and v_new have a row for each of Q's, of one row stride")
+        _like(cu_rows, torch.int32, (cache.B + 1,), "cu_rows")
+        words = 0
+        if tree_mask is not None:
+            words = tree_mask.shape[-1]
+            _like(tree_mask, torch.uint64 if tree_mask.dtype == torch.uint64 else torch.int64, (n, words), "tree_mask")
+        if row_weight is not None:
+            _like(row_weight, torch.float32, (n,), "row_weight")
+        dev = Q.device
+        if out is None:
+            out = torch.empty(n, Hq, d, dtype=Q.dtype, device=dev)
+        else:
+            _like(out, Q.dtype, (n, Hq, d), "out")
+        lse = torch.empty(Hq, n, dtype=torch.float32, device=dev) if details else None
+        w_new = torch.empty(n, cache.Hkv, dtype=torch.float32, device=dev) if details and k_new is not None else None
+        self._check(self._lib.estp_cache_attention(
+            self._h, cache._ref, cache.length.data_ptr(), cache.B, cache.max_slots, Q.data_ptr(), ldq, Hq,
+            _ptr(k_new), _ptr(v_new), ld, cu_rows.data_ptr(), n, max_rows,
+            1.0 / math.sqrt(d) if scale is None else scale, _ptr(tree_mask), words, _ptr(row_weight),
+            1 if accumulate else 0, out.data_ptr(), _ptr(lse), _ptr(w_new), _stream(stream)))
+        return (out, lse, w_new) if details else out
+
+    def cache_evict(self, cache: KVCache, budget: int, recent: int = 0, sinks: int = 0, stream=None):
+        """estp_cache_evict: every sequence is cut to at most `budget` slots, each KV head keeping
+        its last `recent` and first `sinks` tokens and then those of the greatest weight;
+        cache.length is updated in place."""
+        length = cache.length.data_ptr()
+        self._check(self._lib.estp_cache_evict(self._h, cache._ref, length, cache.seen.data_ptr(), length, cache.B,
+                                               budget, recent, sinks, _stream(stream)))

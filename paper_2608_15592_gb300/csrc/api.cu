@@ -5,6 +5,7 @@
 #include <cstring>
 #include <new>
 
+#include "cache.cuh"
 #include "estp_internal.cuh"
 #include "tcgen05.cuh"
 
@@ -112,9 +113,11 @@ estp_status estp_create(estp_ctx** out, int device) {
     if (st != ESTP_OK) { delete ctx; return st; }
     e = cudaDeviceGetAttribute(&ctx->num_sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) { delete ctx; return cuda_fail(e, "cudaDeviceGetAttribute"); }
-    e = cudaMalloc(&ctx->status, sizeof(int));
-    if (e == cudaSuccess) e = cudaMemset(ctx->status, 0, sizeof(int));
+    // the status word and, on the next 128-byte line, the cache kernels' arrival counter
+    e = cudaMalloc(&ctx->status, 256);
+    if (e == cudaSuccess) e = cudaMemset(ctx->status, 0, 256);
     if (e != cudaSuccess) { cudaFree(ctx->status); delete ctx; return cuda_fail(e, "status word"); }
+    ctx->done = reinterpret_cast<uint32_t*>(ctx->status) + 32;
     *out = ctx;
     return ESTP_OK;
 }
@@ -154,7 +157,8 @@ estp_status estp_sync_status(estp_ctx* ctx, estp_stream_t stream) {
     switch (code) {
         case ESTP_OK: return ESTP_OK;
         case ESTP_ERR_INVALID_ARG:
-            return fail(ESTP_ERR_INVALID_ARG, "device check failed: cu_seqlens or max_seqlen");
+            return fail(ESTP_ERR_INVALID_ARG,
+                        "device check failed: cu_seqlens or max_seqlen, or a cache's lengths or page table");
         case ESTP_ERR_TIMEOUT: return fail(ESTP_ERR_TIMEOUT, "a device-side wait timed out");
         default: return fail((estp_status)code, "device status %d", code);
     }
@@ -450,6 +454,147 @@ estp_status estp_misalignment(estp_ctx* ctx, const float* entropy, const float* 
     if (st != ESTP_OK) return st;
     return launch_misalignment(ctx, entropy, importance, cu_seqlens, B, sumT, pct, counts_out,
                                reinterpret_cast<cudaStream_t>(stream));
+}
+
+// Checks a cache and describes it to the kernels.
+static estp_status check_cache(estp_ctx* ctx, const estp_kv_cache* c, int32_t B, CacheView* view) {
+    if (!ctx) return fail(ESTP_ERR_INVALID_ARG, "ctx is NULL");
+    if (!c) return fail(ESTP_ERR_INVALID_ARG, "cache is NULL");
+    if (c->dtype != ESTP_F32 && c->dtype != ESTP_BF16) return fail(ESTP_ERR_INVALID_ARG, "dtype");
+    if (c->head_dim != 64 && c->head_dim != 128)
+        return fail(ESTP_ERR_UNSUPPORTED, "head_dim %d (64 or 128 supported)", c->head_dim);
+    if (c->Hkv < 1 || c->Hkv > 256) return fail(ESTP_ERR_INVALID_ARG, "need 1 <= Hkv <= 256");
+    if (c->page_size < 8 || c->page_size > (1 << 20) || (c->page_size & (c->page_size - 1)))
+        return fail(ESTP_ERR_INVALID_ARG, "page_size must be a power of two in 8..2^20");
+    if (B < 0 || c->n_pages < 0 || c->n_pages > INT32_MAX || c->max_pages < 0)
+        return fail(ESTP_ERR_INVALID_ARG, "need B, n_pages, max_pages >= 0 and n_pages < 2^31");
+    if ((int64_t)c->max_pages * c->page_size > (1 << 30))
+        return fail(ESTP_ERR_INVALID_ARG, "a sequence has at most 2^30 slots");
+    const int64_t es = esize(c->dtype);
+    if (c->slot_stride < c->head_dim || c->head_stride < c->head_dim || c->page_stride < c->head_dim)
+        return fail(ESTP_ERR_INVALID_ARG, "cache strides must be at least head_dim");
+    if (c->page_stride * es % 16 || c->slot_stride * es % 16 || c->head_stride * es % 16)
+        return fail(ESTP_ERR_INVALID_ARG, "cache strides must be multiples of 16 bytes");
+    if (B > 0 && c->n_pages > 0 && (!c->k || !c->v || !c->page_table))
+        return fail(ESTP_ERR_INVALID_ARG, "NULL cache pointer");
+    if (!aligned16(c->k) || !aligned16(c->v))
+        return fail(ESTP_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+    int shift = 0;
+    while ((1 << shift) < c->page_size) ++shift;
+    *view = CacheView{static_cast<char*>(c->k), static_cast<char*>(c->v), c->weight, c->position, c->page_table,
+                      c->page_stride * es, c->slot_stride * es, c->head_stride * es, c->n_pages, c->max_pages,
+                      shift, c->Hkv, c->head_dim};
+    return set_device(ctx);
+}
+
+// Rows beside a cache: [rows, Hkv, head_dim] with a row stride.
+static estp_status check_rows(const estp_kv_cache* c, const void* k, const void* v, int64_t ld) {
+    if (!k || !v) return fail(ESTP_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (ld < (int64_t)c->Hkv * c->head_dim || ld * esize(c->dtype) % 16 || !aligned16(k) || !aligned16(v))
+        return fail(ESTP_ERR_INVALID_ARG, "new rows: 16-byte aligned, row stride >= Hkv * head_dim and a multiple of 16 bytes");
+    return ESTP_OK;
+}
+
+estp_status estp_cache_append(estp_ctx* ctx, const estp_kv_cache* cache, const int32_t* length,
+                              const int32_t* seen, int32_t* length_out, int32_t* seen_out, int32_t B,
+                              const void* k_new, const void* v_new, int64_t ld_new, int64_t n_new,
+                              const float* weight_new, const int32_t* rows, const int32_t* cu_rows,
+                              int64_t n_rows, estp_stream_t stream) {
+    ESTP_NVTX_RANGE("estp_cache_append");
+    CacheView view;
+    estp_status st = check_cache(ctx, cache, B, &view);
+    if (st != ESTP_OK) return st;
+    if (n_rows < 0 || n_rows > INT32_MAX || n_new < 0 || n_new > INT32_MAX)
+        return fail(ESTP_ERR_INVALID_ARG, "need 0 <= n_rows, n_new < 2^31");
+    if (!rows && n_rows > n_new) return fail(ESTP_ERR_INVALID_ARG, "n_rows > n_new without a list of rows");
+    if (B == 0) return ESTP_OK;
+    if (!cu_rows || !length_out || !seen_out || (length != nullptr) != (seen != nullptr))
+        return fail(ESTP_ERR_INVALID_ARG, "need cu_rows, length_out, seen_out, and length and seen or neither");
+    if (n_rows > 0) {
+        st = check_rows(cache, k_new, v_new, ld_new);
+        if (st != ESTP_OK) return st;
+    }
+    return launch_cache_append(ctx, view, cache->head_dim * esize(cache->dtype), B, length, seen, length_out, seen_out,
+                               k_new, v_new, ld_new * esize(cache->dtype), n_new, weight_new, rows, cu_rows, n_rows,
+                               reinterpret_cast<cudaStream_t>(stream));
+}
+
+estp_status estp_cache_attention(estp_ctx* ctx, const estp_kv_cache* cache, const int32_t* length, int32_t B,
+                                 int64_t max_slots, const void* Q, int64_t ldq, int32_t Hq, const void* k_new,
+                                 const void* v_new, int64_t ld_new, const int32_t* cu_rows, int64_t n_rows,
+                                 int32_t max_rows, float softmax_scale, const uint64_t* tree_mask,
+                                 int32_t mask_words, const float* row_weight, int accumulate, void* out,
+                                 float* lse_out, float* weight_new_out, estp_stream_t stream) {
+    ESTP_NVTX_RANGE("estp_cache_attention");
+    CacheAttnArgs a{};
+    estp_status st = check_cache(ctx, cache, B, &a.c);
+    if (st != ESTP_OK) return st;
+    const int es = esize(cache->dtype);
+    if (Hq < 1 || Hq > 256 || Hq % cache->Hkv) return fail(ESTP_ERR_INVALID_ARG, "need Hq <= 256, Hq %% Hkv == 0");
+    if (!(softmax_scale > 0.f) || !std::isfinite(softmax_scale))
+        return fail(ESTP_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+    if (n_rows < 0 || n_rows > INT32_MAX || max_rows < 0 || max_rows > n_rows || max_slots < 0)
+        return fail(ESTP_ERR_INVALID_ARG, "need 0 <= max_rows <= n_rows < 2^31 and max_slots >= 0");
+    const int rep = Hq / cache->Hkv;
+    if (max_rows > kCacheMaxRows || max_rows * rep > kCacheMaxGroupRows)
+        return fail(ESTP_ERR_UNSUPPORTED, "at most %d rows a sequence, and max_rows * Hq / Hkv <= %d", kCacheMaxRows,
+                    kCacheMaxGroupRows);
+    if (B == 0 || n_rows == 0) return ESTP_OK;
+    if (max_rows == 0) return fail(ESTP_ERR_INVALID_ARG, "max_rows is 0 and n_rows is not");
+    if (!length || !cu_rows || !Q || !out) return fail(ESTP_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (ldq < (int64_t)Hq * cache->head_dim || ldq * es % 16 || !aligned16(Q) || !aligned16(out))
+        return fail(ESTP_ERR_INVALID_ARG, "Q and out: 16-byte aligned, ldq >= Hq * head_dim and a multiple of 16 bytes");
+    if ((k_new != nullptr) != (v_new != nullptr)) return fail(ESTP_ERR_INVALID_ARG, "k_new and v_new, or neither");
+    if (k_new) {
+        st = check_rows(cache, k_new, v_new, ld_new);
+        if (st != ESTP_OK) return st;
+    }
+    if (tree_mask && (int64_t)mask_words * 64 < max_rows)
+        return fail(ESTP_ERR_INVALID_ARG, "mask_words * 64 must cover max_rows");
+    if (accumulate && !cache->weight) return fail(ESTP_ERR_INVALID_ARG, "accumulate needs the cache's weights");
+    if (weight_new_out && !k_new) return fail(ESTP_ERR_INVALID_ARG, "weight_new_out needs k_new");
+    a.length = length;
+    a.cu = cu_rows;
+    a.B = B;
+    a.n_rows = n_rows;
+    const int64_t most = (int64_t)B * a.c.capacity();
+    a.n_slots = max_slots < most ? max_slots : most;
+    a.max_rows = max_rows;
+    a.Hq = Hq;
+    a.rep = rep;
+    a.Q = static_cast<const char*>(Q);
+    a.kn = static_cast<const char*>(k_new);
+    a.vn = static_cast<const char*>(v_new);
+    a.ldq = ldq * es;
+    a.ldn = ld_new * es;
+    a.tree = tree_mask;
+    a.words = mask_words;
+    a.row_weight = row_weight;
+    a.scale = softmax_scale;
+    a.scale_log2 = softmax_scale * kLog2e;
+    a.out = static_cast<char*>(out);
+    a.lse = lse_out;
+    a.w_new = weight_new_out;
+    a.accumulate = accumulate != 0;
+    a.status = ctx->status;
+    a.wait_cycles = ctx->wait_cycles;
+    return launch_cache_attention(ctx, a, cache->dtype, reinterpret_cast<cudaStream_t>(stream));
+}
+
+estp_status estp_cache_evict(estp_ctx* ctx, const estp_kv_cache* cache, const int32_t* length,
+                             const int32_t* seen, int32_t* length_out, int32_t B, int32_t budget,
+                             int32_t recent, int32_t sinks, estp_stream_t stream) {
+    ESTP_NVTX_RANGE("estp_cache_evict");
+    CacheView view;
+    estp_status st = check_cache(ctx, cache, B, &view);
+    if (st != ESTP_OK) return st;
+    if (budget < 1 || recent < 0 || sinks < 0 || (int64_t)recent + sinks > budget)
+        return fail(ESTP_ERR_INVALID_ARG, "need budget >= 1, recent, sinks >= 0 and recent + sinks <= budget");
+    if (B == 0) return ESTP_OK;
+    if (!length || !seen || !length_out || !cache->weight || !cache->position)
+        return fail(ESTP_ERR_INVALID_ARG, "need length, seen, length_out and the cache's weights and positions");
+    return launch_cache_evict(ctx, view, cache->head_dim * esize(cache->dtype), B, length, seen, length_out, budget,
+                              recent, sinks, reinterpret_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

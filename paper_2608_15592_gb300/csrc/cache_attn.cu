@@ -1,0 +1,424 @@
+// Attention of a step's rows over a paged KV cache, with the attention weight that every cached
+// slot receives:
+//   s_ij = scale q_i . k_j,  lse_i = ln sum_j e^s_ij,  o_i = sum_j e^(s_ij - lse_i) v_j,
+//   weight_j += sum_i c_i e^(s_ij - lse_i)
+// over the cached slots and the drafts that row i sees.  Two launches:
+//
+// cache_fwd_kernel: a persistent grid over the units of cache.cuh.  Of every group segment it
+// leaves the running maximum m (log2 units), the sum l = sum 2^(s' - m) and O = sum 2^(s' - m) v,
+// s' = s log2(e), and, where the weights are wanted and fit, every unscaled score q.k.
+//
+// cache_finish_kernel: merges the partials of each row in CTA order, writes o and lse, and adds to
+// every slot the weight of its rows, sum_r c_r 2^(s' - M_r) / L_r, from the kept scores or from
+// scores formed again.  No floating-point atomics: every sum has one order.
+//
+// A row that sees nothing (M = -inf, L = 0) gives o = 0 and lse = -inf and no weight.
+#include "cache.cuh"
+
+namespace estp {
+namespace {
+
+constexpr int kThreads = 128;  // one key of a tile each
+constexpr int kRows = 8;       // rows of a block of the CUDA-core kernels
+
+template <class T> struct Unit;  // 16 bytes of a row
+template <> struct Unit<float> {
+    static constexpr int n = 4;
+    static __device__ __forceinline__ void get(const char* p, float* v) {
+        const float4 x = *reinterpret_cast<const float4*>(p);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    }
+    static __device__ __forceinline__ float one(const char* p) { return *reinterpret_cast<const float*>(p); }
+    static __device__ __forceinline__ void put(char* p, float v) { *reinterpret_cast<float*>(p) = v; }
+};
+template <> struct Unit<__nv_bfloat16> {
+    static constexpr int n = 8;
+    static __device__ __forceinline__ void get(const char* p, float* v) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        v[0] = bf16lo(x.x); v[1] = bf16hi(x.x); v[2] = bf16lo(x.y); v[3] = bf16hi(x.y);
+        v[4] = bf16lo(x.z); v[5] = bf16hi(x.z); v[6] = bf16lo(x.w); v[7] = bf16hi(x.w);
+    }
+    static __device__ __forceinline__ float one(const char* p) {
+        return __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(p));
+    }
+    static __device__ __forceinline__ void put(char* p, float v) {
+        *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(v);
+    }
+};
+
+// Where key j of a tile lies: NULL past the tile's keys (or on a page that is none).
+struct KeyRow {
+    const char* k;
+    const char* v;
+    int64_t meta;  // weight element of a cached slot
+};
+__device__ __forceinline__ KeyRow key_row(const CacheAttnArgs& a, const SeqShape& q, int b, int g, int tile, int j,
+                                          int row_bytes) {
+    KeyRow r{nullptr, nullptr, -1};
+    if (tile == q.nt - 1) {
+        if (a.kn != nullptr && j < q.n) {
+            const int64_t off = (int64_t)(a.cu[b] + j) * a.ldn + (int64_t)g * row_bytes;
+            r.k = a.kn + off;
+            r.v = a.vn + off;
+        }
+    } else {
+        const int slot = tile * kCacheTile + j;
+        if (slot < q.len) {
+            const int64_t page = a.c.page_of(b, slot, a.status);
+            if (page >= 0) {
+                const int64_t off = a.c.row(page, slot, g);
+                r.k = a.c.k + off;
+                r.v = a.c.v + off;
+                r.meta = a.c.meta(page, slot, g);
+            }
+        }
+    }
+    return r;
+}
+
+// kRows rows of Q, from row r0 of (b, g), as floats; rows past nr are zero.
+template <class T, int D>
+__device__ __forceinline__ void load_q(const CacheAttnArgs& a, float (*q)[D], int b, int g, int r0, int nr) {
+    constexpr int kU = D / Unit<T>::n;
+    for (int e = threadIdx.x; e < kRows * kU; e += kThreads) {
+        const int r = e / kU, c = e % kU;
+        float v[Unit<T>::n];
+        for (int i = 0; i < Unit<T>::n; ++i) v[i] = 0.f;
+        if (r < nr) {
+            const int i = (r0 + r) / a.rep, h = g * a.rep + (r0 + r) % a.rep;
+            Unit<T>::get(a.Q + (a.cu[b] + i) * a.ldq + ((int64_t)h * D) * sizeof(T) + c * 16, v);
+        }
+        for (int i = 0; i < Unit<T>::n; ++i) q[r][c * Unit<T>::n + i] = v[i];
+    }
+}
+
+template <class T, int D>
+__device__ __forceinline__ void dots(const float (*q)[D], const char* k, float* z) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) z[r] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < D / Unit<T>::n; ++c) {
+        float kv[Unit<T>::n];
+        Unit<T>::get(k + c * 16, kv);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int i = 0; i < Unit<T>::n; ++i) z[r] = fmaf(q[r][c * Unit<T>::n + i], kv[i], z[r]);
+    }
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs a) {
+    __shared__ PlanScratch sc;
+    __shared__ Place place;
+    __shared__ float q[kRows][D];
+    __shared__ float p[kRows][kCacheTile];
+    __shared__ const char* vrow[kCacheTile];
+    __shared__ float red[kThreads / 32][kRows];
+    __shared__ float o_half[kRows][D];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int64_t c = blockIdx.x;
+    const PlanTotals tot = plan_block(a, &sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int64_t u = unit_begin(c, all.units, ctas_of(a, all.units));
+        if (u >= x.unit0 && u < x.unit0 + s.units(a.c.Hkv)) place = x;
+    });
+    const int64_t G = ctas_of(a, tot.units);
+    if (!tot.ok || c >= G) return;
+    int64_t u = unit_begin(c, tot.units, G);
+    const int64_t u1 = unit_begin(c + 1, tot.units, G);
+    Place at = place;
+    constexpr int kHalves = kThreads / D, kKeys = kCacheTile / kHalves;  // PV: threads of a column, keys of each
+    const int col = t % D, half = t / D;
+    while (u < u1) {
+        const SeqShape s = seq_shape(a, at.b);
+        if (u >= at.unit0 + s.units(a.c.Hkv)) {
+            at.unit0 += s.units(a.c.Hkv);
+            at.group0 += (int64_t)a.c.Hkv * s.nrb;
+            ++at.b;
+            continue;
+        }
+        const int64_t loc = u - at.unit0;
+        const int grp = (int)(loc / s.nt), tile0 = (int)(loc % s.nt);
+        const int tile1 = (int)min((int64_t)s.nt, tile0 + (u1 - u));
+        const int g = grp / s.nrb, r0 = grp % s.nrb * kRows, nr = min(kRows, s.n * a.rep - r0);
+        const int64_t row0 = a.cu[at.b];
+        __syncthreads();
+        load_q<T, D>(a, q, at.b, g, r0, nr);
+        float m[kRows], l[kRows], o[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+            o[r] = 0.f;
+        }
+        for (int tile = tile0; tile < tile1; ++tile, ++u) {
+            const bool drafts = tile == s.nt - 1;
+            const KeyRow kr = key_row(a, s, at.b, g, tile, t, D * (int)sizeof(T));
+            __syncthreads();  // p and vrow are free, q is there
+            float z[kRows];
+            if (kr.k != nullptr) dots<T, D>(q, kr.k, z);
+            vrow[t] = kr.v;
+            unsigned hidden = 0;  // rows that do not see this key
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                if (kr.k == nullptr || (drafts && !(r < nr && sees_draft(a, row0, (r0 + r) / a.rep, t)))) {
+                    hidden |= 1u << r;
+                    z[r] = -INFINITY;
+                }
+            }
+            if (a.store)
+                for (int r = 0; r < nr; ++r) a.score[(u * kRows + r) * kCacheTile + t] = z[r];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                float x = z[r];
+                for (int w = 16; w > 0; w >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
+                if (lane == 0) red[warp][r] = x;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const float top = fmaxf(fmaxf(red[0][r], red[1][r]), fmaxf(red[2][r], red[3][r])) * a.scale_log2;
+                const float mn = fmaxf(m[r], top);
+                const float f = m[r] == mn ? 1.f : ex2(m[r] - mn);  // m = -inf: 0, and l = o = 0
+                m[r] = mn;
+                const float e = ex2(fmaf(z[r], a.scale_log2, mn == -INFINITY ? 0.f : -mn));
+                l[r] = fmaf(l[r], f, hidden >> r & 1 ? 0.f : e);
+                o[r] *= f;
+                p[r][t] = hidden >> r & 1 ? -1.f : e;  // no probability: the key adds nothing, whatever its V holds
+            }
+            __syncthreads();
+            for (int j = half * kKeys; j < (half + 1) * kKeys; ++j) {
+                const char* vr = vrow[j];
+                if (vr == nullptr) continue;
+                const float v = Unit<T>::one(vr + col * sizeof(T));
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    const float e = p[r][j];
+                    if (!(e < 0.f)) o[r] = fmaf(e, v, o[r]);
+                }
+            }
+        }
+        // the segment's partial: l over the keys' threads, O over the halves
+        const int64_t slot = c + at.group0 + grp;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            float x = l[r];
+            for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
+            if (lane == 0) red[warp][r] = x;
+            if (half == 1) o_half[r][col] = o[r];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (r >= nr) break;
+            if (t == 0)
+                a.part_ml[slot * kRows + r] = make_float2(m[r], (red[0][r] + red[1][r]) + (red[2][r] + red[3][r]));
+            if (half == 0) a.part_o[(slot * kRows + r) * D + col] = kHalves == 2 ? o[r] + o_half[r][col] : o[r];
+        }
+    }
+}
+
+// Pieces of row r of (b, g): CTAs c0..c1 hold the group, at slot c + group.
+struct Pieces {
+    int64_t c0, c1, group;
+};
+__device__ __forceinline__ Pieces pieces_of(const CacheAttnArgs& a, const Place& at, const SeqShape& s, int g, int r,
+                                            int64_t units) {
+    const int64_t grp = (int64_t)g * s.nrb + r / a.RB, ub = at.unit0 + grp * s.nt;
+    const int64_t G = ctas_of(a, units);
+    return Pieces{cta_of(ub, units, G), cta_of(ub + s.nt - 1, units, G), at.group0 + grp};
+}
+
+// Warp-wide: the row's maximum and sum over its pieces.
+__device__ __forceinline__ float2 merged_ml(const CacheAttnArgs& a, const Pieces& w, int r, int lane) {
+    float M = -INFINITY, L = 0.f;
+    for (int64_t c = w.c0 + lane; c <= w.c1; c += 32) {
+        const float2 x = a.part_ml[(c + w.group) * a.RB + r % a.RB];
+        const float mn = fmaxf(M, x.x);
+        if (mn != -INFINITY) L = fmaf(L, ex2(M - mn), x.y * ex2(x.x - mn));
+        else L += x.y;  // NaN stays
+        M = mn;
+    }
+    for (int o = 16; o > 0; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, M, o), l2 = __shfl_xor_sync(0xffffffffu, L, o);
+        const float mn = fmaxf(M, m2);
+        // unfused products: both lanes of a pair get the same bits
+        if (mn != -INFINITY) L = __fadd_rn(__fmul_rn(L, ex2(M - mn)), __fmul_rn(l2, ex2(m2 - mn)));
+        else L += l2;
+        M = mn;
+    }
+    return make_float2(M, L);
+}
+
+// rows x heads and (KV head, tile) items, both cut evenly over the grid.
+template <class T, int D, bool kStore>
+__global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnArgs a) {
+    __shared__ PlanScratch sc;
+    __shared__ Place place_row, place_item;
+    __shared__ float2 ml[kCacheMaxGroupRows];  // (-M, c / L) of every row of (b, g)
+    __shared__ float q[kStore ? 1 : kRows][D];
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int64_t c = blockIdx.x, G = gridDim.x;
+    const int64_t x0 = unit_begin(c, a.n_rows * a.Hq, G), x1 = unit_begin(c + 1, a.n_rows * a.Hq, G);
+    const PlanTotals tot = plan_block(a, &sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int64_t y = (int64_t)a.cu[x.b] * a.Hq, it = unit_begin(c, all.items, G);
+        if (x0 >= y && x0 < y + (int64_t)s.n * a.Hq) place_row = x;
+        if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) place_item = x;
+    });
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the partials are complete
+    if (!tot.ok) return;
+
+    if (x0 < x1) {  // o and lse: a warp a (row, head)
+        Place at = place_row;
+        SeqShape s = seq_shape(a, at.b);
+        for (int64_t x = x0 + warp; x < x1; x += kThreads / 32) {
+            while (x >= (int64_t)a.cu[at.b + 1] * a.Hq) {
+                at.unit0 += s.units(a.c.Hkv);
+                at.group0 += (int64_t)a.c.Hkv * s.nrb;
+                ++at.b;
+                s = seq_shape(a, at.b);
+            }
+            const int64_t row = x / a.Hq;
+            const int h = (int)(x % a.Hq), i = (int)(row - a.cu[at.b]), r = i * a.rep + h % a.rep;
+            const Pieces w = pieces_of(a, at, s, h / a.rep, r, tot.units);
+            const float2 all = merged_ml(a, w, r, lane);
+            constexpr int kC = D / 32;
+            float o[kC];
+#pragma unroll
+            for (int k = 0; k < kC; ++k) o[k] = 0.f;
+#pragma unroll 4
+            for (int64_t pc = w.c0; pc <= w.c1; ++pc) {
+                const int64_t e = (pc + w.group) * a.RB + r % a.RB;
+                const float m = a.part_ml[e].x;
+                const float f = m == all.x ? 1.f : ex2(m - all.x);
+#pragma unroll
+                for (int k = 0; k < kC; ++k) o[k] = fmaf(f, a.part_o[e * D + k * 32 + lane], o[k]);
+            }
+            const float inv = all.x == -INFINITY && all.y == 0.f ? 0.f : 1.f / all.y;
+            char* to = a.out + (row * a.Hq + h) * D * (int64_t)sizeof(T);
+#pragma unroll
+            for (int k = 0; k < kC; ++k) Unit<T>::put(to + (k * 32 + lane) * sizeof(T), o[k] * inv);
+            if (a.lse != nullptr && lane == 0)
+                a.lse[(int64_t)h * a.n_rows + row] = all.y == 0.f ? -INFINITY : fmaf(all.x, kLn2, logf(all.y));
+        }
+    }
+    if (!a.accumulate && a.w_new == nullptr) return;
+
+    int64_t it = unit_begin(c, tot.items, G);
+    const int64_t it1 = unit_begin(c + 1, tot.items, G);
+    if (it >= it1) return;
+    Place at = place_item;
+    while (it < it1) {
+        const SeqShape s = seq_shape(a, at.b);
+        if (it >= at.item0 + s.items(a.c.Hkv)) {
+            at.unit0 += s.units(a.c.Hkv);
+            at.group0 += (int64_t)a.c.Hkv * s.nrb;
+            at.item0 += s.items(a.c.Hkv);
+            ++at.b;
+            continue;
+        }
+        const int g = (int)((it - at.item0) / s.nt), tile0 = (int)((it - at.item0) % s.nt);
+        const int tile1 = (int)min((int64_t)s.nt, tile0 + (it1 - it));
+        const int64_t row0 = a.cu[at.b];
+        const int R = s.n * a.rep;
+        __syncthreads();
+        for (int r = warp; r < R; r += kThreads / 32) {  // a factor of 0 skips the row
+            const float2 x = merged_ml(a, pieces_of(a, at, s, g, r, tot.units), r, lane);
+            const float cw = a.row_weight != nullptr ? a.row_weight[row0 + r / a.rep] : 1.f;
+            const bool none = cw == 0.f || (x.x == -INFINITY && x.y == 0.f);
+            if (lane == 0) ml[r] = none ? make_float2(0.f, 0.f) : make_float2(x.x == -INFINITY ? 0.f : -x.x, cw / x.y);
+        }
+        __syncthreads();
+        for (int tile = tile0; tile < tile1; ++tile, ++it) {
+            const bool drafts = tile == s.nt - 1;
+            if (drafts ? a.w_new == nullptr : !a.accumulate) continue;
+            const KeyRow kr = key_row(a, s, at.b, g, tile, t, D * (int)sizeof(T));
+            float sum = 0.f;
+            for (int k = 0; k < s.nrb; ++k) {
+                const int r0 = k * a.RB, nr = min(a.RB, R - r0);
+                if (kStore) {
+                    const int64_t u = at.unit0 + ((int64_t)g * s.nrb + k) * s.nt + tile;
+                    const float* z = a.score + u * a.RB * kCacheTile + t;
+                    if (kr.k != nullptr)
+#pragma unroll 8
+                        for (int r = 0; r < nr; ++r) {
+                            const float2 f = ml[r0 + r];
+                            const float x = z[r * kCacheTile];
+                            if (f.y != 0.f && x != -INFINITY) sum = fmaf(ex2(fmaf(x, a.scale_log2, f.x)), f.y, sum);
+                        }
+                } else {
+                    for (int q0 = 0; q0 < nr; q0 += kRows) {
+                        __syncthreads();
+                        load_q<T, D>(a, q, at.b, g, r0 + q0, min(kRows, nr - q0));
+                        __syncthreads();
+                        if (kr.k == nullptr) continue;
+                        float z[kRows];
+                        dots<T, D>(q, kr.k, z);
+#pragma unroll
+                        for (int r = 0; r < kRows; ++r) {
+                            const int rr = r0 + q0 + r;
+                            if (q0 + r >= nr || (drafts && !sees_draft(a, row0, rr / a.rep, t))) continue;
+                            const float2 f = ml[rr];
+                            if (f.y != 0.f) sum = fmaf(ex2(fmaf(z[r], a.scale_log2, f.x)), f.y, sum);
+                        }
+                    }
+                }
+            }
+            if (kr.k == nullptr) continue;
+            if (drafts) a.w_new[(row0 + t) * a.c.Hkv + g] = sum;
+            else a.c.weight[kr.meta] += sum;
+        }
+    }
+}
+
+template <class T, int D>
+estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
+    a.RB = kRows;
+    a.G = ctx->num_sms * 8;
+    const int64_t groups = (int64_t)a.c.Hkv * (a.n_rows * a.rep / a.RB + a.B);
+    const int64_t slots = a.G + groups;
+    // scores of every unit: at most n_slots / 128 + 2 B tiles a KV head, times the row blocks of the
+    // largest sequence
+    const int64_t nrb = ((int64_t)a.max_rows * a.rep + a.RB - 1) / a.RB;
+    const int64_t units = (int64_t)a.c.Hkv * nrb * (a.n_slots / kCacheTile + 2 * (int64_t)a.B);
+    const size_t o_bytes = align_up(sizeof(float) * (size_t)slots * a.RB * D, 256);
+    const size_t ml_bytes = align_up(sizeof(float2) * (size_t)slots * a.RB, 256);
+    const size_t z_bytes = sizeof(float) * (size_t)units * a.RB * kCacheTile;
+    const bool weights = a.accumulate || a.w_new != nullptr;
+    // Kept scores cost 8 bytes a row and key (a write and a read), forming them again a read of K
+    // (D * sizeof(T) bytes a key): kept up to the break-even, and up to 2 GB of them.
+    a.store = weights && (int64_t)a.max_rows * a.rep * 8 <= (int64_t)(D * sizeof(T)) && z_bytes <= (size_t(2) << 30);
+    estp_status s = ws_reserve(ctx, o_bytes + ml_bytes + (a.store ? z_bytes : 0));
+    if (s != ESTP_OK) return s;
+    char* ws = static_cast<char*>(ctx->ws);
+    a.part_o = reinterpret_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float2*>(ws + o_bytes);
+    a.score = reinterpret_cast<float*>(ws + o_bytes + ml_bytes);
+    cache_fwd_kernel<T, D><<<(unsigned)a.G, kThreads, 0, st>>>(a);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, "cache attention launch");
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(ctx->num_sms * 8));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = a.store ? cudaLaunchKernelEx(&cfg, cache_finish_kernel<T, D, true>, a)
+                : cudaLaunchKernelEx(&cfg, cache_finish_kernel<T, D, false>, a);
+    if (e == cudaSuccess) e = cudaGetLastError();
+    return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache attention finish launch");
+}
+
+}  // namespace
+
+estp_status launch_cache_attention(estp_ctx* ctx, CacheAttnArgs& a, estp_dtype dtype, cudaStream_t st) {
+    if (dtype == ESTP_BF16)
+        return a.c.d == 128 ? launch<__nv_bfloat16, 128>(ctx, a, st) : launch<__nv_bfloat16, 64>(ctx, a, st);
+    return a.c.d == 128 ? launch<float, 128>(ctx, a, st) : launch<float, 64>(ctx, a, st);
+}
+
+}  // namespace estp

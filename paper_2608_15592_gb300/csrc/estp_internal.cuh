@@ -16,6 +16,7 @@ struct estp_ctx {
     int device = 0;
     int num_sms = 0;
     int* status = nullptr;      // device status word (estp_status codes)
+    uint32_t* done = nullptr;   // arrival counter of the cache kernels' blocks (zero between launches)
     void* ws = nullptr;         // growable scratch for one call's intermediates
     size_t ws_bytes = 0;
     float* imp_acc = nullptr;   // importance accumulator C_j, fp32 [imp_cap]
