@@ -191,6 +191,10 @@ __device__ __forceinline__ bool sees_draft(const CacheAttnArgs& a, int64_t row0,
     return (a.tree[(row0 + i) * a.words + (j >> 6)] >> (j & 63)) & 1;
 }
 
+// The tensor-core forward of bf16 caches: rows of a block for a call's rows of a (b, KV head), and
+// the launch.
+int cache_tc_rows(int rows);
+estp_status launch_cache_fwd_tc(const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_attention(estp_ctx* ctx, CacheAttnArgs& a, estp_dtype dtype, cudaStream_t st);
 estp_status launch_cache_append(estp_ctx* ctx, const CacheView& c, int row_bytes, int B, const int32_t* length,
                                 const int32_t* seen, int32_t* length_out, int32_t* seen_out, const void* kn,

@@ -374,8 +374,9 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
 
 template <class T, int D>
 estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
-    a.RB = kRows;
-    a.G = ctx->num_sms * 8;
+    constexpr bool kTc = sizeof(T) == 2;
+    a.RB = kTc ? cache_tc_rows(a.max_rows * a.rep) : kRows;
+    a.G = kTc ? ctx->num_sms : ctx->num_sms * 8;
     const int64_t groups = (int64_t)a.c.Hkv * (a.n_rows * a.rep / a.RB + a.B);
     const int64_t slots = a.G + groups;
     // scores of every unit: at most n_slots / 128 + 2 B tiles a KV head, times the row blocks of the
@@ -395,9 +396,15 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(ws + o_bytes);
     a.score = reinterpret_cast<float*>(ws + o_bytes + ml_bytes);
-    cache_fwd_kernel<T, D><<<(unsigned)a.G, kThreads, 0, st>>>(a);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_fail(e, "cache attention launch");
+    cudaError_t e;
+    if constexpr (kTc) {
+        s = launch_cache_fwd_tc(a, st);
+        if (s != ESTP_OK) return s;
+    } else {
+        cache_fwd_kernel<T, D><<<(unsigned)a.G, kThreads, 0, st>>>(a);
+        e = cudaGetLastError();
+        if (e != cudaSuccess) return cuda_fail(e, "cache attention launch");
+    }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;

@@ -1,0 +1,706 @@
+// The forward half of the cache attention (see cache_attn.cu) for bf16 caches, on the tensor cores.
+//
+// Decoding has few rows and many keys, so the keys take the 128 lanes of an MMA and the rows its
+// columns: per tile of 128 keys and block of RB rows
+//   S^T = K Q^T          M = 128 keys, N = RB, K = D
+//   P   = 2^(S^T c - m)  a thread a key; each P is split into two bf16 terms, P = hi + lo, so that
+//                        the second product keeps 16 bits of it
+//   O^T += V^T [hi lo]   M = D, N = 2 RB (hi and lo columns, added at the end), K = 128 keys
+// V^T is the V tile as it is stored (MN-major A), P goes to shared memory with a thread's columns
+// contiguous (MN-major B): nothing is transposed.  A head size of 64 fills M = 128 by reading V
+// twice (a leading offset of 0).
+//
+// The running maximum m of a row only moves when a tile exceeds it by 2^8: a thread forms
+// S c - m, the group votes on whether any is above 8, and only then are the tile's maxima reduced
+// over the lanes and O and l rescaled.  P stays below 2^8, and m is an exact part of the result
+// (every partial is relative to it).
+//
+// One persistent CTA per SM over the units of cache.cuh.
+//   warp 0     TMA producer: K and V tiles in turn through one ring, a box a page (a lane each)
+//   warp 1     MMA issuer; S of the next tile of a segment before O of this one
+//   warps 2..  NB epilogue groups of 4 warps; group nb owns rows nb RB .. of the block: its Q in
+//              shared memory, its S (double-buffered) and O in tensor memory, its P buffer
+// Keys past a sequence's slots hold anything: S^T has them replaced, their P is 0 and their V rows
+// (up to the MMA's 16-key step) are zeroed in shared memory before the product, as 0 x NaN is not 0.
+// A draft whose V is not finite is zeroed there too and added by itself to the rows that see it.
+//
+// Bound by the K and V bytes while RB NB rows cost less than the 64 KB of a tile take to arrive
+// (1.45 us an SM at the copy rate).  Every wait is bounded; on expiry the CTA records
+// ESTP_ERR_TIMEOUT, the group votes to leave, and copies and MMAs are drained before TMEM is freed.
+#include "cache.cuh"
+#include "tcgen05.cuh"
+
+namespace estp {
+namespace {
+
+constexpr int kAtom = kCacheTile * 128;  // 128 keys x 64 bf16
+
+template <int D, int RB, int NB>
+struct Shape {
+    static constexpr int kAtoms = D / 64;
+    static constexpr int kTileBytes = kAtoms * kAtom;
+    static constexpr int kQBytes = kAtoms * RB * 128;
+    static constexpr int kPBytes = RB == 64 ? 2 * kAtom : kAtom;
+    static constexpr int kFixed = NB * (kQBytes + kPBytes);
+    static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 384 - NB * 2 * RB * 4;
+    static constexpr int kStages = kRoom / kTileBytes < 12 ? kRoom / kTileBytes : 12;
+    static constexpr int kThreads = 64 + 128 * NB;
+    static constexpr int kTmem = 4 * RB * NB;  // S: 2 RB a group, O: 2 RB a group
+    // offsets from a 1024-aligned base
+    static constexpr int kPOff = kStages * kTileBytes;
+    static constexpr int kQOff = kPOff + NB * kPBytes;
+    static constexpr int kBarOff = kQOff + NB * kQBytes;
+    static constexpr int kBars = 2 * kStages + 7 * NB + 1;
+    static constexpr int kMiscOff = kBarOff + (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, poison bits
+    static constexpr int kRowOff = kMiscOff + 48;  // a group's [RB] m and [RB] factors
+    static constexpr int kSmem = kRowOff + NB * 2 * RB * 4 + 1024;
+    static_assert(kStages >= 4 && kSmem <= 227 * 1024, "shared memory per CTA");
+    static_assert(kTmem <= 512 && (kTmem & (kTmem - 1)) == 0, "tensor memory");
+};
+
+// tcgen05.ld / .st of 16 or 32 fp32 columns of this thread's lane
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+        "%14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
+    uint32_t r[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(v[k]);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+        "%14, %15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// Orders every later use of v[0..15] after the wait for the load that fills them.
+__device__ __forceinline__ void tie16(float* v) {
+#pragma unroll
+    for (int k = 0; k < 16; k += 8)
+        asm volatile("" : "+f"(v[k]), "+f"(v[k + 1]), "+f"(v[k + 2]), "+f"(v[k + 3]), "+f"(v[k + 4]), "+f"(v[k + 5]),
+                          "+f"(v[k + 6]), "+f"(v[k + 7]));
+}
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+        : "memory");
+}
+
+// MN-major tile, 128-byte swizzle: 64 values of a key a 128-byte row, 8-key groups 1 KB apart, the
+// second 64 values `lead` bytes on.
+__device__ __forceinline__ uint64_t mn_desc(uint32_t addr, uint32_t lead) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+// Barrier of one epilogue group (128 threads) that ors a predicate.
+__device__ __forceinline__ bool group_or(int id, bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.aligned.pred q, %2, 128, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)x), "r"(id)
+        : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ void group_sync(int id) { asm volatile("barrier.cta.sync.aligned %0, 128;" ::"r"(id) : "memory"); }
+
+__device__ __forceinline__ float warp_max(float x) {
+    float y;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t pack_hi_lo(float a, float b, uint32_t& lo) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    const __nv_bfloat162 l = __floats2bfloat162_rn(a - __low2float(h), b - __high2float(h));
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Sums v[0..N) over the warp's lanes; lane k returns with the sum of column k % N (N = 16 or 32).
+template <int N>
+__device__ __forceinline__ float reduce_scatter(float* v, int lane) {
+    if (N == 32) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const bool up = lane & 16;
+            const float send = up ? v[k] : v[k + 16], keep = up ? v[k + 16] : v[k];
+            v[k] = keep + __shfl_xor_sync(0xffffffffu, send, 16);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], 16);
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < o; ++k) {
+            const bool up = lane & o;
+            const float send = up ? v[k] : v[k + o], keep = up ? v[k + o] : v[k];
+            v[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+        }
+    return v[0];
+}
+
+// A segment: consecutive tiles [tile0, tile1) of one (b, g, row block).
+struct Segment {
+    SeqShape s;
+    int b, g, r0, nr, tile0, tile1;
+    int64_t group;
+};
+// Walks the segments of units [u, u1); every role of the CTA walks them by itself.
+struct Walk {
+    Place at;
+    int64_t u, u1;
+    __device__ __forceinline__ bool next(const CacheAttnArgs& a, Segment& o) {
+        while (u < u1) {
+            o.s = seq_shape(a, at.b);
+            const int64_t units = o.s.units(a.c.Hkv);
+            if (u >= at.unit0 + units) {
+                at.unit0 += units;
+                at.group0 += (int64_t)a.c.Hkv * o.s.nrb;
+                ++at.b;
+                continue;
+            }
+            const int64_t loc = u - at.unit0;
+            const int grp = (int)(loc / o.s.nt);
+            o.tile0 = (int)(loc % o.s.nt);
+            o.tile1 = (int)min((int64_t)o.s.nt, o.tile0 + (u1 - u));
+            o.b = at.b;
+            o.g = grp / o.s.nrb;
+            o.r0 = grp % o.s.nrb * a.RB;
+            o.nr = min(a.RB, o.s.n * a.rep - o.r0);
+            o.group = at.group0 + grp;
+            u += o.tile1 - o.tile0;
+            return true;
+        }
+        return false;
+    }
+};
+// Keys of a tile that exist.
+__device__ __forceinline__ int tile_keys(const CacheAttnArgs& a, const SeqShape& s, int tile) {
+    if (tile == s.nt - 1) return a.kn != nullptr ? s.n : 0;
+    return min(kCacheTile, s.len - tile * kCacheTile);
+}
+
+struct TcMaps {
+    CUtensorMap k, v, kn, vn;
+};
+
+template <int D, int RB, int NB>
+__global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
+    cache_fwd_tc_kernel(const __grid_constant__ TcMaps tm, const CacheAttnArgs a, const int box_rows, const int new_rows) {
+    using S = Shape<D, RB, NB>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + S::kBarOff);  // [kStages]
+    uint64_t* empty = full + S::kStages;                            // [kStages]
+    uint64_t* q_full = empty + S::kStages;                          // [NB]
+    uint64_t* s_full = q_full + NB;                                 // [NB][2]
+    uint64_t* s_empty = s_full + 2 * NB;                            // [NB][2]
+    uint64_t* p_full = s_empty + 2 * NB;                            // [NB]
+    uint64_t* pv_done = p_full + NB;                                // [NB]
+    uint64_t* drain = pv_done + NB;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::kMiscOff);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 4);
+    volatile uint32_t* poison = reinterpret_cast<volatile uint32_t*>(sm + S::kMiscOff + 16);  // [2][4] drafts with V not finite
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < NB; ++i) {
+            mbar_init(&q_full[i], 4);
+            mbar_init(&s_full[2 * i], 1);
+            mbar_init(&s_full[2 * i + 1], 1);
+            mbar_init(&s_empty[2 * i], 4);
+            mbar_init(&s_empty[2 * i + 1], 4);
+            mbar_init(&p_full[i], 4);
+            mbar_init(&pv_done[i], 1);
+        }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                     "r"(S::kTmem));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    const int64_t cta = blockIdx.x;
+    // the plan's scratch lies in the ring, which is unused until the barrier below
+    PlanScratch* sc = reinterpret_cast<PlanScratch*>(sm);
+    Place* place = reinterpret_cast<Place*>(sm + 1024);
+    static_assert(sizeof(PlanScratch) <= 1024, "scratch of the plan");
+    const PlanTotals tot = plan_block(a, sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int64_t u = unit_begin(cta, all.units, ctas_of(a, all.units));
+        if (u >= x.unit0 && u < x.unit0 + s.units(a.c.Hkv)) *place = x;
+    });
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int64_t G = ctas_of(a, tot.units);
+    Walk walk{Place{0, 0, 0, 0}, 0, 0};
+    if (tot.ok && cta < G) {
+        walk.at = *place;
+        walk.u = unit_begin(cta, tot.units, G);
+        walk.u1 = unit_begin(cta + 1, tot.units, G);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();  // the ring is the copies' from here
+    Segment sg;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ producer
+        if (lane < 4) {
+            const CUtensorMap* m[4] = {&tm.k, &tm.v, &tm.kn, &tm.vn};
+            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m[lane])) : "memory");
+        }
+        uint32_t e = 0;  // ring entries issued
+        bool ok = true;
+        while (ok && walk.next(a, sg)) {
+            int64_t page = -1;
+            int at = 0;
+            auto look = [&](int tile) {  // this lane's box of a cached tile
+                if (tile >= sg.s.nt - 1) return;
+                const int slot = tile * kCacheTile + lane * box_rows;
+                if (lane * box_rows < kCacheTile && slot < sg.s.len) {
+                    page = a.c.page_of(sg.b, slot, a.status);
+                    if (page < 0) page = a.c.n_pages > 0 ? a.c.n_pages : 1;  // past the pool: reads as zero
+                    at = slot & ((1 << a.c.shift) - 1);
+                }
+            };
+            look(sg.tile0);
+            for (int tile = sg.tile0; ok && tile < sg.tile1; ++tile) {
+                const bool drafts = tile == sg.s.nt - 1;
+                const int keys = tile_keys(a, sg.s, tile);
+                const int rows = drafts ? new_rows : box_rows;
+                const int boxes = drafts ? (keys > 0 ? 1 : 0) : (keys + box_rows - 1) / box_rows;
+                for (int kv = 0; kv < 2; ++kv, ++e) {
+                    const int slot = (int)(e % S::kStages);
+                    const uint32_t use = e / S::kStages;
+                    if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
+                        ok = false;
+                        break;
+                    }
+                    if (lane == 0) mbar_expect_tx(&full[slot], (uint32_t)(boxes * rows * 128 * S::kAtoms));
+                    __syncwarp();
+                    if (lane < boxes) {
+                        uint8_t* to = sm + slot * S::kTileBytes + lane * rows * 128;
+#pragma unroll
+                        for (int x = 0; x < S::kAtoms; ++x) {
+                            if (drafts)
+                                tma_load_3d(to + x * kAtom, kv ? &tm.vn : &tm.kn, x * 64, sg.g, a.cu[sg.b], &full[slot]);
+                            else
+                                tma_load_4d(to + x * kAtom, kv ? &tm.v : &tm.k, x * 64, at, sg.g, (int)page, &full[slot]);
+                        }
+                    }
+                }
+                look(tile + 1);
+            }
+        }
+        if (lane == 0)  // every copy has landed before the CTA can exit
+            for (uint32_t i = 0; i < (uint32_t)S::kStages && i < e; ++i)
+                drain_wait(&full[(e - 1 - i) % S::kStages], ((e - 1 - i) / S::kStages) & 1, a.status);
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------------------------------------------------- MMA issuer
+        if (lane == 0) {
+            constexpr uint32_t kIdS = idesc_bf16(kCacheTile, RB);
+            constexpr uint32_t kIdO = idesc_bf16(kCacheTile, 2 * RB) | (1u << 15) | (1u << 16);
+            uint32_t t = 0;            // tiles begun, over all segments
+            uint32_t steps[NB] = {};   // S issued for a group; O follows in the same order
+            uint32_t q_seen[NB] = {}, pv[NB] = {};
+            bool ok = true, issued = false;
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
+                return ok;
+            };
+            auto issue_s = [&](uint32_t tt, int groups, bool first) {
+                const uint32_t e = 2 * tt;
+                const int slot = (int)(e % S::kStages);
+                if (!wait(&full[slot], (e / S::kStages) & 1)) return;
+                const uint32_t ka = smem_u32(sm + slot * S::kTileBytes);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    if (nb >= groups) break;
+                    if (first && !wait(&q_full[nb], q_seen[nb]++ & 1)) return;
+                    const uint32_t n = steps[nb]++, buf = n & 1, use = n >> 1;
+                    if (use >= 1 && !wait(&s_empty[2 * nb + buf], (use - 1) & 1)) return;
+                    tc_fence_after();
+                    issued = true;
+                    const uint32_t qa = smem_u32(sm + S::kQOff + nb * S::kQBytes);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk)
+                        mma_bf16<kIdS>(tmem + (2 * nb + buf) * RB, sw128_desc(ka + (kk >> 2) * kAtom + (kk & 3) * 32),
+                                       sw128_desc(qa + (kk >> 2) * RB * 128 + (kk & 3) * 32), kk > 0 ? 1u : 0u);
+                    mma_commit(&s_full[2 * nb + buf]);
+                }
+                mma_commit(&empty[slot]);
+            };
+            while (ok && walk.next(a, sg)) {
+                const int groups = (sg.nr + RB - 1) / RB;
+                bool live = false;  // O holds a product of this segment
+                issue_s(t, groups, true);
+                for (int tile = sg.tile0; ok && tile < sg.tile1; ++tile, ++t) {
+                    if (tile + 1 < sg.tile1) issue_s(t + 1, groups, false);
+                    if (!ok) break;
+                    const uint32_t e = 2 * t + 1;
+                    const int slot = (int)(e % S::kStages);
+                    if (!wait(&full[slot], (e / S::kStages) & 1)) break;
+                    const uint32_t va = smem_u32(sm + slot * S::kTileBytes);
+                    const int ksteps = (tile_keys(a, sg.s, tile) + 15) / 16;
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        if (nb >= groups || !wait(&p_full[nb], pv[nb]++ & 1)) break;
+                        tc_fence_after();
+                        issued = true;
+                        const uint32_t pa = smem_u32(sm + S::kPOff + nb * S::kPBytes);
+                        for (int kk = 0; kk < ksteps; ++kk)
+                            mma_bf16<kIdO>(tmem + (uint32_t)(2 * RB * (NB + nb)), mn_desc(va + kk * 2048, D == 128 ? kAtom : 0),
+                                           mn_desc(pa + kk * 2048, kAtom), live || kk > 0 ? 1u : 0u);
+                        mma_commit(&pv_done[nb]);
+                    }
+                    if (!ok) break;
+                    live = live || ksteps > 0;
+                    mma_commit(&empty[slot]);
+                }
+            }
+            if (issued) {
+                mma_commit(drain);
+                drain_wait(drain, 0, a.status);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------- epilogue
+        const int nb = (warp - 2) >> 2, q = warp & 3, bar = 1 + nb;
+        const int j = q * 32 + lane;                 // key of the tile; lane of S and O
+        float* row_m = reinterpret_cast<float*>(sm + S::kRowOff) + nb * 2 * RB;  // m, log2 units
+        float* row_f = row_m + RB;
+        uint8_t* pb = sm + S::kPOff + nb * S::kPBytes;
+        uint8_t* qb = sm + S::kQOff + nb * S::kQBytes;
+        const uint32_t lane_off = (uint32_t)(q * 32) << 16;
+        const uint32_t t_o = tmem + lane_off + (uint32_t)(2 * RB * (NB + nb));
+        uint32_t step = 0, t = 0, seg = 0;
+        bool alive = true;
+        auto wait = [&](uint64_t* b, uint32_t parity) {
+            if (alive) alive = warp_wait(b, parity, abort_flag, a.status, a.wait_cycles);
+        };
+        while (walk.next(a, sg)) {
+            const int base = nb * RB, nr = min(RB, sg.nr - base);  // rows of this group
+            // the poison bits of this segment: group 0 may be one segment ahead of the other
+            volatile uint32_t* odd_drafts = poison + (seg++ & 1) * 4;
+            if (nr <= 0) {                                // none: the other group works alone
+                t += sg.tile1 - sg.tile0;
+                continue;
+            }
+            const int64_t row0 = a.cu[sg.b];
+            // Q of this group's rows (rows past nr are zero), K-major with the 128-byte swizzle
+            for (int x = j; x < RB * (D / 8); x += 128) {
+                const int r = x / (D / 8), ch = x % (D / 8);
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (r < nr) {
+                    const int rr = sg.r0 + base + r, i = rr / a.rep, h = sg.g * a.rep + rr % a.rep;
+                    v = *reinterpret_cast<const uint4*>(a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16);
+                }
+                *reinterpret_cast<uint4*>(qb + (ch >> 3) * RB * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_full[nb]);
+            if (j < RB) row_m[j] = -INFINITY;
+            float l[RB];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) l[r] = 0.f;
+            bool live = false;
+            for (int tile = sg.tile0; tile < sg.tile1; ++tile, ++step, ++t) {
+                const bool drafts = tile == sg.s.nt - 1;
+                const int keys = tile_keys(a, sg.s, tile);
+                const uint32_t buf = step & 1;
+                wait(&s_full[2 * nb + buf], (step >> 1) & 1);
+                tc_fence_after();
+                float z[RB];
+#pragma unroll
+                for (int r = 0; r < RB; r += 16) tmem_ld16(tmem + lane_off + (2 * nb + buf) * RB + r, z + r);
+                tmem_wait_ld();
+#pragma unroll
+                for (int r = 0; r < RB; r += 16) tie16(z + r);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_empty[2 * nb + buf]);
+                if (keys < kCacheTile) {
+                    if (!drafts) {
+                        if (j >= keys) {
+#pragma unroll
+                            for (int r = 0; r < RB; ++r) z[r] = -INFINITY;
+                        }
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < RB; ++r)
+                            if (j >= keys || r >= nr || !sees_draft(a, row0, (sg.r0 + base + r) / a.rep, j)) z[r] = -INFINITY;
+                    }
+                } else if (drafts) {
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+                        if (r >= nr || !sees_draft(a, row0, (sg.r0 + base + r) / a.rep, j)) z[r] = -INFINITY;
+                }
+                if (a.store && alive) {
+                    float* to = a.score + ((walk.u - (sg.tile1 - tile)) * a.RB + base) * kCacheTile + j;
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+                        if (r < nr) to[r * kCacheTile] = z[r];
+                }
+                // does any score exceed its row's m by 2^8?
+                bool up = tile == sg.tile0 || !alive;
+                if (!up) {
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int r = 0; r < RB; r += 2)
+                        top = fmax3(top, fmaf(z[r], a.scale_log2, -row_m[r]), fmaf(z[r + 1], a.scale_log2, -row_m[r + 1]));
+                    up = top > 8.f;
+                }
+                if (group_or(bar, up)) {
+                    if (step > 0) wait(&pv_done[nb], (step - 1) & 1);
+                    tc_fence_after();
+                    if (group_or(bar, !alive)) {
+                        alive = false;
+                        break;
+                    }
+                    float* row_w = reinterpret_cast<float*>(pb);  // [4][RB]: the P buffer is free
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        const float x = warp_max(z[r]);
+                        if (lane == (r & 31)) row_w[q * RB + r] = x;
+                    }
+                    group_sync(bar);
+                    if (j < RB) {
+                        const float x = fmaxf(fmaxf(row_w[j], row_w[RB + j]), fmaxf(row_w[2 * RB + j], row_w[3 * RB + j]));
+                        const float old = row_m[j], m = fmaxf(old, x * a.scale_log2);
+                        row_f[j] = old == m ? 1.f : ex2(old - m);
+                        row_m[j] = m;
+                    }
+                    group_sync(bar);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) l[r] *= row_f[r];
+                    if (live) {
+#pragma unroll 1
+                        for (int c = 0; c < 2 * RB; c += 16) {
+                            float o[16];
+                            tmem_ld16(t_o + c, o);
+                            tmem_wait_ld();
+                            tie16(o);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) o[k] *= row_f[(c + k) % RB];
+                            tmem_st16(t_o + c, o);
+                        }
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    }
+                }
+                // P in place of the scores
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const float m = row_m[r];
+                    const float e = ex2(fmaf(z[r], a.scale_log2, m == -INFINITY ? 0.f : -m));
+                    z[r] = z[r] == -INFINITY ? 0.f : e;
+                    l[r] += z[r];
+                }
+                if (step > 0) wait(&pv_done[nb], (step - 1) & 1);  // the P buffer is free
+                uint8_t* prow = pb + j * 128;
+#pragma unroll
+                for (int r = 0; r < RB; r += 8) {
+                    uint4 h, lo;
+                    h.x = pack_hi_lo(z[r], z[r + 1], lo.x);
+                    h.y = pack_hi_lo(z[r + 2], z[r + 3], lo.y);
+                    h.z = pack_hi_lo(z[r + 4], z[r + 5], lo.z);
+                    h.w = pack_hi_lo(z[r + 6], z[r + 7], lo.w);
+                    const int ch = r / 8;
+                    *reinterpret_cast<uint4*>(prow + ((ch ^ (j & 7)) << 4)) = h;
+                    if (RB == 64) *reinterpret_cast<uint4*>(prow + kAtom + ((ch ^ (j & 7)) << 4)) = lo;
+                    else *reinterpret_cast<uint4*>(prow + (((ch + RB / 8) ^ (j & 7)) << 4)) = lo;
+                }
+                if (nb == 0 && (drafts || (keys & 15))) {
+                    // V rows that must not reach the product: past the keys, and drafts that are not finite
+                    const uint32_t e = 2 * t + 1;
+                    const int slot = (int)(e % S::kStages);
+                    wait(&full[slot], (e / S::kStages) & 1);
+                    uint8_t* vr = sm + slot * S::kTileBytes + j * 128;
+                    bool clear = j >= keys && j < ((keys + 15) & ~15);
+                    if (drafts && j < keys) {
+                        bool odd = false;
+#pragma unroll
+                        for (int x = 0; x < S::kAtoms * 8; ++x) {
+                            const uint4 v = *reinterpret_cast<const uint4*>(vr + (x >> 3) * kAtom + (x & 7) * 16);
+                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                odd |= (w[k] & 0x7F80u) == 0x7F80u || (w[k] & 0x7F800000u) == 0x7F800000u;
+                        }
+                        clear = odd;
+                    }
+                    if (drafts) {
+                        const unsigned bits = __ballot_sync(0xffffffffu, clear && j < keys);
+                        if (lane == 0) odd_drafts[q] = bits;
+                    }
+                    if (clear) {
+#pragma unroll
+                        for (int x = 0; x < S::kAtoms * 8; ++x)
+                            *reinterpret_cast<uint4*>(vr + (x >> 3) * kAtom + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+                tc_fence_before();
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[nb]);
+                live = live || keys > 0;
+            }
+            if (!alive) {  // leave with the group
+                group_or(bar, true);
+                break;
+            }
+            // the segment's partial
+            wait(&pv_done[nb], (step - 1) & 1);
+            tc_fence_after();
+            float* row_w = reinterpret_cast<float*>(qb);  // [4][RB]: every S of the segment is done with Q
+            {
+                constexpr int kN = RB < 32 ? RB : 32;
+#pragma unroll
+                for (int r = 0; r < RB; r += kN) {
+                    const float x = reduce_scatter<kN>(l + r, lane);
+                    if (lane < kN) row_w[q * RB + r + lane] = x;
+                }
+            }
+            if (group_or(bar, !alive)) break;
+            const int64_t part = (cta + sg.group) * a.RB + base;
+            if (j < nr)
+                a.part_ml[part + j] = make_float2(row_m[j], (row_w[j] + row_w[RB + j]) + (row_w[2 * RB + j] + row_w[3 * RB + j]));
+#pragma unroll 1
+            for (int r = 0; r < RB; r += 16) {
+                if (r >= nr) break;
+                float hi[16], lo[16];
+                tmem_ld16(t_o + r, hi);
+                tmem_ld16(t_o + RB + r, lo);
+                tmem_wait_ld();
+                tie16(hi);
+                tie16(lo);
+                if (D == 128 || q < 2) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        if (r + k >= nr) break;
+                        a.part_o[(part + r + k) * D + j] = live ? hi[k] + lo[k] : 0.f;
+                    }
+                }
+            }
+            tc_fence_before();
+            if (sg.tile1 == sg.s.nt && (odd_drafts[0] | odd_drafts[1] | odd_drafts[2] | odd_drafts[3])) {
+                // drafts whose V is not finite: P is still in its buffer
+                if (D == 128 || q < 2) {
+                    for (int x = 0; x < sg.s.n; ++x) {
+                        if (!(odd_drafts[x >> 5] >> (x & 31) & 1)) continue;
+                        const float v = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(
+                            a.vn + (row0 + x) * a.ldn + (int64_t)sg.g * (D * 2) + j * 2));
+                        for (int r = 0; r < nr; ++r) {
+                            if (!sees_draft(a, row0, (sg.r0 + base + r) / a.rep, x)) continue;
+                            const __nv_bfloat16* ph = reinterpret_cast<const __nv_bfloat16*>(pb + x * 128 + (((r >> 3) ^ (x & 7)) << 4)) + (r & 7);
+                            const __nv_bfloat16* pl = reinterpret_cast<const __nv_bfloat16*>(
+                                RB == 64 ? pb + kAtom + x * 128 + (((r >> 3) ^ (x & 7)) << 4)
+                                         : pb + x * 128 + ((((r + RB) >> 3) ^ (x & 7)) << 4)) + (r & 7);
+                            a.part_o[(part + r) * D + j] += (__bfloat162float(*ph) + __bfloat162float(*pl)) * v;
+                        }
+                    }
+                }
+            }
+            group_sync(bar);  // row_w (in Q), row_m and P are free for the next segment
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) {
+        __syncwarp();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmem));
+    }
+}
+
+// Pages as (d, slot, KV head, page); a box is 64 values of box_rows slots of one head.
+estp_status pages_map(CUtensorMap* m, const CacheView& c, const void* base, const void* other, int box_rows) {
+    auto fn = tensor_map_encoder();
+    if (!fn) return fail(ESTP_ERR_CUDA, "cuTensorMapEncodeTiled unavailable");
+    const bool none = c.n_pages == 0;  // no page can be read: a map of the right form over another array
+    cuuint64_t dims[4] = {(cuuint64_t)c.d, (cuuint64_t)1 << c.shift, (cuuint64_t)c.Hkv, none ? 1 : (cuuint64_t)c.n_pages};
+    cuuint64_t strides[3] = {(cuuint64_t)c.slot_stride, (cuuint64_t)c.head_stride, (cuuint64_t)c.page_stride};
+    cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, es[4] = {1, 1, 1, 1};
+    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(none ? other : base), dims, strides, box,
+                          es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? ESTP_OK : fail(ESTP_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
+// New rows as (d, KV head, row); a box is 64 values of box_rows rows of one head.
+estp_status rows_map(CUtensorMap* m, const CacheAttnArgs& a, const void* base, int box_rows) {
+    auto fn = tensor_map_encoder();
+    if (!fn) return fail(ESTP_ERR_CUDA, "cuTensorMapEncodeTiled unavailable");
+    const bool none = base == nullptr;  // never read
+    cuuint64_t dims[3] = {(cuuint64_t)a.c.d, (cuuint64_t)(none ? 1 : a.c.Hkv), (cuuint64_t)a.n_rows};
+    cuuint64_t strides[2] = {(cuuint64_t)a.c.d * 2, (cuuint64_t)(none ? a.ldq : a.ldn)};
+    cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows}, es[3] = {1, 1, 1};
+    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(none ? (const void*)a.Q : base), dims,
+                          strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? ESTP_OK : fail(ESTP_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
+template <int D, int RB, int NB>
+estp_status launch(const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int new_rows, cudaStream_t st) {
+    using S = Shape<D, RB, NB>;
+    cudaError_t e = cudaFuncSetAttribute(cache_fwd_tc_kernel<D, RB, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e != cudaSuccess) return cuda_fail(e, "cache attention smem attribute");
+    cache_fwd_tc_kernel<D, RB, NB><<<(unsigned)a.G, S::kThreads, S::kSmem, st>>>(tm, a, box_rows, new_rows);
+    e = cudaGetLastError();
+    return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache attention launch");
+}
+
+}  // namespace
+
+int cache_tc_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+
+estp_status launch_cache_fwd_tc(const CacheAttnArgs& a, cudaStream_t st) {
+    TcMaps tm;
+    const int page = 1 << a.c.shift, box_rows = page < kCacheTile ? page : kCacheTile;
+    const int new_rows = (a.max_rows + 7) / 8 * 8;
+    estp_status s = pages_map(&tm.k, a.c, a.c.k, a.Q, box_rows);
+    if (s == ESTP_OK) s = pages_map(&tm.v, a.c, a.c.v, a.Q, box_rows);
+    if (s == ESTP_OK) s = rows_map(&tm.kn, a, a.kn, new_rows);
+    if (s == ESTP_OK) s = rows_map(&tm.vn, a, a.vn, new_rows);
+    if (s != ESTP_OK) return s;
+    if (a.c.d == 128) {
+        if (a.RB == 16) return launch<128, 16, 1>(tm, a, box_rows, new_rows, st);
+        if (a.RB == 32) return launch<128, 32, 1>(tm, a, box_rows, new_rows, st);
+        if (a.RB == 64) return launch<128, 64, 1>(tm, a, box_rows, new_rows, st);
+        return launch<128, 64, 2>(tm, a, box_rows, new_rows, st);
+    }
+    if (a.RB == 16) return launch<64, 16, 1>(tm, a, box_rows, new_rows, st);
+    if (a.RB == 32) return launch<64, 32, 1>(tm, a, box_rows, new_rows, st);
+    if (a.RB == 64) return launch<64, 64, 1>(tm, a, box_rows, new_rows, st);
+    return launch<64, 64, 2>(tm, a, box_rows, new_rows, st);
+}
+
+}  // namespace estp

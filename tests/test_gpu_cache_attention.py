@@ -381,3 +381,22 @@ def test_checked_build_agrees(cuda_lib):
         ctx.close()
     for a, b in zip(res[:2], res[2:]):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("n", [1, 60])
+def test_wait_runs_out_then_context_recovers(cuda_lib, n):
+    """A bounded wait of the tensor-core kernels that runs out is recorded, and the next call is right."""
+    rng = np.random.default_rng(n)
+    ctx = cuda_lib.Context(0)
+    cache = R.make_cache(cuda_lib, rng, [700, 90], 2, 128, 16, BF)
+    Q, kn, vn = _rows(rng, 2 * n, 8, 128, BF), _rows(rng, 2 * n, 2, 128, BF), _rows(rng, 2 * n, 2, 128, BF)
+    cu = torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda")
+    ctx.set_wait_limit(2)
+    ctx.cache_attention(cache, Q, kn, vn, cu, n)
+    with pytest.raises(cuda_lib.EstpError) as e:
+        ctx.sync_status()
+    assert e.value.status == cuda_lib.ESTP_ERR_TIMEOUT
+    ctx.set_wait_limit(0)
+    ctx.sync_status()
+    _check(cuda_lib, ctx, cache, Q, kn, vn, [n, n], [R.tree(rng, n), R.tree(rng, n)])
+    ctx.close()
