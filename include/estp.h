@@ -359,7 +359,8 @@ estp_status estp_misalignment(estp_ctx* ctx, const float* entropy, const float* 
  *   k, v       : [n_pages, page_size, Hkv, head_dim] in any order of the strides (elements, the
  *                same for both; head_dim contiguous; 16-byte aligned, multiples of 16 bytes).
  *                Unused slots may hold anything.
- *   weight     : fp32 [n_pages, Hkv, page_size], or NULL (attention without accumulation only)
+ *   weight     : fp32 [n_pages, Hkv, page_size], 16-byte aligned, or NULL (attention without
+ *                accumulation only)
  *   position   : int32 [n_pages, Hkv, page_size], or NULL (not needed by the attention)
  *   page_table : int32 [B, max_pages]; entries past a sequence's slots are not read.  Sequences
  *                may share pages for reading; calls that write (append, evict, accumulate)

@@ -63,10 +63,12 @@ struct CacheAttnArgs {
     const float* row_weight;
     float scale, scale_log2;
     int RB, G;
+    int KS;                      // partials of a segment
     int store;                   // scores are kept for the weights
-    float* part_o;               // [G + groups][RB][d]
-    float2* part_ml;             // [G + groups][RB]: running max (log2 units) and sum
+    float* part_o;               // [G + groups][KS][RB][d]
+    float2* part_ml;             // [G + groups][KS][RB]: running max (log2 units) and sum
     float* score;                // [units][RB][128], unscaled
+    float2* factor;              // [n_rows, Hq]: (-M, c / L), where scores are formed again
     char* out;
     float* lse;
     float* w_new;
@@ -191,10 +193,11 @@ __device__ __forceinline__ bool sees_draft(const CacheAttnArgs& a, int64_t row0,
     return (a.tree[(row0 + i) * a.words + (j >> 6)] >> (j & 63)) & 1;
 }
 
-// The tensor-core forward of bf16 caches: rows of a block for a call's rows of a (b, KV head), and
-// the launch.
-int cache_tc_rows(int rows);
+// The tensor-core forward of bf16 caches: rows of a block and partials of a segment for a call's
+// rows of a (b, KV head), and the launch.
+void cache_tc_shape(int rows, int* RB, int* KS);
 estp_status launch_cache_fwd_tc(const CacheAttnArgs& a, cudaStream_t st);
+estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_attention(estp_ctx* ctx, CacheAttnArgs& a, estp_dtype dtype, cudaStream_t st);
 estp_status launch_cache_append(estp_ctx* ctx, const CacheView& c, int row_bytes, int B, const int32_t* length,
                                 const int32_t* seen, int32_t* length_out, int32_t* seen_out, const void* kn,

@@ -2,15 +2,16 @@
 // slot receives:
 //   s_ij = scale q_i . k_j,  lse_i = ln sum_j e^s_ij,  o_i = sum_j e^(s_ij - lse_i) v_j,
 //   weight_j += sum_i c_i e^(s_ij - lse_i)
-// over the cached slots and the drafts that row i sees.  Two launches:
+// over the cached slots and the drafts that row i sees:
 //
 // cache_fwd_kernel: a persistent grid over the units of cache.cuh.  Of every group segment it
 // leaves the running maximum m (log2 units), the sum l = sum 2^(s' - m) and O = sum 2^(s' - m) v,
 // s' = s log2(e), and, where the weights are wanted and fit, every unscaled score q.k.
 //
 // cache_finish_kernel: merges the partials of each row in CTA order, writes o and lse, and adds to
-// every slot the weight of its rows, sum_r c_r 2^(s' - M_r) / L_r, from the kept scores or from
-// scores formed again.  No floating-point atomics: every sum has one order.
+// every slot the weight of its rows, sum_r c_r 2^(s' - M_r) / L_r, from the kept scores.  With many
+// rows to a key, keeping scores costs more than forming them again: cache_weight_kernel does, a
+// third launch.  No floating-point atomics: every sum has one order.
 //
 // A row that sees nothing (M = -inf, L = 0) gives o = 0 and lse = -inf and no weight.
 #include "cache.cuh"
@@ -20,6 +21,7 @@ namespace {
 
 constexpr int kThreads = 128;  // one key of a tile each
 constexpr int kRows = 8;       // rows of a block of the CUDA-core kernels
+constexpr int kCacheMaxStored = 64;  // rows of a (b, KV head) whose scores are kept at most
 
 template <class T> struct Unit;  // 16 bytes of a row
 template <> struct Unit<float> {
@@ -219,22 +221,24 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
     }
 }
 
-// Pieces of row r of (b, g): CTAs c0..c1 hold the group, at slot c + group.
+// Pieces of row r of (b, g): CTAs c0..c1 hold the group, each with KS partials at slot c + group.
 struct Pieces {
-    int64_t c0, c1, group;
+    int64_t first;  // part_ml element of the first
+    int n;          // the others RB apart
 };
 __device__ __forceinline__ Pieces pieces_of(const CacheAttnArgs& a, const Place& at, const SeqShape& s, int g, int r,
                                             int64_t units) {
     const int64_t grp = (int64_t)g * s.nrb + r / a.RB, ub = at.unit0 + grp * s.nt;
     const int64_t G = ctas_of(a, units);
-    return Pieces{cta_of(ub, units, G), cta_of(ub + s.nt - 1, units, G), at.group0 + grp};
+    const int64_t c0 = cta_of(ub, units, G), c1 = cta_of(ub + s.nt - 1, units, G);
+    return Pieces{(c0 + at.group0 + grp) * a.KS * a.RB + r % a.RB, (int)(c1 - c0 + 1) * a.KS};
 }
 
 // Warp-wide: the row's maximum and sum over its pieces.
-__device__ __forceinline__ float2 merged_ml(const CacheAttnArgs& a, const Pieces& w, int r, int lane) {
+__device__ __forceinline__ float2 merged_ml(const CacheAttnArgs& a, const Pieces& w, int lane) {
     float M = -INFINITY, L = 0.f;
-    for (int64_t c = w.c0 + lane; c <= w.c1; c += 32) {
-        const float2 x = a.part_ml[(c + w.group) * a.RB + r % a.RB];
+    for (int c = lane; c < w.n; c += 32) {
+        const float2 x = a.part_ml[w.first + (int64_t)c * a.RB];
         const float mn = fmaxf(M, x.x);
         if (mn != -INFINITY) L = fmaf(L, ex2(M - mn), x.y * ex2(x.x - mn));
         else L += x.y;  // NaN stays
@@ -251,13 +255,50 @@ __device__ __forceinline__ float2 merged_ml(const CacheAttnArgs& a, const Pieces
     return make_float2(M, L);
 }
 
-// rows x heads and (KV head, tile) items, both cut evenly over the grid.
-template <class T, int D, bool kStore>
+// Walks a CTA's share [it, it1) of the call's items (b, KV head, tile) in runs of one (b, KV head).
+template <class Run>
+__device__ __forceinline__ void for_items(const CacheAttnArgs& a, Place at, int64_t it, int64_t it1, Run run) {
+    while (it < it1) {
+        const SeqShape s = seq_shape(a, at.b);
+        if (it >= at.item0 + s.items(a.c.Hkv)) {
+            at.unit0 += s.units(a.c.Hkv);
+            at.group0 += (int64_t)a.c.Hkv * s.nrb;
+            at.item0 += s.items(a.c.Hkv);
+            ++at.b;
+            continue;
+        }
+        const int g = (int)((it - at.item0) / s.nt), tile0 = (int)((it - at.item0) % s.nt);
+        const int tile1 = (int)min((int64_t)s.nt, tile0 + (it1 - it));
+        run(at, s, g, tile0, tile1);
+        it += tile1 - tile0;
+    }
+}
+
+// Adds the weight of 4 keys to slots that share a page, or writes it for 4 drafts; n of them exist.
+__device__ __forceinline__ void add4(float* p, float4 s, int n) {
+    if (n >= 4) {
+        float4 w = *reinterpret_cast<const float4*>(p);
+        w.x += s.x;
+        w.y += s.y;
+        w.z += s.z;
+        w.w += s.w;
+        *reinterpret_cast<float4*>(p) = w;
+    } else {
+        p[0] += s.x;
+        if (n > 1) p[1] += s.y;
+        if (n > 2) p[2] += s.z;
+    }
+}
+
+// Merges the partials: o and lse, a warp a (row, head), both cut evenly over the grid.  With kept
+// scores it adds the weights too, a warp a tile, a lane 4 keys: the items are cut evenly as well.
+// Without, it leaves (-M, c / L) of every row for the kernel that forms the scores again.
+template <class T, int D>
 __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnArgs a) {
     __shared__ PlanScratch sc;
     __shared__ Place place_row, place_item;
-    __shared__ float2 ml[kCacheMaxGroupRows];  // (-M, c / L) of every row of (b, g)
-    __shared__ float q[kStore ? 1 : kRows][D];
+    __shared__ float2 ml[kCacheMaxStored];  // (-M, c / L) of every row of (b, g)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const int64_t c = blockIdx.x, G = gridDim.x;
     const int64_t x0 = unit_begin(c, a.n_rows * a.Hq, G), x1 = unit_begin(c + 1, a.n_rows * a.Hq, G);
@@ -269,7 +310,13 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the partials are complete
     if (!tot.ok) return;
 
-    if (x0 < x1) {  // o and lse: a warp a (row, head)
+    // (-M, c / L): a row without keys, or of factor 0, has a factor of 0 and is left out
+    auto factor = [&](float2 x, int64_t row) {
+        const float cw = a.row_weight != nullptr ? a.row_weight[row] : 1.f;
+        const bool none = cw == 0.f || (x.x == -INFINITY && x.y == 0.f);
+        return none ? make_float2(0.f, 0.f) : make_float2(x.x == -INFINITY ? 0.f : -x.x, cw / x.y);
+    };
+    if (x0 < x1) {
         Place at = place_row;
         SeqShape s = seq_shape(a, at.b);
         for (int64_t x = x0 + warp; x < x1; x += kThreads / 32) {
@@ -282,14 +329,14 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
             const int64_t row = x / a.Hq;
             const int h = (int)(x % a.Hq), i = (int)(row - a.cu[at.b]), r = i * a.rep + h % a.rep;
             const Pieces w = pieces_of(a, at, s, h / a.rep, r, tot.units);
-            const float2 all = merged_ml(a, w, r, lane);
+            const float2 all = merged_ml(a, w, lane);
             constexpr int kC = D / 32;
             float o[kC];
 #pragma unroll
             for (int k = 0; k < kC; ++k) o[k] = 0.f;
 #pragma unroll 4
-            for (int64_t pc = w.c0; pc <= w.c1; ++pc) {
-                const int64_t e = (pc + w.group) * a.RB + r % a.RB;
+            for (int p = 0; p < w.n; ++p) {
+                const int64_t e = w.first + (int64_t)p * a.RB;
                 const float m = a.part_ml[e].x;
                 const float f = m == all.x ? 1.f : ex2(m - all.x);
 #pragma unroll
@@ -299,83 +346,140 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
             char* to = a.out + (row * a.Hq + h) * D * (int64_t)sizeof(T);
 #pragma unroll
             for (int k = 0; k < kC; ++k) Unit<T>::put(to + (k * 32 + lane) * sizeof(T), o[k] * inv);
-            if (a.lse != nullptr && lane == 0)
-                a.lse[(int64_t)h * a.n_rows + row] = all.y == 0.f ? -INFINITY : fmaf(all.x, kLn2, logf(all.y));
+            if (lane == 0) {
+                if (a.lse != nullptr)
+                    a.lse[(int64_t)h * a.n_rows + row] = all.y == 0.f ? -INFINITY : fmaf(all.x, kLn2, logf(all.y));
+                if (a.factor != nullptr) a.factor[row * a.Hq + h] = factor(all, row);
+            }
         }
     }
-    if (!a.accumulate && a.w_new == nullptr) return;
+    if (!a.store) return;
 
-    int64_t it = unit_begin(c, tot.items, G);
-    const int64_t it1 = unit_begin(c + 1, tot.items, G);
-    if (it >= it1) return;
-    Place at = place_item;
-    while (it < it1) {
-        const SeqShape s = seq_shape(a, at.b);
-        if (it >= at.item0 + s.items(a.c.Hkv)) {
-            at.unit0 += s.units(a.c.Hkv);
-            at.group0 += (int64_t)a.c.Hkv * s.nrb;
-            at.item0 += s.items(a.c.Hkv);
-            ++at.b;
-            continue;
-        }
-        const int g = (int)((it - at.item0) / s.nt), tile0 = (int)((it - at.item0) % s.nt);
-        const int tile1 = (int)min((int64_t)s.nt, tile0 + (it1 - it));
+    for_items(a, place_item, unit_begin(c, tot.items, G), unit_begin(c + 1, tot.items, G),
+              [&](const Place& at, const SeqShape& s, int g, int tile0, int tile1) {
         const int64_t row0 = a.cu[at.b];
         const int R = s.n * a.rep;
         __syncthreads();
-        for (int r = warp; r < R; r += kThreads / 32) {  // a factor of 0 skips the row
-            const float2 x = merged_ml(a, pieces_of(a, at, s, g, r, tot.units), r, lane);
-            const float cw = a.row_weight != nullptr ? a.row_weight[row0 + r / a.rep] : 1.f;
-            const bool none = cw == 0.f || (x.x == -INFINITY && x.y == 0.f);
-            if (lane == 0) ml[r] = none ? make_float2(0.f, 0.f) : make_float2(x.x == -INFINITY ? 0.f : -x.x, cw / x.y);
+        for (int r = warp; r < R; r += kThreads / 32) {
+            const float2 x = merged_ml(a, pieces_of(a, at, s, g, r, tot.units), lane);
+            if (lane == 0) ml[r] = factor(x, row0 + r / a.rep);
         }
         __syncthreads();
-        for (int tile = tile0; tile < tile1; ++tile, ++it) {
+        for (int tile = tile0 + warp; tile < tile1; tile += kThreads / 32) {
+            const bool drafts = tile == s.nt - 1;
+            if (drafts ? a.w_new == nullptr : !a.accumulate) continue;
+            const int n = (drafts ? (a.kn != nullptr ? s.n : 0) : s.len - tile * kCacheTile) - lane * 4;
+            if (n <= 0) continue;
+            float* to = nullptr;
+            if (!drafts) {
+                const int slot = tile * kCacheTile + lane * 4;  // 4 slots of one page
+                const int64_t page = a.c.page_of(at.b, slot, a.status);
+                if (page < 0) continue;
+                to = a.c.weight + a.c.meta(page, slot, g);
+            }
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < s.nrb; ++k) {
+                const int r0 = k * a.RB, nr = min(a.RB, R - r0);
+                const int64_t u = at.unit0 + ((int64_t)g * s.nrb + k) * s.nt + tile;
+                const float4* z = reinterpret_cast<const float4*>(a.score + u * a.RB * kCacheTile) + lane;
+                auto one = [&](float x, float2 f, float& s1) {
+                    if (x != -INFINITY) s1 = fmaf(ex2(fmaf(x, a.scale_log2, f.x)), f.y, s1);
+                };
+#pragma unroll 8
+                for (int r = 0; r < nr; ++r) {
+                    const float2 f = ml[r0 + r];
+                    const float4 x = z[r * (kCacheTile / 4)];
+                    if (f.y != 0.f) {
+                        one(x.x, f, sum.x);
+                        one(x.y, f, sum.y);
+                        one(x.z, f, sum.z);
+                        one(x.w, f, sum.w);
+                    }
+                }
+            }
+            if (!drafts) {
+                add4(to, sum, n);
+            } else {
+                float* w = a.w_new + (row0 + lane * 4) * a.c.Hkv + g;
+                w[0] = sum.x;
+                if (n > 1) w[a.c.Hkv] = sum.y;
+                if (n > 2) w[2 * a.c.Hkv] = sum.z;
+                if (n > 3) w[3 * a.c.Hkv] = sum.w;
+            }
+        }
+    });
+}
+
+// The weights with the scores formed again, fp32: a thread a key, the rows in blocks of kRows.
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnArgs a) {
+    __shared__ PlanScratch sc;
+    __shared__ Place place;
+    __shared__ float q[kRows][D];
+    __shared__ float2 ml[kRows];
+    const int t = threadIdx.x;
+    const int64_t c = blockIdx.x, G = gridDim.x;
+    const PlanTotals tot = plan_block(a, &sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int64_t it = unit_begin(c, all.items, G);
+        if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) place = x;
+    });
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the factors are complete
+    if (!tot.ok) return;
+    for_items(a, place, unit_begin(c, tot.items, G), unit_begin(c + 1, tot.items, G),
+              [&](const Place& at, const SeqShape& s, int g, int tile0, int tile1) {
+        const int64_t row0 = a.cu[at.b];
+        const int R = s.n * a.rep;
+        for (int tile = tile0; tile < tile1; ++tile) {
             const bool drafts = tile == s.nt - 1;
             if (drafts ? a.w_new == nullptr : !a.accumulate) continue;
             const KeyRow kr = key_row(a, s, at.b, g, tile, t, D * (int)sizeof(T));
             float sum = 0.f;
-            for (int k = 0; k < s.nrb; ++k) {
-                const int r0 = k * a.RB, nr = min(a.RB, R - r0);
-                if (kStore) {
-                    const int64_t u = at.unit0 + ((int64_t)g * s.nrb + k) * s.nt + tile;
-                    const float* z = a.score + u * a.RB * kCacheTile + t;
-                    if (kr.k != nullptr)
-#pragma unroll 8
-                        for (int r = 0; r < nr; ++r) {
-                            const float2 f = ml[r0 + r];
-                            const float x = z[r * kCacheTile];
-                            if (f.y != 0.f && x != -INFINITY) sum = fmaf(ex2(fmaf(x, a.scale_log2, f.x)), f.y, sum);
-                        }
-                } else {
-                    for (int q0 = 0; q0 < nr; q0 += kRows) {
-                        __syncthreads();
-                        load_q<T, D>(a, q, at.b, g, r0 + q0, min(kRows, nr - q0));
-                        __syncthreads();
-                        if (kr.k == nullptr) continue;
-                        float z[kRows];
-                        dots<T, D>(q, kr.k, z);
+            for (int r0 = 0; r0 < R; r0 += kRows) {
+                const int nr = min(kRows, R - r0);
+                __syncthreads();
+                load_q<T, D>(a, q, at.b, g, r0, nr);
+                if (t < nr) ml[t] = a.factor[(row0 + (r0 + t) / a.rep) * a.Hq + g * a.rep + (r0 + t) % a.rep];
+                __syncthreads();
+                if (kr.k == nullptr) continue;
+                float z[kRows];
+                dots<T, D>(q, kr.k, z);
 #pragma unroll
-                        for (int r = 0; r < kRows; ++r) {
-                            const int rr = r0 + q0 + r;
-                            if (q0 + r >= nr || (drafts && !sees_draft(a, row0, rr / a.rep, t))) continue;
-                            const float2 f = ml[rr];
-                            if (f.y != 0.f) sum = fmaf(ex2(fmaf(z[r], a.scale_log2, f.x)), f.y, sum);
-                        }
-                    }
+                for (int r = 0; r < kRows; ++r) {
+                    if (r >= nr || (drafts && !sees_draft(a, row0, (r0 + r) / a.rep, t))) continue;
+                    const float2 f = ml[r];
+                    if (f.y != 0.f) sum = fmaf(ex2(fmaf(z[r], a.scale_log2, f.x)), f.y, sum);
                 }
             }
             if (kr.k == nullptr) continue;
             if (drafts) a.w_new[(row0 + t) * a.c.Hkv + g] = sum;
             else a.c.weight[kr.meta] += sum;
         }
-    }
+    });
+}
+
+// A launch that may begin before the one ahead of it has ended (it waits where it needs it).
+template <class Kernel>
+cudaError_t launch_dependent(Kernel kernel, int grid, int threads, size_t smem, const CacheAttnArgs& a, cudaStream_t st) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+    return e == cudaSuccess ? cudaGetLastError() : e;
 }
 
 template <class T, int D>
 estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     constexpr bool kTc = sizeof(T) == 2;
-    a.RB = kTc ? cache_tc_rows(a.max_rows * a.rep) : kRows;
+    a.RB = kRows;
+    a.KS = 1;
+    if (kTc) cache_tc_shape(a.max_rows * a.rep, &a.RB, &a.KS);
     a.G = kTc ? ctx->num_sms : ctx->num_sms * 8;
     const int64_t groups = (int64_t)a.c.Hkv * (a.n_rows * a.rep / a.RB + a.B);
     const int64_t slots = a.G + groups;
@@ -383,19 +487,23 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     // largest sequence
     const int64_t nrb = ((int64_t)a.max_rows * a.rep + a.RB - 1) / a.RB;
     const int64_t units = (int64_t)a.c.Hkv * nrb * (a.n_slots / kCacheTile + 2 * (int64_t)a.B);
-    const size_t o_bytes = align_up(sizeof(float) * (size_t)slots * a.RB * D, 256);
-    const size_t ml_bytes = align_up(sizeof(float2) * (size_t)slots * a.RB, 256);
+    const size_t o_bytes = align_up(sizeof(float) * (size_t)slots * a.KS * a.RB * D, 256);
+    const size_t ml_bytes = align_up(sizeof(float2) * (size_t)slots * a.KS * a.RB, 256);
     const size_t z_bytes = sizeof(float) * (size_t)units * a.RB * kCacheTile;
     const bool weights = a.accumulate || a.w_new != nullptr;
     // Kept scores cost 8 bytes a row and key (a write and a read), forming them again a read of K
     // (D * sizeof(T) bytes a key): kept up to the break-even, and up to 2 GB of them.
-    a.store = weights && (int64_t)a.max_rows * a.rep * 8 <= (int64_t)(D * sizeof(T)) && z_bytes <= (size_t(2) << 30);
-    estp_status s = ws_reserve(ctx, o_bytes + ml_bytes + (a.store ? z_bytes : 0));
+    const int64_t R = (int64_t)a.max_rows * a.rep;
+    a.store = weights && R <= kCacheMaxStored && R * 8 <= (int64_t)(D * sizeof(T)) && z_bytes <= (size_t(2) << 30);
+    const bool again = weights && !a.store;
+    const size_t more = a.store ? z_bytes : again ? sizeof(float2) * (size_t)(a.n_rows * a.Hq) : 0;
+    estp_status s = ws_reserve(ctx, o_bytes + ml_bytes + more);
     if (s != ESTP_OK) return s;
     char* ws = static_cast<char*>(ctx->ws);
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(ws + o_bytes);
-    a.score = reinterpret_cast<float*>(ws + o_bytes + ml_bytes);
+    a.score = a.store ? reinterpret_cast<float*>(ws + o_bytes + ml_bytes) : nullptr;
+    a.factor = again ? reinterpret_cast<float2*>(ws + o_bytes + ml_bytes) : nullptr;
     cudaError_t e;
     if constexpr (kTc) {
         s = launch_cache_fwd_tc(a, st);
@@ -405,19 +513,15 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
         e = cudaGetLastError();
         if (e != cudaSuccess) return cuda_fail(e, "cache attention launch");
     }
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(ctx->num_sms * 8));
-    cfg.blockDim = dim3(kThreads);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = a.store ? cudaLaunchKernelEx(&cfg, cache_finish_kernel<T, D, true>, a)
-                : cudaLaunchKernelEx(&cfg, cache_finish_kernel<T, D, false>, a);
-    if (e == cudaSuccess) e = cudaGetLastError();
-    return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache attention finish launch");
+    e = launch_dependent(cache_finish_kernel<T, D>, ctx->num_sms * 8, kThreads, 0, a, st);
+    if (e != cudaSuccess) return cuda_fail(e, "cache attention finish launch");
+    if (!again) return ESTP_OK;
+    if constexpr (kTc) {
+        return launch_cache_weight_tc(ctx, a, st);
+    } else {
+        e = launch_dependent(cache_weight_kernel<T, D>, ctx->num_sms * 8, kThreads, 0, a, st);
+        return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache weight launch");
+    }
 }
 
 }  // namespace

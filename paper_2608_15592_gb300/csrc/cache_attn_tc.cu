@@ -17,14 +17,15 @@
 //
 // One persistent CTA per SM over the units of cache.cuh.
 //   warp 0     TMA producer: K and V tiles in turn through one ring, a box a page (a lane each)
-//   warp 1     MMA issuer; S of the next tile of a segment before O of this one
-//   warps 2..  NB epilogue groups of 4 warps; group nb owns rows nb RB .. of the block: its Q in
-//              shared memory, its S (double-buffered) and O in tensor memory, its P buffer
+//   warp 1     MMA issuer; S of a segment's next tiles before O of this one
+//   warps 2-9  two epilogue groups of 4 warps, each with its Q in shared memory, its S (double-
+//              buffered) and O in tensor memory and its P buffer; up to 64 rows they take the tiles
+//              in turn, more rows are shared out between them
 // Keys past a sequence's slots hold anything: S^T has them replaced, their P is 0 and their V rows
 // (up to the MMA's 16-key step) are zeroed in shared memory before the product, as 0 x NaN is not 0.
 // A draft whose V is not finite is zeroed there too and added by itself to the rows that see it.
 //
-// Bound by the K and V bytes while RB NB rows cost less than the 64 KB of a tile take to arrive
+// Bound by the K and V bytes while the rows cost less than the 64 KB of a tile take to arrive
 // (1.45 us an SM at the copy rate).  Every wait is bounded; on expiry the CTA records
 // ESTP_ERR_TIMEOUT, the group votes to leave, and copies and MMAs are drained before TMEM is freed.
 #include "cache.cuh"
@@ -35,27 +36,34 @@ namespace {
 
 constexpr int kAtom = kCacheTile * 128;  // 128 keys x 64 bf16
 
-template <int D, int RB, int NB>
+// Two epilogue groups.  KS = 2: they take the tiles of a segment in turn, each with a softmax of its
+// own over the block's RB rows (a group leaves a partial of its own).  KS = 1: every tile goes to
+// both, group g owning rows g RB .. of a block of 2 RB.
+constexpr int kGroups = 2;
+
+template <int D, int RB, int KS>
 struct Shape {
+    static constexpr int kN = RB < 16 ? 16 : RB;  // S columns: an MMA of M = 128 has N >= 16
     static constexpr int kAtoms = D / 64;
     static constexpr int kTileBytes = kAtoms * kAtom;
-    static constexpr int kQBytes = kAtoms * RB * 128;
+    static constexpr int kQBytes = kAtoms * kN * 128;
     static constexpr int kPBytes = RB == 64 ? 2 * kAtom : kAtom;
-    static constexpr int kFixed = NB * (kQBytes + kPBytes);
-    static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 384 - NB * 2 * RB * 4;
+    static constexpr int kFixed = kGroups * (kQBytes + kPBytes);
+    static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 400 - kGroups * 2 * RB * 4;
     static constexpr int kStages = kRoom / kTileBytes < 12 ? kRoom / kTileBytes : 12;
-    static constexpr int kThreads = 64 + 128 * NB;
-    static constexpr int kTmem = 4 * RB * NB;  // S: 2 RB a group, O: 2 RB a group
+    static constexpr int kThreads = 64 + 128 * kGroups;
+    static constexpr int kTmemUsed = kGroups * (2 * kN + 2 * RB);  // S twice, O hi and lo
+    static constexpr int kTmem = kTmemUsed <= 128 ? 128 : kTmemUsed <= 256 ? 256 : 512;
+    static constexpr int kOCol = kGroups * 2 * kN;
     // offsets from a 1024-aligned base
     static constexpr int kPOff = kStages * kTileBytes;
-    static constexpr int kQOff = kPOff + NB * kPBytes;
-    static constexpr int kBarOff = kQOff + NB * kQBytes;
-    static constexpr int kBars = 2 * kStages + 7 * NB + 1;
+    static constexpr int kQOff = kPOff + kGroups * kPBytes;
+    static constexpr int kBarOff = kQOff + kGroups * kQBytes;
+    static constexpr int kBars = 2 * kStages + 7 * kGroups + 1;
     static constexpr int kMiscOff = kBarOff + (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, poison bits
     static constexpr int kRowOff = kMiscOff + 48;  // a group's [RB] m and [RB] factors
-    static constexpr int kSmem = kRowOff + NB * 2 * RB * 4 + 1024;
+    static constexpr int kSmem = kRowOff + kGroups * 2 * RB * 4 + 1024;
     static_assert(kStages >= 4 && kSmem <= 227 * 1024, "shared memory per CTA");
-    static_assert(kTmem <= 512 && (kTmem & (kTmem - 1)) == 0, "tensor memory");
 };
 
 // tcgen05.ld / .st of 16 or 32 fp32 columns of this thread's lane
@@ -81,10 +89,19 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-// Orders every later use of v[0..15] after the wait for the load that fills them.
-__device__ __forceinline__ void tie16(float* v) {
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* v) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr));
 #pragma unroll
-    for (int k = 0; k < 16; k += 8)
+    for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[k]);
+}
+// Orders every later use of v[0..N) after the wait for the load that fills them.
+template <int N>
+__device__ __forceinline__ void tie(float* v) {
+#pragma unroll
+    for (int k = 0; k < N; k += 8)
         asm volatile("" : "+f"(v[k]), "+f"(v[k + 1]), "+f"(v[k + 2]), "+f"(v[k + 3]), "+f"(v[k + 4]), "+f"(v[k + 5]),
                           "+f"(v[k + 6]), "+f"(v[k + 7]));
 }
@@ -132,22 +149,15 @@ __device__ __forceinline__ uint32_t pack_hi_lo(float a, float b, uint32_t& lo) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Sums v[0..N) over the warp's lanes; lane k returns with the sum of column k % N (N = 16 or 32).
+// Sums v[0..N) over the warp's lanes; lane k returns with the sum of column k % N (N = 8, 16, 32).
 template <int N>
 __device__ __forceinline__ float reduce_scatter(float* v, int lane) {
-    if (N == 32) {
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const bool up = lane & 16;
-            const float send = up ? v[k] : v[k + 16], keep = up ? v[k + 16] : v[k];
-            v[k] = keep + __shfl_xor_sync(0xffffffffu, send, 16);
-        }
-    } else {
+    for (int o = 16; o >= N; o >>= 1)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], 16);
-    }
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1)
+    for (int o = N / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int k = 0; k < o; ++k) {
             const bool up = lane & o;
@@ -202,10 +212,11 @@ struct TcMaps {
     CUtensorMap k, v, kn, vn;
 };
 
-template <int D, int RB, int NB>
-__global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
+template <int D, int RB, int KS>
+__global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
     cache_fwd_tc_kernel(const __grid_constant__ TcMaps tm, const CacheAttnArgs a, const int box_rows, const int new_rows) {
-    using S = Shape<D, RB, NB>;
+    using S = Shape<D, RB, KS>;
+    constexpr int NB = kGroups;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
     uint64_t* full = reinterpret_cast<uint64_t*>(sm + S::kBarOff);  // [kStages]
@@ -324,8 +335,8 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
         if (lane == 0) {
-            constexpr uint32_t kIdS = idesc_bf16(kCacheTile, RB);
-            constexpr uint32_t kIdO = idesc_bf16(kCacheTile, 2 * RB) | (1u << 15) | (1u << 16);
+            constexpr uint32_t kIdS = idesc_bf16(kCacheTile, S::kN);
+            constexpr uint32_t kIdO = idesc_bf16(kCacheTile, 2 * RB) | (1u << 15) | (1u << 16);  // both MN-major
             uint32_t t = 0;            // tiles begun, over all segments
             uint32_t steps[NB] = {};   // S issued for a group; O follows in the same order
             uint32_t q_seen[NB] = {}, pv[NB] = {};
@@ -334,15 +345,16 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
                 ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
                 return ok;
             };
-            auto issue_s = [&](uint32_t tt, int groups, bool first) {
-                const uint32_t e = 2 * tt;
+            // S of the segment's i-th tile, for the groups that take it
+            auto issue_s = [&](int i, int groups) {
+                const uint32_t e = 2 * (t + i);
                 const int slot = (int)(e % S::kStages);
                 if (!wait(&full[slot], (e / S::kStages) & 1)) return;
                 const uint32_t ka = smem_u32(sm + slot * S::kTileBytes);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    if (nb >= groups) break;
-                    if (first && !wait(&q_full[nb], q_seen[nb]++ & 1)) return;
+                    if (KS == 2 ? (i & 1) != nb : nb >= groups) continue;
+                    if (i < KS && !wait(&q_full[nb], q_seen[nb]++ & 1)) return;  // the group's first tile
                     const uint32_t n = steps[nb]++, buf = n & 1, use = n >> 1;
                     if (use >= 1 && !wait(&s_empty[2 * nb + buf], (use - 1) & 1)) return;
                     tc_fence_after();
@@ -350,39 +362,41 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
                     const uint32_t qa = smem_u32(sm + S::kQOff + nb * S::kQBytes);
 #pragma unroll
                     for (int kk = 0; kk < D / 16; ++kk)
-                        mma_bf16<kIdS>(tmem + (2 * nb + buf) * RB, sw128_desc(ka + (kk >> 2) * kAtom + (kk & 3) * 32),
-                                       sw128_desc(qa + (kk >> 2) * RB * 128 + (kk & 3) * 32), kk > 0 ? 1u : 0u);
+                        mma_bf16<kIdS>(tmem + (2 * nb + buf) * S::kN, sw128_desc(ka + (kk >> 2) * kAtom + (kk & 3) * 32),
+                                       sw128_desc(qa + (kk >> 2) * S::kN * 128 + (kk & 3) * 32), kk > 0 ? 1u : 0u);
                     mma_commit(&s_full[2 * nb + buf]);
                 }
                 mma_commit(&empty[slot]);
             };
             while (ok && walk.next(a, sg)) {
-                const int groups = (sg.nr + RB - 1) / RB;
-                bool live = false;  // O holds a product of this segment
-                issue_s(t, groups, true);
-                for (int tile = sg.tile0; ok && tile < sg.tile1; ++tile, ++t) {
-                    if (tile + 1 < sg.tile1) issue_s(t + 1, groups, false);
+                const int groups = (sg.nr + RB - 1) / RB, tiles = sg.tile1 - sg.tile0;
+                bool live[NB] = {};  // a group's O holds a product of this segment
+                int ahead = 0;       // tiles whose S is issued: KS beyond the one whose O is
+                for (int i = 0; ok && i < tiles; ++i) {
+                    while (ok && ahead < tiles && ahead <= i + KS) issue_s(ahead++, groups);
                     if (!ok) break;
-                    const uint32_t e = 2 * t + 1;
+                    const uint32_t e = 2 * (t + i) + 1;
                     const int slot = (int)(e % S::kStages);
                     if (!wait(&full[slot], (e / S::kStages) & 1)) break;
                     const uint32_t va = smem_u32(sm + slot * S::kTileBytes);
-                    const int ksteps = (tile_keys(a, sg.s, tile) + 15) / 16;
+                    const int ksteps = (tile_keys(a, sg.s, sg.tile0 + i) + 15) / 16;
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
-                        if (nb >= groups || !wait(&p_full[nb], pv[nb]++ & 1)) break;
+                        if (KS == 2 ? (i & 1) != nb : nb >= groups) continue;
+                        if (!wait(&p_full[nb], pv[nb]++ & 1)) break;
                         tc_fence_after();
                         issued = true;
                         const uint32_t pa = smem_u32(sm + S::kPOff + nb * S::kPBytes);
                         for (int kk = 0; kk < ksteps; ++kk)
-                            mma_bf16<kIdO>(tmem + (uint32_t)(2 * RB * (NB + nb)), mn_desc(va + kk * 2048, D == 128 ? kAtom : 0),
-                                           mn_desc(pa + kk * 2048, kAtom), live || kk > 0 ? 1u : 0u);
+                            mma_bf16<kIdO>(tmem + (uint32_t)(S::kOCol + nb * 2 * RB), mn_desc(va + kk * 2048, D == 128 ? kAtom : 0),
+                                           mn_desc(pa + kk * 2048, kAtom), live[nb] || kk > 0 ? 1u : 0u);
                         mma_commit(&pv_done[nb]);
+                        live[nb] = live[nb] || ksteps > 0;
                     }
                     if (!ok) break;
-                    live = live || ksteps > 0;
                     mma_commit(&empty[slot]);
                 }
+                t += tiles;
             }
             if (issued) {
                 mma_commit(drain);
@@ -399,16 +413,17 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
         uint8_t* pb = sm + S::kPOff + nb * S::kPBytes;
         uint8_t* qb = sm + S::kQOff + nb * S::kQBytes;
         const uint32_t lane_off = (uint32_t)(q * 32) << 16;
-        const uint32_t t_o = tmem + lane_off + (uint32_t)(2 * RB * (NB + nb));
+        const uint32_t t_o = tmem + lane_off + (uint32_t)(S::kOCol + nb * 2 * RB);
+        constexpr int kCols = RB < 16 ? 8 : 16;  // columns of a tensor memory load
         uint32_t step = 0, t = 0, seg = 0;
         bool alive = true;
         auto wait = [&](uint64_t* b, uint32_t parity) {
             if (alive) alive = warp_wait(b, parity, abort_flag, a.status, a.wait_cycles);
         };
         while (walk.next(a, sg)) {
-            const int base = nb * RB, nr = min(RB, sg.nr - base);  // rows of this group
-            // the poison bits of this segment: group 0 may be one segment ahead of the other
-            volatile uint32_t* odd_drafts = poison + (seg++ & 1) * 4;
+            const int base = KS == 2 ? 0 : nb * RB, nr = min(RB, sg.nr - base);  // rows of this group
+            // the drafts' poison bits: a group's own, or shared by both, of which group 0 may be a segment ahead
+            volatile uint32_t* odd_drafts = poison + (KS == 2 ? nb : (int)(seg++ & 1)) * 4;
             if (nr <= 0) {                                // none: the other group works alone
                 t += sg.tile1 - sg.tile0;
                 continue;
@@ -422,17 +437,19 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
                     const int rr = sg.r0 + base + r, i = rr / a.rep, h = sg.g * a.rep + rr % a.rep;
                     v = *reinterpret_cast<const uint4*>(a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16);
                 }
-                *reinterpret_cast<uint4*>(qb + (ch >> 3) * RB * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v;
+                *reinterpret_cast<uint4*>(qb + (ch >> 3) * S::kN * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(&q_full[nb]);
+            const bool any = KS == 1 || nb < sg.tile1 - sg.tile0;  // the group takes a tile
+            if (lane == 0 && any) mbar_arrive(&q_full[nb]);
             if (j < RB) row_m[j] = -INFINITY;
             float l[RB];
 #pragma unroll
             for (int r = 0; r < RB; ++r) l[r] = 0.f;
             bool live = false;
-            for (int tile = sg.tile0; tile < sg.tile1; ++tile, ++step, ++t) {
+            const int first = sg.tile0 + (KS == 2 ? nb : 0);
+            for (int tile = first; tile < sg.tile1; tile += KS, ++step) {
                 const bool drafts = tile == sg.s.nt - 1;
                 const int keys = tile_keys(a, sg.s, tile);
                 const uint32_t buf = step & 1;
@@ -440,10 +457,12 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
                 tc_fence_after();
                 float z[RB];
 #pragma unroll
-                for (int r = 0; r < RB; r += 16) tmem_ld16(tmem + lane_off + (2 * nb + buf) * RB + r, z + r);
+                for (int r = 0; r < RB; r += kCols) {
+                    if (kCols == 8) tmem_ld8(tmem + lane_off + (2 * nb + buf) * S::kN + r, z + r);
+                    else tmem_ld16(tmem + lane_off + (2 * nb + buf) * S::kN + r, z + r);
+                }
                 tmem_wait_ld();
-#pragma unroll
-                for (int r = 0; r < RB; r += 16) tie16(z + r);
+                tie<RB>(z);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&s_empty[2 * nb + buf]);
@@ -470,7 +489,7 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
                         if (r < nr) to[r * kCacheTile] = z[r];
                 }
                 // does any score exceed its row's m by 2^8?
-                bool up = tile == sg.tile0 || !alive;
+                bool up = tile == first || !alive;
                 if (!up) {
                     float top = -INFINITY;
 #pragma unroll
@@ -507,7 +526,7 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
                             float o[16];
                             tmem_ld16(t_o + c, o);
                             tmem_wait_ld();
-                            tie16(o);
+                            tie<16>(o);
 #pragma unroll
                             for (int k = 0; k < 16; ++k) o[k] *= row_f[(c + k) % RB];
                             tmem_st16(t_o + c, o);
@@ -537,9 +556,9 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
                     if (RB == 64) *reinterpret_cast<uint4*>(prow + kAtom + ((ch ^ (j & 7)) << 4)) = lo;
                     else *reinterpret_cast<uint4*>(prow + (((ch + RB / 8) ^ (j & 7)) << 4)) = lo;
                 }
-                if (nb == 0 && (drafts || (keys & 15))) {
+                if ((KS == 2 || nb == 0) && (drafts || (keys & 15))) {
                     // V rows that must not reach the product: past the keys, and drafts that are not finite
-                    const uint32_t e = 2 * t + 1;
+                    const uint32_t e = 2 * (t + (tile - sg.tile0)) + 1;
                     const int slot = (int)(e % S::kStages);
                     wait(&full[slot], (e / S::kStages) & 1);
                     uint8_t* vr = sm + slot * S::kTileBytes + j * 128;
@@ -576,8 +595,9 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
                 group_or(bar, true);
                 break;
             }
+            t += sg.tile1 - sg.tile0;
             // the segment's partial
-            wait(&pv_done[nb], (step - 1) & 1);
+            if (step > 0) wait(&pv_done[nb], (step - 1) & 1);
             tc_fence_after();
             float* row_w = reinterpret_cast<float*>(qb);  // [4][RB]: every S of the segment is done with Q
             {
@@ -589,28 +609,33 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
                 }
             }
             if (group_or(bar, !alive)) break;
-            const int64_t part = (cta + sg.group) * a.RB + base;
+            const int64_t part = ((cta + sg.group) * KS + (KS == 2 ? nb : 0)) * a.RB + base;
             if (j < nr)
                 a.part_ml[part + j] = make_float2(row_m[j], (row_w[j] + row_w[RB + j]) + (row_w[2 * RB + j] + row_w[3 * RB + j]));
 #pragma unroll 1
-            for (int r = 0; r < RB; r += 16) {
+            for (int r = 0; r < RB; r += kCols) {
                 if (r >= nr) break;
-                float hi[16], lo[16];
-                tmem_ld16(t_o + r, hi);
-                tmem_ld16(t_o + RB + r, lo);
+                float hi[kCols], lo[kCols];
+                if (kCols == 8) {
+                    tmem_ld8(t_o + r, hi);
+                    tmem_ld8(t_o + RB + r, lo);
+                } else {
+                    tmem_ld16(t_o + r, hi);
+                    tmem_ld16(t_o + RB + r, lo);
+                }
                 tmem_wait_ld();
-                tie16(hi);
-                tie16(lo);
+                tie<kCols>(hi);
+                tie<kCols>(lo);
                 if (D == 128 || q < 2) {
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
+                    for (int k = 0; k < kCols; ++k) {
                         if (r + k >= nr) break;
                         a.part_o[(part + r + k) * D + j] = live ? hi[k] + lo[k] : 0.f;
                     }
                 }
             }
             tc_fence_before();
-            if (sg.tile1 == sg.s.nt && (odd_drafts[0] | odd_drafts[1] | odd_drafts[2] | odd_drafts[3])) {
+            if (sg.tile1 == sg.s.nt && (KS == 1 || ((sg.tile1 - 1 - sg.tile0) & 1) == nb) && (odd_drafts[0] | odd_drafts[1] | odd_drafts[2] | odd_drafts[3])) {
                 // drafts whose V is not finite: P is still in its buffer
                 if (D == 128 || q < 2) {
                     for (int x = 0; x < sg.s.n; ++x) {
@@ -637,6 +662,312 @@ __global__ void __launch_bounds__(Shape<D, RB, NB>::kThreads, 1)
     if (warp == 1) {
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmem));
+    }
+}
+
+// The weights with the scores formed again (see cache_attn.cu): S^T = K Q^T tile by tile with every
+// row of the (b, KV head) resident, w_j = sum_r c_r 2^(S_jr c - M_r) / L_r, a thread a key.  A CTA takes
+// an equal run of the call's (b, KV head, tile); the blocks of 64 rows of a tile go to the two groups
+// in turn, whose sums are added in their order.  Rows beyond kWRows take another pass over the run,
+// by the same threads.  Bound by K's bytes up to some 170 rows a KV head, then by ex2 (16 a clock).
+constexpr int kWRows = 448, kWBlock = 64, kWStages = 3, kWBufs = 4;
+template <int D>
+struct WShape {
+    static constexpr int kAtoms = D / 64;
+    static constexpr int kTileBytes = kAtoms * kAtom;
+    static constexpr int kBlockBytes = kAtoms * kWBlock * 128;  // Q of one block of rows
+    static constexpr int kQOff = kWStages * kTileBytes;
+    static constexpr int kFOff = kQOff + kWRows / kWBlock * kBlockBytes;  // [kWRows] factors
+    static constexpr int kRedOff = kFOff + kWRows * 8;                    // [2][128] the second group's sums
+    static constexpr int kBarOff = kRedOff + 2 * 128 * 4;
+    static constexpr int kBars = 2 * kWStages + 1 + 4 * kWBufs + 1;
+    static constexpr int kMiscOff = kBarOff + kBars * 8;
+    static constexpr int kSmem = kMiscOff + 16 + 1024;
+    static constexpr int kThreads = 64 + 256;
+    static_assert(kSmem <= 227 * 1024, "shared memory per CTA");
+};
+
+__device__ __forceinline__ bool both_groups_or(bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.aligned.pred q, 3, 256, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)x)
+        : "memory");
+    return r != 0;
+}
+
+// Runs of one (b, KV head) in items [it, it1).
+struct ItemWalk {
+    Place at;
+    int64_t it, it1;
+    SeqShape s;
+    int b, g, tile0, tile1;
+    __device__ __forceinline__ bool next(const CacheAttnArgs& a) {
+        while (it < it1) {
+            s = seq_shape(a, at.b);
+            const int64_t items = s.items(a.c.Hkv);
+            if (it >= at.item0 + items) {
+                at.item0 += items;
+                ++at.b;
+                continue;
+            }
+            b = at.b;
+            g = (int)((it - at.item0) / s.nt);
+            tile0 = (int)((it - at.item0) % s.nt);
+            tile1 = (int)min((int64_t)s.nt, tile0 + (it1 - it));
+            it += tile1 - tile0;
+            // tiles whose weight no one asks for
+            if (!a.accumulate) tile0 = max(tile0, s.nt - 1);
+            if (a.w_new == nullptr) tile1 = min(tile1, s.nt - 1);
+            if (tile0 < tile1) return true;
+        }
+        return false;
+    }
+};
+
+template <int D>
+__global__ void __launch_bounds__(WShape<D>::kThreads, 1)
+    cache_weight_tc_kernel(const __grid_constant__ TcMaps tm, const CacheAttnArgs a, const int box_rows, const int new_rows) {
+    using S = WShape<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + S::kBarOff);  // [kWStages]
+    uint64_t* empty = full + kWStages;
+    uint64_t* q_full = empty + kWStages;
+    uint64_t* s_full = q_full + 1;          // [2][kWBufs]
+    uint64_t* s_empty = s_full + 2 * kWBufs;
+    uint64_t* drain = s_empty + 2 * kWBufs;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::kMiscOff);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 4);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kWStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        mbar_init(q_full, 8);
+        for (int i = 0; i < 2 * kWBufs; ++i) {
+            mbar_init(&s_full[i], 1);
+            mbar_init(&s_empty[i], 4);
+        }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                     "r"(2 * kWBufs * kWBlock));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    const int64_t cta = blockIdx.x, G = gridDim.x;
+    PlanScratch* sc = reinterpret_cast<PlanScratch*>(sm);  // in the ring, unused until the barrier below
+    Place* place = reinterpret_cast<Place*>(sm + 1024);
+    const PlanTotals tot = plan_block(a, sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int64_t it = unit_begin(cta, all.items, G);
+        if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) *place = x;
+    });
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    ItemWalk w{Place{0, 0, 0, 0}, 0, 0};
+    if (tot.ok) {
+        w.it = unit_begin(cta, tot.items, G);
+        w.it1 = unit_begin(cta + 1, tot.items, G);
+        if (w.it < w.it1) w.at = *place;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the factors are complete
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ producer
+        uint32_t e = 0;
+        bool ok = true;
+        while (ok && w.next(a)) {
+            for (int r0 = 0; ok && r0 < w.s.n * a.rep; r0 += kWRows) {
+                for (int tile = w.tile0; tile < w.tile1; ++tile, ++e) {
+                    const bool drafts = tile == w.s.nt - 1;
+                    const int keys = tile_keys(a, w.s, tile), rows = drafts ? new_rows : box_rows;
+                    const int boxes = drafts ? (keys > 0 ? 1 : 0) : (keys + box_rows - 1) / box_rows;
+                    int64_t page = 0;
+                    int at = 0;
+                    if (!drafts && lane < boxes) {
+                        const int slot = tile * kCacheTile + lane * box_rows;
+                        page = a.c.page_of(w.b, slot, a.status);
+                        if (page < 0) page = a.c.n_pages > 0 ? a.c.n_pages : 1;
+                        at = slot & ((1 << a.c.shift) - 1);
+                    }
+                    const int slot = (int)(e % kWStages);
+                    const uint32_t use = e / kWStages;
+                    if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
+                        ok = false;
+                        break;
+                    }
+                    if (lane == 0) mbar_expect_tx(&full[slot], (uint32_t)(boxes * rows * 128 * S::kAtoms));
+                    __syncwarp();
+                    if (lane < boxes) {
+                        uint8_t* to = sm + slot * S::kTileBytes + lane * rows * 128;
+#pragma unroll
+                        for (int x = 0; x < S::kAtoms; ++x) {
+                            if (drafts) tma_load_3d(to + x * kAtom, &tm.kn, x * 64, w.g, a.cu[w.b], &full[slot]);
+                            else tma_load_4d(to + x * kAtom, &tm.k, x * 64, at, w.g, (int)page, &full[slot]);
+                        }
+                    }
+                }
+            }
+        }
+        if (lane == 0)
+            for (uint32_t i = 0; i < (uint32_t)kWStages && i < e; ++i)
+                drain_wait(&full[(e - 1 - i) % kWStages], ((e - 1 - i) / kWStages) & 1, a.status);
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------------------------------------------------- MMA issuer
+        if (lane == 0) {
+            constexpr uint32_t kId = idesc_bf16(kCacheTile, kWBlock);
+            uint32_t e = 0, loads = 0, steps[2] = {0, 0};
+            bool ok = true, issued = false;
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
+                return ok;
+            };
+            while (ok && w.next(a)) {
+                const int R = w.s.n * a.rep;
+                for (int r0 = 0; ok && r0 < R; r0 += kWRows) {
+                    if (!wait(q_full, loads++ & 1)) break;
+                    const int blocks = (min(kWRows, R - r0) + kWBlock - 1) / kWBlock;
+                    for (int tile = w.tile0; ok && tile < w.tile1; ++tile, ++e) {
+                        const int slot = (int)(e % kWStages);
+                        if (!wait(&full[slot], (e / kWStages) & 1)) break;
+                        const uint32_t ka = smem_u32(sm + slot * S::kTileBytes);
+                        for (int k = 0; k < blocks; ++k) {
+                            const int gr = k & 1;
+                            const uint32_t n = steps[gr]++, buf = n % kWBufs, use = n / kWBufs;
+                            if (use >= 1 && !wait(&s_empty[gr * kWBufs + buf], (use - 1) & 1)) break;
+                            tc_fence_after();
+                            issued = true;
+                            const uint32_t qa = smem_u32(sm + S::kQOff + k * S::kBlockBytes);
+#pragma unroll
+                            for (int kk = 0; kk < D / 16; ++kk)
+                                mma_bf16<kId>(tmem + (gr * kWBufs + buf) * kWBlock,
+                                              sw128_desc(ka + (kk >> 2) * kAtom + (kk & 3) * 32),
+                                              sw128_desc(qa + (kk >> 2) * kWBlock * 128 + (kk & 3) * 32), kk > 0 ? 1u : 0u);
+                            mma_commit(&s_full[gr * kWBufs + buf]);
+                        }
+                        if (ok) mma_commit(&empty[slot]);
+                    }
+                }
+            }
+            if (issued) {
+                mma_commit(drain);
+                drain_wait(drain, 0, a.status);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------- epilogue
+        const int gr = (warp - 2) >> 2, q = warp & 3, j = q * 32 + lane, tid = threadIdx.x - 64;
+        float2* fs = reinterpret_cast<float2*>(sm + S::kFOff);
+        float* red = reinterpret_cast<float*>(sm + S::kRedOff);
+        uint32_t step = 0, parity = 0;
+        bool alive = true;
+        while (alive && w.next(a)) {
+            const int R = w.s.n * a.rep;
+            const int64_t row0 = a.cu[w.b];
+            for (int r0 = 0; alive && r0 < R; r0 += kWRows) {
+                const int nr = min(kWRows, R - r0), blocks = (nr + kWBlock - 1) / kWBlock;
+                // Q and factors of this pass's rows; every S of the pass before is done with them
+                for (int x = tid; x < blocks * kWBlock * (D / 8); x += 256) {
+                    const int r = x / (D / 8), ch = x % (D / 8);
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (r < nr) {
+                        const int i = (r0 + r) / a.rep, h = w.g * a.rep + (r0 + r) % a.rep;
+                        v = *reinterpret_cast<const uint4*>(a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16);
+                    }
+                    *reinterpret_cast<uint4*>(sm + S::kQOff + (r / kWBlock) * S::kBlockBytes + (ch >> 3) * kWBlock * 128 +
+                                              (r % kWBlock) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v;
+                }
+                for (int r = tid; r < blocks * kWBlock; r += 256)
+                    fs[r] = r < nr ? a.factor[(row0 + (r0 + r) / a.rep) * a.Hq + w.g * a.rep + (r0 + r) % a.rep]
+                                   : make_float2(0.f, 0.f);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                both_groups_or(false);  // the factors are everyone's
+                if (lane == 0) mbar_arrive(q_full);
+                for (int tile = w.tile0; tile < w.tile1; ++tile, parity ^= 1) {
+                    const bool drafts = tile == w.s.nt - 1;
+                    const int keys = tile_keys(a, w.s, tile);
+                    float* to = nullptr;
+                    float had = 0.f;
+                    if (gr == 0 && j < keys) {  // early: its latency passes under the sums
+                        if (drafts) {
+                            to = a.w_new + (row0 + j) * a.c.Hkv + w.g;
+                            if (r0 > 0) had = *to;
+                        } else {
+                            const int slot = tile * kCacheTile + j;
+                            const int64_t page = a.c.page_of(w.b, slot, a.status);
+                            if (page >= 0) {
+                                to = a.c.weight + a.c.meta(page, slot, w.g);
+                                had = *to;
+                            }
+                        }
+                    }
+                    float sum[2] = {0.f, 0.f};
+                    for (int k = gr; k < blocks; k += 2, ++step) {
+                        const uint32_t buf = step % kWBufs;
+                        if (alive)
+                            alive = warp_wait(&s_full[gr * kWBufs + buf], (step / kWBufs) & 1, abort_flag, a.status, a.wait_cycles);
+                        tc_fence_after();
+                        const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (gr * kWBufs + buf) * kWBlock;
+                        const int cols = min(kWBlock, nr - k * kWBlock);
+#pragma unroll 1
+                        for (int c = 0; c < cols; c += 16) {
+                            float z[16];
+                            tmem_ld16(ta + c, z);
+                            tmem_wait_ld();
+                            tie<16>(z);
+                            const float4* f4 = reinterpret_cast<const float4*>(fs + k * kWBlock + c);
+                            if (!drafts) {
+#pragma unroll
+                                for (int i = 0; i < 16; i += 2) {
+                                    const float4 f = f4[i / 2];
+                                    const float e0 = ex2(fmaf(z[i], a.scale_log2, f.x)), e1 = ex2(fmaf(z[i + 1], a.scale_log2, f.z));
+                                    sum[0] = f.y != 0.f ? fmaf(e0, f.y, sum[0]) : sum[0];
+                                    sum[1] = f.w != 0.f ? fmaf(e1, f.w, sum[1]) : sum[1];
+                                }
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    const int r = k * kWBlock + c + i;
+                                    const float2 f = fs[r];
+                                    if (f.y != 0.f && j < keys && sees_draft(a, row0, (r0 + r) / a.rep, j))
+                                        sum[0] = fmaf(ex2(fmaf(z[i], a.scale_log2, f.x)), f.y, sum[0]);
+                                }
+                            }
+                        }
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&s_empty[gr * kWBufs + buf]);
+                    }
+                    const float mine = sum[0] + sum[1];
+                    if (gr == 1) red[parity * 128 + j] = mine;
+                    if (both_groups_or(!alive)) {
+                        alive = false;
+                        break;
+                    }
+                    if (to != nullptr) *to = had + (mine + red[parity * 128 + j]);
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) {
+        __syncwarp();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kWBufs * kWBlock));
     }
 }
 
@@ -668,39 +999,75 @@ estp_status rows_map(CUtensorMap* m, const CacheAttnArgs& a, const void* base, i
     return r == CUDA_SUCCESS ? ESTP_OK : fail(ESTP_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
-template <int D, int RB, int NB>
+template <int D, int RB, int KS>
 estp_status launch(const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int new_rows, cudaStream_t st) {
-    using S = Shape<D, RB, NB>;
-    cudaError_t e = cudaFuncSetAttribute(cache_fwd_tc_kernel<D, RB, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    using S = Shape<D, RB, KS>;
+    cudaError_t e = cudaFuncSetAttribute(cache_fwd_tc_kernel<D, RB, KS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
     if (e != cudaSuccess) return cuda_fail(e, "cache attention smem attribute");
-    cache_fwd_tc_kernel<D, RB, NB><<<(unsigned)a.G, S::kThreads, S::kSmem, st>>>(tm, a, box_rows, new_rows);
+    cache_fwd_tc_kernel<D, RB, KS><<<(unsigned)a.G, S::kThreads, S::kSmem, st>>>(tm, a, box_rows, new_rows);
     e = cudaGetLastError();
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache attention launch");
 }
 
+template <int D>
+estp_status launch_rows(const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int new_rows, cudaStream_t st) {
+    switch (a.RB) {
+        case 8: return launch<D, 8, 2>(tm, a, box_rows, new_rows, st);
+        case 16: return launch<D, 16, 2>(tm, a, box_rows, new_rows, st);
+        case 32: return launch<D, 32, 2>(tm, a, box_rows, new_rows, st);
+        case 64: return launch<D, 64, 2>(tm, a, box_rows, new_rows, st);
+        default: return launch<D, 64, 1>(tm, a, box_rows, new_rows, st);
+    }
+}
+
 }  // namespace
 
-int cache_tc_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+void cache_tc_shape(int rows, int* RB, int* KS) {
+    *RB = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    *KS = rows <= 64 ? 2 : 1;
+}
+
+static estp_status make_maps(const CacheAttnArgs& a, TcMaps* tm, int* box_rows, int* new_rows) {
+    const int page = 1 << a.c.shift;
+    *box_rows = page < kCacheTile ? page : kCacheTile;
+    *new_rows = (a.max_rows + 7) / 8 * 8;
+    estp_status s = pages_map(&tm->k, a.c, a.c.k, a.Q, *box_rows);
+    if (s == ESTP_OK) s = pages_map(&tm->v, a.c, a.c.v, a.Q, *box_rows);
+    if (s == ESTP_OK) s = rows_map(&tm->kn, a, a.kn, *new_rows);
+    if (s == ESTP_OK) s = rows_map(&tm->vn, a, a.vn, *new_rows);
+    return s;
+}
 
 estp_status launch_cache_fwd_tc(const CacheAttnArgs& a, cudaStream_t st) {
     TcMaps tm;
-    const int page = 1 << a.c.shift, box_rows = page < kCacheTile ? page : kCacheTile;
-    const int new_rows = (a.max_rows + 7) / 8 * 8;
-    estp_status s = pages_map(&tm.k, a.c, a.c.k, a.Q, box_rows);
-    if (s == ESTP_OK) s = pages_map(&tm.v, a.c, a.c.v, a.Q, box_rows);
-    if (s == ESTP_OK) s = rows_map(&tm.kn, a, a.kn, new_rows);
-    if (s == ESTP_OK) s = rows_map(&tm.vn, a, a.vn, new_rows);
+    int box_rows, new_rows;
+    const estp_status s = make_maps(a, &tm, &box_rows, &new_rows);
     if (s != ESTP_OK) return s;
-    if (a.c.d == 128) {
-        if (a.RB == 16) return launch<128, 16, 1>(tm, a, box_rows, new_rows, st);
-        if (a.RB == 32) return launch<128, 32, 1>(tm, a, box_rows, new_rows, st);
-        if (a.RB == 64) return launch<128, 64, 1>(tm, a, box_rows, new_rows, st);
-        return launch<128, 64, 2>(tm, a, box_rows, new_rows, st);
-    }
-    if (a.RB == 16) return launch<64, 16, 1>(tm, a, box_rows, new_rows, st);
-    if (a.RB == 32) return launch<64, 32, 1>(tm, a, box_rows, new_rows, st);
-    if (a.RB == 64) return launch<64, 64, 1>(tm, a, box_rows, new_rows, st);
-    return launch<64, 64, 2>(tm, a, box_rows, new_rows, st);
+    return a.c.d == 128 ? launch_rows<128>(tm, a, box_rows, new_rows, st) : launch_rows<64>(tm, a, box_rows, new_rows, st);
+}
+
+estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st) {
+    TcMaps tm;
+    int box_rows, new_rows;
+    const estp_status s = make_maps(a, &tm, &box_rows, &new_rows);
+    if (s != ESTP_OK) return s;
+    auto kernel = a.c.d == 128 ? cache_weight_tc_kernel<128> : cache_weight_tc_kernel<64>;
+    const int smem = a.c.d == 128 ? WShape<128>::kSmem : WShape<64>::kSmem;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return cuda_fail(e, "cache weight smem attribute");
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctx->num_sms);
+    cfg.blockDim = dim3(WShape<128>::kThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, tm, a, box_rows, new_rows);
+    if (e == cudaSuccess) e = cudaGetLastError();
+    return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache weight launch");
 }
 
 }  // namespace estp
