@@ -107,8 +107,7 @@ struct PlanTotals {
     bool ok;                       // lengths, cu and their sums are what the host was told
 };
 struct PlanScratch {
-    int64_t sum[3][33];
-    unsigned long long slots;
+    int64_t sum[4][33];  // units, groups, items, slots
     int bad;
 };
 
@@ -120,13 +119,9 @@ __device__ __forceinline__ PlanTotals plan_block(const CacheAttnArgs& a, PlanScr
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5, n_warps = blockDim.x >> 5;
     const int run = (a.B + blockDim.x - 1) / blockDim.x;
     const int b0 = min(a.B, t * run), b1 = min(a.B, b0 + run);
-    if (t == 0) {
-        sc->bad = 0;
-        sc->slots = 0;
-    }
+    if (t == 0) sc->bad = 0;
     __syncthreads();
-    int64_t s[3] = {0, 0, 0};
-    unsigned long long slots = 0;
+    int64_t s[4] = {0, 0, 0, 0};
     for (int b = b0; b < b1; ++b) {
         if (!seq_ok(a, b)) {
             sc->bad = 1;
@@ -136,21 +131,22 @@ __device__ __forceinline__ PlanTotals plan_block(const CacheAttnArgs& a, PlanScr
         s[0] += q.units(a.c.Hkv);
         s[1] += (int64_t)a.c.Hkv * q.nrb;
         s[2] += q.items(a.c.Hkv);
-        slots += q.len;
+        s[3] += q.len;
     }
-    if (slots) atomicAdd(&sc->slots, slots);
-    int64_t inc[3];
+    int64_t inc[4];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 4; ++k) {
         inc[k] = s[k];
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t x = __shfl_up_sync(0xffffffffu, inc[k], o);
-            if (lane >= o) inc[k] += x;
+        if (warp * 32 * run < a.B) {  // warps without sequences have nothing to add
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t x = __shfl_up_sync(0xffffffffu, inc[k], o);
+                if (lane >= o) inc[k] += x;
+            }
         }
         if (lane == 31) sc->sum[k][warp] = inc[k];
     }
     __syncthreads();
-    if (t < 3) {
+    if (t < 4) {
         int64_t sum = 0;
         for (int w = 0; w < n_warps; ++w) {
             const int64_t x = sc->sum[t][w];
@@ -161,7 +157,7 @@ __device__ __forceinline__ PlanTotals plan_block(const CacheAttnArgs& a, PlanScr
     }
     __syncthreads();
     const PlanTotals tot{sc->sum[0][32], sc->sum[1][32], sc->sum[2][32],
-                         sc->bad == 0 && sc->slots <= (unsigned long long)a.n_slots};
+                         sc->bad == 0 && sc->sum[3][32] <= a.n_slots};
     if (!tot.ok && t == 0) report(a.status, ESTP_ERR_INVALID_ARG);
     if (tot.ok) {
         Place p{0, sc->sum[0][warp] + inc[0] - s[0], sc->sum[1][warp] + inc[1] - s[1],

@@ -17,10 +17,12 @@
 //
 // One persistent CTA per SM over the units of cache.cuh.
 //   warp 0     TMA producer: K and V tiles in turn through one ring, a box a page (a lane each)
-//   warp 1     MMA issuer; S of a segment's next tiles before O of this one
-//   warps 2-9  two epilogue groups of 4 warps, each with its Q in shared memory, its S (double-
-//              buffered) and O in tensor memory and its P buffer; up to 64 rows they take the tiles
-//              in turn, more rows are shared out between them
+//   warp 1     issues S, as far ahead as K tiles and S buffers allow
+//   warp 2     issues O, as soon as a P is written
+//   warp 3     loads the rows' Q, up to 64 rows a segment ahead
+//   warps 4-11 two epilogue groups of 4 warps, each with its S (double-buffered) and O in tensor
+//              memory and its P buffer; up to 64 rows they take the tiles in turn, more rows are
+//              shared out between them
 // Keys past a sequence's slots hold anything: S^T has them replaced, their P is 0 and their V rows
 // (up to the MMA's 16-key step) are zeroed in shared memory before the product, as 0 x NaN is not 0.
 // A draft whose V is not finite is zeroed there too and added by itself to the rows that see it.
@@ -46,20 +48,26 @@ struct Shape {
     static constexpr int kN = RB < 16 ? 16 : RB;  // S columns: an MMA of M = 128 has N >= 16
     static constexpr int kAtoms = D / 64;
     static constexpr int kTileBytes = kAtoms * kAtom;
-    static constexpr int kQBytes = kAtoms * kN * 128;
-    static constexpr int kPBytes = RB == 64 ? 2 * kAtom : kAtom;
-    static constexpr int kFixed = kGroups * (kQBytes + kPBytes);
-    static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 400 - kGroups * 2 * RB * 4;
+    static constexpr int kQRows = KS == 2 ? kN : 2 * RB;          // rows of a block
+    static constexpr int kQBufs = KS;                             // the next segment's Q loads ahead
+    static constexpr int kQBytes = kAtoms * kQRows * 128;
+    // P: [128 keys] rows of 128 bytes, hi then lo; 64 rows take two, up to 16 share one between the groups
+    static constexpr int kPStep = RB == 64 ? 2 * kAtom : RB == 32 ? kAtom : 64;  // from a group's P to the other's
+    static constexpr int kPBytes = RB == 64 ? 4 * kAtom : RB == 32 ? 2 * kAtom : kAtom;
+    static constexpr int kFixed = kQBufs * kQBytes + kPBytes;
+    static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 400 - kGroups * (RB == 64 ? 2 : 6) * RB * 4;
     static constexpr int kStages = kRoom / kTileBytes < 12 ? kRoom / kTileBytes : 12;
-    static constexpr int kThreads = 64 + 128 * kGroups;
+    static constexpr int kThreads = 128 + 128 * kGroups;
     static constexpr int kTmemUsed = kGroups * (2 * kN + 2 * RB);  // S twice, O hi and lo
     static constexpr int kTmem = kTmemUsed <= 128 ? 128 : kTmemUsed <= 256 ? 256 : 512;
     static constexpr int kOCol = kGroups * 2 * kN;
     // offsets from a 1024-aligned base
     static constexpr int kPOff = kStages * kTileBytes;
-    static constexpr int kQOff = kPOff + kGroups * kPBytes;
-    static constexpr int kBarOff = kQOff + kGroups * kQBytes;
-    static constexpr int kBars = 2 * kStages + 7 * kGroups + 1;
+    static constexpr int kQOff = kPOff + kPBytes;
+    static constexpr int kRedOff = kQOff + kQBufs * kQBytes;   // a group's [4][RB] per-warp values
+    // (64 rows: in the P buffer, when it is free)
+    static constexpr int kBarOff = kRedOff + (RB == 64 ? 0 : kGroups * 4 * RB * 4);
+    static constexpr int kBars = 2 * kStages + 2 * kQBufs + 6 * kGroups + 2;
     static constexpr int kMiscOff = kBarOff + (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, poison bits
     static constexpr int kRowOff = kMiscOff + 48;  // a group's [RB] m and [RB] factors
     static constexpr int kSmem = kRowOff + kGroups * 2 * RB * 4 + 1024;
@@ -221,12 +229,13 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
     uint8_t* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
     uint64_t* full = reinterpret_cast<uint64_t*>(sm + S::kBarOff);  // [kStages]
     uint64_t* empty = full + S::kStages;                            // [kStages]
-    uint64_t* q_full = empty + S::kStages;                          // [NB]
-    uint64_t* s_full = q_full + NB;                                 // [NB][2]
+    uint64_t* q_full = empty + S::kStages;                          // [kQBufs]
+    uint64_t* q_empty = q_full + S::kQBufs;                         // [kQBufs]
+    uint64_t* s_full = q_empty + S::kQBufs;                         // [NB][2]
     uint64_t* s_empty = s_full + 2 * NB;                            // [NB][2]
     uint64_t* p_full = s_empty + 2 * NB;                            // [NB]
     uint64_t* pv_done = p_full + NB;                                // [NB]
-    uint64_t* drain = pv_done + NB;
+    uint64_t* drain = pv_done + NB;                                 // [2] each issuer's MMAs done
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::kMiscOff);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 4);
     volatile uint32_t* poison = reinterpret_cast<volatile uint32_t*>(sm + S::kMiscOff + 16);  // [2][4] drafts with V not finite
@@ -238,8 +247,11 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
+        for (int i = 0; i < S::kQBufs; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 1);
+        }
         for (int i = 0; i < NB; ++i) {
-            mbar_init(&q_full[i], 4);
             mbar_init(&s_full[2 * i], 1);
             mbar_init(&s_full[2 * i + 1], 1);
             mbar_init(&s_empty[2 * i], 4);
@@ -247,7 +259,8 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
             mbar_init(&p_full[i], 4);
             mbar_init(&pv_done[i], 1);
         }
-        mbar_init(drain, 1);
+        mbar_init(&drain[0], 1);
+        mbar_init(&drain[1], 1);
         *abort_flag = 0;
         mbar_fence_init();
     }
@@ -260,8 +273,8 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
     const int64_t cta = blockIdx.x;
     // the plan's scratch lies in the ring, which is unused until the barrier below
     PlanScratch* sc = reinterpret_cast<PlanScratch*>(sm);
-    Place* place = reinterpret_cast<Place*>(sm + 1024);
-    static_assert(sizeof(PlanScratch) <= 1024, "scratch of the plan");
+    Place* place = reinterpret_cast<Place*>(sm + 1088);
+    static_assert(sizeof(PlanScratch) <= 1088, "scratch of the plan");
     const PlanTotals tot = plan_block(a, sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
         const int64_t u = unit_begin(cta, all.units, ctas_of(a, all.units));
         if (u >= x.unit0 && u < x.unit0 + s.units(a.c.Hkv)) *place = x;
@@ -333,49 +346,66 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                 drain_wait(&full[(e - 1 - i) % S::kStages], ((e - 1 - i) / S::kStages) & 1, a.status);
         __syncwarp();
     } else if (warp == 1) {
-        // ---------------------------------------------------------- MMA issuer
+        // ------------------------------------------------------------ S issuer
         if (lane == 0) {
             constexpr uint32_t kIdS = idesc_bf16(kCacheTile, S::kN);
-            constexpr uint32_t kIdO = idesc_bf16(kCacheTile, 2 * RB) | (1u << 15) | (1u << 16);  // both MN-major
-            uint32_t t = 0;            // tiles begun, over all segments
-            uint32_t steps[NB] = {};   // S issued for a group; O follows in the same order
-            uint32_t q_seen[NB] = {}, pv[NB] = {};
+            uint32_t t = 0, seg = 0;   // tiles and segments begun
+            uint32_t steps[NB] = {};   // S issued for a group
             bool ok = true, issued = false;
             auto wait = [&](uint64_t* bar, uint32_t parity) {
                 ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
                 return ok;
             };
-            // S of the segment's i-th tile, for the groups that take it
-            auto issue_s = [&](int i, int groups) {
-                const uint32_t e = 2 * (t + i);
-                const int slot = (int)(e % S::kStages);
-                if (!wait(&full[slot], (e / S::kStages) & 1)) return;
-                const uint32_t ka = smem_u32(sm + slot * S::kTileBytes);
+            while (ok && walk.next(a, sg)) {
+                const int groups = (sg.nr + RB - 1) / RB, tiles = sg.tile1 - sg.tile0;
+                const uint32_t qb = seg % S::kQBufs;
+                if (!wait(&q_full[qb], (seg / S::kQBufs) & 1)) break;
+                ++seg;
+                for (int i = 0; ok && i < tiles; ++i, ++t) {
+                    const uint32_t e = 2 * t;
+                    const int slot = (int)(e % S::kStages);
+                    if (!wait(&full[slot], (e / S::kStages) & 1)) break;
+                    const uint32_t ka = smem_u32(sm + slot * S::kTileBytes);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    if (KS == 2 ? (i & 1) != nb : nb >= groups) continue;
-                    if (i < KS && !wait(&q_full[nb], q_seen[nb]++ & 1)) return;  // the group's first tile
-                    const uint32_t n = steps[nb]++, buf = n & 1, use = n >> 1;
-                    if (use >= 1 && !wait(&s_empty[2 * nb + buf], (use - 1) & 1)) return;
-                    tc_fence_after();
-                    issued = true;
-                    const uint32_t qa = smem_u32(sm + S::kQOff + nb * S::kQBytes);
+                    for (int nb = 0; nb < NB; ++nb) {
+                        if (KS == 2 ? (i & 1) != nb : nb >= groups) continue;
+                        const uint32_t n = steps[nb]++, buf = n & 1, use = n >> 1;
+                        if (use >= 1 && !wait(&s_empty[2 * nb + buf], (use - 1) & 1)) break;
+                        tc_fence_after();
+                        issued = true;
+                        const uint32_t qa = smem_u32(sm + S::kQOff + qb * S::kQBytes + (KS == 2 ? 0 : nb * RB * 128));
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk)
-                        mma_bf16<kIdS>(tmem + (2 * nb + buf) * S::kN, sw128_desc(ka + (kk >> 2) * kAtom + (kk & 3) * 32),
-                                       sw128_desc(qa + (kk >> 2) * S::kN * 128 + (kk & 3) * 32), kk > 0 ? 1u : 0u);
-                    mma_commit(&s_full[2 * nb + buf]);
+                        for (int kk = 0; kk < D / 16; ++kk)
+                            mma_bf16<kIdS>(tmem + (2 * nb + buf) * S::kN, sw128_desc(ka + (kk >> 2) * kAtom + (kk & 3) * 32),
+                                           sw128_desc(qa + (kk >> 2) * S::kQRows * 128 + (kk & 3) * 32), kk > 0 ? 1u : 0u);
+                        mma_commit(&s_full[2 * nb + buf]);
+                    }
+                    if (ok) mma_commit(&empty[slot]);
                 }
-                mma_commit(&empty[slot]);
+                if (ok) mma_commit(&q_empty[qb]);
+            }
+            if (issued) {
+                mma_commit(&drain[0]);
+                drain_wait(&drain[0], 0, a.status);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 2) {
+        // ------------------------------------------------------------ O issuer
+        // apart from S, whose wait for the next K must not hold back a finished P and the V slot behind it
+        if (lane == 0) {
+            constexpr uint32_t kIdO = idesc_bf16(kCacheTile, 2 * RB) | (1u << 15) | (1u << 16);  // both MN-major
+            uint32_t t = 0, pv[NB] = {};
+            bool ok = true, issued = false;
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
+                return ok;
             };
             while (ok && walk.next(a, sg)) {
                 const int groups = (sg.nr + RB - 1) / RB, tiles = sg.tile1 - sg.tile0;
                 bool live[NB] = {};  // a group's O holds a product of this segment
-                int ahead = 0;       // tiles whose S is issued: KS beyond the one whose O is
-                for (int i = 0; ok && i < tiles; ++i) {
-                    while (ok && ahead < tiles && ahead <= i + KS) issue_s(ahead++, groups);
-                    if (!ok) break;
-                    const uint32_t e = 2 * (t + i) + 1;
+                for (int i = 0; ok && i < tiles; ++i, ++t) {
+                    const uint32_t e = 2 * t + 1;
                     const int slot = (int)(e % S::kStages);
                     if (!wait(&full[slot], (e / S::kStages) & 1)) break;
                     const uint32_t va = smem_u32(sm + slot * S::kTileBytes);
@@ -386,32 +416,64 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                         if (!wait(&p_full[nb], pv[nb]++ & 1)) break;
                         tc_fence_after();
                         issued = true;
-                        const uint32_t pa = smem_u32(sm + S::kPOff + nb * S::kPBytes);
+                        const uint32_t pa = smem_u32(sm + S::kPOff) + nb * S::kPStep;
                         for (int kk = 0; kk < ksteps; ++kk)
                             mma_bf16<kIdO>(tmem + (uint32_t)(S::kOCol + nb * 2 * RB), mn_desc(va + kk * 2048, D == 128 ? kAtom : 0),
                                            mn_desc(pa + kk * 2048, kAtom), live[nb] || kk > 0 ? 1u : 0u);
                         mma_commit(&pv_done[nb]);
                         live[nb] = live[nb] || ksteps > 0;
                     }
-                    if (!ok) break;
-                    mma_commit(&empty[slot]);
+                    if (ok) mma_commit(&empty[slot]);
                 }
-                t += tiles;
             }
             if (issued) {
-                mma_commit(drain);
-                drain_wait(drain, 0, a.status);
+                mma_commit(&drain[1]);
+                drain_wait(&drain[1], 0, a.status);
             }
+        }
+        __syncwarp();
+    } else if (warp == 3) {
+        // ------------------------------------------------------------ Q loader
+        // a segment's rows (zeros past them), K-major with the 128-byte swizzle
+        uint32_t seg = 0;
+        while (walk.next(a, sg)) {
+            const uint32_t qb = seg % S::kQBufs, use = seg / S::kQBufs;
+            if (use >= 1 && !warp_wait(&q_empty[qb], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) break;
+            ++seg;
+            const int64_t row0 = a.cu[sg.b];
+            const uint32_t to = smem_u32(sm + S::kQOff + qb * S::kQBytes);
+#pragma unroll 4
+            for (int x = lane; x < S::kQRows * (D / 8); x += 32) {
+                const int r = x / (D / 8), ch = x % (D / 8);
+                const int rr = r < sg.nr ? sg.r0 + r : sg.r0, i = rr / a.rep, h = sg.g * a.rep + rr % a.rep;
+                const char* from = a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                 to + (ch >> 3) * S::kQRows * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
+                             "l"(from), "r"(r < sg.nr ? 16 : 0)
+                             : "memory");
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_full[qb]);
         }
         __syncwarp();
     } else {
         // ------------------------------------------------------------- epilogue
-        const int nb = (warp - 2) >> 2, q = warp & 3, bar = 1 + nb;
+        const int nb = (warp - 4) >> 2, q = warp & 3, bar = 1 + nb;
         const int j = q * 32 + lane;                 // key of the tile; lane of S and O
         float* row_m = reinterpret_cast<float*>(sm + S::kRowOff) + nb * 2 * RB;  // m, log2 units
         float* row_f = row_m + RB;
-        uint8_t* pb = sm + S::kPOff + nb * S::kPBytes;
-        uint8_t* qb = sm + S::kQOff + nb * S::kQBytes;
+        uint8_t* pb = sm + S::kPOff;
+        // [4][RB], used when the P buffer is free
+        float* row_w = RB == 64 ? reinterpret_cast<float*>(pb + nb * S::kPStep)
+                                : reinterpret_cast<float*>(sm + S::kRedOff) + nb * 4 * RB;
+        // 16-byte chunk c of key k's P row
+        auto p_chunk = [&](int k, int c) {
+            if (RB == 64) return pb + nb * S::kPStep + (c >> 3) * kAtom + k * 128 + (((c & 7) ^ (k & 7)) << 4);
+            if (RB == 32) return pb + nb * S::kPStep + k * 128 + ((c ^ (k & 7)) << 4);
+            return pb + k * 128 + (((nb * (S::kPStep / 16) + c) ^ (k & 7)) << 4);
+        };
         const uint32_t lane_off = (uint32_t)(q * 32) << 16;
         const uint32_t t_o = tmem + lane_off + (uint32_t)(S::kOCol + nb * 2 * RB);
         constexpr int kCols = RB < 16 ? 8 : 16;  // columns of a tensor memory load
@@ -429,20 +491,6 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                 continue;
             }
             const int64_t row0 = a.cu[sg.b];
-            // Q of this group's rows (rows past nr are zero), K-major with the 128-byte swizzle
-            for (int x = j; x < RB * (D / 8); x += 128) {
-                const int r = x / (D / 8), ch = x % (D / 8);
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (r < nr) {
-                    const int rr = sg.r0 + base + r, i = rr / a.rep, h = sg.g * a.rep + rr % a.rep;
-                    v = *reinterpret_cast<const uint4*>(a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16);
-                }
-                *reinterpret_cast<uint4*>(qb + (ch >> 3) * S::kN * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v;
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            const bool any = KS == 1 || nb < sg.tile1 - sg.tile0;  // the group takes a tile
-            if (lane == 0 && any) mbar_arrive(&q_full[nb]);
             if (j < RB) row_m[j] = -INFINITY;
             float l[RB];
 #pragma unroll
@@ -504,7 +552,6 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                         alive = false;
                         break;
                     }
-                    float* row_w = reinterpret_cast<float*>(pb);  // [4][RB]: the P buffer is free
 #pragma unroll
                     for (int r = 0; r < RB; ++r) {
                         const float x = warp_max(z[r]);
@@ -543,7 +590,6 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                     l[r] += z[r];
                 }
                 if (step > 0) wait(&pv_done[nb], (step - 1) & 1);  // the P buffer is free
-                uint8_t* prow = pb + j * 128;
 #pragma unroll
                 for (int r = 0; r < RB; r += 8) {
                     uint4 h, lo;
@@ -551,10 +597,8 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                     h.y = pack_hi_lo(z[r + 2], z[r + 3], lo.y);
                     h.z = pack_hi_lo(z[r + 4], z[r + 5], lo.z);
                     h.w = pack_hi_lo(z[r + 6], z[r + 7], lo.w);
-                    const int ch = r / 8;
-                    *reinterpret_cast<uint4*>(prow + ((ch ^ (j & 7)) << 4)) = h;
-                    if (RB == 64) *reinterpret_cast<uint4*>(prow + kAtom + ((ch ^ (j & 7)) << 4)) = lo;
-                    else *reinterpret_cast<uint4*>(prow + (((ch + RB / 8) ^ (j & 7)) << 4)) = lo;
+                    *reinterpret_cast<uint4*>(p_chunk(j, r / 8)) = h;
+                    *reinterpret_cast<uint4*>(p_chunk(j, (r + RB) / 8)) = lo;
                 }
                 if ((KS == 2 || nb == 0) && (drafts || (keys & 15))) {
                     // V rows that must not reach the product: past the keys, and drafts that are not finite
@@ -591,27 +635,12 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                 if (lane == 0) mbar_arrive(&p_full[nb]);
                 live = live || keys > 0;
             }
-            if (!alive) {  // leave with the group
-                group_or(bar, true);
-                break;
-            }
             t += sg.tile1 - sg.tile0;
             // the segment's partial
             if (step > 0) wait(&pv_done[nb], (step - 1) & 1);
+            if (group_or(bar, !alive)) break;  // the group leaves together
             tc_fence_after();
-            float* row_w = reinterpret_cast<float*>(qb);  // [4][RB]: every S of the segment is done with Q
-            {
-                constexpr int kN = RB < 32 ? RB : 32;
-#pragma unroll
-                for (int r = 0; r < RB; r += kN) {
-                    const float x = reduce_scatter<kN>(l + r, lane);
-                    if (lane < kN) row_w[q * RB + r + lane] = x;
-                }
-            }
-            if (group_or(bar, !alive)) break;
             const int64_t part = ((cta + sg.group) * KS + (KS == 2 ? nb : 0)) * a.RB + base;
-            if (j < nr)
-                a.part_ml[part + j] = make_float2(row_m[j], (row_w[j] + row_w[RB + j]) + (row_w[2 * RB + j] + row_w[3 * RB + j]));
 #pragma unroll 1
             for (int r = 0; r < RB; r += kCols) {
                 if (r >= nr) break;
@@ -644,16 +673,26 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                             a.vn + (row0 + x) * a.ldn + (int64_t)sg.g * (D * 2) + j * 2));
                         for (int r = 0; r < nr; ++r) {
                             if (!sees_draft(a, row0, (sg.r0 + base + r) / a.rep, x)) continue;
-                            const __nv_bfloat16* ph = reinterpret_cast<const __nv_bfloat16*>(pb + x * 128 + (((r >> 3) ^ (x & 7)) << 4)) + (r & 7);
-                            const __nv_bfloat16* pl = reinterpret_cast<const __nv_bfloat16*>(
-                                RB == 64 ? pb + kAtom + x * 128 + (((r >> 3) ^ (x & 7)) << 4)
-                                         : pb + x * 128 + ((((r + RB) >> 3) ^ (x & 7)) << 4)) + (r & 7);
+                            const __nv_bfloat16* ph = reinterpret_cast<const __nv_bfloat16*>(p_chunk(x, r >> 3)) + (r & 7);
+                            const __nv_bfloat16* pl = reinterpret_cast<const __nv_bfloat16*>(p_chunk(x, (r + RB) >> 3)) + (r & 7);
                             a.part_o[(part + r) * D + j] += (__bfloat162float(*ph) + __bfloat162float(*pl)) * v;
                         }
                     }
                 }
             }
-            group_sync(bar);  // row_w (in Q), row_m and P are free for the next segment
+            if (RB == 64) group_sync(bar);  // P is read
+            {
+                constexpr int kN = RB < 32 ? RB : 32;
+#pragma unroll
+                for (int r = 0; r < RB; r += kN) {
+                    const float x = reduce_scatter<kN>(l + r, lane);
+                    if (lane < kN) row_w[q * RB + r + lane] = x;
+                }
+            }
+            group_sync(bar);
+            if (j < nr)
+                a.part_ml[part + j] = make_float2(row_m[j], (row_w[j] + row_w[RB + j]) + (row_w[2 * RB + j] + row_w[3 * RB + j]));
+            group_sync(bar);  // row_w, row_m and P are free for the next segment
         }
     }
     tc_fence_before();
@@ -766,7 +805,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
     tc_fence_before();
     const int64_t cta = blockIdx.x, G = gridDim.x;
     PlanScratch* sc = reinterpret_cast<PlanScratch*>(sm);  // in the ring, unused until the barrier below
-    Place* place = reinterpret_cast<Place*>(sm + 1024);
+    Place* place = reinterpret_cast<Place*>(sm + 1088);
     const PlanTotals tot = plan_block(a, sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
         const int64_t it = unit_begin(cta, all.items, G);
         if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) *place = x;
