@@ -16,10 +16,10 @@
 // (every partial is relative to it).
 //
 // One persistent CTA per SM over the units of cache.cuh.
-//   warp 0     TMA producer: K and V tiles in turn through one ring, a box a page (a lane each)
+//   warps 0, 3 TMA producers of the K and of the V tiles, which take turns in one ring, a box a page
+//              (a lane each); warp 3 also loads the rows' Q, up to 64 rows a segment ahead
 //   warp 1     issues S, as far ahead as K tiles and S buffers allow
 //   warp 2     issues O, as soon as a P is written
-//   warp 3     loads the rows' Q, up to 64 rows a segment ahead
 //   warps 4-11 two epilogue groups of 4 warps, each with its S (double-buffered) and O in tensor
 //              memory and its P buffer; up to 64 rows they take the tiles in turn, more rows are
 //              shared out between them
@@ -220,6 +220,64 @@ struct TcMaps {
     CUtensorMap k, v, kn, vn;
 };
 
+// The page table of a sequence as a producer warp reads it: 32 entries at a time, a lane each, the
+// next 32 already on their way (looked up tile by tile, the table's latency was two thirds of a
+// tile's time).
+struct PageWindow {
+    const int32_t* row;
+    int last, base, cur, nxt;  // last page in use; page index of lane 0; entries
+    __device__ __forceinline__ int load(int i) const { return i <= last ? row[i] : 0; }
+    __device__ __forceinline__ void open(const CacheAttnArgs& a, const SeqShape& s, int b, int tile, int lane) {
+        row = a.c.table + (int64_t)b * a.c.ld_table;
+        last = (s.len - 1) >> a.c.shift;  // -1 without slots
+        base = (int)((int64_t)tile * kCacheTile >> a.c.shift);
+        cur = load(base + lane);
+        nxt = load(base + 32 + lane);
+    }
+    // entry of page index i; first is the smallest of the warp's
+    __device__ __forceinline__ int get(int first, int i, int lane) {
+        while (first >= base + 32) {
+            base += 32;
+            cur = nxt;
+            nxt = load(base + 32 + lane);
+        }
+        const int x = __shfl_sync(0xffffffffu, cur, (i - base) & 31), y = __shfl_sync(0xffffffffu, nxt, (i - base) & 31);
+        return i - base < 32 ? x : y;
+    }
+};
+
+// A producer warp's copies of one tile: a lane a box of box_rows slots (or one of new_rows drafts).
+template <int D>
+__device__ __forceinline__ void load_tile(const CacheAttnArgs& a, const CUtensorMap* pages, const CUtensorMap* rows,
+                                          PageWindow& win, const SeqShape& s, int b, int g, int tile, int box_rows,
+                                          int new_rows, uint8_t* to, uint64_t* bar, int lane) {
+    const int keys = tile_keys(a, s, tile);
+    if (tile == s.nt - 1) {
+        if (lane == 0) {
+            mbar_expect_tx(bar, keys > 0 ? (uint32_t)(new_rows * 2 * D) : 0u);
+            if (keys > 0)
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x) tma_load_3d(to + x * kAtom, rows, x * 64, g, a.cu[b], bar);
+        }
+    } else {
+        const int boxes = (keys + box_rows - 1) / box_rows, slot = tile * kCacheTile + lane * box_rows;
+        int page = win.get(tile * kCacheTile >> a.c.shift, slot >> a.c.shift, lane);
+        if (lane == 0) mbar_expect_tx(bar, (uint32_t)(boxes * box_rows * 2 * D));
+        __syncwarp();
+        if (lane < boxes) {
+            if (page < 0 || page >= a.c.n_pages) {
+                report(a.status, ESTP_ERR_INVALID_ARG);
+                page = a.c.n_pages > 0 ? (int)a.c.n_pages : 1;  // past the pool: reads as zero
+            }
+            to += lane * box_rows * 128;
+#pragma unroll
+            for (int x = 0; x < D / 64; ++x)
+                tma_load_4d(to + x * kAtom, pages, x * 64, slot & ((1 << a.c.shift) - 1), g, page, bar);
+        }
+    }
+    __syncwarp();
+}
+
 template <int D, int RB, int KS>
 __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
     cache_fwd_tc_kernel(const __grid_constant__ TcMaps tm, const CacheAttnArgs a, const int box_rows, const int new_rows) {
@@ -238,6 +296,7 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
     uint64_t* drain = pv_done + NB;                                 // [2] each issuer's MMAs done
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::kMiscOff);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 4);
+    volatile int* issued_tiles = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 8);  // [2] K, V
     volatile uint32_t* poison = reinterpret_cast<volatile uint32_t*>(sm + S::kMiscOff + 16);  // [2][4] drafts with V not finite
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -292,58 +351,60 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
     __syncthreads();  // the ring is the copies' from here
     Segment sg;
 
-    if (warp == 0) {
-        // ------------------------------------------------------------ producer
-        if (lane < 4) {
-            const CUtensorMap* m[4] = {&tm.k, &tm.v, &tm.kn, &tm.vn};
-            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m[lane])) : "memory");
-        }
-        uint32_t e = 0;  // ring entries issued
+    if (warp == 0 || warp == 3) {
+        // ------------------------------------------------------------ producers
+        // warp 0 the K tiles (even ring entries), warp 3 the V tiles (odd ones) and the rows' Q
+        const int kv = warp == 3;
+        if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(
+                          kv ? (lane ? &tm.vn : &tm.v) : (lane ? &tm.kn : &tm.k))) : "memory");
+        uint32_t t = 0, q_seg = 0;  // tiles issued; segments whose Q is loaded
         bool ok = true;
-        while (ok && walk.next(a, sg)) {
-            int64_t page = -1;
-            int at = 0;
-            auto look = [&](int tile) {  // this lane's box of a cached tile
-                if (tile >= sg.s.nt - 1) return;
-                const int slot = tile * kCacheTile + lane * box_rows;
-                if (lane * box_rows < kCacheTile && slot < sg.s.len) {
-                    page = a.c.page_of(sg.b, slot, a.status);
-                    if (page < 0) page = a.c.n_pages > 0 ? a.c.n_pages : 1;  // past the pool: reads as zero
-                    at = slot & ((1 << a.c.shift) - 1);
-                }
-            };
-            look(sg.tile0);
-            for (int tile = sg.tile0; ok && tile < sg.tile1; ++tile) {
-                const bool drafts = tile == sg.s.nt - 1;
-                const int keys = tile_keys(a, sg.s, tile);
-                const int rows = drafts ? new_rows : box_rows;
-                const int boxes = drafts ? (keys > 0 ? 1 : 0) : (keys + box_rows - 1) / box_rows;
-                for (int kv = 0; kv < 2; ++kv, ++e) {
-                    const int slot = (int)(e % S::kStages);
-                    const uint32_t use = e / S::kStages;
-                    if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
-                        ok = false;
-                        break;
-                    }
-                    if (lane == 0) mbar_expect_tx(&full[slot], (uint32_t)(boxes * rows * 128 * S::kAtoms));
-                    __syncwarp();
-                    if (lane < boxes) {
-                        uint8_t* to = sm + slot * S::kTileBytes + lane * rows * 128;
-#pragma unroll
-                        for (int x = 0; x < S::kAtoms; ++x) {
-                            if (drafts)
-                                tma_load_3d(to + x * kAtom, kv ? &tm.vn : &tm.kn, x * 64, sg.g, a.cu[sg.b], &full[slot]);
-                            else
-                                tma_load_4d(to + x * kAtom, kv ? &tm.v : &tm.k, x * 64, at, sg.g, (int)page, &full[slot]);
-                        }
-                    }
-                }
-                look(tile + 1);
+        Walk q_walk = walk;
+        Segment qs;
+        // Q of the next segment (zeros past its rows), K-major with the 128-byte swizzle
+        auto load_q = [&]() {
+            if (!q_walk.next(a, qs)) return;
+            const uint32_t qb = q_seg % S::kQBufs, use = q_seg / S::kQBufs;
+            if (use >= 1 && !warp_wait(&q_empty[qb], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
+                ok = false;
+                return;
             }
+            ++q_seg;
+            const int64_t row0 = a.cu[qs.b];
+            const uint32_t to = smem_u32(sm + S::kQOff + qb * S::kQBytes);
+#pragma unroll 4
+            for (int x = lane; x < S::kQRows * (D / 8); x += 32) {
+                const int r = x / (D / 8), ch = x % (D / 8);
+                const int rr = r < qs.nr ? qs.r0 + r : qs.r0, i = rr / a.rep, h = qs.g * a.rep + rr % a.rep;
+                const char* from = a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                 to + (ch >> 3) * S::kQRows * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
+                             "l"(from), "r"(r < qs.nr ? 16 : 0)
+                             : "memory");
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_full[qb]);
+        };
+        if (kv) load_q();
+        PageWindow win;
+        while (ok && walk.next(a, sg)) {
+            win.open(a, sg.s, sg.b, sg.tile0, lane);
+            for (int tile = sg.tile0; tile < sg.tile1; ++tile, ++t) {
+                const uint32_t e = 2 * t + kv, use = e / S::kStages;
+                const int slot = (int)(e % S::kStages);
+                if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
+                    ok = false;
+                    break;
+                }
+                load_tile<D>(a, kv ? &tm.v : &tm.k, kv ? &tm.vn : &tm.kn, win, sg.s, sg.b, sg.g, tile, box_rows, new_rows,
+                             sm + slot * S::kTileBytes, &full[slot], lane);
+                if (kv && S::kQBufs == 2 && tile == sg.tile0) load_q();  // a failure shows at the next wait
+            }
+            if (ok && kv && S::kQBufs == 1) load_q();
         }
-        if (lane == 0)  // every copy has landed before the CTA can exit
-            for (uint32_t i = 0; i < (uint32_t)S::kStages && i < e; ++i)
-                drain_wait(&full[(e - 1 - i) % S::kStages], ((e - 1 - i) / S::kStages) & 1, a.status);
+        if (lane == 0) issued_tiles[kv] = (int)t;
         __syncwarp();
     } else if (warp == 1) {
         // ------------------------------------------------------------ S issuer
@@ -430,32 +491,6 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                 mma_commit(&drain[1]);
                 drain_wait(&drain[1], 0, a.status);
             }
-        }
-        __syncwarp();
-    } else if (warp == 3) {
-        // ------------------------------------------------------------ Q loader
-        // a segment's rows (zeros past them), K-major with the 128-byte swizzle
-        uint32_t seg = 0;
-        while (walk.next(a, sg)) {
-            const uint32_t qb = seg % S::kQBufs, use = seg / S::kQBufs;
-            if (use >= 1 && !warp_wait(&q_empty[qb], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) break;
-            ++seg;
-            const int64_t row0 = a.cu[sg.b];
-            const uint32_t to = smem_u32(sm + S::kQOff + qb * S::kQBytes);
-#pragma unroll 4
-            for (int x = lane; x < S::kQRows * (D / 8); x += 32) {
-                const int r = x / (D / 8), ch = x % (D / 8);
-                const int rr = r < sg.nr ? sg.r0 + r : sg.r0, i = rr / a.rep, h = sg.g * a.rep + rr % a.rep;
-                const char* from = a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                 to + (ch >> 3) * S::kQRows * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
-                             "l"(from), "r"(r < sg.nr ? 16 : 0)
-                             : "memory");
-            }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&q_full[qb]);
         }
         __syncwarp();
     } else {
@@ -698,6 +733,18 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (threadIdx.x == 0 && *abort_flag) {
+        // a CTA that gave up: the last copy into every slot of the ring lands before it exits (all others
+        // have been waited for by the issuers)
+        const int n = 2 * max(issued_tiles[0], issued_tiles[1]);
+        uint32_t seen = 0;
+        for (int e = n - 1; e >= 0 && e >= n - 2 * S::kStages; --e) {
+            const int slot = e % S::kStages;
+            if (e / 2 >= issued_tiles[e & 1] || (seen >> slot & 1)) continue;
+            seen |= 1u << slot;
+            drain_wait(&full[slot], (e / S::kStages) & 1, a.status);
+        }
+    }
     if (warp == 1) {
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmem));
@@ -826,36 +873,19 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
         // ------------------------------------------------------------ producer
         uint32_t e = 0;
         bool ok = true;
+        PageWindow win;
         while (ok && w.next(a)) {
             for (int r0 = 0; ok && r0 < w.s.n * a.rep; r0 += kWRows) {
+                win.open(a, w.s, w.b, w.tile0, lane);
                 for (int tile = w.tile0; tile < w.tile1; ++tile, ++e) {
-                    const bool drafts = tile == w.s.nt - 1;
-                    const int keys = tile_keys(a, w.s, tile), rows = drafts ? new_rows : box_rows;
-                    const int boxes = drafts ? (keys > 0 ? 1 : 0) : (keys + box_rows - 1) / box_rows;
-                    int64_t page = 0;
-                    int at = 0;
-                    if (!drafts && lane < boxes) {
-                        const int slot = tile * kCacheTile + lane * box_rows;
-                        page = a.c.page_of(w.b, slot, a.status);
-                        if (page < 0) page = a.c.n_pages > 0 ? a.c.n_pages : 1;
-                        at = slot & ((1 << a.c.shift) - 1);
-                    }
                     const int slot = (int)(e % kWStages);
                     const uint32_t use = e / kWStages;
                     if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
                         ok = false;
                         break;
                     }
-                    if (lane == 0) mbar_expect_tx(&full[slot], (uint32_t)(boxes * rows * 128 * S::kAtoms));
-                    __syncwarp();
-                    if (lane < boxes) {
-                        uint8_t* to = sm + slot * S::kTileBytes + lane * rows * 128;
-#pragma unroll
-                        for (int x = 0; x < S::kAtoms; ++x) {
-                            if (drafts) tma_load_3d(to + x * kAtom, &tm.kn, x * 64, w.g, a.cu[w.b], &full[slot]);
-                            else tma_load_4d(to + x * kAtom, &tm.k, x * 64, at, w.g, (int)page, &full[slot]);
-                        }
-                    }
+                    load_tile<D>(a, &tm.k, &tm.kn, win, w.s, w.b, w.g, tile, box_rows, new_rows, sm + slot * S::kTileBytes,
+                                 &full[slot], lane);
                 }
             }
         }
