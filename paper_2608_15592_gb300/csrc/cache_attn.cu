@@ -98,7 +98,7 @@ template <class T, int D>
 __device__ __forceinline__ void dots(const float (*q)[D], const char* k, float* z) {
 #pragma unroll
     for (int r = 0; r < kRows; ++r) z[r] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int c = 0; c < D / Unit<T>::n; ++c) {
         float kv[Unit<T>::n];
         Unit<T>::get(k + c * 16, kv);
@@ -162,13 +162,20 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
             if (kr.k != nullptr) dots<T, D>(q, kr.k, z);
             vrow[t] = kr.v;
             unsigned hidden = 0;  // rows that do not see this key
+            if (drafts) {
+                const Seers seers = seers_of(a, row0, kr.k != nullptr ? s.n : 0, t);
+                RowDraft row(r0, a.rep);
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                if (kr.k == nullptr || (drafts && !(r < nr && sees_draft(a, row0, (r0 + r) / a.rep, t)))) {
-                    hidden |= 1u << r;
-                    z[r] = -INFINITY;
+                for (int r = 0; r < kRows; ++r) {
+                    if (r >= nr || !seers.has(row.i)) hidden |= 1u << r;
+                    row.next(a.rep);
                 }
+            } else if (kr.k == nullptr) {
+                hidden = (1u << kRows) - 1;
             }
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+                if (hidden >> r & 1) z[r] = -INFINITY;
             if (a.store)
                 for (int r = 0; r < nr; ++r) a.score[(u * kRows + r) * kCacheTile + t] = z[r];
 #pragma unroll
@@ -187,17 +194,30 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
                 const float e = ex2(fmaf(z[r], a.scale_log2, mn == -INFINITY ? 0.f : -mn));
                 l[r] = fmaf(l[r], f, hidden >> r & 1 ? 0.f : e);
                 o[r] *= f;
-                p[r][t] = hidden >> r & 1 ? -1.f : e;  // no probability: the key adds nothing, whatever its V holds
+                p[r][t] = hidden >> r & 1 ? (drafts ? -1.f : 0.f) : e;  // -1: no probability, the draft is left out
             }
             __syncthreads();
-            for (int j = half * kKeys; j < (half + 1) * kKeys; ++j) {
-                const char* vr = vrow[j];
-                if (vr == nullptr) continue;
-                const float v = Unit<T>::one(vr + col * sizeof(T));
+            constexpr int kBatch = 16;  // V rows in flight
+            for (int j0 = half * kKeys; j0 < (half + 1) * kKeys; j0 += kBatch) {
+                float v[kBatch];
 #pragma unroll
-                for (int r = 0; r < kRows; ++r) {
-                    const float e = p[r][j];
-                    if (!(e < 0.f)) o[r] = fmaf(e, v, o[r]);
+                for (int k = 0; k < kBatch; ++k) {
+                    const char* vr = vrow[j0 + k];
+                    v[k] = vr != nullptr ? Unit<T>::one(vr + col * sizeof(T)) : 0.f;
+                }
+                if (!drafts) {
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+                        for (int r = 0; r < kRows; ++r) o[r] = fmaf(p[r][j0 + k], v[k], o[r]);
+                } else {  // what a hidden draft's V holds adds nothing, 0 x NaN included
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+                        for (int r = 0; r < kRows; ++r) {
+                            const float e = p[r][j0 + k];
+                            if (!(e < 0.f)) o[r] = fmaf(e, v[k], o[r]);
+                        }
                 }
             }
         }
@@ -234,24 +254,22 @@ __device__ __forceinline__ Pieces pieces_of(const CacheAttnArgs& a, const Place&
     return Pieces{(c0 + at.group0 + grp) * a.KS * a.RB + r % a.RB, (int)(c1 - c0 + 1) * a.KS};
 }
 
+// Joins (M, L) with another running maximum and sum.  Unfused products: two lanes that join each
+// other's get the same bits.
+__device__ __forceinline__ void merge_ml(float& M, float& L, float2 x) {
+    const float mn = fmaxf(M, x.x);
+    // -inf on both sides: nothing was summed, or NaN, which stays
+    if (mn != -INFINITY) L = __fadd_rn(__fmul_rn(L, ex2(M - mn)), __fmul_rn(x.y, ex2(x.x - mn)));
+    else L += x.y;
+    M = mn;
+}
+
 // Warp-wide: the row's maximum and sum over its pieces.
 __device__ __forceinline__ float2 merged_ml(const CacheAttnArgs& a, const Pieces& w, int lane) {
     float M = -INFINITY, L = 0.f;
-    for (int c = lane; c < w.n; c += 32) {
-        const float2 x = a.part_ml[w.first + (int64_t)c * a.RB];
-        const float mn = fmaxf(M, x.x);
-        if (mn != -INFINITY) L = fmaf(L, ex2(M - mn), x.y * ex2(x.x - mn));
-        else L += x.y;  // NaN stays
-        M = mn;
-    }
-    for (int o = 16; o > 0; o >>= 1) {
-        const float m2 = __shfl_xor_sync(0xffffffffu, M, o), l2 = __shfl_xor_sync(0xffffffffu, L, o);
-        const float mn = fmaxf(M, m2);
-        // unfused products: both lanes of a pair get the same bits
-        if (mn != -INFINITY) L = __fadd_rn(__fmul_rn(L, ex2(M - mn)), __fmul_rn(l2, ex2(m2 - mn)));
-        else L += l2;
-        M = mn;
-    }
+    for (int c = lane; c < w.n; c += 32) merge_ml(M, L, a.part_ml[w.first + (int64_t)c * a.RB]);
+    for (int o = 16; o > 0; o >>= 1)
+        merge_ml(M, L, make_float2(__shfl_xor_sync(0xffffffffu, M, o), __shfl_xor_sync(0xffffffffu, L, o)));
     return make_float2(M, L);
 }
 
@@ -274,50 +292,42 @@ __device__ __forceinline__ void for_items(const CacheAttnArgs& a, Place at, int6
     }
 }
 
-// Adds the weight of 4 keys to slots that share a page, or writes it for 4 drafts; n of them exist.
-__device__ __forceinline__ void add4(float* p, float4 s, int n) {
-    if (n >= 4) {
-        float4 w = *reinterpret_cast<const float4*>(p);
-        w.x += s.x;
-        w.y += s.y;
-        w.z += s.z;
-        w.w += s.w;
-        *reinterpret_cast<float4*>(p) = w;
-    } else {
-        p[0] += s.x;
-        if (n > 1) p[1] += s.y;
-        if (n > 2) p[2] += s.z;
-    }
+// (-M, c / L) of a row: a row without keys, or of factor 0, has a factor of 0 and is left out.
+__device__ __forceinline__ float2 weight_factor(const CacheAttnArgs& a, float2 x, int64_t row) {
+    const float cw = a.row_weight != nullptr ? a.row_weight[row] : 1.f;
+    const bool none = cw == 0.f || (x.x == -INFINITY && x.y == 0.f);
+    return none ? make_float2(0.f, 0.f) : make_float2(x.x == -INFINITY ? 0.f : -x.x, cw / x.y);
 }
 
-// Merges the partials: o and lse, a warp a (row, head), both cut evenly over the grid.  With kept
-// scores it adds the weights too, a warp a tile, a lane 4 keys: the items are cut evenly as well.
-// Without, it leaves (-M, c / L) of every row for the kernel that forms the scores again.
+// The first a.row_blocks blocks merge the partials: o and lse, a warp a (row, head), cut evenly over
+// them; without kept scores they leave (-M, c / L) of every row for the kernel that forms the scores
+// again.  With kept scores the other blocks add the weights, the (b, KV head, tile) items cut evenly
+// over them: a warp a tile, a lane 4 keys.
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnArgs a) {
     __shared__ PlanScratch sc;
-    __shared__ Place place_row, place_item;
+    __shared__ Place place;
     __shared__ float2 ml[kCacheMaxStored];  // (-M, c / L) of every row of (b, g)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    const int64_t c = blockIdx.x, G = gridDim.x;
+    const bool for_rows = (int)blockIdx.x < a.row_blocks;
+    const int64_t c = for_rows ? blockIdx.x : blockIdx.x - a.row_blocks;
+    const int64_t G = for_rows ? a.row_blocks : gridDim.x - a.row_blocks;
     const int64_t x0 = unit_begin(c, a.n_rows * a.Hq, G), x1 = unit_begin(c + 1, a.n_rows * a.Hq, G);
     const PlanTotals tot = plan_block(a, &sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
-        const int64_t y = (int64_t)a.cu[x.b] * a.Hq, it = unit_begin(c, all.items, G);
-        if (x0 >= y && x0 < y + (int64_t)s.n * a.Hq) place_row = x;
-        if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) place_item = x;
+        if (for_rows) {
+            const int64_t y = (int64_t)a.cu[x.b] * a.Hq;
+            if (x0 >= y && x0 < y + (int64_t)s.n * a.Hq) place = x;
+        } else {
+            const int64_t it = unit_begin(c, all.items, G);
+            if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) place = x;
+        }
     });
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the partials are complete
     if (!tot.ok) return;
-
-    // (-M, c / L): a row without keys, or of factor 0, has a factor of 0 and is left out
-    auto factor = [&](float2 x, int64_t row) {
-        const float cw = a.row_weight != nullptr ? a.row_weight[row] : 1.f;
-        const bool none = cw == 0.f || (x.x == -INFINITY && x.y == 0.f);
-        return none ? make_float2(0.f, 0.f) : make_float2(x.x == -INFINITY ? 0.f : -x.x, cw / x.y);
-    };
-    if (x0 < x1) {
-        Place at = place_row;
+    if (for_rows) {
+        if (x0 >= x1) return;
+        Place at = place;
         SeqShape s = seq_shape(a, at.b);
         for (int64_t x = x0 + warp; x < x1; x += kThreads / 32) {
             while (x >= (int64_t)a.cu[at.b + 1] * a.Hq) {
@@ -349,20 +359,31 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
             if (lane == 0) {
                 if (a.lse != nullptr)
                     a.lse[(int64_t)h * a.n_rows + row] = all.y == 0.f ? -INFINITY : fmaf(all.x, kLn2, logf(all.y));
-                if (a.factor != nullptr) a.factor[row * a.Hq + h] = factor(all, row);
+                if (a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, all, row);
             }
         }
+        return;
     }
-    if (!a.store) return;
-
-    for_items(a, place_item, unit_begin(c, tot.items, G), unit_begin(c + 1, tot.items, G),
+    for_items(a, place, unit_begin(c, tot.items, G), unit_begin(c + 1, tot.items, G),
               [&](const Place& at, const SeqShape& s, int g, int tile0, int tile1) {
         const int64_t row0 = a.cu[at.b];
         const int R = s.n * a.rep;
         __syncthreads();
-        for (int r = warp; r < R; r += kThreads / 32) {
-            const float2 x = merged_ml(a, pieces_of(a, at, s, g, r, tot.units), lane);
-            if (lane == 0) ml[r] = factor(x, row0 + r / a.rep);
+        for (int rw = warp * 4; rw < R; rw += kThreads / 8) {  // 8 lanes a row
+            const int r = rw + (lane >> 3);
+            float M = -INFINITY, L = 0.f;
+            if (r < R) {
+                const Pieces w = pieces_of(a, at, s, g, r, tot.units);
+                for (int p = lane & 7; p < w.n; p += 8) {
+                    const float2 x = a.part_ml[w.first + (int64_t)p * a.RB];
+                    merge_ml(M, L, x);
+                }
+            }
+            for (int o = 4; o > 0; o >>= 1) {
+                const float2 x = make_float2(__shfl_xor_sync(0xffffffffu, M, o), __shfl_xor_sync(0xffffffffu, L, o));
+                merge_ml(M, L, x);
+            }
+            if (r < R && (lane & 7) == 0) ml[r] = weight_factor(a, make_float2(M, L), row0 + r / a.rep);
         }
         __syncthreads();
         for (int tile = tile0 + warp; tile < tile1; tile += kThreads / 32) {
@@ -371,11 +392,13 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
             const int n = (drafts ? (a.kn != nullptr ? s.n : 0) : s.len - tile * kCacheTile) - lane * 4;
             if (n <= 0) continue;
             float* to = nullptr;
+            float4 had = make_float4(0.f, 0.f, 0.f, 0.f);
             if (!drafts) {
                 const int slot = tile * kCacheTile + lane * 4;  // 4 slots of one page
                 const int64_t page = a.c.page_of(at.b, slot, a.status);
                 if (page < 0) continue;
                 to = a.c.weight + a.c.meta(page, slot, g);
+                if (n >= 4) had = *reinterpret_cast<const float4*>(to);
             }
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int k = 0; k < s.nrb; ++k) {
@@ -397,14 +420,18 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
                     }
                 }
             }
-            if (!drafts) {
-                add4(to, sum, n);
-            } else {
+            if (drafts) {
                 float* w = a.w_new + (row0 + lane * 4) * a.c.Hkv + g;
                 w[0] = sum.x;
                 if (n > 1) w[a.c.Hkv] = sum.y;
                 if (n > 2) w[2 * a.c.Hkv] = sum.z;
                 if (n > 3) w[3 * a.c.Hkv] = sum.w;
+            } else if (n >= 4) {
+                *reinterpret_cast<float4*>(to) = make_float4(had.x + sum.x, had.y + sum.y, had.z + sum.z, had.w + sum.w);
+            } else {
+                to[0] += sum.x;
+                if (n > 1) to[1] += sum.y;
+                if (n > 2) to[2] += sum.z;
             }
         }
     });
@@ -433,6 +460,8 @@ __global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnA
             const bool drafts = tile == s.nt - 1;
             if (drafts ? a.w_new == nullptr : !a.accumulate) continue;
             const KeyRow kr = key_row(a, s, at.b, g, tile, t, D * (int)sizeof(T));
+            Seers seers{{0, 0}};
+            if (drafts) seers = seers_of(a, row0, kr.k != nullptr ? s.n : 0, t);
             float sum = 0.f;
             for (int r0 = 0; r0 < R; r0 += kRows) {
                 const int nr = min(kRows, R - r0);
@@ -445,7 +474,7 @@ __global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnA
                 dots<T, D>(q, kr.k, z);
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
-                    if (r >= nr || (drafts && !sees_draft(a, row0, (r0 + r) / a.rep, t))) continue;
+                    if (r >= nr || (drafts && !seers.has((r0 + r) / a.rep))) continue;
                     const float2 f = ml[r];
                     if (f.y != 0.f) sum = fmaf(ex2(fmaf(z[r], a.scale_log2, f.x)), f.y, sum);
                 }
@@ -513,7 +542,12 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
         e = cudaGetLastError();
         if (e != cudaSuccess) return cuda_fail(e, "cache attention launch");
     }
-    e = launch_dependent(cache_finish_kernel<T, D>, ctx->num_sms * 8, kThreads, 0, a, st);
+    // a warp a (row, head) up to 4 blocks an SM; the items of kept scores over up to 12 more
+    const int64_t row_blocks = (a.n_rows * a.Hq + kThreads / 32 - 1) / (kThreads / 32), some = 4 * ctx->num_sms;
+    a.row_blocks = (int)(row_blocks < some ? row_blocks : some);
+    const int64_t items = (int64_t)a.c.Hkv * (a.n_slots / kCacheTile + 2 * (int64_t)a.B), many = 12 * ctx->num_sms;
+    const int item_blocks = a.store ? (int)(items < many ? items : many) : 0;
+    e = launch_dependent(cache_finish_kernel<T, D>, a.row_blocks + item_blocks, kThreads, 0, a, st);
     if (e != cudaSuccess) return cuda_fail(e, "cache attention finish launch");
     if (!again) return ESTP_OK;
     if constexpr (kTc) {

@@ -549,21 +549,17 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&s_empty[2 * nb + buf]);
-                if (keys < kCacheTile) {
-                    if (!drafts) {
-                        if (j >= keys) {
+                if (drafts) {
+                    const Seers seers = seers_of(a, row0, keys, j);
+                    RowDraft at(sg.r0 + base, a.rep);
 #pragma unroll
-                            for (int r = 0; r < RB; ++r) z[r] = -INFINITY;
-                        }
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < RB; ++r)
-                            if (j >= keys || r >= nr || !sees_draft(a, row0, (sg.r0 + base + r) / a.rep, j)) z[r] = -INFINITY;
+                    for (int r = 0; r < RB; ++r) {
+                        if (r >= nr || !seers.has(at.i)) z[r] = -INFINITY;
+                        at.next(a.rep);
                     }
-                } else if (drafts) {
+                } else if (j >= keys) {
 #pragma unroll
-                    for (int r = 0; r < RB; ++r)
-                        if (r >= nr || !sees_draft(a, row0, (sg.r0 + base + r) / a.rep, j)) z[r] = -INFINITY;
+                    for (int r = 0; r < RB; ++r) z[r] = -INFINITY;
                 }
                 if (a.store && alive) {
                     float* to = a.score + ((walk.u - (sg.tile1 - tile)) * a.RB + base) * kCacheTile + j;
@@ -704,10 +700,11 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                 if (D == 128 || q < 2) {
                     for (int x = 0; x < sg.s.n; ++x) {
                         if (!(odd_drafts[x >> 5] >> (x & 31) & 1)) continue;
+                        const Seers seers = seers_of(a, row0, sg.s.n, x);
                         const float v = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(
                             a.vn + (row0 + x) * a.ldn + (int64_t)sg.g * (D * 2) + j * 2));
                         for (int r = 0; r < nr; ++r) {
-                            if (!sees_draft(a, row0, (sg.r0 + base + r) / a.rep, x)) continue;
+                            if (!seers.has((sg.r0 + base + r) / a.rep)) continue;
                             const __nv_bfloat16* ph = reinterpret_cast<const __nv_bfloat16*>(p_chunk(x, r >> 3)) + (r & 7);
                             const __nv_bfloat16* pl = reinterpret_cast<const __nv_bfloat16*>(p_chunk(x, (r + RB) >> 3)) + (r & 7);
                             a.part_o[(part + r) * D + j] += (__bfloat162float(*ph) + __bfloat162float(*pl)) * v;
@@ -984,6 +981,8 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                         }
                     }
                     float sum[2] = {0.f, 0.f};
+                    Seers seers{{0, 0}};
+                    if (drafts) seers = seers_of(a, row0, keys, j);
                     for (int k = gr; k < blocks; k += 2, ++step) {
                         const uint32_t buf = step % kWBufs;
                         if (alive)
@@ -1007,12 +1006,13 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                                     sum[1] = f.w != 0.f ? fmaf(e1, f.w, sum[1]) : sum[1];
                                 }
                             } else {
+                                RowDraft at(r0 + k * kWBlock + c, a.rep);
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) {
-                                    const int r = k * kWBlock + c + i;
-                                    const float2 f = fs[r];
-                                    if (f.y != 0.f && j < keys && sees_draft(a, row0, (r0 + r) / a.rep, j))
-                                        sum[0] = fmaf(ex2(fmaf(z[i], a.scale_log2, f.x)), f.y, sum[0]);
+                                    const float2 f = fs[k * kWBlock + c + i];
+                                    const float e = ex2(fmaf(z[i], a.scale_log2, f.x));
+                                    if (f.y != 0.f && seers.has(at.i)) sum[0] = fmaf(e, f.y, sum[0]);
+                                    at.next(a.rep);
                                 }
                             }
                         }

@@ -179,14 +179,26 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const EvictArgs a)
     const int run = ((n + C - 1) / C + 31) / 32 * 32;
     const int lo = min(n, rank * run), hi = min(n, lo + run);
     auto form_key = [&](int slot) -> uint32_t {
-        const int64_t page = a.c.page_of(b, slot, a.status);
-        if (page < 0) return 0u;
-        const int64_t m = a.c.meta(page, slot, g);
-        const int pos = a.c.position[m];
-        const float w = a.c.weight[m];
-        return pos < a.sinks || pos >= seen - a.recent ? 0xffffffffu : weight_key(w);
+        const int page = a.c.table[(int64_t)b * a.c.ld_table + (slot >> a.c.shift)];
+        const bool there = page >= 0 && page < a.c.n_pages;
+        if (!there) report(a.status, ESTP_ERR_INVALID_ARG);
+        const int64_t m = a.c.meta(there ? page : 0, slot, g);
+        const int pos = there ? a.c.position[m] : 0;
+        const float w = there ? a.c.weight[m] : 0.f;
+        return !there ? 0u : pos < a.sinks || pos >= seen - a.recent ? 0xffffffffu : weight_key(w);
     };
-    for (int s = lo + t; s < hi && s - lo < a.key_cap; s += kEvictThreads) keys[s - lo] = form_key(s);
+    {
+        constexpr int kBatch = 4;  // slots a thread has in flight
+        const int top = min(hi, lo + a.key_cap);
+        for (int s0 = lo + t; s0 < top; s0 += kBatch * kEvictThreads) {
+            uint32_t k[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) k[i] = s0 + i * kEvictThreads < top ? form_key(s0 + i * kEvictThreads) : 0u;
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (s0 + i * kEvictThreads < top) keys[s0 + i * kEvictThreads - lo] = k[i];
+        }
+    }
     __syncthreads();
     auto key = [&](int slot) { return slot - lo < a.key_cap ? keys[slot - lo] : form_key(slot); };
 
@@ -310,20 +322,45 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const EvictArgs a)
     cl.sync();  // the lists are complete, and no CTA reads another's shared memory any more
     const int per = a.row_bytes / 16;  // 8, 16 or 32 lanes a row: as many rows a warp at once as fit
     const int sub = lane / per, at = lane % per, together = 32 / per;
-    for (int j0 = (rank * kEvictWarps + warp) * together; j0 < moves; j0 += C * kEvictWarps * together) {
-        const int j = j0 + sub;
-        if (j >= moves) continue;
-        const int dst = list_f[j], src = list_p[j];
-        const int64_t pd = a.c.page_of(b, dst, a.status), ps = a.c.page_of(b, src, a.status);
-        if (pd < 0 || ps < 0) continue;
-        const int64_t from = a.c.row(ps, src, g) + at * 16, to = a.c.row(pd, dst, g) + at * 16;
-        const uint4 x = *reinterpret_cast<const uint4*>(a.c.k + from), y = *reinterpret_cast<const uint4*>(a.c.v + from);
-        *reinterpret_cast<uint4*>(a.c.k + to) = x;
-        *reinterpret_cast<uint4*>(a.c.v + to) = y;
-        if (at == 0) {
-            const int64_t ms = a.c.meta(ps, src, g), md = a.c.meta(pd, dst, g);
-            a.c.weight[md] = a.c.weight[ms];
-            a.c.position[md] = a.c.position[ms];
+    constexpr int kBatch = 4;  // rows a lane has in flight
+    const int stride = C * kEvictWarps * together;
+    for (int j0 = (rank * kEvictWarps + warp) * together + sub; j0 < moves; j0 += kBatch * stride) {
+        int dst[kBatch], src[kBatch], pd[kBatch], ps[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int j = j0 + i * stride;
+            dst[i] = j < moves ? list_f[j] : -1;
+            src[i] = j < moves ? list_p[j] : 0;
+        }
+        const int32_t* table = a.c.table + (int64_t)b * a.c.ld_table;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            pd[i] = dst[i] >= 0 ? table[dst[i] >> a.c.shift] : -1;
+            ps[i] = dst[i] >= 0 ? table[src[i] >> a.c.shift] : -1;
+        }
+        uint4 x[kBatch], y[kBatch];
+        float w[kBatch];
+        int pos[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if (pd[i] < 0 || ps[i] < 0 || pd[i] >= a.c.n_pages || ps[i] >= a.c.n_pages) dst[i] = -1;  // reported with its key
+            if (dst[i] < 0) continue;
+            const int64_t from = a.c.row(ps[i], src[i], g) + at * 16, ms = a.c.meta(ps[i], src[i], g);
+            x[i] = *reinterpret_cast<const uint4*>(a.c.k + from);
+            y[i] = *reinterpret_cast<const uint4*>(a.c.v + from);
+            w[i] = a.c.weight[ms];
+            pos[i] = a.c.position[ms];
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if (dst[i] < 0) continue;
+            const int64_t to = a.c.row(pd[i], dst[i], g) + at * 16, md = a.c.meta(pd[i], dst[i], g);
+            *reinterpret_cast<uint4*>(a.c.k + to) = x[i];
+            *reinterpret_cast<uint4*>(a.c.v + to) = y[i];
+            if (at == 0) {
+                a.c.weight[md] = w[i];
+                a.c.position[md] = pos[i];
+            }
         }
     }
 }
