@@ -184,44 +184,26 @@ __device__ __forceinline__ int64_t ctas_of(const CacheAttnArgs& a, int64_t total
 __device__ __forceinline__ int64_t unit_begin(int64_t c, int64_t total, int64_t G) { return c * total / G; }
 __device__ __forceinline__ int64_t cta_of(int64_t u, int64_t total, int64_t G) { return ((u + 1) * G - 1) / total; }
 
-// The drafts of a sequence (n, from row0) that see draft j: bit i of 128.
-struct Seers {
-    uint64_t w[2];
-    __device__ __forceinline__ bool has(int i) const { return (i < 64 ? w[0] >> i : w[1] >> (i - 64)) & 1; }
-};
-__device__ __forceinline__ Seers seers_of(const CacheAttnArgs& a, int64_t row0, int n, int j) {
-    Seers s{{0, 0}};
-    if (j >= n) return s;
-    if (a.tree == nullptr) {  // i >= j
-        s.w[0] = j < 64 ? ~0ull << j : 0;
-        s.w[1] = j < 64 ? ~0ull : ~0ull << (j - 64);
-        return s;
-    }
+// Which of the rows first .. first + nr - 1 (nr <= 64) of a (b, KV head) see draft j of the sequence's
+// n drafts (from row0): bit r for row first + r, which is draft (first + r) / rep.
+__device__ __forceinline__ uint64_t rows_that_see(const CacheAttnArgs& a, int64_t row0, int n, int j, int first, int nr) {
+    if (j >= n || nr <= 0) return 0;
+    const int i0 = first / a.rep, i1 = (first + nr - 1) / a.rep;
     const uint64_t* p = a.tree + row0 * a.words + (j >> 6);
-    for (int i0 = 0; i0 < n; i0 += 16) {
-        uint64_t x[16];
+    uint64_t rows = 0;
+    for (int i = i0; i <= i1; i += 8) {
+        bool sees[8];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) x[k] = i0 + k < n ? p[(int64_t)(i0 + k) * a.words] : 0;  // in flight together
-        uint64_t bits = 0;
+        for (int k = 0; k < 8; ++k)  // loads in flight together
+            sees[k] = i + k <= i1 && (a.tree == nullptr ? j <= i + k : p[(int64_t)(i + k) * a.words] >> (j & 63) & 1);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) bits |= (x[k] >> (j & 63) & 1) << k;
-        if (i0 < 64) s.w[0] |= bits << i0;
-        else s.w[1] |= bits << (i0 - 64);
-    }
-    return s;
-}
-
-// Drafts of consecutive rows of a (b, KV head): row r is draft r / rep.
-struct RowDraft {
-    int i, left;
-    __device__ __forceinline__ RowDraft(int r, int rep) : i(r / rep), left(rep - r % rep) {}
-    __device__ __forceinline__ void next(int rep) {
-        if (--left == 0) {
-            ++i;
-            left = rep;
+        for (int k = 0; k < 8; ++k) {
+            const int lo = max((i + k) * a.rep - first, 0), hi = min((i + k + 1) * a.rep - first, nr);
+            if (sees[k]) rows |= ~0ull >> (64 - (hi - lo)) << lo;
         }
     }
-};
+    return rows;
+}
 
 // The tensor-core forward of bf16 caches: rows of a block and partials of a segment for a call's
 // rows of a (b, KV head), and the launch.

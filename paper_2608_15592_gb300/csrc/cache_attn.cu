@@ -163,13 +163,7 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
             vrow[t] = kr.v;
             unsigned hidden = 0;  // rows that do not see this key
             if (drafts) {
-                const Seers seers = seers_of(a, row0, kr.k != nullptr ? s.n : 0, t);
-                RowDraft row(r0, a.rep);
-#pragma unroll
-                for (int r = 0; r < kRows; ++r) {
-                    if (r >= nr || !seers.has(row.i)) hidden |= 1u << r;
-                    row.next(a.rep);
-                }
+                hidden = ~(unsigned)rows_that_see(a, row0, kr.k != nullptr ? s.n : 0, t, r0, nr);
             } else if (kr.k == nullptr) {
                 hidden = (1u << kRows) - 1;
             }
@@ -460,8 +454,6 @@ __global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnA
             const bool drafts = tile == s.nt - 1;
             if (drafts ? a.w_new == nullptr : !a.accumulate) continue;
             const KeyRow kr = key_row(a, s, at.b, g, tile, t, D * (int)sizeof(T));
-            Seers seers{{0, 0}};
-            if (drafts) seers = seers_of(a, row0, kr.k != nullptr ? s.n : 0, t);
             float sum = 0.f;
             for (int r0 = 0; r0 < R; r0 += kRows) {
                 const int nr = min(kRows, R - r0);
@@ -472,9 +464,10 @@ __global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnA
                 if (kr.k == nullptr) continue;
                 float z[kRows];
                 dots<T, D>(q, kr.k, z);
+                const uint64_t seen = drafts ? rows_that_see(a, row0, s.n, t, r0, nr) : ~0ull;
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
-                    if (r >= nr || (drafts && !seers.has((r0 + r) / a.rep))) continue;
+                    if (r >= nr || !(seen >> r & 1)) continue;
                     const float2 f = ml[r];
                     if (f.y != 0.f) sum = fmaf(ex2(fmaf(z[r], a.scale_log2, f.x)), f.y, sum);
                 }

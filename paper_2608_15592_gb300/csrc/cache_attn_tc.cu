@@ -55,7 +55,7 @@ struct Shape {
     static constexpr int kPStep = RB == 64 ? 2 * kAtom : RB == 32 ? kAtom : 64;  // from a group's P to the other's
     static constexpr int kPBytes = RB == 64 ? 4 * kAtom : RB == 32 ? 2 * kAtom : kAtom;
     static constexpr int kFixed = kQBufs * kQBytes + kPBytes;
-    static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 400 - kGroups * (RB == 64 ? 2 : 6) * RB * 4;
+    static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 400 - kGroups * (RB == 64 ? 3 : 7) * RB * 4;
     static constexpr int kStages = kRoom / kTileBytes < 12 ? kRoom / kTileBytes : 12;
     static constexpr int kThreads = 128 + 128 * kGroups;
     static constexpr int kTmemUsed = kGroups * (2 * kN + 2 * RB);  // S twice, O hi and lo
@@ -69,8 +69,8 @@ struct Shape {
     static constexpr int kBarOff = kRedOff + (RB == 64 ? 0 : kGroups * 4 * RB * 4);
     static constexpr int kBars = 2 * kStages + 2 * kQBufs + 6 * kGroups + 2;
     static constexpr int kMiscOff = kBarOff + (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, poison bits
-    static constexpr int kRowOff = kMiscOff + 48;  // a group's [RB] m and [RB] factors
-    static constexpr int kSmem = kRowOff + kGroups * 2 * RB * 4 + 1024;
+    static constexpr int kRowOff = kMiscOff + 48;  // a group's [RB] m, [RB] factors, [RB] -m
+    static constexpr int kSmem = kRowOff + kGroups * 3 * RB * 4 + 1024;
     static_assert(kStages >= 4 && kSmem <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -144,12 +144,6 @@ __device__ __forceinline__ bool group_or(int id, bool x) {
 }
 __device__ __forceinline__ void group_sync(int id) { asm volatile("barrier.cta.sync.aligned %0, 128;" ::"r"(id) : "memory"); }
 
-__device__ __forceinline__ float warp_max(float x) {
-    float y;
-    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 __device__ __forceinline__ uint32_t pack_hi_lo(float a, float b, uint32_t& lo) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     const __nv_bfloat162 l = __floats2bfloat162_rn(a - __low2float(h), b - __high2float(h));
@@ -157,21 +151,25 @@ __device__ __forceinline__ uint32_t pack_hi_lo(float a, float b, uint32_t& lo) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Sums v[0..N) over the warp's lanes; lane k returns with the sum of column k % N (N = 8, 16, 32).
-template <int N>
-__device__ __forceinline__ float reduce_scatter(float* v, int lane) {
+// Reduces N columns (8, 16 or 32) over the warp's lanes; lane k returns with column k % N.  Every step
+// halves the columns a lane still holds.
+template <int N, class Op>
+__device__ __forceinline__ float reduce_scatter(const float* z, int lane, Op op) {
+    float v[N / 2];
 #pragma unroll
-    for (int o = 16; o >= N; o >>= 1)
+    for (int k = 0; k < N / 2; ++k) {
+        const bool up = lane & (N / 2);
+        v[k] = op(up ? z[k + N / 2] : z[k], __shfl_xor_sync(0xffffffffu, up ? z[k] : z[k + N / 2], N / 2));
+    }
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-#pragma unroll
-    for (int o = N / 2; o > 0; o >>= 1)
+    for (int o = N / 4; o > 0; o >>= 1)
 #pragma unroll
         for (int k = 0; k < o; ++k) {
             const bool up = lane & o;
-            const float send = up ? v[k] : v[k + o], keep = up ? v[k + o] : v[k];
-            v[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+            v[k] = op(up ? v[k + o] : v[k], __shfl_xor_sync(0xffffffffu, up ? v[k] : v[k + o], o));
         }
+#pragma unroll
+    for (int o = N; o < 32; o <<= 1) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], o));
     return v[0];
 }
 
@@ -497,8 +495,9 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
         // ------------------------------------------------------------- epilogue
         const int nb = (warp - 4) >> 2, q = warp & 3, bar = 1 + nb;
         const int j = q * 32 + lane;                 // key of the tile; lane of S and O
-        float* row_m = reinterpret_cast<float*>(sm + S::kRowOff) + nb * 2 * RB;  // m, log2 units
+        float* row_m = reinterpret_cast<float*>(sm + S::kRowOff) + nb * 3 * RB;  // m, log2 units
         float* row_f = row_m + RB;
+        float* row_n = row_f + RB;                   // -m, or 0 where m is -inf
         uint8_t* pb = sm + S::kPOff;
         // [4][RB], used when the P buffer is free
         float* row_w = RB == 64 ? reinterpret_cast<float*>(pb + nb * S::kPStep)
@@ -527,77 +526,91 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
             }
             const int64_t row0 = a.cu[sg.b];
             if (j < RB) row_m[j] = -INFINITY;
-            float l[RB];
+            float2 l[RB / 2];
 #pragma unroll
-            for (int r = 0; r < RB; ++r) l[r] = 0.f;
-            bool live = false;
+            for (int r = 0; r < RB / 2; ++r) l[r] = make_float2(0.f, 0.f);
+            bool live = false, lost = true;  // lost: a row has no m yet, every tile looks for one
             const int first = sg.tile0 + (KS == 2 ? nb : 0);
+            const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
             for (int tile = first; tile < sg.tile1; tile += KS, ++step) {
                 const bool drafts = tile == sg.s.nt - 1;
                 const int keys = tile_keys(a, sg.s, tile);
                 const uint32_t buf = step & 1;
+                uint64_t seen = ~0ull;  // rows that see this thread's key
+                if (drafts) seen = rows_that_see(a, row0, keys, j, sg.r0 + base, nr);
+                else if (j >= keys) seen = 0;
                 wait(&s_full[2 * nb + buf], (step >> 1) & 1);
                 tc_fence_after();
                 float z[RB];
+                auto load_s = [&]() {
 #pragma unroll
-                for (int r = 0; r < RB; r += kCols) {
-                    if (kCols == 8) tmem_ld8(tmem + lane_off + (2 * nb + buf) * S::kN + r, z + r);
-                    else tmem_ld16(tmem + lane_off + (2 * nb + buf) * S::kN + r, z + r);
-                }
-                tmem_wait_ld();
-                tie<RB>(z);
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&s_empty[2 * nb + buf]);
-                if (drafts) {
-                    const Seers seers = seers_of(a, row0, keys, j);
-                    RowDraft at(sg.r0 + base, a.rep);
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        if (r >= nr || !seers.has(at.i)) z[r] = -INFINITY;
-                        at.next(a.rep);
+                    for (int r = 0; r < RB; r += kCols) {
+                        if (kCols == 8) tmem_ld8(tmem + lane_off + (2 * nb + buf) * S::kN + r, z + r);
+                        else tmem_ld16(tmem + lane_off + (2 * nb + buf) * S::kN + r, z + r);
                     }
-                } else if (j >= keys) {
+                    tmem_wait_ld();
+                    tie<RB>(z);
+                    if (drafts || keys < kCacheTile) {
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) z[r] = -INFINITY;
-                }
+                        for (int r = 0; r < RB; ++r)
+                            if (!(seen >> r & 1)) z[r] = -INFINITY;
+                    }
+                };
+                load_s();
                 if (a.store && alive) {
                     float* to = a.score + ((walk.u - (sg.tile1 - tile)) * a.RB + base) * kCacheTile + j;
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
                         if (r < nr) to[r * kCacheTile] = z[r];
                 }
-                // does any score exceed its row's m by 2^8?
-                bool up = tile == first || !alive;
-                if (!up) {
-                    float top = -INFINITY;
+                // S c - m; does any score exceed its row's m by 2^8?
+                float top = -INFINITY;
+                auto relative = [&]() {
 #pragma unroll
-                    for (int r = 0; r < RB; r += 2)
-                        top = fmax3(top, fmaf(z[r], a.scale_log2, -row_m[r]), fmaf(z[r + 1], a.scale_log2, -row_m[r + 1]));
-                    up = top > 8.f;
-                }
-                if (group_or(bar, up)) {
+                    for (int r = 0; r < RB; r += 4) {
+                        const float4 n = *reinterpret_cast<const float4*>(row_n + r);
+                        const float2 x = __ffma2_rn(make_float2(z[r], z[r + 1]), c2, make_float2(n.x, n.y));
+                        const float2 y = __ffma2_rn(make_float2(z[r + 2], z[r + 3]), c2, make_float2(n.z, n.w));
+                        z[r] = x.x;
+                        z[r + 1] = x.y;
+                        z[r + 2] = y.x;
+                        z[r + 3] = y.y;
+                        top = fmax3(fmax3(top, x.x, x.y), y.x, y.y);
+                    }
+                };
+                if (!lost) relative();
+                if (group_or(bar, lost || top > 8.f || !alive)) {
                     if (step > 0) wait(&pv_done[nb], (step - 1) & 1);
                     tc_fence_after();
                     if (group_or(bar, !alive)) {
                         alive = false;
                         break;
                     }
+                    if (!lost) load_s();
+                    constexpr int kR = RB < 32 ? RB : 32;
+                    const auto larger = [](float x, float y) { return fmaxf(x, y); };
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        const float x = warp_max(z[r]);
-                        if (lane == (r & 31)) row_w[q * RB + r] = x;
+                    for (int r = 0; r < RB; r += kR) {
+                        const float x = reduce_scatter<kR>(z + r, lane, larger);
+                        if (lane < kR) row_w[q * RB + r + lane] = x;
                     }
                     group_sync(bar);
+                    bool none = false;
                     if (j < RB) {
                         const float x = fmaxf(fmaxf(row_w[j], row_w[RB + j]), fmaxf(row_w[2 * RB + j], row_w[3 * RB + j]));
                         const float old = row_m[j], m = fmaxf(old, x * a.scale_log2);
+                        none = m == -INFINITY;
                         row_f[j] = old == m ? 1.f : ex2(old - m);
                         row_m[j] = m;
+                        row_n[j] = none ? 0.f : -m;
                     }
-                    group_sync(bar);
+                    lost = group_or(bar, none);
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) l[r] *= row_f[r];
+                    for (int r = 0; r < RB; r += 4) {
+                        const float4 f = *reinterpret_cast<const float4*>(row_f + r);
+                        l[r / 2] = __fmul2_rn(l[r / 2], make_float2(f.x, f.y));
+                        l[r / 2 + 1] = __fmul2_rn(l[r / 2 + 1], make_float2(f.z, f.w));
+                    }
                     if (live) {
 #pragma unroll 1
                         for (int c = 0; c < 2 * RB; c += 16) {
@@ -611,14 +624,17 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                         }
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                     }
+                    relative();
                 }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_empty[2 * nb + buf]);
                 // P in place of the scores
 #pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    const float m = row_m[r];
-                    const float e = ex2(fmaf(z[r], a.scale_log2, m == -INFINITY ? 0.f : -m));
-                    z[r] = z[r] == -INFINITY ? 0.f : e;
-                    l[r] += z[r];
+                for (int r = 0; r < RB; r += 2) {
+                    z[r] = ex2(z[r]);
+                    z[r + 1] = ex2(z[r + 1]);
+                    l[r / 2] = __fadd2_rn(l[r / 2], make_float2(z[r], z[r + 1]));
                 }
                 if (step > 0) wait(&pv_done[nb], (step - 1) & 1);  // the P buffer is free
 #pragma unroll
@@ -700,11 +716,11 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                 if (D == 128 || q < 2) {
                     for (int x = 0; x < sg.s.n; ++x) {
                         if (!(odd_drafts[x >> 5] >> (x & 31) & 1)) continue;
-                        const Seers seers = seers_of(a, row0, sg.s.n, x);
+                        const uint64_t seen = rows_that_see(a, row0, sg.s.n, x, sg.r0 + base, nr);
                         const float v = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(
                             a.vn + (row0 + x) * a.ldn + (int64_t)sg.g * (D * 2) + j * 2));
                         for (int r = 0; r < nr; ++r) {
-                            if (!seers.has((sg.r0 + base + r) / a.rep)) continue;
+                            if (!(seen >> r & 1)) continue;
                             const __nv_bfloat16* ph = reinterpret_cast<const __nv_bfloat16*>(p_chunk(x, r >> 3)) + (r & 7);
                             const __nv_bfloat16* pl = reinterpret_cast<const __nv_bfloat16*>(p_chunk(x, (r + RB) >> 3)) + (r & 7);
                             a.part_o[(part + r) * D + j] += (__bfloat162float(*ph) + __bfloat162float(*pl)) * v;
@@ -715,9 +731,16 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
             if (RB == 64) group_sync(bar);  // P is read
             {
                 constexpr int kN = RB < 32 ? RB : 32;
+                const auto plus = [](float x, float y) { return x + y; };
 #pragma unroll
                 for (int r = 0; r < RB; r += kN) {
-                    const float x = reduce_scatter<kN>(l + r, lane);
+                    float v[kN];
+#pragma unroll
+                    for (int k = 0; k < kN; k += 2) {
+                        v[k] = l[(r + k) / 2].x;
+                        v[k + 1] = l[(r + k) / 2].y;
+                    }
+                    const float x = reduce_scatter<kN>(v, lane, plus);
                     if (lane < kN) row_w[q * RB + r + lane] = x;
                 }
             }
@@ -981,8 +1004,6 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                         }
                     }
                     float sum[2] = {0.f, 0.f};
-                    Seers seers{{0, 0}};
-                    if (drafts) seers = seers_of(a, row0, keys, j);
                     for (int k = gr; k < blocks; k += 2, ++step) {
                         const uint32_t buf = step % kWBufs;
                         if (alive)
@@ -990,6 +1011,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                         tc_fence_after();
                         const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (gr * kWBufs + buf) * kWBlock;
                         const int cols = min(kWBlock, nr - k * kWBlock);
+                        uint64_t seen = drafts ? rows_that_see(a, row0, keys, j, r0 + k * kWBlock, cols) : 0;
 #pragma unroll 1
                         for (int c = 0; c < cols; c += 16) {
                             float z[16];
@@ -1006,14 +1028,13 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                                     sum[1] = f.w != 0.f ? fmaf(e1, f.w, sum[1]) : sum[1];
                                 }
                             } else {
-                                RowDraft at(r0 + k * kWBlock + c, a.rep);
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) {
                                     const float2 f = fs[k * kWBlock + c + i];
                                     const float e = ex2(fmaf(z[i], a.scale_log2, f.x));
-                                    if (f.y != 0.f && seers.has(at.i)) sum[0] = fmaf(e, f.y, sum[0]);
-                                    at.next(a.rep);
+                                    if (f.y != 0.f && (seen >> i & 1)) sum[0] = fmaf(e, f.y, sum[0]);
                                 }
+                                seen >>= 16;
                             }
                         }
                         tc_fence_before();

@@ -11,10 +11,9 @@
 // takes one (sequence, head), each CTA an equal run of its slots:
 //   1. ranks of its slots as 32-bit keys in shared memory (formed again from the cache where they
 //      do not fit);
-//   2. the key T of rank `budget` by four rounds of 256 bins, the CTAs' histograms added through
+//   2. the key T of rank `budget` by three rounds of 2048 bins, the CTAs' histograms added through
 //      distributed shared memory;
-//   3. counts of keys equal to T, of freed slots and of kept ones past the budget, scanned over
-//      warps and CTAs, give every slot its place in the two lists;
+//   3. one tally of the slots against T, exchanged once, gives every slot its place in the two lists;
 //   4. the moves, dealt to all warps of the cluster.
 // Integer work throughout: results do not depend on the launch.
 #include <cooperative_groups.h>
@@ -66,6 +65,20 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendA
     const int64_t e = (int64_t)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
     bool ok = false;
     int b = 0, slot = 0, pos = 0;
+    const int per = a.row_bytes / 16, n = a.c.Hkv * per;
+    // the row's first 16-byte units, on their way while the slot is found
+    constexpr int kAhead = 4;
+    const int64_t src = e < a.n_rows ? (a.rows != nullptr ? a.rows[e] : e) : -1;
+    const bool there = src >= 0 && src < a.n_src;
+    const char* kr = a.kn + src * a.ldn;
+    const char* vr = a.vn + src * a.ldn;
+    uint4 x[kAhead], y[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (there && lane + 32 * i < n) {
+            x[i] = ld_stream(kr + (int64_t)(lane + 32 * i) * 16);
+            y[i] = ld_stream(vr + (int64_t)(lane + 32 * i) * 16);
+        }
     if (e < a.n_rows && e < a.cu[a.B] && a.cu[0] <= e) {
         // the last b with cu[b] <= e: 32 probes a step
         int lo = 0, hi = a.B;  // cu[lo] <= e < cu[hi]
@@ -97,23 +110,23 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendA
         }
     }
     if (!ok) return;
-    const int64_t src = a.rows != nullptr ? a.rows[e] : e;
-    if (src < 0 || src >= a.n_src) {
+    if (!there) {
         if (lane == 0) report(a.status, ESTP_ERR_INVALID_ARG);
         return;
     }
     const int64_t page = a.c.page_of(b, slot, a.status);
     if (page < 0) return;
-    const int per = a.row_bytes / 16, n = a.c.Hkv * per;
-    const char* kr = a.kn + src * a.ldn;
-    const char* vr = a.vn + src * a.ldn;
-    for (int i = lane; i < n; i += 32) {
+    auto put = [&](int i, const uint4& u, const uint4& w) {
         const int g = i / per, o = (i - g * per) * 16;
         const int64_t to = a.c.row(page, slot, g) + o;
-        const uint4 x = ld_stream(kr + (int64_t)i * 16), y = ld_stream(vr + (int64_t)i * 16);
-        *reinterpret_cast<uint4*>(a.c.k + to) = x;
-        *reinterpret_cast<uint4*>(a.c.v + to) = y;
-    }
+        *reinterpret_cast<uint4*>(a.c.k + to) = u;
+        *reinterpret_cast<uint4*>(a.c.v + to) = w;
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (lane + 32 * i < n) put(lane + 32 * i, x[i], y[i]);
+    for (int i = lane + 32 * kAhead; i < n; i += 32)
+        put(i, ld_stream(kr + (int64_t)i * 16), ld_stream(vr + (int64_t)i * 16));
     for (int g = lane; g < a.c.Hkv; g += 32) {
         const int64_t m = a.c.meta(page, slot, g);
         if (a.c.weight != nullptr) a.c.weight[m] = a.weight != nullptr ? a.weight[src * a.c.Hkv + g] : 0.f;
@@ -123,6 +136,9 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendA
 
 constexpr int kEvictThreads = 512, kEvictWarps = kEvictThreads / 32;
 constexpr int kMaxCluster = 8;
+constexpr int kRounds = 3, kBins = 2048;  // digits of 11, 11 and 10 bits, from the top
+constexpr int kBinsOf = kBins / kEvictThreads;
+static_assert(kBinsOf == 4, "a thread sums one 16-byte group of bins");
 
 struct EvictArgs {
     CacheView c;
@@ -133,7 +149,7 @@ struct EvictArgs {
     int budget, recent, sinks;
     int key_cap;            // keys a CTA holds in shared memory
     int max_moves;
-    int32_t* list;          // [groups][2][max_moves]: freed slots, kept slots past the budget
+    int2* list;             // [groups][2][max_moves] (page, slot of it): freed slots, kept slots past the budget
     uint32_t* done;
     int* status;
 };
@@ -145,17 +161,25 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// What a CTA tells the others of its cluster.
-struct EvictShare {
-    uint32_t hist[4][256];
-    int equal, freed, kept_past;
+// Slots of a run by their key against T: those that say how many are freed and kept past the budget
+// once the number of kept equals is known.  Kept equals are the first in slot order, so those below
+// the budget come before those past it.
+struct Tally {
+    int below_lt, below_eq, past_gt, past_eq;
+    __device__ __forceinline__ int kept_equal(int left, int equal_before) const {
+        return max(0, min(left - equal_before, below_eq + past_eq));
+    }
+    __device__ __forceinline__ int freed(int kept) const { return below_lt + below_eq - min(kept, below_eq); }
+    __device__ __forceinline__ int kept_past(int kept) const { return past_gt + max(0, kept - below_eq); }
 };
 
-__global__ void __launch_bounds__(kEvictThreads) evict_kernel(const EvictArgs a) {
-    extern __shared__ uint32_t keys[];
-    __shared__ EvictShare sh;
-    __shared__ int warp_sum[2][kEvictWarps];
-    __shared__ uint32_t pick[2];
+// Two CTAs an SM: 64 registers
+__global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs a) {
+    extern __shared__ uint32_t dyn[];
+    uint32_t* hist = dyn;                     // [kRounds][kBins]
+    uint32_t* keys = dyn + kRounds * kBins;   // [key_cap]
+    __shared__ Tally tally[kEvictWarps], cta_tally;
+    __shared__ uint32_t warp_sum[kEvictWarps], pick[2];
     cg::cluster_group cl = cg::this_cluster();
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
@@ -163,7 +187,7 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const EvictArgs a)
     const int len = a.length[b], seen = a.seen[b];
     const bool bad = len < 0 || len > a.c.capacity();
     const int n = bad ? 0 : len;
-    for (int i = t; i < 4 * 256; i += kEvictThreads) (&sh.hist[0][0])[i] = 0;
+    for (int i = t; i < kRounds * kBins / 4; i += kEvictThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     __shared__ bool last;
     if (t == 0) last = last_arrival(a.done, gridDim.x);
@@ -178,8 +202,9 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const EvictArgs a)
 
     const int run = ((n + C - 1) / C + 31) / 32 * 32;
     const int lo = min(n, rank * run), hi = min(n, lo + run);
+    const int32_t* table = a.c.table + (int64_t)b * a.c.ld_table;
     auto form_key = [&](int slot) -> uint32_t {
-        const int page = a.c.table[(int64_t)b * a.c.ld_table + (slot >> a.c.shift)];
+        const int page = table[slot >> a.c.shift];
         const bool there = page >= 0 && page < a.c.n_pages;
         if (!there) report(a.status, ESTP_ERR_INVALID_ARG);
         const int64_t m = a.c.meta(there ? page : 0, slot, g);
@@ -202,159 +227,176 @@ __global__ void __launch_bounds__(kEvictThreads) evict_kernel(const EvictArgs a)
     __syncthreads();
     auto key = [&](int slot) { return slot - lo < a.key_cap ? keys[slot - lo] : form_key(slot); };
 
-    // the key of rank `budget`, digit by digit from the top; `left` keys of it are still to be found
+    // the key T of rank `budget`, digit by digit; `left` keys equal to what is known of it are still wanted
     uint32_t T = 0;
     int left = a.budget;
-    for (int d = 0; d < 4; ++d) {
-        const int shift = 24 - 8 * d;
+#pragma unroll
+    for (int d = 0; d < kRounds; ++d) {
+        const int bits = d == kRounds - 1 ? 10 : 11, shift = d == 0 ? 21 : d == 1 ? 10 : 0;
+        uint32_t* h = hist + d * kBins;
         for (int s0 = lo + warp * 32; s0 < hi; s0 += kEvictThreads) {
             const int s = s0 + lane;
             const uint32_t k = s < hi ? key(s) : 0u;
-            const bool in = s < hi && (d == 0 || (k ^ T) >> (shift + 8) == 0);
-            const uint32_t bin = in ? k >> shift & 255u : 256u;
-            const unsigned same = __match_any_sync(0xffffffffu, bin);
-            if (in && lane == __ffs(same) - 1) atomicAdd(&sh.hist[d][bin], (uint32_t)__popc(same));
+            const bool in = s < hi && (d == 0 || (k ^ T) >> (shift + bits) == 0);
+            const unsigned safe = __ballot_sync(0xffffffffu, in && k == 0xffffffffu);  // many alike: one add
+            if (in && k != 0xffffffffu) atomicAdd(&h[k >> shift & ((1u << bits) - 1)], 1u);
+            if (safe && lane == 0) atomicAdd(&h[(1u << bits) - 1], (uint32_t)__popc(safe));
         }
-        cl.sync();
-        if (warp == 0) {  // bins of 8 a lane, the highest digit in lane 0
-            uint32_t h[8], sum = 0;
+        if (C > 1) cl.sync();
+        else __syncthreads();
+        // thread t: bins top - 4 t .. top - 4 t - 3 of the whole cluster
+        const int bin = kBins - 4 - 4 * t;
+        uint4 sum = *reinterpret_cast<const uint4*>(h + bin);
+        if (C > 1) {
+            uint4 other[kMaxCluster - 1];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int bin = 255 - (lane * 8 + i);
-                h[i] = 0;
-                for (int r = 0; r < C; ++r) h[i] += cl.map_shared_rank(&sh, r)->hist[d][bin];
-                sum += h[i];
-            }
-            uint32_t inc = sum;
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t x = __shfl_up_sync(0xffffffffu, inc, o);
-                if (lane >= o) inc += x;
-            }
-            uint32_t above = inc - sum;
+            for (int r = 1; r < kMaxCluster; ++r)
+                if (r < C) other[r - 1] = *reinterpret_cast<const uint4*>(cl.map_shared_rank(h, (rank + r) % C) + bin);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (above < (uint32_t)left && (uint32_t)left <= above + h[i]) {
-                    pick[0] = 255 - (lane * 8 + i);
+            for (int r = 1; r < kMaxCluster; ++r)
+                if (r < C) {
+                    sum.x += other[r - 1].x;
+                    sum.y += other[r - 1].y;
+                    sum.z += other[r - 1].z;
+                    sum.w += other[r - 1].w;
+                }
+        }
+        const uint32_t mine = sum.x + sum.y + sum.z + sum.w;
+        uint32_t inc = mine;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += x;
+        }
+        if (lane == 31) warp_sum[warp] = inc;
+        __syncthreads();
+        uint32_t above = lane < warp ? warp_sum[lane] : 0u;
+        for (int o = 16; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+        above += inc - mine;
+        if (above < (uint32_t)left && (uint32_t)left <= above + mine) {  // one thread
+            const uint32_t c4[4] = {sum.w, sum.z, sum.y, sum.x};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (above < (uint32_t)left && (uint32_t)left <= above + c4[i]) {
+                    pick[0] = bin + 3 - i;
                     pick[1] = left - above;
                 }
-                above += h[i];
+                above += c4[i];
             }
         }
         __syncthreads();
         T |= pick[0] << shift;
         left = (int)pick[1];
-        __syncthreads();
     }
 
-    // slots equal to T before each warp's run of this CTA
+    // every warp's run of slots, tallied against T
     const int per_warp = (run / 32 + kEvictWarps - 1) / kEvictWarps * 32;
     const int w0 = min(hi, lo + warp * per_warp), w1 = min(hi, w0 + per_warp);
-    auto scan_warps = [&](int* sums, int mine, int* total) {  // exclusive over the block's warps
-        if (lane == 0) sums[warp] = mine;
-        __syncthreads();
-        int before = 0, all = 0;
-        for (int w = 0; w < kEvictWarps; ++w) {
-            before += w < warp ? sums[w] : 0;
-            all += sums[w];
-        }
-        *total = all;
-        return before;
-    };
-    int n_eq = 0;
+    Tally mine{0, 0, 0, 0};
     for (int s0 = w0; s0 < w1; s0 += 32) {
         const int s = s0 + lane;
-        n_eq += __popc(__ballot_sync(0xffffffffu, s < w1 && key(s) == T));
-    }
-    int total;
-    int eq = scan_warps(warp_sum[0], n_eq, &total);
-    if (t == 0) sh.equal = total;
-    cl.sync();
-    for (int r = 0; r < rank; ++r) eq += cl.map_shared_rank(&sh, r)->equal;
-    const int eq0 = eq;
-
-    // freed slots below the budget and kept ones at or past it
-    auto classify = [&](int s, int& eq_run, bool& freed, bool& past) {
         const uint32_t k = s < w1 ? key(s) : 0u;
-        const unsigned is_eq = __ballot_sync(0xffffffffu, s < w1 && k == T);
-        const int my_eq = eq_run + __popc(is_eq & ((1u << lane) - 1));
-        const bool keep = s < w1 && (k > T || (k == T && my_eq < left));
-        eq_run += __popc(is_eq);
-        freed = s < w1 && s < a.budget && !keep;
-        past = keep && s >= a.budget;
-    };
-    int nf = 0, np = 0;
-    bool freed, past;
-    for (int s0 = w0; s0 < w1; s0 += 32) {
-        classify(s0 + lane, eq, freed, past);
-        nf += __popc(__ballot_sync(0xffffffffu, freed));
-        np += __popc(__ballot_sync(0xffffffffu, past));
+        const bool below = s < a.budget;
+        const unsigned in = __ballot_sync(0xffffffffu, s < w1), eq = __ballot_sync(0xffffffffu, s < w1 && k == T);
+        const unsigned gt = __ballot_sync(0xffffffffu, s < w1 && k > T), bl = __ballot_sync(0xffffffffu, below);
+        mine.below_lt += __popc(in & bl & ~eq & ~gt);
+        mine.below_eq += __popc(eq & bl);
+        mine.past_gt += __popc(gt & ~bl);
+        mine.past_eq += __popc(eq & ~bl);
     }
+    if (lane == 0) tally[warp] = mine;
     __syncthreads();
-    int tf, tp;
-    int f0 = scan_warps(warp_sum[0], nf, &tf), p0 = scan_warps(warp_sum[1], np, &tp);
-    if (t == 0) {
-        sh.freed = tf;
-        sh.kept_past = tp;
-    }
-    cl.sync();
-    int moves = 0;
-    for (int r = 0; r < C; ++r) {
-        const EvictShare* o = cl.map_shared_rank(&sh, r);
-        if (r < rank) {
-            f0 += o->freed;
-            p0 += o->kept_past;
+    auto warp_add = [&](Tally x) {  // over the warp's lanes
+        for (int o = 16; o > 0; o >>= 1) {
+            x.below_lt += __shfl_xor_sync(0xffffffffu, x.below_lt, o);
+            x.below_eq += __shfl_xor_sync(0xffffffffu, x.below_eq, o);
+            x.past_gt += __shfl_xor_sync(0xffffffffu, x.past_gt, o);
+            x.past_eq += __shfl_xor_sync(0xffffffffu, x.past_eq, o);
         }
-        moves += o->freed;
-    }
-    int32_t* list_f = a.list + (int64_t)group * 2 * a.max_moves;
-    int32_t* list_p = list_f + a.max_moves;
-    eq = eq0;
+        return x;
+    };
+    const Tally none{0, 0, 0, 0};
+    const Tally cta_all = warp_add(lane < kEvictWarps ? tally[lane] : none);
+    if (t == 0) cta_tally = cta_all;
+    if (C > 1) cl.sync();
+    else __syncthreads();
+    // what lies before this CTA's run and before this warp's: equals first, then the lists' places
+    const Tally of_rank = lane < C ? *cl.map_shared_rank(&cta_tally, lane) : none;
+    const Tally of_warp = lane < kEvictWarps ? tally[lane] : none;
+    auto before = [&](int x, int upto) {  // sum of x over the lanes below `upto`
+        x = lane < upto ? x : 0;
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        return x;
+    };
+    auto lane_before = [&](int x) {  // exclusive scan over the lanes
+        int inc = x;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += y;
+        }
+        return inc - x;
+    };
+    const int rank_eq = of_rank.below_eq + of_rank.past_eq, warp_eq = of_warp.below_eq + of_warp.past_eq;
+    const int rank_kept = of_rank.kept_equal(left, lane_before(rank_eq));
+    const int eq_cta = before(rank_eq, rank);
+    const int warp_kept = of_warp.kept_equal(left, eq_cta + lane_before(warp_eq));
+    const int moves = before(of_rank.freed(rank_kept), 32);
+    int f0 = before(of_rank.freed(rank_kept), rank) + before(of_warp.freed(warp_kept), warp);
+    int p0 = before(of_rank.kept_past(rank_kept), rank) + before(of_warp.kept_past(warp_kept), warp);
+    int eq0 = eq_cta + before(warp_eq, warp);
+
+    int2* list_f = a.list + (int64_t)group * 2 * a.max_moves;
+    int2* list_p = list_f + a.max_moves;
+    const unsigned lower = (1u << lane) - 1;
     for (int s0 = w0; s0 < w1; s0 += 32) {
         const int s = s0 + lane;
-        classify(s, eq, freed, past);
+        const uint32_t k = s < w1 ? key(s) : 0u;
+        const unsigned eq = __ballot_sync(0xffffffffu, s < w1 && k == T);
+        const bool keep = s < w1 && (k > T || (k == T && eq0 + __popc(eq & lower) < left));
+        eq0 += __popc(eq);
+        const bool freed = s < w1 && s < a.budget && !keep, past = keep && s >= a.budget;
         const unsigned bf = __ballot_sync(0xffffffffu, freed), bp = __ballot_sync(0xffffffffu, past);
-        const unsigned below = (1u << lane) - 1;
-        if (freed) list_f[f0 + __popc(bf & below)] = s;
-        if (past) list_p[p0 + __popc(bp & below)] = s;
+        if (freed || past) {
+            const int2 e = make_int2(table[s >> a.c.shift], s);
+            if (freed) list_f[f0 + __popc(bf & lower)] = e;
+            else list_p[p0 + __popc(bp & lower)] = e;
+        }
         f0 += __popc(bf);
         p0 += __popc(bp);
     }
-    cl.sync();  // the lists are complete, and no CTA reads another's shared memory any more
+    if (C > 1) cl.sync();  // the lists are complete, and no CTA reads another's shared memory any more
+    else __syncthreads();
     const int per = a.row_bytes / 16;  // 8, 16 or 32 lanes a row: as many rows a warp at once as fit
     const int sub = lane / per, at = lane % per, together = 32 / per;
     constexpr int kBatch = 4;  // rows a lane has in flight
     const int stride = C * kEvictWarps * together;
     for (int j0 = (rank * kEvictWarps + warp) * together + sub; j0 < moves; j0 += kBatch * stride) {
-        int dst[kBatch], src[kBatch], pd[kBatch], ps[kBatch];
+        int2 dst[kBatch], src[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int j = j0 + i * stride;
-            dst[i] = j < moves ? list_f[j] : -1;
-            src[i] = j < moves ? list_p[j] : 0;
-        }
-        const int32_t* table = a.c.table + (int64_t)b * a.c.ld_table;
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            pd[i] = dst[i] >= 0 ? table[dst[i] >> a.c.shift] : -1;
-            ps[i] = dst[i] >= 0 ? table[src[i] >> a.c.shift] : -1;
+            dst[i] = j < moves ? list_f[j] : make_int2(-1, 0);
+            src[i] = j < moves ? list_p[j] : make_int2(-1, 0);
         }
         uint4 x[kBatch], y[kBatch];
         float w[kBatch];
         int pos[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            if (pd[i] < 0 || ps[i] < 0 || pd[i] >= a.c.n_pages || ps[i] >= a.c.n_pages) dst[i] = -1;  // reported with its key
-            if (dst[i] < 0) continue;
-            const int64_t from = a.c.row(ps[i], src[i], g) + at * 16, ms = a.c.meta(ps[i], src[i], g);
+            // a page that is none was reported with its key
+            if (src[i].x < 0 || src[i].x >= a.c.n_pages || dst[i].x >= a.c.n_pages) dst[i].x = -1;
+            if (dst[i].x < 0) continue;
+            const int64_t from = a.c.row(src[i].x, src[i].y, g) + at * 16, ms = a.c.meta(src[i].x, src[i].y, g);
             x[i] = *reinterpret_cast<const uint4*>(a.c.k + from);
             y[i] = *reinterpret_cast<const uint4*>(a.c.v + from);
-            w[i] = a.c.weight[ms];
-            pos[i] = a.c.position[ms];
+            if (at == 0) {
+                w[i] = a.c.weight[ms];
+                pos[i] = a.c.position[ms];
+            }
         }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            if (dst[i] < 0) continue;
-            const int64_t to = a.c.row(pd[i], dst[i], g) + at * 16, md = a.c.meta(pd[i], dst[i], g);
+            if (dst[i].x < 0) continue;
+            const int64_t to = a.c.row(dst[i].x, dst[i].y, g) + at * 16, md = a.c.meta(dst[i].x, dst[i].y, g);
             *reinterpret_cast<uint4*>(a.c.k + to) = x[i];
             *reinterpret_cast<uint4*>(a.c.v + to) = y[i];
             if (at == 0) {
@@ -383,22 +425,23 @@ estp_status launch_cache_evict(estp_ctx* ctx, const CacheView& c, int row_bytes,
                                const int32_t* seen, int32_t* length_out, int budget, int recent, int sinks,
                                cudaStream_t st) {
     const int64_t groups = (int64_t)B * c.Hkv, cap = c.capacity();
-    // CTAs of a cluster: enough clusters' CTAs for the SMs, while each keeps a run of 1024 slots
+    // CTAs of a cluster: up to two an SM over all groups, while each keeps a run of 512 slots
     int C = 1;
-    while (C < kMaxCluster && groups * C * 2 <= ctx->num_sms && cap >= (int64_t)C * 2 * 1024) C *= 2;
+    while (C < kMaxCluster && groups * C * 2 <= 2 * ctx->num_sms && cap >= (int64_t)C * 2 * 512) C *= 2;
     const int64_t run = ((cap + C - 1) / C + 31) / 32 * 32;
     const int64_t max_keys = 48 * 1024;  // 192 KB
     EvictArgs a{c, row_bytes, B, length, seen, length_out, budget, recent, sinks};
     a.key_cap = (int)(run < max_keys ? run : max_keys);
     const int64_t moves = cap > budget ? (cap - budget < budget ? cap - budget : budget) : 0;
     a.max_moves = (int)moves;
-    estp_status s = ws_reserve(ctx, sizeof(int32_t) * 2 * (size_t)groups * (size_t)moves + 16);
+    estp_status s = ws_reserve(ctx, sizeof(int2) * 2 * (size_t)groups * (size_t)moves + 16);
     if (s != ESTP_OK) return s;
-    a.list = static_cast<int32_t*>(ctx->ws);
+    a.list = static_cast<int2*>(ctx->ws);
     a.done = ctx->done;
     a.status = ctx->status;
-    const size_t smem = sizeof(uint32_t) * (size_t)a.key_cap;
-    cudaError_t e = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(max_keys * 4));
+    const size_t smem = sizeof(uint32_t) * ((size_t)a.key_cap + kRounds * kBins);
+    cudaError_t e = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         (int)((max_keys + kRounds * kBins) * 4));
     if (e != cudaSuccess) return cuda_fail(e, "cache evict smem attribute");
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
