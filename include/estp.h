@@ -361,7 +361,8 @@ estp_status estp_misalignment(estp_ctx* ctx, const float* entropy, const float* 
  *                Unused slots may hold anything.
  *   weight     : fp32 [n_pages, Hkv, page_size], 16-byte aligned, or NULL (attention without
  *                accumulation only)
- *   position   : int32 [n_pages, Hkv, page_size], or NULL (not needed by the attention)
+ *   position   : int32 [n_pages, Hkv, page_size], 16-byte aligned, or NULL (not needed by the
+ *                attention)
  *   page_table : int32 [B, max_pages]; entries past a sequence's slots are not read.  Sequences
  *                may share pages for reading; calls that write (append, evict, accumulate)
  *                need every page in one sequence only.

@@ -477,8 +477,8 @@ static estp_status check_cache(estp_ctx* ctx, const estp_kv_cache* c, int32_t B,
         return fail(ESTP_ERR_INVALID_ARG, "cache strides must be multiples of 16 bytes");
     if (B > 0 && c->n_pages > 0 && (!c->k || !c->v || !c->page_table))
         return fail(ESTP_ERR_INVALID_ARG, "NULL cache pointer");
-    if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->weight))
-        return fail(ESTP_ERR_INVALID_ARG, "k, v and weight must be 16-byte aligned");
+    if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->weight) || !aligned16(c->position))
+        return fail(ESTP_ERR_INVALID_ARG, "k, v, weight and position must be 16-byte aligned");
     int shift = 0;
     while ((1 << shift) < c->page_size) ++shift;
     *view = CacheView{static_cast<char*>(c->k), static_cast<char*>(c->v), c->weight, c->position, c->page_table,

@@ -62,24 +62,26 @@ __device__ __forceinline__ bool append_ok(const AppendArgs& a, int lo, int hi, i
 
 __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendArgs a) {
     const int lane = threadIdx.x & 31;
-    const int64_t e = (int64_t)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
-    bool ok = false;
-    int b = 0, slot = 0, pos = 0;
     const int per = a.row_bytes / 16, n = a.c.Hkv * per;
-    // the row's first 16-byte units, on their way while the slot is found
-    constexpr int kAhead = 4;
-    const int64_t src = e < a.n_rows ? (a.rows != nullptr ? a.rows[e] : e) : -1;
-    const bool there = src >= 0 && src < a.n_src;
-    const char* kr = a.kn + src * a.ldn;
-    const char* vr = a.vn + src * a.ldn;
-    uint4 x[kAhead], y[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        if (there && lane + 32 * i < n) {
-            x[i] = ld_stream(kr + (int64_t)(lane + 32 * i) * 16);
-            y[i] = ld_stream(vr + (int64_t)(lane + 32 * i) * 16);
+    const int64_t total = min((int64_t)max(a.cu[a.B], 0), a.n_rows), e0 = max(a.cu[0], 0);
+    for (int64_t e = e0 + (int64_t)blockIdx.x * kAppendWarps + (threadIdx.x >> 5); e < total;
+         e += (int64_t)gridDim.x * kAppendWarps) {
+        const int64_t src = a.rows != nullptr ? a.rows[e] : e;
+        if (src < 0 || src >= a.n_src) {
+            if (lane == 0) report(a.status, ESTP_ERR_INVALID_ARG);
+            continue;
         }
-    if (e < a.n_rows && e < a.cu[a.B] && a.cu[0] <= e) {
+        // the row's first 16-byte units, on their way while its slot is found
+        constexpr int kAhead = 2;
+        const char* kr = a.kn + src * a.ldn;
+        const char* vr = a.vn + src * a.ldn;
+        uint4 x[kAhead], y[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (lane + 32 * i < n) {
+                x[i] = ld_stream(kr + (lane + 32 * i) * 16);
+                y[i] = ld_stream(vr + (lane + 32 * i) * 16);
+            }
         // the last b with cu[b] <= e: 32 probes a step
         int lo = 0, hi = a.B;  // cu[lo] <= e < cu[hi]
         while (hi - lo > 1) {
@@ -89,48 +91,40 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendA
             hi = min(hi, lo + (k + 1) * step);
             lo += k * step;
         }
-        b = lo;
-        const int first = a.cu[b], next = a.cu[b + 1], len = a.length != nullptr ? a.length[b] : 0;
-        slot = len + (int)(e - first);
-        pos = (a.length != nullptr ? a.seen[b] : 0) + (int)(e - first);
-        ok = append_ok(a, first, next, len) && e >= first && e < next;
-    }
-    __syncthreads();
-    __shared__ bool last;
-    if (threadIdx.x == 0) last = last_arrival(a.done, gridDim.x);
-    __syncthreads();
-    if (last) {
-        for (int i = threadIdx.x; i < a.B; i += blockDim.x) {
-            const int first = a.cu[i], next = a.cu[i + 1], len = a.length != nullptr ? a.length[i] : 0;
-            const int seen = a.length != nullptr ? a.seen[i] : 0;
-            const bool fits = append_ok(a, first, next, len) && (i > 0 || first == 0);
-            if (!fits) report(a.status, ESTP_ERR_INVALID_ARG);
-            a.length_out[i] = len + (fits ? next - first : 0);
-            a.seen_out[i] = seen + (fits ? next - first : 0);
+        const int b = lo, first = a.cu[b], next = a.cu[b + 1], len = a.length != nullptr ? a.length[b] : 0;
+        if (!append_ok(a, first, next, len) || e < first || e >= next) continue;  // reported below
+        const int slot = len + (int)(e - first), pos = (a.length != nullptr ? a.seen[b] : 0) + (int)(e - first);
+        const int64_t page = a.c.page_of(b, slot, a.status);
+        if (page < 0) continue;
+        auto put = [&](int i, const uint4& u, const uint4& w) {
+            const int g = i / per, o = (i - g * per) * 16;
+            const int64_t to = a.c.row(page, slot, g) + o;
+            *reinterpret_cast<uint4*>(a.c.k + to) = u;
+            *reinterpret_cast<uint4*>(a.c.v + to) = w;
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (lane + 32 * i < n) put(lane + 32 * i, x[i], y[i]);
+        for (int i = lane + 32 * kAhead; i < n; i += 32)
+            put(i, ld_stream(kr + (int64_t)i * 16), ld_stream(vr + (int64_t)i * 16));
+        for (int g = lane; g < a.c.Hkv; g += 32) {
+            const int64_t m = a.c.meta(page, slot, g);
+            if (a.c.weight != nullptr) a.c.weight[m] = a.weight != nullptr ? a.weight[src * a.c.Hkv + g] : 0.f;
+            if (a.c.position != nullptr) a.c.position[m] = pos;
         }
     }
-    if (!ok) return;
-    if (!there) {
-        if (lane == 0) report(a.status, ESTP_ERR_INVALID_ARG);
-        return;
-    }
-    const int64_t page = a.c.page_of(b, slot, a.status);
-    if (page < 0) return;
-    auto put = [&](int i, const uint4& u, const uint4& w) {
-        const int g = i / per, o = (i - g * per) * 16;
-        const int64_t to = a.c.row(page, slot, g) + o;
-        *reinterpret_cast<uint4*>(a.c.k + to) = u;
-        *reinterpret_cast<uint4*>(a.c.v + to) = w;
-    };
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        if (lane + 32 * i < n) put(lane + 32 * i, x[i], y[i]);
-    for (int i = lane + 32 * kAhead; i < n; i += 32)
-        put(i, ld_stream(kr + (int64_t)i * 16), ld_stream(vr + (int64_t)i * 16));
-    for (int g = lane; g < a.c.Hkv; g += 32) {
-        const int64_t m = a.c.meta(page, slot, g);
-        if (a.c.weight != nullptr) a.c.weight[m] = a.weight != nullptr ? a.weight[src * a.c.Hkv + g] : 0.f;
-        if (a.c.position != nullptr) a.c.position[m] = pos;
+    __shared__ bool last;
+    __syncthreads();
+    if (threadIdx.x == 0) last = last_arrival(a.done, gridDim.x);
+    __syncthreads();
+    if (!last) return;
+    for (int i = threadIdx.x; i < a.B; i += blockDim.x) {
+        const int first = a.cu[i], next = a.cu[i + 1], len = a.length != nullptr ? a.length[i] : 0;
+        const int seen = a.length != nullptr ? a.seen[i] : 0;
+        const bool fits = append_ok(a, first, next, len) && (i > 0 || first == 0);
+        if (!fits) report(a.status, ESTP_ERR_INVALID_ARG);
+        a.length_out[i] = len + (fits ? next - first : 0);
+        a.seen_out[i] = seen + (fits ? next - first : 0);
     }
 }
 
@@ -200,32 +194,41 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
         }
     if (n <= a.budget) return;  // the whole cluster
 
-    const int run = ((n + C - 1) / C + 31) / 32 * 32;
+    const int run = ((n + C - 1) / C + 127) / 128 * 128;  // a warp takes 128 slots at a time, a lane 4
     const int lo = min(n, rank * run), hi = min(n, lo + run);
     const int32_t* table = a.c.table + (int64_t)b * a.c.ld_table;
-    auto form_key = [&](int slot) -> uint32_t {
+    // keys of 4 slots of one page, from a multiple of 4; 0 past the sequence's slots
+    auto form_keys = [&](int slot) -> uint4 {
         const int page = table[slot >> a.c.shift];
-        const bool there = page >= 0 && page < a.c.n_pages;
-        if (!there) report(a.status, ESTP_ERR_INVALID_ARG);
-        const int64_t m = a.c.meta(there ? page : 0, slot, g);
-        const int pos = there ? a.c.position[m] : 0;
-        const float w = there ? a.c.weight[m] : 0.f;
-        return !there ? 0u : pos < a.sinks || pos >= seen - a.recent ? 0xffffffffu : weight_key(w);
+        if (page < 0 || page >= a.c.n_pages) {
+            report(a.status, ESTP_ERR_INVALID_ARG);
+            return make_uint4(0, 0, 0, 0);
+        }
+        const int64_t m = a.c.meta(page, slot, g);
+        const int4 pos = *reinterpret_cast<const int4*>(a.c.position + m);
+        const float4 w = *reinterpret_cast<const float4*>(a.c.weight + m);
+        auto one = [&](int p, float x, int s) {
+            return s >= n ? 0u : p < a.sinks || p >= seen - a.recent ? 0xffffffffu : weight_key(x);
+        };
+        return make_uint4(one(pos.x, w.x, slot), one(pos.y, w.y, slot + 1), one(pos.z, w.z, slot + 2), one(pos.w, w.w, slot + 3));
     };
     {
-        constexpr int kBatch = 4;  // slots a thread has in flight
+        constexpr int kBatch = 2;  // 8 slots a thread has in flight
         const int top = min(hi, lo + a.key_cap);
-        for (int s0 = lo + t; s0 < top; s0 += kBatch * kEvictThreads) {
-            uint32_t k[kBatch];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) k[i] = s0 + i * kEvictThreads < top ? form_key(s0 + i * kEvictThreads) : 0u;
+        for (int s0 = lo + 4 * t; s0 < top; s0 += kBatch * 4 * kEvictThreads) {
+            uint4 k[kBatch];
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
-                if (s0 + i * kEvictThreads < top) keys[s0 + i * kEvictThreads - lo] = k[i];
+                if (s0 + i * 4 * kEvictThreads < top) k[i] = form_keys(s0 + i * 4 * kEvictThreads);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (s0 + i * 4 * kEvictThreads < top) *reinterpret_cast<uint4*>(keys + (s0 + i * 4 * kEvictThreads - lo)) = k[i];
         }
     }
     __syncthreads();
-    auto key = [&](int slot) { return slot - lo < a.key_cap ? keys[slot - lo] : form_key(slot); };
+    auto keys_of = [&](int slot) {
+        return slot - lo < a.key_cap ? *reinterpret_cast<const uint4*>(keys + (slot - lo)) : form_keys(slot);
+    };
 
     // the key T of rank `budget`, digit by digit; `left` keys equal to what is known of it are still wanted
     uint32_t T = 0;
@@ -234,13 +237,17 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
     for (int d = 0; d < kRounds; ++d) {
         const int bits = d == kRounds - 1 ? 10 : 11, shift = d == 0 ? 21 : d == 1 ? 10 : 0;
         uint32_t* h = hist + d * kBins;
-        for (int s0 = lo + warp * 32; s0 < hi; s0 += kEvictThreads) {
-            const int s = s0 + lane;
-            const uint32_t k = s < hi ? key(s) : 0u;
-            const bool in = s < hi && (d == 0 || (k ^ T) >> (shift + bits) == 0);
-            const unsigned safe = __ballot_sync(0xffffffffu, in && k == 0xffffffffu);  // many alike: one add
-            if (in && k != 0xffffffffu) atomicAdd(&h[k >> shift & ((1u << bits) - 1)], 1u);
-            if (safe && lane == 0) atomicAdd(&h[(1u << bits) - 1], (uint32_t)__popc(safe));
+        for (int s = lo + 4 * t; s < hi; s += 4 * kEvictThreads) {
+            const uint4 k4 = keys_of(s);
+            const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+            int safe = 0;  // alike and many: counted apart
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (s + i >= hi || (d > 0 && (k[i] ^ T) >> (shift + bits) != 0)) continue;
+                if (k[i] == 0xffffffffu) ++safe;
+                else atomicAdd(&h[k[i] >> shift & ((1u << bits) - 1)], 1u);
+            }
+            if (safe) atomicAdd(&h[(1u << bits) - 1], (uint32_t)safe);
         }
         if (C > 1) cl.sync();
         else __syncthreads();
@@ -289,22 +296,22 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
     }
 
     // every warp's run of slots, tallied against T
-    const int per_warp = (run / 32 + kEvictWarps - 1) / kEvictWarps * 32;
+    const int per_warp = (run / 128 + kEvictWarps - 1) / kEvictWarps * 128;
     const int w0 = min(hi, lo + warp * per_warp), w1 = min(hi, w0 + per_warp);
     Tally mine{0, 0, 0, 0};
-    for (int s0 = w0; s0 < w1; s0 += 32) {
-        const int s = s0 + lane;
-        const uint32_t k = s < w1 ? key(s) : 0u;
-        const bool below = s < a.budget;
-        const unsigned in = __ballot_sync(0xffffffffu, s < w1), eq = __ballot_sync(0xffffffffu, s < w1 && k == T);
-        const unsigned gt = __ballot_sync(0xffffffffu, s < w1 && k > T), bl = __ballot_sync(0xffffffffu, below);
-        mine.below_lt += __popc(in & bl & ~eq & ~gt);
-        mine.below_eq += __popc(eq & bl);
-        mine.past_gt += __popc(gt & ~bl);
-        mine.past_eq += __popc(eq & ~bl);
+    for (int s = w0 + 4 * lane; s < w1; s += 128) {
+        const uint4 k4 = keys_of(s);
+        const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (s + i >= w1) continue;
+            const bool below = s + i < a.budget;
+            mine.below_lt += below && k[i] < T;
+            mine.below_eq += below && k[i] == T;
+            mine.past_gt += !below && k[i] > T;
+            mine.past_eq += !below && k[i] == T;
+        }
     }
-    if (lane == 0) tally[warp] = mine;
-    __syncthreads();
     auto warp_add = [&](Tally x) {  // over the warp's lanes
         for (int o = 16; o > 0; o >>= 1) {
             x.below_lt += __shfl_xor_sync(0xffffffffu, x.below_lt, o);
@@ -314,6 +321,9 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
         }
         return x;
     };
+    mine = warp_add(mine);
+    if (lane == 0) tally[warp] = mine;
+    __syncthreads();
     const Tally none{0, 0, 0, 0};
     const Tally cta_all = warp_add(lane < kEvictWarps ? tally[lane] : none);
     if (t == 0) cta_tally = cta_all;
@@ -346,22 +356,38 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
 
     int2* list_f = a.list + (int64_t)group * 2 * a.max_moves;
     int2* list_p = list_f + a.max_moves;
-    const unsigned lower = (1u << lane) - 1;
-    for (int s0 = w0; s0 < w1; s0 += 32) {
-        const int s = s0 + lane;
-        const uint32_t k = s < w1 ? key(s) : 0u;
-        const unsigned eq = __ballot_sync(0xffffffffu, s < w1 && k == T);
-        const bool keep = s < w1 && (k > T || (k == T && eq0 + __popc(eq & lower) < left));
-        eq0 += __popc(eq);
-        const bool freed = s < w1 && s < a.budget && !keep, past = keep && s >= a.budget;
-        const unsigned bf = __ballot_sync(0xffffffffu, freed), bp = __ballot_sync(0xffffffffu, past);
-        if (freed || past) {
-            const int2 e = make_int2(table[s >> a.c.shift], s);
-            if (freed) list_f[f0 + __popc(bf & lower)] = e;
-            else list_p[p0 + __popc(bp & lower)] = e;
+    for (int s0 = w0; s0 < w1; s0 += 128) {
+        const int s = s0 + 4 * lane;
+        const uint4 k4 = s < w1 ? keys_of(s) : make_uint4(0, 0, 0, 0);
+        const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+        int eq = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) eq += s + i < w1 && k[i] == T;
+        const int eq_scan = lane_before(eq);
+        unsigned freed = 0, past = 0;
+        int e = eq0 + eq_scan;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool in = s + i < w1, keep = in && (k[i] > T || (k[i] == T && e < left));
+            e += in && k[i] == T;
+            if (in && s + i < a.budget && !keep) freed |= 1u << i;
+            if (keep && s + i >= a.budget) past |= 1u << i;
         }
-        f0 += __popc(bf);
-        p0 += __popc(bp);
+        // both counts in one scan: each is at most 128
+        const int both = __popc(freed) | __popc(past) << 16, scan = lane_before(both);
+        int f = f0 + (scan & 0xffff), p = p0 + (scan >> 16);
+        if (freed | past) {
+            const int page = table[s >> a.c.shift];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (freed >> i & 1) list_f[f++] = make_int2(page, s + i);
+                if (past >> i & 1) list_p[p++] = make_int2(page, s + i);
+            }
+        }
+        const int all = __shfl_sync(0xffffffffu, scan + both, 31);
+        f0 += all & 0xffff;
+        p0 += all >> 16;
+        eq0 += __shfl_sync(0xffffffffu, eq_scan + eq, 31);
     }
     if (C > 1) cl.sync();  // the lists are complete, and no CTA reads another's shared memory any more
     else __syncthreads();
@@ -415,7 +441,9 @@ estp_status launch_cache_append(estp_ctx* ctx, const CacheView& c, int row_bytes
                                 const int32_t* rows, const int32_t* cu, int64_t n_rows, cudaStream_t st) {
     AppendArgs a{c, row_bytes, B, length, seen, length_out, seen_out, static_cast<const char*>(kn),
                  static_cast<const char*>(vn), ldn_bytes, n_src, weight, rows, cu, n_rows, ctx->done, ctx->status};
-    const int64_t grid = n_rows > 0 ? (n_rows + kAppendWarps - 1) / kAppendWarps : 1;
+    // a warp an entry, up to 5 blocks an SM (40 warps of 2 KB or more in flight), then several
+    const int64_t blocks = n_rows > 0 ? (n_rows + kAppendWarps - 1) / kAppendWarps : 1, most = 5 * ctx->num_sms;
+    const int64_t grid = blocks < most ? blocks : most;
     append_kernel<<<(unsigned)grid, 32 * kAppendWarps, 0, st>>>(a);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache append launch");
@@ -428,7 +456,7 @@ estp_status launch_cache_evict(estp_ctx* ctx, const CacheView& c, int row_bytes,
     // CTAs of a cluster: up to two an SM over all groups, while each keeps a run of 512 slots
     int C = 1;
     while (C < kMaxCluster && groups * C * 2 <= 2 * ctx->num_sms && cap >= (int64_t)C * 2 * 512) C *= 2;
-    const int64_t run = ((cap + C - 1) / C + 31) / 32 * 32;
+    const int64_t run = ((cap + C - 1) / C + 127) / 128 * 128;
     const int64_t max_keys = 48 * 1024;  // 192 KB
     EvictArgs a{c, row_bytes, B, length, seen, length_out, budget, recent, sinks};
     a.key_cap = (int)(run < max_keys ? run : max_keys);
