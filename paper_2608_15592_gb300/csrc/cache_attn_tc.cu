@@ -776,21 +776,27 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
 // an equal run of the call's (b, KV head, tile); the blocks of 64 rows of a tile go to the two groups
 // in turn, whose sums are added in their order.  Rows beyond kWRows take another pass over the run,
 // by the same threads.  Bound by K's bytes up to some 170 rows a KV head, then by ex2 (16 a clock).
-constexpr int kWRows = 448, kWBlock = 64, kWStages = 3, kWBufs = 4;
+constexpr int kWRows = 448, kWBlock = 64, kWMinStages = 3, kWMaxStages = 6, kWBufs = 4;
 template <int D>
 struct WShape {
     static constexpr int kAtoms = D / 64;
     static constexpr int kTileBytes = kAtoms * kAtom;
     static constexpr int kBlockBytes = kAtoms * kWBlock * 128;  // Q of one block of rows
-    static constexpr int kQOff = kWStages * kTileBytes;
-    static constexpr int kFOff = kQOff + kWRows / kWBlock * kBlockBytes;  // [kWRows] factors
-    static constexpr int kRedOff = kFOff + kWRows * 8;                    // [2][128] the second group's sums
-    static constexpr int kBarOff = kRedOff + 2 * 128 * 4;
-    static constexpr int kBars = 2 * kWStages + 1 + 4 * kWBufs + 1;
-    static constexpr int kMiscOff = kBarOff + kBars * 8;
-    static constexpr int kSmem = kMiscOff + 16 + 1024;
+    // from a 1024-aligned base: barriers, factors and sums first, then Q blocks and as many K tiles as fit
+    static constexpr int kBars = 2 * kWMaxStages + 1 + 4 * kWBufs + 1;
+    static constexpr int kMiscOff = kBars * 8;          // tmem address, abort flag
+    static constexpr int kRedOff = 256;                 // [2][128] the second group's sums
+    static constexpr int kFOff = kRedOff + 2 * 128 * 4; // [kWRows] factors
+    static constexpr int kQOff = (kFOff + kWRows * 8 + 1023) / 1024 * 1024;
+    static_assert(kMiscOff + 8 <= kRedOff, "barriers");
     static constexpr int kThreads = 64 + 256;
-    static_assert(kSmem <= 227 * 1024, "shared memory per CTA");
+    static constexpr int kRoom = 227 * 1024 - 1024 - kQOff;
+    static int stages(int blocks) {
+        const int n = (kRoom - blocks * kBlockBytes) / kTileBytes;
+        return n < kWMaxStages ? n : kWMaxStages;
+    }
+    static int smem(int blocks) { return 1024 + kQOff + blocks * kBlockBytes + stages(blocks) * kTileBytes; }
+    static_assert(kRoom - kWRows / kWBlock * kBlockBytes >= kWMinStages * kTileBytes, "shared memory per CTA");
 };
 
 __device__ __forceinline__ bool both_groups_or(bool x) {
@@ -837,13 +843,15 @@ struct ItemWalk {
 
 template <int D>
 __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
-    cache_weight_tc_kernel(const __grid_constant__ TcMaps tm, const CacheAttnArgs a, const int box_rows, const int new_rows) {
+    cache_weight_tc_kernel(const __grid_constant__ TcMaps tm, const CacheAttnArgs a, const int box_rows, const int new_rows,
+                           const int q_blocks, const int n_stages) {
     using S = WShape<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
-    uint64_t* full = reinterpret_cast<uint64_t*>(sm + S::kBarOff);  // [kWStages]
-    uint64_t* empty = full + kWStages;
-    uint64_t* q_full = empty + kWStages;
+    uint8_t* ring = sm + S::kQOff + q_blocks * S::kBlockBytes;
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm);  // [kWMaxStages]
+    uint64_t* empty = full + kWMaxStages;
+    uint64_t* q_full = empty + kWMaxStages;
     uint64_t* s_full = q_full + 1;          // [2][kWBufs]
     uint64_t* s_empty = s_full + 2 * kWBufs;
     uint64_t* drain = s_empty + 2 * kWBufs;
@@ -851,7 +859,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 4);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kWStages; ++i) {
+        for (int i = 0; i < kWMaxStages; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
@@ -871,8 +879,8 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
     }
     tc_fence_before();
     const int64_t cta = blockIdx.x, G = gridDim.x;
-    PlanScratch* sc = reinterpret_cast<PlanScratch*>(sm);  // in the ring, unused until the barrier below
-    Place* place = reinterpret_cast<Place*>(sm + 1088);
+    PlanScratch* sc = reinterpret_cast<PlanScratch*>(ring);  // in the ring, unused until the barrier below
+    Place* place = reinterpret_cast<Place*>(ring + 1088);
     const PlanTotals tot = plan_block(a, sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
         const int64_t it = unit_begin(cta, all.items, G);
         if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) *place = x;
@@ -898,20 +906,20 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
             for (int r0 = 0; ok && r0 < w.s.n * a.rep; r0 += kWRows) {
                 win.open(a, w.s, w.b, w.tile0, lane);
                 for (int tile = w.tile0; tile < w.tile1; ++tile, ++e) {
-                    const int slot = (int)(e % kWStages);
-                    const uint32_t use = e / kWStages;
+                    const int slot = (int)(e % n_stages);
+                    const uint32_t use = e / n_stages;
                     if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
                         ok = false;
                         break;
                     }
-                    load_tile<D>(a, &tm.k, &tm.kn, win, w.s, w.b, w.g, tile, box_rows, new_rows, sm + slot * S::kTileBytes,
+                    load_tile<D>(a, &tm.k, &tm.kn, win, w.s, w.b, w.g, tile, box_rows, new_rows, ring + slot * S::kTileBytes,
                                  &full[slot], lane);
                 }
             }
         }
         if (lane == 0)
-            for (uint32_t i = 0; i < (uint32_t)kWStages && i < e; ++i)
-                drain_wait(&full[(e - 1 - i) % kWStages], ((e - 1 - i) / kWStages) & 1, a.status);
+            for (uint32_t i = 0; i < (uint32_t)n_stages && i < e; ++i)
+                drain_wait(&full[(e - 1 - i) % n_stages], ((e - 1 - i) / n_stages) & 1, a.status);
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
@@ -929,9 +937,9 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                     if (!wait(q_full, loads++ & 1)) break;
                     const int blocks = (min(kWRows, R - r0) + kWBlock - 1) / kWBlock;
                     for (int tile = w.tile0; ok && tile < w.tile1; ++tile, ++e) {
-                        const int slot = (int)(e % kWStages);
-                        if (!wait(&full[slot], (e / kWStages) & 1)) break;
-                        const uint32_t ka = smem_u32(sm + slot * S::kTileBytes);
+                        const int slot = (int)(e % n_stages);
+                        if (!wait(&full[slot], (e / n_stages) & 1)) break;
+                        const uint32_t ka = smem_u32(ring + slot * S::kTileBytes);
                         for (int k = 0; k < blocks; ++k) {
                             const int gr = k & 1;
                             const uint32_t n = steps[gr]++, buf = n % kWBufs, use = n / kWBufs;
@@ -969,19 +977,20 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
             for (int r0 = 0; alive && r0 < R; r0 += kWRows) {
                 const int nr = min(kWRows, R - r0), blocks = (nr + kWBlock - 1) / kWBlock;
                 // Q and factors of this pass's rows; every S of the pass before is done with them
+#pragma unroll 4
                 for (int x = tid; x < blocks * kWBlock * (D / 8); x += 256) {
                     const int r = x / (D / 8), ch = x % (D / 8);
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (r < nr) {
-                        const int i = (r0 + r) / a.rep, h = w.g * a.rep + (r0 + r) % a.rep;
-                        v = *reinterpret_cast<const uint4*>(a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16);
-                    }
-                    *reinterpret_cast<uint4*>(sm + S::kQOff + (r / kWBlock) * S::kBlockBytes + (ch >> 3) * kWBlock * 128 +
-                                              (r % kWBlock) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v;
+                    const int rr = r < nr ? r0 + r : r0, i = rr / a.rep, h = w.g * a.rep + rr % a.rep;
+                    const char* from = a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16;
+                    const uint32_t at = smem_u32(sm + S::kQOff) + (r / kWBlock) * S::kBlockBytes + (ch >> 3) * kWBlock * 128 +
+                                        (r % kWBlock) * 128 + (((ch & 7) ^ (r & 7)) << 4);
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(r < nr ? 16 : 0)
+                                 : "memory");
                 }
                 for (int r = tid; r < blocks * kWBlock; r += 256)
                     fs[r] = r < nr ? a.factor[(row0 + (r0 + r) / a.rep) * a.Hq + w.g * a.rep + (r0 + r) % a.rep]
                                    : make_float2(0.f, 0.f);
+                asm volatile("cp.async.wait_all;" ::: "memory");
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 both_groups_or(false);  // the factors are everyone's
                 if (lane == 0) mbar_arrive(q_full);
@@ -1011,35 +1020,27 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                         tc_fence_after();
                         const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (gr * kWBufs + buf) * kWBlock;
                         const int cols = min(kWBlock, nr - k * kWBlock);
-                        uint64_t seen = drafts ? rows_that_see(a, row0, keys, j, r0 + k * kWBlock, cols) : 0;
-#pragma unroll 1
-                        for (int c = 0; c < cols; c += 16) {
-                            float z[16];
-                            tmem_ld16(ta + c, z);
-                            tmem_wait_ld();
-                            tie<16>(z);
-                            const float4* f4 = reinterpret_cast<const float4*>(fs + k * kWBlock + c);
-                            if (!drafts) {
+                        const uint64_t seen = drafts ? rows_that_see(a, row0, keys, j, r0 + k * kWBlock, cols) : ~0ull;
+                        float z[kWBlock];
 #pragma unroll
-                                for (int i = 0; i < 16; i += 2) {
-                                    const float4 f = f4[i / 2];
-                                    const float e0 = ex2(fmaf(z[i], a.scale_log2, f.x)), e1 = ex2(fmaf(z[i + 1], a.scale_log2, f.z));
-                                    sum[0] = f.y != 0.f ? fmaf(e0, f.y, sum[0]) : sum[0];
-                                    sum[1] = f.w != 0.f ? fmaf(e1, f.w, sum[1]) : sum[1];
-                                }
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    const float2 f = fs[k * kWBlock + c + i];
-                                    const float e = ex2(fmaf(z[i], a.scale_log2, f.x));
-                                    if (f.y != 0.f && (seen >> i & 1)) sum[0] = fmaf(e, f.y, sum[0]);
-                                }
-                                seen >>= 16;
-                            }
-                        }
+                        for (int c = 0; c < kWBlock; c += 16) tmem_ld16(ta + c, z + c);
+                        tmem_wait_ld();
+                        tie<kWBlock>(z);
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&s_empty[gr * kWBufs + buf]);
+                        const float4* f4 = reinterpret_cast<const float4*>(fs + k * kWBlock);
+#pragma unroll
+                        for (int c = 0; c < kWBlock; c += 16) {
+                            if (c >= cols) break;
+#pragma unroll
+                            for (int i = c; i < c + 16; i += 2) {  // columns past the rows have a factor of 0
+                                const float4 f = f4[i / 2];
+                                const float e0 = ex2(fmaf(z[i], a.scale_log2, f.x)), e1 = ex2(fmaf(z[i + 1], a.scale_log2, f.z));
+                                sum[0] = f.y != 0.f && (seen >> i & 1) ? fmaf(e0, f.y, sum[0]) : sum[0];
+                                sum[1] = f.w != 0.f && (seen >> i & 2) ? fmaf(e1, f.w, sum[1]) : sum[1];
+                            }
+                        }
                     }
                     const float mine = sum[0] + sum[1];
                     if (gr == 1) red[parity * 128 + j] = mine;
@@ -1142,8 +1143,10 @@ estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaSt
     const estp_status s = make_maps(a, &tm, &box_rows, &new_rows);
     if (s != ESTP_OK) return s;
     auto kernel = a.c.d == 128 ? cache_weight_tc_kernel<128> : cache_weight_tc_kernel<64>;
-    const int smem = a.c.d == 128 ? WShape<128>::kSmem : WShape<64>::kSmem;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const int rows = a.max_rows * a.rep < kWRows ? a.max_rows * a.rep : kWRows, blocks = (rows + kWBlock - 1) / kWBlock;
+    const int smem = a.c.d == 128 ? WShape<128>::smem(blocks) : WShape<64>::smem(blocks);
+    const int stages = a.c.d == 128 ? WShape<128>::stages(blocks) : WShape<64>::stages(blocks);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
     if (e != cudaSuccess) return cuda_fail(e, "cache weight smem attribute");
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1155,7 +1158,7 @@ estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaSt
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, tm, a, box_rows, new_rows);
+    e = cudaLaunchKernelEx(&cfg, kernel, tm, a, box_rows, new_rows, blocks, stages);
     if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache weight launch");
 }
