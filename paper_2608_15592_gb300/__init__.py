@@ -181,8 +181,8 @@ class MlpHead:
 
 def _like(t, dtype, shape, name):
     """A dense tensor of this type and shape (None passes)."""
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
-        raise ValueError(f"{name} is a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
+        raise ValueError(f"{name} is a contiguous {dtype} tensor of shape {shape}")
 
 
 class KVCache:
@@ -220,13 +220,21 @@ class KVCache:
         self._ref = ctypes.addressof(self._c)
 
     def _rows(self, t, heads, name):
-        """Row stride of a [rows, heads, d] tensor of the cache's type."""
-        if t.dtype != self.dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim:
+        """Row stride of a [rows, heads, d] tensor of the cache's type whose heads are contiguous."""
+        rows, h, d = t.shape
+        s0, s1, s2 = t.stride()
+        if h != heads or d != self.head_dim or t.dtype != self.dtype:
             raise ValueError(f"{name} is a {self.dtype} tensor [rows, {heads}, {self.head_dim}]")
-        rows, s0, s1, s2 = t.shape[0], *t.stride()
-        if rows and (s2 != 1 or (heads > 1 and s1 != self.head_dim)):
+        if rows and (s2 != 1 or (heads > 1 and s1 != d)):
             raise ValueError(f"{name}: a row's heads are contiguous")
-        return s0 if rows > 1 else heads * self.head_dim
+        return s0 if rows > 1 else heads * d
+
+    def _new_rows(self, k_new, v_new):
+        """The row stride that new rows' K and V share."""
+        ld = self._rows(k_new, self.Hkv, "k_new")
+        if v_new.shape != k_new.shape or self._rows(v_new, self.Hkv, "v_new") != ld:
+            raise ValueError("k_new and v_new share their shape and row stride")
+        return ld
 
 
 class Context:
@@ -465,9 +473,7 @@ class Context:
         and cache.seen are updated in place."""
         import torch
         n = k_new.shape[0]
-        ld = cache._rows(k_new, cache.Hkv, "k_new")
-        if cache._rows(v_new, cache.Hkv, "v_new") != ld or v_new.shape[0] != n:
-            raise ValueError("k_new and v_new share their shape and row stride")
+        ld = cache._new_rows(k_new, v_new)
         if weight is not None:
             _like(weight, torch.float32, (n, cache.Hkv), "weight")
         _like(cu_rows, torch.int32, (cache.B + 1,), "cu_rows")
@@ -490,11 +496,11 @@ class Context:
         import torch
         n, Hq, d = Q.shape
         ldq = cache._rows(Q, Hq, "Q")
-        ld = 0
+        ld, kp, vp = 0, None, None
         if k_new is not None:
-            ld = cache._rows(k_new, cache.Hkv, "k_new")
-            if cache._rows(v_new, cache.Hkv, "v_new") != ld or k_new.shape[0] != n or v_new.shape[0] != n:
-                raise ValueError("k_new and v_new have a row for each of Q's, of one row stride")
+            if k_new.shape[0] != n or v_new.shape[0] != n:
+                raise ValueError("k_new and v_new have a row for each of Q's")
+            ld, kp, vp = cache._new_rows(k_new, v_new), k_new.data_ptr(), v_new.data_ptr()
         _like(cu_rows, torch.int32, (cache.B + 1,), "cu_rows")
         words = 0
         if tree_mask is not None:
@@ -504,16 +510,22 @@ class Context:
             _like(row_weight, torch.float32, (n,), "row_weight")
         dev = Q.device
         if out is None:
-            out = torch.empty(n, Hq, d, dtype=Q.dtype, device=dev)
+            out = torch.empty((n, Hq, d), dtype=cache.dtype, device=dev)
         else:
-            _like(out, Q.dtype, (n, Hq, d), "out")
-        lse = torch.empty(Hq, n, dtype=torch.float32, device=dev) if details else None
-        w_new = torch.empty(n, cache.Hkv, dtype=torch.float32, device=dev) if details and k_new is not None else None
-        self._check(self._lib.estp_cache_attention(
-            self._h, cache._ref, cache.length.data_ptr(), cache.B, cache.max_slots, Q.data_ptr(), ldq, Hq,
-            _ptr(k_new), _ptr(v_new), ld, cu_rows.data_ptr(), n, max_rows,
-            1.0 / math.sqrt(d) if scale is None else scale, _ptr(tree_mask), words, _ptr(row_weight),
-            1 if accumulate else 0, out.data_ptr(), _ptr(lse), _ptr(w_new), _stream(stream)))
+            _like(out, cache.dtype, (n, Hq, d), "out")
+        lse = w_new = lp = wp = None
+        if details:
+            lse = torch.empty((Hq, n), dtype=torch.float32, device=dev)
+            lp = lse.data_ptr()
+            if kp is not None:
+                w_new = torch.empty((n, cache.Hkv), dtype=torch.float32, device=dev)
+                wp = w_new.data_ptr()
+        status = self._lib.estp_cache_attention(
+            self._h, cache._ref, cache.length.data_ptr(), cache.B, cache.max_slots, Q.data_ptr(), ldq, Hq, kp, vp, ld,
+            cu_rows.data_ptr(), n, max_rows, d ** -0.5 if scale is None else scale, _ptr(tree_mask), words,
+            _ptr(row_weight), 1 if accumulate else 0, out.data_ptr(), lp, wp, _stream(stream))
+        if status:
+            self._check(status)
         return (out, lse, w_new) if details else out
 
     def cache_evict(self, cache: KVCache, budget: int, recent: int = 0, sinks: int = 0, stream=None):

@@ -64,6 +64,7 @@ struct CacheAttnArgs {
     float scale, scale_log2;
     int RB, G;
     int KS;                      // partials of a segment
+    int whole;                   // the forward finishes the groups that one CTA holds by itself
     int row_blocks;              // blocks of the finish kernel that merge rows
     int store;                   // scores are kept for the weights
     float* part_o;               // [G + groups][KS][RB][d]
@@ -81,8 +82,10 @@ struct CacheAttnArgs {
 // What sequence b brings to the call.
 struct SeqShape {
     int len, n, nrb, nt;
-    __device__ __forceinline__ int64_t units(int Hkv) const { return (int64_t)Hkv * nrb * nt; }
-    __device__ __forceinline__ int64_t items(int Hkv) const { return n > 0 ? (int64_t)Hkv * nt : 0; }
+    // the host has made sure that the call's units fit 31 bits
+    __device__ __forceinline__ int groups(int Hkv) const { return Hkv * nrb; }
+    __device__ __forceinline__ int units(int Hkv) const { return Hkv * nrb * nt; }
+    __device__ __forceinline__ int items(int Hkv) const { return n > 0 ? Hkv * nt : 0; }
 };
 __device__ __forceinline__ bool seq_ok(const CacheAttnArgs& a, int b) {
     const int len = a.length[b], lo = a.cu[b], hi = a.cu[b + 1];
@@ -101,88 +104,134 @@ __device__ __forceinline__ SeqShape seq_shape(const CacheAttnArgs& a, int b) {
 // Sums over the sequences before sequence b.
 struct Place {
     int b;
-    int64_t unit0, group0, item0;  // units, groups, items (KV head, tile) before it
+    int unit0, group0, item0;  // units, groups, items (KV head, tile) before it
+    __device__ __forceinline__ void pass(const SeqShape& s, int Hkv) {
+        ++b;
+        unit0 += s.units(Hkv);
+        group0 += s.groups(Hkv);
+        item0 += s.items(Hkv);
+    }
 };
 struct PlanTotals {
-    int64_t units, groups, items;
-    bool ok;                       // lengths, cu and their sums are what the host was told
+    int units, groups, items;
+    bool ok;                   // lengths, cu and their sums are what the host was told
 };
 struct PlanScratch {
-    int64_t sum[4][33];  // units, groups, items, slots
+    int sum[3][33];            // units, groups, items
+    int64_t slots[32];
+    Place place;
     int bad;
 };
 
-// Block-wide (a multiple of 32 threads): the call's totals, and visit(place, shape, totals) for every
-// sequence, by one thread each.  A thread sums a run of consecutive sequences; an exclusive scan over
-// the block gives each run's start.  Ends in a barrier.
-template <class Visit>
-__device__ __forceinline__ PlanTotals plan_block(const CacheAttnArgs& a, PlanScratch* sc, Visit visit) {
-    const int t = threadIdx.x, lane = t & 31, warp = t >> 5, n_warps = blockDim.x >> 5;
+__device__ __forceinline__ int scan_lanes(int x, int lane) {  // inclusive
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
+
+// The call's totals, and the place of the one sequence that want(place, shape, totals) picks (b = B
+// where it picks none).  Every thread of the block calls it.  Up to 32 sequences every warp scans
+// them by itself, a lane each, and no thread waits for another; more are shared out over the block
+// (a multiple of 32 threads), a run of consecutive ones a thread.
+template <class Want>
+__device__ __forceinline__ PlanTotals plan(const CacheAttnArgs& a, PlanScratch* sc, Place* out, Want want) {
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5, n_warps = blockDim.x >> 5, Hkv = a.c.Hkv;
+    if (a.B <= 32) {
+        const bool mine = lane < a.B, ok = !mine || seq_ok(a, lane);
+        SeqShape s{0, 0, 0, 0};
+        if (mine && ok) s = seq_shape(a, lane);
+        int64_t slots = s.len;
+        for (int o = 16; o > 0; o >>= 1) slots += __shfl_xor_sync(0xffffffffu, slots, o);
+        const int u = mine ? s.units(Hkv) : 0, g = s.groups(Hkv), i = mine ? s.items(Hkv) : 0;
+        const int iu = scan_lanes(u, lane), ig = scan_lanes(g, lane), ii = scan_lanes(i, lane);
+        const PlanTotals tot{__shfl_sync(0xffffffffu, iu, 31), __shfl_sync(0xffffffffu, ig, 31),
+                             __shfl_sync(0xffffffffu, ii, 31), __all_sync(0xffffffffu, ok) && slots <= a.n_slots};
+        if (!tot.ok) {
+            if (t == 0) report(a.status, ESTP_ERR_INVALID_ARG);
+            return tot;
+        }
+        Place p{lane, iu - u, ig - g, ii - i};
+        const unsigned hit = __ballot_sync(0xffffffffu, mine && want(p, s, tot));
+        const int from = hit ? __ffs(hit) - 1 : 0;
+        out->b = hit ? from : a.B;
+        out->unit0 = __shfl_sync(0xffffffffu, p.unit0, from);
+        out->group0 = __shfl_sync(0xffffffffu, p.group0, from);
+        out->item0 = __shfl_sync(0xffffffffu, p.item0, from);
+        return tot;
+    }
     const int run = (a.B + blockDim.x - 1) / blockDim.x;
     const int b0 = min(a.B, t * run), b1 = min(a.B, b0 + run);
-    if (t == 0) sc->bad = 0;
+    if (t == 0) {
+        sc->bad = 0;
+        sc->place = Place{a.B, 0, 0, 0};
+    }
     __syncthreads();
-    int64_t s[4] = {0, 0, 0, 0};
+    int s[3] = {0, 0, 0};
+    int64_t slots = 0;
     for (int b = b0; b < b1; ++b) {
         if (!seq_ok(a, b)) {
             sc->bad = 1;
             break;
         }
         const SeqShape q = seq_shape(a, b);
-        s[0] += q.units(a.c.Hkv);
-        s[1] += (int64_t)a.c.Hkv * q.nrb;
-        s[2] += q.items(a.c.Hkv);
-        s[3] += q.len;
+        s[0] += q.units(Hkv);
+        s[1] += q.groups(Hkv);
+        s[2] += q.items(Hkv);
+        slots += q.len;
     }
-    int64_t inc[4];
+    int inc[3];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        inc[k] = s[k];
-        if (warp * 32 * run < a.B) {  // warps without sequences have nothing to add
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t x = __shfl_up_sync(0xffffffffu, inc[k], o);
-                if (lane >= o) inc[k] += x;
-            }
-        }
+    for (int k = 0; k < 3; ++k) {
+        inc[k] = scan_lanes(s[k], lane);
         if (lane == 31) sc->sum[k][warp] = inc[k];
     }
+    for (int o = 16; o > 0; o >>= 1) slots += __shfl_xor_sync(0xffffffffu, slots, o);
+    if (lane == 0) sc->slots[warp] = slots;
     __syncthreads();
-    if (t < 4) {
-        int64_t sum = 0;
-        for (int w = 0; w < n_warps; ++w) {
-            const int64_t x = sc->sum[t][w];
-            sc->sum[t][w] = sum;
-            sum += x;
-        }
-        sc->sum[t][32] = sum;
+    // every warp adds up the warps before it
+    int before[3], all[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const int x = scan_lanes(lane < n_warps ? sc->sum[k][lane] : 0, lane);
+        all[k] = __shfl_sync(0xffffffffu, x, 31);
+        const int y = __shfl_sync(0xffffffffu, x, warp > 0 ? warp - 1 : 0);
+        before[k] = warp > 0 ? y : 0;
+    }
+    slots = lane < n_warps ? sc->slots[lane] : 0;
+    for (int o = 16; o > 0; o >>= 1) slots += __shfl_xor_sync(0xffffffffu, slots, o);
+    const PlanTotals tot{all[0], all[1], all[2], sc->bad == 0 && slots <= a.n_slots};
+    if (!tot.ok) {
+        if (t == 0) report(a.status, ESTP_ERR_INVALID_ARG);
+        return tot;
+    }
+    Place p{b0, before[0] + inc[0] - s[0], before[1] + inc[1] - s[1], before[2] + inc[2] - s[2]};
+    while (p.b < b1) {
+        const SeqShape q = seq_shape(a, p.b);
+        if (want(p, q, tot)) sc->place = p;
+        p.pass(q, Hkv);
     }
     __syncthreads();
-    const PlanTotals tot{sc->sum[0][32], sc->sum[1][32], sc->sum[2][32],
-                         sc->bad == 0 && sc->sum[3][32] <= a.n_slots};
-    if (!tot.ok && t == 0) report(a.status, ESTP_ERR_INVALID_ARG);
-    if (tot.ok) {
-        Place p{0, sc->sum[0][warp] + inc[0] - s[0], sc->sum[1][warp] + inc[1] - s[1],
-                sc->sum[2][warp] + inc[2] - s[2]};
-        for (int b = b0; b < b1; ++b) {
-            const SeqShape q = seq_shape(a, b);
-            p.b = b;
-            visit(p, q, tot);
-            p.unit0 += q.units(a.c.Hkv);
-            p.group0 += (int64_t)a.c.Hkv * q.nrb;
-            p.item0 += q.items(a.c.Hkv);
-        }
-    }
-    __syncthreads();
+    *out = sc->place;
     return tot;
 }
 
-// The CTAs that get units (each at least one), and the CTA that holds unit u when G CTAs share
-// `total` units: CTA c holds [c total / G, (c + 1) total / G).
-__device__ __forceinline__ int64_t ctas_of(const CacheAttnArgs& a, int64_t total) {
-    return total < a.G ? total : a.G;
+// `total` cut into G shares that differ by one at most: the first of share c, and the share of x.
+__device__ __forceinline__ int share_begin(int c, int total, int G) { return c * (total / G) + min(c, total % G); }
+__device__ __forceinline__ int share_of(int x, int total, int G) {
+    const int each = total / G, more = total % G, wide = more * (each + 1);
+    return x < wide ? x / (each + 1) : more + (x - wide) / each;
 }
-__device__ __forceinline__ int64_t unit_begin(int64_t c, int64_t total, int64_t G) { return c * total / G; }
-__device__ __forceinline__ int64_t cta_of(int64_t u, int64_t total, int64_t G) { return ((u + 1) * G - 1) / total; }
+// CTAs of the forward that get units, each at least one.
+__device__ __forceinline__ int ctas_of(const CacheAttnArgs& a, int total) { return min(total, a.G); }
+
+// (-M, c / L) of a row: a row without keys, or of factor 0, has a factor of 0 and is left out.
+__device__ __forceinline__ float2 weight_factor(const CacheAttnArgs& a, float2 x, int64_t row) {
+    const float cw = a.row_weight != nullptr ? a.row_weight[row] : 1.f;
+    const bool none = cw == 0.f || (x.x == -INFINITY && x.y == 0.f);
+    return none ? make_float2(0.f, 0.f) : make_float2(x.x == -INFINITY ? 0.f : -x.x, cw / x.y);
+}
 
 // Which of the rows first .. first + nr - 1 (nr <= 64) of a (b, KV head) see draft j of the sequence's
 // n drafts (from row0): bit r for row first + r, which is draft (first + r) / rep.

@@ -112,7 +112,6 @@ __device__ __forceinline__ void dots(const float (*q)[D], const char* k, float* 
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs a) {
     __shared__ PlanScratch sc;
-    __shared__ Place place;
     __shared__ float q[kRows][D];
     __shared__ float p[kRows][kCacheTile];
     __shared__ const char* vrow[kCacheTile];
@@ -120,29 +119,26 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
     __shared__ float o_half[kRows][D];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    const int64_t c = blockIdx.x;
-    const PlanTotals tot = plan_block(a, &sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
-        const int64_t u = unit_begin(c, all.units, ctas_of(a, all.units));
-        if (u >= x.unit0 && u < x.unit0 + s.units(a.c.Hkv)) place = x;
+    const int c = blockIdx.x;
+    Place at;
+    const PlanTotals tot = plan(a, &sc, &at, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int u = share_begin(c, all.units, ctas_of(a, all.units));
+        return u >= x.unit0 && u < x.unit0 + s.units(a.c.Hkv);
     });
-    const int64_t G = ctas_of(a, tot.units);
+    const int G = ctas_of(a, tot.units);
     if (!tot.ok || c >= G) return;
-    int64_t u = unit_begin(c, tot.units, G);
-    const int64_t u1 = unit_begin(c + 1, tot.units, G);
-    Place at = place;
+    int u = share_begin(c, tot.units, G);
+    const int u1 = share_begin(c + 1, tot.units, G);
     constexpr int kHalves = kThreads / D, kKeys = kCacheTile / kHalves;  // PV: threads of a column, keys of each
     const int col = t % D, half = t / D;
     while (u < u1) {
         const SeqShape s = seq_shape(a, at.b);
         if (u >= at.unit0 + s.units(a.c.Hkv)) {
-            at.unit0 += s.units(a.c.Hkv);
-            at.group0 += (int64_t)a.c.Hkv * s.nrb;
-            ++at.b;
+            at.pass(s, a.c.Hkv);
             continue;
         }
-        const int64_t loc = u - at.unit0;
-        const int grp = (int)(loc / s.nt), tile0 = (int)(loc % s.nt);
-        const int tile1 = (int)min((int64_t)s.nt, tile0 + (u1 - u));
+        const int loc = u - at.unit0, grp = loc / s.nt, tile0 = loc % s.nt;
+        const int tile1 = min(s.nt, tile0 + (u1 - u));
         const int g = grp / s.nrb, r0 = grp % s.nrb * kRows, nr = min(kRows, s.n * a.rep - r0);
         const int64_t row0 = a.cu[at.b];
         __syncthreads();
@@ -171,7 +167,7 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
             for (int r = 0; r < kRows; ++r)
                 if (hidden >> r & 1) z[r] = -INFINITY;
             if (a.store)
-                for (int r = 0; r < nr; ++r) a.score[(u * kRows + r) * kCacheTile + t] = z[r];
+                for (int r = 0; r < nr; ++r) a.score[((int64_t)u * kRows + r) * kCacheTile + t] = z[r];
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
                 float x = z[r];
@@ -241,11 +237,10 @@ struct Pieces {
     int n;          // the others RB apart
 };
 __device__ __forceinline__ Pieces pieces_of(const CacheAttnArgs& a, const Place& at, const SeqShape& s, int g, int r,
-                                            int64_t units) {
-    const int64_t grp = (int64_t)g * s.nrb + r / a.RB, ub = at.unit0 + grp * s.nt;
-    const int64_t G = ctas_of(a, units);
-    const int64_t c0 = cta_of(ub, units, G), c1 = cta_of(ub + s.nt - 1, units, G);
-    return Pieces{(c0 + at.group0 + grp) * a.KS * a.RB + r % a.RB, (int)(c1 - c0 + 1) * a.KS};
+                                            int units) {
+    const int grp = g * s.nrb + r / a.RB, ub = at.unit0 + grp * s.nt, G = ctas_of(a, units);
+    const int c0 = share_of(ub, units, G), c1 = share_of(ub + s.nt - 1, units, G);
+    return Pieces{(int64_t)(c0 + at.group0 + grp) * a.KS * a.RB + r % a.RB, (c1 - c0 + 1) * a.KS};
 }
 
 // Joins (M, L) with another running maximum and sum.  Unfused products: two lanes that join each
@@ -269,88 +264,87 @@ __device__ __forceinline__ float2 merged_ml(const CacheAttnArgs& a, const Pieces
 
 // Walks a CTA's share [it, it1) of the call's items (b, KV head, tile) in runs of one (b, KV head).
 template <class Run>
-__device__ __forceinline__ void for_items(const CacheAttnArgs& a, Place at, int64_t it, int64_t it1, Run run) {
+__device__ __forceinline__ void for_items(const CacheAttnArgs& a, Place at, int it, int it1, Run run) {
     while (it < it1) {
         const SeqShape s = seq_shape(a, at.b);
         if (it >= at.item0 + s.items(a.c.Hkv)) {
-            at.unit0 += s.units(a.c.Hkv);
-            at.group0 += (int64_t)a.c.Hkv * s.nrb;
-            at.item0 += s.items(a.c.Hkv);
-            ++at.b;
+            at.pass(s, a.c.Hkv);
             continue;
         }
-        const int g = (int)((it - at.item0) / s.nt), tile0 = (int)((it - at.item0) % s.nt);
-        const int tile1 = (int)min((int64_t)s.nt, tile0 + (it1 - it));
+        const int g = (it - at.item0) / s.nt, tile0 = (it - at.item0) % s.nt;
+        const int tile1 = min(s.nt, tile0 + (it1 - it));
         run(at, s, g, tile0, tile1);
         it += tile1 - tile0;
     }
 }
 
-// (-M, c / L) of a row: a row without keys, or of factor 0, has a factor of 0 and is left out.
-__device__ __forceinline__ float2 weight_factor(const CacheAttnArgs& a, float2 x, int64_t row) {
-    const float cw = a.row_weight != nullptr ? a.row_weight[row] : 1.f;
-    const bool none = cw == 0.f || (x.x == -INFINITY && x.y == 0.f);
-    return none ? make_float2(0.f, 0.f) : make_float2(x.x == -INFINITY ? 0.f : -x.x, cw / x.y);
-}
-
-// The first a.row_blocks blocks merge the partials: o and lse, a warp a (row, head), cut evenly over
-// them; without kept scores they leave (-M, c / L) of every row for the kernel that forms the scores
+// The first a.row_blocks blocks merge the partials: o and lse, a block a (row, head), cut evenly over
+// them (a row of one long sequence has a partial of every CTA: a warp a row took 17 us with 76); without kept scores they leave (-M, c / L) of every row for the kernel that forms the scores
 // again.  With kept scores the other blocks add the weights, the (b, KV head, tile) items cut evenly
 // over them: a warp a tile, a lane 4 keys.
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnArgs a) {
     __shared__ PlanScratch sc;
-    __shared__ Place place;
     __shared__ float2 ml[kCacheMaxStored];  // (-M, c / L) of every row of (b, g)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const bool for_rows = (int)blockIdx.x < a.row_blocks;
-    const int64_t c = for_rows ? blockIdx.x : blockIdx.x - a.row_blocks;
-    const int64_t G = for_rows ? a.row_blocks : gridDim.x - a.row_blocks;
-    const int64_t x0 = unit_begin(c, a.n_rows * a.Hq, G), x1 = unit_begin(c + 1, a.n_rows * a.Hq, G);
-    const PlanTotals tot = plan_block(a, &sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
-        if (for_rows) {
-            const int64_t y = (int64_t)a.cu[x.b] * a.Hq;
-            if (x0 >= y && x0 < y + (int64_t)s.n * a.Hq) place = x;
-        } else {
-            const int64_t it = unit_begin(c, all.items, G);
-            if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) place = x;
-        }
+    const int c = for_rows ? blockIdx.x : blockIdx.x - a.row_blocks;
+    const int G = for_rows ? a.row_blocks : gridDim.x - a.row_blocks, rows = (int)a.n_rows * a.Hq;
+    const int x0 = share_begin(c, rows, G), x1 = share_begin(c + 1, rows, G);
+    Place at;
+    const PlanTotals tot = plan(a, &sc, &at, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int y = a.cu[x.b] * a.Hq, it = share_begin(c, all.items, G);
+        return for_rows ? x0 >= y && x0 < y + s.n * a.Hq : it >= x.item0 && it < x.item0 + s.items(a.c.Hkv);
     });
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the partials are complete
     if (!tot.ok) return;
     if (for_rows) {
         if (x0 >= x1) return;
-        Place at = place;
+        // a block a row: its warps take the pieces in turn, 8 in flight, and are added in order
+        __shared__ float part[kThreads / 32][D];
+        constexpr int kC = D / 32;
         SeqShape s = seq_shape(a, at.b);
-        for (int64_t x = x0 + warp; x < x1; x += kThreads / 32) {
-            while (x >= (int64_t)a.cu[at.b + 1] * a.Hq) {
-                at.unit0 += s.units(a.c.Hkv);
-                at.group0 += (int64_t)a.c.Hkv * s.nrb;
-                ++at.b;
+        for (int x = x0; x < x1; ++x) {
+            while (x >= a.cu[at.b + 1] * a.Hq) {
+                at.pass(s, a.c.Hkv);
                 s = seq_shape(a, at.b);
             }
             const int64_t row = x / a.Hq;
-            const int h = (int)(x % a.Hq), i = (int)(row - a.cu[at.b]), r = i * a.rep + h % a.rep;
+            const int h = x % a.Hq, i = (int)row - a.cu[at.b], r = i * a.rep + h % a.rep;
             const Pieces w = pieces_of(a, at, s, h / a.rep, r, tot.units);
+            if (a.whole && w.n == a.KS) continue;
             const float2 all = merged_ml(a, w, lane);
-            constexpr int kC = D / 32;
             float o[kC];
 #pragma unroll
             for (int k = 0; k < kC; ++k) o[k] = 0.f;
-#pragma unroll 4
-            for (int p = 0; p < w.n; ++p) {
-                const int64_t e = w.first + (int64_t)p * a.RB;
-                const float m = a.part_ml[e].x;
-                const float f = m == all.x ? 1.f : ex2(m - all.x);
+            for (int p0 = warp; p0 < w.n; p0 += 8 * (kThreads / 32)) {
+                float m[8], v[8][kC];
 #pragma unroll
-                for (int k = 0; k < kC; ++k) o[k] = fmaf(f, a.part_o[e * D + k * 32 + lane], o[k]);
+                for (int u = 0; u < 8; ++u) {
+                    const int p = p0 + u * (kThreads / 32);
+                    const int64_t e = w.first + (int64_t)p * a.RB;
+                    m[u] = p < w.n ? a.part_ml[e].x : -INFINITY;
+#pragma unroll
+                    for (int k = 0; k < kC; ++k) v[u][k] = p < w.n ? a.part_o[e * D + k * 32 + lane] : 0.f;
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const float f = m[u] == all.x ? 1.f : ex2(m[u] - all.x);
+#pragma unroll
+                    for (int k = 0; k < kC; ++k) o[k] = fmaf(f, v[u][k], o[k]);
+                }
             }
-            const float inv = all.x == -INFINITY && all.y == 0.f ? 0.f : 1.f / all.y;
-            char* to = a.out + (row * a.Hq + h) * D * (int64_t)sizeof(T);
+            __syncthreads();  // the row before is written
 #pragma unroll
-            for (int k = 0; k < kC; ++k) Unit<T>::put(to + (k * 32 + lane) * sizeof(T), o[k] * inv);
-            if (lane == 0) {
+            for (int k = 0; k < kC; ++k) part[warp][k * 32 + lane] = o[k];
+            __syncthreads();
+            const float inv = all.x == -INFINITY && all.y == 0.f ? 0.f : 1.f / all.y;
+            if (t < D) {
+                const float sum = (part[0][t] + part[1][t]) + (part[2][t] + part[3][t]);
+                Unit<T>::put(a.out + ((row * a.Hq + h) * D + t) * (int64_t)sizeof(T), sum * inv);
+            }
+            if (t == 0) {
                 if (a.lse != nullptr)
                     a.lse[(int64_t)h * a.n_rows + row] = all.y == 0.f ? -INFINITY : fmaf(all.x, kLn2, logf(all.y));
                 if (a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, all, row);
@@ -358,19 +352,24 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
         }
         return;
     }
-    for_items(a, place, unit_begin(c, tot.items, G), unit_begin(c + 1, tot.items, G),
+    for_items(a, at, share_begin(c, tot.items, G), share_begin(c + 1, tot.items, G),
               [&](const Place& at, const SeqShape& s, int g, int tile0, int tile1) {
         const int64_t row0 = a.cu[at.b];
         const int R = s.n * a.rep;
+        if (a.whole && pieces_of(a, at, s, g, 0, tot.units).n == a.KS) return;  // (kept scores: one block of rows)
         __syncthreads();
         for (int rw = warp * 4; rw < R; rw += kThreads / 8) {  // 8 lanes a row
             const int r = rw + (lane >> 3);
             float M = -INFINITY, L = 0.f;
             if (r < R) {
                 const Pieces w = pieces_of(a, at, s, g, r, tot.units);
-                for (int p = lane & 7; p < w.n; p += 8) {
-                    const float2 x = a.part_ml[w.first + (int64_t)p * a.RB];
-                    merge_ml(M, L, x);
+                for (int p0 = lane & 7; p0 < w.n; p0 += 32) {  // 4 in flight
+                    float2 x[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        x[u] = p0 + 8 * u < w.n ? a.part_ml[w.first + (int64_t)(p0 + 8 * u) * a.RB] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) merge_ml(M, L, x[u]);
                 }
             }
             for (int o = 4; o > 0; o >>= 1) {
@@ -397,7 +396,7 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int k = 0; k < s.nrb; ++k) {
                 const int r0 = k * a.RB, nr = min(a.RB, R - r0);
-                const int64_t u = at.unit0 + ((int64_t)g * s.nrb + k) * s.nt + tile;
+                const int64_t u = at.unit0 + (g * s.nrb + k) * s.nt + tile;
                 const float4* z = reinterpret_cast<const float4*>(a.score + u * a.RB * kCacheTile) + lane;
                 auto one = [&](float x, float2 f, float& s1) {
                     if (x != -INFINITY) s1 = fmaf(ex2(fmaf(x, a.scale_log2, f.x)), f.y, s1);
@@ -435,18 +434,18 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnArgs a) {
     __shared__ PlanScratch sc;
-    __shared__ Place place;
     __shared__ float q[kRows][D];
     __shared__ float2 ml[kRows];
     const int t = threadIdx.x;
-    const int64_t c = blockIdx.x, G = gridDim.x;
-    const PlanTotals tot = plan_block(a, &sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
-        const int64_t it = unit_begin(c, all.items, G);
-        if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) place = x;
+    const int c = blockIdx.x, G = gridDim.x;
+    Place at;
+    const PlanTotals tot = plan(a, &sc, &at, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int it = share_begin(c, all.items, G);
+        return it >= x.item0 && it < x.item0 + s.items(a.c.Hkv);
     });
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the factors are complete
     if (!tot.ok) return;
-    for_items(a, place, unit_begin(c, tot.items, G), unit_begin(c + 1, tot.items, G),
+    for_items(a, at, share_begin(c, tot.items, G), share_begin(c + 1, tot.items, G),
               [&](const Place& at, const SeqShape& s, int g, int tile0, int tile1) {
         const int64_t row0 = a.cu[at.b];
         const int R = s.n * a.rep;
@@ -502,6 +501,7 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     a.RB = kRows;
     a.KS = 1;
     if (kTc) cache_tc_shape(a.max_rows * a.rep, &a.RB, &a.KS);
+    a.whole = kTc;
     a.G = kTc ? ctx->num_sms : ctx->num_sms * 8;
     const int64_t groups = (int64_t)a.c.Hkv * (a.n_rows * a.rep / a.RB + a.B);
     const int64_t slots = a.G + groups;
@@ -509,6 +509,8 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     // largest sequence
     const int64_t nrb = ((int64_t)a.max_rows * a.rep + a.RB - 1) / a.RB;
     const int64_t units = (int64_t)a.c.Hkv * nrb * (a.n_slots / kCacheTile + 2 * (int64_t)a.B);
+    if (units > INT32_MAX || a.n_rows * a.Hq > INT32_MAX)
+        return fail(ESTP_ERR_UNSUPPORTED, "max_slots and rows: more than 2^31 tiles of work, or rows times heads");
     const size_t o_bytes = align_up(sizeof(float) * (size_t)slots * a.KS * a.RB * D, 256);
     const size_t ml_bytes = align_up(sizeof(float2) * (size_t)slots * a.KS * a.RB, 256);
     const size_t z_bytes = sizeof(float) * (size_t)units * a.RB * kCacheTile;
@@ -535,8 +537,8 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
         e = cudaGetLastError();
         if (e != cudaSuccess) return cuda_fail(e, "cache attention launch");
     }
-    // a warp a (row, head) up to 4 blocks an SM; the items of kept scores over up to 12 more
-    const int64_t row_blocks = (a.n_rows * a.Hq + kThreads / 32 - 1) / (kThreads / 32), some = 4 * ctx->num_sms;
+    // a block a (row, head) up to 4 an SM; the items of kept scores over up to 12 more
+    const int64_t row_blocks = a.n_rows * a.Hq, some = 4 * ctx->num_sms;
     a.row_blocks = (int)(row_blocks < some ? row_blocks : some);
     const int64_t items = (int64_t)a.c.Hkv * (a.n_slots / kCacheTile + 2 * (int64_t)a.B), many = 12 * ctx->num_sms;
     const int item_blocks = a.store ? (int)(items < many ? items : many) : 0;

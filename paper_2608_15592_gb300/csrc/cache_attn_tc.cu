@@ -49,13 +49,14 @@ struct Shape {
     static constexpr int kAtoms = D / 64;
     static constexpr int kTileBytes = kAtoms * kAtom;
     static constexpr int kQRows = KS == 2 ? kN : 2 * RB;          // rows of a block
-    static constexpr int kQBufs = KS;                             // the next segment's Q loads ahead
+    static constexpr int kQBufs = RB == 64 ? 1 : 2;               // two: the next segment's Q loads ahead
+    static constexpr int kRowArrays = KS == 2 ? 6 : 3;            // [RB] floats a group keeps
     static constexpr int kQBytes = kAtoms * kQRows * 128;
     // P: [128 keys] rows of 128 bytes, hi then lo; 64 rows take two, up to 16 share one between the groups
     static constexpr int kPStep = RB == 64 ? 2 * kAtom : RB == 32 ? kAtom : 64;  // from a group's P to the other's
     static constexpr int kPBytes = RB == 64 ? 4 * kAtom : RB == 32 ? 2 * kAtom : kAtom;
     static constexpr int kFixed = kQBufs * kQBytes + kPBytes;
-    static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 400 - kGroups * (RB == 64 ? 3 : 7) * RB * 4;
+    static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 400 - kGroups * (kRowArrays + (RB == 64 ? 0 : 4)) * RB * 4;
     static constexpr int kStages = kRoom / kTileBytes < 12 ? kRoom / kTileBytes : 12;
     static constexpr int kThreads = 128 + 128 * kGroups;
     static constexpr int kTmemUsed = kGroups * (2 * kN + 2 * RB);  // S twice, O hi and lo
@@ -69,8 +70,8 @@ struct Shape {
     static constexpr int kBarOff = kRedOff + (RB == 64 ? 0 : kGroups * 4 * RB * 4);
     static constexpr int kBars = 2 * kStages + 2 * kQBufs + 6 * kGroups + 2;
     static constexpr int kMiscOff = kBarOff + (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, poison bits
-    static constexpr int kRowOff = kMiscOff + 48;  // a group's [RB] m, [RB] factors, [RB] -m
-    static constexpr int kSmem = kRowOff + kGroups * 3 * RB * 4 + 1024;
+    static constexpr int kRowOff = kMiscOff + 48;  // a group's row arrays
+    static constexpr int kSmem = kRowOff + kGroups * kRowArrays * RB * 4 + 1024;
     static_assert(kStages >= 4 && kSmem <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -105,13 +106,25 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* v) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[k]);
 }
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, float* v) {
+    uint32_t r[4];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(taddr));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(r[k]);
+}
+template <int N>
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float* v) {
+    if (N == 4) tmem_ld4(taddr, v);
+    else if (N == 8) tmem_ld8(taddr, v);
+    else tmem_ld16(taddr, v);
+}
 // Orders every later use of v[0..N) after the wait for the load that fills them.
 template <int N>
 __device__ __forceinline__ void tie(float* v) {
 #pragma unroll
-    for (int k = 0; k < N; k += 8)
-        asm volatile("" : "+f"(v[k]), "+f"(v[k + 1]), "+f"(v[k + 2]), "+f"(v[k + 3]), "+f"(v[k + 4]), "+f"(v[k + 5]),
-                          "+f"(v[k + 6]), "+f"(v[k + 7]));
+    for (int k = 0; k < N; k += 4) asm volatile("" : "+f"(v[k]), "+f"(v[k + 1]), "+f"(v[k + 2]), "+f"(v[k + 3]));
 }
 
 __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
@@ -139,6 +152,19 @@ __device__ __forceinline__ bool group_or(int id, bool x) {
         "selp.u32 %0, 1, 0, q;\n\t}"
         : "=r"(r)
         : "r"((uint32_t)x), "r"(id)
+        : "memory");
+    return r != 0;
+}
+// The same for both groups.
+__device__ __forceinline__ bool both_groups_or(bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.aligned.pred q, 3, 256, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)x)
         : "memory");
     return r != 0;
 }
@@ -177,26 +203,22 @@ __device__ __forceinline__ float reduce_scatter(const float* z, int lane, Op op)
 struct Segment {
     SeqShape s;
     int b, g, r0, nr, tile0, tile1;
-    int64_t group;
+    int group;
 };
 // Walks the segments of units [u, u1); every role of the CTA walks them by itself.
 struct Walk {
     Place at;
-    int64_t u, u1;
+    int u, u1;
     __device__ __forceinline__ bool next(const CacheAttnArgs& a, Segment& o) {
         while (u < u1) {
             o.s = seq_shape(a, at.b);
-            const int64_t units = o.s.units(a.c.Hkv);
-            if (u >= at.unit0 + units) {
-                at.unit0 += units;
-                at.group0 += (int64_t)a.c.Hkv * o.s.nrb;
-                ++at.b;
+            if (u >= at.unit0 + o.s.units(a.c.Hkv)) {
+                at.pass(o.s, a.c.Hkv);
                 continue;
             }
-            const int64_t loc = u - at.unit0;
-            const int grp = (int)(loc / o.s.nt);
-            o.tile0 = (int)(loc % o.s.nt);
-            o.tile1 = (int)min((int64_t)o.s.nt, o.tile0 + (u1 - u));
+            const int loc = u - at.unit0, grp = loc / o.s.nt;
+            o.tile0 = loc % o.s.nt;
+            o.tile1 = min(o.s.nt, o.tile0 + (u1 - u));
             o.b = at.b;
             o.g = grp / o.s.nrb;
             o.r0 = grp % o.s.nrb * a.RB;
@@ -327,26 +349,23 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     tc_fence_before();
-    const int64_t cta = blockIdx.x;
-    // the plan's scratch lies in the ring, which is unused until the barrier below
-    PlanScratch* sc = reinterpret_cast<PlanScratch*>(sm);
-    Place* place = reinterpret_cast<Place*>(sm + 1088);
-    static_assert(sizeof(PlanScratch) <= 1088, "scratch of the plan");
-    const PlanTotals tot = plan_block(a, sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
-        const int64_t u = unit_begin(cta, all.units, ctas_of(a, all.units));
-        if (u >= x.unit0 && u < x.unit0 + s.units(a.c.Hkv)) *place = x;
-    });
+    __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
-    const int64_t G = ctas_of(a, tot.units);
+    const int cta = blockIdx.x;
+    // the plan's scratch lies in the ring, which is unused until the barrier below
     Walk walk{Place{0, 0, 0, 0}, 0, 0};
-    if (tot.ok && cta < G) {
-        walk.at = *place;
-        walk.u = unit_begin(cta, tot.units, G);
-        walk.u1 = unit_begin(cta + 1, tot.units, G);
+    Place place;
+    const PlanTotals tot = plan(a, reinterpret_cast<PlanScratch*>(sm), &place, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int u = share_begin(cta, all.units, ctas_of(a, all.units));
+        return u >= x.unit0 && u < x.unit0 + s.units(a.c.Hkv);
+    });
+    const uint32_t tmem = *tmem_slot;
+    const int G = ctas_of(a, tot.units);
+    if (tot.ok && cta < G) walk = Walk{place, share_begin(cta, tot.units, G), share_begin(cta + 1, tot.units, G)};
+    if (a.B > 32) {  // the plan used its scratch
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
     }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncthreads();  // the ring is the copies' from here
     Segment sg;
 
     if (warp == 0 || warp == 3) {
@@ -495,18 +514,18 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
         // ------------------------------------------------------------- epilogue
         const int nb = (warp - 4) >> 2, q = warp & 3, bar = 1 + nb;
         const int j = q * 32 + lane;                 // key of the tile; lane of S and O
-        float* row_m = reinterpret_cast<float*>(sm + S::kRowOff) + nb * 3 * RB;  // m, log2 units
-        float* row_f = row_m + RB;
+        float* row_m = reinterpret_cast<float*>(sm + S::kRowOff) + nb * S::kRowArrays * RB;  // m, log2 units
+        float* row_f = row_m + RB;                   // rescaling factors; l at the end of a segment
         float* row_n = row_f + RB;                   // -m, or 0 where m is -inf
         uint8_t* pb = sm + S::kPOff;
         // [4][RB], used when the P buffer is free
         float* row_w = RB == 64 ? reinterpret_cast<float*>(pb + nb * S::kPStep)
                                 : reinterpret_cast<float*>(sm + S::kRedOff) + nb * 4 * RB;
-        // 16-byte chunk c of key k's P row
-        auto p_chunk = [&](int k, int c) {
-            if (RB == 64) return pb + nb * S::kPStep + (c >> 3) * kAtom + k * 128 + (((c & 7) ^ (k & 7)) << 4);
-            if (RB == 32) return pb + nb * S::kPStep + k * 128 + ((c ^ (k & 7)) << 4);
-            return pb + k * 128 + (((nb * (S::kPStep / 16) + c) ^ (k & 7)) << 4);
+        // 16-byte chunk c of key k's P row of a group
+        auto p_chunk = [&](int group, int k, int c) {
+            if (RB == 64) return pb + group * S::kPStep + (c >> 3) * kAtom + k * 128 + (((c & 7) ^ (k & 7)) << 4);
+            if (RB == 32) return pb + group * S::kPStep + k * 128 + ((c ^ (k & 7)) << 4);
+            return pb + k * 128 + (((group * (S::kPStep / 16) + c) ^ (k & 7)) << 4);
         };
         const uint32_t lane_off = (uint32_t)(q * 32) << 16;
         const uint32_t t_o = tmem + lane_off + (uint32_t)(S::kOCol + nb * 2 * RB);
@@ -544,10 +563,8 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                 float z[RB];
                 auto load_s = [&]() {
 #pragma unroll
-                    for (int r = 0; r < RB; r += kCols) {
-                        if (kCols == 8) tmem_ld8(tmem + lane_off + (2 * nb + buf) * S::kN + r, z + r);
-                        else tmem_ld16(tmem + lane_off + (2 * nb + buf) * S::kN + r, z + r);
-                    }
+                    for (int r = 0; r < RB; r += kCols)
+                        tmem_ld_cols<kCols>(tmem + lane_off + (2 * nb + buf) * S::kN + r, z + r);
                     tmem_wait_ld();
                     tie<RB>(z);
                     if (drafts || keys < kCacheTile) {
@@ -558,7 +575,7 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                 };
                 load_s();
                 if (a.store && alive) {
-                    float* to = a.score + ((walk.u - (sg.tile1 - tile)) * a.RB + base) * kCacheTile + j;
+                    float* to = a.score + ((int64_t)(walk.u - (sg.tile1 - tile)) * a.RB + base) * kCacheTile + j;
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
                         if (r < nr) to[r * kCacheTile] = z[r];
@@ -644,8 +661,8 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                     h.y = pack_hi_lo(z[r + 2], z[r + 3], lo.y);
                     h.z = pack_hi_lo(z[r + 4], z[r + 5], lo.z);
                     h.w = pack_hi_lo(z[r + 6], z[r + 7], lo.w);
-                    *reinterpret_cast<uint4*>(p_chunk(j, r / 8)) = h;
-                    *reinterpret_cast<uint4*>(p_chunk(j, (r + RB) / 8)) = lo;
+                    *reinterpret_cast<uint4*>(p_chunk(nb, j, r / 8)) = h;
+                    *reinterpret_cast<uint4*>(p_chunk(nb, j, (r + RB) / 8)) = lo;
                 }
                 if ((KS == 2 || nb == 0) && (drafts || (keys & 15))) {
                     // V rows that must not reach the product: past the keys, and drafts that are not finite
@@ -685,50 +702,38 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
             t += sg.tile1 - sg.tile0;
             // the segment's partial
             if (step > 0) wait(&pv_done[nb], (step - 1) & 1);
-            if (group_or(bar, !alive)) break;  // the group leaves together
+            // a segment that is its whole group (both epilogue groups share it where KS = 2) is finished here
+            const bool whole = sg.tile0 == 0 && sg.tile1 == sg.s.nt;
+            if (KS == 2 ? both_groups_or(!alive) : group_or(bar, !alive)) break;  // who shares barriers leaves together
             tc_fence_after();
-            const int64_t part = ((cta + sg.group) * KS + (KS == 2 ? nb : 0)) * a.RB + base;
+            // drafts whose V is not finite were left out of O: their P is still in its buffer, row by row
+            if (sg.tile1 == sg.s.nt && (KS == 1 || ((sg.tile1 - 1 - sg.tile0) & 1) == nb) &&
+                (odd_drafts[0] | odd_drafts[1] | odd_drafts[2] | odd_drafts[3])) {
 #pragma unroll 1
-            for (int r = 0; r < RB; r += kCols) {
-                if (r >= nr) break;
-                float hi[kCols], lo[kCols];
-                if (kCols == 8) {
-                    tmem_ld8(t_o + r, hi);
-                    tmem_ld8(t_o + RB + r, lo);
-                } else {
-                    tmem_ld16(t_o + r, hi);
-                    tmem_ld16(t_o + RB + r, lo);
-                }
-                tmem_wait_ld();
-                tie<kCols>(hi);
-                tie<kCols>(lo);
-                if (D == 128 || q < 2) {
-#pragma unroll
-                    for (int k = 0; k < kCols; ++k) {
-                        if (r + k >= nr) break;
-                        a.part_o[(part + r + k) * D + j] = live ? hi[k] + lo[k] : 0.f;
-                    }
-                }
-            }
-            tc_fence_before();
-            if (sg.tile1 == sg.s.nt && (KS == 1 || ((sg.tile1 - 1 - sg.tile0) & 1) == nb) && (odd_drafts[0] | odd_drafts[1] | odd_drafts[2] | odd_drafts[3])) {
-                // drafts whose V is not finite: P is still in its buffer
-                if (D == 128 || q < 2) {
+                for (int r = 0; r < nr; ++r) {
+                    float s = 0.f;
                     for (int x = 0; x < sg.s.n; ++x) {
-                        if (!(odd_drafts[x >> 5] >> (x & 31) & 1)) continue;
-                        const uint64_t seen = rows_that_see(a, row0, sg.s.n, x, sg.r0 + base, nr);
+                        if ((D == 64 && q >= 2) || !(odd_drafts[x >> 5] >> (x & 31) & 1)) continue;
+                        if (!(rows_that_see(a, row0, sg.s.n, x, sg.r0 + base + r, 1) & 1)) continue;
                         const float v = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(
                             a.vn + (row0 + x) * a.ldn + (int64_t)sg.g * (D * 2) + j * 2));
-                        for (int r = 0; r < nr; ++r) {
-                            if (!(seen >> r & 1)) continue;
-                            const __nv_bfloat16* ph = reinterpret_cast<const __nv_bfloat16*>(p_chunk(x, r >> 3)) + (r & 7);
-                            const __nv_bfloat16* pl = reinterpret_cast<const __nv_bfloat16*>(p_chunk(x, (r + RB) >> 3)) + (r & 7);
-                            a.part_o[(part + r) * D + j] += (__bfloat162float(*ph) + __bfloat162float(*pl)) * v;
-                        }
+                        const __nv_bfloat16* ph = reinterpret_cast<const __nv_bfloat16*>(p_chunk(nb, x, r >> 3)) + (r & 7);
+                        const __nv_bfloat16* pl = reinterpret_cast<const __nv_bfloat16*>(p_chunk(nb, x, (r + RB) >> 3)) + (r & 7);
+                        s += (__bfloat162float(*ph) + __bfloat162float(*pl)) * v;
                     }
+                    __syncwarp();
+                    uint32_t o;
+                    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(o) : "r"(t_o + r));
+                    tmem_wait_ld();
+                    asm volatile("" : "+r"(o));
+                    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(t_o + r),
+                                 "r"(__float_as_uint(__uint_as_float(o) + s))
+                                 : "memory");
                 }
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                tc_fence_before();
             }
-            if (RB == 64) group_sync(bar);  // P is read
+            // l over the keys' threads, into row_f
             {
                 constexpr int kN = RB < 32 ? RB : 32;
                 const auto plus = [](float x, float y) { return x + y; };
@@ -741,12 +746,170 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                         v[k + 1] = l[(r + k) / 2].y;
                     }
                     const float x = reduce_scatter<kN>(v, lane, plus);
-                    if (lane < kN) row_w[q * RB + r + lane] = x;
+                    if (RB < 64) {
+                        if (lane < kN) row_w[q * RB + r + lane] = x;
+                    } else {
+                        l[r / 2].x = x;
+                    }
                 }
             }
-            group_sync(bar);
-            if (j < nr)
-                a.part_ml[part + j] = make_float2(row_m[j], (row_w[j] + row_w[RB + j]) + (row_w[2 * RB + j] + row_w[3 * RB + j]));
+            if (RB < 64) {
+                group_sync(bar);
+                if (j < RB) row_f[j] = (row_w[j] + row_w[RB + j]) + (row_w[2 * RB + j] + row_w[3 * RB + j]);
+            } else {  // row_w is the P buffer, which may be wanted yet: warp after warp
+#pragma unroll 1
+                for (int w = 0; w < 4; ++w) {
+                    if (q == w)
+#pragma unroll
+                        for (int r = 0; r < RB; r += 32) row_f[r + lane] = (w > 0 ? row_f[r + lane] : 0.f) + l[r / 2].x;
+                    group_sync(bar);
+                }
+            }
+            if (!whole) {
+                const int64_t part = ((int64_t)(cta + sg.group) * KS + (KS == 2 ? nb : 0)) * a.RB + base;
+                group_sync(bar);
+                if (j < nr) a.part_ml[part + j] = make_float2(row_m[j], row_f[j]);
+#pragma unroll 1
+                for (int r = 0; r < RB; r += kCols) {
+                    if (r >= nr) break;
+                    float hi[kCols], lo[kCols];
+                    tmem_ld_cols<kCols>(t_o + r, hi);
+                    tmem_ld_cols<kCols>(t_o + RB + r, lo);
+                    tmem_wait_ld();
+                    tie<kCols>(hi);
+                    tie<kCols>(lo);
+                    if (D == 128 || q < 2) {
+#pragma unroll
+                        for (int k = 0; k < kCols; ++k) {
+                            if (r + k >= nr) break;
+                            a.part_o[(part + r + k) * D + j] = live ? hi[k] + lo[k] : 0.f;
+                        }
+                    }
+                }
+            } else {
+                // wa, wb: what the groups' O count in o (a group without a key counts 0); -M; c / L
+                float* row_a = KS == 2 ? row_n + RB : row_f;
+                float* row_b = row_a + RB;
+                float* row_c = row_b + RB;
+                if (KS == 2) both_groups_or(false);
+                else group_sync(bar);
+                tc_fence_after();
+                if (j < RB) {
+                    float M = row_m[j], L = row_f[j], fa = 1.f, fb = 0.f;
+                    if (KS == 2) {
+                        const float* g0 = reinterpret_cast<const float*>(sm + S::kRowOff);
+                        const float ma = g0[j], mb = g0[S::kRowArrays * RB + j];
+                        M = fmaxf(ma, mb);
+                        fa = ma == -INFINITY ? 0.f : ex2(ma - M);
+                        fb = mb == -INFINITY ? 0.f : ex2(mb - M);
+                        // NaN stays where a group has no maximum either
+                        L = (fa != 0.f ? fa * g0[RB + j] : M == -INFINITY ? g0[RB + j] : 0.f) +
+                            (fb != 0.f ? fb * g0[S::kRowArrays * RB + RB + j] : M == -INFINITY ? g0[S::kRowArrays * RB + RB + j] : 0.f);
+                        if (L != L) fa = fb = 1.f;
+                    }
+                    const bool none = M == -INFINITY && L == 0.f;
+                    const float inv = none ? 0.f : 1.f / L;
+                    if ((KS == 1 || nb == 0) && j < nr) {
+                        const int rr = sg.r0 + base + j, h = sg.g * a.rep + rr % a.rep;
+                        const int64_t row = row0 + rr / a.rep;
+                        if (a.lse != nullptr) a.lse[(int64_t)h * a.n_rows + row] = L == 0.f ? -INFINITY : fmaf(M, kLn2, logf(L));
+                        if (a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, make_float2(M, L), row);
+                    }
+                    if (KS == 2) {
+                        const float2 f = j < nr ? weight_factor(a, make_float2(M, L), row0 + (sg.r0 + base + j) / a.rep) : make_float2(0.f, 0.f);
+                        row_a[j] = fa * inv;
+                        row_b[j] = fb * inv;
+                        row_n[j] = f.x;
+                        row_c[j] = f.y;
+                    } else {
+                        row_f[j] = none ? 0.f : inv;
+                    }
+                }
+                group_sync(bar);
+                // o of half the rows (KS = 2), or of the group's: lane = column
+                constexpr int kMine = KS == 2 ? RB / 2 : RB, kStep = kMine < 16 ? (kMine < 8 ? 4 : 8) : 16;
+                const uint32_t t_a = KS == 2 ? tmem + lane_off + (uint32_t)S::kOCol : t_o;
+#pragma unroll 1
+                for (int r = KS == 2 ? nb * kMine : 0, end = r + kMine; r < end; r += kStep) {
+                    if (r >= nr) break;
+                    float hi[kStep], lo[kStep], hb[kStep], lb[kStep];
+                    tmem_ld_cols<kStep>(t_a + r, hi);
+                    tmem_ld_cols<kStep>(t_a + RB + r, lo);
+                    if (KS == 2) {
+                        tmem_ld_cols<kStep>(t_a + 2 * RB + r, hb);
+                        tmem_ld_cols<kStep>(t_a + 3 * RB + r, lb);
+                    }
+                    tmem_wait_ld();
+                    tie<kStep>(hi);
+                    tie<kStep>(lo);
+                    if (KS == 2) {
+                        tie<kStep>(hb);
+                        tie<kStep>(lb);
+                    }
+                    if (D == 128 || q < 2) {
+#pragma unroll
+                        for (int k = 0; k < kStep; ++k) {
+                            if (r + k >= nr) break;
+                            const float wa = row_a[r + k], wb = KS == 2 ? row_b[r + k] : 0.f;
+                            float o = wa != 0.f && (KS == 2 || live) ? (hi[k] + lo[k]) * wa : 0.f;
+                            if (KS == 2 && wb != 0.f) o = fmaf(hb[k] + lb[k], wb, o);
+                            const int rr = sg.r0 + base + r + k, h = sg.g * a.rep + rr % a.rep;
+                            reinterpret_cast<__nv_bfloat16*>(a.out)[((row0 + rr / a.rep) * a.Hq + h) * D + j] = __float2bfloat16_rn(o);
+                        }
+                    }
+                }
+                tc_fence_before();
+                if (KS == 2) {
+                    both_groups_or(false);  // O is read: the next segment's may begin
+                    if (a.store) {
+                        // the weights of the tiles whose scores this thread kept
+                        constexpr int kAt = 2, kR = 8;  // tiles and rows in flight
+                        for (int tile = first; tile < sg.tile1; tile += kAt * KS) {
+                            float* to[kAt];
+                            float had[kAt], sum[kAt];
+#pragma unroll
+                            for (int i = 0; i < kAt; ++i) {
+                                const int tt = tile + i * KS;
+                                to[i] = nullptr;
+                                had[i] = sum[i] = 0.f;
+                                if (tt >= sg.tile1 || j >= tile_keys(a, sg.s, tt)) continue;
+                                if (tt == sg.s.nt - 1) {
+                                    if (a.w_new != nullptr) to[i] = a.w_new + (row0 + j) * a.c.Hkv + sg.g;
+                                } else if (a.accumulate) {
+                                    const int slot = tt * kCacheTile + j;
+                                    const int64_t page = a.c.page_of(sg.b, slot, a.status);
+                                    if (page >= 0) {
+                                        to[i] = a.c.weight + a.c.meta(page, slot, sg.g);
+                                        had[i] = *to[i];
+                                    }
+                                }
+                            }
+                            for (int r0 = 0; r0 < nr; r0 += kR) {
+                                float z[kAt][kR];
+#pragma unroll
+                                for (int i = 0; i < kAt; ++i) {
+                                    const float* from = a.score + ((int64_t)(walk.u - (sg.tile1 - tile - i * KS)) * a.RB + r0) * kCacheTile + j;
+#pragma unroll
+                                    for (int r = 0; r < kR; ++r)
+                                        z[i][r] = to[i] != nullptr && r0 + r < nr ? from[r * kCacheTile] : -INFINITY;
+                                }
+#pragma unroll
+                                for (int i = 0; i < kAt; ++i)
+#pragma unroll
+                                    for (int r = 0; r < kR; ++r) {
+                                        const float f = row_c[r0 + r];
+                                        if (f != 0.f && z[i][r] != -INFINITY)
+                                            sum[i] = fmaf(ex2(fmaf(z[i][r], a.scale_log2, row_n[r0 + r])), f, sum[i]);
+                                    }
+                            }
+#pragma unroll
+                            for (int i = 0; i < kAt; ++i)
+                                if (to[i] != nullptr) *to[i] = had[i] + sum[i];
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
             group_sync(bar);  // row_w, row_m and P are free for the next segment
         }
     }
@@ -799,38 +962,23 @@ struct WShape {
     static_assert(kRoom - kWRows / kWBlock * kBlockBytes >= kWMinStages * kTileBytes, "shared memory per CTA");
 };
 
-__device__ __forceinline__ bool both_groups_or(bool x) {
-    uint32_t r;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 p, %1, 0;\n\t"
-        "barrier.cta.red.or.aligned.pred q, 3, 256, p;\n\t"
-        "selp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(r)
-        : "r"((uint32_t)x)
-        : "memory");
-    return r != 0;
-}
-
 // Runs of one (b, KV head) in items [it, it1).
 struct ItemWalk {
     Place at;
-    int64_t it, it1;
+    int it, it1;
     SeqShape s;
     int b, g, tile0, tile1;
     __device__ __forceinline__ bool next(const CacheAttnArgs& a) {
         while (it < it1) {
             s = seq_shape(a, at.b);
-            const int64_t items = s.items(a.c.Hkv);
-            if (it >= at.item0 + items) {
-                at.item0 += items;
-                ++at.b;
+            if (it >= at.item0 + s.items(a.c.Hkv)) {
+                at.pass(s, a.c.Hkv);
                 continue;
             }
             b = at.b;
-            g = (int)((it - at.item0) / s.nt);
-            tile0 = (int)((it - at.item0) % s.nt);
-            tile1 = (int)min((int64_t)s.nt, tile0 + (it1 - it));
+            g = (it - at.item0) / s.nt;
+            tile0 = (it - at.item0) % s.nt;
+            tile1 = min(s.nt, tile0 + (it1 - it));
             it += tile1 - tile0;
             // tiles whose weight no one asks for
             if (!a.accumulate) tile0 = max(tile0, s.nt - 1);
@@ -878,23 +1026,25 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     tc_fence_before();
-    const int64_t cta = blockIdx.x, G = gridDim.x;
-    PlanScratch* sc = reinterpret_cast<PlanScratch*>(ring);  // in the ring, unused until the barrier below
-    Place* place = reinterpret_cast<Place*>(ring + 1088);
-    const PlanTotals tot = plan_block(a, sc, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
-        const int64_t it = unit_begin(cta, all.items, G);
-        if (it >= x.item0 && it < x.item0 + s.items(a.c.Hkv)) *place = x;
-    });
+    __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    const int cta = blockIdx.x, G = gridDim.x;
+    Place place;
+    const PlanTotals tot = plan(a, reinterpret_cast<PlanScratch*>(ring), &place, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int it = share_begin(cta, all.items, G);
+        return it >= x.item0 && it < x.item0 + s.items(a.c.Hkv);
+    });
     ItemWalk w{Place{0, 0, 0, 0}, 0, 0};
     if (tot.ok) {
-        w.it = unit_begin(cta, tot.items, G);
-        w.it1 = unit_begin(cta + 1, tot.items, G);
-        if (w.it < w.it1) w.at = *place;
+        w.it = share_begin(cta, tot.items, G);
+        w.it1 = share_begin(cta + 1, tot.items, G);
+        w.at = place;
     }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncthreads();
+    if (a.B > 32) {  // the plan used its scratch, in the ring
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the factors are complete
 
     if (warp == 0) {
