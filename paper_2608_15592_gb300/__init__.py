@@ -209,7 +209,7 @@ class KVCache:
         _like(position, torch.int32, (n_pages, Hkv, page), "position")
         self.k, self.v, self.page_table, self.length, self.seen = k, v, page_table, length, seen
         self.weight, self.position = weight, position
-        self.B = B
+        self.B, self._cu_shape = B, (B + 1,)
         self.Hkv, self.head_dim, self.dtype = Hkv, d, k.dtype
         bound = B * per * page
         if weight is not None:
@@ -221,6 +221,8 @@ class KVCache:
 
     def _rows(self, t, heads, name):
         """Row stride of a [rows, heads, d] tensor of the cache's type whose heads are contiguous."""
+        if t.dim() != 3:
+            raise ValueError(f"{name} is a {self.dtype} tensor [rows, {heads}, {self.head_dim}]")
         rows, h, d = t.shape
         s0, s1, s2 = t.stride()
         if h != heads or d != self.head_dim or t.dtype != self.dtype:
@@ -232,8 +234,8 @@ class KVCache:
     def _new_rows(self, k_new, v_new):
         """The row stride that new rows' K and V share."""
         ld = self._rows(k_new, self.Hkv, "k_new")
-        if v_new.shape != k_new.shape or self._rows(v_new, self.Hkv, "v_new") != ld:
-            raise ValueError("k_new and v_new share their shape and row stride")
+        if v_new.shape != k_new.shape or v_new.stride() != k_new.stride() or v_new.dtype != k_new.dtype:
+            raise ValueError("k_new and v_new share their type, shape and strides")
         return ld
 
 
@@ -476,7 +478,7 @@ class Context:
         ld = cache._new_rows(k_new, v_new)
         if weight is not None:
             _like(weight, torch.float32, (n, cache.Hkv), "weight")
-        _like(cu_rows, torch.int32, (cache.B + 1,), "cu_rows")
+        _like(cu_rows, torch.int32, cache._cu_shape, "cu_rows")
         if rows is not None:
             _like(rows, torch.int32, (rows.numel(),), "rows")
         length, seen = cache.length.data_ptr(), cache.seen.data_ptr()
@@ -501,7 +503,7 @@ class Context:
             if k_new.shape[0] != n or v_new.shape[0] != n:
                 raise ValueError("k_new and v_new have a row for each of Q's")
             ld, kp, vp = cache._new_rows(k_new, v_new), k_new.data_ptr(), v_new.data_ptr()
-        _like(cu_rows, torch.int32, (cache.B + 1,), "cu_rows")
+        _like(cu_rows, torch.int32, cache._cu_shape, "cu_rows")
         words = 0
         if tree_mask is not None:
             words = tree_mask.shape[-1]

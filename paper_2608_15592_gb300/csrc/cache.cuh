@@ -65,12 +65,13 @@ struct CacheAttnArgs {
     int RB, G;
     int KS;                      // partials of a segment
     int whole;                   // the forward finishes the groups that one CTA holds by itself
-    int row_blocks;              // blocks of the finish kernel that merge rows
+    int row_blocks;              // blocks of the finish kernel that merge rows, warps of one of them
+    int row_warps;
     int store;                   // scores are kept for the weights
     float* part_o;               // [G + groups][KS][RB][d]
     float2* part_ml;             // [G + groups][KS][RB]: running max (log2 units) and sum
     float* score;                // [units][RB][128], unscaled
-    float2* factor;              // [n_rows, Hq]: (-M, c / L), where scores are formed again
+    float2* factor;              // [n_rows, Hq]: (-M, c / L), where the weights are wanted
     char* out;
     float* lse;
     float* w_new;
@@ -257,7 +258,7 @@ __device__ __forceinline__ uint64_t rows_that_see(const CacheAttnArgs& a, int64_
 // The tensor-core forward of bf16 caches: rows of a block and partials of a segment for a call's
 // rows of a (b, KV head), and the launch.
 void cache_tc_shape(int rows, int* RB, int* KS);
-estp_status launch_cache_fwd_tc(const CacheAttnArgs& a, cudaStream_t st);
+estp_status launch_cache_fwd_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_attention(estp_ctx* ctx, CacheAttnArgs& a, estp_dtype dtype, cudaStream_t st);
 estp_status launch_cache_append(estp_ctx* ctx, const CacheView& c, int row_bytes, int B, const int32_t* length,

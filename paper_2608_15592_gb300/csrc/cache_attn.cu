@@ -278,14 +278,14 @@ __device__ __forceinline__ void for_items(const CacheAttnArgs& a, Place at, int 
     }
 }
 
-// The first a.row_blocks blocks merge the partials: o and lse, a block a (row, head), cut evenly over
-// them (a row of one long sequence has a partial of every CTA: a warp a row took 17 us with 76); without kept scores they leave (-M, c / L) of every row for the kernel that forms the scores
+// The first a.row_blocks blocks merge the partials: o and lse, a warp or a block a (row, head), cut
+// evenly over them; without kept scores they leave (-M, c / L) of every row for the kernel that forms the scores
 // again.  With kept scores the other blocks add the weights, the (b, KV head, tile) items cut evenly
-// over them: a warp a tile, a lane 4 keys.
+// over their warps: a warp a tile, a lane 4 keys.
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnArgs a) {
+__global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAttnArgs a) {
     __shared__ PlanScratch sc;
-    __shared__ float2 ml[kCacheMaxStored];  // (-M, c / L) of every row of (b, g)
+    __shared__ float2 ml[kThreads / 32][kCacheMaxStored];  // a warp's (-M, c / L) of every row of (b, g)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const bool for_rows = (int)blockIdx.x < a.row_blocks;
@@ -301,11 +301,11 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
     if (!tot.ok) return;
     if (for_rows) {
         if (x0 >= x1) return;
-        // a block a row: its warps take the pieces in turn, 8 in flight, and are added in order
         __shared__ float part[kThreads / 32][D];
         constexpr int kC = D / 32;
         SeqShape s = seq_shape(a, at.b);
-        for (int x = x0; x < x1; ++x) {
+        const int wide = a.row_warps;  // warps of a row: they take its pieces in turn, 8 in flight, and are added in order
+        for (int x = x0 + (wide == 1 ? warp : 0); x < x1; x += wide == 1 ? kThreads / 32 : 1) {
             while (x >= a.cu[at.b + 1] * a.Hq) {
                 at.pass(s, a.c.Hkv);
                 s = seq_shape(a, at.b);
@@ -318,11 +318,11 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
             float o[kC];
 #pragma unroll
             for (int k = 0; k < kC; ++k) o[k] = 0.f;
-            for (int p0 = warp; p0 < w.n; p0 += 8 * (kThreads / 32)) {
+            for (int p0 = wide == 1 ? 0 : warp; p0 < w.n; p0 += 8 * wide) {
                 float m[8], v[8][kC];
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
-                    const int p = p0 + u * (kThreads / 32);
+                    const int p = p0 + u * wide;
                     const int64_t e = w.first + (int64_t)p * a.RB;
                     m[u] = p < w.n ? a.part_ml[e].x : -INFINITY;
 #pragma unroll
@@ -335,16 +335,19 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
                     for (int k = 0; k < kC; ++k) o[k] = fmaf(f, v[u][k], o[k]);
                 }
             }
-            __syncthreads();  // the row before is written
-#pragma unroll
-            for (int k = 0; k < kC; ++k) part[warp][k * 32 + lane] = o[k];
-            __syncthreads();
             const float inv = all.x == -INFINITY && all.y == 0.f ? 0.f : 1.f / all.y;
-            if (t < D) {
-                const float sum = (part[0][t] + part[1][t]) + (part[2][t] + part[3][t]);
-                Unit<T>::put(a.out + ((row * a.Hq + h) * D + t) * (int64_t)sizeof(T), sum * inv);
+            char* to = a.out + (row * a.Hq + h) * D * (int64_t)sizeof(T);
+            if (wide == 1) {
+#pragma unroll
+                for (int k = 0; k < kC; ++k) Unit<T>::put(to + (k * 32 + lane) * sizeof(T), o[k] * inv);
+            } else {
+                __syncthreads();  // the row before is written
+#pragma unroll
+                for (int k = 0; k < kC; ++k) part[warp][k * 32 + lane] = o[k];
+                __syncthreads();
+                if (t < D) Unit<T>::put(to + t * sizeof(T), ((part[0][t] + part[1][t]) + (part[2][t] + part[3][t])) * inv);
             }
-            if (t == 0) {
+            if (lane == 0 && (wide == 1 || warp == 0)) {
                 if (a.lse != nullptr)
                     a.lse[(int64_t)h * a.n_rows + row] = all.y == 0.f ? -INFINITY : fmaf(all.x, kLn2, logf(all.y));
                 if (a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, all, row);
@@ -352,73 +355,81 @@ __global__ void __launch_bounds__(kThreads) cache_finish_kernel(const CacheAttnA
         }
         return;
     }
-    for_items(a, at, share_begin(c, tot.items, G), share_begin(c + 1, tot.items, G),
+    // every warp for itself: an equal part of the block's items
+    const int it0 = share_begin(c, tot.items, G), part = share_begin(c + 1, tot.items, G) - it0;
+    float2* f = ml[warp];
+    for_items(a, at, it0 + share_begin(warp, part, kThreads / 32), it0 + share_begin(warp + 1, part, kThreads / 32),
               [&](const Place& at, const SeqShape& s, int g, int tile0, int tile1) {
         const int64_t row0 = a.cu[at.b];
         const int R = s.n * a.rep;
-        if (a.whole && pieces_of(a, at, s, g, 0, tot.units).n == a.KS) return;  // (kept scores: one block of rows)
-        __syncthreads();
-        for (int rw = warp * 4; rw < R; rw += kThreads / 8) {  // 8 lanes a row
-            const int r = rw + (lane >> 3);
-            float M = -INFINITY, L = 0.f;
-            if (r < R) {
-                const Pieces w = pieces_of(a, at, s, g, r, tot.units);
-                for (int p0 = lane & 7; p0 < w.n; p0 += 32) {  // 4 in flight
-                    float2 x[4];
+        __syncwarp();
+        if (a.whole && pieces_of(a, at, s, g, 0, tot.units).n == a.KS) {  // (kept scores of bf16: one block of rows)
+            for (int r = lane; r < R; r += 32) f[r] = a.factor[(row0 + r / a.rep) * a.Hq + g * a.rep + r % a.rep];
+        } else {
+            for (int rw = 0; rw < R; rw += 4) {  // 8 lanes a row
+                const int r = rw + (lane >> 3);
+                float M = -INFINITY, L = 0.f;
+                if (r < R) {
+                    const Pieces w = pieces_of(a, at, s, g, r, tot.units);
+                    for (int p0 = lane & 7; p0 < w.n; p0 += 32) {  // 4 in flight
+                        float2 x[4];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        x[u] = p0 + 8 * u < w.n ? a.part_ml[w.first + (int64_t)(p0 + 8 * u) * a.RB] : make_float2(-INFINITY, 0.f);
+                        for (int u = 0; u < 4; ++u)
+                            x[u] = p0 + 8 * u < w.n ? a.part_ml[w.first + (int64_t)(p0 + 8 * u) * a.RB] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) merge_ml(M, L, x[u]);
+                        for (int u = 0; u < 4; ++u) merge_ml(M, L, x[u]);
+                    }
                 }
+                for (int o = 4; o > 0; o >>= 1)
+                    merge_ml(M, L, make_float2(__shfl_xor_sync(0xffffffffu, M, o), __shfl_xor_sync(0xffffffffu, L, o)));
+                if (r < R && (lane & 7) == 0) f[r] = weight_factor(a, make_float2(M, L), row0 + r / a.rep);
             }
-            for (int o = 4; o > 0; o >>= 1) {
-                const float2 x = make_float2(__shfl_xor_sync(0xffffffffu, M, o), __shfl_xor_sync(0xffffffffu, L, o));
-                merge_ml(M, L, x);
-            }
-            if (r < R && (lane & 7) == 0) ml[r] = weight_factor(a, make_float2(M, L), row0 + r / a.rep);
         }
-        __syncthreads();
-        for (int tile = tile0 + warp; tile < tile1; tile += kThreads / 32) {
+        __syncwarp();
+        for (int tile = tile0; tile < tile1; ++tile) {
             const bool drafts = tile == s.nt - 1;
-            if (drafts ? a.w_new == nullptr : !a.accumulate) continue;
-            const int n = (drafts ? (a.kn != nullptr ? s.n : 0) : s.len - tile * kCacheTile) - lane * 4;
+            const int slot = tile * kCacheTile + lane * 4;
+            const int n = (drafts ? (a.kn != nullptr && a.w_new != nullptr ? s.n : 0)
+                                  : (a.accumulate ? s.len - tile * kCacheTile : 0)) - lane * 4;
             if (n <= 0) continue;
             float* to = nullptr;
-            float4 had = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (!drafts) {
-                const int slot = tile * kCacheTile + lane * 4;  // 4 slots of one page
+            float4 had = make_float4(0.f, 0.f, 0.f, 0.f), sum = had;
+            if (!drafts) {  // 4 slots of one page
                 const int64_t page = a.c.page_of(at.b, slot, a.status);
                 if (page < 0) continue;
                 to = a.c.weight + a.c.meta(page, slot, g);
                 if (n >= 4) had = *reinterpret_cast<const float4*>(to);
             }
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            auto one = [&](float x, float2 y, float& s1) {
+                if (x != -INFINITY) s1 = fmaf(ex2(fmaf(x, a.scale_log2, y.x)), y.y, s1);
+            };
             for (int k = 0; k < s.nrb; ++k) {
                 const int r0 = k * a.RB, nr = min(a.RB, R - r0);
-                const int64_t u = at.unit0 + (g * s.nrb + k) * s.nt + tile;
-                const float4* z = reinterpret_cast<const float4*>(a.score + u * a.RB * kCacheTile) + lane;
-                auto one = [&](float x, float2 f, float& s1) {
-                    if (x != -INFINITY) s1 = fmaf(ex2(fmaf(x, a.scale_log2, f.x)), f.y, s1);
-                };
-#pragma unroll 8
-                for (int r = 0; r < nr; ++r) {
-                    const float2 f = ml[r0 + r];
-                    const float4 x = z[r * (kCacheTile / 4)];
-                    if (f.y != 0.f) {
-                        one(x.x, f, sum.x);
-                        one(x.y, f, sum.y);
-                        one(x.z, f, sum.z);
-                        one(x.w, f, sum.w);
+                const int u = at.unit0 + (g * s.nrb + k) * s.nt + tile;
+                const float4* z = reinterpret_cast<const float4*>(a.score + (int64_t)u * a.RB * kCacheTile) + lane;
+                constexpr int kBatch = 8;  // rows in flight
+                for (int q0 = 0; q0 < nr; q0 += kBatch) {
+                    float4 x[kBatch];
+#pragma unroll
+                    for (int r = 0; r < kBatch; ++r)
+                        if (q0 + r < nr) x[r] = z[(q0 + r) * (kCacheTile / 4)];
+#pragma unroll
+                    for (int r = 0; r < kBatch; ++r) {
+                        const float2 y = q0 + r < nr ? f[r0 + q0 + r] : make_float2(0.f, 0.f);
+                        if (y.y == 0.f) continue;
+                        one(x[r].x, y, sum.x);
+                        one(x[r].y, y, sum.y);
+                        one(x[r].z, y, sum.z);
+                        one(x[r].w, y, sum.w);
                     }
                 }
             }
             if (drafts) {
-                float* w = a.w_new + (row0 + lane * 4) * a.c.Hkv + g;
-                w[0] = sum.x;
-                if (n > 1) w[a.c.Hkv] = sum.y;
-                if (n > 2) w[2 * a.c.Hkv] = sum.z;
-                if (n > 3) w[3 * a.c.Hkv] = sum.w;
+                float* d = a.w_new + (row0 + lane * 4) * a.c.Hkv + g;
+                d[0] = sum.x;
+                if (n > 1) d[a.c.Hkv] = sum.y;
+                if (n > 2) d[2 * a.c.Hkv] = sum.z;
+                if (n > 3) d[3 * a.c.Hkv] = sum.w;
             } else if (n >= 4) {
                 *reinterpret_cast<float4*>(to) = make_float4(had.x + sum.x, had.y + sum.y, had.z + sum.z, had.w + sum.w);
             } else {
@@ -520,27 +531,32 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     const int64_t R = (int64_t)a.max_rows * a.rep;
     a.store = weights && R <= kCacheMaxStored && R * 8 <= (int64_t)(D * sizeof(T)) && z_bytes <= (size_t(2) << 30);
     const bool again = weights && !a.store;
-    const size_t more = a.store ? z_bytes : again ? sizeof(float2) * (size_t)(a.n_rows * a.Hq) : 0;
+    const size_t f_bytes = weights ? align_up(sizeof(float2) * (size_t)(a.n_rows * a.Hq), 256) : 0;
+    const size_t more = f_bytes + (a.store ? z_bytes : 0);
     estp_status s = ws_reserve(ctx, o_bytes + ml_bytes + more);
     if (s != ESTP_OK) return s;
     char* ws = static_cast<char*>(ctx->ws);
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(ws + o_bytes);
-    a.score = a.store ? reinterpret_cast<float*>(ws + o_bytes + ml_bytes) : nullptr;
-    a.factor = again ? reinterpret_cast<float2*>(ws + o_bytes + ml_bytes) : nullptr;
+    a.factor = weights ? reinterpret_cast<float2*>(ws + o_bytes + ml_bytes) : nullptr;
+    a.score = a.store ? reinterpret_cast<float*>(ws + o_bytes + ml_bytes + f_bytes) : nullptr;
     cudaError_t e;
     if constexpr (kTc) {
-        s = launch_cache_fwd_tc(a, st);
+        s = launch_cache_fwd_tc(ctx, a, st);
         if (s != ESTP_OK) return s;
     } else {
         cache_fwd_kernel<T, D><<<(unsigned)a.G, kThreads, 0, st>>>(a);
         e = cudaGetLastError();
         if (e != cudaSuccess) return cuda_fail(e, "cache attention launch");
     }
-    // a block a (row, head) up to 4 an SM; the items of kept scores over up to 12 more
-    const int64_t row_blocks = a.n_rows * a.Hq, some = 4 * ctx->num_sms;
+    // Few rows have many partials each (28 rows of one 32K sequence have 76: 17 us for a warp a row, 4 for
+    // a block); many rows keep the GPU busy a warp each (6600 rows: 14 us, 30 for a block).  One wave of 8
+    // blocks an SM: 2 for them, 6 for the items of kept scores.
+    const int64_t some = 2 * ctx->num_sms;
+    a.row_warps = a.n_rows * a.Hq <= some ? kThreads / 32 : 1;
+    const int64_t row_blocks = (a.n_rows * a.Hq * a.row_warps + kThreads / 32 - 1) / (kThreads / 32);
     a.row_blocks = (int)(row_blocks < some ? row_blocks : some);
-    const int64_t items = (int64_t)a.c.Hkv * (a.n_slots / kCacheTile + 2 * (int64_t)a.B), many = 12 * ctx->num_sms;
+    const int64_t items = (int64_t)a.c.Hkv * (a.n_slots / kCacheTile + 2 * (int64_t)a.B), many = 6 * ctx->num_sms;
     const int item_blocks = a.store ? (int)(items < many ? items : many) : 0;
     e = launch_dependent(cache_finish_kernel<T, D>, a.row_blocks + item_blocks, kThreads, 0, a, st);
     if (e != cudaSuccess) return cuda_fail(e, "cache attention finish launch");

@@ -50,7 +50,7 @@ struct Shape {
     static constexpr int kTileBytes = kAtoms * kAtom;
     static constexpr int kQRows = KS == 2 ? kN : 2 * RB;          // rows of a block
     static constexpr int kQBufs = RB == 64 ? 1 : 2;               // two: the next segment's Q loads ahead
-    static constexpr int kRowArrays = KS == 2 ? 6 : 3;            // [RB] floats a group keeps
+    static constexpr int kRowArrays = KS == 2 ? 5 : 3;            // [RB] floats a group keeps
     static constexpr int kQBytes = kAtoms * kQRows * 128;
     // P: [128 keys] rows of 128 bytes, hi then lo; 64 rows take two, up to 16 share one between the groups
     static constexpr int kPStep = RB == 64 ? 2 * kAtom : RB == 32 ? kAtom : 64;  // from a group's P to the other's
@@ -787,10 +787,9 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                     }
                 }
             } else {
-                // wa, wb: what the groups' O count in o (a group without a key counts 0); -M; c / L
+                // what the groups' O count in o (a group without a key counts 0)
                 float* row_a = KS == 2 ? row_n + RB : row_f;
                 float* row_b = row_a + RB;
-                float* row_c = row_b + RB;
                 if (KS == 2) both_groups_or(false);
                 else group_sync(bar);
                 tc_fence_after();
@@ -815,15 +814,8 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                         if (a.lse != nullptr) a.lse[(int64_t)h * a.n_rows + row] = L == 0.f ? -INFINITY : fmaf(M, kLn2, logf(L));
                         if (a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, make_float2(M, L), row);
                     }
-                    if (KS == 2) {
-                        const float2 f = j < nr ? weight_factor(a, make_float2(M, L), row0 + (sg.r0 + base + j) / a.rep) : make_float2(0.f, 0.f);
-                        row_a[j] = fa * inv;
-                        row_b[j] = fb * inv;
-                        row_n[j] = f.x;
-                        row_c[j] = f.y;
-                    } else {
-                        row_f[j] = none ? 0.f : inv;
-                    }
+                    row_a[j] = fa * inv;
+                    if (KS == 2) row_b[j] = fb * inv;
                 }
                 group_sync(bar);
                 // o of half the rows (KS = 2), or of the group's: lane = column
@@ -859,55 +851,7 @@ __global__ void __launch_bounds__(Shape<D, RB, KS>::kThreads, 1)
                     }
                 }
                 tc_fence_before();
-                if (KS == 2) {
-                    both_groups_or(false);  // O is read: the next segment's may begin
-                    if (a.store) {
-                        // the weights of the tiles whose scores this thread kept
-                        constexpr int kAt = 2, kR = 8;  // tiles and rows in flight
-                        for (int tile = first; tile < sg.tile1; tile += kAt * KS) {
-                            float* to[kAt];
-                            float had[kAt], sum[kAt];
-#pragma unroll
-                            for (int i = 0; i < kAt; ++i) {
-                                const int tt = tile + i * KS;
-                                to[i] = nullptr;
-                                had[i] = sum[i] = 0.f;
-                                if (tt >= sg.tile1 || j >= tile_keys(a, sg.s, tt)) continue;
-                                if (tt == sg.s.nt - 1) {
-                                    if (a.w_new != nullptr) to[i] = a.w_new + (row0 + j) * a.c.Hkv + sg.g;
-                                } else if (a.accumulate) {
-                                    const int slot = tt * kCacheTile + j;
-                                    const int64_t page = a.c.page_of(sg.b, slot, a.status);
-                                    if (page >= 0) {
-                                        to[i] = a.c.weight + a.c.meta(page, slot, sg.g);
-                                        had[i] = *to[i];
-                                    }
-                                }
-                            }
-                            for (int r0 = 0; r0 < nr; r0 += kR) {
-                                float z[kAt][kR];
-#pragma unroll
-                                for (int i = 0; i < kAt; ++i) {
-                                    const float* from = a.score + ((int64_t)(walk.u - (sg.tile1 - tile - i * KS)) * a.RB + r0) * kCacheTile + j;
-#pragma unroll
-                                    for (int r = 0; r < kR; ++r)
-                                        z[i][r] = to[i] != nullptr && r0 + r < nr ? from[r * kCacheTile] : -INFINITY;
-                                }
-#pragma unroll
-                                for (int i = 0; i < kAt; ++i)
-#pragma unroll
-                                    for (int r = 0; r < kR; ++r) {
-                                        const float f = row_c[r0 + r];
-                                        if (f != 0.f && z[i][r] != -INFINITY)
-                                            sum[i] = fmaf(ex2(fmaf(z[i][r], a.scale_log2, row_n[r0 + r])), f, sum[i]);
-                                    }
-                            }
-#pragma unroll
-                            for (int i = 0; i < kAt; ++i)
-                                if (to[i] != nullptr) *to[i] = had[i] + sum[i];
-                        }
-                    }
-                }
+                if (KS == 2) both_groups_or(false);  // O is read: the next segment's may begin
             }
             tc_fence_before();
             group_sync(bar);  // row_w, row_m and P are free for the next segment
@@ -1241,9 +1185,10 @@ estp_status rows_map(CUtensorMap* m, const CacheAttnArgs& a, const void* base, i
 }
 
 template <int D, int RB, int KS>
-estp_status launch(const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int new_rows, cudaStream_t st) {
+estp_status launch(estp_ctx* ctx, const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int new_rows, cudaStream_t st) {
     using S = Shape<D, RB, KS>;
-    cudaError_t e = cudaFuncSetAttribute(cache_fwd_tc_kernel<D, RB, KS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    constexpr int kBit = 2 + (D == 128 ? 8 : 0) + (RB == 8 ? 0 : RB == 16 ? 1 : RB == 32 ? 2 : KS == 2 ? 3 : 4);
+    cudaError_t e = set_smem(ctx, kBit, cache_fwd_tc_kernel<D, RB, KS>, S::kSmem);
     if (e != cudaSuccess) return cuda_fail(e, "cache attention smem attribute");
     cache_fwd_tc_kernel<D, RB, KS><<<(unsigned)a.G, S::kThreads, S::kSmem, st>>>(tm, a, box_rows, new_rows);
     e = cudaGetLastError();
@@ -1251,13 +1196,13 @@ estp_status launch(const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int n
 }
 
 template <int D>
-estp_status launch_rows(const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int new_rows, cudaStream_t st) {
+estp_status launch_rows(estp_ctx* ctx, const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int new_rows, cudaStream_t st) {
     switch (a.RB) {
-        case 8: return launch<D, 8, 2>(tm, a, box_rows, new_rows, st);
-        case 16: return launch<D, 16, 2>(tm, a, box_rows, new_rows, st);
-        case 32: return launch<D, 32, 2>(tm, a, box_rows, new_rows, st);
-        case 64: return launch<D, 64, 2>(tm, a, box_rows, new_rows, st);
-        default: return launch<D, 64, 1>(tm, a, box_rows, new_rows, st);
+        case 8: return launch<D, 8, 2>(ctx, tm, a, box_rows, new_rows, st);
+        case 16: return launch<D, 16, 2>(ctx, tm, a, box_rows, new_rows, st);
+        case 32: return launch<D, 32, 2>(ctx, tm, a, box_rows, new_rows, st);
+        case 64: return launch<D, 64, 2>(ctx, tm, a, box_rows, new_rows, st);
+        default: return launch<D, 64, 1>(ctx, tm, a, box_rows, new_rows, st);
     }
 }
 
@@ -1279,12 +1224,12 @@ static estp_status make_maps(const CacheAttnArgs& a, TcMaps* tm, int* box_rows, 
     return s;
 }
 
-estp_status launch_cache_fwd_tc(const CacheAttnArgs& a, cudaStream_t st) {
+estp_status launch_cache_fwd_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st) {
     TcMaps tm;
     int box_rows, new_rows;
     const estp_status s = make_maps(a, &tm, &box_rows, &new_rows);
     if (s != ESTP_OK) return s;
-    return a.c.d == 128 ? launch_rows<128>(tm, a, box_rows, new_rows, st) : launch_rows<64>(tm, a, box_rows, new_rows, st);
+    return a.c.d == 128 ? launch_rows<128>(ctx, tm, a, box_rows, new_rows, st) : launch_rows<64>(ctx, tm, a, box_rows, new_rows, st);
 }
 
 estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st) {
@@ -1296,7 +1241,7 @@ estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaSt
     const int rows = a.max_rows * a.rep < kWRows ? a.max_rows * a.rep : kWRows, blocks = (rows + kWBlock - 1) / kWBlock;
     const int smem = a.c.d == 128 ? WShape<128>::smem(blocks) : WShape<64>::smem(blocks);
     const int stages = a.c.d == 128 ? WShape<128>::stages(blocks) : WShape<64>::stages(blocks);
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    cudaError_t e = set_smem(ctx, a.c.d == 128 ? 31 : 30, kernel, 227 * 1024);
     if (e != cudaSuccess) return cuda_fail(e, "cache weight smem attribute");
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

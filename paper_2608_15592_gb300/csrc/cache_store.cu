@@ -468,8 +468,7 @@ estp_status launch_cache_evict(estp_ctx* ctx, const CacheView& c, int row_bytes,
     a.done = ctx->done;
     a.status = ctx->status;
     const size_t smem = sizeof(uint32_t) * ((size_t)a.key_cap + kRounds * kBins);
-    cudaError_t e = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)((max_keys + kRounds * kBins) * 4));
+    cudaError_t e = set_smem(ctx, 0, evict_kernel, (size_t)(max_keys + kRounds * kBins) * 4);
     if (e != cudaSuccess) return cuda_fail(e, "cache evict smem attribute");
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;

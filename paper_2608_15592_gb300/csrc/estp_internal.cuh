@@ -30,6 +30,7 @@ struct estp_ctx {
     uint32_t imp_flags = 0;     // flags of the opening call (divisor variant, self term)
     uint32_t* pool_done = nullptr;      // per-prompt arrival counters of the pooling kernel
     int32_t pool_done_cap = 0;
+    uint32_t smem_set = 0;      // cache kernels whose shared memory limit is set on the device, a bit each
     // limit of the attention kernels' abortable waits (estp_set_wait_limit)
     long long wait_cycles = kWaitCycles;
 };
@@ -51,6 +52,15 @@ estp_status fail(estp_status st, const char* fmt, ...);
 estp_status cuda_fail(cudaError_t e, const char* what);
 estp_status ws_reserve(estp_ctx* ctx, size_t bytes);
 estp_status set_device(estp_ctx* ctx);
+
+// Raises a kernel's dynamic shared memory limit, once a context (`bit` is the kernel's own).
+template <class Kernel>
+cudaError_t set_smem(estp_ctx* ctx, int bit, Kernel kernel, size_t bytes) {
+    if (ctx->smem_set >> bit & 1) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) ctx->smem_set |= 1u << bit;
+    return e;
+}
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
