@@ -255,10 +255,10 @@ __device__ __forceinline__ uint64_t rows_that_see(const CacheAttnArgs& a, int64_
     return rows;
 }
 
-// The tensor-core forward of bf16 caches: rows of a block and partials of a segment for a call's
-// rows of a (b, KV head), and the launch.
-void cache_tc_shape(int rows, int* RB, int* KS);
+// The tensor-core forwards of bf16 caches: keys on the lanes (up to 32 rows a (b, KV head)), rows on the
+// lanes (more).
 estp_status launch_cache_fwd_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
+estp_status launch_cache_rows_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_attention(estp_ctx* ctx, CacheAttnArgs& a, estp_dtype dtype, cudaStream_t st);
 estp_status launch_cache_append(estp_ctx* ctx, const CacheView& c, int row_bytes, int B, const int32_t* length,

@@ -14,7 +14,7 @@
 // third launch.  No floating-point atomics: every sum has one order.
 //
 // A row that sees nothing (M = -inf, L = 0) gives o = 0 and lse = -inf and no weight.
-#include "cache.cuh"
+#include "cache_tc.cuh"
 
 namespace estp {
 namespace {
@@ -489,29 +489,16 @@ __global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnA
     });
 }
 
-// A launch that may begin before the one ahead of it has ended (it waits where it needs it).
-template <class Kernel>
-cudaError_t launch_dependent(Kernel kernel, int grid, int threads, size_t smem, const CacheAttnArgs& a, cudaStream_t st) {
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
-    return e == cudaSuccess ? cudaGetLastError() : e;
-}
-
 template <class T, int D>
 estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     constexpr bool kTc = sizeof(T) == 2;
     a.RB = kRows;
     a.KS = 1;
-    if (kTc) cache_tc_shape(a.max_rows * a.rep, &a.RB, &a.KS);
+    if (kTc) {
+        const int rows = a.max_rows * a.rep;
+        a.RB = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
+        a.KS = a.RB <= 128 ? 2 : 1;
+    }
     a.whole = kTc;
     a.G = kTc ? ctx->num_sms : ctx->num_sms * 8;
     const int64_t groups = (int64_t)a.c.Hkv * (a.n_rows * a.rep / a.RB + a.B);
@@ -542,7 +529,7 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     a.score = a.store ? reinterpret_cast<float*>(ws + o_bytes + ml_bytes + f_bytes) : nullptr;
     cudaError_t e;
     if constexpr (kTc) {
-        s = launch_cache_fwd_tc(ctx, a, st);
+        s = a.RB <= 32 ? launch_cache_fwd_tc(ctx, a, st) : launch_cache_rows_tc(ctx, a, st);
         if (s != ESTP_OK) return s;
     } else {
         cache_fwd_kernel<T, D><<<(unsigned)a.G, kThreads, 0, st>>>(a);
@@ -558,13 +545,13 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     a.row_blocks = (int)(row_blocks < some ? row_blocks : some);
     const int64_t items = (int64_t)a.c.Hkv * (a.n_slots / kCacheTile + 2 * (int64_t)a.B), many = 6 * ctx->num_sms;
     const int item_blocks = a.store ? (int)(items < many ? items : many) : 0;
-    e = launch_dependent(cache_finish_kernel<T, D>, a.row_blocks + item_blocks, kThreads, 0, a, st);
+    e = launch_dependent(cache_finish_kernel<T, D>, a.row_blocks + item_blocks, kThreads, 0, st, a);
     if (e != cudaSuccess) return cuda_fail(e, "cache attention finish launch");
     if (!again) return ESTP_OK;
     if constexpr (kTc) {
         return launch_cache_weight_tc(ctx, a, st);
     } else {
-        e = launch_dependent(cache_weight_kernel<T, D>, ctx->num_sms * 8, kThreads, 0, a, st);
+        e = launch_dependent(cache_weight_kernel<T, D>, ctx->num_sms * 8, kThreads, 0, st, a);
         return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache weight launch");
     }
 }

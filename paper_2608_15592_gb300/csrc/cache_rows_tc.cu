@@ -1,0 +1,532 @@
+// The forward half of the cache attention (see cache_attn.cu) for bf16 caches and more than 32 rows a
+// (sequence, KV head), as wide draft trees give: the rows take the 128 lanes of an MMA.
+//   S = Q K^T          M = 128 rows, N = 128 keys, K = D, into TMEM
+//   P = 2^(S c - m)    a thread a row: the running maximum and sum need no exchange between lanes.
+//                      Each P is two bf16 terms, hi + lo (16 bits of it enter the second product), written
+//                      over the S that they come from: of every 32 columns, 16 of hi and 16 of lo
+//   O += hi V + lo V   A = P from TMEM, B = the V tile as it is stored (MN-major), into TMEM
+// (With the keys on the lanes, as cache_attn_tc.cu has them, 64 rows are 64 columns a thread: their
+// maxima over the lanes, l and P in registers cost 2.4 us a tile where the copies need 1.45.)
+//
+// A row's m only moves when a tile exceeds it by 2^8; the warps whose rows do then rescale O and l.
+//
+// One persistent CTA per SM over the units of cache.cuh, two epilogue groups of 128 threads, each with
+// an S/P buffer and an O (all 512 columns).  KS = 1: a block is 256 rows, 128 a group, and every tile
+// goes to both.  KS = 2: a block is 128 rows and the groups take the tiles in turn, each with a
+// partial of its own.  Either way one group's softmax runs under the other's products.
+//   warps 0, 2 TMA producers of the K and of the V tiles (one ring, K and V in turn)
+//   warp 1     issues the products; the pipe runs them in the order of issue, so the S that overwrites
+//              a P comes after the product that reads it
+//   warp 3     idle
+//   warps 4-11 the epilogue groups, which also load their rows' Q
+// Bound, at 256 rows, by the tensor pipe (1536 clocks a group and tile); at 128 by the copies.
+// Keys past a sequence's slots, drafts that are not finite and waits are treated as in
+// cache_attn_tc.cu.
+#include "cache_tc.cuh"
+
+namespace estp {
+namespace {
+
+template <int D, int KS>
+struct RowShape {
+    static constexpr int kRows = KS == 2 ? 128 : 256;
+    static constexpr int kAtoms = D / 64;
+    static constexpr int kTileBytes = kAtoms * kAtom;  // 128 keys, or 128 rows of Q
+    static constexpr int kQBytes = kRows / 128 * kTileBytes;
+    static constexpr int kRoom = 227 * 1024 - 1024 - kQBytes - 512;
+    static constexpr int kStages = kRoom / kTileBytes < 12 ? kRoom / kTileBytes : 12;
+    static constexpr int kThreads = 384;
+    static constexpr int kQOff = kStages * kTileBytes;
+    static constexpr int kBarOff = kQOff + kQBytes;
+    static constexpr int kBars = 2 * kStages + 9;
+    static constexpr int kMiscOff = kBarOff + (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, tiles issued, odd drafts
+    static constexpr int kSmem = kMiscOff + 48 + 1024;
+    static_assert(kStages >= 4 && kSmem <= 227 * 1024, "shared memory per CTA");
+};
+
+// D (TMEM) += A (TMEM) B, B an MN-major shared memory tile
+template <uint32_t kIdesc>
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b), "r"(kIdesc), "r"(acc));
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+        "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
+template <int D, int KS>
+__global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
+    cache_rows_tc_kernel(const __grid_constant__ TcMaps tm, const CacheAttnArgs a, const int box_rows, const int new_rows) {
+    using S = RowShape<D, KS>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + S::kBarOff);  // [kStages]
+    uint64_t* empty = full + S::kStages;                            // [kStages]
+    uint64_t* q_full = empty + S::kStages;                          // [2], KS = 2: the first
+    uint64_t* s_full = q_full + 2;                                  // [2]
+    uint64_t* p_full = s_full + 2;                                  // [2]
+    uint64_t* o_full = p_full + 2;                                  // [2]
+    uint64_t* drain = o_full + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::kMiscOff);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 4);
+    volatile int* issued_tiles = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 8);  // [2] K, V
+    volatile uint32_t* odd = reinterpret_cast<volatile uint32_t*>(sm + S::kMiscOff + 16);  // [2][4] drafts with V not finite
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], KS == 2 ? 8 : 4);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i], 4);
+            mbar_init(&o_full[i], 1);
+        }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int cta = blockIdx.x;
+    Walk walk{Place{0, 0, 0, 0}, 0, 0};
+    Place place;
+    const PlanTotals tot = plan(a, reinterpret_cast<PlanScratch*>(sm), &place, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+        const int u = share_begin(cta, all.units, ctas_of(a, all.units));
+        return u >= x.unit0 && u < x.unit0 + s.units(a.c.Hkv);
+    });
+    const int G = ctas_of(a, tot.units);
+    if (tot.ok && cta < G) walk = Walk{place, share_begin(cta, tot.units, G), share_begin(cta + 1, tot.units, G)};
+    if (a.B > 32) {  // the plan used its scratch, in the ring
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+    }
+    Segment sg;
+
+    if (warp == 0 || warp == 2) {
+        // ------------------------------------------------------------ producers
+        const int kv = warp == 2;
+        if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(
+                          kv ? (lane ? &tm.vn : &tm.v) : (lane ? &tm.kn : &tm.k))) : "memory");
+        uint32_t t = 0;
+        bool ok = true;
+        PageWindow win;
+        while (ok && walk.next(a, sg)) {
+            win.open(a, sg.s, sg.b, sg.tile0, lane);
+            for (int tile = sg.tile0; tile < sg.tile1; ++tile, ++t) {
+                const uint32_t e = 2 * t + kv, use = e / S::kStages;
+                const int slot = (int)(e % S::kStages);
+                if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
+                    ok = false;
+                    break;
+                }
+                load_tile<D>(a, kv ? &tm.v : &tm.k, kv ? &tm.vn : &tm.kn, win, sg.s, sg.b, sg.g, tile, box_rows, new_rows,
+                             sm + slot * S::kTileBytes, &full[slot], lane);
+            }
+        }
+        if (lane == 0) issued_tiles[kv] = (int)t;
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------------------------------------------------- MMA issuer
+        if (lane == 0) {
+            constexpr uint32_t kIdS = idesc_bf16(128, 128);
+            constexpr uint32_t kIdO = idesc_bf16(128, D) | (1u << 16);  // B MN-major
+            uint32_t t = 0, q_seen[2] = {0, 0}, p_seen[2] = {0, 0};
+            bool ok = true, issued = false;
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
+                return ok;
+            };
+            auto release = [&](uint32_t e) {
+                if (ok) mma_commit(&empty[e % S::kStages]);
+            };
+            while (ok && walk.next(a, sg)) {
+                const int tiles = sg.tile1 - sg.tile0, groups = KS == 2 ? 2 : (sg.nr + 127) / 128;
+                bool live[2] = {false, false};
+                auto product_s = [&](int i, int w) {  // S of the segment's tile i for group w
+                    const uint32_t e = 2 * (t + i);
+                    const int slot = (int)(e % S::kStages);
+                    if (i < KS && (KS == 1 || w == 0) && !wait(&q_full[w], q_seen[w]++ & 1)) return;
+                    if (!wait(&full[slot], (e / S::kStages) & 1)) return;
+                    tc_fence_after();
+                    issued = true;
+                    const uint32_t ka = smem_u32(sm + slot * S::kTileBytes);
+                    const uint32_t qa = smem_u32(sm + S::kQOff) + (KS == 1 ? w * S::kTileBytes : 0);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t off = (kk >> 2) * kAtom + (kk & 3) * 32;
+                        mma_bf16<kIdS>(tmem + w * 128, sw128_desc(qa + off), sw128_desc(ka + off), kk > 0 ? 1u : 0u);
+                    }
+                    mma_commit(&s_full[w]);
+                };
+                auto product_o = [&](int i, int w) {
+                    const uint32_t e = 2 * (t + i) + 1;
+                    const int slot = (int)(e % S::kStages);
+                    if (!wait(&full[slot], (e / S::kStages) & 1) || !wait(&p_full[w], p_seen[w]++ & 1)) return;
+                    tc_fence_after();
+                    issued = true;
+                    const uint32_t va = smem_u32(sm + slot * S::kTileBytes), p = tmem + w * 128, o = tmem + 256 + w * 128;
+                    const int ksteps = (tile_keys(a, sg.s, sg.tile0 + i) + 15) / 16;
+                    for (int kk = 0; kk < ksteps; ++kk) {
+                        const uint64_t v = mn_desc(va + kk * 2048, kAtom);
+                        const uint32_t at = p + (kk >> 1) * 32 + (kk & 1) * 8;
+                        mma_ts<kIdO>(o, at, v, live[w] || kk > 0 ? 1u : 0u);
+                        mma_ts<kIdO>(o, at + 16, v, 1u);
+                    }
+                    live[w] = live[w] || ksteps > 0;
+                    if (i + KS >= tiles) mma_commit(&o_full[w]);
+                };
+                if (KS == 2) {
+                    for (int i = 0; ok && i < 2 && i < tiles; ++i) {
+                        product_s(i, i);
+                        release(2 * (t + i));
+                    }
+                    for (int i = 0; ok && i < tiles; ++i) {
+                        product_o(i, i & 1);
+                        release(2 * (t + i) + 1);
+                        if (ok && i + 2 < tiles) {
+                            product_s(i + 2, i & 1);
+                            release(2 * (t + i + 2));
+                        }
+                    }
+                } else {
+                    for (int w = 0; ok && w < groups; ++w) product_s(0, w);
+                    release(2 * t);
+                    for (int i = 0; ok && i < tiles; ++i) {
+                        for (int w = 0; ok && w < groups; ++w) {
+                            product_o(i, w);
+                            if (w == groups - 1) release(2 * (t + i) + 1);
+                            if (ok && i + 1 < tiles) product_s(i + 1, w);
+                        }
+                        if (i + 1 < tiles) release(2 * (t + i + 1));
+                    }
+                }
+                t += tiles;
+            }
+            if (issued) {
+                mma_commit(drain);
+                drain_wait(drain, 0, a.status);
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------- epilogue
+        const int w = (warp - 4) >> 2, q = warp & 3, bar = 1 + w;
+        const int j = q * 32 + lane;  // lane of TMEM: row of the group; and V row that it may clear
+        const uint32_t lane_off = (uint32_t)(q * 32) << 16;
+        const uint32_t t_s = tmem + lane_off + w * 128, t_o = tmem + lane_off + 256 + w * 128;
+        uint32_t t = 0, seg = 0, steps = 0, ends = 0;
+        bool alive = true;
+        auto wait = [&](uint64_t* b, uint32_t parity) {
+            if (alive) alive = warp_wait(b, parity, abort_flag, a.status, a.wait_cycles);
+        };
+        while (walk.next(a, sg)) {
+            const int tiles = sg.tile1 - sg.tile0, base = KS == 1 ? w * 128 : 0;
+            volatile uint32_t* odd_drafts = odd + (KS == 2 ? w : (int)(seg & 1)) * 4;  // shared: group 0 may be a segment ahead
+            ++seg;
+            if (base >= sg.nr) {  // no row for this group
+                t += tiles;
+                continue;
+            }
+            const int64_t row0 = a.cu[sg.b];
+            {  // Q (zeros past the rows), K-major with the 128-byte swizzle: of this group, or of both by both
+                const uint32_t to = smem_u32(sm + S::kQOff) + (KS == 1 ? w * S::kTileBytes : 0);
+                constexpr int kBy = KS == 1 ? 128 : 256;
+#pragma unroll 4
+                for (int x = KS == 1 ? j : w * 128 + j; x < 128 * (D / 8); x += kBy) {
+                    const int r = x / (D / 8), ch = x % (D / 8);
+                    const bool there = base + r < sg.nr;
+                    const int rr = sg.r0 + (there ? base + r : 0), i = rr / a.rep, h = sg.g * a.rep + rr % a.rep;
+                    const char* from = a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                     to + (ch >> 3) * kAtom + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
+                                 "l"(from), "r"(there ? 16 : 0)
+                                 : "memory");
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&q_full[KS == 1 ? w : 0]);
+            }
+            const int rr = sg.r0 + base + j;  // this thread's row of the (b, KV head)
+            const bool mine = base + j < sg.nr;
+            const int draft = mine ? rr / a.rep : 0;
+            float m = -INFINITY, l = 0.f;
+            bool live = false;
+            const float c = a.scale_log2;
+            const int first = sg.tile0 + (KS == 2 ? w : 0);
+            for (int tile = first; tile < sg.tile1; tile += KS, ++steps) {
+                const bool drafts = tile == sg.s.nt - 1;
+                const int keys = tile_keys(a, sg.s, tile);
+                uint64_t seen[2] = {~0ull, ~0ull};  // keys that this row sees
+                if (drafts) {
+                    if (a.tree != nullptr) {
+                        const uint64_t* p = a.tree + (row0 + draft) * a.words;
+                        seen[0] = p[0];
+                        seen[1] = a.words > 1 ? p[1] : 0;
+                    } else {
+                        seen[0] = draft >= 63 ? ~0ull : (1ull << (draft + 1)) - 1;
+                        seen[1] = draft >= 127 ? ~0ull : draft < 64 ? 0 : (1ull << (draft - 63)) - 1;
+                    }
+                }
+                if (keys < kCacheTile) {
+                    seen[0] &= keys >= 64 ? ~0ull : (1ull << keys) - 1;
+                    seen[1] &= keys <= 64 ? 0 : (1ull << (keys - 64)) - 1;
+                }
+                const bool masked = drafts || keys < kCacheTile;
+                wait(&s_full[w], steps & 1);
+                tc_fence_after();
+                float z[64];
+                auto load = [&](int half) {  // 64 keys of S, hidden ones at -inf
+                    tmem_ld32(t_s + half * 64, z);
+                    tmem_ld32(t_s + half * 64 + 32, z + 32);
+                    tmem_wait_ld();
+                    tie<64>(z);
+                    if (masked) {
+                        const uint64_t bits = seen[half];
+#pragma unroll
+                        for (int k = 0; k < 64; ++k)
+                            if (!(bits >> k & 1)) z[k] = -INFINITY;
+                    }
+                };
+                float top = -INFINITY;
+                auto highest = [&]() {
+                    float t4[4] = {top, z[0], z[1], z[2]};
+#pragma unroll
+                    for (int k = 3; k < 63; k += 8) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (k + 2 * i + 1 < 64) t4[i] = fmax3(t4[i], z[k + 2 * i], z[k + 2 * i + 1]);
+                    }
+                    top = fmaxf(fmax3(t4[0], t4[1], z[63]), fmaxf(t4[2], t4[3]));
+                };
+                load(0);
+                highest();
+                load(1);
+                highest();
+                // m moves when the tile exceeds it by 2^8 (always where there is none)
+                const float high = top * c;
+                float f = 1.f;
+                if (high > m + 8.f) {
+                    f = ex2(m - high);
+                    m = high;
+                }
+                l *= f;
+                if (__any_sync(0xffffffffu, f != 1.f) && live) {
+#pragma unroll 1
+                    for (int x = 0; x < D; x += 32) {
+                        float o[32];
+                        tmem_ld32(t_o + x, o);
+                        tmem_wait_ld();
+                        tie<32>(o);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] *= f;
+                        tmem_st32(t_o + x, reinterpret_cast<const uint32_t*>(o));
+                    }
+                }
+                const float nm = m == -INFINITY ? 0.f : -m;
+                float2 sum = make_float2(0.f, 0.f);
+                auto exponentials = [&](int half) {
+                    const float2 c2 = make_float2(c, c), n2 = make_float2(nm, nm);
+#pragma unroll
+                    for (int x = 0; x < 64; x += 32) {
+                        uint32_t p[32];
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2) {
+                            const float2 y = __ffma2_rn(make_float2(z[x + k], z[x + k + 1]), c2, n2);
+                            const float2 e = make_float2(ex2(y.x), ex2(y.y));
+                            sum = __fadd2_rn(sum, e);
+                            p[k / 2] = pack_hi_lo(e.x, e.y, p[16 + k / 2]);
+                        }
+                        tmem_st32(t_s + half * 64 + x, p);
+                    }
+                };
+                exponentials(1);  // still in registers
+                load(0);
+                exponentials(0);
+                l += sum.x + sum.y;
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                if ((KS == 2 || w == 0) && (drafts || (keys & 15))) {
+                    // V rows that must not reach the product: past the keys, and drafts that are not finite
+                    const uint32_t e = 2 * (t + (tile - sg.tile0)) + 1;
+                    const int slot = (int)(e % S::kStages);
+                    wait(&full[slot], (e / S::kStages) & 1);
+                    uint8_t* vr = sm + slot * S::kTileBytes + j * 128;
+                    bool clear = j >= keys && j < ((keys + 15) & ~15);
+                    if (drafts && j < keys) clear = row_not_finite<D>(vr);
+                    if (drafts) {
+                        const unsigned bits = __ballot_sync(0xffffffffu, clear && j < keys);
+                        if (lane == 0) odd_drafts[q] = bits;
+                    }
+                    if (clear) clear_row<D>(vr);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[w]);
+                live = live || keys > 0;
+            }
+            t += tiles;
+            if (first < sg.tile1) wait(&o_full[w], ends++ & 1);  // the last product of the segment
+            const bool whole = sg.tile0 == 0 && sg.tile1 == sg.s.nt;
+            if (KS == 2 ? both_groups_or(!alive) : group_or(bar, !alive)) break;  // who shares barriers leaves together
+            tc_fence_after();
+            // drafts whose V is not finite were left out of O; their P is still in its place
+            if (sg.tile1 == sg.s.nt && (KS == 1 || ((tiles - 1) & 1) == w) &&
+                (odd_drafts[0] | odd_drafts[1] | odd_drafts[2] | odd_drafts[3])) {
+#pragma unroll 1
+                for (int x = 0; x < sg.s.n; ++x) {
+                    if (!(odd_drafts[x >> 5] >> (x & 31) & 1)) continue;
+                    const bool sees = mine && (a.tree != nullptr ? a.tree[(row0 + draft) * a.words + (x >> 6)] >> (x & 63) & 1 : x <= draft);
+                    uint32_t hi, lo;
+                    const uint32_t at = t_s + (x >> 5) * 32 + ((x & 31) >> 1);
+                    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(hi) : "r"(at));
+                    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(lo) : "r"(at + 16));
+                    tmem_wait_ld();
+                    asm volatile("" : "+r"(hi), "+r"(lo));
+                    const float p = x & 1 ? bf16hi(hi) + bf16hi(lo) : bf16lo(hi) + bf16lo(lo);
+                    const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(a.vn + (row0 + x) * a.ldn + (int64_t)sg.g * (D * 2));
+#pragma unroll 1
+                    for (int y = 0; y < D; y += 16) {
+                        float o[16];
+                        tmem_ld16(t_o + y, o);
+                        tmem_wait_ld();
+                        tie<16>(o);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            if (sees) o[k] = fmaf(p, __bfloat162float(v[y + k]), o[k]);
+                        tmem_st16(t_o + y, o);
+                    }
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                }
+            }
+            const int h = sg.g * a.rep + rr % a.rep;
+            const int64_t row = row0 + draft;
+            if (!whole) {
+                const int64_t part = ((int64_t)(cta + sg.group) * KS + (KS == 2 ? w : 0)) * a.RB + base + j;
+                if (mine) a.part_ml[part] = make_float2(m, l);
+#pragma unroll 1
+                for (int x = 0; x < D; x += 32) {
+                    float o[32];
+                    tmem_ld32(t_o + x, o);
+                    tmem_wait_ld();
+                    tie<32>(o);
+                    if (mine)
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4)
+                            *reinterpret_cast<float4*>(a.part_o + part * D + x + k) =
+                                live ? make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                tc_fence_before();
+                if (KS == 2) both_groups_or(false);  // Q and O are free for the next segment
+            } else {
+                // a group of one CTA is finished here; KS = 2: with the other group's half, which lies on the same lanes
+                float M = m, L = l, fa = 1.f, fb = 0.f;
+                if (KS == 2) {
+                    float2* ml = reinterpret_cast<float2*>(sm + S::kQOff);  // [2][128]: every S is done with Q
+                    ml[w * 128 + j] = make_float2(m, l);
+                    tc_fence_before();
+                    both_groups_or(false);
+                    tc_fence_after();
+                    const float2 o = ml[(1 - w) * 128 + j];
+                    M = fmaxf(m, o.x);
+                    fa = m == -INFINITY ? 0.f : ex2(m - M);
+                    fb = o.x == -INFINITY ? 0.f : ex2(o.x - M);
+                    const float la = fa != 0.f ? fa * l : M == -INFINITY ? l : 0.f, lb = fb != 0.f ? fb * o.y : M == -INFINITY ? o.y : 0.f;
+                    L = w == 0 ? la + lb : lb + la;
+                    if (L != L) fa = fb = 1.f;  // NaN stays
+                }
+                const bool none = M == -INFINITY && L == 0.f;
+                const float inv = none ? 0.f : 1.f / L;
+                fa *= inv;
+                fb *= inv;
+                if (mine && (KS == 1 || w == 0)) {
+                    if (a.lse != nullptr) a.lse[(int64_t)h * a.n_rows + row] = L == 0.f ? -INFINITY : fmaf(M, kLn2, logf(L));
+                    if (a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, make_float2(M, L), row);
+                }
+                // KS = 2: each group writes half of the columns
+                const uint32_t t_b = tmem + lane_off + 256 + (1 - w) * 128;
+                constexpr int kCols = KS == 2 ? D / 2 : D;
+                const int x0 = KS == 2 ? w * kCols : 0;
+                __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (row * a.Hq + h) * D;
+#pragma unroll 1
+                for (int x = x0; x < x0 + kCols; x += 16) {
+                    float o[16], b[16];
+                    tmem_ld16(t_o + x, o);
+                    if (KS == 2) tmem_ld16(t_b + x, b);
+                    tmem_wait_ld();
+                    tie<16>(o);
+                    if (KS == 2) tie<16>(b);
+                    if (!mine) continue;
+                    uint32_t v[8];
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2) {
+                        float y[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            y[i] = fa != 0.f ? o[k + i] * fa : 0.f;
+                            if (KS == 2 && fb != 0.f) y[i] = fmaf(b[k + i], fb, y[i]);
+                        }
+                        const __nv_bfloat162 t2 = __floats2bfloat162_rn(y[0], y[1]);
+                        v[k / 2] = *reinterpret_cast<const uint32_t*>(&t2);
+                    }
+                    *reinterpret_cast<uint4*>(out + x) = make_uint4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<uint4*>(out + x + 8) = make_uint4(v[4], v[5], v[6], v[7]);
+                }
+                tc_fence_before();
+                if (KS == 2) both_groups_or(false);  // Q and O are free for the next segment
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (threadIdx.x == 0 && *abort_flag) drain_ring(full, S::kStages, issued_tiles, a.status);
+    if (warp == 1) {
+        __syncwarp();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+    }
+}
+
+template <int D, int KS>
+estp_status launch(estp_ctx* ctx, const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int new_rows, cudaStream_t st) {
+    using S = RowShape<D, KS>;
+    cudaError_t e = set_smem(ctx, 20 + (D == 128 ? 2 : 0) + KS - 1, cache_rows_tc_kernel<D, KS>, S::kSmem);
+    if (e != cudaSuccess) return cuda_fail(e, "cache attention smem attribute");
+    cache_rows_tc_kernel<D, KS><<<(unsigned)a.G, S::kThreads, S::kSmem, st>>>(tm, a, box_rows, new_rows);
+    e = cudaGetLastError();
+    return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache attention launch");
+}
+
+}  // namespace
+
+estp_status launch_cache_rows_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st) {
+    TcMaps tm;
+    int box_rows, new_rows;
+    const estp_status s = make_maps(a, &tm, &box_rows, &new_rows);
+    if (s != ESTP_OK) return s;
+    if (a.c.d == 128) return a.KS == 2 ? launch<128, 2>(ctx, tm, a, box_rows, new_rows, st) : launch<128, 1>(ctx, tm, a, box_rows, new_rows, st);
+    return a.KS == 2 ? launch<64, 2>(ctx, tm, a, box_rows, new_rows, st) : launch<64, 1>(ctx, tm, a, box_rows, new_rows, st);
+}
+
+}  // namespace estp
