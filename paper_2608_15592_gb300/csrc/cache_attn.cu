@@ -331,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     const float f = m[u] == all.x ? 1.f : ex2(m[u] - all.x);
+                    if (f == 0.f) continue;  // an empty partial holds nothing
 #pragma unroll
                     for (int k = 0; k < kC; ++k) o[k] = fmaf(f, v[u][k], o[k]);
                 }
@@ -497,7 +498,7 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     if (kTc) {
         const int rows = a.max_rows * a.rep;
         a.RB = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
-        a.KS = a.RB <= 128 ? 2 : 1;
+        a.KS = 2;
     }
     a.whole = kTc;
     a.G = kTc ? ctx->num_sms : ctx->num_sms * 8;

@@ -246,11 +246,8 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                         if (use >= 1 && !wait(&s_empty[2 * nb + buf], (use - 1) & 1)) break;
                         tc_fence_after();
                         issued = true;
-                        const uint32_t qa = smem_u32(sm + S::kQOff + qb * S::kQBytes);
-#pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk)
-                            mma_bf16<kIdS>(tmem + (2 * nb + buf) * S::kN, sw128_desc(ka + (kk >> 2) * kAtom + (kk & 3) * 32),
-                                           sw128_desc(qa + (kk >> 2) * S::kN * 128 + (kk & 3) * 32), kk > 0 ? 1u : 0u);
+                        product_k_major<kIdS, D>(tmem + (2 * nb + buf) * S::kN, ka, kAtom,
+                                                 smem_u32(sm + S::kQOff + qb * S::kQBytes), S::kN * 128);
                         mma_commit(&s_full[2 * nb + buf]);
                     }
                     if (ok) mma_commit(&empty[slot]);
@@ -290,9 +287,16 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                         tc_fence_after();
                         issued = true;
                         const uint32_t pa = smem_u32(sm + S::kPOff) + nb * S::kPStep;
-                        for (int kk = 0; kk < ksteps; ++kk)
-                            mma_bf16<kIdO>(tmem + (uint32_t)(S::kOCol + nb * 2 * RB), mn_desc(va + kk * 2048, D == 128 ? kAtom : 0),
-                                           mn_desc(pa + kk * 2048, kAtom), live[nb] || kk > 0 ? 1u : 0u);
+                        const uint64_t vd = mn_desc(va, D == 128 ? kAtom : 0), pd = mn_desc(pa, kAtom);
+                        const uint32_t o = tmem + (uint32_t)(S::kOCol + nb * 2 * RB);
+                        if (ksteps == 8) {
+#pragma unroll
+                            for (int kk = 0; kk < 8; ++kk)  // 16 keys, 2 KB, a step
+                                mma_bf16<kIdO>(o, vd + kk * 128, pd + kk * 128, kk > 0 ? 1u : live[nb] ? 1u : 0u);
+                        } else {
+                            for (int kk = 0; kk < ksteps; ++kk)
+                                mma_bf16<kIdO>(o, vd + kk * 128, pd + kk * 128, live[nb] || kk > 0 ? 1u : 0u);
+                        }
                         mma_commit(&pv_done[nb]);
                         live[nb] = live[nb] || ksteps > 0;
                     }

@@ -11,15 +11,16 @@
 // A row's m only moves when a tile exceeds it by 2^8; the warps whose rows do then rescale O and l.
 //
 // One persistent CTA per SM over the units of cache.cuh, two epilogue groups of 128 threads, each with
-// an S/P buffer and an O (all 512 columns).  KS = 1: a block is 256 rows, 128 a group, and every tile
-// goes to both.  KS = 2: a block is 128 rows and the groups take the tiles in turn, each with a
-// partial of its own.  Either way one group's softmax runs under the other's products.
+// an S/P buffer and an O (all 512 columns).  A block of up to 128 rows is split by tiles: the groups
+// take them in turn, each with a partial of its own.  A block of up to 256 rows is split by rows, 128 a
+// group, and every tile goes to both.  Either way one group's softmax runs under the other's products.
 //   warps 0, 2 TMA producers of the K and of the V tiles (one ring, K and V in turn)
 //   warp 1     issues the products; the pipe runs them in the order of issue, so the S that overwrites
 //              a P comes after the product that reads it
 //   warp 3     idle
 //   warps 4-11 the epilogue groups, which also load their rows' Q
-// Bound, at 256 rows, by the tensor pipe (1536 clocks a group and tile); at 128 by the copies.
+// Bound, at 256 rows, by the tensor pipe (24 products of 64 clocks a group and tile, and half as slow
+// again beside the epilogue's own tensor memory traffic); up to 128 nearly by the copies.
 // Keys past a sequence's slots, drafts that are not finite and waits are treated as in
 // cache_attn_tc.cu.
 #include "cache_tc.cuh"
@@ -27,21 +28,22 @@
 namespace estp {
 namespace {
 
-template <int D, int KS>
+template <int D>
 struct RowShape {
-    static constexpr int kRows = KS == 2 ? 128 : 256;
     static constexpr int kAtoms = D / 64;
     static constexpr int kTileBytes = kAtoms * kAtom;  // 128 keys, or 128 rows of Q
-    static constexpr int kQBytes = kRows / 128 * kTileBytes;
-    static constexpr int kRoom = 227 * 1024 - 1024 - kQBytes - 512;
-    static constexpr int kStages = kRoom / kTileBytes < 12 ? kRoom / kTileBytes : 12;
+    static constexpr int kMaxStages = 12;
     static constexpr int kThreads = 384;
-    static constexpr int kQOff = kStages * kTileBytes;
-    static constexpr int kBarOff = kQOff + kQBytes;
-    static constexpr int kBars = 2 * kStages + 9;
-    static constexpr int kMiscOff = kBarOff + (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, tiles issued, odd drafts
-    static constexpr int kSmem = kMiscOff + 48 + 1024;
-    static_assert(kStages >= 4 && kSmem <= 227 * 1024, "shared memory per CTA");
+    // from a 1024-aligned base: barriers and flags, Q (one tile of rows or two), the ring
+    static constexpr int kBars = 2 * kMaxStages + 9;
+    static constexpr int kMiscOff = (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, tiles issued, odd drafts
+    static constexpr int kQOff = 1024;
+    static_assert(kMiscOff + 48 <= kQOff, "barriers");
+    static int stages(int q_tiles) {
+        const int n = (227 * 1024 - 1024 - kQOff) / kTileBytes - q_tiles;
+        return n < kMaxStages ? n : kMaxStages;
+    }
+    static int smem(int q_tiles) { return 1024 + kQOff + (q_tiles + stages(q_tiles)) * kTileBytes; }
 };
 
 // D (TMEM) += A (TMEM) B, B an MN-major shared memory tile
@@ -65,18 +67,20 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
         : "memory");
 }
 
-template <int D, int KS>
-__global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
-    cache_rows_tc_kernel(const __grid_constant__ TcMaps tm, const CacheAttnArgs a, const int box_rows, const int new_rows) {
-    using S = RowShape<D, KS>;
+template <int D>
+__global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
+    cache_rows_tc_kernel(const __grid_constant__ TcMaps tm, const CacheAttnArgs a, const int box_rows, const int new_rows,
+                         const int n_stages) {
+    using S = RowShape<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
-    uint64_t* full = reinterpret_cast<uint64_t*>(sm + S::kBarOff);  // [kStages]
-    uint64_t* empty = full + S::kStages;                            // [kStages]
-    uint64_t* q_full = empty + S::kStages;                          // [2], KS = 2: the first
-    uint64_t* s_full = q_full + 2;                                  // [2]
-    uint64_t* p_full = s_full + 2;                                  // [2]
-    uint64_t* o_full = p_full + 2;                                  // [2]
+    uint8_t* ring = sm + S::kQOff + (a.RB / 128) * S::kTileBytes;
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm);  // [kMaxStages]
+    uint64_t* empty = full + S::kMaxStages;            // [kMaxStages]
+    uint64_t* q_full = empty + S::kMaxStages;          // both groups' rows
+    uint64_t* s_full = q_full + 1;                     // [2]
+    uint64_t* p_full = s_full + 2;                     // [2]
+    uint64_t* o_full = p_full + 2;                     // [2]
     uint64_t* drain = o_full + 2;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::kMiscOff);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 4);
@@ -86,12 +90,12 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < S::kStages; ++i) {
+        for (int i = 0; i < n_stages; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
+        mbar_init(q_full, 8);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&q_full[i], KS == 2 ? 8 : 4);
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
             mbar_init(&o_full[i], 1);
@@ -111,7 +115,7 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
     const int cta = blockIdx.x;
     Walk walk{Place{0, 0, 0, 0}, 0, 0};
     Place place;
-    const PlanTotals tot = plan(a, reinterpret_cast<PlanScratch*>(sm), &place, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
+    const PlanTotals tot = plan(a, reinterpret_cast<PlanScratch*>(ring), &place, [&](const Place& x, const SeqShape& s, const PlanTotals& all) {
         const int u = share_begin(cta, all.units, ctas_of(a, all.units));
         return u >= x.unit0 && u < x.unit0 + s.units(a.c.Hkv);
     });
@@ -134,14 +138,14 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
         while (ok && walk.next(a, sg)) {
             win.open(a, sg.s, sg.b, sg.tile0, lane);
             for (int tile = sg.tile0; tile < sg.tile1; ++tile, ++t) {
-                const uint32_t e = 2 * t + kv, use = e / S::kStages;
-                const int slot = (int)(e % S::kStages);
+                const uint32_t e = 2 * t + kv, use = e / n_stages;
+                const int slot = (int)(e % n_stages);
                 if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
                     ok = false;
                     break;
                 }
                 load_tile<D>(a, kv ? &tm.v : &tm.k, kv ? &tm.vn : &tm.kn, win, sg.s, sg.b, sg.g, tile, box_rows, new_rows,
-                             sm + slot * S::kTileBytes, &full[slot], lane);
+                             ring + slot * S::kTileBytes, &full[slot], lane);
             }
         }
         if (lane == 0) issued_tiles[kv] = (int)t;
@@ -151,52 +155,55 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
         if (lane == 0) {
             constexpr uint32_t kIdS = idesc_bf16(128, 128);
             constexpr uint32_t kIdO = idesc_bf16(128, D) | (1u << 16);  // B MN-major
-            uint32_t t = 0, q_seen[2] = {0, 0}, p_seen[2] = {0, 0};
+            uint32_t t = 0, seg = 0, p_seen[2] = {0, 0};
             bool ok = true, issued = false;
             auto wait = [&](uint64_t* bar, uint32_t parity) {
                 ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
                 return ok;
             };
             auto release = [&](uint32_t e) {
-                if (ok) mma_commit(&empty[e % S::kStages]);
+                if (ok) mma_commit(&empty[e % n_stages]);
             };
             while (ok && walk.next(a, sg)) {
-                const int tiles = sg.tile1 - sg.tile0, groups = KS == 2 ? 2 : (sg.nr + 127) / 128;
+                const int tiles = sg.tile1 - sg.tile0;
+                const bool split = sg.nr <= 128;  // by tiles; else by rows
                 bool live[2] = {false, false};
+                if (!wait(q_full, seg++ & 1)) break;
                 auto product_s = [&](int i, int w) {  // S of the segment's tile i for group w
                     const uint32_t e = 2 * (t + i);
-                    const int slot = (int)(e % S::kStages);
-                    if (i < KS && (KS == 1 || w == 0) && !wait(&q_full[w], q_seen[w]++ & 1)) return;
-                    if (!wait(&full[slot], (e / S::kStages) & 1)) return;
+                    const int slot = (int)(e % n_stages);
+                    if (!wait(&full[slot], (e / n_stages) & 1)) return;
                     tc_fence_after();
                     issued = true;
-                    const uint32_t ka = smem_u32(sm + slot * S::kTileBytes);
-                    const uint32_t qa = smem_u32(sm + S::kQOff) + (KS == 1 ? w * S::kTileBytes : 0);
-#pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
-                        const uint32_t off = (kk >> 2) * kAtom + (kk & 3) * 32;
-                        mma_bf16<kIdS>(tmem + w * 128, sw128_desc(qa + off), sw128_desc(ka + off), kk > 0 ? 1u : 0u);
-                    }
+                    const uint32_t ka = smem_u32(ring + slot * S::kTileBytes);
+                    const uint32_t qa = smem_u32(sm + S::kQOff) + (split ? 0 : w * S::kTileBytes);
+                    product_k_major<kIdS, D>(tmem + w * 128, qa, kAtom, ka, kAtom);
                     mma_commit(&s_full[w]);
                 };
                 auto product_o = [&](int i, int w) {
                     const uint32_t e = 2 * (t + i) + 1;
-                    const int slot = (int)(e % S::kStages);
-                    if (!wait(&full[slot], (e / S::kStages) & 1) || !wait(&p_full[w], p_seen[w]++ & 1)) return;
+                    const int slot = (int)(e % n_stages);
+                    if (!wait(&full[slot], (e / n_stages) & 1) || !wait(&p_full[w], p_seen[w]++ & 1)) return;
                     tc_fence_after();
                     issued = true;
-                    const uint32_t va = smem_u32(sm + slot * S::kTileBytes), p = tmem + w * 128, o = tmem + 256 + w * 128;
+                    const uint32_t va = smem_u32(ring + slot * S::kTileBytes), p = tmem + w * 128, o = tmem + 256 + w * 128;
                     const int ksteps = (tile_keys(a, sg.s, sg.tile0 + i) + 15) / 16;
-                    for (int kk = 0; kk < ksteps; ++kk) {
-                        const uint64_t v = mn_desc(va + kk * 2048, kAtom);
+                    const uint64_t vd = mn_desc(va, kAtom);
+                    auto keys16 = [&](int kk, uint32_t acc) {  // 16 keys, 2 KB of V: hi and lo
                         const uint32_t at = p + (kk >> 1) * 32 + (kk & 1) * 8;
-                        mma_ts<kIdO>(o, at, v, live[w] || kk > 0 ? 1u : 0u);
-                        mma_ts<kIdO>(o, at + 16, v, 1u);
+                        mma_ts<kIdO>(o, at, vd + kk * 128, acc);
+                        mma_ts<kIdO>(o, at + 16, vd + kk * 128, 1u);
+                    };
+                    if (ksteps == 8) {
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk) keys16(kk, kk > 0 ? 1u : live[w] ? 1u : 0u);
+                    } else {
+                        for (int kk = 0; kk < ksteps; ++kk) keys16(kk, live[w] || kk > 0 ? 1u : 0u);
                     }
                     live[w] = live[w] || ksteps > 0;
-                    if (i + KS >= tiles) mma_commit(&o_full[w]);
+                    if (i + (split ? 2 : 1) >= tiles) mma_commit(&o_full[w]);
                 };
-                if (KS == 2) {
+                if (split) {
                     for (int i = 0; ok && i < 2 && i < tiles; ++i) {
                         product_s(i, i);
                         release(2 * (t + i));
@@ -210,12 +217,12 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
                         }
                     }
                 } else {
-                    for (int w = 0; ok && w < groups; ++w) product_s(0, w);
+                    for (int w = 0; ok && w < 2; ++w) product_s(0, w);
                     release(2 * t);
                     for (int i = 0; ok && i < tiles; ++i) {
-                        for (int w = 0; ok && w < groups; ++w) {
+                        for (int w = 0; ok && w < 2; ++w) {
                             product_o(i, w);
-                            if (w == groups - 1) release(2 * (t + i) + 1);
+                            if (w == 1) release(2 * (t + i) + 1);
                             if (ok && i + 1 < tiles) product_s(i + 1, w);
                         }
                         if (i + 1 < tiles) release(2 * (t + i + 1));
@@ -231,42 +238,38 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
         __syncwarp();
     } else if (warp >= 4) {
         // ------------------------------------------------------------- epilogue
-        const int w = (warp - 4) >> 2, q = warp & 3, bar = 1 + w;
+        const int w = (warp - 4) >> 2, q = warp & 3;
         const int j = q * 32 + lane;  // lane of TMEM: row of the group; and V row that it may clear
         const uint32_t lane_off = (uint32_t)(q * 32) << 16;
         const uint32_t t_s = tmem + lane_off + w * 128, t_o = tmem + lane_off + 256 + w * 128;
-        uint32_t t = 0, seg = 0, steps = 0, ends = 0;
+        uint32_t t = 0, steps = 0, ends = 0;
         bool alive = true;
         auto wait = [&](uint64_t* b, uint32_t parity) {
             if (alive) alive = warp_wait(b, parity, abort_flag, a.status, a.wait_cycles);
         };
         while (walk.next(a, sg)) {
-            const int tiles = sg.tile1 - sg.tile0, base = KS == 1 ? w * 128 : 0;
-            volatile uint32_t* odd_drafts = odd + (KS == 2 ? w : (int)(seg & 1)) * 4;  // shared: group 0 may be a segment ahead
-            ++seg;
-            if (base >= sg.nr) {  // no row for this group
-                t += tiles;
-                continue;
-            }
+            const int tiles = sg.tile1 - sg.tile0;
+            const bool split = sg.nr <= 128;
+            const int base = split ? 0 : w * 128;
+            volatile uint32_t* odd_drafts = odd + (split ? w : 0) * 4;
             const int64_t row0 = a.cu[sg.b];
-            {  // Q (zeros past the rows), K-major with the 128-byte swizzle: of this group, or of both by both
-                const uint32_t to = smem_u32(sm + S::kQOff) + (KS == 1 ? w * S::kTileBytes : 0);
-                constexpr int kBy = KS == 1 ? 128 : 256;
+            {  // Q (zeros past the rows), K-major with the 128-byte swizzle
+                const uint32_t to = smem_u32(sm + S::kQOff);
 #pragma unroll 4
-                for (int x = KS == 1 ? j : w * 128 + j; x < 128 * (D / 8); x += kBy) {
+                for (int x = w * 128 + j; x < (split ? 128 : 256) * (D / 8); x += 256) {
                     const int r = x / (D / 8), ch = x % (D / 8);
-                    const bool there = base + r < sg.nr;
-                    const int rr = sg.r0 + (there ? base + r : 0), i = rr / a.rep, h = sg.g * a.rep + rr % a.rep;
+                    const bool there = r < sg.nr;
+                    const int rq = sg.r0 + (there ? r : 0), i = rq / a.rep, h = sg.g * a.rep + rq % a.rep;
                     const char* from = a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16;
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                     to + (ch >> 3) * kAtom + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
+                                     to + (r >> 7) * S::kTileBytes + (ch >> 3) * kAtom + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4)),
                                  "l"(from), "r"(there ? 16 : 0)
                                  : "memory");
                 }
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&q_full[KS == 1 ? w : 0]);
+                if (lane == 0) mbar_arrive(q_full);
             }
             const int rr = sg.r0 + base + j;  // this thread's row of the (b, KV head)
             const bool mine = base + j < sg.nr;
@@ -274,8 +277,8 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
             float m = -INFINITY, l = 0.f;
             bool live = false;
             const float c = a.scale_log2;
-            const int first = sg.tile0 + (KS == 2 ? w : 0);
-            for (int tile = first; tile < sg.tile1; tile += KS, ++steps) {
+            const int first = sg.tile0 + (split ? w : 0);
+            for (int tile = first; tile < sg.tile1; tile += split ? 2 : 1, ++steps) {
                 const bool drafts = tile == sg.s.nt - 1;
                 const int keys = tile_keys(a, sg.s, tile);
                 uint64_t seen[2] = {~0ull, ~0ull};  // keys that this row sees
@@ -366,12 +369,12 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
                 exponentials(0);
                 l += sum.x + sum.y;
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                if ((KS == 2 || w == 0) && (drafts || (keys & 15))) {
+                if ((split || w == 0) && (drafts || (keys & 15))) {
                     // V rows that must not reach the product: past the keys, and drafts that are not finite
                     const uint32_t e = 2 * (t + (tile - sg.tile0)) + 1;
-                    const int slot = (int)(e % S::kStages);
-                    wait(&full[slot], (e / S::kStages) & 1);
-                    uint8_t* vr = sm + slot * S::kTileBytes + j * 128;
+                    const int slot = (int)(e % n_stages);
+                    wait(&full[slot], (e / n_stages) & 1);
+                    uint8_t* vr = ring + slot * S::kTileBytes + j * 128;
                     bool clear = j >= keys && j < ((keys + 15) & ~15);
                     if (drafts && j < keys) clear = row_not_finite<D>(vr);
                     if (drafts) {
@@ -389,10 +392,10 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
             t += tiles;
             if (first < sg.tile1) wait(&o_full[w], ends++ & 1);  // the last product of the segment
             const bool whole = sg.tile0 == 0 && sg.tile1 == sg.s.nt;
-            if (KS == 2 ? both_groups_or(!alive) : group_or(bar, !alive)) break;  // who shares barriers leaves together
+            if (both_groups_or(!alive)) break;  // the groups leave together
             tc_fence_after();
             // drafts whose V is not finite were left out of O; their P is still in its place
-            if (sg.tile1 == sg.s.nt && (KS == 1 || ((tiles - 1) & 1) == w) &&
+            if (sg.tile1 == sg.s.nt && (!split || ((tiles - 1) & 1) == w) &&
                 (odd_drafts[0] | odd_drafts[1] | odd_drafts[2] | odd_drafts[3])) {
 #pragma unroll 1
                 for (int x = 0; x < sg.s.n; ++x) {
@@ -423,8 +426,12 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
             const int h = sg.g * a.rep + rr % a.rep;
             const int64_t row = row0 + draft;
             if (!whole) {
-                const int64_t part = ((int64_t)(cta + sg.group) * KS + (KS == 2 ? w : 0)) * a.RB + base + j;
-                if (mine) a.part_ml[part] = make_float2(m, l);
+                // split by rows: the second partial is empty
+                const int64_t two = (int64_t)(cta + sg.group) * 2 * a.RB, part = two + (split ? w * a.RB : base) + j;
+                if (mine) {
+                    a.part_ml[part] = make_float2(m, l);
+                    if (!split) a.part_ml[part + a.RB] = make_float2(-INFINITY, 0.f);
+                }
 #pragma unroll 1
                 for (int x = 0; x < D; x += 32) {
                     float o[32];
@@ -438,11 +445,11 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
                                 live ? make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
                 tc_fence_before();
-                if (KS == 2) both_groups_or(false);  // Q and O are free for the next segment
+                both_groups_or(false);  // Q and O are free for the next segment
             } else {
-                // a group of one CTA is finished here; KS = 2: with the other group's half, which lies on the same lanes
-                float M = m, L = l, fa = 1.f, fb = 0.f;
-                if (KS == 2) {
+                // a group of one CTA is finished here; split by tiles: with the other group's half, which lies on the same lanes
+                float M = m, L = l, fa = 1.f, fb = 0.f;  // (fb = 0: no other)
+                if (split) {
                     float2* ml = reinterpret_cast<float2*>(sm + S::kQOff);  // [2][128]: every S is done with Q
                     ml[w * 128 + j] = make_float2(m, l);
                     tc_fence_before();
@@ -460,23 +467,22 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
                 const float inv = none ? 0.f : 1.f / L;
                 fa *= inv;
                 fb *= inv;
-                if (mine && (KS == 1 || w == 0)) {
+                if (mine && (!split || w == 0)) {
                     if (a.lse != nullptr) a.lse[(int64_t)h * a.n_rows + row] = L == 0.f ? -INFINITY : fmaf(M, kLn2, logf(L));
                     if (a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, make_float2(M, L), row);
                 }
-                // KS = 2: each group writes half of the columns
+                // split by tiles: each group writes half of the columns
                 const uint32_t t_b = tmem + lane_off + 256 + (1 - w) * 128;
-                constexpr int kCols = KS == 2 ? D / 2 : D;
-                const int x0 = KS == 2 ? w * kCols : 0;
+                const int cols = split ? D / 2 : D, x0 = split ? w * cols : 0;
                 __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (row * a.Hq + h) * D;
 #pragma unroll 1
-                for (int x = x0; x < x0 + kCols; x += 16) {
+                for (int x = x0; x < x0 + cols; x += 16) {
                     float o[16], b[16];
                     tmem_ld16(t_o + x, o);
-                    if (KS == 2) tmem_ld16(t_b + x, b);
+                    tmem_ld16(t_b + x, b);
                     tmem_wait_ld();
                     tie<16>(o);
-                    if (KS == 2) tie<16>(b);
+                    tie<16>(b);
                     if (!mine) continue;
                     uint32_t v[8];
 #pragma unroll
@@ -485,7 +491,7 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             y[i] = fa != 0.f ? o[k + i] * fa : 0.f;
-                            if (KS == 2 && fb != 0.f) y[i] = fmaf(b[k + i], fb, y[i]);
+                            if (fb != 0.f) y[i] = fmaf(b[k + i], fb, y[i]);
                         }
                         const __nv_bfloat162 t2 = __floats2bfloat162_rn(y[0], y[1]);
                         v[k / 2] = *reinterpret_cast<const uint32_t*>(&t2);
@@ -494,26 +500,30 @@ __global__ void __launch_bounds__(RowShape<D, KS>::kThreads, 1)
                     *reinterpret_cast<uint4*>(out + x + 8) = make_uint4(v[4], v[5], v[6], v[7]);
                 }
                 tc_fence_before();
-                if (KS == 2) both_groups_or(false);  // Q and O are free for the next segment
+                both_groups_or(false);  // Q and O are free for the next segment
             }
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (threadIdx.x == 0 && *abort_flag) drain_ring(full, S::kStages, issued_tiles, a.status);
+    if (threadIdx.x == 0 && *abort_flag) drain_ring(full, n_stages, issued_tiles, a.status);
     if (warp == 1) {
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
     }
 }
 
-template <int D, int KS>
-estp_status launch(estp_ctx* ctx, const TcMaps& tm, const CacheAttnArgs& a, int box_rows, int new_rows, cudaStream_t st) {
-    using S = RowShape<D, KS>;
-    cudaError_t e = set_smem(ctx, 20 + (D == 128 ? 2 : 0) + KS - 1, cache_rows_tc_kernel<D, KS>, S::kSmem);
+template <int D>
+estp_status launch(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st) {
+    using S = RowShape<D>;
+    TcMaps tm;
+    int box_rows, new_rows;
+    const estp_status s = make_maps(a, &tm, &box_rows, &new_rows);
+    if (s != ESTP_OK) return s;
+    cudaError_t e = set_smem(ctx, D == 128 ? 21 : 20, cache_rows_tc_kernel<D>, 227 * 1024);
     if (e != cudaSuccess) return cuda_fail(e, "cache attention smem attribute");
-    cache_rows_tc_kernel<D, KS><<<(unsigned)a.G, S::kThreads, S::kSmem, st>>>(tm, a, box_rows, new_rows);
+    cache_rows_tc_kernel<D><<<(unsigned)a.G, S::kThreads, S::smem(a.RB / 128), st>>>(tm, a, box_rows, new_rows, S::stages(a.RB / 128));
     e = cudaGetLastError();
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache attention launch");
 }
@@ -521,12 +531,7 @@ estp_status launch(estp_ctx* ctx, const TcMaps& tm, const CacheAttnArgs& a, int 
 }  // namespace
 
 estp_status launch_cache_rows_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st) {
-    TcMaps tm;
-    int box_rows, new_rows;
-    const estp_status s = make_maps(a, &tm, &box_rows, &new_rows);
-    if (s != ESTP_OK) return s;
-    if (a.c.d == 128) return a.KS == 2 ? launch<128, 2>(ctx, tm, a, box_rows, new_rows, st) : launch<128, 1>(ctx, tm, a, box_rows, new_rows, st);
-    return a.KS == 2 ? launch<64, 2>(ctx, tm, a, box_rows, new_rows, st) : launch<64, 1>(ctx, tm, a, box_rows, new_rows, st);
+    return a.c.d == 128 ? launch<128>(ctx, a, st) : launch<64>(ctx, a, st);
 }
 
 }  // namespace estp

@@ -76,6 +76,20 @@ __device__ __forceinline__ uint64_t mn_desc(uint32_t addr, uint32_t lead) {
            ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 
+// The issue of a product is a thread's own instructions: descriptors are formed once and stepped by adding
+// (the address field counts 16 bytes and does not overflow), and whole tiles are unrolled.  Formed anew
+// and looped over, an MMA took 140 clocks to issue where the pipe needs 64.
+
+// D (TMEM) = K Q^T or Q K^T: both K-major, rows of A and B 128 bytes, second 64 columns lead_a, lead_b on
+template <uint32_t kIdesc, int D>
+__device__ __forceinline__ void product_k_major(uint32_t d_tmem, uint32_t a, uint32_t lead_a, uint32_t b, uint32_t lead_b) {
+    const uint64_t ad = sw128_desc(a), bd = sw128_desc(b);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+        mma_bf16<kIdesc>(d_tmem, ad + (kk >> 2) * (lead_a >> 4) + (kk & 3) * 2, bd + (kk >> 2) * (lead_b >> 4) + (kk & 3) * 2,
+                         kk > 0 ? 1u : 0u);
+}
+
 // Barrier of one epilogue group (128 threads) that ors a predicate.
 __device__ __forceinline__ bool group_or(int id, bool x) {
     uint32_t r;

@@ -1,7 +1,7 @@
 // The cache attention's weights with the scores formed again (see cache_attn.cu) for bf16 caches: S^T = K Q^T tile by tile with every
 // row of the (b, KV head) resident, w_j = sum_r c_r 2^(S_jr c - M_r) / L_r, a thread a key.  A CTA takes
-// an equal run of the call's (b, KV head, tile); the blocks of 64 rows of a tile go to the two groups
-// in turn, whose sums are added in their order.  Rows beyond kWRows take another pass over the run,
+// an equal run of the call's (b, KV head, tile), which go to the two epilogue groups in turn, all
+// blocks of 64 rows of a tile to one.  Rows beyond kWRows take another pass over the run,
 // by the same threads.  Bound by K's bytes up to some 170 rows a KV head, then by ex2 (16 a clock).
 #include "cache_tc.cuh"
 
@@ -17,10 +17,9 @@ struct WShape {
     // from a 1024-aligned base: barriers, factors and sums first, then Q blocks and as many K tiles as fit
     static constexpr int kBars = 2 * kWMaxStages + 1 + 4 * kWBufs + 1;
     static constexpr int kMiscOff = kBars * 8;          // tmem address, abort flag
-    static constexpr int kRedOff = 256;                 // [2][128] the second group's sums
-    static constexpr int kFOff = kRedOff + 2 * 128 * 4; // [kWRows] factors
+    static constexpr int kFOff = 256;                   // [kWRows] factors
     static constexpr int kQOff = (kFOff + kWRows * 8 + 1023) / 1024 * 1024;
-    static_assert(kMiscOff + 8 <= kRedOff, "barriers");
+    static_assert(kMiscOff + 8 <= kFOff, "barriers");
     static constexpr int kThreads = 64 + 256;
     static constexpr int kRoom = 227 * 1024 - 1024 - kQOff;
     static int stages(int blocks) {
@@ -159,18 +158,14 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                         const int slot = (int)(e % n_stages);
                         if (!wait(&full[slot], (e / n_stages) & 1)) break;
                         const uint32_t ka = smem_u32(ring + slot * S::kTileBytes);
+                        const int gr = (tile - w.tile0) & 1;
                         for (int k = 0; k < blocks; ++k) {
-                            const int gr = k & 1;
                             const uint32_t n = steps[gr]++, buf = n % kWBufs, use = n / kWBufs;
                             if (use >= 1 && !wait(&s_empty[gr * kWBufs + buf], (use - 1) & 1)) break;
                             tc_fence_after();
                             issued = true;
-                            const uint32_t qa = smem_u32(sm + S::kQOff + k * S::kBlockBytes);
-#pragma unroll
-                            for (int kk = 0; kk < D / 16; ++kk)
-                                mma_bf16<kId>(tmem + (gr * kWBufs + buf) * kWBlock,
-                                              sw128_desc(ka + (kk >> 2) * kAtom + (kk & 3) * 32),
-                                              sw128_desc(qa + (kk >> 2) * kWBlock * 128 + (kk & 3) * 32), kk > 0 ? 1u : 0u);
+                            product_k_major<kId, D>(tmem + (gr * kWBufs + buf) * kWBlock, ka, kAtom,
+                                                    smem_u32(sm + S::kQOff + k * S::kBlockBytes), kWBlock * 128);
                             mma_commit(&s_full[gr * kWBufs + buf]);
                         }
                         if (ok) mma_commit(&empty[slot]);
@@ -187,8 +182,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
         // ------------------------------------------------------------- epilogue
         const int gr = (warp - 2) >> 2, q = warp & 3, j = q * 32 + lane, tid = threadIdx.x - 64;
         float2* fs = reinterpret_cast<float2*>(sm + S::kFOff);
-        float* red = reinterpret_cast<float*>(sm + S::kRedOff);
-        uint32_t step = 0, parity = 0;
+        uint32_t step = 0;
         bool alive = true;
         while (alive && w.next(a)) {
             const int R = w.s.n * a.rep;
@@ -213,12 +207,12 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 both_groups_or(false);  // the factors are everyone's
                 if (lane == 0) mbar_arrive(q_full);
-                for (int tile = w.tile0; tile < w.tile1; ++tile, parity ^= 1) {
+                for (int tile = w.tile0 + gr; tile < w.tile1; tile += 2) {
                     const bool drafts = tile == w.s.nt - 1;
                     const int keys = tile_keys(a, w.s, tile);
                     float* to = nullptr;
                     float had = 0.f;
-                    if (gr == 0 && j < keys) {  // early: its latency passes under the sums
+                    if (j < keys) {  // early: its latency passes under the sums
                         if (drafts) {
                             to = a.w_new + (row0 + j) * a.c.Hkv + w.g;
                             if (r0 > 0) had = *to;
@@ -232,7 +226,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                         }
                     }
                     float sum[2] = {0.f, 0.f};
-                    for (int k = gr; k < blocks; k += 2, ++step) {
+                    for (int k = 0; k < blocks; ++k, ++step) {
                         const uint32_t buf = step % kWBufs;
                         if (alive)
                             alive = warp_wait(&s_full[gr * kWBufs + buf], (step / kWBufs) & 1, abort_flag, a.status, a.wait_cycles);
@@ -261,14 +255,9 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                             }
                         }
                     }
-                    const float mine = sum[0] + sum[1];
-                    if (gr == 1) red[parity * 128 + j] = mine;
-                    if (both_groups_or(!alive)) {
-                        alive = false;
-                        break;
-                    }
-                    if (to != nullptr) *to = had + (mine + red[parity * 128 + j]);
+                    if (to != nullptr) *to = had + (sum[0] + sum[1]);
                 }
+                if (both_groups_or(!alive)) alive = false;  // Q and the factors are free
             }
         }
     }
