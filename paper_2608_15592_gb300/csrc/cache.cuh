@@ -1,6 +1,7 @@
 // The paged KV cache as the kernels see it, and the cut of an attention call into units.
 //
-// A call's units are (sequence b, KV head g, block of RB rows, tile of 128 keys).  The rows of
+// A call's units are (sequence b, KV head g, block of RB rows, tile of 128 keys), a tile of a block of
+// more than 128 rows counted twice (it costs twice).  The rows of
 // (b, g) are its n_b drafts times the rep query heads that read KV head g, row r = i rep + h';
 // the tiles are the cached slots in order and, last, one tile of the drafts themselves.  Units
 // are numbered with the tile fastest, then the row block, the KV head and the sequence; the
@@ -83,9 +84,10 @@ struct CacheAttnArgs {
 // What sequence b brings to the call.
 struct SeqShape {
     int len, n, nrb, nt;
+    int cost, last;  // units of a tile: of a KV head's blocks together, and of its last block
     // the host has made sure that the call's units fit 31 bits
     __device__ __forceinline__ int groups(int Hkv) const { return Hkv * nrb; }
-    __device__ __forceinline__ int units(int Hkv) const { return Hkv * nrb * nt; }
+    __device__ __forceinline__ int units(int Hkv) const { return Hkv * cost * nt; }
     __device__ __forceinline__ int items(int Hkv) const { return n > 0 ? Hkv * nt : 0; }
 };
 __device__ __forceinline__ bool seq_ok(const CacheAttnArgs& a, int b) {
@@ -99,6 +101,8 @@ __device__ __forceinline__ SeqShape seq_shape(const CacheAttnArgs& a, int b) {
     s.n = a.cu[b + 1] - a.cu[b];
     s.nrb = (s.n * a.rep + a.RB - 1) / a.RB;
     s.nt = (s.len + kCacheTile - 1) / kCacheTile + 1;
+    s.last = s.n * a.rep - (s.nrb - 1) * a.RB > 128 ? 2 : 1;
+    s.cost = s.nrb > 0 ? (s.nrb - 1) * (a.RB > 128 ? 2 : 1) + s.last : 0;
     return s;
 }
 
@@ -131,6 +135,13 @@ __device__ __forceinline__ int scan_lanes(int x, int lane) {  // inclusive
     }
     return x;
 }
+
+// Launches.  Every kernel of the cache may begin before the one ahead of it in the stream has ended
+// (launch_dependent), and waits for it (await_stream) before it touches anything; only then does it let
+// the next begin.  So the kernels after the first of a call may read the call's inputs, such as the
+// lengths, before their own wait.
+__device__ __forceinline__ void await_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void admit_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // The call's totals, and the place of the one sequence that want(place, shape, totals) picks (b = B
 // where it picks none).  Every thread of the block calls it.  Up to 32 sequences every warp scans
@@ -224,8 +235,37 @@ __device__ __forceinline__ int share_of(int x, int total, int G) {
     const int each = total / G, more = total % G, wide = more * (each + 1);
     return x < wide ? x / (each + 1) : more + (x - wide) / each;
 }
-// CTAs of the forward that get units, each at least one.
-__device__ __forceinline__ int ctas_of(const CacheAttnArgs& a, int total) { return min(total, a.G); }
+// CTAs of the forward that get units, each at least one, or two where tiles may cost two: then every CTA
+// whose share lies within a group holds the first unit of a tile, which is whose the tile is.
+__device__ __forceinline__ int ctas_of(const CacheAttnArgs& a, int total) {
+    return min(a.RB > 128 ? max(total / 2, 1) : total, a.G);
+}
+// The part of a sequence's units from loc on, count of them, that lies in one group: block k of KV head g,
+// tiles [tile0, tile1) (none, where the tile of the first unit is another CTA's); `units` is how many.
+struct Span {
+    int g, k, tile0, tile1, units;
+};
+__device__ __forceinline__ Span span_of(const CacheAttnArgs& a, const SeqShape& s, int loc, int count) {
+    Span x;
+    if (a.RB <= 128) {  // a unit a tile
+        const int grp = loc / s.nt;
+        x.tile0 = loc - grp * s.nt;
+        x.tile1 = min(s.nt, x.tile0 + count);
+        x.units = x.tile1 - x.tile0;
+        x.g = s.nrb == 1 ? grp : grp / s.nrb;
+        x.k = grp - x.g * s.nrb;
+        return x;
+    }
+    const int per = 2, head = s.cost * s.nt, block = per * s.nt;
+    x.g = loc / head;
+    const int in = loc % head;
+    x.k = min(in / block, s.nrb - 1);
+    const int c = x.k < s.nrb - 1 ? per : s.last, off = in - x.k * block;
+    x.units = min(count, c * s.nt - off);
+    x.tile0 = (off + c - 1) / c;
+    x.tile1 = (off + x.units + c - 1) / c;
+    return x;
+}
 
 // (-M, c / L) of a row: a row without keys, or of factor 0, has a factor of 0 and is left out.
 __device__ __forceinline__ float2 weight_factor(const CacheAttnArgs& a, float2 x, int64_t row) {
@@ -257,6 +297,23 @@ __device__ __forceinline__ uint64_t rows_that_see(const CacheAttnArgs& a, int64_
 
 // The tensor-core forwards of bf16 caches: keys on the lanes (up to 32 rows a (b, KV head)), rows on the
 // lanes (more).
+// A launch that may begin before the one ahead of it has ended.
+template <class Kernel, class... Args>
+cudaError_t launch_dependent(Kernel kernel, int64_t grid, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    return e == cudaSuccess ? cudaGetLastError() : e;
+}
+
 estp_status launch_cache_fwd_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_rows_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);

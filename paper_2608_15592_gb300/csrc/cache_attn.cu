@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
     __shared__ const char* vrow[kCacheTile];
     __shared__ float red[kThreads / 32][kRows];
     __shared__ float o_half[kRows][D];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    await_stream();
+    admit_next();
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const int c = blockIdx.x;
     Place at;
@@ -137,9 +138,9 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
             at.pass(s, a.c.Hkv);
             continue;
         }
-        const int loc = u - at.unit0, grp = loc / s.nt, tile0 = loc % s.nt;
-        const int tile1 = min(s.nt, tile0 + (u1 - u));
-        const int g = grp / s.nrb, r0 = grp % s.nrb * kRows, nr = min(kRows, s.n * a.rep - r0);
+        const Span span = span_of(a, s, u - at.unit0, u1 - u);
+        const int g = span.g, grp = g * s.nrb + span.k, tile0 = span.tile0, tile1 = span.tile1;
+        const int r0 = span.k * kRows, nr = min(kRows, s.n * a.rep - r0);
         const int64_t row0 = a.cu[at.b];
         __syncthreads();
         load_q<T, D>(a, q, at.b, g, r0, nr);
@@ -238,8 +239,9 @@ struct Pieces {
 };
 __device__ __forceinline__ Pieces pieces_of(const CacheAttnArgs& a, const Place& at, const SeqShape& s, int g, int r,
                                             int units) {
-    const int grp = g * s.nrb + r / a.RB, ub = at.unit0 + grp * s.nt, G = ctas_of(a, units);
-    const int c0 = share_of(ub, units, G), c1 = share_of(ub + s.nt - 1, units, G);
+    const int k = r / a.RB, per = a.RB > 128 ? 2 : 1, grp = g * s.nrb + k, G = ctas_of(a, units);
+    const int ub = at.unit0 + (g * s.cost + k * per) * s.nt;
+    const int c0 = share_of(ub, units, G), c1 = share_of(ub + (k < s.nrb - 1 ? per : s.last) * (s.nt - 1), units, G);
     return Pieces{(int64_t)(c0 + at.group0 + grp) * a.KS * a.RB + r % a.RB, (c1 - c0 + 1) * a.KS};
 }
 
@@ -286,7 +288,7 @@ template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAttnArgs a) {
     __shared__ PlanScratch sc;
     __shared__ float2 ml[kThreads / 32][kCacheMaxStored];  // a warp's (-M, c / L) of every row of (b, g)
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    admit_next();
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const bool for_rows = (int)blockIdx.x < a.row_blocks;
     const int c = for_rows ? blockIdx.x : blockIdx.x - a.row_blocks;
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
         const int y = a.cu[x.b] * a.Hq, it = share_begin(c, all.items, G);
         return for_rows ? x0 >= y && x0 < y + s.n * a.Hq : it >= x.item0 && it < x.item0 + s.items(a.c.Hkv);
     });
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the partials are complete
+    await_stream();  // the partials are complete
     if (!tot.ok) return;
     if (for_rows) {
         if (x0 >= x1) return;
@@ -455,7 +457,8 @@ __global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnA
         const int it = share_begin(c, all.items, G);
         return it >= x.item0 && it < x.item0 + s.items(a.c.Hkv);
     });
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the factors are complete
+    await_stream();  // the factors are complete
+    admit_next();
     if (!tot.ok) return;
     for_items(a, at, share_begin(c, tot.items, G), share_begin(c + 1, tot.items, G),
               [&](const Place& at, const SeqShape& s, int g, int tile0, int tile1) {
@@ -508,7 +511,7 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     // largest sequence
     const int64_t nrb = ((int64_t)a.max_rows * a.rep + a.RB - 1) / a.RB;
     const int64_t units = (int64_t)a.c.Hkv * nrb * (a.n_slots / kCacheTile + 2 * (int64_t)a.B);
-    if (units > INT32_MAX || a.n_rows * a.Hq > INT32_MAX)
+    if (2 * units > INT32_MAX || a.n_rows * a.Hq > INT32_MAX)
         return fail(ESTP_ERR_UNSUPPORTED, "max_slots and rows: more than 2^31 tiles of work, or rows times heads");
     const size_t o_bytes = align_up(sizeof(float) * (size_t)slots * a.KS * a.RB * D, 256);
     const size_t ml_bytes = align_up(sizeof(float2) * (size_t)slots * a.KS * a.RB, 256);
@@ -533,15 +536,14 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
         s = a.RB <= 32 ? launch_cache_fwd_tc(ctx, a, st) : launch_cache_rows_tc(ctx, a, st);
         if (s != ESTP_OK) return s;
     } else {
-        cache_fwd_kernel<T, D><<<(unsigned)a.G, kThreads, 0, st>>>(a);
-        e = cudaGetLastError();
+        e = launch_dependent(cache_fwd_kernel<T, D>, a.G, kThreads, 0, st, a);
         if (e != cudaSuccess) return cuda_fail(e, "cache attention launch");
     }
     // Few rows have many partials each (28 rows of one 32K sequence have 76: 17 us for a warp a row, 4 for
     // a block); many rows keep the GPU busy a warp each (6600 rows: 14 us, 30 for a block).  One wave of 8
-    // blocks an SM: 2 for them, 6 for the items of kept scores.
-    const int64_t some = 2 * ctx->num_sms;
-    a.row_warps = a.n_rows * a.Hq <= some ? kThreads / 32 : 1;
+    // blocks an SM: 2 for them and 6 for the items of kept scores, or all for them.
+    const int64_t some = (a.store ? 2 : 8) * ctx->num_sms;
+    a.row_warps = a.n_rows * a.Hq <= 2 * ctx->num_sms ? kThreads / 32 : 1;
     const int64_t row_blocks = (a.n_rows * a.Hq * a.row_warps + kThreads / 32 - 1) / (kThreads / 32);
     a.row_blocks = (int)(row_blocks < some ? row_blocks : some);
     const int64_t items = (int64_t)a.c.Hkv * (a.n_slots / kCacheTile + 2 * (int64_t)a.B), many = 6 * ctx->num_sms;

@@ -115,7 +115,6 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
     volatile int* issued_tiles = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 8);  // [2] K, V
     volatile uint32_t* odd = reinterpret_cast<volatile uint32_t*>(sm + S::kMiscOff + 16);  // [2][4] drafts with V not finite
 
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) {
@@ -147,6 +146,8 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    await_stream();
+    admit_next();
     const int cta = blockIdx.x;
     // the plan's scratch lies in the ring, which is unused until the barrier below
     Walk walk{Place{0, 0, 0, 0}, 0, 0};
@@ -615,8 +616,7 @@ estp_status launch(estp_ctx* ctx, const TcMaps& tm, const CacheAttnArgs& a, int 
     const int bit = 2 + (D == 128 ? 8 : 0) + (RB == 8 ? 0 : RB == 16 ? 1 : 2);
     cudaError_t e = set_smem(ctx, bit, cache_fwd_tc_kernel<D, RB>, S::kSmem);
     if (e != cudaSuccess) return cuda_fail(e, "cache attention smem attribute");
-    cache_fwd_tc_kernel<D, RB><<<(unsigned)a.G, S::kThreads, S::kSmem, st>>>(tm, a, box_rows, new_rows);
-    e = cudaGetLastError();
+    e = launch_dependent(cache_fwd_tc_kernel<D, RB>, a.G, S::kThreads, S::kSmem, st, tm, a, box_rows, new_rows);
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache attention launch");
 }
 

@@ -87,7 +87,6 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     volatile int* issued_tiles = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 8);  // [2] K, V
     volatile uint32_t* odd = reinterpret_cast<volatile uint32_t*>(sm + S::kMiscOff + 16);  // [2][4] drafts with V not finite
 
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < n_stages; ++i) {
@@ -111,6 +110,8 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    await_stream();
+    admit_next();
     const uint32_t tmem = *tmem_slot;
     const int cta = blockIdx.x;
     Walk walk{Place{0, 0, 0, 0}, 0, 0};
@@ -523,8 +524,8 @@ estp_status launch(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st) {
     if (s != ESTP_OK) return s;
     cudaError_t e = set_smem(ctx, D == 128 ? 21 : 20, cache_rows_tc_kernel<D>, 227 * 1024);
     if (e != cudaSuccess) return cuda_fail(e, "cache attention smem attribute");
-    cache_rows_tc_kernel<D><<<(unsigned)a.G, S::kThreads, S::smem(a.RB / 128), st>>>(tm, a, box_rows, new_rows, S::stages(a.RB / 128));
-    e = cudaGetLastError();
+    const int q_tiles = a.RB / 128;
+    e = launch_dependent(cache_rows_tc_kernel<D>, a.G, S::kThreads, (size_t)S::smem(q_tiles), st, tm, a, box_rows, new_rows, S::stages(q_tiles));
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache attention launch");
 }
 

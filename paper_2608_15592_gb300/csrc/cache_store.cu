@@ -61,6 +61,8 @@ __device__ __forceinline__ bool append_ok(const AppendArgs& a, int lo, int hi, i
 }
 
 __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendArgs a) {
+    await_stream();
+    admit_next();
     const int lane = threadIdx.x & 31;
     const int per = a.row_bytes / 16, n = a.c.Hkv * per;
     const int64_t total = min((int64_t)max(a.cu[a.B], 0), a.n_rows), e0 = max(a.cu[0], 0);
@@ -177,11 +179,13 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
     cg::cluster_group cl = cg::this_cluster();
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+    for (int i = t; i < kRounds * kBins / 4; i += kEvictThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+    await_stream();
+    admit_next();
     const int group = blockIdx.x / C, b = group / a.c.Hkv, g = group % a.c.Hkv;
     const int len = a.length[b], seen = a.seen[b];
     const bool bad = len < 0 || len > a.c.capacity();
     const int n = bad ? 0 : len;
-    for (int i = t; i < kRounds * kBins / 4; i += kEvictThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     __shared__ bool last;
     if (t == 0) last = last_arrival(a.done, gridDim.x);
@@ -444,8 +448,7 @@ estp_status launch_cache_append(estp_ctx* ctx, const CacheView& c, int row_bytes
     // a warp an entry, up to 5 blocks an SM (40 warps of 2 KB or more in flight), then several
     const int64_t blocks = n_rows > 0 ? (n_rows + kAppendWarps - 1) / kAppendWarps : 1, most = 5 * ctx->num_sms;
     const int64_t grid = blocks < most ? blocks : most;
-    append_kernel<<<(unsigned)grid, 32 * kAppendWarps, 0, st>>>(a);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_dependent(append_kernel, grid, 32 * kAppendWarps, 0, st, a);
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache append launch");
 }
 
@@ -470,18 +473,20 @@ estp_status launch_cache_evict(estp_ctx* ctx, const CacheView& c, int row_bytes,
     const size_t smem = sizeof(uint32_t) * ((size_t)a.key_cap + kRounds * kBins);
     cudaError_t e = set_smem(ctx, 0, evict_kernel, (size_t)(max_keys + kRounds * kBins) * 4);
     if (e != cudaSuccess) return cuda_fail(e, "cache evict smem attribute");
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)C;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(groups * C));
     cfg.blockDim = dim3(kEvictThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     e = cudaLaunchKernelEx(&cfg, evict_kernel, a);
     if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache evict launch");

@@ -142,15 +142,16 @@ struct Walk {
                 at.pass(o.s, a.c.Hkv);
                 continue;
             }
-            const int loc = u - at.unit0, grp = loc / o.s.nt;
-            o.tile0 = loc % o.s.nt;
-            o.tile1 = min(o.s.nt, o.tile0 + (u1 - u));
+            const Span x = span_of(a, o.s, u - at.unit0, u1 - u);
+            u += x.units;
+            if (x.tile0 >= x.tile1) continue;
+            o.tile0 = x.tile0;
+            o.tile1 = x.tile1;
             o.b = at.b;
-            o.g = grp / o.s.nrb;
-            o.r0 = grp % o.s.nrb * a.RB;
+            o.g = x.g;
+            o.r0 = x.k * a.RB;
             o.nr = min(a.RB, o.s.n * a.rep - o.r0);
-            o.group = at.group0 + grp;
-            u += o.tile1 - o.tile0;
+            o.group = at.group0 + x.g * o.s.nrb + x.k;
             return true;
         }
         return false;
@@ -295,22 +296,5 @@ inline estp_status make_maps(const CacheAttnArgs& a, TcMaps* tm, int* box_rows, 
     return s;
 }
 
-
-// A launch that may begin before the one ahead of it has ended (it waits where it needs it).
-template <class Kernel, class... Args>
-cudaError_t launch_dependent(Kernel kernel, int grid, int threads, size_t smem, cudaStream_t st, const Args&... args) {
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
-    return e == cudaSuccess ? cudaGetLastError() : e;
-}
 
 }  // namespace estp

@@ -113,7 +113,8 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the factors are complete
+    await_stream();  // the factors are complete
+    admit_next();
 
     if (warp == 0) {
         // ------------------------------------------------------------ producer
