@@ -64,13 +64,12 @@ struct CacheAttnArgs {
     const float* row_weight;
     float scale, scale_log2;
     int RB, G;
-    int KS;                      // partials of a segment
     int whole;                   // the forward finishes the groups that one CTA holds by itself
     int row_blocks;              // blocks of the finish kernel that merge rows, warps of one of them
     int row_warps;
     int store;                   // scores are kept for the weights
-    float* part_o;               // [G + groups][KS][RB][d]
-    float2* part_ml;             // [G + groups][KS][RB]: running max (log2 units) and sum
+    float* part_o;               // [G + groups][RB][d]
+    float2* part_ml;             // [G + groups][RB]: running max (log2 units) and sum
     float* score;                // [units][RB][128], unscaled
     float2* factor;              // [n_rows, Hq]: (-M, c / L), where the weights are wanted
     char* out;

@@ -118,7 +118,6 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
     __shared__ float red[kThreads / 32][kRows];
     __shared__ float o_half[kRows][D];
     await_stream();
-    admit_next();
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const int c = blockIdx.x;
     Place at;
@@ -230,9 +229,10 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
             if (half == 0) a.part_o[(slot * kRows + r) * D + col] = kHalves == 2 ? o[r] + o_half[r][col] : o[r];
         }
     }
+    admit_next();
 }
 
-// Pieces of row r of (b, g): CTAs c0..c1 hold the group, each with KS partials at slot c + group.
+// Pieces of row r of (b, g): CTAs c0..c1 hold the group, each with a partial at slot c + group.
 struct Pieces {
     int64_t first;  // part_ml element of the first
     int n;          // the others RB apart
@@ -242,7 +242,7 @@ __device__ __forceinline__ Pieces pieces_of(const CacheAttnArgs& a, const Place&
     const int k = r / a.RB, per = a.RB > 128 ? 2 : 1, grp = g * s.nrb + k, G = ctas_of(a, units);
     const int ub = at.unit0 + (g * s.cost + k * per) * s.nt;
     const int c0 = share_of(ub, units, G), c1 = share_of(ub + (k < s.nrb - 1 ? per : s.last) * (s.nt - 1), units, G);
-    return Pieces{(int64_t)(c0 + at.group0 + grp) * a.KS * a.RB + r % a.RB, (c1 - c0 + 1) * a.KS};
+    return Pieces{(int64_t)(c0 + at.group0 + grp) * a.RB + r % a.RB, c1 - c0 + 1};
 }
 
 // Joins (M, L) with another running maximum and sum.  Unfused products: two lanes that join each
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
             const int64_t row = x / a.Hq;
             const int h = x % a.Hq, i = (int)row - a.cu[at.b], r = i * a.rep + h % a.rep;
             const Pieces w = pieces_of(a, at, s, h / a.rep, r, tot.units);
-            if (a.whole && w.n == a.KS) continue;
+            if (a.whole && w.n == 1) continue;
             const float2 all = merged_ml(a, w, lane);
             float o[kC];
 #pragma unroll
@@ -333,7 +333,6 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     const float f = m[u] == all.x ? 1.f : ex2(m[u] - all.x);
-                    if (f == 0.f) continue;  // an empty partial holds nothing
 #pragma unroll
                     for (int k = 0; k < kC; ++k) o[k] = fmaf(f, v[u][k], o[k]);
                 }
@@ -366,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
         const int64_t row0 = a.cu[at.b];
         const int R = s.n * a.rep;
         __syncwarp();
-        if (a.whole && pieces_of(a, at, s, g, 0, tot.units).n == a.KS) {  // (kept scores of bf16: one block of rows)
+        if (a.whole && pieces_of(a, at, s, g, 0, tot.units).n == 1) {  // (kept scores of bf16: one block of rows)
             for (int r = lane; r < R; r += 32) f[r] = a.factor[(row0 + r / a.rep) * a.Hq + g * a.rep + r % a.rep];
         } else {
             for (int rw = 0; rw < R; rw += 4) {  // 8 lanes a row
@@ -497,11 +496,9 @@ template <class T, int D>
 estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     constexpr bool kTc = sizeof(T) == 2;
     a.RB = kRows;
-    a.KS = 1;
     if (kTc) {
         const int rows = a.max_rows * a.rep;
         a.RB = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
-        a.KS = 2;
     }
     a.whole = kTc;
     a.G = kTc ? ctx->num_sms : ctx->num_sms * 8;
@@ -513,8 +510,8 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     const int64_t units = (int64_t)a.c.Hkv * nrb * (a.n_slots / kCacheTile + 2 * (int64_t)a.B);
     if (2 * units > INT32_MAX || a.n_rows * a.Hq > INT32_MAX)
         return fail(ESTP_ERR_UNSUPPORTED, "max_slots and rows: more than 2^31 tiles of work, or rows times heads");
-    const size_t o_bytes = align_up(sizeof(float) * (size_t)slots * a.KS * a.RB * D, 256);
-    const size_t ml_bytes = align_up(sizeof(float2) * (size_t)slots * a.KS * a.RB, 256);
+    const size_t o_bytes = align_up(sizeof(float) * (size_t)slots * a.RB * D, 256);
+    const size_t ml_bytes = align_up(sizeof(float2) * (size_t)slots * a.RB, 256);
     const size_t z_bytes = sizeof(float) * (size_t)units * a.RB * kCacheTile;
     const bool weights = a.accumulate || a.w_new != nullptr;
     // Kept scores cost 8 bytes a row and key (a write and a read), forming them again a read of K
@@ -539,7 +536,7 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
         e = launch_dependent(cache_fwd_kernel<T, D>, a.G, kThreads, 0, st, a);
         if (e != cudaSuccess) return cuda_fail(e, "cache attention launch");
     }
-    // Few rows have many partials each (28 rows of one 32K sequence have 76: 17 us for a warp a row, 4 for
+    // Few rows have many partials each (28 rows of one 32K sequence with 76: 17 us for a warp a row, 4 for
     // a block); many rows keep the GPU busy a warp each (6600 rows: 14 us, 30 for a block).  One wave of 8
     // blocks an SM: 2 for them and 6 for the items of kept scores, or all for them.
     const int64_t some = (a.store ? 2 : 8) * ctx->num_sms;

@@ -39,7 +39,7 @@ namespace estp {
 namespace {
 
 // Two epilogue groups: they take the tiles of a segment in turn, each with a softmax of its own over the
-// block's RB rows, so that a segment leaves two partials (or both are joined here).
+// block's RB rows, joined at its end.
 constexpr int kGroups = 2;
 
 template <int D, int RB>
@@ -147,7 +147,6 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
     __syncthreads();
     tc_fence_after();
     await_stream();
-    admit_next();
     const int cta = blockIdx.x;
     // the plan's scratch lies in the ring, which is unused until the barrier below
     Walk walk{Place{0, 0, 0, 0}, 0, 0};
@@ -288,16 +287,9 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                         tc_fence_after();
                         issued = true;
                         const uint32_t pa = smem_u32(sm + S::kPOff) + nb * S::kPStep;
-                        const uint64_t vd = mn_desc(va, D == 128 ? kAtom : 0), pd = mn_desc(pa, kAtom);
-                        const uint32_t o = tmem + (uint32_t)(S::kOCol + nb * 2 * RB);
-                        if (ksteps == 8) {
-#pragma unroll
-                            for (int kk = 0; kk < 8; ++kk)  // 16 keys, 2 KB, a step
-                                mma_bf16<kIdO>(o, vd + kk * 128, pd + kk * 128, kk > 0 ? 1u : live[nb] ? 1u : 0u);
-                        } else {
-                            for (int kk = 0; kk < ksteps; ++kk)
-                                mma_bf16<kIdO>(o, vd + kk * 128, pd + kk * 128, live[nb] || kk > 0 ? 1u : 0u);
-                        }
+                        for (int kk = 0; kk < ksteps; ++kk)
+                            mma_bf16<kIdO>(tmem + (uint32_t)(S::kOCol + nb * 2 * RB), mn_desc(va + kk * 2048, D == 128 ? kAtom : 0),
+                                           mn_desc(pa + kk * 2048, kAtom), live[nb] || kk > 0 ? 1u : 0u);
                         mma_commit(&pv_done[nb]);
                         live[nb] = live[nb] || ksteps > 0;
                     }
@@ -519,83 +511,68 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
             }
             group_sync(bar);
             if (j < RB) row_f[j] = (row_w[j] + row_w[RB + j]) + (row_w[2 * RB + j] + row_w[3 * RB + j]);
-            if (!whole) {
-                const int64_t part = ((int64_t)(cta + sg.group) * kGroups + nb) * a.RB;
-                group_sync(bar);
-                if (j < nr) a.part_ml[part + j] = make_float2(row_m[j], row_f[j]);
-#pragma unroll 1
-                for (int r = 0; r < RB; r += kCols) {
-                    if (r >= nr) break;
-                    float hi[kCols], lo[kCols];
-                    tmem_ld_cols<kCols>(t_o + r, hi);
-                    tmem_ld_cols<kCols>(t_o + RB + r, lo);
-                    tmem_wait_ld();
-                    tie<kCols>(hi);
-                    tie<kCols>(lo);
-                    if (D == 128 || q < 2) {
-#pragma unroll
-                        for (int k = 0; k < kCols; ++k) {
-                            if (r + k >= nr) break;
-                            a.part_o[(part + r + k) * D + j] = live ? hi[k] + lo[k] : 0.f;
-                        }
-                    }
-                }
-            } else {
-                // what the groups' O count in o (a group without a key counts 0)
-                float* row_a = row_n + RB;
-                float* row_b = row_a + RB;
-                both_groups_or(false);
-                tc_fence_after();
-                if (j < RB) {
-                    const float *m0 = reinterpret_cast<const float*>(sm + S::kRowOff), *m1 = m0 + S::kRowArrays * RB;
-                    const float ma = m0[j], mb = m1[j], la = m0[RB + j], lb = m1[RB + j], M = fmaxf(ma, mb);
-                    float fa = ma == -INFINITY ? 0.f : ex2(ma - M), fb = mb == -INFINITY ? 0.f : ex2(mb - M);
-                    // a group without a maximum adds nothing, or NaN, which stays
-                    const float L = (fa != 0.f ? fa * la : M == -INFINITY ? la : 0.f) + (fb != 0.f ? fb * lb : M == -INFINITY ? lb : 0.f);
-                    if (L != L) fa = fb = 1.f;
-                    const bool none = M == -INFINITY && L == 0.f;
-                    const float inv = none ? 0.f : 1.f / L;
-                    if (nb == 0 && j < nr) {
+            // the groups' halves joined: what their O count (a group without a key counts 0), and the whole's scale
+            float* row_a = row_n + RB;
+            float* row_b = row_a + RB;
+            tc_fence_before();
+            both_groups_or(false);
+            tc_fence_after();
+            const int64_t part = (int64_t)(cta + sg.group) * a.RB;
+            if (j < RB) {
+                const float *m0 = reinterpret_cast<const float*>(sm + S::kRowOff), *m1 = m0 + S::kRowArrays * RB;
+                const float ma = m0[j], mb = m1[j], la = m0[RB + j], lb = m1[RB + j], M = fmaxf(ma, mb);
+                float fa = ma == -INFINITY ? 0.f : ex2(ma - M), fb = mb == -INFINITY ? 0.f : ex2(mb - M);
+                // a group without a maximum adds nothing, or NaN, which stays
+                const float L = (fa != 0.f ? fa * la : M == -INFINITY ? la : 0.f) + (fb != 0.f ? fb * lb : M == -INFINITY ? lb : 0.f);
+                if (L != L) fa = fb = 1.f;
+                const float scale = !whole ? 1.f : M == -INFINITY && L == 0.f ? 0.f : 1.f / L;
+                row_a[j] = fa * scale;
+                row_b[j] = fb * scale;
+                if (nb == 0 && j < nr) {
+                    if (whole) {
                         const int rr = sg.r0 + j, h = sg.g * a.rep + rr % a.rep;
                         const int64_t row = row0 + rr / a.rep;
                         if (a.lse != nullptr) a.lse[(int64_t)h * a.n_rows + row] = L == 0.f ? -INFINITY : fmaf(M, kLn2, logf(L));
                         if (a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, make_float2(M, L), row);
+                    } else {
+                        a.part_ml[part + j] = make_float2(M, L);
                     }
-                    row_a[j] = fa * inv;
-                    row_b[j] = fb * inv;
                 }
-                group_sync(bar);
-                // o of half the rows: lane = column
-                constexpr int kMine = RB / 2, kStep = kMine;
-                const uint32_t t_a = tmem + lane_off + (uint32_t)S::kOCol;
-#pragma unroll 1
-                for (int r = nb * kMine; r < (nb + 1) * kMine; r += kStep) {
-                    if (r >= nr) break;
-                    float hi[kStep], lo[kStep], hb[kStep], lb[kStep];
-                    tmem_ld_cols<kStep>(t_a + r, hi);
-                    tmem_ld_cols<kStep>(t_a + RB + r, lo);
-                    tmem_ld_cols<kStep>(t_a + 2 * RB + r, hb);
-                    tmem_ld_cols<kStep>(t_a + 3 * RB + r, lb);
-                    tmem_wait_ld();
-                    tie<kStep>(hi);
-                    tie<kStep>(lo);
-                    tie<kStep>(hb);
-                    tie<kStep>(lb);
-                    if (D == 128 || q < 2) {
+            }
+            group_sync(bar);
+            // O of half the rows a group: lane = column
+            constexpr int kMine = RB / 2;
+            const uint32_t t_a = tmem + lane_off + (uint32_t)S::kOCol;
+            {
+                const int r = nb * kMine;
+                float hi[kMine], lo[kMine], hb[kMine], lb[kMine];
+                tmem_ld_cols<kMine>(t_a + r, hi);
+                tmem_ld_cols<kMine>(t_a + RB + r, lo);
+                tmem_ld_cols<kMine>(t_a + 2 * RB + r, hb);
+                tmem_ld_cols<kMine>(t_a + 3 * RB + r, lb);
+                tmem_wait_ld();
+                tie<kMine>(hi);
+                tie<kMine>(lo);
+                tie<kMine>(hb);
+                tie<kMine>(lb);
+                if (D == 128 || q < 2) {
 #pragma unroll
-                        for (int k = 0; k < kStep; ++k) {
-                            if (r + k >= nr) break;
-                            const float wa = row_a[r + k], wb = row_b[r + k];
-                            float o = wa != 0.f ? (hi[k] + lo[k]) * wa : 0.f;
-                            if (wb != 0.f) o = fmaf(hb[k] + lb[k], wb, o);
+                    for (int k = 0; k < kMine; ++k) {
+                        if (r + k >= nr) break;
+                        const float wa = row_a[r + k], wb = row_b[r + k];
+                        float o = wa != 0.f ? (hi[k] + lo[k]) * wa : 0.f;
+                        if (wb != 0.f) o = fmaf(hb[k] + lb[k], wb, o);
+                        if (whole) {
                             const int rr = sg.r0 + r + k, h = sg.g * a.rep + rr % a.rep;
                             reinterpret_cast<__nv_bfloat16*>(a.out)[((row0 + rr / a.rep) * a.Hq + h) * D + j] = __float2bfloat16_rn(o);
+                        } else {
+                            a.part_o[(part + r + k) * D + j] = o;
                         }
                     }
                 }
-                tc_fence_before();
-                both_groups_or(false);  // O is read: the next segment's may begin
             }
+            tc_fence_before();
+            both_groups_or(false);  // O is read: the next segment's may begin
             tc_fence_before();
             group_sync(bar);  // row_w, row_m and P are free for the next segment
         }
@@ -603,6 +580,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    admit_next();  // (earlier, the next kernel's waiting blocks cost this one 3 %)
     if (threadIdx.x == 0 && *abort_flag) drain_ring(full, S::kStages, issued_tiles, a.status);
     if (warp == 1) {
         __syncwarp();

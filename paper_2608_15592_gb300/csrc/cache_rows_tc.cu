@@ -12,7 +12,7 @@
 //
 // One persistent CTA per SM over the units of cache.cuh, two epilogue groups of 128 threads, each with
 // an S/P buffer and an O (all 512 columns).  A block of up to 128 rows is split by tiles: the groups
-// take them in turn, each with a partial of its own.  A block of up to 256 rows is split by rows, 128 a
+// take them in turn, each with a softmax of its own, and are joined at a segment's end.  A block of up to 256 rows is split by rows, 128 a
 // group, and every tile goes to both.  Either way one group's softmax runs under the other's products.
 //   warps 0, 2 TMA producers of the K and of the V tiles (one ring, K and V in turn)
 //   warp 1     issues the products; the pipe runs them in the order of issue, so the S that overwrites
@@ -111,7 +111,6 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     __syncthreads();
     tc_fence_after();
     await_stream();
-    admit_next();
     const uint32_t tmem = *tmem_slot;
     const int cta = blockIdx.x;
     Walk walk{Place{0, 0, 0, 0}, 0, 0};
@@ -426,88 +425,72 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
             }
             const int h = sg.g * a.rep + rr % a.rep;
             const int64_t row = row0 + draft;
-            if (!whole) {
-                // split by rows: the second partial is empty
-                const int64_t two = (int64_t)(cta + sg.group) * 2 * a.RB, part = two + (split ? w * a.RB : base) + j;
-                if (mine) {
-                    a.part_ml[part] = make_float2(m, l);
-                    if (!split) a.part_ml[part + a.RB] = make_float2(-INFINITY, 0.f);
-                }
-#pragma unroll 1
-                for (int x = 0; x < D; x += 32) {
-                    float o[32];
-                    tmem_ld32(t_o + x, o);
-                    tmem_wait_ld();
-                    tie<32>(o);
-                    if (mine)
-#pragma unroll
-                        for (int k = 0; k < 32; k += 4)
-                            *reinterpret_cast<float4*>(a.part_o + part * D + x + k) =
-                                live ? make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
+            // split by tiles: joined with the other group's half, which lies on the same lanes
+            float M = m, L = l, fa = live ? 1.f : 0.f, fb = 0.f;
+            if (split) {
+                float2* ml = reinterpret_cast<float2*>(sm + S::kQOff);  // [2][128]: every S is done with Q
+                ml[w * 128 + j] = make_float2(m, l);
                 tc_fence_before();
-                both_groups_or(false);  // Q and O are free for the next segment
-            } else {
-                // a group of one CTA is finished here; split by tiles: with the other group's half, which lies on the same lanes
-                float M = m, L = l, fa = 1.f, fb = 0.f;  // (fb = 0: no other)
-                if (split) {
-                    float2* ml = reinterpret_cast<float2*>(sm + S::kQOff);  // [2][128]: every S is done with Q
-                    ml[w * 128 + j] = make_float2(m, l);
-                    tc_fence_before();
-                    both_groups_or(false);
-                    tc_fence_after();
-                    const float2 o = ml[(1 - w) * 128 + j];
-                    M = fmaxf(m, o.x);
-                    fa = m == -INFINITY ? 0.f : ex2(m - M);
-                    fb = o.x == -INFINITY ? 0.f : ex2(o.x - M);
-                    const float la = fa != 0.f ? fa * l : M == -INFINITY ? l : 0.f, lb = fb != 0.f ? fb * o.y : M == -INFINITY ? o.y : 0.f;
-                    L = w == 0 ? la + lb : lb + la;
-                    if (L != L) fa = fb = 1.f;  // NaN stays
-                }
-                const bool none = M == -INFINITY && L == 0.f;
-                const float inv = none ? 0.f : 1.f / L;
-                fa *= inv;
-                fb *= inv;
-                if (mine && (!split || w == 0)) {
-                    if (a.lse != nullptr) a.lse[(int64_t)h * a.n_rows + row] = L == 0.f ? -INFINITY : fmaf(M, kLn2, logf(L));
-                    if (a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, make_float2(M, L), row);
-                }
-                // split by tiles: each group writes half of the columns
-                const uint32_t t_b = tmem + lane_off + 256 + (1 - w) * 128;
-                const int cols = split ? D / 2 : D, x0 = split ? w * cols : 0;
-                __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (row * a.Hq + h) * D;
+                both_groups_or(false);
+                tc_fence_after();
+                const float2 o = ml[(1 - w) * 128 + j];
+                M = fmaxf(m, o.x);
+                fa = m == -INFINITY ? 0.f : ex2(m - M);
+                fb = o.x == -INFINITY ? 0.f : ex2(o.x - M);
+                const float la = fa != 0.f ? fa * l : M == -INFINITY ? l : 0.f, lb = fb != 0.f ? fb * o.y : M == -INFINITY ? o.y : 0.f;
+                L = w == 0 ? la + lb : lb + la;
+                if (L != L) fa = fb = 1.f;  // NaN stays
+            }
+            const float scale = !whole ? 1.f : M == -INFINITY && L == 0.f ? 0.f : 1.f / L;
+            fa *= scale;
+            fb *= scale;
+            const int64_t part = (int64_t)(cta + sg.group) * a.RB + base + j;
+            if (mine && (!split || w == 0)) {
+                if (!whole) a.part_ml[part] = make_float2(M, L);
+                if (whole && a.lse != nullptr) a.lse[(int64_t)h * a.n_rows + row] = L == 0.f ? -INFINITY : fmaf(M, kLn2, logf(L));
+                if (whole && a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, make_float2(M, L), row);
+            }
+            // split by tiles: each group writes half of the columns
+            const uint32_t t_b = tmem + lane_off + 256 + (1 - w) * 128;
+            const int cols = split ? D / 2 : D, x0 = split ? w * cols : 0;
+            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (row * a.Hq + h) * D;
 #pragma unroll 1
-                for (int x = x0; x < x0 + cols; x += 16) {
-                    float o[16], b[16];
-                    tmem_ld16(t_o + x, o);
-                    tmem_ld16(t_b + x, b);
-                    tmem_wait_ld();
-                    tie<16>(o);
-                    tie<16>(b);
-                    if (!mine) continue;
+            for (int x = x0; x < x0 + cols; x += 16) {
+                float o[16], b[16];
+                tmem_ld16(t_o + x, o);
+                tmem_ld16(t_b + x, b);
+                tmem_wait_ld();
+                tie<16>(o);
+                tie<16>(b);
+                if (!mine) continue;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    o[k] = fa != 0.f ? o[k] * fa : 0.f;
+                    if (fb != 0.f) o[k] = fmaf(b[k], fb, o[k]);
+                }
+                if (whole) {
                     uint32_t v[8];
 #pragma unroll
-                    for (int k = 0; k < 16; k += 2) {
-                        float y[2];
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            y[i] = fa != 0.f ? o[k + i] * fa : 0.f;
-                            if (fb != 0.f) y[i] = fmaf(b[k + i], fb, y[i]);
-                        }
-                        const __nv_bfloat162 t2 = __floats2bfloat162_rn(y[0], y[1]);
-                        v[k / 2] = *reinterpret_cast<const uint32_t*>(&t2);
+                    for (int k = 0; k < 8; ++k) {
+                        const __nv_bfloat162 t2 = __floats2bfloat162_rn(o[2 * k], o[2 * k + 1]);
+                        v[k] = *reinterpret_cast<const uint32_t*>(&t2);
                     }
                     *reinterpret_cast<uint4*>(out + x) = make_uint4(v[0], v[1], v[2], v[3]);
                     *reinterpret_cast<uint4*>(out + x + 8) = make_uint4(v[4], v[5], v[6], v[7]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4)
+                        *reinterpret_cast<float4*>(a.part_o + part * D + x + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                 }
-                tc_fence_before();
-                both_groups_or(false);  // Q and O are free for the next segment
             }
+            tc_fence_before();
+            both_groups_or(false);  // Q and O are free for the next segment
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    admit_next();
     if (threadIdx.x == 0 && *abort_flag) drain_ring(full, n_stages, issued_tiles, a.status);
     if (warp == 1) {
         __syncwarp();
