@@ -17,8 +17,8 @@
 // (every partial is relative to it).
 //
 // One persistent CTA per SM over the units of cache.cuh.
-//   warps 0, 3 TMA producers of the K and of the V tiles, which take turns in one ring, a box a page
-//              (a lane each); warp 3 also loads the rows' Q, a segment ahead
+//   warps 0, 3 TMA producers of the K and of the V tiles, a ring each, a box a page (a lane each); warp
+//              3 also loads the rows' Q, a segment ahead
 //   warp 1     issues S, as far ahead as K tiles and S buffers allow
 //   warp 2     issues O, as soon as a P is written
 //   warps 4-11 two epilogue groups of 4 warps, each with its S (double-buffered) and O in tensor
@@ -56,6 +56,7 @@ struct Shape {
     static constexpr int kFixed = kQBufs * kQBytes + kPBytes;
     static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 400 - kGroups * (kRowArrays + 4) * RB * 4;
     static constexpr int kStages = kRoom / kTileBytes < 12 ? kRoom / kTileBytes : 12;
+    static constexpr int kKStages = kStages / 2;   // V tiles wait longer in their slots
     static constexpr int kThreads = 128 + 128 * kGroups;
     static constexpr int kTmemUsed = kGroups * (2 * kN + 2 * RB);  // S twice, O hi and lo
     static constexpr int kTmem = kTmemUsed <= 128 ? 128 : kTmemUsed <= 256 ? 256 : 512;
@@ -101,8 +102,10 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
     constexpr int NB = kGroups;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
-    uint64_t* full = reinterpret_cast<uint64_t*>(sm + S::kBarOff);  // [kStages]
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + S::kBarOff);  // [kStages], K then V
     uint64_t* empty = full + S::kStages;                            // [kStages]
+    const Ring ring_k{full, empty, sm, S::kKStages, S::kTileBytes};
+    const Ring ring_v{full + S::kKStages, empty + S::kKStages, sm + S::kKStages * S::kTileBytes, S::kStages - S::kKStages, S::kTileBytes};
     uint64_t* q_full = empty + S::kStages;                          // [kQBufs]
     uint64_t* q_empty = q_full + S::kQBufs;                         // [kQBufs]
     uint64_t* s_full = q_empty + S::kQBufs;                         // [NB][2]
@@ -168,6 +171,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
         // ------------------------------------------------------------ producers
         // warp 0 the K tiles (even ring entries), warp 3 the V tiles (odd ones) and the rows' Q
         const int kv = warp == 3;
+        const Ring ring = kv ? ring_v : ring_k;
         if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(
                           kv ? (lane ? &tm.vn : &tm.v) : (lane ? &tm.kn : &tm.k))) : "memory");
         uint32_t t = 0, q_seg = 0;  // tiles issued; segments whose Q is loaded
@@ -205,14 +209,12 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
         while (ok && walk.next(a, sg)) {
             win.open(a, sg.s, sg.b, sg.tile0, lane);
             for (int tile = sg.tile0; tile < sg.tile1; ++tile, ++t) {
-                const uint32_t e = 2 * t + kv, use = e / S::kStages;
-                const int slot = (int)(e % S::kStages);
-                if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
+                if (t >= (uint32_t)ring.n && !warp_wait(ring.freed(t), ring.parity(t - ring.n), abort_flag, a.status, a.wait_cycles)) {
                     ok = false;
                     break;
                 }
                 load_tile<D>(a, kv ? &tm.v : &tm.k, kv ? &tm.vn : &tm.kn, win, sg.s, sg.b, sg.g, tile, box_rows, new_rows,
-                             sm + slot * S::kTileBytes, &full[slot], lane);
+                             ring.tile(t), ring.filled(t), lane);
                 if (kv && tile == sg.tile0) load_q();  // a failure shows at the next wait
             }
         }
@@ -235,10 +237,8 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                 if (!wait(&q_full[qb], (seg / S::kQBufs) & 1)) break;
                 ++seg;
                 for (int i = 0; ok && i < tiles; ++i, ++t) {
-                    const uint32_t e = 2 * t;
-                    const int slot = (int)(e % S::kStages);
-                    if (!wait(&full[slot], (e / S::kStages) & 1)) break;
-                    const uint32_t ka = smem_u32(sm + slot * S::kTileBytes);
+                    if (!wait(ring_k.filled(t), ring_k.parity(t))) break;
+                    const uint32_t ka = smem_u32(ring_k.tile(t));
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
                         if ((i & 1) != nb) continue;
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                                                  smem_u32(sm + S::kQOff + qb * S::kQBytes), S::kN * 128);
                         mma_commit(&s_full[2 * nb + buf]);
                     }
-                    if (ok) mma_commit(&empty[slot]);
+                    if (ok) mma_commit(ring_k.freed(t));
                 }
                 if (ok) mma_commit(&q_empty[qb]);
             }
@@ -275,10 +275,8 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                 const int tiles = sg.tile1 - sg.tile0;
                 bool live[NB] = {};  // a group's O holds a product of this segment
                 for (int i = 0; ok && i < tiles; ++i, ++t) {
-                    const uint32_t e = 2 * t + 1;
-                    const int slot = (int)(e % S::kStages);
-                    if (!wait(&full[slot], (e / S::kStages) & 1)) break;
-                    const uint32_t va = smem_u32(sm + slot * S::kTileBytes);
+                    if (!wait(ring_v.filled(t), ring_v.parity(t))) break;
+                    const uint32_t va = smem_u32(ring_v.tile(t));
                     const int ksteps = (tile_keys(a, sg.s, sg.tile0 + i) + 15) / 16;
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
@@ -293,7 +291,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                         mma_commit(&pv_done[nb]);
                         live[nb] = live[nb] || ksteps > 0;
                     }
-                    if (ok) mma_commit(&empty[slot]);
+                    if (ok) mma_commit(ring_v.freed(t));
                 }
             }
             if (issued) {
@@ -445,10 +443,9 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                 }
                 if (drafts || (keys & 15)) {
                     // V rows that must not reach the product: past the keys, and drafts that are not finite
-                    const uint32_t e = 2 * (t + (tile - sg.tile0)) + 1;
-                    const int slot = (int)(e % S::kStages);
-                    wait(&full[slot], (e / S::kStages) & 1);
-                    uint8_t* vr = sm + slot * S::kTileBytes + j * 128;
+                    const uint32_t tv = t + (tile - sg.tile0);
+                    wait(ring_v.filled(tv), ring_v.parity(tv));
+                    uint8_t* vr = ring_v.tile(tv) + j * 128;
                     bool clear = j >= keys && j < ((keys + 15) & ~15);
                     if (drafts && j < keys) clear = row_not_finite<D>(vr);
                     if (drafts) {
@@ -581,7 +578,10 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
     __syncthreads();
     tc_fence_after();
     admit_next();  // (earlier, the next kernel's waiting blocks cost this one 3 %)
-    if (threadIdx.x == 0 && *abort_flag) drain_ring(full, S::kStages, issued_tiles, a.status);
+    if (threadIdx.x == 0 && *abort_flag) {
+        ring_k.drain(issued_tiles[0], a.status);
+        ring_v.drain(issued_tiles[1], a.status);
+    }
     if (warp == 1) {
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmem));

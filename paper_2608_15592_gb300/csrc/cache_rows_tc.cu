@@ -14,7 +14,7 @@
 // an S/P buffer and an O (all 512 columns).  A block of up to 128 rows is split by tiles: the groups
 // take them in turn, each with a softmax of its own, and are joined at a segment's end.  A block of up to 256 rows is split by rows, 128 a
 // group, and every tile goes to both.  Either way one group's softmax runs under the other's products.
-//   warps 0, 2 TMA producers of the K and of the V tiles (one ring, K and V in turn)
+//   warps 0, 2 TMA producers of the K and of the V tiles, a ring each
 //   warp 1     issues the products; the pipe runs them in the order of issue, so the S that overwrites
 //              a P comes after the product that reads it
 //   warp 3     idle
@@ -75,8 +75,11 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = smem_raw + (-smem_u32(smem_raw) & 1023u);
     uint8_t* ring = sm + S::kQOff + (a.RB / 128) * S::kTileBytes;
-    uint64_t* full = reinterpret_cast<uint64_t*>(sm);  // [kMaxStages]
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm);  // [kMaxStages], K then V
     uint64_t* empty = full + S::kMaxStages;            // [kMaxStages]
+    const int k_stages = n_stages / 2;                 // V tiles wait longer in their slots
+    const Ring ring_k{full, empty, ring, k_stages, S::kTileBytes};
+    const Ring ring_v{full + k_stages, empty + k_stages, ring + k_stages * S::kTileBytes, n_stages - k_stages, S::kTileBytes};
     uint64_t* q_full = empty + S::kMaxStages;          // both groups' rows
     uint64_t* s_full = q_full + 1;                     // [2]
     uint64_t* p_full = s_full + 2;                     // [2]
@@ -130,6 +133,7 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     if (warp == 0 || warp == 2) {
         // ------------------------------------------------------------ producers
         const int kv = warp == 2;
+        const Ring mine = kv ? ring_v : ring_k;
         if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(
                           kv ? (lane ? &tm.vn : &tm.v) : (lane ? &tm.kn : &tm.k))) : "memory");
         uint32_t t = 0;
@@ -138,14 +142,12 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
         while (ok && walk.next(a, sg)) {
             win.open(a, sg.s, sg.b, sg.tile0, lane);
             for (int tile = sg.tile0; tile < sg.tile1; ++tile, ++t) {
-                const uint32_t e = 2 * t + kv, use = e / n_stages;
-                const int slot = (int)(e % n_stages);
-                if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
+                if (t >= (uint32_t)mine.n && !warp_wait(mine.freed(t), mine.parity(t - mine.n), abort_flag, a.status, a.wait_cycles)) {
                     ok = false;
                     break;
                 }
                 load_tile<D>(a, kv ? &tm.v : &tm.k, kv ? &tm.vn : &tm.kn, win, sg.s, sg.b, sg.g, tile, box_rows, new_rows,
-                             ring + slot * S::kTileBytes, &full[slot], lane);
+                             mine.tile(t), mine.filled(t), lane);
             }
         }
         if (lane == 0) issued_tiles[kv] = (int)t;
@@ -161,8 +163,8 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
                 ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
                 return ok;
             };
-            auto release = [&](uint32_t e) {
-                if (ok) mma_commit(&empty[e % n_stages]);
+            auto release = [&](uint64_t* freed) {
+                if (ok) mma_commit(freed);
             };
             while (ok && walk.next(a, sg)) {
                 const int tiles = sg.tile1 - sg.tile0;
@@ -170,23 +172,19 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
                 bool live[2] = {false, false};
                 if (!wait(q_full, seg++ & 1)) break;
                 auto product_s = [&](int i, int w) {  // S of the segment's tile i for group w
-                    const uint32_t e = 2 * (t + i);
-                    const int slot = (int)(e % n_stages);
-                    if (!wait(&full[slot], (e / n_stages) & 1)) return;
+                    if (!wait(ring_k.filled(t + i), ring_k.parity(t + i))) return;
                     tc_fence_after();
                     issued = true;
-                    const uint32_t ka = smem_u32(ring + slot * S::kTileBytes);
+                    const uint32_t ka = smem_u32(ring_k.tile(t + i));
                     const uint32_t qa = smem_u32(sm + S::kQOff) + (split ? 0 : w * S::kTileBytes);
                     product_k_major<kIdS, D>(tmem + w * 128, qa, kAtom, ka, kAtom);
                     mma_commit(&s_full[w]);
                 };
                 auto product_o = [&](int i, int w) {
-                    const uint32_t e = 2 * (t + i) + 1;
-                    const int slot = (int)(e % n_stages);
-                    if (!wait(&full[slot], (e / n_stages) & 1) || !wait(&p_full[w], p_seen[w]++ & 1)) return;
+                    if (!wait(ring_v.filled(t + i), ring_v.parity(t + i)) || !wait(&p_full[w], p_seen[w]++ & 1)) return;
                     tc_fence_after();
                     issued = true;
-                    const uint32_t va = smem_u32(ring + slot * S::kTileBytes), p = tmem + w * 128, o = tmem + 256 + w * 128;
+                    const uint32_t va = smem_u32(ring_v.tile(t + i)), p = tmem + w * 128, o = tmem + 256 + w * 128;
                     const int ksteps = (tile_keys(a, sg.s, sg.tile0 + i) + 15) / 16;
                     const uint64_t vd = mn_desc(va, kAtom);
                     auto keys16 = [&](int kk, uint32_t acc) {  // 16 keys, 2 KB of V: hi and lo
@@ -206,26 +204,26 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
                 if (split) {
                     for (int i = 0; ok && i < 2 && i < tiles; ++i) {
                         product_s(i, i);
-                        release(2 * (t + i));
+                        release(ring_k.freed(t + i));
                     }
                     for (int i = 0; ok && i < tiles; ++i) {
                         product_o(i, i & 1);
-                        release(2 * (t + i) + 1);
+                        release(ring_v.freed(t + i));
                         if (ok && i + 2 < tiles) {
                             product_s(i + 2, i & 1);
-                            release(2 * (t + i + 2));
+                            release(ring_k.freed(t + i + 2));
                         }
                     }
                 } else {
                     for (int w = 0; ok && w < 2; ++w) product_s(0, w);
-                    release(2 * t);
+                    release(ring_k.freed(t));
                     for (int i = 0; ok && i < tiles; ++i) {
                         for (int w = 0; ok && w < 2; ++w) {
                             product_o(i, w);
-                            if (w == 1) release(2 * (t + i) + 1);
+                            if (w == 1) release(ring_v.freed(t + i));
                             if (ok && i + 1 < tiles) product_s(i + 1, w);
                         }
-                        if (i + 1 < tiles) release(2 * (t + i + 1));
+                        if (i + 1 < tiles) release(ring_k.freed(t + i + 1));
                     }
                 }
                 t += tiles;
@@ -371,10 +369,9 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 if ((split || w == 0) && (drafts || (keys & 15))) {
                     // V rows that must not reach the product: past the keys, and drafts that are not finite
-                    const uint32_t e = 2 * (t + (tile - sg.tile0)) + 1;
-                    const int slot = (int)(e % n_stages);
-                    wait(&full[slot], (e / n_stages) & 1);
-                    uint8_t* vr = ring + slot * S::kTileBytes + j * 128;
+                    const uint32_t tv = t + (tile - sg.tile0);
+                    wait(ring_v.filled(tv), ring_v.parity(tv));
+                    uint8_t* vr = ring_v.tile(tv) + j * 128;
                     bool clear = j >= keys && j < ((keys + 15) & ~15);
                     if (drafts && j < keys) clear = row_not_finite<D>(vr);
                     if (drafts) {
@@ -491,7 +488,10 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     __syncthreads();
     tc_fence_after();
     admit_next();
-    if (threadIdx.x == 0 && *abort_flag) drain_ring(full, n_stages, issued_tiles, a.status);
+    if (threadIdx.x == 0 && *abort_flag) {
+        ring_k.drain(issued_tiles[0], a.status);
+        ring_v.drain(issued_tiles[1], a.status);
+    }
     if (warp == 1) {
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));

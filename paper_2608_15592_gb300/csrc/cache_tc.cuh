@@ -244,18 +244,23 @@ __device__ __forceinline__ void clear_row(uint8_t* row) {
     for (int x = 0; x < D / 8; ++x) *reinterpret_cast<uint4*>(row + (x >> 3) * kAtom + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
 }
 
-// A CTA that gave up: the last copy into every slot of the ring lands before it exits (all others have
-// been waited for by the issuers).  issued[0] K tiles lie in the even entries, issued[1] V tiles in the odd.
-__device__ __forceinline__ void drain_ring(uint64_t* full, int stages, const volatile int* issued, int* status) {
-    const int n = 2 * max(issued[0], issued[1]);
-    uint32_t seen = 0;
-    for (int e = n - 1; e >= 0 && e >= n - 2 * stages; --e) {
-        const int slot = e % stages;
-        if (e / 2 >= issued[e & 1] || (seen >> slot & 1)) continue;
-        seen |= 1u << slot;
-        drain_wait(&full[slot], (e / stages) & 1, status);
+// The rings of K and V tiles.  Each has its own slots and its own producer warp: a slot's barriers are
+// followed by parity, which holds only if one warp issues all of the slot's copies in order (shared by two,
+// a warp that was a phase ahead of the other would take a phase two back for its own).
+struct Ring {
+    uint64_t *full, *empty;
+    uint8_t* tiles;
+    int n, tile_bytes;
+    __device__ __forceinline__ int slot(uint32_t t) const { return (int)(t % n); }
+    __device__ __forceinline__ uint32_t parity(uint32_t t) const { return (t / n) & 1; }
+    __device__ __forceinline__ uint8_t* tile(uint32_t t) const { return tiles + slot(t) * tile_bytes; }
+    __device__ __forceinline__ uint64_t* filled(uint32_t t) const { return &full[slot(t)]; }
+    __device__ __forceinline__ uint64_t* freed(uint32_t t) const { return &empty[slot(t)]; }
+    // a CTA that gave up: the last copy into every slot lands before it exits (others have been waited for)
+    __device__ __forceinline__ void drain(int issued, int* status) const {
+        for (int t = issued - 1; t >= 0 && t >= issued - n; --t) drain_wait(filled(t), parity(t), status);
     }
-}
+};
 
 // Pages as (d, slot, KV head, page); a box is 64 values of box_rows slots of one head.
 inline estp_status pages_map(CUtensorMap* m, const CacheView& c, const void* base, const void* other, int box_rows) {

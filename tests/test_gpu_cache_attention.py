@@ -86,6 +86,14 @@ CASES = [
     ([33, 520], [5, 128], 8, 1, 64, 32),
     ([777], [4], 64, 1, 128, 16),
     ([4000], [1], 7, 1, 128, 8),
+    # many tiles a CTA in every kernel: several turns of the rings, several sequences a CTA
+    ([9000, 12000, 700, 8000], [1, 1, 1, 1], 64, 16, 128, 64),
+    ([9000, 7000, 500, 8000], [3, 4, 1, 4], 64, 16, 128, 128),
+    ([9000, 7000, 500, 8000], [7, 8, 5, 8], 64, 16, 128, 64),
+    ([9000, 7000, 500, 8000], [7, 8, 5, 8], 64, 16, 64, 32),
+    ([5000, 4000, 500, 3000], [30, 20, 9, 17], 64, 16, 128, 64),
+    ([5000, 4000, 500, 3000], [70, 40, 9, 100], 32, 8, 128, 64),
+    ([5000, 4000, 500, 3000], [70, 40, 9, 100], 32, 8, 64, 16),
 ]
 
 
