@@ -56,7 +56,7 @@ struct Shape {
     static constexpr int kFixed = kQBufs * kQBytes + kPBytes;
     static constexpr int kRoom = 227 * 1024 - 1024 - kFixed - 400 - kGroups * (kRowArrays + 4) * RB * 4;
     static constexpr int kStages = kRoom / kTileBytes < 12 ? kRoom / kTileBytes : 12;
-    static constexpr int kKStages = kStages / 2;   // V tiles wait longer in their slots
+    static constexpr int kKStages = (kStages - 1) / 2;  // a V tile waits through the softmax: 3 + 3 slots cost 16 of 445 us, 4 + 2 30
     static constexpr int kThreads = 128 + 128 * kGroups;
     static constexpr int kTmemUsed = kGroups * (2 * kN + 2 * RB);  // S twice, O hi and lo
     static constexpr int kTmem = kTmemUsed <= 128 ? 128 : kTmemUsed <= 256 ? 256 : 512;
