@@ -8,7 +8,8 @@
 namespace estp {
 namespace {
 
-constexpr int kWRows = 448, kWBlock = 64, kWMinStages = 3, kWMaxStages = 6, kWBufs = 4;
+constexpr int kWRows = 448, kWBlock = 64, kWMinStages = 3, kWMaxStages = 6, kWBufs = 2;
+constexpr int kWCols = 2 * kWBlock;  // of one product: two blocks of rows, the last perhaps one
 template <int D>
 struct WShape {
     static constexpr int kAtoms = D / 64;
@@ -17,9 +18,10 @@ struct WShape {
     // from a 1024-aligned base: barriers, factors and sums first, then Q blocks and as many K tiles as fit
     static constexpr int kBars = 2 * kWMaxStages + 1 + 4 * kWBufs + 1;
     static constexpr int kMiscOff = kBars * 8;          // tmem address, abort flag
-    static constexpr int kFOff = 256;                   // [kWRows] factors
+    static constexpr int kNzOff = kMiscOff + 16;        // [kWRows / 32] rows with a factor
+    static constexpr int kFOff = 256;                   // [kWRows / 2][4] factors of two rows: offsets, then multiples
     static constexpr int kQOff = (kFOff + kWRows * 8 + 1023) / 1024 * 1024;
-    static_assert(kMiscOff + 8 <= kFOff, "barriers");
+    static_assert(kNzOff + kWRows / 8 <= kFOff, "barriers");
     static constexpr int kThreads = 64 + 256;
     static constexpr int kRoom = 227 * 1024 - 1024 - kQOff;
     static int stages(int blocks) {
@@ -90,7 +92,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
-                     "r"(2 * kWBufs * kWBlock));
+                     "r"(2 * kWBufs * kWCols));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     tc_fence_before();
@@ -143,7 +145,8 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
         if (lane == 0) {
-            constexpr uint32_t kId = idesc_bf16(kCacheTile, kWBlock);
+            constexpr uint32_t kId2 = idesc_bf16(kCacheTile, kWCols), kId1 = idesc_bf16(kCacheTile, kWBlock);
+            const uint32_t q_atom = q_blocks * kWBlock * 128;
             uint32_t e = 0, loads = 0, steps[2] = {0, 0};
             bool ok = true, issued = false;
             auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -160,13 +163,16 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                         if (!wait(&full[slot], (e / n_stages) & 1)) break;
                         const uint32_t ka = smem_u32(ring + slot * S::kTileBytes);
                         const int gr = (tile - w.tile0) & 1;
-                        for (int k = 0; k < blocks; ++k) {
+                        for (int k = 0; k < blocks; k += 2) {
                             const uint32_t n = steps[gr]++, buf = n % kWBufs, use = n / kWBufs;
                             if (use >= 1 && !wait(&s_empty[gr * kWBufs + buf], (use - 1) & 1)) break;
                             tc_fence_after();
                             issued = true;
-                            product_k_major<kId, D>(tmem + (gr * kWBufs + buf) * kWBlock, ka, kAtom,
-                                                    smem_u32(sm + S::kQOff + k * S::kBlockBytes), kWBlock * 128);
+                            const uint32_t to = tmem + (gr * kWBufs + buf) * kWCols, qa = smem_u32(sm + S::kQOff) + k * kWBlock * 128;
+                            if (k + 1 < blocks)
+                                product_k_major<kId2, D>(to, ka, kAtom, qa, q_atom);
+                            else
+                                product_k_major<kId1, D>(to, ka, kAtom, qa, q_atom);
                             mma_commit(&s_full[gr * kWBufs + buf]);
                         }
                         if (ok) mma_commit(&empty[slot]);
@@ -182,7 +188,9 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
     } else {
         // ------------------------------------------------------------- epilogue
         const int gr = (warp - 2) >> 2, q = warp & 3, j = q * 32 + lane, tid = threadIdx.x - 64;
-        float2* fs = reinterpret_cast<float2*>(sm + S::kFOff);
+        float* fs = reinterpret_cast<float*>(sm + S::kFOff);
+        uint32_t* nz = reinterpret_cast<uint32_t*>(sm + S::kNzOff);
+        const uint32_t q_atom = q_blocks * kWBlock * 128;  // Q: [D / 64][rows] of 128 bytes
         uint32_t step = 0;
         bool alive = true;
         while (alive && w.next(a)) {
@@ -196,14 +204,18 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                     const int r = x / (D / 8), ch = x % (D / 8);
                     const int rr = r < nr ? r0 + r : r0, i = rr / a.rep, h = w.g * a.rep + rr % a.rep;
                     const char* from = a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16;
-                    const uint32_t at = smem_u32(sm + S::kQOff) + (r / kWBlock) * S::kBlockBytes + (ch >> 3) * kWBlock * 128 +
-                                        (r % kWBlock) * 128 + (((ch & 7) ^ (r & 7)) << 4);
+                    const uint32_t at = smem_u32(sm + S::kQOff) + (ch >> 3) * q_atom + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(r < nr ? 16 : 0)
                                  : "memory");
                 }
-                for (int r = tid; r < blocks * kWBlock; r += 256)
-                    fs[r] = r < nr ? a.factor[(row0 + (r0 + r) / a.rep) * a.Hq + w.g * a.rep + (r0 + r) % a.rep]
-                                   : make_float2(0.f, 0.f);
+                for (int r = tid; r < blocks * kWBlock; r += 256) {  // whole warps
+                    float2 f = make_float2(0.f, 0.f);
+                    if (r < nr) f = a.factor[(row0 + (r0 + r) / a.rep) * a.Hq + w.g * a.rep + (r0 + r) % a.rep];
+                    fs[(r >> 1) * 4 + (r & 1)] = f.x;
+                    fs[(r >> 1) * 4 + 2 + (r & 1)] = f.y;
+                    const uint32_t bits = __ballot_sync(0xffffffffu, f.y != 0.f);
+                    if (lane == 0) nz[r >> 5] = bits;
+                }
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 both_groups_or(false);  // the factors are everyone's
@@ -226,37 +238,54 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                             }
                         }
                     }
-                    float sum[2] = {0.f, 0.f};
-                    for (int k = 0; k < blocks; ++k, ++step) {
+                    float2 sum[2] = {};
+                    for (int k = 0; k < blocks; ++k) {
                         const uint32_t buf = step % kWBufs;
-                        if (alive)
-                            alive = warp_wait(&s_full[gr * kWBufs + buf], (step / kWBufs) & 1, abort_flag, a.status, a.wait_cycles);
-                        tc_fence_after();
-                        const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (gr * kWBufs + buf) * kWBlock;
+                        if (!(k & 1)) {
+                            if (alive)
+                                alive = warp_wait(&s_full[gr * kWBufs + buf], (step / kWBufs) & 1, abort_flag, a.status, a.wait_cycles);
+                            tc_fence_after();
+                        }
+                        const uint32_t ta = tmem + ((uint32_t)(q * 32) << 16) + (gr * kWBufs + buf) * kWCols + (k & 1) * kWBlock;
                         const int cols = min(kWBlock, nr - k * kWBlock);
-                        const uint64_t seen = drafts ? rows_that_see(a, row0, keys, j, r0 + k * kWBlock, cols) : ~0ull;
+                        uint64_t seen = (uint64_t)nz[2 * k + 1] << 32 | nz[2 * k];  // none past the rows
+                        if (drafts) seen &= rows_that_see(a, row0, keys, j, r0 + k * kWBlock, cols);
                         float z[kWBlock];
-#pragma unroll
-                        for (int c = 0; c < kWBlock; c += 16) tmem_ld16(ta + c, z + c);
+                        tmem_ld32(ta, z);
+                        tmem_ld32(ta + 32, z + 32);
                         tmem_wait_ld();
                         tie<kWBlock>(z);
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&s_empty[gr * kWBufs + buf]);
-                        const float4* f4 = reinterpret_cast<const float4*>(fs + k * kWBlock);
+                        if ((k & 1) || k + 1 == blocks) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&s_empty[gr * kWBufs + buf]);
+                            ++step;
+                        }
+                        const float4* f4 = reinterpret_cast<const float4*>(fs + k * kWBlock * 2);
+                        const float2 c2 = make_float2(a.scale_log2, a.scale_log2);
+                        if (__all_sync(0xffffffffu, seen == ~0ull)) {
 #pragma unroll
-                        for (int c = 0; c < kWBlock; c += 16) {
-                            if (c >= cols) break;
-#pragma unroll
-                            for (int i = c; i < c + 16; i += 2) {  // columns past the rows have a factor of 0
+                            for (int i = 0; i < kWBlock; i += 2) {
                                 const float4 f = f4[i / 2];
-                                const float e0 = ex2(fmaf(z[i], a.scale_log2, f.x)), e1 = ex2(fmaf(z[i + 1], a.scale_log2, f.z));
-                                sum[0] = f.y != 0.f && (seen >> i & 1) ? fmaf(e0, f.y, sum[0]) : sum[0];
-                                sum[1] = f.w != 0.f && (seen >> i & 2) ? fmaf(e1, f.w, sum[1]) : sum[1];
+                                const float2 y = __ffma2_rn(make_float2(z[i], z[i + 1]), c2, make_float2(f.x, f.y));
+                                sum[i / 2 & 1] = __ffma2_rn(make_float2(ex2(y.x), ex2(y.y)), make_float2(f.z, f.w), sum[i / 2 & 1]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < kWBlock; c += 16) {
+                                if (c >= cols) break;
+#pragma unroll
+                                for (int i = c; i < c + 16; i += 2) {
+                                    const float4 f = f4[i / 2];
+                                    const float2 y = __ffma2_rn(make_float2(z[i], z[i + 1]), c2, make_float2(f.x, f.y));
+                                    float2& s2 = sum[i / 2 & 1];
+                                    if (seen >> i & 1) s2.x = fmaf(ex2(y.x), f.z, s2.x);
+                                    if (seen >> i & 2) s2.y = fmaf(ex2(y.y), f.w, s2.y);
+                                }
                             }
                         }
                     }
-                    if (to != nullptr) *to = had + (sum[0] + sum[1]);
+                    if (to != nullptr) *to = had + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
                 }
                 if (both_groups_or(!alive)) alive = false;  // Q and the factors are free
             }
@@ -267,7 +296,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
     tc_fence_after();
     if (warp == 1) {
         __syncwarp();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kWBufs * kWBlock));
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kWBufs * kWCols));
     }
 }
 
