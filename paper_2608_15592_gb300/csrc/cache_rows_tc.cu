@@ -35,7 +35,7 @@ struct RowShape {
     static constexpr int kMaxStages = 12;
     static constexpr int kThreads = 384;
     // from a 1024-aligned base: barriers and flags, Q (one tile of rows or two), the ring
-    static constexpr int kBars = 2 * kMaxStages + 9;
+    static constexpr int kBars = 2 * kMaxStages + 11;
     static constexpr int kMiscOff = (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, tiles issued, odd drafts
     static constexpr int kQOff = 1024;
     static_assert(kMiscOff + 48 <= kQOff, "barriers");
@@ -82,9 +82,9 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     const Ring ring_v{full + k_stages, empty + k_stages, ring + k_stages * S::kTileBytes, n_stages - k_stages, S::kTileBytes};
     uint64_t* q_full = empty + S::kMaxStages;          // both groups' rows
     uint64_t* s_full = q_full + 1;                     // [2]
-    uint64_t* p_full = s_full + 2;                     // [2]
-    uint64_t* o_full = p_full + 2;                     // [2]
-    uint64_t* drain = o_full + 2;
+    uint64_t* p_full = s_full + 2;                     // [2][2] halves of the keys
+    uint64_t* o_full = p_full + 4;                     // [2]
+    uint64_t* drain = o_full + 2;                      // [2]
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + S::kMiscOff);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 4);
     volatile int* issued_tiles = reinterpret_cast<volatile int*>(sm + S::kMiscOff + 8);  // [2] K, V
@@ -94,15 +94,17 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < n_stages; ++i) {
             mbar_init(&full[i], 1);
-            mbar_init(&empty[i], 1);
+            mbar_init(&empty[i], 2);  // both issuers
         }
         mbar_init(q_full, 8);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s_full[i], 1);
-            mbar_init(&p_full[i], 4);
+            mbar_init(&p_full[2 * i], 4);
+            mbar_init(&p_full[2 * i + 1], 4);
             mbar_init(&o_full[i], 1);
         }
-        mbar_init(drain, 1);
+        mbar_init(&drain[0], 1);
+        mbar_init(&drain[1], 1);
         *abort_flag = 0;
         mbar_fence_init();
     }
@@ -152,89 +154,88 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
         }
         if (lane == 0) issued_tiles[kv] = (int)t;
         __syncwarp();
-    } else if (warp == 1) {
-        // ---------------------------------------------------------- MMA issuer
+    } else if (warp < 4) {
+        // --------------------------------------------------------- MMA issuers
         if (lane == 0) {
             constexpr uint32_t kIdS = idesc_bf16(128, 128);
             constexpr uint32_t kIdO = idesc_bf16(128, D) | (1u << 16);  // B MN-major
-            uint32_t t = 0, seg = 0, p_seen[2] = {0, 0};
+            const int w = warp >> 1;  // the group
+            const uint32_t sp = tmem + w * 128, o = tmem + 256 + w * 128;
+            uint32_t t = 0, seg = 0, p_seen = 0;
             bool ok = true, issued = false;
             auto wait = [&](uint64_t* bar, uint32_t parity) {
                 ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
                 return ok;
             };
-            auto release = [&](uint64_t* freed) {
-                if (ok) mma_commit(freed);
-            };
             while (ok && walk.next(a, sg)) {
                 const int tiles = sg.tile1 - sg.tile0;
                 const bool split = sg.nr <= 128;  // by tiles; else by rows
-                bool live[2] = {false, false};
-                if (!wait(q_full, seg++ & 1)) break;
-                auto product_s = [&](int i, int w) {  // S of the segment's tile i for group w
+                const int first = split ? w : 0, step = split ? 2 : 1;
+                int k_at = 0, v_at = 0;  // tiles that this issuer is done with
+                bool live = false;
+                // a segment without tiles for the group may be over before its Q is seen here
+                if (first < tiles && !wait(q_full, seg & 1)) break;
+                ++seg;
+                auto pass = [&](const Ring& r, int& at, int to) {  // the other group's tiles
+                    for (; ok && at < to; ++at)
+                        if (wait(r.filled(t + at), r.parity(t + at))) mbar_arrive(r.freed(t + at));
+                };
+                auto product_s = [&](int i) {  // S of the segment's tile i
+                    pass(ring_k, k_at, i);
                     if (!wait(ring_k.filled(t + i), ring_k.parity(t + i))) return;
                     tc_fence_after();
                     issued = true;
-                    const uint32_t ka = smem_u32(ring_k.tile(t + i));
-                    const uint32_t qa = smem_u32(sm + S::kQOff) + (split ? 0 : w * S::kTileBytes);
-                    product_k_major<kIdS, D>(tmem + w * 128, qa, kAtom, ka, kAtom);
+                    product_k_major<kIdS, D>(sp, smem_u32(sm + S::kQOff) + (split ? 0 : w * S::kTileBytes), kAtom,
+                                             smem_u32(ring_k.tile(t + i)), kAtom);
                     mma_commit(&s_full[w]);
+                    mma_commit(ring_k.freed(t + i));
+                    k_at = i + 1;
                 };
-                auto product_o = [&](int i, int w) {
-                    if (!wait(ring_v.filled(t + i), ring_v.parity(t + i)) || !wait(&p_full[w], p_seen[w]++ & 1)) return;
+                auto product_o = [&](int i) {
+                    pass(ring_v, v_at, i);
+                    if (!wait(ring_v.filled(t + i), ring_v.parity(t + i)) || !wait(&p_full[2 * w + 1], p_seen & 1)) return;
                     tc_fence_after();
                     issued = true;
-                    const uint32_t va = smem_u32(ring_v.tile(t + i)), p = tmem + w * 128, o = tmem + 256 + w * 128;
                     const int ksteps = (tile_keys(a, sg.s, sg.tile0 + i) + 15) / 16;
-                    const uint64_t vd = mn_desc(va, kAtom);
+                    const uint64_t vd = mn_desc(smem_u32(ring_v.tile(t + i)), kAtom);
                     auto keys16 = [&](int kk, uint32_t acc) {  // 16 keys, 2 KB of V: hi and lo
-                        const uint32_t at = p + (kk >> 1) * 32 + (kk & 1) * 8;
+                        const uint32_t at = sp + (kk >> 1) * 32 + (kk & 1) * 8;
                         mma_ts<kIdO>(o, at, vd + kk * 128, acc);
                         mma_ts<kIdO>(o, at + 16, vd + kk * 128, 1u);
                     };
                     if (ksteps == 8) {
 #pragma unroll
-                        for (int kk = 0; kk < 8; ++kk) keys16(kk, kk > 0 ? 1u : live[w] ? 1u : 0u);
+                        for (int kk = 4; kk < 8; ++kk) keys16(kk, kk > 4 ? 1u : live ? 1u : 0u);
+                        if (!wait(&p_full[2 * w], p_seen++ & 1)) return;
+                        tc_fence_after();
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) keys16(kk, 1u);
                     } else {
-                        for (int kk = 0; kk < ksteps; ++kk) keys16(kk, live[w] || kk > 0 ? 1u : 0u);
+                        if (!wait(&p_full[2 * w], p_seen++ & 1)) return;
+                        tc_fence_after();
+                        for (int kk = 0; kk < ksteps; ++kk) keys16(kk, live || kk > 0 ? 1u : 0u);
                     }
-                    live[w] = live[w] || ksteps > 0;
-                    if (i + (split ? 2 : 1) >= tiles) mma_commit(&o_full[w]);
+                    live = live || ksteps > 0;
+                    if (i + step >= tiles) mma_commit(&o_full[w]);
+                    mma_commit(ring_v.freed(t + i));
+                    v_at = i + 1;
                 };
-                if (split) {
-                    for (int i = 0; ok && i < 2 && i < tiles; ++i) {
-                        product_s(i, i);
-                        release(ring_k.freed(t + i));
-                    }
-                    for (int i = 0; ok && i < tiles; ++i) {
-                        product_o(i, i & 1);
-                        release(ring_v.freed(t + i));
-                        if (ok && i + 2 < tiles) {
-                            product_s(i + 2, i & 1);
-                            release(ring_k.freed(t + i + 2));
-                        }
-                    }
-                } else {
-                    for (int w = 0; ok && w < 2; ++w) product_s(0, w);
-                    release(ring_k.freed(t));
-                    for (int i = 0; ok && i < tiles; ++i) {
-                        for (int w = 0; ok && w < 2; ++w) {
-                            product_o(i, w);
-                            if (w == 1) release(ring_v.freed(t + i));
-                            if (ok && i + 1 < tiles) product_s(i + 1, w);
-                        }
-                        if (i + 1 < tiles) release(ring_k.freed(t + i + 1));
-                    }
+                if (first < tiles) product_s(first);
+                for (int i = first; ok && i < tiles; i += step) {
+                    product_o(i);
+                    if (ok && i + step < tiles) product_s(i + step);
                 }
+                pass(ring_k, k_at, tiles);
+                pass(ring_v, v_at, tiles);
                 t += tiles;
             }
             if (issued) {
-                mma_commit(drain);
-                drain_wait(drain, 0, a.status);
+                mma_commit(&drain[w]);
+                drain_wait(&drain[w], 0, a.status);
             }
         }
         __syncwarp();
-    } else if (warp >= 4) {
+    } else {
         // ------------------------------------------------------------- epilogue
         const int w = (warp - 4) >> 2, q = warp & 3;
         const int j = q * 32 + lane;  // lane of TMEM: row of the group; and V row that it may clear
@@ -362,12 +363,8 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
                         tmem_st32(t_s + half * 64 + x, p);
                     }
                 };
-                exponentials(1);  // still in registers
-                load(0);
-                exponentials(0);
-                l += sum.x + sum.y;
-                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                if ((split || w == 0) && (drafts || (keys & 15))) {
+                const bool unsound = drafts || (keys & 15);
+                if (unsound && (split || w == 0)) {
                     // V rows that must not reach the product: past the keys, and drafts that are not finite
                     const uint32_t tv = t + (tile - sg.tile0);
                     wait(ring_v.filled(tv), ring_v.parity(tv));
@@ -381,9 +378,19 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
                     if (clear) clear_row<D>(vr);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[w]);
+                if (unsound && !split) both_groups_or(false);  // both groups' products read the cleared rows
+                auto half_done = [&](int half) {
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[2 * w + half]);
+                };
+                exponentials(1);  // still in registers
+                half_done(1);
+                load(0);
+                exponentials(0);
+                l += sum.x + sum.y;
+                half_done(0);
                 live = live || keys > 0;
             }
             t += tiles;
