@@ -409,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
                 const int r0 = k * a.RB, nr = min(a.RB, R - r0);
                 const int u = at.unit0 + (g * s.nrb + k) * s.nt + tile;
                 const float4* z = reinterpret_cast<const float4*>(a.score + (int64_t)u * a.RB * kCacheTile) + lane;
-                constexpr int kBatch = 8;  // rows in flight
+                constexpr int kBatch = 4;  // rows in flight; 8 spill, 25 us more over 256 sequences of some 2k
                 for (int q0 = 0; q0 < nr; q0 += kBatch) {
                     float4 x[kBatch];
 #pragma unroll
