@@ -13,6 +13,9 @@
 // rows to a key, keeping scores costs more than forming them again: cache_weight_kernel does, a
 // third launch.  No floating-point atomics: every sum has one order.
 //
+// The finish is bound by latency when there are few rows (4 to 7 us), by its bytes with many sequences: a
+// tile of 4 rows and 128 keys is 2 KB of scores beside 1 KB of weights, read and written.
+//
 // A row that sees nothing (M = -inf, L = 0) gives o = 0 and lse = -inf and no weight.
 #include "cache_tc.cuh"
 

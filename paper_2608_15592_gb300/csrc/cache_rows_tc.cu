@@ -12,15 +12,20 @@
 //
 // One persistent CTA per SM over the units of cache.cuh, two epilogue groups of 128 threads, each with
 // an S/P buffer and an O (all 512 columns).  A block of up to 128 rows is split by tiles: the groups
-// take them in turn, each with a softmax of its own, and are joined at a segment's end.  A block of up to 256 rows is split by rows, 128 a
-// group, and every tile goes to both.  Either way one group's softmax runs under the other's products.
+// take them in turn, each with a softmax of its own, and are joined at a segment's end.  A block of up
+// to 256 rows is split by rows, 128 a group, and every tile goes to both.  Either way one group's
+// softmax runs under the other's products.
 //   warps 0, 2 TMA producers of the K and of the V tiles, a ring each
-//   warp 1     issues the products; the pipe runs them in the order of issue, so the S that overwrites
-//              a P comes after the product that reads it
-//   warp 3     idle
-//   warps 4-11 the epilogue groups, which also load their rows' Q
-// Bound, at 256 rows, by the tensor pipe (24 products of 64 clocks a group and tile, and half as slow
-// again beside the epilogue's own tensor memory traffic); up to 128 nearly by the copies.
+//   warps 1, 3 issue the products of a group each; the pipe runs a warp's in the order of issue, so the
+//              S that overwrites a P comes after the product that reads it.  A tile's slot is free when
+//              both have let go of it.  (One warp for both groups held each back for the other: 178 us
+//              against 152 for 8 sequences of 8k with 9 to 17 drafts, 8 query heads a KV head.)
+//   warps 4-11 the epilogue groups, which also load their rows' Q.  The second half of the keys is
+//              handed on first, so that its product runs under the first half's exponentials (152 to
+//              148 us).  Two warps to a group's 32 rows have 96 registers a thread: 198 us.
+// Bound by the turn of a group: 1.5 us of softmax and 1.6 of products (24 of 64 clocks, the other
+// group's between them) for every tile, 1.55 us a tile with two groups, where the tensor pipe needs 0.85
+// and the copies 1.45.  Another S buffer would part them, but the columns are spent.
 // Keys past a sequence's slots, drafts that are not finite and waits are treated as in
 // cache_attn_tc.cu.
 #include "cache_tc.cuh"

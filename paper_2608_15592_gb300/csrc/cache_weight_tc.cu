@@ -1,8 +1,12 @@
-// The cache attention's weights with the scores formed again (see cache_attn.cu) for bf16 caches: S^T = K Q^T tile by tile with every
-// row of the (b, KV head) resident, w_j = sum_r c_r 2^(S_jr c - M_r) / L_r, a thread a key.  A CTA takes
-// an equal run of the call's (b, KV head, tile), which go to the two epilogue groups in turn, all
-// blocks of 64 rows of a tile to one.  Rows beyond kWRows take another pass over the run,
-// by the same threads.  Bound by K's bytes up to some 170 rows a KV head, then by ex2 (16 a clock).
+// The cache attention's weights with the scores formed again (see cache_attn.cu) for bf16 caches:
+// S^T = K Q^T tile by tile with every row of the (b, KV head) resident, 128 rows a product (64 take the
+// tensor pipe as long), w_j = sum_r c_r 2^(S_jr c - M_r) / L_r, a thread a key.  A CTA takes an equal run
+// of the call's (b, KV head, tile), which go to the two epilogue groups in turn, all rows of a tile to
+// one.  Where 64 rows all count, two at a time in packed FMAs; else each by the mask of rows that see
+// the key and have a factor (a factor of 0 must not meet a score that is not finite).  Rows beyond
+// kWRows take another pass over the run, by the same threads.
+// Bound by K's bytes up to some 170 rows a KV head (8 sequences of 8k: a tile each 0.84 us, 5.9 TB/s), then
+// by ex2 and the issue of the sums.
 #include "cache_tc.cuh"
 
 namespace estp {
