@@ -94,6 +94,10 @@ CASES = [
     ([5000, 4000, 500, 3000], [30, 20, 9, 17], 64, 16, 128, 64),
     ([5000, 4000, 500, 3000], [70, 40, 9, 100], 32, 8, 128, 64),
     ([5000, 4000, 500, 3000], [70, 40, 9, 100], 32, 8, 64, 16),
+    # more sequences than a warp has lanes
+    ([37 * i % 300 for i in range(70)], [1 - (i % 9 == 4) for i in range(70)], 12, 3, 64, 16),
+    ([53 * i % 700 for i in range(40)], [i % 6 for i in range(40)], 12, 3, 128, 32),
+    ([71 * i % 400 for i in range(36)], [i * 5 % 41 for i in range(36)], 8, 2, 128, 64),
 ]
 
 
