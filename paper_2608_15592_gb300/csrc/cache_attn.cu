@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kThreads = 128;  // one key of a tile each
 constexpr int kRows = 8;       // rows of a block of the CUDA-core kernels
+constexpr int kBlocks = 3;     // of those an SM: 168 registers a thread (4 blocks: 79 us where 3 take 66, as below)
 constexpr int kCacheMaxStored = 64;  // rows of a (b, KV head) whose scores are kept at most
 
 template <class T> struct Unit;  // 16 bytes of a row
@@ -37,7 +38,6 @@ template <> struct Unit<float> {
     static __device__ __forceinline__ void put(char* p, float v) { *reinterpret_cast<float*>(p) = v; }
 };
 template <> struct Unit<__nv_bfloat16> {
-    static constexpr int n = 8;
     static __device__ __forceinline__ void get(const char* p, float* v) {
         const uint4 x = *reinterpret_cast<const uint4*>(p);
         v[0] = bf16lo(x.x); v[1] = bf16hi(x.x); v[2] = bf16lo(x.y); v[3] = bf16hi(x.y);
@@ -97,26 +97,66 @@ __device__ __forceinline__ void load_q(const CacheAttnArgs& a, float (*q)[D], in
     }
 }
 
-template <class T, int D>
-__device__ __forceinline__ void dots(const float (*q)[D], const char* k, float* z) {
+// z[r] = q_r . k, k the calling thread's key row (NULL: 0), by a whole warp for its 32 keys: 8 lanes read
+// a row together, 128 bytes at a time (a lane a row touches as many cache lines as lanes an instruction:
+// 103 us for 5 drafts and 8 query heads a KV head over 20000 fp32 tokens of 2 x 128, 66 so), and 4 keys a
+// lane share each read of q.  zs: the warp's 32 rows of scratch.
+template <int D>
+__device__ __forceinline__ void dots(const float (*q)[D], const char* k, float (*zs)[kRows], float* z) {
+    static_assert(kRows == 8, "8 lanes a key, a row each at the end");
+    constexpr int kPer = 4;
+    const int lane = threadIdx.x & 31, sub = lane & 7, grp = lane >> 3;
+#pragma unroll 1
+    for (int k0 = 0; k0 < 32; k0 += 4 * kPer) {
+        const char* kp[kPer];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) z[r] = 0.f;
-#pragma unroll 8
-    for (int c = 0; c < D / Unit<T>::n; ++c) {
-        float kv[Unit<T>::n];
-        Unit<T>::get(k + c * 16, kv);
+        for (int i = 0; i < kPer; ++i)
+            kp[i] = reinterpret_cast<const char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k), k0 + 4 * i + grp));
+        float2 acc[kPer][kRows] = {};  // even and odd dimensions: packed FMAs
 #pragma unroll
-        for (int r = 0; r < kRows; ++r)
+        for (int c = 0; c < D / 32; ++c) {
+            float4 kv[kPer];
 #pragma unroll
-            for (int i = 0; i < Unit<T>::n; ++i) z[r] = fmaf(q[r][c * Unit<T>::n + i], kv[i], z[r]);
+            for (int i = 0; i < kPer; ++i)
+                kv[i] = kp[i] != nullptr ? *reinterpret_cast<const float4*>(kp[i] + (c * 8 + sub) * 16) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const float4 x = *reinterpret_cast<const float4*>(&q[r][(c * 8 + sub) * 4]);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    acc[i][r] = __ffma2_rn(make_float2(x.x, x.y), make_float2(kv[i].x, kv[i].y), acc[i][r]);
+                    acc[i][r] = __ffma2_rn(make_float2(x.z, x.w), make_float2(kv[i].z, kv[i].w), acc[i][r]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {  // over the 8 lanes: each step halves the rows a lane still holds
+            float v[kRows];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) v[r] = acc[i][r].x + acc[i][r].y;
+#pragma unroll
+            for (int o = kRows / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int r = 0; r < o; ++r) {
+                    const bool up = sub & o;
+                    v[r] = (up ? v[r + o] : v[r]) + __shfl_xor_sync(0xffffffffu, up ? v[r] : v[r + o], o);
+                }
+            zs[k0 + 4 * i + grp][sub] = v[0];
+        }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < kRows; r += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(&zs[lane][r]);
+        z[r] = x.x; z[r + 1] = x.y; z[r + 2] = x.z; z[r + 3] = x.w;
     }
 }
 
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs a) {
+__global__ void __launch_bounds__(kThreads, kBlocks) cache_fwd_kernel(const CacheAttnArgs a) {
     __shared__ PlanScratch sc;
-    __shared__ float q[kRows][D];
-    __shared__ float p[kRows][kCacheTile];
+    __shared__ __align__(16) float q[kRows][D];
+    __shared__ __align__(16) float p[kCacheTile][kRows];
     __shared__ const char* vrow[kCacheTile];
     __shared__ float red[kThreads / 32][kRows];
     __shared__ float o_half[kRows][D];
@@ -146,19 +186,19 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
         const int64_t row0 = a.cu[at.b];
         __syncthreads();
         load_q<T, D>(a, q, at.b, g, r0, nr);
-        float m[kRows], l[kRows], o[kRows];
+        float m[kRows], l[kRows];
+        float2 o[kRows / 2] = {};  // two rows each
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             m[r] = -INFINITY;
             l[r] = 0.f;
-            o[r] = 0.f;
         }
         for (int tile = tile0; tile < tile1; ++tile, ++u) {
             const bool drafts = tile == s.nt - 1;
             const KeyRow kr = key_row(a, s, at.b, g, tile, t, D * (int)sizeof(T));
             __syncthreads();  // p and vrow are free, q is there
             float z[kRows];
-            if (kr.k != nullptr) dots<T, D>(q, kr.k, z);
+            dots<D>(q, kr.k, p + warp * 32, z);  // p is free: every thread overwrites its own row
             vrow[t] = kr.v;
             unsigned hidden = 0;  // rows that do not see this key
             if (drafts) {
@@ -178,6 +218,7 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
                 if (lane == 0) red[warp][r] = x;
             }
             __syncthreads();
+            float pr[kRows];
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
                 const float top = fmaxf(fmaxf(red[0][r], red[1][r]), fmaxf(red[2][r], red[3][r])) * a.scale_log2;
@@ -186,9 +227,11 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
                 m[r] = mn;
                 const float e = ex2(fmaf(z[r], a.scale_log2, mn == -INFINITY ? 0.f : -mn));
                 l[r] = fmaf(l[r], f, hidden >> r & 1 ? 0.f : e);
-                o[r] *= f;
-                p[r][t] = hidden >> r & 1 ? (drafts ? -1.f : 0.f) : e;  // -1: no probability, the draft is left out
+                (r & 1 ? o[r / 2].y : o[r / 2].x) *= f;
+                pr[r] = hidden >> r & 1 ? (drafts ? -1.f : 0.f) : e;  // -1: no probability, the draft is left out
             }
+#pragma unroll
+            for (int r = 0; r < kRows; r += 4) *reinterpret_cast<float4*>(&p[t][r]) = make_float4(pr[r], pr[r + 1], pr[r + 2], pr[r + 3]);
             __syncthreads();
             constexpr int kBatch = 16;  // V rows in flight
             for (int j0 = half * kKeys; j0 < (half + 1) * kKeys; j0 += kBatch) {
@@ -202,14 +245,20 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
 #pragma unroll
                     for (int k = 0; k < kBatch; ++k)
 #pragma unroll
-                        for (int r = 0; r < kRows; ++r) o[r] = fmaf(p[r][j0 + k], v[k], o[r]);
+                        for (int r = 0; r < kRows; r += 4) {
+                            const float4 e = *reinterpret_cast<const float4*>(&p[j0 + k][r]);
+                            const float2 v2 = make_float2(v[k], v[k]);
+                            o[r / 2] = __ffma2_rn(make_float2(e.x, e.y), v2, o[r / 2]);
+                            o[r / 2 + 1] = __ffma2_rn(make_float2(e.z, e.w), v2, o[r / 2 + 1]);
+                        }
                 } else {  // what a hidden draft's V holds adds nothing, 0 x NaN included
 #pragma unroll
                     for (int k = 0; k < kBatch; ++k)
 #pragma unroll
                         for (int r = 0; r < kRows; ++r) {
-                            const float e = p[r][j0 + k];
-                            if (!(e < 0.f)) o[r] = fmaf(e, v[k], o[r]);
+                            const float e = p[j0 + k][r];
+                            float& x = r & 1 ? o[r / 2].y : o[r / 2].x;
+                            if (!(e < 0.f)) x = fmaf(e, v[k], x);
                         }
                 }
             }
@@ -221,7 +270,7 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
             float x = l[r];
             for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
             if (lane == 0) red[warp][r] = x;
-            if (half == 1) o_half[r][col] = o[r];
+            if (half == 1) o_half[r][col] = r & 1 ? o[r / 2].y : o[r / 2].x;
         }
         __syncthreads();
 #pragma unroll
@@ -229,7 +278,8 @@ __global__ void __launch_bounds__(kThreads) cache_fwd_kernel(const CacheAttnArgs
             if (r >= nr) break;
             if (t == 0)
                 a.part_ml[slot * kRows + r] = make_float2(m[r], (red[0][r] + red[1][r]) + (red[2][r] + red[3][r]));
-            if (half == 0) a.part_o[(slot * kRows + r) * D + col] = kHalves == 2 ? o[r] + o_half[r][col] : o[r];
+            const float x = r & 1 ? o[r / 2].y : o[r / 2].x;
+            if (half == 0) a.part_o[(slot * kRows + r) * D + col] = kHalves == 2 ? x + o_half[r][col] : x;
         }
     }
     admit_next();
@@ -448,9 +498,10 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
 
 // The weights with the scores formed again, fp32: a thread a key, the rows in blocks of kRows.
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnArgs a) {
+__global__ void __launch_bounds__(kThreads, kBlocks) cache_weight_kernel(const CacheAttnArgs a) {
     __shared__ PlanScratch sc;
-    __shared__ float q[kRows][D];
+    __shared__ __align__(16) float q[kRows][D];
+    __shared__ __align__(16) float zs[kThreads][kRows];
     __shared__ float2 ml[kRows];
     const int t = threadIdx.x;
     const int c = blockIdx.x, G = gridDim.x;
@@ -477,9 +528,9 @@ __global__ void __launch_bounds__(kThreads) cache_weight_kernel(const CacheAttnA
                 load_q<T, D>(a, q, at.b, g, r0, nr);
                 if (t < nr) ml[t] = a.factor[(row0 + (r0 + t) / a.rep) * a.Hq + g * a.rep + (r0 + t) % a.rep];
                 __syncthreads();
-                if (kr.k == nullptr) continue;
                 float z[kRows];
-                dots<T, D>(q, kr.k, z);
+                dots<D>(q, kr.k, zs + (t & ~31), z);
+                if (kr.k == nullptr) continue;
                 const uint64_t seen = drafts ? rows_that_see(a, row0, s.n, t, r0, nr) : ~0ull;
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
@@ -504,7 +555,7 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
         a.RB = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
     }
     a.whole = kTc;
-    a.G = kTc ? ctx->num_sms : ctx->num_sms * 8;
+    a.G = ctx->num_sms * (kTc ? 1 : kBlocks);
     const int64_t groups = (int64_t)a.c.Hkv * (a.n_rows * a.rep / a.RB + a.B);
     const int64_t slots = a.G + groups;
     // scores of every unit: at most n_slots / 128 + 2 B tiles a KV head, times the row blocks of the
@@ -554,7 +605,7 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     if constexpr (kTc) {
         return launch_cache_weight_tc(ctx, a, st);
     } else {
-        e = launch_dependent(cache_weight_kernel<T, D>, ctx->num_sms * 8, kThreads, 0, st, a);
+        e = launch_dependent(cache_weight_kernel<T, D>, ctx->num_sms * kBlocks, kThreads, 0, st, a);
         return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cache weight launch");
     }
 }
