@@ -553,6 +553,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                 tie<kMine>(hb);
                 tie<kMine>(lb);
                 if (D == 128 || q < 2) {
+                    int i = (sg.r0 + r) / a.rep, h = sg.g * a.rep + (sg.r0 + r) % a.rep;  // draft and head of the row
 #pragma unroll
                     for (int k = 0; k < kMine; ++k) {
                         if (r + k >= nr) break;
@@ -560,11 +561,11 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                         float o = wa != 0.f ? (hi[k] + lo[k]) * wa : 0.f;
                         if (wb != 0.f) o = fmaf(hb[k] + lb[k], wb, o);
                         if (whole) {
-                            const int rr = sg.r0 + r + k, h = sg.g * a.rep + rr % a.rep;
-                            reinterpret_cast<__nv_bfloat16*>(a.out)[((row0 + rr / a.rep) * a.Hq + h) * D + j] = __float2bfloat16_rn(o);
+                            reinterpret_cast<__nv_bfloat16*>(a.out)[((row0 + i) * a.Hq + h) * D + j] = __float2bfloat16_rn(o);
                         } else {
                             a.part_o[(part + r + k) * D + j] = o;
                         }
+                        if (++h == (sg.g + 1) * a.rep) ++i, h -= a.rep;
                     }
                 }
             }

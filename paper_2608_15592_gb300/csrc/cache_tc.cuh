@@ -229,7 +229,7 @@ __device__ __forceinline__ void load_tile(const CacheAttnArgs& a, const CUtensor
 template <int D>
 __device__ __forceinline__ bool row_not_finite(const uint8_t* row) {
     bool odd = false;
-#pragma unroll
+#pragma unroll 2
     for (int x = 0; x < D / 8; ++x) {
         const uint4 v = *reinterpret_cast<const uint4*>(row + (x >> 3) * kAtom + (x & 7) * 16);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -240,7 +240,7 @@ __device__ __forceinline__ bool row_not_finite(const uint8_t* row) {
 }
 template <int D>
 __device__ __forceinline__ void clear_row(uint8_t* row) {
-#pragma unroll
+#pragma unroll 1
     for (int x = 0; x < D / 8; ++x) *reinterpret_cast<uint4*>(row + (x >> 3) * kAtom + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
 }
 
