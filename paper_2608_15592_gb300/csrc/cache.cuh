@@ -94,14 +94,17 @@ __device__ __forceinline__ bool seq_ok(const CacheAttnArgs& a, int b) {
     return len >= 0 && len <= a.c.capacity() && lo >= 0 && hi >= lo && hi - lo <= a.max_rows && hi <= a.n_rows &&
            (b > 0 || lo == 0) && (b + 1 < a.B || hi == a.n_rows);
 }
+// kRB: the rows of a block where the kernel knows them (0: a.RB), which leaves little of the divisions
+template <int kRB = 0>
 __device__ __forceinline__ SeqShape seq_shape(const CacheAttnArgs& a, int b) {
+    const int RB = kRB != 0 ? kRB : a.RB;
     SeqShape s;
     s.len = a.length[b];
     s.n = a.cu[b + 1] - a.cu[b];
-    s.nrb = (s.n * a.rep + a.RB - 1) / a.RB;
+    s.nrb = (s.n * a.rep + RB - 1) / RB;
     s.nt = (s.len + kCacheTile - 1) / kCacheTile + 1;
-    s.last = s.n * a.rep - (s.nrb - 1) * a.RB > 128 ? 2 : 1;
-    s.cost = s.nrb > 0 ? (s.nrb - 1) * (a.RB > 128 ? 2 : 1) + s.last : 0;
+    s.last = s.n * a.rep - (s.nrb - 1) * RB > 128 ? 2 : 1;
+    s.cost = RB <= 128 ? s.nrb : s.nrb > 0 ? (s.nrb - 1) * 2 + s.last : 0;
     return s;
 }
 
@@ -244,9 +247,10 @@ __device__ __forceinline__ int ctas_of(const CacheAttnArgs& a, int total) {
 struct Span {
     int g, k, tile0, tile1, units;
 };
+template <int kRB = 0>
 __device__ __forceinline__ Span span_of(const CacheAttnArgs& a, const SeqShape& s, int loc, int count) {
     Span x;
-    if (a.RB <= 128) {  // a unit a tile
+    if ((kRB != 0 ? kRB : a.RB) <= 128) {  // a unit a tile
         const int grp = loc / s.nt;
         x.tile0 = loc - grp * s.nt;
         x.tile1 = min(s.nt, x.tile0 + count);
@@ -277,6 +281,10 @@ __device__ __forceinline__ float2 weight_factor(const CacheAttnArgs& a, float2 x
 // n drafts (from row0): bit r for row first + r, which is draft (first + r) / rep.
 __device__ __forceinline__ uint64_t rows_that_see(const CacheAttnArgs& a, int64_t row0, int n, int j, int first, int nr) {
     if (j >= n || nr <= 0) return 0;
+    if (a.tree == nullptr) {  // those from draft j's own on
+        const int lo = max(j * a.rep - first, 0);
+        return lo < nr ? ~0ull >> (64 - nr) & ~0ull << lo : 0;
+    }
     const int i0 = first / a.rep, i1 = (first + nr - 1) / a.rep;
     const uint64_t* p = a.tree + row0 * a.words + (j >> 6);
     uint64_t rows = 0;
@@ -284,7 +292,7 @@ __device__ __forceinline__ uint64_t rows_that_see(const CacheAttnArgs& a, int64_
         bool sees[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k)  // loads in flight together
-            sees[k] = i + k <= i1 && (a.tree == nullptr ? j <= i + k : p[(int64_t)(i + k) * a.words] >> (j & 63) & 1);
+            sees[k] = i + k <= i1 && (p[(int64_t)(i + k) * a.words] >> (j & 63) & 1);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int lo = max((i + k) * a.rep - first, 0), hi = min((i + k + 1) * a.rep - first, nr);

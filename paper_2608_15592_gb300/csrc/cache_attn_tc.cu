@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
         Segment qs;
         // Q of the next segment (zeros past its rows), K-major with the 128-byte swizzle
         auto load_q = [&]() {
-            if (!q_walk.next(a, qs)) return;
+            if (!q_walk.next<RB>(a, qs)) return;
             const uint32_t qb = q_seg % S::kQBufs, use = q_seg / S::kQBufs;
             if (use >= 1 && !warp_wait(&q_empty[qb], (use - 1) & 1, abort_flag, a.status, a.wait_cycles)) {
                 ok = false;
@@ -189,11 +189,14 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
             ++q_seg;
             const int64_t row0 = a.cu[qs.b];
             const uint32_t to = smem_u32(sm + S::kQOff + qb * S::kQBytes);
-#pragma unroll 4
-            for (int x = lane; x < S::kN * (D / 8); x += 32) {
-                const int r = x / (D / 8), ch = x % (D / 8);
-                const int rr = r < qs.nr ? qs.r0 + r : qs.r0, i = rr / a.rep, h = qs.g * a.rep + rr % a.rep;
-                const char* from = a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16;
+            constexpr int kTogether = 32 / (D / 8);  // rows at a time
+            const int ch = lane % (D / 8);
+            int i = (qs.r0 + lane / (D / 8)) / a.rep, h = (qs.r0 + lane / (D / 8)) % a.rep;
+#pragma unroll 1
+            for (int r = lane / (D / 8); r < S::kN; r += kTogether) {
+                const char* from = a.Q + ch * 16;
+                if (r < qs.nr) from += (row0 + i) * a.ldq + (int64_t)(qs.g * a.rep + h) * (D * 2);
+                for (h += kTogether; h >= a.rep; h -= a.rep) ++i;
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
                                  to + (ch >> 3) * S::kN * 128 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
                              "l"(from), "r"(r < qs.nr ? 16 : 0)
@@ -206,7 +209,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
         };
         if (kv) load_q();
         PageWindow win;
-        while (ok && walk.next(a, sg)) {
+        while (ok && walk.next<RB>(a, sg)) {
             win.open(a, sg.s, sg.b, sg.tile0, lane);
             for (int tile = sg.tile0; tile < sg.tile1; ++tile, ++t) {
                 if (t >= (uint32_t)ring.n && !warp_wait(ring.freed(t), ring.parity(t - ring.n), abort_flag, a.status, a.wait_cycles)) {
@@ -231,7 +234,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                 ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
                 return ok;
             };
-            while (ok && walk.next(a, sg)) {
+            while (ok && walk.next<RB>(a, sg)) {
                 const int tiles = sg.tile1 - sg.tile0;
                 const uint32_t qb = seg % S::kQBufs;
                 if (!wait(&q_full[qb], (seg / S::kQBufs) & 1)) break;
@@ -271,7 +274,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                 ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
                 return ok;
             };
-            while (ok && walk.next(a, sg)) {
+            while (ok && walk.next<RB>(a, sg)) {
                 const int tiles = sg.tile1 - sg.tile0;
                 bool live[NB] = {};  // a group's O holds a product of this segment
                 for (int i = 0; ok && i < tiles; ++i, ++t) {
@@ -323,7 +326,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
         auto wait = [&](uint64_t* b, uint32_t parity) {
             if (alive) alive = warp_wait(b, parity, abort_flag, a.status, a.wait_cycles);
         };
-        while (walk.next(a, sg)) {
+        while (walk.next<RB>(a, sg)) {
             const int nr = sg.nr;
             const int64_t row0 = a.cu[sg.b];
             if (j < RB) row_m[j] = -INFINITY;

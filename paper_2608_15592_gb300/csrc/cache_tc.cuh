@@ -135,14 +135,15 @@ struct Segment {
 struct Walk {
     Place at;
     int u, u1;
+    template <int kRB = 0>
     __device__ __forceinline__ bool next(const CacheAttnArgs& a, Segment& o) {
         while (u < u1) {
-            o.s = seq_shape(a, at.b);
+            o.s = seq_shape<kRB>(a, at.b);
             if (u >= at.unit0 + o.s.units(a.c.Hkv)) {
                 at.pass(o.s, a.c.Hkv);
                 continue;
             }
-            const Span x = span_of(a, o.s, u - at.unit0, u1 - u);
+            const Span x = span_of<kRB>(a, o.s, u - at.unit0, u1 - u);
             u += x.units;
             if (x.tile0 >= x.tile1) continue;
             o.tile0 = x.tile0;
