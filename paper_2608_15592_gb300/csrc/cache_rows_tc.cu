@@ -259,12 +259,15 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
             const int64_t row0 = a.cu[sg.b];
             {  // Q (zeros past the rows), K-major with the 128-byte swizzle
                 const uint32_t to = smem_u32(sm + S::kQOff);
-#pragma unroll 4
-                for (int x = w * 128 + j; x < (split ? 128 : 256) * (D / 8); x += 256) {
-                    const int r = x / (D / 8), ch = x % (D / 8);
+                constexpr int kTogether = 256 / (D / 8);  // rows at a time
+                const int x = w * 128 + j, ch = x % (D / 8);
+                int i = (sg.r0 + x / (D / 8)) / a.rep, h = (sg.r0 + x / (D / 8)) % a.rep;
+#pragma unroll 2
+                for (int r = x / (D / 8); r < (split ? 128 : 256); r += kTogether) {
                     const bool there = r < sg.nr;
-                    const int rq = sg.r0 + (there ? r : 0), i = rq / a.rep, h = sg.g * a.rep + rq % a.rep;
-                    const char* from = a.Q + (row0 + i) * a.ldq + (int64_t)h * (D * 2) + ch * 16;
+                    const char* from = a.Q + ch * 16;
+                    if (there) from += (row0 + i) * a.ldq + (int64_t)(sg.g * a.rep + h) * (D * 2);
+                    for (h += kTogether; h >= a.rep; h -= a.rep) ++i;
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
                                      to + (r >> 7) * S::kTileBytes + (ch >> 3) * kAtom + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4)),
                                  "l"(from), "r"(there ? 16 : 0)
