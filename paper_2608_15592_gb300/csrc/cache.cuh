@@ -288,13 +288,13 @@ __device__ __forceinline__ uint64_t rows_that_see(const CacheAttnArgs& a, int64_
     const int i0 = first / a.rep, i1 = (first + nr - 1) / a.rep;
     const uint64_t* p = a.tree + row0 * a.words + (j >> 6);
     uint64_t rows = 0;
-    for (int i = i0; i <= i1; i += 8) {
-        bool sees[8];
+    for (int i = i0; i <= i1; i += 4) {
+        bool sees[4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)  // loads in flight together
+        for (int k = 0; k < 4; ++k)  // loads in flight together
             sees[k] = i + k <= i1 && (p[(int64_t)(i + k) * a.words] >> (j & 63) & 1);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 4; ++k) {
             const int lo = max((i + k) * a.rep - first, 0), hi = min((i + k + 1) * a.rep - first, nr);
             if (sees[k]) rows |= ~0ull >> (64 - (hi - lo)) << lo;
         }

@@ -476,6 +476,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
 #pragma unroll 1
                 for (int r = 0; r < nr; ++r) {
                     float s = 0.f;
+#pragma unroll 1
                     for (int x = 0; x < sg.s.n; ++x) {
                         if ((D == 64 && q >= 2) || !(odd_drafts[x >> 5] >> (x & 31) & 1)) continue;
                         if (!(rows_that_see(a, row0, sg.s.n, x, sg.r0 + r, 1) & 1)) continue;
