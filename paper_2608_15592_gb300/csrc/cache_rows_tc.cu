@@ -40,7 +40,7 @@ struct RowShape {
     static constexpr int kMaxStages = 12;
     static constexpr int kThreads = 384;
     // from a 1024-aligned base: barriers and flags, Q (one tile of rows or two), the ring
-    static constexpr int kBars = 2 * kMaxStages + 11;
+    static constexpr int kBars = 2 * kMaxStages + 12;
     static constexpr int kMiscOff = (kBars * 8 + 15) / 16 * 16;  // tmem address, abort flag, tiles issued, odd drafts
     static constexpr int kQOff = 1024;
     static_assert(kMiscOff + 48 <= kQOff, "barriers");
@@ -85,8 +85,8 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     const int k_stages = n_stages / 2;                 // V tiles wait longer in their slots
     const Ring ring_k{full, empty, ring, k_stages, S::kTileBytes};
     const Ring ring_v{full + k_stages, empty + k_stages, ring + k_stages * S::kTileBytes, n_stages - k_stages, S::kTileBytes};
-    uint64_t* q_full = empty + S::kMaxStages;          // both groups' rows
-    uint64_t* s_full = q_full + 1;                     // [2]
+    uint64_t* q_full = empty + S::kMaxStages;          // [2] a group's rows, a phase a segment that has a tile for it
+    uint64_t* s_full = q_full + 2;                     // [2]
     uint64_t* p_full = s_full + 2;                     // [2][2] halves of the keys
     uint64_t* o_full = p_full + 4;                     // [2]
     uint64_t* drain = o_full + 2;                      // [2]
@@ -101,8 +101,8 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 2);  // both issuers
         }
-        mbar_init(q_full, 8);
         for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 8);  // the epilogue warps
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[2 * i], 4);
             mbar_init(&p_full[2 * i + 1], 4);
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
             constexpr uint32_t kIdO = idesc_bf16(128, D) | (1u << 16);  // B MN-major
             const int w = warp >> 1;  // the group
             const uint32_t sp = tmem + w * 128, o = tmem + 256 + w * 128;
-            uint32_t t = 0, seg = 0, p_seen = 0;
+            uint32_t t = 0, q_seen = 0, p_seen = 0;
             bool ok = true, issued = false;
             auto wait = [&](uint64_t* bar, uint32_t parity) {
                 ok = ok && wait_bar(bar, parity, abort_flag, a.status, a.wait_cycles);
@@ -178,9 +178,9 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
                 const int first = split ? w : 0, step = split ? 2 : 1;
                 int k_at = 0, v_at = 0;  // tiles that this issuer is done with
                 bool live = false;
-                // a segment without tiles for the group may be over before its Q is seen here
-                if (first < tiles && !wait(q_full, seg & 1)) break;
-                ++seg;
+                // Q is awaited where the group has a tile, and only there is its barrier arrived at: a phase that this
+                // warp let pass would leave it a parity behind, on which the next wait is over before Q is there
+                if (first < tiles && !wait(&q_full[w], q_seen++ & 1)) break;
                 auto pass = [&](const Ring& r, int& at, int to) {  // the other group's tiles
                     for (; ok && at < to; ++at)
                         if (wait(r.filled(t + at), r.parity(t + at))) mbar_arrive(r.freed(t + at));
@@ -276,7 +276,10 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(q_full);
+                if (lane == 0) {
+                    mbar_arrive(&q_full[0]);
+                    if (!split || tiles > 1) mbar_arrive(&q_full[1]);
+                }
             }
             const int rr = sg.r0 + base + j;  // this thread's row of the (b, KV head)
             const bool mine = base + j < sg.nr;
