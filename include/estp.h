@@ -430,6 +430,11 @@ estp_status estp_cache_append(estp_ctx* ctx, const estp_kv_cache* cache, const i
  *   lse_out        : fp32 [Hq, n_rows], or NULL
  *   weight_new_out : fp32 [n_rows, Hkv], what the rows' own keys received, or NULL
  * fp32 accumulation.
+ * If one of the call's waits runs out (ESTP_ERR_TIMEOUT), out, lse_out and weight_new_out are undefined and
+ * the cache's weights are left alone, by this call and by the context's later ones, until estp_sync_status
+ * has returned the error: the step can be made again.  (Where the wait is one of the last launch, which only
+ * adds weights, a slot has either its old weight or what it should have got, or that of some of the rows
+ * where a KV head has more than 448.)
  * Repeated calls give identical outputs; the sums have one order for given lengths. */
 estp_status estp_cache_attention(estp_ctx* ctx, const estp_kv_cache* cache, const int32_t* length, int32_t B,
                                  int64_t max_slots, const void* Q, int64_t ldq, int32_t Hq, const void* k_new,

@@ -113,11 +113,12 @@ estp_status estp_create(estp_ctx** out, int device) {
     if (st != ESTP_OK) { delete ctx; return st; }
     e = cudaDeviceGetAttribute(&ctx->num_sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) { delete ctx; return cuda_fail(e, "cudaDeviceGetAttribute"); }
-    // the status word and, on the next 128-byte line, the cache kernels' arrival counter
+    // the status word and, on the next 128-byte line, the cache kernels' arrival counter and timeout mark
     e = cudaMalloc(&ctx->status, 256);
     if (e == cudaSuccess) e = cudaMemset(ctx->status, 0, 256);
     if (e != cudaSuccess) { cudaFree(ctx->status); delete ctx; return cuda_fail(e, "status word"); }
     ctx->done = reinterpret_cast<uint32_t*>(ctx->status) + 32;
+    ctx->timed_out = ctx->status + 48;
     *out = ctx;
     return ESTP_OK;
 }
@@ -152,6 +153,7 @@ estp_status estp_sync_status(estp_ctx* ctx, estp_stream_t stream) {
     int code = 0;
     e = cudaMemcpyAsync(&code, ctx->status, sizeof(int), cudaMemcpyDeviceToHost, s);
     if (e == cudaSuccess) e = cudaMemsetAsync(ctx->status, 0, sizeof(int), s);
+    if (e == cudaSuccess) e = cudaMemsetAsync(ctx->timed_out, 0, sizeof(int), s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     if (e != cudaSuccess) return cuda_fail(e, "reading the status word");
     switch (code) {
@@ -577,6 +579,7 @@ estp_status estp_cache_attention(estp_ctx* ctx, const estp_kv_cache* cache, cons
     a.w_new = weight_new_out;
     a.accumulate = accumulate != 0;
     a.status = ctx->status;
+    a.timed_out = ctx->timed_out;
     a.wait_cycles = ctx->wait_cycles;
     return launch_cache_attention(ctx, a, cache->dtype, reinterpret_cast<cudaStream_t>(stream));
 }

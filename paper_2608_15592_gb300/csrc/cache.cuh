@@ -77,6 +77,7 @@ struct CacheAttnArgs {
     float* w_new;
     int accumulate;
     int* status;
+    volatile int* timed_out;     // a kernel of the attention gave up: the weights stay as they are
     long long wait_cycles;
 };
 

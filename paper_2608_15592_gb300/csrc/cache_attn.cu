@@ -17,6 +17,9 @@
 // tile of 4 rows and 128 keys is 2 KB of scores beside 1 KB of weights, read and written.
 //
 // A row that sees nothing (M = -inf, L = 0) gives o = 0 and lse = -inf and no weight.
+//
+// Weights cannot be formed a second time: after a wait that ran out nothing is added to them, by this call
+// or a later one, until the program has read the status.
 #include "cache_tc.cuh"
 
 namespace estp {
@@ -353,6 +356,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
         return for_rows ? x0 >= y && x0 < y + s.n * a.Hq : it >= x.item0 && it < x.item0 + s.items(a.c.Hkv);
     });
     await_stream();  // the partials are complete
+    const bool lost = *a.timed_out != 0;  // or a wait ran out, and nothing is added from what they happen to hold
     if (!tot.ok) return;
     if (for_rows) {
         if (x0 >= x1) return;
@@ -410,6 +414,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
         }
         return;
     }
+    if (lost) return;
     // every warp for itself: an equal part of the block's items
     const int it0 = share_begin(c, tot.items, G), part = share_begin(c + 1, tot.items, G) - it0;
     float2* f = ml[warp];
@@ -512,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) cache_weight_kernel(const C
     });
     await_stream();  // the factors are complete
     admit_next();
-    if (!tot.ok) return;
+    if (!tot.ok || *a.timed_out != 0) return;
     for_items(a, at, share_begin(c, tot.items, G), share_begin(c + 1, tot.items, G),
               [&](const Place& at, const SeqShape& s, int g, int tile0, int tile1) {
         const int64_t row0 = a.cu[at.b];

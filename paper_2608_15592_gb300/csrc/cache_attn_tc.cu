@@ -586,6 +586,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
     tc_fence_after();
     admit_next();  // (earlier, the next kernel's waiting blocks cost this one 3 %)
     if (threadIdx.x == 0 && *abort_flag) {
+        *a.timed_out = 1;  // the partials and scores are not all there
         ring_k.drain(issued_tiles[0], a.status);
         ring_v.drain(issued_tiles[1], a.status);
     }

@@ -507,6 +507,7 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
     tc_fence_after();
     admit_next();
     if (threadIdx.x == 0 && *abort_flag) {
+        *a.timed_out = 1;  // the partials and scores are not all there
         ring_k.drain(issued_tiles[0], a.status);
         ring_v.drain(issued_tiles[1], a.status);
     }

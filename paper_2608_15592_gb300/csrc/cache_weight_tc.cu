@@ -197,6 +197,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
         const uint32_t q_atom = q_blocks * kWBlock * 128;  // Q: [D / 64][rows] of 128 bytes
         uint32_t step = 0;
         bool alive = true;
+        const bool lost = *a.timed_out != 0;  // the factors are not all there: no weight is written
         while (alive && w.next(a)) {
             const int R = w.s.n * a.rep;
             const int64_t row0 = a.cu[w.b];
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                             }
                         }
                     }
-                    if (to != nullptr) *to = had + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
+                    if (to != nullptr && alive && !lost) *to = had + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
                 }
                 if (both_groups_or(!alive)) alive = false;  // Q and the factors are free
             }
@@ -298,6 +299,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (threadIdx.x == 0 && *abort_flag) *a.timed_out = 1;
     if (warp == 1) {
         __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kWBufs * kWCols));

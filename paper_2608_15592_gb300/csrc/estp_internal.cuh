@@ -16,6 +16,7 @@ struct estp_ctx {
     int device = 0;
     int num_sms = 0;
     int* status = nullptr;      // device status word (estp_status codes)
+    int* timed_out = nullptr;   // set where a wait of the cache attention ran out, until the status is read
     uint32_t* done = nullptr;   // arrival counter of the cache kernels' blocks (zero between launches)
     void* ws = nullptr;         // growable scratch for one call's intermediates
     size_t ws_bytes = 0;
