@@ -194,30 +194,55 @@ class KVCache:
     weight     fp32 [n_pages, Hkv, page_size], position: int32 of that shape, or None
     max_slots  a bound of the slots in use over all sequences (default: what the page table can
                hold; with weights, which need every page in one sequence only, at most the pool's)
+
+    Each is an attribute that may be replaced (a longer page table, a larger pool); the call after
+    that looks all of them over again, together.
     """
 
+    _TENSORS = frozenset(("k", "v", "page_table", "length", "seen", "weight", "position"))
+
     def __init__(self, k, v, page_table, length, seen, weight=None, position=None, max_slots=None):
+        self.k, self.v, self.page_table, self.length, self.seen = k, v, page_table, length, seen
+        self.weight, self.position = weight, position
+        self.max_slots = max_slots
+        self._struct()
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name in self._TENSORS:
+            object.__setattr__(self, "_ref", None)
+
+    @property
+    def max_slots(self) -> int:
+        self._struct()
+        return self._bound if self._slots is None else self._slots
+
+    @max_slots.setter
+    def max_slots(self, value):
+        self._slots = None if value is None else int(value)
+
+    def _struct(self):
+        """Address of the estp_kv_cache, formed anew where a tensor was replaced."""
+        if self._ref is not None:
+            return self._ref
         import torch
+        k, v, page_table, weight, position = self.k, self.v, self.page_table, self.weight, self.position
         n_pages, page, Hkv, d = k.shape
         if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype or (k.numel() and k.stride(3) != 1):
             raise ValueError("k and v share their type, shape and strides, with contiguous rows")
         B, per = page_table.shape
         _like(page_table, torch.int32, (B, per), "page_table")
-        _like(length, torch.int32, (B,), "length")
-        _like(seen, torch.int32, (B,), "seen")
+        _like(self.length, torch.int32, (B,), "length")
+        _like(self.seen, torch.int32, (B,), "seen")
         _like(weight, torch.float32, (n_pages, Hkv, page), "weight")
         _like(position, torch.int32, (n_pages, Hkv, page), "position")
-        self.k, self.v, self.page_table, self.length, self.seen = k, v, page_table, length, seen
-        self.weight, self.position = weight, position
         self.B, self._cu_shape = B, (B + 1,)
         self.Hkv, self.head_dim, self.dtype = Hkv, d, k.dtype
-        bound = B * per * page
-        if weight is not None:
-            bound = min(bound, n_pages * page)
-        self.max_slots = bound if max_slots is None else int(max_slots)
+        self._bound = B * per * page if weight is None else min(B * per, n_pages) * page
         self._c = _KVCache(_ptr(k), _ptr(v), _ptr(weight), _ptr(position), _ptr(page_table), k.stride(0),
                            k.stride(1), k.stride(2), n_pages, per, page, Hkv, d, _dtype(k))
         self._ref = ctypes.addressof(self._c)
+        return self._ref
 
     def _rows(self, t, heads, name):
         """Row stride of a [rows, heads, d] tensor of the cache's type whose heads are contiguous."""
@@ -474,6 +499,7 @@ class Context:
         gives their attention weights so far.  fresh: the sequences start empty.  cache.length
         and cache.seen are updated in place."""
         import torch
+        ref = cache._struct()
         n = k_new.shape[0]
         ld = cache._new_rows(k_new, v_new)
         if weight is not None:
@@ -483,7 +509,7 @@ class Context:
             _like(rows, torch.int32, (rows.numel(),), "rows")
         length, seen = cache.length.data_ptr(), cache.seen.data_ptr()
         self._check(self._lib.estp_cache_append(
-            self._h, cache._ref, None if fresh else length, None if fresh else seen, length, seen, cache.B,
+            self._h, ref, None if fresh else length, None if fresh else seen, length, seen, cache.B,
             k_new.data_ptr(), v_new.data_ptr(), ld, n, _ptr(weight), _ptr(rows), cu_rows.data_ptr(),
             n if rows is None else rows.numel(), _stream(stream)))
 
@@ -496,6 +522,7 @@ class Context:
         of a row set where it sees the sequence's j-th row.  accumulate adds the attention the
         slots receive, times row_weight [n], to cache.weight."""
         import torch
+        ref = cache._struct()
         n, Hq, d = Q.shape
         ldq = cache._rows(Q, Hq, "Q")
         ld, kp, vp = 0, None, None
@@ -523,7 +550,7 @@ class Context:
                 w_new = torch.empty((n, cache.Hkv), dtype=torch.float32, device=dev)
                 wp = w_new.data_ptr()
         status = self._lib.estp_cache_attention(
-            self._h, cache._ref, cache.length.data_ptr(), cache.B, cache.max_slots, Q.data_ptr(), ldq, Hq, kp, vp, ld,
+            self._h, ref, cache.length.data_ptr(), cache.B, cache.max_slots, Q.data_ptr(), ldq, Hq, kp, vp, ld,
             cu_rows.data_ptr(), n, max_rows, d ** -0.5 if scale is None else scale, _ptr(tree_mask), words,
             _ptr(row_weight), 1 if accumulate else 0, out.data_ptr(), lp, wp, _stream(stream))
         if status:
@@ -534,6 +561,6 @@ class Context:
         """estp_cache_evict: every sequence is cut to at most `budget` slots, each KV head keeping
         its last `recent` and first `sinks` tokens and then those of the greatest weight;
         cache.length is updated in place."""
-        length = cache.length.data_ptr()
-        self._check(self._lib.estp_cache_evict(self._h, cache._ref, length, cache.seen.data_ptr(), length, cache.B,
+        ref, length = cache._struct(), cache.length.data_ptr()
+        self._check(self._lib.estp_cache_evict(self._h, ref, length, cache.seen.data_ptr(), length, cache.B,
                                                budget, recent, sinks, _stream(stream)))
