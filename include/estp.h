@@ -365,7 +365,7 @@ estp_status estp_misalignment(estp_ctx* ctx, const float* entropy, const float* 
  *                attention)
  *   page_table : int32 [B, max_pages]; entries past a sequence's slots are not read.  Sequences
  *                may share pages for reading; calls that write (append, evict, accumulate)
- *                need every page in one sequence only.
+ *                need every page in one sequence only.  NULL where max_pages is 0.
  *   page_size  : a power of two, 8 .. 2^20
  * The struct is a HOST pointer, its arrays caller-owned device memory.  Per sequence a program
  * also holds length int32 [B] (slots in use) and seen int32 [B] (tokens so far: the position of

@@ -477,8 +477,9 @@ static estp_status check_cache(estp_ctx* ctx, const estp_kv_cache* c, int32_t B,
         return fail(ESTP_ERR_INVALID_ARG, "cache strides must be at least head_dim");
     if (c->page_stride * es % 16 || c->slot_stride * es % 16 || c->head_stride * es % 16)
         return fail(ESTP_ERR_INVALID_ARG, "cache strides must be multiples of 16 bytes");
-    if (B > 0 && c->n_pages > 0 && (!c->k || !c->v || !c->page_table))
-        return fail(ESTP_ERR_INVALID_ARG, "NULL cache pointer");
+    if (B > 0 && c->n_pages > 0 && (!c->k || !c->v)) return fail(ESTP_ERR_INVALID_ARG, "NULL cache pointer");
+    // read for every slot that a length claims, whether or not the pool has a page
+    if (B > 0 && c->max_pages > 0 && !c->page_table) return fail(ESTP_ERR_INVALID_ARG, "page_table is NULL");
     if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->weight) || !aligned16(c->position))
         return fail(ESTP_ERR_INVALID_ARG, "k, v, weight and position must be 16-byte aligned");
     int shift = 0;
