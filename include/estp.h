@@ -448,7 +448,8 @@ estp_status estp_cache_attention(estp_ctx* ctx, const estp_kv_cache* cache, cons
  * the greatest weight (NaN below everything), the lower slot first among equals.  Kept rows from
  * slots at or past `budget`, in order, move into the slots below it that were freed, in order,
  * with their weights and positions; other rows stay where they are.  length_out[b] =
- * min(length[b], budget) (may be length).  The pages past it are the caller's again.
+ * min(length[b], budget) (may be length).  The pages past it are the caller's again.  A sequence
+ * whose length does not fit its table keeps it and records ESTP_ERR_INVALID_ARG.
  * recent + sinks <= budget. */
 estp_status estp_cache_evict(estp_ctx* ctx, const estp_kv_cache* cache, const int32_t* length,
                              const int32_t* seen, int32_t* length_out, int32_t B, int32_t budget,

@@ -203,8 +203,9 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
     if (last)
         for (int i = t; i < a.B; i += kEvictThreads) {
             const int l = a.length[i];
-            if (l < 0 || l > a.c.capacity()) report(a.status, ESTP_ERR_INVALID_ARG);
-            a.length_out[i] = min(l, a.budget);
+            const bool fits = l >= 0 && l <= a.c.capacity();  // else nothing was ranked or moved: the length stays
+            if (!fits) report(a.status, ESTP_ERR_INVALID_ARG);
+            a.length_out[i] = fits ? min(l, a.budget) : l;
         }
     if (n <= a.budget) return;  // the whole cluster
 
