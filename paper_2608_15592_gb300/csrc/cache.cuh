@@ -39,6 +39,10 @@ struct CacheView {
     __device__ __forceinline__ int64_t meta(int64_t page, int slot, int g) const {
         return ((page * Hkv + g) << shift) + (slot & ((1 << shift) - 1));
     }
+    // bounds of the checked build: a slot's place in the pool
+    __device__ __forceinline__ bool inside(int64_t page, int slot, int g, int* status) const {
+        return in_bounds(page >= 0 && page < n_pages && slot >= 0 && slot < capacity() && g >= 0 && g < Hkv, status);
+    }
     // page of a slot of sequence b; -1 (reported) when the table holds no page of the pool there
     __device__ __forceinline__ int64_t page_of(int b, int slot, int* status) const {
         const int p = table[(int64_t)b * ld_table + (slot >> shift)];
@@ -68,9 +72,10 @@ struct CacheAttnArgs {
     int row_blocks;              // blocks of the finish kernel that merge rows, warps of one of them
     int row_warps;
     int store;                   // scores are kept for the weights
-    float* part_o;               // [G + groups][RB][d]
-    float2* part_ml;             // [G + groups][RB]: running max (log2 units) and sum
-    float* score;                // [units][RB][128], unscaled
+    int64_t n_parts, n_units;    // bounds of the slots of partials, of the units
+    float* part_o;               // [n_parts][RB][d]
+    float2* part_ml;             // [n_parts][RB]: running max (log2 units) and sum
+    float* score;                // [n_units][RB][128], unscaled
     float2* factor;              // [n_rows, Hq]: (-M, c / L), where the weights are wanted
     char* out;
     float* lse;
@@ -79,6 +84,14 @@ struct CacheAttnArgs {
     int* status;
     volatile int* timed_out;     // a kernel of the attention gave up: the weights stay as they are
     long long wait_cycles;
+    // bounds of the checked build: the slots of n partials from one on, a unit, rows of the call
+    __device__ __forceinline__ bool part_inside(int64_t slot, int n = 1) const {
+        return in_bounds(slot >= 0 && n >= 1 && slot + n <= n_parts, status);
+    }
+    __device__ __forceinline__ bool unit_inside(int64_t u) const { return in_bounds(u >= 0 && u < n_units, status); }
+    __device__ __forceinline__ bool row_inside(int64_t row, int n = 1) const {
+        return in_bounds(row >= 0 && n >= 1 && row + n <= n_rows, status);
+    }
 };
 
 // What sequence b brings to the call.

@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) cache_fwd_kernel(const Cach
 #pragma unroll
             for (int r = 0; r < kRows; ++r)
                 if (hidden >> r & 1) z[r] = -INFINITY;
-            if (a.store)
+            if (a.store && a.unit_inside(u))
                 for (int r = 0; r < nr; ++r) a.score[((int64_t)u * kRows + r) * kCacheTile + t] = z[r];
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) cache_fwd_kernel(const Cach
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            if (r >= nr) break;
+            if (r >= nr || !a.part_inside(slot)) break;
             if (t == 0)
                 a.part_ml[slot * kRows + r] = make_float2(m[r], (red[0][r] + red[1][r]) + (red[2][r] + red[3][r]));
             const float x = r & 1 ? o[r / 2].y : o[r / 2].x;
@@ -373,6 +373,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
             const int h = x % a.Hq, i = (int)row - a.cu[at.b], r = i * a.rep + h % a.rep;
             const Pieces w = pieces_of(a, at, s, h / a.rep, r, tot.units);
             if (a.whole && w.n == 1) continue;
+            if (!a.part_inside(w.first / a.RB, w.n) || !a.row_inside(row)) continue;  // alike for all who share a barrier
             const float2 all = merged_ml(a, w, lane);
             float o[kC];
 #pragma unroll
@@ -424,13 +425,15 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
         const int R = s.n * a.rep;
         __syncwarp();
         if (a.whole && pieces_of(a, at, s, g, 0, tot.units).n == 1) {  // (kept scores of bf16: one block of rows)
-            for (int r = lane; r < R; r += 32) f[r] = a.factor[(row0 + r / a.rep) * a.Hq + g * a.rep + r % a.rep];
+            for (int r = lane; r < R; r += 32)
+                f[r] = a.row_inside(row0 + r / a.rep) ? a.factor[(row0 + r / a.rep) * a.Hq + g * a.rep + r % a.rep] : make_float2(0.f, 0.f);
         } else {
             for (int rw = 0; rw < R; rw += 4) {  // 8 lanes a row
                 const int r = rw + (lane >> 3);
                 float M = -INFINITY, L = 0.f;
                 if (r < R) {
-                    const Pieces w = pieces_of(a, at, s, g, r, tot.units);
+                    Pieces w = pieces_of(a, at, s, g, r, tot.units);
+                    if (!a.part_inside(w.first / a.RB, w.n)) w.n = 0;
                     for (int p0 = lane & 7; p0 < w.n; p0 += 32) {  // 4 in flight
                         float2 x[4];
 #pragma unroll
@@ -456,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
             float4 had = make_float4(0.f, 0.f, 0.f, 0.f), sum = had;
             if (!drafts) {  // 4 slots of one page
                 const int64_t page = a.c.page_of(at.b, slot, a.status);
-                if (page < 0) continue;
+                if (page < 0 || !a.c.inside(page, slot, g, a.status)) continue;
                 to = a.c.weight + a.c.meta(page, slot, g);
                 if (n >= 4) had = *reinterpret_cast<const float4*>(to);
             }
@@ -466,6 +469,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
             for (int k = 0; k < s.nrb; ++k) {
                 const int r0 = k * a.RB, nr = min(a.RB, R - r0);
                 const int u = at.unit0 + (g * s.nrb + k) * s.nt + tile;
+                if (!a.unit_inside(u)) break;
                 const float4* z = reinterpret_cast<const float4*>(a.score + (int64_t)u * a.RB * kCacheTile) + lane;
                 constexpr int kBatch = 4;  // rows in flight; 8 spill, 25 us more over 256 sequences of some 2k
                 for (int q0 = 0; q0 < nr; q0 += kBatch) {
@@ -485,6 +489,7 @@ __global__ void __launch_bounds__(kThreads, 8) cache_finish_kernel(const CacheAt
                 }
             }
             if (drafts) {
+                if (!a.row_inside(row0 + lane * 4, min(n, 4))) continue;
                 float* d = a.w_new + (row0 + lane * 4) * a.c.Hkv + g;
                 d[0] = sum.x;
                 if (n > 1) d[a.c.Hkv] = sum.y;
@@ -531,7 +536,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) cache_weight_kernel(const C
                 const int nr = min(kRows, R - r0);
                 __syncthreads();
                 load_q<T, D>(a, q, at.b, g, r0, nr);
-                if (t < nr) ml[t] = a.factor[(row0 + (r0 + t) / a.rep) * a.Hq + g * a.rep + (r0 + t) % a.rep];
+                if (t < nr) {
+                    const int64_t row = row0 + (r0 + t) / a.rep;
+                    ml[t] = a.row_inside(row) ? a.factor[row * a.Hq + g * a.rep + (r0 + t) % a.rep] : make_float2(0.f, 0.f);
+                }
                 __syncthreads();
                 float z[kRows];
                 dots<D>(q, kr.k, zs + (t & ~31), z);
@@ -545,8 +553,11 @@ __global__ void __launch_bounds__(kThreads, kBlocks) cache_weight_kernel(const C
                 }
             }
             if (kr.k == nullptr) continue;
-            if (drafts) a.w_new[(row0 + t) * a.c.Hkv + g] = sum;
-            else a.c.weight[kr.meta] += sum;
+            if (drafts) {
+                if (a.row_inside(row0 + t)) a.w_new[(row0 + t) * a.c.Hkv + g] = sum;
+            } else if (in_bounds(kr.meta >= 0 && kr.meta < a.c.meta(a.c.n_pages, 0, 0), a.status)) {
+                a.c.weight[kr.meta] += sum;
+            }
         }
     });
 }
@@ -567,6 +578,8 @@ estp_status launch(estp_ctx* ctx, CacheAttnArgs& a, cudaStream_t st) {
     // largest sequence
     const int64_t nrb = ((int64_t)a.max_rows * a.rep + a.RB - 1) / a.RB;
     const int64_t units = (int64_t)a.c.Hkv * nrb * (a.n_slots / kCacheTile + 2 * (int64_t)a.B);
+    a.n_parts = slots;
+    a.n_units = units;
     if (2 * units > INT32_MAX || a.n_rows * a.Hq > INT32_MAX)
         return fail(ESTP_ERR_UNSUPPORTED, "max_slots and rows: more than 2^31 tiles of work, or rows times heads");
     const size_t o_bytes = align_up(sizeof(float) * (size_t)slots * a.RB * D, 256);

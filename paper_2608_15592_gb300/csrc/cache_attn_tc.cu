@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                     }
                 };
                 load_s();
-                if (a.store && alive) {
+                if (a.store && alive && a.unit_inside(walk.u - (sg.tile1 - tile))) {
                     float* to = a.score + ((int64_t)(walk.u - (sg.tile1 - tile)) * a.RB) * kCacheTile + j;
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                 const float scale = !whole ? 1.f : M == -INFINITY && L == 0.f ? 0.f : 1.f / L;
                 row_a[j] = fa * scale;
                 row_b[j] = fb * scale;
-                if (nb == 0 && j < nr) {
+                if (nb == 0 && j < nr && (whole ? a.row_inside(row0 + (sg.r0 + j) / a.rep) : a.part_inside(cta + sg.group))) {
                     if (whole) {
                         const int rr = sg.r0 + j, h = sg.g * a.rep + rr % a.rep;
                         const int64_t row = row0 + rr / a.rep;
@@ -567,8 +567,9 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
                         float o = wa != 0.f ? (hi[k] + lo[k]) * wa : 0.f;
                         if (wb != 0.f) o = fmaf(hb[k] + lb[k], wb, o);
                         if (whole) {
-                            reinterpret_cast<__nv_bfloat16*>(a.out)[((row0 + i) * a.Hq + h) * D + j] = __float2bfloat16_rn(o);
-                        } else {
+                            if (a.row_inside(row0 + i))
+                                reinterpret_cast<__nv_bfloat16*>(a.out)[((row0 + i) * a.Hq + h) * D + j] = __float2bfloat16_rn(o);
+                        } else if (a.part_inside(cta + sg.group)) {
                             a.part_o[(part + r + k) * D + j] = o;
                         }
                         if (++h == (sg.g + 1) * a.rep) ++i, h -= a.rep;

@@ -460,7 +460,8 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
             fa *= scale;
             fb *= scale;
             const int64_t part = (int64_t)(cta + sg.group) * a.RB + base + j;
-            if (mine && (!split || w == 0)) {
+            const bool inside = !mine || (whole ? a.row_inside(row) : a.part_inside(cta + sg.group));
+            if (mine && inside && (!split || w == 0)) {
                 if (!whole) a.part_ml[part] = make_float2(M, L);
                 if (whole && a.lse != nullptr) a.lse[(int64_t)h * a.n_rows + row] = L == 0.f ? -INFINITY : fmaf(M, kLn2, logf(L));
                 if (whole && a.factor != nullptr) a.factor[row * a.Hq + h] = weight_factor(a, make_float2(M, L), row);
@@ -477,7 +478,7 @@ __global__ void __launch_bounds__(RowShape<D>::kThreads, 1)
                 tmem_wait_ld();
                 tie<16>(o);
                 tie<16>(b);
-                if (!mine) continue;
+                if (!mine || !inside) continue;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
                     o[k] = fa != 0.f ? o[k] * fa : 0.f;

@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 4) append_kernel(const Appe
         if (!append_ok(a, first, next, len) || e < first || e >= next) continue;  // reported below
         const int slot = len + (int)(e - first), pos = (a.length != nullptr ? a.seen[b] : 0) + (int)(e - first);
         const int64_t page = a.c.page_of(b, slot, a.status);
-        if (page < 0) continue;
+        if (page < 0 || !a.c.inside(page, slot, 0, a.status) || !in_bounds(src < a.n_src, a.status)) continue;
         auto put = [&](int i, const uint4& p, const uint4& q) {
             const int g = i / per, o = (i - g * per) * 16;
             const int64_t to = a.c.row(page, slot, g) + o;
@@ -395,8 +395,8 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
             const int page = table[s >> a.c.shift];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (freed >> i & 1) list_f[f++] = make_int2(page, s + i);
-                if (past >> i & 1) list_p[p++] = make_int2(page, s + i);
+                if (freed >> i & 1 && in_bounds(f >= 0 && f < a.max_moves, a.status)) list_f[f++] = make_int2(page, s + i);
+                if (past >> i & 1 && in_bounds(p >= 0 && p < a.max_moves, a.status)) list_p[p++] = make_int2(page, s + i);
             }
         }
         const int all = __shfl_sync(0xffffffffu, scan + both, 31);
@@ -415,8 +415,9 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int j = j0 + i * stride;
-            dst[i] = j < moves ? list_f[j] : make_int2(-1, 0);
-            src[i] = j < moves ? list_p[j] : make_int2(-1, 0);
+            const bool there = j < moves && in_bounds(j < a.max_moves, a.status);
+            dst[i] = there ? list_f[j] : make_int2(-1, 0);
+            src[i] = there ? list_p[j] : make_int2(-1, 0);
         }
         uint4 x[kBatch], y[kBatch];
         float w[kBatch];
@@ -425,6 +426,7 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(const EvictArgs
         for (int i = 0; i < kBatch; ++i) {
             // a page that is none was reported with its key
             if (src[i].x < 0 || src[i].x >= a.c.n_pages || dst[i].x >= a.c.n_pages) dst[i].x = -1;
+            if (dst[i].x >= 0 && !(a.c.inside(src[i].x, src[i].y, g, a.status) && a.c.inside(dst[i].x, dst[i].y, g, a.status))) dst[i].x = -1;
             if (dst[i].x < 0) continue;
             const int64_t from = a.c.row(src[i].x, src[i].y, g) + at * 16, ms = a.c.meta(src[i].x, src[i].y, g);
             x[i] = *reinterpret_cast<const uint4*>(a.c.k + from);

@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                 }
                 for (int r = tid; r < blocks * kWBlock; r += 256) {  // whole warps
                     float2 f = make_float2(0.f, 0.f);
-                    if (r < nr) f = a.factor[(row0 + (r0 + r) / a.rep) * a.Hq + w.g * a.rep + (r0 + r) % a.rep];
+                    if (r < nr && a.row_inside(row0 + (r0 + r) / a.rep)) f = a.factor[(row0 + (r0 + r) / a.rep) * a.Hq + w.g * a.rep + (r0 + r) % a.rep];
                     fs[(r >> 1) * 4 + (r & 1)] = f.x;
                     fs[(r >> 1) * 4 + 2 + (r & 1)] = f.y;
                     const uint32_t bits = __ballot_sync(0xffffffffu, f.y != 0.f);
@@ -232,12 +232,14 @@ __global__ void __launch_bounds__(WShape<D>::kThreads, 1)
                     float had = 0.f;
                     if (j < keys) {  // early: its latency passes under the sums
                         if (drafts) {
-                            to = a.w_new + (row0 + j) * a.c.Hkv + w.g;
-                            if (r0 > 0) had = *to;
+                            if (a.row_inside(row0 + j)) {
+                                to = a.w_new + (row0 + j) * a.c.Hkv + w.g;
+                                if (r0 > 0) had = *to;
+                            }
                         } else {
                             const int slot = tile * kCacheTile + j;
                             const int64_t page = a.c.page_of(w.b, slot, a.status);
-                            if (page >= 0) {
+                            if (page >= 0 && a.c.inside(page, slot, w.g, a.status)) {
                                 to = a.c.weight + a.c.meta(page, slot, w.g);
                                 had = *to;
                             }
