@@ -391,8 +391,10 @@ typedef struct {
  * lengths and counts go to length_out and seen_out, which may be length and seen.
  *   length, seen   : int32 [B], or both NULL: every sequence starts empty (its old rows are dropped)
  *   k_new, v_new   : [n_new, Hkv, head_dim] of the cache's type, row stride ld_new elements
- *   weight_new     : fp32 [n_new, Hkv], the rows' weights so far (the prefill's importance, or
- *                    estp_cache_attention's weight_new_out), or NULL for 0
+ *   weight_new     : fp32 [n_new, Hkv], the rows' weights so far (estp_cache_attention's
+ *                    weight_new_out, or the prefill's importance on the same scale: of one layer,
+ *                    ESTP_IMP_DIV_NONE, times Hq / Hkv, as a weight sums over the query heads of the
+ *                    KV head and the importance is their mean), or NULL for 0
  *   rows           : int32 [n_rows], the row of k_new that entry e takes (accepted drafts, for
  *                    instance), or NULL: row e
  *   cu_rows        : int32 [B + 1], cu_rows[0] = 0; n_rows is at least cu_rows[B] (a bound: entries

@@ -496,7 +496,8 @@ class Context:
                      fresh: bool = False, stream=None):
         """estp_cache_append: rows of k_new, v_new [n, Hkv, d] enter the cache, cu_rows[b] ..
         cu_rows[b+1]-1 into sequence b; `rows` (int32) picks rows of k_new, `weight` [n, Hkv]
-        gives their attention weights so far.  fresh: the sequences start empty.  cache.length
+        gives their attention weights so far: of cache_attention, or one layer's importance with
+        divisor="none" times Hq / Hkv, which is the same scale.  fresh: the sequences start empty.  cache.length
         and cache.seen are updated in place."""
         import torch
         ref = cache._struct()
