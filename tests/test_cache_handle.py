@@ -111,3 +111,42 @@ def test_a_bound_of_the_slots_stays():
     assert cache.max_slots == 20
     cache.max_slots = 30
     assert cache.max_slots == 30
+
+
+def _new(n, Hkv, d=64, extra=0):
+    """Rows of a wider array, n of them."""
+    return torch.zeros(n, Hkv + extra, d, dtype=torch.bfloat16)[:, :Hkv]
+
+
+@pytest.mark.parametrize("n,Hkv", [(1, 2), (0, 2), (1, 1)])
+def test_strides_that_are_never_stepped_by_need_not_agree(n, Hkv):
+    """One row: K from a fused projection, V of its own (a batch of one in decoding)."""
+    ctx, cache = _context(), estp.KVCache(**_tensors(B=1, Hkv=Hkv))
+    kn, vn, q = _new(n, Hkv, extra=5), _new(n, Hkv), _new(n, 2 * Hkv)
+    cu = torch.zeros(2, dtype=torch.int32)
+    ctx.cache_append(cache, kn, vn, cu, stream=_Stream())
+    ctx.cache_attention(cache, q, kn, vn, cu, 1, stream=_Stream())
+    ctx.cache_attention(cache, q, vn, kn, cu, 1, stream=_Stream())
+    assert [c[2][9] for c in ctx._lib.calls[:1]] == [Hkv * 64] and [c[2][10] for c in ctx._lib.calls[1:]] == [Hkv * 64] * 2
+
+
+def test_rows_of_one_head():
+    """A single KV head: the heads' stride is never stepped by, the rows' is."""
+    ctx, cache = _context(), estp.KVCache(**_tensors(Hkv=1))
+    cu = torch.zeros(3, dtype=torch.int32)
+    wide = torch.zeros(3, 128, dtype=torch.bfloat16)
+    kn = wide[:, :64].unsqueeze(1)                   # strides 128, 64, 1
+    vn = wide[:, 64:].reshape(3, 1, 64).as_strided((3, 1, 64), (128, 7, 1))
+    ctx.cache_append(cache, kn, vn, cu, stream=_Stream())
+    assert ctx._lib.calls[-1][2][9] == 128
+
+
+@pytest.mark.parametrize("kn,vn", [(_new(2, 2, extra=1), _new(2, 2)), (_new(2, 2), _new(3, 2)), (_new(2, 2), _new(2, 2).float()),
+                                   (_new(2, 2), torch.zeros(2, 64, 2, dtype=torch.bfloat16).transpose(1, 2)),
+                                   (torch.zeros(1, 64, 2, dtype=torch.bfloat16).transpose(1, 2), _new(1, 2)),
+                                   (_new(1, 2), torch.zeros(1, 64, 2, dtype=torch.bfloat16).transpose(1, 2))])
+def test_rows_that_do_not_agree_are_refused(kn, vn):
+    ctx, cache = _context(), estp.KVCache(**_tensors(B=1))
+    with pytest.raises(ValueError):
+        ctx.cache_append(cache, kn, vn, torch.zeros(2, dtype=torch.int32), stream=_Stream())
+    assert ctx._lib.calls == []
