@@ -416,13 +416,18 @@ estp_status estp_cache_append(estp_ctx* ctx, const estp_kv_cache* cache, const i
  * Query head h reads KV head h / (Hq / Hkv).  A row that sees nothing, or scores of -inf only,
  * gives zeros and lse = -inf.
  *   max_slots      : a bound of the sum of the lengths (it sizes the workspace; more slots on
- *                    the device record ESTP_ERR_INVALID_ARG)
+ *                    the device record ESTP_ERR_INVALID_ARG).  Where weights are asked for and a KV
+ *                    head has few rows (at 8 bytes a row no more than a key has), the scores take 4
+ *                    bytes for each of max_rows * Hq / Hkv (rounded up to 8, 16 or 32; fp32: to a
+ *                    multiple of 8), KV head and slot of this bound; where that is more than 2 GB,
+ *                    or there are more rows, the weights take another read of K instead
  *   Q              : [n_rows, Hq, head_dim] of the cache's type, row stride ldq elements
  *   k_new, v_new   : [n_rows, Hkv, head_dim], row stride ld_new, the rows' own K and V, or both
  *                    NULL: rows see cached slots only
- *   cu_rows        : int32 [B + 1], from 0 to n_rows; a sequence may have no row
- *   max_rows       : at least every sequence's rows; <= 128, and max_rows * Hq / Hkv <= 1024
- *                    (else ESTP_ERR_UNSUPPORTED)
+ *   cu_rows        : int32 [B + 1], from 0 to n_rows (exactly: every row belongs to a sequence); a
+ *                    sequence may have no row
+ *   max_rows       : at least every sequence's rows and at most n_rows; <= 128, and
+ *                    max_rows * Hq / Hkv <= 1024 (else ESTP_ERR_UNSUPPORTED)
  *   tree_mask      : uint64 [n_rows, mask_words]: bit j of row i is set where i sees the
  *                    sequence's j-th row (its own bit included); NULL: row i sees rows j <= i.
  *                    What a hidden row holds, NaN among it, reaches no other row.
@@ -452,7 +457,8 @@ estp_status estp_cache_attention(estp_ctx* ctx, const estp_kv_cache* cache, cons
  * with their weights and positions; other rows stay where they are.  length_out[b] =
  * min(length[b], budget) (may be length).  The pages past it are the caller's again.  A sequence
  * whose length does not fit its table keeps it and records ESTP_ERR_INVALID_ARG.
- * recent + sinks <= budget. */
+ * recent + sinks <= budget.  The workspace holds 16 bytes for each sequence, KV head and slot that may
+ * have to move: min(budget, max_pages * page_size - budget), by the table's width, not by the lengths. */
 estp_status estp_cache_evict(estp_ctx* ctx, const estp_kv_cache* cache, const int32_t* length,
                              const int32_t* seen, int32_t* length_out, int32_t B, int32_t budget,
                              int32_t recent, int32_t sinks, estp_stream_t stream);

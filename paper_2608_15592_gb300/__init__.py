@@ -193,7 +193,8 @@ class KVCache:
     page_table int32 [B, max_pages];  length, seen: int32 [B], updated in place
     weight     fp32 [n_pages, Hkv, page_size], position: int32 of that shape, or None
     max_slots  a bound of the slots in use over all sequences (default: what the page table can
-               hold; with weights, which need every page in one sequence only, at most the pool's)
+               hold; with weights, which need every page in one sequence only, at most the pool's).
+               The scratch of cache_attention grows with it, that of cache_evict with the table
 
     Each is an attribute that may be replaced (a longer page table, a larger pool); the call after
     that looks all of them over again, together.

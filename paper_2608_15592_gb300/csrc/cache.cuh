@@ -153,9 +153,11 @@ __device__ __forceinline__ int scan_lanes(int x, int lane) {  // inclusive
 }
 
 // Launches.  Every kernel of the cache may begin before the one ahead of it in the stream has ended
-// (launch_dependent), and waits for it (await_stream) before it touches anything; only then does it let
-// the next begin.  So the kernels after the first of a call may read the call's inputs, such as the
-// lengths, before their own wait.
+// (launch_dependent).  The first kernel of a call waits for that one (await_stream) before it touches
+// anything, and only after its wait lets the next begin (admit_next).  So when a later kernel of the call
+// begins, everything ahead of the call is over: it may read the call's inputs, such as the lengths, and
+// admit its own successor before its wait, but nothing that the call's kernels write, and it waits before
+// it ends.
 __device__ __forceinline__ void await_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void admit_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
@@ -316,8 +318,6 @@ __device__ __forceinline__ uint64_t rows_that_see(const CacheAttnArgs& a, int64_
     return rows;
 }
 
-// The tensor-core forwards of bf16 caches: keys on the lanes (up to 32 rows a (b, KV head)), rows on the
-// lanes (more).
 // A launch that may begin before the one ahead of it has ended.
 template <class Kernel, class... Args>
 cudaError_t launch_dependent(Kernel kernel, int64_t grid, int threads, size_t smem, cudaStream_t st, const Args&... args) {
@@ -335,6 +335,8 @@ cudaError_t launch_dependent(Kernel kernel, int64_t grid, int threads, size_t sm
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
 
+// The tensor-core forwards of bf16 caches: keys on the lanes (up to 32 rows a (b, KV head)), rows on the
+// lanes (more).
 estp_status launch_cache_fwd_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_rows_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);
 estp_status launch_cache_weight_tc(estp_ctx* ctx, const CacheAttnArgs& a, cudaStream_t st);

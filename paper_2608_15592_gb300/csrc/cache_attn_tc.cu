@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(Shape<D, RB>::kThreads, 1)
 
     if (warp == 0 || warp == 3) {
         // ------------------------------------------------------------ producers
-        // warp 0 the K tiles (even ring entries), warp 3 the V tiles (odd ones) and the rows' Q
+        // warp 0 the K tiles, warp 3 the V tiles and the rows' Q
         const int kv = warp == 3;
         const Ring ring = kv ? ring_v : ring_k;
         if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(

@@ -11,7 +11,7 @@
 // A row's m only moves when a tile exceeds it by 2^8; the warps whose rows do then rescale O and l.
 //
 // One persistent CTA per SM over the units of cache.cuh, two epilogue groups of 128 threads, each with
-// an S/P buffer and an O (all 512 columns).  A block of up to 128 rows is split by tiles: the groups
+// an S/P buffer and an O of 128 columns (all 512).  A block of up to 128 rows is split by tiles: the groups
 // take them in turn, each with a softmax of its own, and are joined at a segment's end.  A block of up
 // to 256 rows is split by rows, 128 a group, and every tile goes to both.  Either way one group's
 // softmax runs under the other's products.
@@ -25,7 +25,8 @@
 //              148 us).  Two warps to a group's 32 rows have 96 registers a thread: 198 us.
 // Bound by the turn of a group: 1.5 us of softmax and 1.6 of products (24 of 64 clocks, the other
 // group's between them) for every tile, 1.55 us a tile with two groups, where the tensor pipe needs 0.85
-// and the copies 1.45.  Another S buffer would part them, but the columns are spent.
+// and the copies 1.45.  Another S buffer would part them.  At head size 128 the columns are spent; at 64 an
+// O takes half of the columns kept for it, and a third S buffer would fit: it is not built.
 // Keys past a sequence's slots, drafts that are not finite and waits are treated as in
 // cache_attn_tc.cu.
 #include "cache_tc.cuh"
