@@ -463,6 +463,78 @@ estp_status estp_cache_evict(estp_ctx* ctx, const estp_kv_cache* cache, const in
                              const int32_t* seen, int32_t* length_out, int32_t B, int32_t budget,
                              int32_t recent, int32_t sinks, estp_stream_t stream);
 
+/* ------------------------------------------------------------------ (f)
+ * What training and serving read off the same distributions as (a): the paper stops at their
+ * entropy.  For row r of logits z and a temperature T > 0 (at least 1e-6),
+ *   lse = ln sum_v exp(z_v / T),  ln p_v = z_v / T - lse.
+ * The calls of this group take logits [n_rows, ld] of ESTP_BF16 or ESTP_F32 as estp_token_entropy
+ * does, of which the first V <= 2^30 columns are read.  Unlike there, a logit may be -inf (a masked
+ * token, p = 0), or the type's lowest value.  A row of -inf alone has ln p = -inf, entropy 0 and
+ * gradients of 0.  A row that holds NaN or +inf gives NaN.  Sums are held in fp32.
+ * Their scratch has a fixed size and comes with the context: they allocate nothing, a first call may
+ * be captured in a graph.
+ *
+ * Log probabilities of given tokens, with entropy and the greatest alternatives:
+ *   targets          : int32 [n_rows], a token of each row; negative: none (its log probability is
+ *                      given as 0); at or past V: NaN, and ESTP_ERR_INVALID_ARG in the status word.
+ *                      NULL where logprob_out is NULL
+ *   top_k            : alternatives a row, 0 .. min(V, 128): the greatest logits, descending, the
+ *                      lower token first among equals (-0 equals +0)
+ *   logprob_out      : fp32 [n_rows]       ln p of the target, or NULL
+ *   entropy_out      : fp32 [n_rows]       -sum_v p_v ln p_v in nats, or NULL
+ *   norm_out         : fp32 [n_rows, 2]    {max_v z_v, sum_v exp((z_v - max) / T)} (8-byte aligned),
+ *                      or NULL: lse = max / T + ln sum; the gradient takes it.  {-inf, 0} for a row of
+ *                      -inf alone
+ *   top_ids_out      : int32 [n_rows, top_k]; -1 in a row that gives NaN
+ *   top_logprobs_out : fp32 [n_rows, top_k] ln p of them, or NULL */
+estp_status estp_token_logprobs(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                                int64_t ld, const int32_t* targets, float temperature, int32_t top_k,
+                                float* logprob_out, float* entropy_out, float* norm_out, int32_t* top_ids_out,
+                                float* top_logprobs_out, estp_stream_t stream);
+
+/* The gradient of estp_token_logprobs' outputs with respect to the logits: for the upstream gradients
+ * g of the target's log probability, a_j of the alternatives', h of the entropy and l of lse,
+ *   T dz_v = g [v = target] + sum_j a_j [v = id_j] + p_v (l - g - sum_j a_j) - h p_v (ln p_v + H).
+ *   norm, entropy  : norm_out and (where grad_entropy is given) entropy_out of the forward call on the
+ *                    same logits and temperature
+ *   targets        : as there; a row without target gets nothing from grad_logprob
+ *   top_ids        : int32 [n_rows, top_k], top_k <= min(V, 128); negative: none, repeated ones add up;
+ *                    at or past V (a target too): left out, and ESTP_ERR_INVALID_ARG in the status word
+ *   grad_logprob, grad_entropy, grad_lse : fp32 [n_rows], grad_top: fp32 [n_rows, top_k]; each may be NULL
+ *   grad_logits    : [n_rows, ld_grad] of the logits' type, 16-byte aligned rows; may be the logits
+ *                    themselves (ld_grad = ld), else does not overlap them.  Columns past V stay as they are
+ * A row whose upstream gradients are 0 gets zeros, whatever its logits. */
+estp_status estp_token_logprobs_grad(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                                     int64_t ld, const float* norm, const float* entropy, const int32_t* targets,
+                                     float temperature, int32_t top_k, const int32_t* top_ids,
+                                     const float* grad_logprob, const float* grad_entropy, const float* grad_lse,
+                                     const float* grad_top, void* grad_logits, int64_t ld_grad,
+                                     estp_stream_t stream);
+
+/* Distillation from a teacher of whom K tokens a row are known, with its gradient in the same call:
+ *   loss_r = sum_j q_j (ln q_j - ln p_id_j) [+ q_r (ln q_r - ln p_r)]
+ *   tail = 0 : q is the softmax of teacher_logits / T over the row's K tokens (logits or log
+ *              probabilities alike); no rest
+ *   tail = 1 : teacher_logits are log probabilities at temperature T, q_j = exp of them; the rest
+ *              q_r = max(0, 1 - sum_j q_j) is one bucket, p_r the student's mass outside the K tokens
+ *   grad_logits = row_weight_r dloss_r/dz (the student's logits; the teacher's are constants)
+ *   teacher_ids    : int32 [n_rows, K], 1 <= K <= 128; negative: no entry (its logit is not read); at or
+ *                    past V: left out, and ESTP_ERR_INVALID_ARG in the status word.  tail = 0: a
+ *                    repeated token counts each time.  tail = 1: it is left out but for the first time,
+ *                    with ESTP_ERR_INVALID_ARG in the status word
+ *   teacher_logits : fp32 [n_rows, K]
+ *   row_weight     : fp32 [n_rows], factors of the gradient (1 / tokens, T^2, a loss mask), NULL for 1
+ *   loss_out       : fp32 [n_rows], not multiplied by row_weight
+ *   grad_logits    : as estp_token_logprobs_grad's (in place allowed), or NULL for the loss alone
+ * A row without entries (or, tail = 0, with entries of -inf only) has loss 0 and a gradient of 0,
+ * whatever its logits; so has the gradient of a row of weight 0.  A named token of q_j > 0 whose logit
+ * is -inf makes the loss +inf; so does a rest where the student has no other token, unless it is at
+ * most 2^-20 and so the rounding of the log probabilities (then it is taken as 0). */
+estp_status estp_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                              int64_t ld, const int32_t* teacher_ids, const float* teacher_logits, int32_t K,
+                              float temperature, int tail, const float* row_weight, float* loss_out,
+                              void* grad_logits, int64_t ld_grad, estp_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

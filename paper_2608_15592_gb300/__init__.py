@@ -42,7 +42,7 @@ EXPORTS = ("estp_create", "estp_destroy", "estp_last_error", "estp_sync_status",
            "estp_head_loss", "estp_misalignment", "estp_lm_head_entropy",
            "estp_mlp_head_predict", "estp_mlp_head_loss", "estp_attn_forward_importance",
            "estp_set_wait_limit", "estp_cache_append", "estp_cache_attention",
-           "estp_cache_evict")
+           "estp_cache_evict", "estp_token_logprobs", "estp_token_logprobs_grad", "estp_distill_loss")
 
 
 class EstpError(RuntimeError):
@@ -121,6 +121,11 @@ def load_library(path: str = LIB_PATH):
         "estp_cache_attention": ([P, P, P, I32, I64, P, I64, I32, P, P, I64, P, I64, I32, F, P, I32, P,
                                   ctypes.c_int, P, P, P, P], ctypes.c_int),
         "estp_cache_evict": ([P, P, P, P, P, I32, I32, I32, I32, P], ctypes.c_int),
+        "estp_token_logprobs": ([P, P, ctypes.c_int, I64, I64, I64, P, F, I32, P, P, P, P, P, P], ctypes.c_int),
+        "estp_token_logprobs_grad": ([P, P, ctypes.c_int, I64, I64, I64, P, P, P, F, I32, P, P, P, P, P, P, I64, P],
+                                     ctypes.c_int),
+        "estp_distill_loss": ([P, P, ctypes.c_int, I64, I64, I64, P, P, I32, F, ctypes.c_int, P, P, P, I64, P],
+                              ctypes.c_int),
     }
     for name, (args, res) in sigs.items():
         fn = getattr(lib, name)
@@ -177,6 +182,24 @@ class MlpHead:
     W2: "object"
     b2: "object"
     centers: "object"
+
+
+@dataclass
+class TokenLogprobs:
+    """What token_logprobs returns: logprob [n] (None without targets), entropy [n], norm [n, 2] (the
+    greatest logit and the sum of exponentials against it), top_ids and top_logprobs [n, top_k]
+    (None without), and the temperature they belong to."""
+    logprob: "object"
+    entropy: "object"
+    norm: "object"
+    top_ids: "object"
+    top_logprobs: "object"
+    temperature: float = 1.0
+
+    @property
+    def lse(self):
+        """ln sum_v exp(z_v / temperature) per row, fp32 [n]."""
+        return self.norm[:, 0] / self.temperature + self.norm[:, 1].log()
 
 
 def _like(t, dtype, shape, name):
@@ -569,3 +592,117 @@ class Context:
         ref, length = cache._struct(), cache.length.data_ptr()
         self._check(self._lib.estp_cache_evict(self._h, ref, length, cache.seen.data_ptr(), length, cache.B,
                                                budget, recent, sinks, _stream(stream)))
+
+    # ------------------------------------------------------------------ (f)
+    def _here(self, **tensors):
+        """Each tensor (None passes) is on the context's device."""
+        for name, t in tensors.items():
+            if t is not None and t.get_device() != self.device:
+                raise ValueError(f"{name} is not on the context's device cuda:{self.device}")
+
+    def _logits(self, logits, V):
+        """Rows, V and row stride of logits [rows, >= V] whose rows are contiguous."""
+        if logits.dim() != 2 or (logits.numel() and logits.stride(1) != 1):
+            raise ValueError("logits is a [rows, V] tensor with contiguous rows")
+        rows, cols = logits.shape
+        V = cols if V is None else V
+        if not 1 <= V <= cols:
+            raise ValueError("V is in 1 .. the columns of logits")
+        return rows, V, logits.stride(0) if rows > 1 else cols + -cols % (16 // logits.element_size())
+
+    def _grad_like(self, logits, V, out, new):
+        """Where the gradient of logits goes, [rows, V]: `out`, or a new tensor whose rows start on 16 bytes."""
+        per = 16 // logits.element_size()
+        rows = logits.shape[0]
+        if out is None:
+            wide = new((rows, V + -V % per), logits.dtype)
+            return wide[:, :V], wide.shape[1]
+        if out.dim() != 2 or out.shape[0] != rows or out.shape[1] < V or out.dtype != logits.dtype or (
+                out.numel() and out.stride(1) != 1):
+            raise ValueError("out is a [rows, >= V] tensor of the logits' type with contiguous rows")
+        return out, out.stride(0) if rows > 1 else out.shape[1] + -out.shape[1] % per
+
+    def _new(self, device, stream):
+        """Allocates outputs for work on `stream` (None: the current one)."""
+        import torch
+        if stream is None:
+            return lambda shape, dtype: torch.empty(shape, dtype=dtype, device=device)
+
+        def new(shape, dtype):
+            with torch.cuda.stream(stream):
+                return torch.empty(shape, dtype=dtype, device=device)
+        return new
+
+    def token_logprobs(self, logits, targets=None, top_k: int = 0, temperature: float = 1.0, V: int | None = None,
+                       stream=None) -> TokenLogprobs:
+        """estp_token_logprobs on logits [rows, >= V]: ln p of `targets` (int32 [rows], negative: none),
+        the entropy, what the gradient needs, and the top_k greatest alternatives."""
+        import torch
+        rows, V, ld = self._logits(logits, V)
+        self._here(logits=logits, targets=targets)
+        if targets is not None:
+            _like(targets, torch.int32, (rows,), "targets")
+        f32, new = torch.float32, self._new(logits.device, stream)
+        lp = None if targets is None else new((rows,), f32)
+        entropy, norm = new((rows,), f32), new((rows, 2), f32)
+        ids, tops = (new((rows, top_k), torch.int32), new((rows, top_k), f32)) if top_k > 0 else (None, None)
+        self._check(self._lib.estp_token_logprobs(
+            self._h, logits.data_ptr(), _dtype(logits), rows, V, ld, _ptr(targets), temperature, top_k, _ptr(lp),
+            entropy.data_ptr(), norm.data_ptr(), _ptr(ids), _ptr(tops), _stream(stream)))
+        return TokenLogprobs(lp, entropy, norm, ids, tops, temperature)
+
+    def token_logprobs_grad(self, logits, targets, lp: TokenLogprobs, grad_logprob=None, grad_entropy=None,
+                            grad_lse=None, grad_top=None, V: int | None = None, out=None, stream=None):
+        """estp_token_logprobs_grad: the gradient of the logits [rows, V], of the fields of `lp` (from
+        token_logprobs on the same logits and targets) with the upstream gradients grad_logprob,
+        grad_entropy, grad_lse [rows] and grad_top [rows, top_k].  out: where it goes, logits itself allowed."""
+        import torch
+        rows, V, ld = self._logits(logits, V)
+        self._here(logits=logits, targets=targets, norm=lp.norm, entropy=lp.entropy, top_ids=lp.top_ids, out=out,
+                   grad_logprob=grad_logprob, grad_entropy=grad_entropy, grad_lse=grad_lse, grad_top=grad_top)
+        f32, k = torch.float32, 0
+        _like(lp.norm, f32, (rows, 2), "norm")
+        if targets is not None:
+            _like(targets, torch.int32, (rows,), "targets")
+        _like(grad_logprob, f32, (rows,), "grad_logprob")
+        _like(grad_lse, f32, (rows,), "grad_lse")
+        if grad_entropy is not None:
+            _like(grad_entropy, f32, (rows,), "grad_entropy")
+            _like(lp.entropy, f32, (rows,), "entropy")
+        if grad_top is not None:
+            if lp.top_ids is None:
+                raise ValueError("grad_top needs the alternatives that it belongs to")
+            k = lp.top_ids.shape[1]
+            _like(lp.top_ids, torch.int32, (rows, k), "top_ids")
+            _like(grad_top, f32, (rows, k), "grad_top")
+        out, ldo = self._grad_like(logits, V, out, self._new(logits.device, stream))
+        self._check(self._lib.estp_token_logprobs_grad(
+            self._h, logits.data_ptr(), _dtype(logits), rows, V, ld, lp.norm.data_ptr(), _ptr(lp.entropy),
+            _ptr(targets), lp.temperature, k, _ptr(lp.top_ids), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(grad_lse),
+            _ptr(grad_top), out.data_ptr(), ldo, _stream(stream)))
+        return out
+
+    def distill_loss(self, logits, teacher_ids, teacher_logits, temperature: float = 1.0, tail: bool = False,
+                     row_weight=None, grads: bool = True, V: int | None = None, out=None, stream=None):
+        """estp_distill_loss: the divergence of the student's logits [rows, >= V] from the teacher's top
+        tokens (teacher_ids int32, teacher_logits fp32 [rows, K]): the loss [rows] and, with grads, its
+        gradient [rows, V] times row_weight [rows].  tail: teacher_logits are log probabilities
+        at this temperature and the rest of the vocabulary is one bucket.  out: where the
+        gradient goes, logits itself allowed."""
+        import torch
+        rows, V, ld = self._logits(logits, V)
+        self._here(logits=logits, teacher_ids=teacher_ids, teacher_logits=teacher_logits, row_weight=row_weight, out=out)
+        K = teacher_ids.shape[-1]
+        _like(teacher_ids, torch.int32, (rows, K), "teacher_ids")
+        _like(teacher_logits, torch.float32, (rows, K), "teacher_logits")
+        if row_weight is not None:
+            _like(row_weight, torch.float32, (rows,), "row_weight")
+        new = self._new(logits.device, stream)
+        loss, gp, ldo = new((rows,), torch.float32), None, 0
+        if grads:
+            out, ldo = self._grad_like(logits, V, out, new)
+            gp = out.data_ptr()
+        self._check(self._lib.estp_distill_loss(
+            self._h, logits.data_ptr(), _dtype(logits), rows, V, ld, teacher_ids.data_ptr(), teacher_logits.data_ptr(),
+            K, temperature, 1 if tail else 0, _ptr(row_weight), loss.data_ptr(), gp, ldo, _stream(stream)))
+        return (loss, out) if grads else loss

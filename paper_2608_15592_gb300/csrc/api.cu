@@ -8,6 +8,7 @@
 #include "cache.cuh"
 #include "estp_internal.cuh"
 #include "tcgen05.cuh"
+#include "vocab.cuh"
 
 namespace estp {
 
@@ -117,6 +118,16 @@ estp_status estp_create(estp_ctx** out, int device) {
     e = cudaMalloc(&ctx->status, 256);
     if (e == cudaSuccess) e = cudaMemset(ctx->status, 0, 256);
     if (e != cudaSuccess) { cudaFree(ctx->status); delete ctx; return cuda_fail(e, "status word"); }
+    // the log probability kernels' parts and lists: a bound of what any call needs (7.7 MB), so that no
+    // call allocates and a captured one keeps its buffers whatever comes after it
+    const size_t slots = 2 * (size_t)ctx->num_sms * kVocabBlocks * (kVocabThreads / 32);
+    e = cudaMalloc(&ctx->vocab_part, slots * (sizeof(float4) + kMaxAlternatives * sizeof(uint64_t)));
+    if (e != cudaSuccess) {
+        cudaFree(ctx->status);
+        delete ctx;
+        return cuda_fail(e, "log probability workspace");
+    }
+    ctx->vocab_lists = reinterpret_cast<uint64_t*>(ctx->vocab_part + slots);
     ctx->done = reinterpret_cast<uint32_t*>(ctx->status) + 32;
     ctx->timed_out = ctx->status + 48;
     *out = ctx;
@@ -130,6 +141,7 @@ void estp_destroy(estp_ctx* ctx) {
     cudaFree(ctx->ws);
     cudaFree(ctx->imp_acc);
     cudaFree(ctx->pool_done);
+    cudaFree(ctx->vocab_part);
     cudaFree(ctx->status);
     delete ctx;
 }
@@ -160,7 +172,8 @@ estp_status estp_sync_status(estp_ctx* ctx, estp_stream_t stream) {
         case ESTP_OK: return ESTP_OK;
         case ESTP_ERR_INVALID_ARG:
             return fail(ESTP_ERR_INVALID_ARG,
-                        "device check failed: cu_seqlens or max_seqlen, or a cache's lengths or page table");
+                        "device check failed: cu_seqlens or max_seqlen, a cache's lengths or page table, or a "
+                        "token id");
         case ESTP_ERR_TIMEOUT: return fail(ESTP_ERR_TIMEOUT, "a device-side wait timed out");
         default: return fail((estp_status)code, "device status %d", code);
     }
@@ -184,6 +197,96 @@ estp_status estp_token_entropy(estp_ctx* ctx, const void* logits, estp_dtype dty
     if (st != ESTP_OK) return st;
     return launch_entropy(ctx, logits, dtype, n_rows, V, ld, cu_seqlens, B, entropy_out,
                           reinterpret_cast<cudaStream_t>(stream));
+}
+
+// What the calls on rows of logits check alike.  grad: NULL, or where a gradient of the logits goes.
+static estp_status check_vocab(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                               int64_t ld, float temperature, const void* grad, int64_t ld_grad) {
+    if (!ctx) return fail(ESTP_ERR_INVALID_ARG, "ctx is NULL");
+    if (dtype != ESTP_F32 && dtype != ESTP_BF16) return fail(ESTP_ERR_INVALID_ARG, "dtype");
+    if (n_rows < 0 || V < 1 || ld < V)
+        return fail(ESTP_ERR_INVALID_ARG, "need n_rows >= 0, V >= 1, ld >= V");
+    if (V > kMaxVocab) return fail(ESTP_ERR_UNSUPPORTED, "V exceeds 2^30");
+    if (n_rows > INT32_MAX || ld > (int64_t(1) << 40)) return fail(ESTP_ERR_UNSUPPORTED, "n_rows or ld");
+    if (!(temperature >= kMinTemperature) || !std::isfinite(temperature))
+        return fail(ESTP_ERR_INVALID_ARG, "temperature must be finite and at least 1e-6");
+    if (n_rows == 0) return ESTP_OK;
+    if (!logits) return fail(ESTP_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (!aligned16(logits) || (ld * esize(dtype)) % 16)
+        return fail(ESTP_ERR_INVALID_ARG, "logits base and row stride must be 16-byte aligned");
+    if (grad) {
+        if (ld_grad < V || ld_grad > (int64_t(1) << 40)) return fail(ESTP_ERR_INVALID_ARG, "need ld_grad >= V");
+        if (!aligned16(grad) || (ld_grad * esize(dtype)) % 16)
+            return fail(ESTP_ERR_INVALID_ARG, "grad_logits base and row stride must be 16-byte aligned");
+        const char *z = static_cast<const char*>(logits), *g = static_cast<const char*>(grad);
+        const int64_t zn = ((n_rows - 1) * ld + V) * esize(dtype), gn = ((n_rows - 1) * ld_grad + V) * esize(dtype);
+        if (z < g + gn && g < z + zn && !(z == g && (ld == ld_grad || n_rows == 1)))
+            return fail(ESTP_ERR_INVALID_ARG, "grad_logits is the logits themselves or does not overlap them");
+    }
+    return ESTP_OK;
+}
+
+estp_status estp_token_logprobs(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                                int64_t ld, const int32_t* targets, float temperature, int32_t top_k,
+                                float* logprob_out, float* entropy_out, float* norm_out, int32_t* top_ids_out,
+                                float* top_logprobs_out, estp_stream_t stream) {
+    ESTP_NVTX_RANGE("estp_token_logprobs");
+    estp_status st = check_vocab(ctx, logits, dtype, n_rows, V, ld, temperature, nullptr, 0);
+    if (st != ESTP_OK) return st;
+    if (top_k < 0 || top_k > V) return fail(ESTP_ERR_INVALID_ARG, "top_k must be in 0..V");
+    if (top_k > kMaxAlternatives) return fail(ESTP_ERR_UNSUPPORTED, "top_k %d (at most %d)", top_k, kMaxAlternatives);
+    if (n_rows == 0) return ESTP_OK;
+    if (logprob_out && !targets) return fail(ESTP_ERR_INVALID_ARG, "log probabilities need targets");
+    if (top_k > 0 && !top_ids_out) return fail(ESTP_ERR_INVALID_ARG, "top_ids_out is NULL");
+    if (reinterpret_cast<uintptr_t>(norm_out) & 7) return fail(ESTP_ERR_INVALID_ARG, "norm_out must be 8-byte aligned");
+    st = set_device(ctx);
+    if (st != ESTP_OK) return st;
+    return launch_token_logprobs(ctx, logits, dtype, n_rows, V, ld, targets, temperature, top_k, logprob_out,
+                                 entropy_out, norm_out, top_ids_out, top_logprobs_out,
+                                 reinterpret_cast<cudaStream_t>(stream));
+}
+
+estp_status estp_token_logprobs_grad(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                                     int64_t ld, const float* norm, const float* entropy, const int32_t* targets,
+                                     float temperature, int32_t top_k, const int32_t* top_ids,
+                                     const float* grad_logprob, const float* grad_entropy, const float* grad_lse,
+                                     const float* grad_top, void* grad_logits, int64_t ld_grad,
+                                     estp_stream_t stream) {
+    ESTP_NVTX_RANGE("estp_token_logprobs_grad");
+    estp_status st = check_vocab(ctx, logits, dtype, n_rows, V, ld, temperature, grad_logits, ld_grad);
+    if (st != ESTP_OK) return st;
+    if (grad_top && (top_k < 1 || top_k > V)) return fail(ESTP_ERR_INVALID_ARG, "grad_top needs 1 <= top_k <= V");
+    if (grad_top && top_k > kMaxAlternatives)
+        return fail(ESTP_ERR_UNSUPPORTED, "top_k %d (at most %d)", top_k, kMaxAlternatives);
+    if (n_rows == 0) return ESTP_OK;
+    if (!norm || !grad_logits) return fail(ESTP_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (reinterpret_cast<uintptr_t>(norm) & 7) return fail(ESTP_ERR_INVALID_ARG, "norm must be 8-byte aligned");
+    if (grad_logprob && !targets) return fail(ESTP_ERR_INVALID_ARG, "grad_logprob needs targets");
+    if (grad_entropy && !entropy) return fail(ESTP_ERR_INVALID_ARG, "grad_entropy needs the entropy");
+    if (grad_top && !top_ids) return fail(ESTP_ERR_INVALID_ARG, "grad_top needs top_ids");
+    st = set_device(ctx);
+    if (st != ESTP_OK) return st;
+    return launch_token_logprobs_grad(ctx, logits, dtype, n_rows, V, ld, norm, entropy, targets, temperature,
+                                      top_k, top_ids, grad_logprob, grad_entropy, grad_lse, grad_top, grad_logits,
+                                      ld_grad, reinterpret_cast<cudaStream_t>(stream));
+}
+
+estp_status estp_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                              int64_t ld, const int32_t* teacher_ids, const float* teacher_logits, int32_t K,
+                              float temperature, int tail, const float* row_weight, float* loss_out,
+                              void* grad_logits, int64_t ld_grad, estp_stream_t stream) {
+    ESTP_NVTX_RANGE("estp_distill_loss");
+    estp_status st = check_vocab(ctx, logits, dtype, n_rows, V, ld, temperature, grad_logits, ld_grad);
+    if (st != ESTP_OK) return st;
+    if (K < 1) return fail(ESTP_ERR_INVALID_ARG, "K must be at least 1");
+    if (K > kMaxAlternatives) return fail(ESTP_ERR_UNSUPPORTED, "K %d (at most %d)", K, kMaxAlternatives);
+    if (n_rows == 0) return ESTP_OK;
+    if (!teacher_ids || !teacher_logits || !loss_out) return fail(ESTP_ERR_INVALID_ARG, "NULL tensor pointer");
+    st = set_device(ctx);
+    if (st != ESTP_OK) return st;
+    return launch_distill_loss(ctx, logits, dtype, n_rows, V, ld, teacher_ids, teacher_logits, K, temperature,
+                               tail != 0, row_weight, loss_out, grad_logits, ld_grad,
+                               reinterpret_cast<cudaStream_t>(stream));
 }
 
 static estp_status check_attn(estp_ctx* ctx, const void* Q, const void* K, estp_dtype dtype,

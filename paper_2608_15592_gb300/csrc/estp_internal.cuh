@@ -31,6 +31,8 @@ struct estp_ctx {
     uint32_t imp_flags = 0;     // flags of the opening call (divisor variant, self term)
     uint32_t* pool_done = nullptr;      // per-prompt arrival counters of the pooling kernel
     int32_t pool_done_cap = 0;
+    float4* vocab_part = nullptr;    // parts of rows cut between warps, two a piece (log probabilities)
+    uint64_t* vocab_lists = nullptr; // and their lists of alternatives; a fixed size, from estp_create on
     uint32_t smem_set = 0;      // cache kernels whose shared memory limit is set on the device, a bit each
     // limit of the attention kernels' abortable waits (estp_set_wait_limit)
     long long wait_cycles = kWaitCycles;
@@ -166,6 +168,19 @@ estp_status launch_attn_forward(estp_ctx* ctx, const void* Q, const void* K, con
 estp_status launch_importance_finalize(estp_ctx* ctx, const float* acc, const int32_t* cu, int B,
                                        int64_t sumT, int n_layers, int n_heads, uint32_t flags,
                                        float* out, cudaStream_t st);
+
+estp_status launch_token_logprobs(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                                  int64_t ld, const int32_t* targets, float T, int top_k, float* logprob,
+                                  float* entropy, float* norm, int32_t* top_ids, float* top_logprobs,
+                                  cudaStream_t st);
+estp_status launch_token_logprobs_grad(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                                       int64_t ld, const float* norm, const float* entropy, const int32_t* targets,
+                                       float T, int top_k, const int32_t* top_ids, const float* g_logprob,
+                                       const float* g_entropy, const float* g_lse, const float* g_top, void* out,
+                                       int64_t ld_out, cudaStream_t st);
+estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
+                                int64_t ld, const int32_t* ids, const float* teacher, int K, float T, bool tail,
+                                const float* weight, float* loss, void* out, int64_t ld_out, cudaStream_t st);
 
 estp_status launch_pool(estp_ctx* ctx, const void* hidden, estp_dtype dtype, int64_t D,
                         int64_t ldh, const float* H, const float* S, const int32_t* cu, int B,
