@@ -468,7 +468,7 @@ estp_status estp_cache_evict(estp_ctx* ctx, const estp_kv_cache* cache, const in
  * entropy.  For row r of logits z and a temperature T > 0 (at least 1e-6),
  *   lse = ln sum_v exp(z_v / T),  ln p_v = z_v / T - lse.
  * The calls of this group take logits [n_rows, ld] of ESTP_BF16 or ESTP_F32 as estp_token_entropy
- * does, of which the first V <= 2^30 columns are read.  Unlike there, a logit may be -inf (a masked
+ * does, of which the first V <= 2^26 columns are read.  Unlike there, a logit may be -inf (a masked
  * token, p = 0), or the type's lowest value.  A row of -inf alone has ln p = -inf, entropy 0 and
  * gradients of 0.  A row that holds NaN or +inf gives NaN.  Sums are held in fp32.
  * Their scratch has a fixed size and comes with the context: they allocate nothing, a first call may

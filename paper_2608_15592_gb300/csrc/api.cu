@@ -206,7 +206,7 @@ static estp_status check_vocab(estp_ctx* ctx, const void* logits, estp_dtype dty
     if (dtype != ESTP_F32 && dtype != ESTP_BF16) return fail(ESTP_ERR_INVALID_ARG, "dtype");
     if (n_rows < 0 || V < 1 || ld < V)
         return fail(ESTP_ERR_INVALID_ARG, "need n_rows >= 0, V >= 1, ld >= V");
-    if (V > kMaxVocab) return fail(ESTP_ERR_UNSUPPORTED, "V exceeds 2^30");
+    if (V > kMaxVocab) return fail(ESTP_ERR_UNSUPPORTED, "V exceeds 2^26");
     if (n_rows > INT32_MAX || ld > (int64_t(1) << 40)) return fail(ESTP_ERR_UNSUPPORTED, "n_rows or ld");
     if (!(temperature >= kMinTemperature) || !std::isfinite(temperature))
         return fail(ESTP_ERR_INVALID_ARG, "temperature must be finite and at least 1e-6");

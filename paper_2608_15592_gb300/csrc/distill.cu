@@ -10,17 +10,14 @@
 // where the named tokens hold nearly everything; the sum has a maximum of its own, so it does not
 // underflow beside a named token far above.
 //
-// A block takes a row: named units are marked in a bitmap, the statistics are taken in a first pass,
-// one warp forms the loss and the row's factors, and the gradient is written in a second pass,
-// whose reads come from L2.
+// Bound: the gradient needs the row's sum before its first element, so a row is either read twice or
+// kept.  Here it is kept: a cluster of C CTAs takes a row, each a slice that fits its shared memory
+// beside those of the other CTAs of the SM, so logits are read once and the gradient is written once.
 #include "vocab.cuh"
 
 namespace estp {
 namespace {
 
-constexpr int kDistillThreads = 512;
-constexpr int kDistillWarps = kDistillThreads / 32;
-constexpr int kSpanUnits = 1 << 16;  // units of a row that the bitmap covers at a time (8 KB)
 constexpr int kK = kMaxAlternatives;
 
 struct DistillArgs {
@@ -39,154 +36,282 @@ struct DistillArgs {
     int* status;
 };
 
-struct DistillShared {
-    uint32_t bits[kSpanUnits / 32];
-    int32_t id[kK];
-    float lq[kK], q[kK], z[kK], fix[kK];  // ln q, q, the student's logit, the gradient
-    RowStat part[kDistillWarps];
-    float A, pivot, Q, rest;
-    int some;
+// The teacher's side of a row, which its logits have no part in but for those of the named tokens.
+struct Teacher {
+    int32_t id[kK];            // -1: none
+    float lq[kK], q[kK], z[kK];  // ln q, q, the student's logit
+    RowStat in;                // with the tail: statistics of the named tokens
+    float Q, rest, g;          // g = row weight / T
+    int some, repeated;        // has entries; has a token twice
 };
 
-template <class F>
-__device__ __forceinline__ float warp_reduce(float x, F f) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) x = f(x, __shfl_xor_sync(0xffffffffu, x, off));
-    return x;
-}
+// What every element of a row's gradient takes from its sums.
+struct Factors {
+    float m, s;      // maximum and sum of all tokens
+    float pivot, A;  // an element that is not named: A 2^((z - pivot) c)
+    float M, near;   // where pivot has a near frame: near 2^(z c - M)
+    bool framed;
+    float rest;
+    bool empty, zero;
+};
+
 __device__ __forceinline__ float warp_sum(float x) {
-    return warp_reduce(x, [](float a, float b) { return a + b; });
-}
-__device__ __forceinline__ double warp_sum(double x) {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
     return x;
 }
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+    return x;
+}
 
-// The teacher's side of a row (one warp): q and ln q of the named tokens, the rest, and the student's
-// logits there.
-template <bool kBf16>
-__device__ void teacher_row(const DistillArgs& a, int64_t r, DistillShared& s) {
+// A row's entries, four a lane (entry 32 i + lane), on their way into Teacher: tokens and values first, then the
+// student's logits, which need the tokens' addresses.  Each is asked for a row before it is used.
+constexpr int kPer = kK / 32;
+struct Entries {
+    int32_t id[kPer];
+    uint32_t z[kPer];  // bits as loaded: a conversion would wait for them
+    float x[kPer], w;
+    bool repeated;
+};
+
+// What a row's entries are copied to first (asked for two rows ahead).
+struct Asked {
+    int32_t id[kK];
+    float x[kK], w;
+};
+
+__device__ __forceinline__ void copy_word(void* to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+__device__ __forceinline__ void ask_entries(const DistillArgs& a, int64_t r, Asked& q) {
+    if (r >= a.n_rows) return;
     const int lane = threadIdx.x & 31;
-    const char* row = a.base + r * a.ld_bytes;
-    float x[kK / 32], top = -INFINITY;
-    bool some = false;
-#pragma unroll
-    for (int i = 0; i < kK / 32; ++i) {
-        const int j = i * 32 + lane;
-        x[i] = -INFINITY;
-        if (j < a.K && s.id[j] >= 0) {
-            x[i] = a.teacher[r * a.K + j];
-            s.z[j] = logit_at<kBf16>(row, s.id[j]);
-            some = true;
-        }
-        top = fmaxf(top, x[i]);
+    for (int j = lane; j < a.K; j += 32) {
+        const int64_t at = r * a.K + j;
+        if (!in_bounds(at < a.n_rows * a.K, a.status)) continue;
+        copy_word(&q.id[j], a.ids + at);
+        copy_word(&q.x[j], a.teacher + at);
     }
-    float Q, rest = 0.f;
-    some = __any_sync(0xffffffffu, some);
-    if (a.tail) {
-        double sum = 0.;
+    if (lane == 0 && a.weight) copy_word(&q.w, a.weight + r);
+}
+
+__device__ __forceinline__ void take_entries(const DistillArgs& a, const Asked& q, Entries& e) {
+    const int lane = threadIdx.x & 31;
+    copies_done();
+    __syncwarp();
+    e.w = a.weight ? q.w : 1.f;
 #pragma unroll
-        for (int i = 0; i < kK / 32; ++i) {
-            const int j = i * 32 + lane;
-            const float q = expf(x[i]);
-            sum += (double)q;
-            if (j < a.K) {
-                s.q[j] = q;
-                s.lq[j] = x[i];
+    for (int i = 0; i < kPer; ++i) {
+        const int j = i * 32 + lane;
+        e.id[i] = j < a.K ? q.id[j] : -1;
+        e.x[i] = j < a.K ? q.x[j] : -INFINITY;
+    }
+    __syncwarp();
+}
+
+// Tokens outside of the vocabulary are left out; repeated ones are found by a table of kSlots places with linear
+// probing, empty (-1) before and after.  Then the logits are asked for.
+constexpr int kSlots = 512;
+template <bool kBf16>
+__device__ __forceinline__ void check_entries(const DistillArgs& a, int64_t r, Entries& e, int32_t* table) {
+    const int lane = threadIdx.x & 31;
+    uint32_t slot[kPer];
+    int old[kPer];
+    bool bad = false, again = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if (e.id[i] >= a.V) {
+            bad = true;
+            e.id[i] = -1;
+        }
+        slot[i] = (uint32_t)e.id[i] * 2654435761u >> 23;
+        old[i] = e.id[i] >= 0 ? atomicCAS(&table[slot[i]], -1, e.id[i]) : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        for (int tries = 1; tries < kSlots && old[i] != -1 && old[i] != e.id[i]; ++tries) {
+            slot[i] = (slot[i] + 1) % kSlots;
+            old[i] = atomicCAS(&table[slot[i]], -1, e.id[i]);
+        }
+        again |= e.id[i] >= 0 && old[i] == e.id[i];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (e.id[i] >= 0) table[slot[i]] = -1;
+    e.repeated = __any_sync(0xffffffffu, again);
+    if (e.repeated && a.tail) {  // a token has one probability: but for its first entry it is left out
+        uint32_t out = 0;
+        for (int k = 0; k < a.K; ++k) {
+            int o = -1;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int of = __shfl_sync(0xffffffffu, e.id[i], k & 31);
+                if (i == k >> 5) o = of;
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (k < i * 32 + lane && o == e.id[i] && o >= 0) out |= 1u << i;
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (out >> i & 1) e.id[i] = -1;
+        bad = true;
+    }
+    if (bad) report(a.status, ESTP_ERR_INVALID_ARG);
+    const char* row = a.base + r * a.ld_bytes;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        e.z[i] = kBf16 ? 0xFF80u : 0xFF800000u;
+        if (e.id[i] >= 0)
+            e.z[i] = kBf16 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[e.id[i]] : reinterpret_cast<const uint32_t*>(row)[e.id[i]];
+        if (e.id[i] < 0) e.x[i] = -INFINITY;
+    }
+    __syncwarp();
+}
+
+template <bool kBf16>
+__device__ __forceinline__ void put_entries(const DistillArgs& a, const Entries& e, Teacher& t) {
+    const int lane = threadIdx.x & 31;
+    float z[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) z[i] = __uint_as_float(kBf16 ? e.z[i] << 16 : e.z[i]);
+    bool some = false;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        some |= e.id[i] >= 0;
+        top = fmaxf(top, e.x[i]);
+    }
+    some = __any_sync(0xffffffffu, some);
+    float Q, rest = 0.f, q[kPer], lq[kPer];
+    if (a.tail) {
+        // 1 - sum q in 64 bits: each q is a rounded exponential, but their sum adds no error
+        double sum = 0.;
+        RowStat in = no_stat();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            lq[i] = e.x[i];
+            q[i] = 0.f;
+            if (i * 32 < a.K) {
+                q[i] = expf(e.x[i]);
+                sum += (double)q[i];
+                const bool bad = isnan(z[i]) || z[i] == INFINITY;
+                if (e.id[i] >= 0) join(in, RowStat{z[i], bad ? NAN : z[i] == -INFINITY ? 0.f : 1.f, 0.f}, a.c);
             }
         }
-        sum = warp_sum(sum);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
         Q = (float)sum;
         rest = !some || sum > 1. ? 0.f : (float)(1. - sum);
+        join_lanes<false>(in, a.c);
+        t.in = in;
     } else {
-        top = pivot(warp_reduce(top, [](float p, float q) { return fmaxf(p, q); }));
-        float e[kK / 32], sum = 0.f;
+        top = pivot(warp_max(top));
+        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < kK / 32; ++i) {
-            e[i] = expf((x[i] - top) / a.T);
-            sum += e[i];
+        for (int i = 0; i < kPer; ++i) {
+            lq[i] = q[i] = 0.f;
+            if (i * 32 < a.K) {
+                lq[i] = (e.x[i] - top) / a.T;
+                q[i] = expf(lq[i]);
+                sum += q[i];
+            }
         }
         sum = warp_sum(sum);
-        const bool none = sum == 0.f;  // every entry of -inf: no teacher
+        const bool none = sum == 0.f;  // no entry, or only such of -inf
         const float l = none ? 0.f : logf(sum);
 #pragma unroll
-        for (int i = 0; i < kK / 32; ++i) {
-            const int j = i * 32 + lane;
-            if (j < a.K) {
-                s.q[j] = none ? 0.f : e[i] / sum;
-                s.lq[j] = (x[i] - top) / a.T - l;
-            }
+        for (int i = 0; i < kPer; ++i) {
+            q[i] = none ? 0.f : q[i] / sum;
+            lq[i] -= l;
         }
         Q = none ? 0.f : 1.f;
         some = !none;
     }
-    if (lane == 0) {
-        s.Q = Q;
-        s.rest = rest;
-        s.some = some;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int j = i * 32 + lane;
+        t.id[j] = e.id[i];
+        t.q[j] = q[i];
+        t.lq[j] = lq[i];
+        t.z[j] = z[i];
     }
+    if (lane == 0) {
+        t.Q = Q;
+        t.rest = rest;
+        t.some = some;
+        t.repeated = e.repeated;
+        t.g = e.w / a.T;
+    }
+    __syncwarp();
 }
 
-// The loss and the row's factors (one warp), from the statistics `st` of every token, or with the tail
-// of the tokens that are not named.
-__device__ void finish_row(const DistillArgs& a, int64_t r, DistillShared& s, const RowStat& st, float g) {
-    const int lane = threadIdx.x & 31;
-    const float Q = s.Q;
-    float rest = s.rest;
-    // Where the student has no other token, what the teacher leaves to them may be the rounding of its log
-    // probabilities: sum q_j |x_j| 2^-24 + 2^-23 at most, below 2^-20 for the entropies that 128 tokens have.
-    const bool no_other = st.s == 0.f;
-    if (a.tail && no_other && rest <= 0x1p-20f) rest = 0.f;
+// From the statistics `st` of every token, or with the tail of those that are not named.
+__device__ __forceinline__ Factors row_factors(const DistillArgs& a, const Teacher& t, const RowStat& st) {
+    Factors f;
     RowStat all = st;
+    if (a.tail) join(all, t.in, a.c);
+    f.m = pivot(all.m);
+    f.s = all.s;
+    f.empty = all.s == 0.f;
+    f.zero = !t.some || t.g == 0.f;
+    f.pivot = f.m;
+    f.A = f.empty ? 0.f : t.g * t.Q / all.s;
+    f.rest = t.rest;
     if (a.tail) {
-        RowStat in = no_stat();
-#pragma unroll
-        for (int i = 0; i < kK / 32; ++i) {
-            const int j = i * 32 + lane;
-            if (j < a.K && s.id[j] >= 0) join(in, RowStat{s.z[j], isnan(s.z[j]) || s.z[j] == INFINITY ? NAN : s.z[j] == -INFINITY ? 0.f : 1.f, 0.f}, a.c);
-        }
-        join_lanes(in, a.c);
-        join(all, in, a.c);
+        // Where the student has no other token, what the teacher leaves to them may be the rounding of its log
+        // probabilities: sum q_j |x_j| 2^-24 + 2^-23 at most, below 2^-20 for the entropies that 128 tokens have.
+        const bool no_other = st.s == 0.f;
+        if (no_other && f.rest <= 0x1p-20f) f.rest = 0.f;
+        // the exponentials of these elements are taken against the maximum that their own sum belongs to
+        f.pivot = pivot(st.m);
+        f.A = no_other || f.empty
+                  ? 0.f
+                  : t.g * ((t.Q + f.rest) * ex2(max_nan((f.pivot - f.m) * a.c, kCut)) / all.s - f.rest / st.s);
     }
-    const bool empty = all.s == 0.f;
-    const float m = pivot(all.m), ls = empty ? -INFINITY : logf(all.s);
+    f.M = f.pivot * a.c;
+    f.framed = near_frame(f.M);
+    f.near = f.A * ex2(-frame_off(f.pivot, a.c));
+    return f;
+}
+
+// One warp.
+__device__ __forceinline__ float row_loss(const DistillArgs& a, const Teacher& t, const RowStat& st, const Factors& f) {
+    const int lane = threadIdx.x & 31;
+    if (!t.some) return 0.f;
+    const float ls = f.empty ? -INFINITY : logf(f.s);
     float loss = 0.f;
-#pragma unroll
-    for (int i = 0; i < kK / 32; ++i) {
-        const int j = i * 32 + lane;
-        if (j < a.K && s.id[j] >= 0) {
-            const float q = s.q[j], lp = empty ? -INFINITY : (s.z[j] - m) / a.T - ls;
-            // q first: beside a logit of the type's lowest value ln p may exceed fp32 where the loss does not
-            if (q != 0.f) loss += empty ? INFINITY : q * (s.lq[j] + ls) + q * (m - s.z[j]) / a.T;
-            if (a.tail) s.fix[j] = empty ? 0.f : g * ((Q + rest) * expf(lp) - q);
-            else s.fix[j] = empty ? 0.f : -g * q;
-        }
+    for (int j = lane; j < a.K; j += 32) {
+        const float q = t.q[j];
+        // q first: beside a logit of the type's lowest value ln p may exceed fp32 where the loss does not
+        if (t.id[j] >= 0 && q != 0.f) loss += f.empty ? INFINITY : q * (t.lq[j] + ls) + q * (f.m - t.z[j]) / a.T;
     }
     loss = warp_sum(loss);
-    // the exponentials of the second pass are taken against the maximum that its sums belong to
-    float A = empty ? 0.f : g * (Q + rest) / all.s;
-    if (a.tail) {
-        const float mo = pivot(st.m);
-        if (rest != 0.f) loss += rest * (logf(rest) - (no_other || empty ? -INFINITY : (mo - m) / a.T + (logf(st.s) - ls)));
-        A = no_other || empty ? 0.f : g * ((Q + rest) * ex2(max_nan((mo - m) * a.c, kCut)) / all.s - rest / st.s);
-        if (lane == 0) s.pivot = mo;
-    } else if (lane == 0) {
-        s.pivot = m;
-    }
-    if (lane == 0) {
-        s.A = A;
-        a.loss[r] = s.some ? loss : 0.f;
-    }
+    if (f.rest != 0.f)
+        loss += f.rest * (logf(f.rest) - (st.s == 0.f ? -INFINITY : (f.pivot - f.m) / a.T + (logf(st.s) - ls)));
+    return loss;
 }
 
-// Calls f(j) in every lane for each named token j of the unit that lane `f_lane` holds.
+// The gradient at a named token, given what it would be were it not one.
+__device__ __forceinline__ float named_grad(const DistillArgs& a, const Teacher& t, const Factors& f, int j, float x) {
+    if (f.empty) return 0.f;
+    if (!a.tail) return x - t.g * t.q[j];
+    const float p = ex2(max_nan((t.z[j] - f.m) * a.c, kCut)) / f.s;
+    return t.g * ((t.Q + f.rest) * p - t.q[j]);
+}
+
+// Calls f(j) in every lane for each token j of a unit.
 template <class F>
-__device__ __forceinline__ void each_named(const DistillShared& s, int K, int per, int unit, F f) {
+__device__ __forceinline__ void each_named(const Teacher& t, int K, int per, int unit, F f) {
     const int lane = threadIdx.x & 31;
     for (int i0 = 0; i0 < K; i0 += 32) {
         const int i = i0 + lane;
-        const int id = i < K ? s.id[i] : -1;
+        const int id = i < K ? t.id[i] : -1;
         uint32_t hit = __ballot_sync(0xffffffffu, id >= 0 && id / per == unit);
         while (hit) {
             const int j = i0 + __ffs(hit) - 1;
@@ -196,101 +321,328 @@ __device__ __forceinline__ void each_named(const DistillShared& s, int K, int pe
     }
 }
 
+// Named tokens among a warp's 32 units from `unit` on become -inf; `lanes` marks the units.
 template <bool kBf16>
-__device__ __forceinline__ void mask_element(uint4& v, int at) {
+__device__ __forceinline__ void mask_named(const Teacher& t, int K, uint32_t lanes, int unit, uint4& v) {
+    constexpr int per = kBf16 ? 8 : 4;
+    const int lane = threadIdx.x & 31;
     uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+    while (lanes) {
+        const int l = __ffs(lanes) - 1;
+        lanes &= lanes - 1;
+        each_named(t, K, per, unit + l, [&](int j) {
+            const int at = t.id[j] - (unit + l) * per;
 #pragma unroll
-    for (int e = 0; e < (kBf16 ? 8 : 4); ++e)
-        if (e == at) {
-            if (!kBf16) w[e] = 0xFF800000u;
-            else if (e & 1) w[e >> 1] = (w[e >> 1] & 0x0000FFFFu) | 0xFF800000u;
-            else w[e >> 1] = (w[e >> 1] & 0xFFFF0000u) | 0x0000FF80u;
-        }
-}
-
-// Marks (or clears) the units of [span, span + kSpanUnits) that hold a named token.
-__device__ __forceinline__ void mark(const DistillArgs& a, DistillShared& s, int per, int span, bool set) {
-    for (int j = threadIdx.x; j < a.K; j += kDistillThreads) {
-        const unsigned k = (unsigned)(s.id[j] / per - span);
-        if (s.id[j] >= 0 && k < (unsigned)kSpanUnits) {
-            if (set) atomicOr(&s.bits[k >> 5], 1u << (k & 31));
-            else s.bits[k >> 5] = 0;
-        }
+            for (int e = 0; e < per; ++e)
+                if (lane == l && e == at) {
+                    if (!kBf16) w[e] = 0xFF800000u;
+                    else if (e & 1) w[e >> 1] = (w[e >> 1] & 0x0000FFFFu) | 0xFF800000u;
+                    else w[e >> 1] = (w[e >> 1] & 0xFFFF0000u) | 0x0000FF80u;
+                }
+        });
     }
 }
 
-template <bool kBf16>
-__device__ __forceinline__ void store_row_unit(char* row, int c, int V, const float (&x)[8]) {
-    constexpr int per = kBf16 ? 8 : 4;
-    char* p = row + (int64_t)c * 16;
-    if (V - c * per >= per) {
-        uint4 o;
-        if (kBf16) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(&o);
+template <bool kBf16, bool kFramed>
+__device__ __forceinline__ void other_grad(const Factors& f, const uint4& v, float c, float (&x)[8]) {
+    const float2 c2 = make_float2(c, c);
+    const float2 off = kFramed ? make_float2(-f.M, -f.M) : make_float2(-f.pivot, -f.pivot);
+    const float2 A2 = kFramed ? make_float2(f.near, f.near) : make_float2(f.A, f.A);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t*>(&b);
-            }
-        } else {
-            o = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-        }
-        __stcs(reinterpret_cast<uint4*>(p), o);
+    for (int i = 0; i < (kBf16 ? 4 : 2); ++i) {
+        const float2 d = kFramed ? __ffma2_rn(pair<kBf16>(v, i), c2, off) : __fmul2_rn(__fadd2_rn(pair<kBf16>(v, i), off), c2);
+        const float2 g = __fmul2_rn(A2, make_float2(ex2(d.x), ex2(d.y)));
+        x[2 * i] = g.x;
+        x[2 * i + 1] = g.y;
+    }
+}
+
+// ------------------------------------------------------------------ rows kept by a cluster
+// Eight warps hold the slice.  A thread copies its own units into shared memory (cp.async), reads them from
+// there twice and, once it has read a unit for the last time, copies the next row's into its place: so the next
+// row is on its way while this one is computed and written, and no barrier stands between a copy
+// and its use.  The ninth warp is a row ahead on the teacher's side (tokens, their logits, q), forms the loss behind
+// the barrier, and puts the named tokens' gradients over what the others wrote there one row later.
+// One cluster barrier a row: before it each warp stores its statistics into every CTA of the cluster,
+// after it every warp joins them for itself.  Up to three CTAs an SM.
+constexpr int kHold = 256;             // threads that hold the slice
+constexpr int kHoldWarps = kHold / 32;
+constexpr int kClusterThreads = kHold + 32;
+constexpr int kMaxCluster = 8;
+constexpr int kSliceBytes = 200 * 1024;  // most of a CTA's dynamic shared memory
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void store_remote(const void* p, uint32_t rank, float x, float y) {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\t"
+        "mapa.shared::cluster.u32 a, %0, %1;\n\t"
+        "st.shared::cluster.v2.f32 [a], {%2, %3};\n\t}" ::"r"((uint32_t)__cvta_generic_to_shared(p)),
+        "r"(rank), "f"(x), "f"(y)
+        : "memory");
+}
+
+__device__ __forceinline__ void copy_unit(uint4* to, const char* from) {
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from)
+                 : "memory");
+}
+// A thread's units of a slice: tid, tid + kHold, .. below n; u0: the slice's first unit.
+struct Slice {
+    uint4* kept;
+    const uint32_t* bits;  // with the tail: units that hold a named token
+    int n, u0;
+};
+
+// N of the thread's units, from `at` on, into the statistics; `next`: the next row's first copied unit, or NULL.
+template <bool kBf16, int N, bool kRefill>
+__device__ __forceinline__ void hold_units(const DistillArgs& a, const Teacher& t, const Slice& s, int at, const char* next,
+                                           LaneStat<false>& st) {
+    constexpr int per = kBf16 ? 8 : 4;
+    const int tid = threadIdx.x, warp = tid >> 5;
+    uint4 v[N];
+    if (at + N * kHold <= min(s.n, a.V / per - s.u0)) {  // whole units all
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = s.kept[at + k * kHold + tid];
     } else {
 #pragma unroll
-        for (int e = 0; e < per; ++e)
-            if (c * per + e < V) {
-                if (kBf16) reinterpret_cast<__nv_bfloat16*>(p)[e] = __float2bfloat16_rn(x[e]);
-                else reinterpret_cast<float*>(p)[e] = x[e];
-            }
+        for (int k = 0; k < N; ++k) {
+            const int c = at + k * kHold + tid, valid = a.V - (s.u0 + c) * per;
+            v[k] = c < s.n ? s.kept[c] : masked_unit<kBf16>();
+            if (valid < per) mask_unit<kBf16>(v[k], valid);
+        }
+    }
+    if (a.tail) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int w = at + k * kHold + warp * 32;  // the warp's units
+            const uint32_t lanes = w < s.n ? s.bits[w >> 5] : 0;
+            if (lanes) mask_named<kBf16>(t, a.K, lanes, s.u0 + w, v[k]);
+        }
+    }
+    st.template add_units<kBf16>(v, units_max<kBf16, N>(v), a.c);
+    if (kRefill && next) {  // (every value has been used)
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (at + k * kHold + tid < s.n) copy_unit(&s.kept[at + k * kHold + tid], next + (int64_t)(at + k * kHold + tid) * 16);
     }
 }
 
-template <bool kBf16>
-__global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillArgs a) {
-    constexpr int per = kBf16 ? 8 : 4, kStep = 32 * kVocabUnroll;
-    __shared__ DistillShared s;
+template <bool kBf16, bool kFramed>
+__device__ __forceinline__ void kept_grad(const DistillArgs& a, const Factors& f, const Slice& s, char* out, const char* next) {
+    constexpr int per = kBf16 ? 8 : 4;
+    const int tid = threadIdx.x, whole = min(s.n, a.V / per - s.u0);
+    int c = tid;
+    for (; c + 3 * kHold < whole; c += 4 * kHold) {
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = s.kept[c + k * kHold];
+        char* p = out + (int64_t)c * 16;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float x[8];
+            other_grad<kBf16, kFramed>(f, v[k], a.c, x);
+            store_whole<kBf16>(p + k * (kHold * 16), x);
+        }
+        if (next) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) copy_unit(&s.kept[c + k * kHold], next + (int64_t)(c + k * kHold) * 16);
+        }
+    }
+    for (; c < s.n; c += kHold) {
+        float x[8];
+        other_grad<kBf16, kFramed>(f, s.kept[c], a.c, x);
+        store_unit<kBf16>(out, c, a.V - s.u0 * per, x);
+        if (next) copy_unit(&s.kept[c], next + (int64_t)c * 16);
+    }
+}
+
+template <bool kBf16, bool kGrad>
+__global__ void __launch_bounds__(kClusterThreads, 3) distill_cluster_kernel(const DistillArgs a, int slice, int C) {
+    constexpr int per = kBf16 ? 8 : 4;
+    extern __shared__ uint4 room[];
+    __shared__ Teacher teachers[3];                         // of three rows: last, this and next
+    __shared__ float2 stats[2][kMaxCluster * kHoldWarps];  // m, s of each warp of the cluster, of two rows
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (int i = tid; i < kSpanUnits / 32; i += kDistillThreads) s.bits[i] = 0;
+    const int rank = blockIdx.x % C, n_clusters = gridDim.x / C, words = (slice + 31) / 32;
+    const int u0 = min(rank * slice, a.nvec), n = min(slice, a.nvec - u0);
+    uint32_t* bits = reinterpret_cast<uint32_t*>(room + slice);  // [3][words]
+    const bool holds = warp < kHoldWarps;
+
+    __shared__ int32_t table[kSlots];
+    __shared__ Asked asked;
+    // the ninth warp: the teacher's side of a row, once its entries and their logits have come
+    auto put = [&](const Entries& e, int k) {
+        uint32_t* b = bits + k * words;
+        if (a.tail) {
+            for (int i = lane; i < words; i += 32) b[i] = 0;
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const unsigned u = (unsigned)(e.id[i] / per - u0);
+                if (e.id[i] >= 0 && u < (unsigned)n) atomicOr(&b[u >> 5], 1u << (u & 31));
+            }
+        }
+        put_entries<kBf16>(a, e, teachers[k]);
+    };
+    // the named tokens of the slice, over what an unnamed one would have there
+    auto put_named = [&](int64_t r, const Teacher& t, const Factors& f) {
+        if (f.zero) return;
+        char* out = a.out + r * a.out_bytes;
+        for (int j0 = 0; j0 < a.K; j0 += 32) {
+            const int j = j0 + lane, id = j < a.K ? t.id[j] : -1;
+            const unsigned u = (unsigned)(id / per - u0);
+            const bool mine = id >= 0 && u < (unsigned)n;
+            float x = 0.f;
+            if (mine) x = a.tail ? 0.f : f.A * ex2(max_nan((t.z[j] - f.pivot) * a.c, kCut));
+            bool first = mine;
+            if (a.tail) {
+                if (mine) x = named_grad(a, t, f, j, 0.f);
+            } else if (!t.repeated) {
+                if (mine) x = named_grad(a, t, f, j, x);
+            } else {
+                // a repeated token counts each time: its first place has the sum
+                for (int k = 0; k < a.K; ++k)
+                    if (mine && t.id[k] == id) {
+                        x = named_grad(a, t, f, k, x);
+                        first &= k >= j;
+                    }
+            }
+            if (first && in_bounds(id < a.V, a.status)) {
+                if (kBf16) reinterpret_cast<__nv_bfloat16*>(out)[id] = __float2bfloat16_rn(x);
+                else reinterpret_cast<float*>(out)[id] = x;
+            }
+        }
+    };
+
+    int64_t r = blockIdx.x / C;
+    Entries e;  // of the next row, with its logits; `asked` is of the one after it
+    if (holds) {
+        if (r < a.n_rows) {
+            const char* from = a.base + r * a.ld_bytes + (int64_t)u0 * 16;
+            for (int c = tid; c < n; c += kHold) copy_unit(&room[c], from + (int64_t)c * 16);
+        }
+    } else if (r < a.n_rows) {
+        for (int i = lane; i < kSlots; i += 32) table[i] = -1;
+        __syncwarp();
+        ask_entries(a, r, asked);
+        take_entries(a, asked, e);
+        ask_entries(a, r + n_clusters, asked);
+        check_entries<kBf16>(a, r, e, table);
+        put(e, 0);
+        if (r + n_clusters < a.n_rows) {
+            take_entries(a, asked, e);
+            ask_entries(a, r + 2 * (int64_t)n_clusters, asked);
+            check_entries<kBf16>(a, r + n_clusters, e, table);
+        }
+    }
+    __syncthreads();
+    Factors f{};
+    for (int i = 0; r < a.n_rows; r += n_clusters, ++i) {
+        const Teacher& t = teachers[i % 3];
+        const Slice s{room, bits + i % 3 * words, n, u0};
+        const int64_t after = r + n_clusters;
+        const char* next = after < a.n_rows ? a.base + after * a.ld_bytes + (int64_t)u0 * 16 : nullptr;
+        float2* mine = stats[i & 1];
+        if (holds) {
+            copies_done();
+            LaneStat<false> st;
+            int at = 0;
+            for (; at + 6 * kHold < n; at += 8 * kHold) hold_units<kBf16, 8, !kGrad>(a, t, s, at, next, st);
+            for (; at < n; at += 2 * kHold) hold_units<kBf16, 2, !kGrad>(a, t, s, at, next, st);
+            RowStat x = st.row(a.c);
+            join_lanes<false>(x, a.c);
+            if (lane < C) store_remote(&mine[rank * kHoldWarps + warp], lane, x.m, x.s);
+        } else if (next) {
+            put(e, (i + 1) % 3);
+            if (after + n_clusters < a.n_rows) {
+                take_entries(a, asked, e);
+                ask_entries(a, after + 2 * (int64_t)n_clusters, asked);
+                check_entries<kBf16>(a, after + n_clusters, e, table);
+            }
+        }
+        __syncwarp();
+        cluster_sync();
+        RowStat st = no_stat();
+        for (int k = lane; k < C * kHoldWarps; k += 32) {
+            if (k < 32) st = RowStat{mine[k].x, mine[k].y, 0.f};
+            else join(st, RowStat{mine[k].x, mine[k].y, 0.f}, a.c);
+        }
+        join_lanes<false>(st, a.c);
+        if (!holds && kGrad && i > 0) put_named(r - n_clusters, teachers[(i + 2) % 3], f);
+        f = row_factors(a, t, st);
+        if (!holds) {
+            if (rank == 0) {
+                const float loss = row_loss(a, t, st, f);
+                if (lane == 0) a.loss[r] = loss;
+            }
+        } else if (kGrad) {
+            char* out = a.out + r * a.out_bytes + (int64_t)u0 * 16;
+            if (f.zero) {
+                const float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                for (int c = tid; c < n; c += kHold) {
+                    store_unit<kBf16>(out, c, a.V - u0 * per, x);
+                    if (next) copy_unit(&room[c], next + (int64_t)c * 16);
+                }
+            } else if (f.framed) {
+                kept_grad<kBf16, true>(a, f, s, out, next);
+            } else {
+                kept_grad<kBf16, false>(a, f, s, out, next);
+            }
+        }
+        __syncwarp();
+    }
+    if (kGrad) {
+        __syncthreads();  // the last row's stores
+        const int rows = (int)((r - blockIdx.x / C) / n_clusters);
+        if (!holds && rows > 0) put_named(r - n_clusters, teachers[(rows - 1) % 3], f);
+    }
+}
+
+// ------------------------------------------------------------------ longer rows
+// A block takes a row in two passes; named units are marked for a span of it at a time.
+constexpr int kLongThreads = 512;
+constexpr int kLongWarps = kLongThreads / 32;
+constexpr int kSpanUnits = 1 << 16;
+
+template <bool kBf16>
+__global__ void __launch_bounds__(kLongThreads) distill_long_kernel(const DistillArgs a) {
+    constexpr int per = kBf16 ? 8 : 4, kStep = 32 * kVocabUnroll;
+    __shared__ Teacher t;
+    __shared__ uint32_t bits[kSpanUnits / 32];
+    __shared__ RowStat part[kLongWarps];
+    __shared__ int32_t table[kSlots];
+    __shared__ Asked asked;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    for (int i = tid; i < kSpanUnits / 32; i += kLongThreads) bits[i] = 0;
+    for (int i = tid; i < kSlots; i += kLongThreads) table[i] = -1;
+    auto mark = [&](int span, bool set) {
+        for (int j = tid; j < a.K; j += kLongThreads) {
+            const unsigned k = (unsigned)(t.id[j] / per - span);
+            if (t.id[j] >= 0 && k < (unsigned)kSpanUnits) {
+                if (set) atomicOr(&bits[k >> 5], 1u << (k & 31));
+                else bits[k >> 5] = 0;
+            }
+        }
+        __syncthreads();
+    };
     for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
-        if (!in_bounds(r >= 0 && a.nvec * (int64_t)per >= a.V, a.status)) return;
         const char* row = a.base + r * a.ld_bytes;
         __syncthreads();
-        for (int j = tid; j < a.K; j += kDistillThreads) {
-            int id = a.ids[r * a.K + j];
-            if (id >= a.V) {
-                report(a.status, ESTP_ERR_INVALID_ARG);
-                id = -1;
-            }
-            s.id[j] = id;
+        if (warp == 0) {
+            Entries e;
+            ask_entries(a, r, asked);
+            take_entries(a, asked, e);
+            check_entries<kBf16>(a, r, e, table);
+            put_entries<kBf16>(a, e, t);
         }
         __syncthreads();
-        if (a.tail) {  // a token has one probability: a repeated one is left out
-            for (int j = tid; j < a.K; j += kDistillThreads) {
-                bool again = false;
-                for (int i = 0; i < j; ++i) again |= s.id[i] == s.id[j];
-                s.fix[j] = again && s.id[j] >= 0 ? 1.f : 0.f;
-            }
-            __syncthreads();
-            for (int j = tid; j < a.K; j += kDistillThreads)
-                if (s.fix[j] != 0.f) {
-                    report(a.status, ESTP_ERR_INVALID_ARG);
-                    s.id[j] = -1;
-                }
-            __syncthreads();
-        }
-        if (warp == 0) teacher_row<kBf16>(a, r, s);
-        const float g = (a.weight ? a.weight[r] : 1.f) / a.T;
-        // first pass: the statistics
-        LaneStat st;
-        const float2 c2 = make_float2(a.c, a.c);
+        LaneStat<false> st;
         for (int span = 0; span < a.nvec; span += kSpanUnits) {
             const int stop = min(a.nvec, span + kSpanUnits);
-            if (a.tail) {
-                mark(a, s, per, span, true);
-                __syncthreads();
-            }
-            for (int b = span + warp * kStep; b < stop; b += kDistillWarps * kStep) {
+            mark(span, true);
+            for (int b = span + warp * kStep; b < stop; b += kLongWarps * kStep) {
                 uint4 v[kVocabUnroll];
 #pragma unroll
                 for (int k = 0; k < kVocabUnroll; ++k) v[k] = load_unit<kBf16>(row, b + 32 * k + lane, stop, a.V);
@@ -298,84 +650,89 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillA
 #pragma unroll
                     for (int k = 0; k < kVocabUnroll; ++k) {
                         const int c = b + 32 * k;
-                        uint32_t lanes = c < stop ? s.bits[(c - span) >> 5] : 0;
-                        while (lanes) {
-                            const int f = __ffs(lanes) - 1;
-                            lanes &= lanes - 1;
-                            each_named(s, a.K, per, c + f, [&](int j) {
-                                const int at = s.id[j] - (c + f) * per;
-                                if (lane == f) mask_element<kBf16>(v[k], at);
-                            });
-                        }
+                        const uint32_t lanes = c < stop ? bits[(c - span) >> 5] : 0;
+                        if (lanes) mask_named<kBf16>(t, a.K, lanes, c, v[k]);
                     }
                 }
-                float bm = unit_max<kBf16>(v[0]);
-#pragma unroll
-                for (int k = 1; k < kVocabUnroll; ++k) bm = fmaxf(bm, unit_max<kBf16>(v[k]));
-                const float p = -st.raise(bm, a.c);
-                const float2 np = make_float2(p, p);
-#pragma unroll
-                for (int k = 0; k < kVocabUnroll; ++k) add_unit<kBf16>(v[k], np, c2, st);
+                st.template add_units<kBf16>(v, units_max<kBf16, kVocabUnroll>(v), a.c);
             }
-            if (a.tail) {
-                __syncthreads();
-                mark(a, s, per, span, false);
-                __syncthreads();
-            }
+            __syncthreads();
+            mark(span, false);
         }
-        RowStat mine = st.row();
-        join_lanes(mine, a.c);
-        if (lane == 0) s.part[warp] = mine;
+        RowStat s = st.row(a.c);
+        join_lanes(s, a.c);
+        if (lane == 0) part[warp] = s;
         __syncthreads();
+        RowStat all = lane < kLongWarps ? part[lane] : no_stat();
+        join_lanes(all, a.c);
+        const Factors f = row_factors(a, t, all);
         if (warp == 0) {
-            RowStat all = lane < kDistillWarps ? s.part[lane] : no_stat();
-            join_lanes(all, a.c);
-            finish_row(a, r, s, all, g);
+            const float loss = row_loss(a, t, all, f);
+            if (lane == 0) a.loss[r] = loss;
         }
-        __syncthreads();
         if (!a.out) continue;
-        // second pass: the gradient
         char* out = a.out + r * a.out_bytes;
-        const bool zero = !s.some || g == 0.f;
-        const float2 np = make_float2(-s.pivot, -s.pivot);
-        const float A = s.A;
         for (int span = 0; span < a.nvec; span += kSpanUnits) {
             const int stop = min(a.nvec, span + kSpanUnits);
-            mark(a, s, per, span, true);
-            __syncthreads();
-            for (int b = span + warp * kStep; b < stop; b += kDistillWarps * kStep) {
-                uint4 v[kVocabUnroll];
-#pragma unroll
-                for (int k = 0; k < kVocabUnroll; ++k) v[k] = load_unit<kBf16>(row, b + 32 * k + lane, stop, a.V);
-#pragma unroll
-                for (int k = 0; k < kVocabUnroll; ++k) {
-                    const int c = b + 32 * k;
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < per; e += 2) {
-                        const float2 d = __fmul2_rn(__fadd2_rn(make_float2(element<kBf16>(v[k], e), element<kBf16>(v[k], e + 1)), np), c2);
-                        x[e] = zero ? 0.f : A * ex2(d.x);
-                        x[e + 1] = zero ? 0.f : A * ex2(d.y);
-                    }
-                    uint32_t lanes = c < stop && !zero ? s.bits[(c - span) >> 5] : 0;
-                    while (lanes) {
-                        const int f = __ffs(lanes) - 1;
-                        lanes &= lanes - 1;
-                        each_named(s, a.K, per, c + f, [&](int j) {
-                            const int at = s.id[j] - (c + f) * per;
+            mark(span, true);
+            for (int c = span + warp * 32; c < stop; c += kLongThreads) {
+                float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                if (!f.zero) {
+                    other_grad<kBf16, false>(f, load_unit<kBf16>(row, c + lane, stop, a.V), a.c, x);
+                    const uint32_t lanes = bits[(c - span) >> 5];
+                    for (uint32_t left = lanes; left; left &= left - 1) {
+                        const int l = __ffs(left) - 1;
+                        each_named(t, a.K, per, c + l, [&](int j) {
 #pragma unroll
                             for (int e = 0; e < per; ++e)
-                                if (lane == f && e == at) x[e] = a.tail ? s.fix[j] : x[e] + s.fix[j];
+                                if (lane == l && (c + l) * per + e == t.id[j]) x[e] = named_grad(a, t, f, j, x[e]);
                         });
                     }
-                    if (c + lane < stop) store_row_unit<kBf16>(out, c + lane, a.V, x);
                 }
+                if (c + lane < stop) store_unit<kBf16>(out, c + lane, a.V, x);
             }
             __syncthreads();
-            mark(a, s, per, span, false);
-            __syncthreads();
+            mark(span, false);
         }
     }
+}
+
+// ------------------------------------------------------------------ launch
+using ClusterKernel = void (*)(DistillArgs, int, int);
+template <bool kBf16>
+ClusterKernel cluster_kernel(bool grad) {
+    return grad ? distill_cluster_kernel<kBf16, true> : distill_cluster_kernel<kBf16, false>;
+}
+
+constexpr size_t kSharedStatic = sizeof(Teacher) * 3 + sizeof(int32_t) * kSlots + sizeof(Asked) + sizeof(float2) * 2 * kMaxCluster * kHoldWarps;
+
+// CTAs an SM with `bytes` of dynamic shared memory each (1 KB of the SM's goes to every CTA).
+int ctas_per_sm(size_t bytes) {
+    const size_t n = (size_t)(228 * 1024) / (bytes + kSharedStatic + 1024);
+    return n > 3 ? 3 : (int)n;
+}
+
+// Clusters of C that the GPU holds at once, asked once for each kernel, C and number of CTAs an SM.
+int clusters_at_once(estp_ctx* ctx, ClusterKernel kernel, int which, int C, size_t bytes, int per_sm) {
+    int& known = ctx->distill_clusters[which][per_sm - 1][C - 1];
+    if (known) return known;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(C * ctx->num_sms));
+    cfg.blockDim = dim3(kClusterThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+    }
+    known = n > 0 ? n : -1;  // -1: no such cluster here
+    return known;
 }
 
 }  // namespace
@@ -384,6 +741,7 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
                                 int64_t ld, const int32_t* ids, const float* teacher, int K, float T, bool tail,
                                 const float* weight, float* loss, void* out, int64_t ld_out, cudaStream_t st) {
     DistillArgs a;
+    const bool bf16 = dtype == ESTP_BF16;
     const int per = 16 / esize(dtype);
     a.base = static_cast<const char*>(logits);
     a.ld_bytes = ld * esize(dtype);
@@ -401,11 +759,57 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
     a.out = static_cast<char*>(out);
     a.out_bytes = ld_out * esize(dtype);
     a.status = ctx->status;
-    const int64_t most = (int64_t)ctx->num_sms * 2;
-    const unsigned blocks = (unsigned)(n_rows < most ? n_rows : most);
-    if (dtype == ESTP_BF16) distill_kernel<true><<<blocks, kDistillThreads, 0, st>>>(a);
-    else distill_kernel<false><<<blocks, kDistillThreads, 0, st>>>(a);
-    const cudaError_t e = cudaGetLastError();
+
+    // The cluster size by what a wave of rows takes: a unit's share of the memory's rate (0.36 ns of an SM's
+    // for the read, as much for the write) on the CTAs that share an SM, and 2 us a row of barrier, joins and latency.
+    const int which = (bf16 ? 2 : 0) + (out ? 1 : 0);
+    const ClusterKernel kernel = bf16 ? cluster_kernel<true>(out != nullptr) : cluster_kernel<false>(out != nullptr);
+    if (!(ctx->distill_set >> which & 1)) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
+        if (e != cudaSuccess) return cuda_fail(e, "distillation kernel's shared memory");
+        ctx->distill_set |= 1u << which;
+    }
+    int C = 0, clusters = 0;
+    double best = 0.;
+    for (int c = 1; c <= kMaxCluster; ++c) {
+        const int slice = (a.nvec + c - 1) / c;
+        const size_t bytes = (size_t)slice * 16 + 3 * (size_t)((slice + 31) / 32) * 4;
+        if (bytes > kSliceBytes) continue;
+        const int per_sm = ctas_per_sm(bytes);
+        const int at_once = clusters_at_once(ctx, kernel, which, c, bytes, per_sm);
+        if (at_once < 1) continue;
+        const int64_t waves = (n_rows + at_once - 1) / at_once;
+        const int64_t share = (n_rows * c + ctx->num_sms - 1) / ctx->num_sms;  // CTAs an SM really has
+        // (a CTA by itself reaches some 0.4 of the rate)
+        const double sharing = share < per_sm ? (share < 3 ? 2.5 : (double)share) : per_sm < 3 ? 2.5 : (double)per_sm;
+        const double cost = (double)waves * ((out ? 0.72 : 0.36) * slice * sharing + 2000.);
+        if (C == 0 || cost < best) {
+            best = cost;
+            C = c;
+            clusters = n_rows < at_once ? (int)n_rows : at_once;
+        }
+    }
+    if (C == 0) {
+        const int64_t most = (int64_t)ctx->num_sms * 2;
+        const unsigned blocks = (unsigned)(n_rows < most ? n_rows : most);
+        if (bf16) distill_long_kernel<true><<<blocks, kLongThreads, 0, st>>>(a);
+        else distill_long_kernel<false><<<blocks, kLongThreads, 0, st>>>(a);
+        const cudaError_t e = cudaGetLastError();
+        return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
+    }
+    const int slice = (a.nvec + C - 1) / C;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(C * clusters));
+    cfg.blockDim = dim3(kClusterThreads);
+    cfg.dynamicSmemBytes = (size_t)slice * 16 + 3 * (size_t)((slice + 31) / 32) * 4;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, slice, C);
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
 }
 

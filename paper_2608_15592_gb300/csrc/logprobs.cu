@@ -19,6 +19,8 @@
 namespace estp {
 namespace {
 
+constexpr int kWarps = kVocabThreads / 32;
+
 // ------------------------------------------------------------------ keys and lists
 __device__ __forceinline__ uint32_t ordered(float z) {
     const uint32_t b = __float_as_uint(z + 0.f);  // -0 as +0
@@ -80,18 +82,34 @@ __device__ __forceinline__ void merge_keys(uint64_t (&x)[R], const uint64_t (&y)
     for (int j = 16 * R; j > 0; j /= 2) exchange<R>(x, 64 * R, j, lane);
 }
 
-// A warp's list and the candidates that wait for it (shared memory).
+// The same of two lists in shared memory, into the first.
+template <int R>
+__device__ __forceinline__ void merge_lists(uint64_t* to, const uint64_t* from, int lane) {
+    uint64_t x[R], y[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        x[r] = to[r * 32 + lane];
+        y[r] = from[r * 32 + lane];
+    }
+    merge_keys<R>(x, y, lane);
+#pragma unroll
+    for (int r = 0; r < R; ++r) to[r * 32 + lane] = x[r];
+    __syncwarp();
+}
+
+// A warp's list, the candidates that wait for it, and the units that wait to be looked at (shared memory).
 template <int R>
 struct Candidates {
     static constexpr int kBatch = 32 * R;
     uint64_t list[kBatch];
-    uint64_t waiting[kBatch + 256];  // a unit of each lane goes in before the count is looked at
-    int count;
+    uint64_t waiting[kBatch + 256];  // a unit of each lane goes in before the count is looked at again
+    uint32_t units[64];              // a batch adds up to 32, and 32 are taken at once
+    int count, n_units;
 };
 
-// Merges waiting candidates, whole batches or (all) every one; returns the bound that follows.
+// Merges waiting candidates into the list, whole batches or (all) every one.
 template <int R>
-__device__ __noinline__ float take_waiting(Candidates<R>* q, int top_k, bool all, float bound) {
+__device__ __noinline__ void take_waiting(Candidates<R>* q, int top_k, bool all) {
     const int lane = threadIdx.x & 31;
     int n = q->count;
     uint64_t x[R];
@@ -106,15 +124,67 @@ __device__ __noinline__ float take_waiting(Candidates<R>* q, int top_k, bool all
         sort_keys<R>(y, lane);
         merge_keys<R>(x, y, lane);
     }
+    __syncwarp();
 #pragma unroll
     for (int r = 0; r < R; ++r) q->list[r * 32 + lane] = x[r];
-    __syncwarp();
     if (lane == 0) q->count = n;
-    const uint64_t last = q->list[top_k - 1];
     __syncwarp();
-    if (last == 0) return bound;
-    const uint32_t o = (uint32_t)(last >> 32) + 1;  // the next number above it
-    return fmaxf(bound, unordered(o));
+}
+
+// Looks at the units that wait, one a lane at a time (their second read comes from L2), and returns the
+// bound for the tokens that follow all of them.
+template <bool kBf16, int R>
+__device__ __noinline__ float take_units(Candidates<R>* q, const char* row, int c0, int limit, int top_k, float bound,
+                                         int* status) {
+    constexpr int per = kBf16 ? 8 : 4;
+    const int lane = threadIdx.x & 31, n = q->n_units;
+    // these units are not in the order of the tokens: an equal of the list's last may come before it or after
+    uint64_t last = q->list[top_k - 1];
+    float cut = last ? fmaxf(bound, key_logit(last)) : bound;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const uint32_t mine = i0 + lane < n ? q->units[i0 + lane] : 0;
+        uint32_t hits = mine & ((1u << kVocabUnroll) - 1);
+        const int place = c0 + (int)(mine >> kVocabUnroll);
+        while (__any_sync(0xffffffffu, hits != 0)) {
+            if (hits) {
+                const int c = place + 32 * (__ffs(hits) - 1), first = c * per;
+                hits &= hits - 1;
+                if (first < limit) {  // (a lane past the segment marks its -inf where there is no bound yet)
+                    const uint4 u = ld_stream(row + (int64_t)c * 16);
+                    uint32_t in = 0;
+#pragma unroll
+                    for (int e = 0; e < per; ++e) in |= element<kBf16>(u, e) >= cut ? 1u << e : 0u;
+                    if (limit - first < per) in &= (1u << (limit - first)) - 1;
+                    if (last && key_logit(last) == cut) {
+                        const int before = key_token(last) - first;  // tokens of the unit that come before the last
+                        uint32_t equal = 0;
+#pragma unroll
+                        for (int e = 0; e < per; ++e) equal |= element<kBf16>(u, e) == cut ? 1u << e : 0u;
+                        if (before < per) in &= ~equal | (before > 0 ? (1u << before) - 1 : 0u);
+                    }
+                    if (in) {
+                        int at = atomicAdd(&q->count, __popc(in));
+                        do {
+                            const int e = __ffs(in) - 1;
+                            in &= in - 1;
+                            if (in_bounds(at < 32 * R + 256, status)) q->waiting[at] = key_of(element_of<kBf16>(u, e), first + e);
+                            ++at;
+                        } while (in);
+                    }
+                }
+            }
+            __syncwarp();
+            if (q->count >= 32 * R) {
+                take_waiting<R>(q, top_k, false);
+                last = q->list[top_k - 1];
+                if (last) cut = fmaxf(cut, key_logit(last));
+            }
+            __syncwarp();
+        }
+    }
+    if (lane == 0) q->n_units = 0;
+    __syncwarp();
+    return last ? fmaxf(bound, unordered((uint32_t)(last >> 32) + 1)) : bound;  // the next number above it
 }
 
 // A logit that at least top_k of the warp's 32 G values reach (or -inf): the order bits from the top
@@ -159,10 +229,9 @@ template <bool kBf16, int R>
 __device__ __forceinline__ RowStat stream_row(const LpArgs& a, const char* row, int c0, int c1, Candidates<R>* q) {
     constexpr int per = kBf16 ? 8 : 4;
     const int lane = threadIdx.x & 31, V = a.rows.V;
-    const float2 c2 = make_float2(a.c, a.c);
     const int limit = min(V, c1 * per);                  // tokens of the segment end here
-    const int whole = limit - c1 * per < 0 ? c1 - 1 : c1;  // units without a partial one
-    LaneStat st;
+    const int whole = min(c1, V / per);                  // units before a partial one
+    LaneStat<true> st;
     float bound = -INFINITY;
     for (int b = c0; b < c1; b += 32 * kVocabUnroll) {
         uint4 v[kVocabUnroll];
@@ -175,62 +244,33 @@ __device__ __forceinline__ RowStat stream_row(const LpArgs& a, const char* row, 
 #pragma unroll
             for (int k = 0; k < kVocabUnroll; ++k) v[k] = load_unit<kBf16>(row, c + 32 * k, c1, V);
         }
-        float mx[kVocabUnroll], bm;
-#pragma unroll
-        for (int k = 0; k < kVocabUnroll; ++k) mx[k] = unit_max<kBf16>(v[k]);
-        bm = mx[0];
-#pragma unroll
-        for (int k = 1; k < kVocabUnroll; ++k) bm = fmaxf(bm, mx[k]);
+        const float bm = units_max<kBf16, kVocabUnroll>(v);
         if constexpr (R > 0) {
             if (b == c0) {
                 constexpr int G = 2 * R, w = kVocabUnroll / G;
                 float g[G];
 #pragma unroll
-                for (int i = 0; i < G; ++i) {
-                    g[i] = mx[i * w];
-#pragma unroll
-                    for (int k = 1; k < w; ++k) g[i] = fmaxf(g[i], mx[i * w + k]);
-                }
+                for (int i = 0; i < G; ++i) g[i] = units_max<kBf16, w>(v + i * w);
                 bound = reached_by<G>(g, a.top_k);
             }
+            // a lane with candidates leaves its place and a bit for each unit that holds one
             if (__any_sync(0xffffffffu, bm >= bound)) {
-                uint32_t hit = 0;  // units that some lane has a candidate in
+                uint32_t hits = 0;
 #pragma unroll
-                for (int k = 0; k < kVocabUnroll; ++k) hit |= __any_sync(0xffffffffu, mx[k] >= bound) ? 1u << k : 0u;
-                while (hit) {
-                    const int k = __ffs(hit) - 1;
-                    hit &= hit - 1;
-                    uint4 u = v[0];
-#pragma unroll
-                    for (int i = 1; i < kVocabUnroll; ++i)
-                        if (i == k) u = v[i];
-                    const int first = (c + 32 * k) * per;
-                    uint32_t in = 0;
-#pragma unroll
-                    for (int e = 0; e < per; ++e)
-                        if (element<kBf16>(u, e) >= bound && first + e < limit) in |= 1u << e;
-                    if (in) {
-                        int at = atomicAdd(&q->count, __popc(in));
-#pragma unroll
-                        for (int e = 0; e < per; ++e)
-                            if (in >> e & 1) {
-                                if (in_bounds(at < 32 * R + 256, a.status)) q->waiting[at] = key_of(element<kBf16>(u, e), first + e);
-                                ++at;
-                            }
-                    }
-                    __syncwarp();
-                    if (q->count >= 32 * R) bound = take_waiting<R>(q, a.top_k, false, bound);
-                    __syncwarp();
-                }
+                for (int k = 0; k < kVocabUnroll; ++k) hits |= units_max<kBf16, 1>(v + k) >= bound ? 1u << k : 0u;
+                if (hits) q->units[atomicAdd(&q->n_units, 1)] = (uint32_t)(c - c0) << kVocabUnroll | hits;
+                __syncwarp();
+                if (q->n_units >= 32) bound = take_units<kBf16, R>(q, row, c0, limit, a.top_k, bound, a.status);
+                __syncwarp();
             }
         }
-        const float p = -st.raise(bm, a.c);
-        const float2 np = make_float2(p, p);
-#pragma unroll
-        for (int k = 0; k < kVocabUnroll; ++k) add_unit<kBf16>(v[k], np, c2, st);
+        st.template add_units<kBf16>(v, bm, a.c);
     }
-    if constexpr (R > 0) take_waiting<R>(q, a.top_k, true, bound);
-    return st.row();
+    if constexpr (R > 0) {
+        take_units<kBf16, R>(q, row, c0, limit, a.top_k, bound, a.status);
+        take_waiting<R>(q, a.top_k, true);
+    }
+    return st.row(a.c);
 }
 
 // What a row's statistics and list say, written by a warp.
@@ -268,14 +308,29 @@ __device__ __forceinline__ void write_row(const LpArgs& a, int64_t r, const char
     }
 }
 
+// The row that all of block b's pieces lie in, or -1: its warps then join their parts themselves.
+__device__ __forceinline__ int64_t row_of_block(const VocabRows& a, int64_t b) {
+    const int64_t lo = b * kWarps, hi = lo + kWarps < a.pieces ? lo + kWarps : a.pieces;
+    const int64_t r = piece_start(a, lo) / a.nvec;
+    return (piece_start(a, hi) - 1) / a.nvec == r ? r : -1;
+}
+
 template <bool kBf16, int R>
 __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(const LpArgs a) {
-    __shared__ Candidates<R ? R : 1> cand[R ? kVocabThreads / 32 : 1];
+    constexpr int kLists = R ? R : 1;
+    __shared__ Candidates<kLists> cand[R ? kWarps : 1];
+    __shared__ RowStat stats[kWarps];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join may be scheduled
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t w = (int64_t)blockIdx.x * (kVocabThreads / 32) + warp;
-    if (w >= a.rows.pieces) return;
-    Candidates<R ? R : 1>* q = R ? &cand[warp] : nullptr;
-    const int64_t start = piece_start(a.rows, w), end = piece_start(a.rows, w + 1);
+    const int64_t w = (int64_t)blockIdx.x * kWarps + warp;
+    const bool one_row = row_of_block(a.rows, blockIdx.x) >= 0;
+    Candidates<kLists>* q = R ? &cand[warp] : nullptr;
+    const int64_t start = w < a.rows.pieces ? piece_start(a.rows, w) : 0, end = w < a.rows.pieces ? piece_start(a.rows, w + 1) : 0;
+    RowStat st = no_stat();
+    if (R > 0 && start == end) {
+        for (int i = lane; i < 32 * R; i += 32) q->list[i] = 0;
+        __syncwarp();
+    }
     for (int64_t u = start; u < end;) {
         const int64_t r = u / a.rows.nvec, u0 = r * a.rows.nvec;
         const int c0 = (int)(u - u0), c1 = (int)(min(end, u0 + a.rows.nvec) - u0);
@@ -283,13 +338,13 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(c
         if constexpr (R > 0) {
             __syncwarp();
             for (int i = lane; i < 32 * R; i += 32) q->list[i] = 0;
-            if (lane == 0) q->count = 0;
+            if (lane == 0) q->count = q->n_units = 0;
             __syncwarp();
         }
-        RowStat st;
         if constexpr (R > 0) st = stream_row<kBf16, R>(a, row, c0, c1, q);
         else st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);
         join_lanes(st, a.c);
+        if (one_row) break;
         if (c0 == 0 && c1 == a.rows.nvec) {
             write_row<kBf16, R>(a, r, row, st, R ? q->list : nullptr);
         } else {
@@ -300,46 +355,74 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(c
         }
         u = u0 + c1;
     }
+    if (!one_row) return;
+    // pairs of warps, the lower half taking from the upper one
+    for (int half = kWarps / 2; half > 0; half /= 2) {
+        if (lane == 0) stats[warp] = st;
+        __syncthreads();
+        if (warp < half) {
+            join(st, stats[warp + half], a.c);
+            if constexpr (R > 0) merge_lists<R>(q->list, cand[warp + half].list, lane);
+        }
+        __syncthreads();
+    }
+    if (warp != 0) return;
+    const int64_t r = start / a.rows.nvec, lo = blockIdx.x * (int64_t)kWarps;
+    const int64_t next = piece_start(a.rows, lo + kWarps < a.rows.pieces ? lo + kWarps : a.rows.pieces);
+    if (start == r * a.rows.nvec && next == start + a.rows.nvec) {
+        write_row<kBf16, R>(a, r, a.rows.base + r * a.rows.ld_bytes, st, R ? q->list : nullptr);
+    } else {  // in the place of the block's first piece
+        if (lane == 0) a.part[w * 2] = make_float4(st.m, st.s, st.t, 0.f);
+        if constexpr (R > 0)
+            for (int i = lane; i < 32 * R; i += 32) a.lists[w * 2 * (32 * R) + i] = q->list[i];
+    }
 }
 
-// Rows cut between pieces, `warps` warps a row (1 or all of the block's): each joins every warps-th
-// part in order, and the first joins what the others found.
+// Rows cut between pieces, `warps` warps a row (1 or all of the block's): each joins the parts of every
+// warps-th block of the forward in order, then pairs of warps join what they have.
 template <bool kBf16, int R>
 __global__ void __launch_bounds__(kVocabThreads) logprobs_join_kernel(const LpArgs a, int warps) {
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the parts are complete
-    constexpr int kWarps = kVocabThreads / 32, kList = R ? 32 * R : 1;
+    constexpr int kList = R ? 32 * R : 1;
     __shared__ uint64_t lists[kWarps][kList];
-    __shared__ float4 parts[kWarps];
+    __shared__ RowStat stats[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % warps;
     const int64_t r = ((int64_t)blockIdx.x * kWarps + warp) / warps;
     int64_t lo = 0, hi = 0;
+    bool cut = false;
     if (r < a.rows.n_rows) {
         lo = piece_of(a.rows, r * a.rows.nvec);
         hi = piece_of(a.rows, (r + 1) * a.rows.nvec - 1);
+        // one piece that held the whole row has written it, or one block
+        cut = lo < hi;
+        if (cut && lo / kWarps == hi / kWarps && row_of_block(a.rows, lo / kWarps) == r &&
+            piece_start(a.rows, lo / kWarps * kWarps) == r * a.rows.nvec &&
+            piece_start(a.rows, min((lo / kWarps + 1) * kWarps, a.rows.pieces)) == (r + 1) * a.rows.nvec)
+            cut = false;
     }
-    const bool cut = lo < hi;  // one piece that held the whole row has written it
     RowStat st = no_stat();
     uint64_t x[R ? R : 1];
 #pragma unroll
     for (int i = 0; i < (R ? R : 1); ++i) x[i] = 0;
-    if (cut) {
+    auto take = [&](int64_t slot) {
+        const float4 p = a.part[slot];
         if constexpr (R > 0) {
-            for (int64_t w = lo + sub; w <= hi; w += warps) {
-                const int64_t slot = w * 2 + (piece_start(a.rows, w) / a.rows.nvec == r ? 0 : 1);
-                const float4 p = a.part[slot];
-                join(st, RowStat{p.x, p.y, p.z}, a.c);
-                uint64_t y[R];
+            uint64_t y[R];
 #pragma unroll
-                for (int i = 0; i < R; ++i) y[i] = a.lists[slot * kList + i * 32 + lane];
-                merge_keys<R>(x, y, lane);
+            for (int i = 0; i < R; ++i) y[i] = a.lists[slot * kList + i * 32 + lane];
+            merge_keys<R>(x, y, lane);
+        }
+        join(st, RowStat{p.x, p.y, p.z}, a.c);
+    };
+    if (cut) {
+        for (int64_t b = lo / kWarps + sub; b <= hi / kWarps; b += warps) {
+            if (row_of_block(a.rows, b) == r) {
+                take(b * kWarps * 2);
+            } else {
+                const int64_t last = min(hi, (b + 1) * kWarps - 1);
+                for (int64_t w = b * kWarps > lo ? b * kWarps : lo; w <= last; ++w)
+                    take(w * 2 + (piece_start(a.rows, w) / a.rows.nvec == r ? 0 : 1));
             }
-        } else {
-            for (int64_t w = lo + sub * 32 + lane; w <= hi; w += warps * 32) {
-                const int64_t slot = w * 2 + (piece_start(a.rows, w) / a.rows.nvec == r ? 0 : 1);
-                const float4 p = a.part[slot];
-                join(st, RowStat{p.x, p.y, p.z}, a.c);
-            }
-            join_lanes(st, a.c);
         }
     }
     if (R > 0) {
@@ -347,32 +430,20 @@ __global__ void __launch_bounds__(kVocabThreads) logprobs_join_kernel(const LpAr
         for (int i = 0; i < R; ++i) lists[warp][i * 32 + lane] = x[i];
         __syncwarp();
     }
-    if (warps > 1) {
-        if (lane == 0) parts[warp] = make_float4(st.m, st.s, st.t, 0.f);
+    for (int half = warps / 2; half > 0; half /= 2) {  // (warps is the same for the whole grid)
+        if (lane == 0) stats[warp] = st;
         __syncthreads();
-        if (warp == 0 && cut)
-            for (int k = 1; k < kWarps; ++k) {
-                const float4 p = parts[k];
-                join(st, RowStat{p.x, p.y, p.z}, a.c);
-                if constexpr (R > 0) {
-                    uint64_t y[R];
-#pragma unroll
-                    for (int i = 0; i < R; ++i) y[i] = lists[k][i * 32 + lane];
-                    merge_keys<R>(x, y, lane);
-                }
-            }
-        if (R > 0 && warp == 0) {
-#pragma unroll
-            for (int i = 0; i < R; ++i) lists[0][i * 32 + lane] = x[i];
-            __syncwarp();
+        if (warp < half && cut) {
+            join(st, stats[warp + half], a.c);
+            if constexpr (R > 0) merge_lists<R>(lists[warp], lists[warp + half], lane);
         }
+        __syncthreads();
     }
     if (cut && sub == 0) write_row<kBf16, R>(a, r, a.rows.base + r * a.rows.ld_bytes, st, lists[warp]);
 }
 
 template <bool kBf16, int R>
 cudaError_t launch_forward(const LpArgs& a, cudaStream_t st) {
-    constexpr int kWarps = kVocabThreads / 32;
     logprobs_kernel<kBf16, R><<<(unsigned)((a.rows.pieces + kWarps - 1) / kWarps), kVocabThreads, 0, st>>>(a);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
@@ -415,7 +486,7 @@ struct LpGradArgs {
     int* status;
 };
 
-constexpr int kGradUnroll = 4;
+constexpr int kGradUnroll = 4, kGradBlocks = 4;
 
 // The tokens of a row that have a term of their own.
 struct Named {
@@ -424,41 +495,100 @@ struct Named {
     uint32_t bits[32];  // units of the present 1024 that hold one
 };
 
-template <bool kBf16>
-__device__ __forceinline__ void store_unit(char* row, int c, int V, const float (&x)[8]) {
-    constexpr int per = kBf16 ? 8 : 4;
-    char* p = row + (int64_t)c * 16;
-    if (V - c * per >= per) {
-        uint4 o;
-        if (kBf16) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(&o);
+// What the elements of a row's gradient have in common: dz_v = 2^d (A + B d), d = z c - M in the near
+// frame of the maximum (vocab.cuh), or (z - m) c where it has none.
+struct RowGrad {
+    float m, M, A, B;
+    bool framed;
+};
+
+template <bool kBf16, bool kEntropy, bool kFramed>
+__device__ __forceinline__ void grad_unit(const uint4& v, const RowGrad& g, float c, float (&x)[8]) {
+    const float2 c2 = make_float2(c, c), A2 = make_float2(g.A, g.A), B2 = make_float2(g.B, g.B);
+    const float2 off = kFramed ? make_float2(-g.M, -g.M) : make_float2(-g.m, -g.m);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t*>(&b);
-            }
-        } else {
-            o = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    for (int i = 0; i < (kBf16 ? 4 : 2); ++i) {
+        float2 d = kFramed ? __ffma2_rn(pair<kBf16>(v, i), c2, off) : __fmul2_rn(__fadd2_rn(pair<kBf16>(v, i), off), c2);
+        float2 f = A2;
+        if (kEntropy) {
+            d.x = max_nan(d.x, kCut);  // (2^d d is 0 for a masked token)
+            d.y = max_nan(d.y, kCut);
+            f = __ffma2_rn(B2, d, A2);
         }
-        __stcs(reinterpret_cast<uint4*>(p), o);
-    } else {  // the row's last, partial unit: what lies behind the vocabulary stays as it is
-#pragma unroll
-        for (int e = 0; e < per; ++e)
-            if (c * per + e < V) {
-                if (kBf16) reinterpret_cast<__nv_bfloat16*>(p)[e] = __float2bfloat16_rn(x[e]);
-                else reinterpret_cast<float*>(p)[e] = x[e];
-            }
+        const float2 y = __fmul2_rn(make_float2(ex2(d.x), ex2(d.y)), f);
+        x[2 * i] = y.x;
+        x[2 * i + 1] = y.y;
     }
 }
 
-// dz_v = e (A + B d) + sum over named tokens, e = 2^d, d = (z_v - m) c.  A warp a piece, as in the
-// forward pass; a lane reads a unit before it writes it, so the gradient may take the logits' place.
+// Adds the terms of the named tokens of the units that `lanes` marks, of a warp's 32 from `unit` on.
 template <bool kBf16>
-__global__ void __launch_bounds__(kVocabThreads) logprobs_grad_kernel(const LpGradArgs a) {
+__device__ __noinline__ void add_named(const Named& q, int n, uint32_t lanes, int unit, float* x) {
     constexpr int per = kBf16 ? 8 : 4;
-    __shared__ Named named[kVocabThreads / 32];
+    const int lane = threadIdx.x & 31;
+    while (lanes) {
+        const int l = __ffs(lanes) - 1;
+        lanes &= lanes - 1;
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            const int i = i0 + lane;
+            const int id = i < n ? q.id[i] : -1;
+            uint32_t hit = __ballot_sync(0xffffffffu, id >= 0 && id / per == unit + l);
+            while (hit) {
+                const int j = i0 + __ffs(hit) - 1;
+                hit &= hit - 1;
+                if (lane == l) x[q.id[j] - (unit + l) * per] += q.g[j];
+            }
+        }
+    }
+}
+
+// Units [chunk, stop) of a row, at most 1024; `steps` marks the 32s that hold a named token, lane l's `word` the
+// units of step l.
+template <bool kBf16, bool kEntropy, bool kFramed>
+__device__ __forceinline__ void grad_chunk(const char* row, char* out, int chunk, int stop, int V, const RowGrad& g, float c,
+                                           const Named& q, int n_named, uint32_t word, uint32_t steps) {
+    constexpr int per = kBf16 ? 8 : 4;
+    const int lane = threadIdx.x & 31, whole = min(stop, V / per);  // units before a partial one
+    int b = chunk;
+    for (; b + 32 * kGradUnroll <= whole; b += 32 * kGradUnroll) {
+        uint4 v[kGradUnroll];
+        const int64_t at = (int64_t)(b + lane) * 16;
+#pragma unroll
+        for (int k = 0; k < kGradUnroll; ++k) v[k] = ld_stream(row + at + k * 512);
+#pragma unroll
+        for (int k = 0; k < kGradUnroll; ++k) {
+            float x[8];
+            grad_unit<kBf16, kEntropy, kFramed>(v[k], g, c, x);
+            const int step = (b - chunk) / 32 + k;
+            if (steps >> step & 1) {
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < per; ++e) y[e] = x[e];
+                add_named<kBf16>(q, n_named, __shfl_sync(0xffffffffu, word, step), b + 32 * k, y);
+#pragma unroll
+                for (int e = 0; e < per; ++e) x[e] = y[e];
+            }
+            store_whole<kBf16>(out + at + k * 512, x);
+        }
+    }
+    for (; b < stop; b += 32) {
+        const uint4 v = load_unit<kBf16>(row, b + lane, stop, V);
+        float x[8];
+        grad_unit<kBf16, kEntropy, kFramed>(v, g, c, x);
+        const int step = (b - chunk) / 32;
+        if (steps >> step & 1) add_named<kBf16>(q, n_named, __shfl_sync(0xffffffffu, word, step), b, x);
+        if (b + lane < stop) store_unit<kBf16>(out, b + lane, V, x);
+    }
+}
+
+// A warp a piece, as in the forward pass; a lane reads a unit before it writes it, so the gradient may
+// take the logits' place.
+template <bool kBf16>
+__global__ void __launch_bounds__(kVocabThreads, kGradBlocks) logprobs_grad_kernel(const LpGradArgs a) {
+    constexpr int per = kBf16 ? 8 : 4;
+    __shared__ Named named[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, V = a.rows.V;
-    const int64_t w = (int64_t)blockIdx.x * (kVocabThreads / 32) + warp;
+    const int64_t w = (int64_t)blockIdx.x * kWarps + warp;
     if (w >= a.rows.pieces) return;
     Named& q = named[warp];
     const int64_t start = piece_start(a.rows, w), end = piece_start(a.rows, w + 1);
@@ -471,7 +601,6 @@ __global__ void __launch_bounds__(kVocabThreads) logprobs_grad_kernel(const LpGr
         u = u0 + c1;
         if (!in_bounds(r < a.rows.n_rows && c0 < c1 && c1 <= a.rows.nvec, a.status)) return;
         const float2 norm = a.norm[r];
-        const float m = pivot(norm.x);
         const bool empty = norm.y == 0.f;
         // named tokens and the sum of their gradients
         float pull = 0.f;
@@ -510,16 +639,17 @@ __global__ void __launch_bounds__(kVocabThreads) logprobs_grad_kernel(const LpGr
             pull += g;
         }
         __syncwarp();
-        const float gH = a.g_entropy ? a.g_entropy[r] : 0.f, gl = a.g_lse ? a.g_lse[r] : 0.f;
-        float A = 0.f, B = 0.f;
-        if (!empty) {
-            const float f = inv_T / norm.y;
-            A = f * (gl - pull + (gH != 0.f ? gH * (logf(norm.y) - a.entropy[r]) : 0.f));
-            B = -f * gH * kLn2;
-        }
+        const float gH = a.g_entropy && !empty ? a.g_entropy[r] : 0.f, gl = a.g_lse ? a.g_lse[r] : 0.f;
         // nothing for the row as a whole: zeros, whatever its logits hold
         const bool flat = empty || (gl - pull == 0.f && gH == 0.f);
-        const float2 np = make_float2(-m, -m), c2 = make_float2(a.c, a.c), A2 = make_float2(A, A), B2 = make_float2(B, B);
+        RowGrad g{pivot(norm.x), 0.f, 0.f, 0.f, false};
+        g.M = g.m * a.c;
+        g.framed = near_frame(g.M);
+        if (!flat) {
+            const float f = inv_T / norm.y, off = frame_off(g.m, a.c), back = ex2(-off);
+            g.B = -f * gH * kLn2 * back;
+            g.A = f * (gl - pull + (gH != 0.f ? gH * (logf(norm.y) - a.entropy[r]) : 0.f)) * back - g.B * off;
+        }
         for (int chunk = c0; chunk < c1; chunk += 1024) {
             // the units of this chunk with a named token, lane l's word those of its step l
             bool any = false;
@@ -538,46 +668,19 @@ __global__ void __launch_bounds__(kVocabThreads) logprobs_grad_kernel(const LpGr
                 __syncwarp();
             }
             const int stop = min(c1, chunk + 1024);
-            for (int b = chunk; b < stop; b += 32 * kGradUnroll) {
-                uint4 v[kGradUnroll];
-#pragma unroll
-                for (int k = 0; k < kGradUnroll; ++k) v[k] = load_unit<kBf16>(row, b + 32 * k + lane, stop, V);
-#pragma unroll
-                for (int k = 0; k < kGradUnroll; ++k) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < per; e += 2) {
-                        float2 d = __fmul2_rn(__fadd2_rn(make_float2(element<kBf16>(v[k], e), element<kBf16>(v[k], e + 1)), np), c2);
-                        d.x = max_nan(d.x, kCut);
-                        d.y = max_nan(d.y, kCut);
-                        const float2 g = __fmul2_rn(make_float2(ex2(d.x), ex2(d.y)), __ffma2_rn(B2, d, A2));
-                        x[e] = flat ? 0.f : g.x;
-                        x[e + 1] = flat ? 0.f : g.y;
-                    }
-                    const int step = (b - chunk) / 32 + k, c = b + 32 * k + lane;
-                    if (steps >> step & 1) {
-                        uint32_t lanes = __shfl_sync(0xffffffffu, word, step);
-                        while (lanes) {
-                            const int f = __ffs(lanes) - 1, unit = c - lane + f;
-                            lanes &= lanes - 1;
-                            for (int i0 = 0; i0 < n_named; i0 += 32) {
-                                const int i = i0 + lane;
-                                const int id = i < n_named ? q.id[i] : -1;
-                                uint32_t hit = __ballot_sync(0xffffffffu, id >= 0 && id / per == unit);
-                                while (hit) {
-                                    const int j = i0 + __ffs(hit) - 1;
-                                    hit &= hit - 1;
-                                    const int at = q.id[j] - unit * per;
-                                    const float g = q.g[j];
-#pragma unroll
-                                    for (int e = 0; e < per; ++e)
-                                        if (lane == f && e == at) x[e] += g;
-                                }
-                            }
-                        }
-                    }
-                    if (c < stop) store_unit<kBf16>(out, c, V, x);
+            if (flat) {
+                for (int b = chunk; b < stop; b += 32) {
+                    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    const int step = (b - chunk) / 32;
+                    if (steps >> step & 1) add_named<kBf16>(q, n_named, __shfl_sync(0xffffffffu, word, step), b, x);
+                    if (b + lane < stop) store_unit<kBf16>(out, b + lane, V, x);
                 }
+            } else if (!g.framed) {
+                grad_chunk<kBf16, true, false>(row, out, chunk, stop, V, g, a.c, q, n_named, word, steps);
+            } else if (gH != 0.f) {
+                grad_chunk<kBf16, true, true>(row, out, chunk, stop, V, g, a.c, q, n_named, word, steps);
+            } else {
+                grad_chunk<kBf16, false, true>(row, out, chunk, stop, V, g, a.c, q, n_named, word, steps);
             }
         }
     }
@@ -590,7 +693,7 @@ estp_status launch_token_logprobs(estp_ctx* ctx, const void* logits, estp_dtype 
                                   float* entropy, float* norm, int32_t* top_ids, float* top_logprobs,
                                   cudaStream_t st) {
     LpArgs a;
-    a.rows = vocab_rows(ctx, logits, dtype, n_rows, V, ld, 32 * kVocabUnroll);
+    a.rows = vocab_rows(ctx, logits, dtype, n_rows, V, ld, 32 * kVocabUnroll, kVocabBlocks);
     a.targets = targets;
     a.T = T;
     a.c = (float)(1.4426950408889634 / (double)T);
@@ -613,7 +716,7 @@ estp_status launch_token_logprobs_grad(estp_ctx* ctx, const void* logits, estp_d
                                        const float* g_entropy, const float* g_lse, const float* g_top, void* out,
                                        int64_t ld_out, cudaStream_t st) {
     LpGradArgs a;
-    a.rows = vocab_rows(ctx, logits, dtype, n_rows, V, ld, 32 * kGradUnroll);
+    a.rows = vocab_rows(ctx, logits, dtype, n_rows, V, ld, 32 * kGradUnroll, kGradBlocks);
     a.out = static_cast<char*>(out);
     a.out_bytes = ld_out * esize(dtype);
     a.norm = reinterpret_cast<const float2*>(norm);
@@ -628,7 +731,6 @@ estp_status launch_token_logprobs_grad(estp_ctx* ctx, const void* logits, estp_d
     a.c = (float)(1.4426950408889634 / (double)T);
     a.top_k = top_k;
     a.status = ctx->status;
-    constexpr int kWarps = kVocabThreads / 32;
     const unsigned blocks = (unsigned)((a.rows.pieces + kWarps - 1) / kWarps);
     if (dtype == ESTP_BF16) logprobs_grad_kernel<true><<<blocks, kVocabThreads, 0, st>>>(a);
     else logprobs_grad_kernel<false><<<blocks, kVocabThreads, 0, st>>>(a);

@@ -18,7 +18,7 @@ constexpr int kVocabThreads = 256;
 constexpr int kVocabBlocks = 3;       // resident blocks an SM the registers of the streams are sized for
 constexpr int kVocabUnroll = 8;       // 16-byte loads a lane has in flight
 constexpr int kMaxAlternatives = 128;  // entries of a row's list
-constexpr int64_t kMaxVocab = 1 << 30;  // a token's index, and that of its unit, in 32 bits
+constexpr int64_t kMaxVocab = 1 << 26;  // the index of a row's 16-byte unit in 24 bits
 constexpr float kMinTemperature = 1e-6f;  // log2(e) / T stays far from overflow
 constexpr float kCut = -200.f;
 
@@ -50,7 +50,7 @@ __device__ __forceinline__ int64_t piece_of(const VocabRows& a, int64_t u) {
 }
 
 inline VocabRows vocab_rows(const estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
-                            int64_t ld, int min_units) {
+                            int64_t ld, int min_units, int blocks) {
     VocabRows a;
     const int per = 16 / esize(dtype);
     a.base = static_cast<const char*>(logits);
@@ -59,7 +59,7 @@ inline VocabRows vocab_rows(const estp_ctx* ctx, const void* logits, estp_dtype 
     a.V = (int32_t)V;
     a.nvec = (int32_t)((V + per - 1) / per);
     a.units = n_rows * a.nvec;
-    const int64_t most = (int64_t)ctx->num_sms * kVocabBlocks * (kVocabThreads / 32);
+    const int64_t most = (int64_t)ctx->num_sms * blocks * (kVocabThreads / 32);
     const int64_t want = (a.units + min_units - 1) / min_units;
     a.pieces = want < most ? want : most;
     return a;
@@ -82,69 +82,140 @@ __device__ __forceinline__ void join(RowStat& a, const RowStat& b, float c) {
     a.m = m;
 }
 
+// The lanes' statistics joined: the maximum first, then sums against it.
+template <bool kT = true>
 __device__ __forceinline__ void join_lanes(RowStat& a, float c) {
+    float m = a.m;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    const float d = max_nan((a.m - pivot(m)) * c, kCut), f = ex2(d);
+    float s = f * a.s, t = f * fmaf(d, a.s, a.t);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
-        const RowStat b{__shfl_xor_sync(0xffffffffu, a.m, off), __shfl_xor_sync(0xffffffffu, a.s, off),
-                        __shfl_xor_sync(0xffffffffu, a.t, off)};
-        join(a, b, c);
+        s += __shfl_xor_sync(0xffffffffu, s, off);
+        if (kT) t += __shfl_xor_sync(0xffffffffu, t, off);
     }
+    a = RowStat{m, s, t};
 }
 
-// A lane's sums, in two pairs to shorten the chains of additions.
+// Greatest logit of N units (NaN is passed over: the sums show it).
+template <bool kBf16, int N>
+__device__ __forceinline__ float units_max(const uint4* v) {
+    if (kBf16) {
+        __nv_bfloat162 x[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v[k]);
+            x[k] = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+        }
+#pragma unroll
+        for (int w = N / 2; w > 0; w /= 2)
+#pragma unroll
+            for (int k = 0; k < w; ++k) x[k] = __hmax2(x[k], x[k + w]);
+        return fmaxf(__low2float(x[0]), __high2float(x[0]));
+    }
+    float x = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        x = fmaxf(x, fmaxf(fmaxf(__uint_as_float(v[k].x), __uint_as_float(v[k].y)), fmaxf(__uint_as_float(v[k].z), __uint_as_float(v[k].w))));
+    return x;
+}
+
+// Two consecutive elements of a unit, as fp32.
+template <bool kBf16>
+__device__ __forceinline__ float2 pair(const uint4& v, int i) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
+    if (kBf16) return make_float2(bf16lo(w[i]), bf16hi(w[i]));
+    return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+}
+
+// The near frame.  d = (z - m) c costs an addition and a product; z c - M with M = m c rounded is one
+// fused operation, and off by the same delta = m c - M (which fma(m, c, -M) gives) in every term: 2^d
+// by the factor 2^delta.  Where |M| <= 2^20 delta is at most 1/16, and sums in that frame
+// are brought back exactly enough: s = 2^-delta s', t = 2^-delta (t' - delta s').
+constexpr float kNear = 1048576.f;
+__device__ __forceinline__ bool near_frame(float M) { return fabsf(M) <= kNear; }
+__device__ __forceinline__ float frame_off(float m, float c) { return near_frame(m * c) ? fmaf(m, c, -(m * c)) : 0.f; }
+
+// A lane's sums, in two pairs to shorten the chains of additions; kT: with sum 2^d d.  They are in the near
+// frame of m where it has one, else relative to m itself.
+template <bool kT>
 struct LaneStat {
     float m;
     float2 s0, s1, t0, t1;
     __device__ __forceinline__ LaneStat() : m(-INFINITY) { s0 = s1 = t0 = t1 = make_float2(0.f, 0.f); }
-    __device__ __forceinline__ RowStat row() const {
-        return RowStat{m, (s0.x + s0.y) + (s1.x + s1.y), (t0.x + t0.y) + (t1.x + t1.y)};
-    }
-    // Sums in units of the new maximum; returns what is subtracted from the logits.
-    __device__ __forceinline__ float raise(float bm, float c) {
-        const float nm = fmaxf(m, bm), p = pivot(nm);
-        const float dm = max_nan((m - p) * c, kCut), f = ex2(dm);
-        const float2 f2 = make_float2(f, f), d2 = make_float2(dm, dm);
-        t0 = __fmul2_rn(f2, __ffma2_rn(d2, s0, t0));
-        t1 = __fmul2_rn(f2, __ffma2_rn(d2, s1, t1));
+
+    __device__ __forceinline__ void scale(float f, float d) {  // s <- f s, t <- f (t + d s)
+        const float2 f2 = make_float2(f, f), d2 = make_float2(d, d);
+        if (kT) {
+            t0 = __fmul2_rn(f2, __ffma2_rn(d2, s0, t0));
+            t1 = __fmul2_rn(f2, __ffma2_rn(d2, s1, t1));
+        }
         s0 = __fmul2_rn(f2, s0);
         s1 = __fmul2_rn(f2, s1);
+    }
+    __device__ __forceinline__ void take(const LaneStat& b, float f, float d) {  // the same, and b's are added
+        const float2 f2 = make_float2(f, f), d2 = make_float2(d, d);
+        if (kT) {
+            t0 = __ffma2_rn(f2, __ffma2_rn(d2, s0, t0), b.t0);
+            t1 = __ffma2_rn(f2, __ffma2_rn(d2, s1, t1), b.t1);
+        }
+        s0 = __ffma2_rn(f2, s0, b.s0);
+        s1 = __ffma2_rn(f2, s1, b.s1);
+    }
+    __device__ __forceinline__ void add(float2 d, int i) {
+        const float2 e = make_float2(ex2(d.x), ex2(d.y));
+        float2 &s = i & 1 ? s1 : s0, &t = i & 1 ? t1 : t0;
+        s = __fadd2_rn(s, e);
+        if (kT) t = __ffma2_rn(e, d, t);
+    }
+
+    // N units (of every lane of the warp) whose greatest logit is bm.
+    template <bool kBf16, int N>
+    __device__ __forceinline__ void add_units(const uint4 (&v)[N], float bm, float c) {
+        const float nm = fmaxf(m, bm), Mo = m * c, M = nm * c;
+        const float2 c2 = make_float2(c, c);
+        LaneStat b;  // the sums of these units alone
+        const bool far = !near_frame(M) || (!near_frame(Mo) && Mo > M + kCut);
+        if (!__any_sync(0xffffffffu, far)) {
+            const float2 nM = make_float2(-M, -M);
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+#pragma unroll
+                for (int i = 0; i < (kBf16 ? 4 : 2); ++i) b.add(__ffma2_rn(pair<kBf16>(v[k], i), c2, nM), i);
+            // 2^d d of a masked token is 0 * -inf here: NaN says to take the longer way
+            if (!kT || !__any_sync(0xffffffffu, isnan((b.t0.x + b.t0.y) + (b.t1.x + b.t1.y)))) {
+                const float dm = fmaxf(Mo - M, kCut);
+                take(b, ex2(dm), dm);
+                m = nm;
+                return;
+            }
+            b = LaneStat();
+        }
+        const float before = frame_off(m, c), after = frame_off(nm, c), p = pivot(nm);
+        scale(ex2(-before), -before);
+        const float dm = max_nan((m - p) * c, kCut);
+        const float2 np = make_float2(-p, -p);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int i = 0; i < (kBf16 ? 4 : 2); ++i) {
+                float2 d = __fmul2_rn(__fadd2_rn(pair<kBf16>(v[k], i), np), c2);
+                d.x = max_nan(d.x, kCut);
+                d.y = max_nan(d.y, kCut);
+                b.add(d, i);
+            }
+        take(b, ex2(dm), dm);
         m = nm;
-        return p;
+        scale(ex2(after), after);
+    }
+
+    __device__ __forceinline__ RowStat row(float c) {
+        const float off = frame_off(m, c);
+        scale(ex2(-off), -off);
+        return RowStat{m, (s0.x + s0.y) + (s1.x + s1.y), (t0.x + t0.y) + (t1.x + t1.y)};
     }
 };
-
-__device__ __forceinline__ void add_pair(float x, float y, float2 np, float2 c2, float2& s, float2& t) {
-    float2 d = __fmul2_rn(__fadd2_rn(make_float2(x, y), np), c2);
-    d.x = max_nan(d.x, kCut);
-    d.y = max_nan(d.y, kCut);
-    const float2 e = make_float2(ex2(d.x), ex2(d.y));
-    s = __fadd2_rn(s, e);
-    t = __ffma2_rn(e, d, t);
-}
-
-template <bool kBf16>
-__device__ __forceinline__ void add_unit(const uint4& v, float2 np, float2 c2, LaneStat& a) {
-    if (kBf16) {
-        add_pair(bf16lo(v.x), bf16hi(v.x), np, c2, a.s0, a.t0);
-        add_pair(bf16lo(v.y), bf16hi(v.y), np, c2, a.s1, a.t1);
-        add_pair(bf16lo(v.z), bf16hi(v.z), np, c2, a.s0, a.t0);
-        add_pair(bf16lo(v.w), bf16hi(v.w), np, c2, a.s1, a.t1);
-    } else {
-        add_pair(__uint_as_float(v.x), __uint_as_float(v.y), np, c2, a.s0, a.t0);
-        add_pair(__uint_as_float(v.z), __uint_as_float(v.w), np, c2, a.s1, a.t1);
-    }
-}
-
-// Greatest logit of a unit (NaN is passed over: the sums show it).
-template <bool kBf16>
-__device__ __forceinline__ float unit_max(const uint4& v) {
-    if (kBf16) {
-        const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
-        const __nv_bfloat162 x = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
-        return fmaxf(__low2float(x), __high2float(x));
-    }
-    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
-}
 
 // A unit whose elements from `valid` on are -inf: they count nowhere.
 template <bool kBf16>
@@ -183,10 +254,53 @@ __device__ __forceinline__ float element(const uint4& v, int e) {
     return e & 1 ? bf16hi(w[e >> 1]) : bf16lo(w[e >> 1]);
 }
 
+// The same where e is not known to the compiler.
+template <bool kBf16>
+__device__ __forceinline__ float element_of(const uint4& v, int e) {
+    const int i = kBf16 ? e >> 1 : e;
+    const uint32_t lo = i & 1 ? v.y : v.x, hi = i & 1 ? v.w : v.z, w = i & 2 ? hi : lo;
+    if (!kBf16) return __uint_as_float(w);
+    return e & 1 ? bf16hi(w) : bf16lo(w);
+}
+
 template <bool kBf16>
 __device__ __forceinline__ float logit_at(const char* row, int v) {
     if (kBf16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[v]);
     return reinterpret_cast<const float*>(row)[v];
+}
+
+// A unit from fp32 values.
+template <bool kBf16>
+__device__ __forceinline__ void store_whole(char* p, const float (&x)[8]) {
+    uint4 o;
+    if (kBf16) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+    } else {
+        o = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+    __stcs(reinterpret_cast<uint4*>(p), o);
+}
+
+// Unit c of a row of V.
+template <bool kBf16>
+__device__ __forceinline__ void store_unit(char* row, int c, int V, const float (&x)[8]) {
+    constexpr int per = kBf16 ? 8 : 4;
+    char* p = row + (int64_t)c * 16;
+    if (V - c * per >= per) {
+        store_whole<kBf16>(p, x);
+    } else {  // the row's last, partial unit: what lies behind the vocabulary stays as it is
+#pragma unroll
+        for (int e = 0; e < per; ++e)
+            if (c * per + e < V) {
+                if (kBf16) reinterpret_cast<__nv_bfloat16*>(p)[e] = __float2bfloat16_rn(x[e]);
+                else reinterpret_cast<float*>(p)[e] = x[e];
+            }
+    }
 }
 
 }  // namespace estp

@@ -63,10 +63,11 @@ def test_kinds(cuda_lib, dtype, tail, kind, T):
     _check(cuda_lib.Context(0), R.logits(kind, 14, 1003, dtype), T, 16, tail, weight=False)
 
 
-def test_a_row_longer_than_the_bitmap(cuda_lib):
-    """More units than a block marks at a time."""
+@pytest.mark.parametrize("V", [300007, 500001])
+def test_long_rows(cuda_lib, V):
+    """The longest that a cluster keeps, and one of more units than a block marks at a time."""
     for tail in (False, True):
-        _check(cuda_lib.Context(0), R.logits("normal", 2, 300007, F32, seed=4), 1.0, 24, tail)
+        _check(cuda_lib.Context(0), R.logits("normal", 2, V, F32, seed=4), 1.0, 24, tail)
 
 
 def test_repeated_tokens(cuda_lib):
