@@ -594,44 +594,52 @@ class Context:
                                                budget, recent, sinks, _stream(stream)))
 
     # ------------------------------------------------------------------ (f)
-    def _here(self, **tensors):
-        """Each tensor (None passes) is on the context's device."""
-        for name, t in tensors.items():
-            if t is not None and t.get_device() != self.device:
-                raise ValueError(f"{name} is not on the context's device cuda:{self.device}")
-
     def _logits(self, logits, V):
         """Rows, V and row stride of logits [rows, >= V] whose rows are contiguous."""
-        if logits.dim() != 2 or (logits.numel() and logits.stride(1) != 1):
+        if logits.dim() != 2:
             raise ValueError("logits is a [rows, V] tensor with contiguous rows")
         rows, cols = logits.shape
-        V = cols if V is None else V
-        if not 1 <= V <= cols:
+        s0, s1 = logits.stride()
+        if s1 != 1 and rows and cols > 1:
+            raise ValueError("logits is a [rows, V] tensor with contiguous rows")
+        if logits.get_device() != self.device:
+            raise ValueError(f"logits is not on the context's device cuda:{self.device}")
+        if V is None:
+            V = cols
+        elif not 1 <= V <= cols:
             raise ValueError("V is in 1 .. the columns of logits")
-        return rows, V, logits.stride(0) if rows > 1 else cols + -cols % (16 // logits.element_size())
+        return rows, V, s0 if rows > 1 else cols + -cols % (16 // logits.element_size())
 
-    def _grad_like(self, logits, V, out, new):
+    def _is(self, t, dtype, shape, name):
+        """A dense tensor of this type and shape on the context's device."""
+        if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} is a contiguous {dtype} tensor of shape {shape}")
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} is not on the context's device cuda:{self.device}")
+        return t.data_ptr()
+
+    @staticmethod
+    def _empty(shape, dtype, device, stream):
+        """An output for work on `stream` (None: the current one)."""
+        import torch
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+    def _grad_out(self, logits, rows, V, out, stream):
         """Where the gradient of logits goes, [rows, V]: `out`, or a new tensor whose rows start on 16 bytes."""
         per = 16 // logits.element_size()
-        rows = logits.shape[0]
         if out is None:
-            wide = new((rows, V + -V % per), logits.dtype)
-            return wide[:, :V], wide.shape[1]
+            wide = V + -V % per
+            out = self._empty((rows, wide), logits.dtype, logits.device, stream)
+            return (out if wide == V else out[:, :V]), wide
         if out.dim() != 2 or out.shape[0] != rows or out.shape[1] < V or out.dtype != logits.dtype or (
                 out.numel() and out.stride(1) != 1):
             raise ValueError("out is a [rows, >= V] tensor of the logits' type with contiguous rows")
+        if out.get_device() != self.device:
+            raise ValueError(f"out is not on the context's device cuda:{self.device}")
         return out, out.stride(0) if rows > 1 else out.shape[1] + -out.shape[1] % per
-
-    def _new(self, device, stream):
-        """Allocates outputs for work on `stream` (None: the current one)."""
-        import torch
-        if stream is None:
-            return lambda shape, dtype: torch.empty(shape, dtype=dtype, device=device)
-
-        def new(shape, dtype):
-            with torch.cuda.stream(stream):
-                return torch.empty(shape, dtype=dtype, device=device)
-        return new
 
     def token_logprobs(self, logits, targets=None, top_k: int = 0, temperature: float = 1.0, V: int | None = None,
                        stream=None) -> TokenLogprobs:
@@ -639,16 +647,21 @@ class Context:
         the entropy, what the gradient needs, and the top_k greatest alternatives."""
         import torch
         rows, V, ld = self._logits(logits, V)
-        self._here(logits=logits, targets=targets)
+        f32, dev = torch.float32, logits.device
+        lp = ids = tops = tp = lpp = ip = kp = None
         if targets is not None:
-            _like(targets, torch.int32, (rows,), "targets")
-        f32, new = torch.float32, self._new(logits.device, stream)
-        lp = None if targets is None else new((rows,), f32)
-        entropy, norm = new((rows,), f32), new((rows, 2), f32)
-        ids, tops = (new((rows, top_k), torch.int32), new((rows, top_k), f32)) if top_k > 0 else (None, None)
-        self._check(self._lib.estp_token_logprobs(
-            self._h, logits.data_ptr(), _dtype(logits), rows, V, ld, _ptr(targets), temperature, top_k, _ptr(lp),
-            entropy.data_ptr(), norm.data_ptr(), _ptr(ids), _ptr(tops), _stream(stream)))
+            tp = self._is(targets, torch.int32, (rows,), "targets")
+            lp = self._empty((rows,), f32, dev, stream)
+            lpp = lp.data_ptr()
+        entropy, norm = self._empty((rows,), f32, dev, stream), self._empty((rows, 2), f32, dev, stream)
+        if top_k > 0:
+            ids, tops = self._empty((rows, top_k), torch.int32, dev, stream), self._empty((rows, top_k), f32, dev, stream)
+            ip, kp = ids.data_ptr(), tops.data_ptr()
+        status = self._lib.estp_token_logprobs(
+            self._h, logits.data_ptr(), _dtype(logits), rows, V, ld, tp, temperature, top_k, lpp, entropy.data_ptr(),
+            norm.data_ptr(), ip, kp, _stream(stream))
+        if status:
+            self._check(status)
         return TokenLogprobs(lp, entropy, norm, ids, tops, temperature)
 
     def token_logprobs_grad(self, logits, targets, lp: TokenLogprobs, grad_logprob=None, grad_entropy=None,
@@ -658,28 +671,28 @@ class Context:
         grad_entropy, grad_lse [rows] and grad_top [rows, top_k].  out: where it goes, logits itself allowed."""
         import torch
         rows, V, ld = self._logits(logits, V)
-        self._here(logits=logits, targets=targets, norm=lp.norm, entropy=lp.entropy, top_ids=lp.top_ids, out=out,
-                   grad_logprob=grad_logprob, grad_entropy=grad_entropy, grad_lse=grad_lse, grad_top=grad_top)
-        f32, k = torch.float32, 0
-        _like(lp.norm, f32, (rows, 2), "norm")
+        f32, per_row, k = torch.float32, (rows,), 0
+        norm = self._is(lp.norm, f32, (rows, 2), "norm")
+        tp = gp = hp = ep = sp = ap = ip = None
         if targets is not None:
-            _like(targets, torch.int32, (rows,), "targets")
-        _like(grad_logprob, f32, (rows,), "grad_logprob")
-        _like(grad_lse, f32, (rows,), "grad_lse")
+            tp = self._is(targets, torch.int32, per_row, "targets")
+        if grad_logprob is not None:
+            gp = self._is(grad_logprob, f32, per_row, "grad_logprob")
         if grad_entropy is not None:
-            _like(grad_entropy, f32, (rows,), "grad_entropy")
-            _like(lp.entropy, f32, (rows,), "entropy")
+            hp, ep = self._is(grad_entropy, f32, per_row, "grad_entropy"), self._is(lp.entropy, f32, per_row, "entropy")
+        if grad_lse is not None:
+            sp = self._is(grad_lse, f32, per_row, "grad_lse")
         if grad_top is not None:
             if lp.top_ids is None:
                 raise ValueError("grad_top needs the alternatives that it belongs to")
-            k = lp.top_ids.shape[1]
-            _like(lp.top_ids, torch.int32, (rows, k), "top_ids")
-            _like(grad_top, f32, (rows, k), "grad_top")
-        out, ldo = self._grad_like(logits, V, out, self._new(logits.device, stream))
-        self._check(self._lib.estp_token_logprobs_grad(
-            self._h, logits.data_ptr(), _dtype(logits), rows, V, ld, lp.norm.data_ptr(), _ptr(lp.entropy),
-            _ptr(targets), lp.temperature, k, _ptr(lp.top_ids), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(grad_lse),
-            _ptr(grad_top), out.data_ptr(), ldo, _stream(stream)))
+            k = lp.top_ids.shape[-1]
+            ip, ap = self._is(lp.top_ids, torch.int32, (rows, k), "top_ids"), self._is(grad_top, f32, (rows, k), "grad_top")
+        out, ldo = self._grad_out(logits, rows, V, out, stream)
+        status = self._lib.estp_token_logprobs_grad(
+            self._h, logits.data_ptr(), _dtype(logits), rows, V, ld, norm, ep, tp, lp.temperature, k, ip, gp, hp, sp, ap,
+            out.data_ptr(), ldo, _stream(stream))
+        if status:
+            self._check(status)
         return out
 
     def distill_loss(self, logits, teacher_ids, teacher_logits, temperature: float = 1.0, tail: bool = False,
@@ -691,18 +704,17 @@ class Context:
         gradient goes, logits itself allowed."""
         import torch
         rows, V, ld = self._logits(logits, V)
-        self._here(logits=logits, teacher_ids=teacher_ids, teacher_logits=teacher_logits, row_weight=row_weight, out=out)
         K = teacher_ids.shape[-1]
-        _like(teacher_ids, torch.int32, (rows, K), "teacher_ids")
-        _like(teacher_logits, torch.float32, (rows, K), "teacher_logits")
-        if row_weight is not None:
-            _like(row_weight, torch.float32, (rows,), "row_weight")
-        new = self._new(logits.device, stream)
-        loss, gp, ldo = new((rows,), torch.float32), None, 0
+        ip = self._is(teacher_ids, torch.int32, (rows, K), "teacher_ids")
+        xp = self._is(teacher_logits, torch.float32, (rows, K), "teacher_logits")
+        wp = None if row_weight is None else self._is(row_weight, torch.float32, (rows,), "row_weight")
+        loss, gp, ldo = self._empty((rows,), torch.float32, logits.device, stream), None, 0
         if grads:
-            out, ldo = self._grad_like(logits, V, out, new)
+            out, ldo = self._grad_out(logits, rows, V, out, stream)
             gp = out.data_ptr()
-        self._check(self._lib.estp_distill_loss(
-            self._h, logits.data_ptr(), _dtype(logits), rows, V, ld, teacher_ids.data_ptr(), teacher_logits.data_ptr(),
-            K, temperature, 1 if tail else 0, _ptr(row_weight), loss.data_ptr(), gp, ldo, _stream(stream)))
+        status = self._lib.estp_distill_loss(
+            self._h, logits.data_ptr(), _dtype(logits), rows, V, ld, ip, xp, K, temperature, 1 if tail else 0, wp,
+            loss.data_ptr(), gp, ldo, _stream(stream))
+        if status:
+            self._check(status)
         return (loss, out) if grads else loss

@@ -40,6 +40,8 @@ estp_status cuda_fail(cudaError_t e, const char* what) {
 }
 
 estp_status set_device(estp_ctx* ctx) {
+    int now = -1;  // (asking takes less than setting)
+    if (cudaGetDevice(&now) == cudaSuccess && now == ctx->device) return ESTP_OK;
     cudaError_t e = cudaSetDevice(ctx->device);
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cudaSetDevice");
 }
@@ -121,13 +123,16 @@ estp_status estp_create(estp_ctx** out, int device) {
     // the log probability kernels' parts and lists: a bound of what any call needs (7.7 MB), so that no
     // call allocates and a captured one keeps its buffers whatever comes after it
     const size_t slots = 2 * (size_t)ctx->num_sms * kVocabBlocks * (kVocabThreads / 32);
-    e = cudaMalloc(&ctx->vocab_part, slots * (sizeof(float4) + kMaxAlternatives * sizeof(uint64_t)));
+    e = cudaMalloc(&ctx->vocab_part, slots * (sizeof(float4) + kMaxAlternatives * sizeof(uint64_t) + sizeof(uint32_t)));
+    ctx->vocab_lists = reinterpret_cast<uint64_t*>(ctx->vocab_part + slots);
+    ctx->vocab_count = reinterpret_cast<uint32_t*>(ctx->vocab_lists + slots * kMaxAlternatives);
+    if (e == cudaSuccess) e = cudaMemset(ctx->vocab_count, 0, slots * sizeof(uint32_t));
     if (e != cudaSuccess) {
+        cudaFree(ctx->vocab_part);
         cudaFree(ctx->status);
         delete ctx;
         return cuda_fail(e, "log probability workspace");
     }
-    ctx->vocab_lists = reinterpret_cast<uint64_t*>(ctx->vocab_part + slots);
     ctx->done = reinterpret_cast<uint32_t*>(ctx->status) + 32;
     ctx->timed_out = ctx->status + 48;
     *out = ctx;

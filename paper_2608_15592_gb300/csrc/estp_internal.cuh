@@ -33,6 +33,7 @@ struct estp_ctx {
     int32_t pool_done_cap = 0;
     float4* vocab_part = nullptr;    // parts of rows cut between warps, two a piece (log probabilities)
     uint64_t* vocab_lists = nullptr; // and their lists of alternatives; a fixed size, from estp_create on
+    uint32_t* vocab_count = nullptr; // arrival counters of rows (zero between launches)
     int distill_clusters[4][3][8] = {};  // clusters the GPU holds at once, by kernel, CTAs an SM and cluster size
     uint32_t distill_set = 0;            // distillation kernels whose shared memory limit is set, a bit each
     uint32_t smem_set = 0;      // cache kernels whose shared memory limit is set on the device, a bit each

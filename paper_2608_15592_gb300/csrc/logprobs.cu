@@ -4,7 +4,8 @@
 // logprobs_kernel streams the logits once: a warp takes one of the equal pieces of the flat run of
 // 16-byte units (vocab.cuh), keeps (m, s, t) per lane and, where alternatives are asked for, the
 // list of the 32 R greatest logits it has met.  A row that lies within a piece is finished by its warp; of a
-// row cut between warps each writes its part, and logprobs_join_kernel joins the parts in order.
+// row cut between warps each writes its part (a block that lies in one row one part), and whoever writes a
+// row's last part joins all of them, in an order that does not depend on who that is.
 //
 // The list.  A candidate is a 64-bit key: the logit's bits in the order of the numbers above the token's
 // index, inverted; so keys are unique, a greater key is a greater logit or the same one at a lower
@@ -34,40 +35,41 @@ __device__ __forceinline__ float key_logit(uint64_t k) { return unordered((uint3
 __device__ __forceinline__ int key_token(uint64_t k) { return (int)(0xFFFFFFFFu - (uint32_t)k); }
 
 // 32 R keys a warp, key i in register i / 32 of lane i % 32 (0: none).
-// One step of a bitonic network: keys i and i ^ j, the greater one to the lower index where
-// bit `size` of i is clear.
+// The steps j, j / 2, .. 1 of a bitonic network: keys i and i ^ j, the greater one to the lower index
+// where bit `size` of i is clear.  (Loops, not unrolled: this code runs seldom, between code that
+// should stay in the instruction cache.)
 template <int R>
-__device__ __forceinline__ void exchange(uint64_t (&x)[R], int size, int j, int lane) {
-    if (j < 32) {
+__device__ __forceinline__ void exchanges(uint64_t (&x)[R], int size, int j, int lane) {
+#pragma unroll
+    for (int w = R / 2; w > 0; w /= 2)
+        if (32 * w <= j) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if ((r & w) == 0) {
+                    const bool down = (r * 32 & size) != 0;
+                    const uint64_t a = x[r], b = x[r | w];
+                    if ((a < b) != down) {
+                        x[r] = b;
+                        x[r | w] = a;
+                    }
+                }
+        }
+#pragma unroll 1
+    for (j = j < 16 ? j : 16; j > 0; j >>= 1) {
+        const bool low = (lane & j) == 0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const uint64_t y = __shfl_xor_sync(0xffffffffu, x[r], j);
-            const int i = r * 32 + lane;
-            const bool up = ((i & size) == 0) == ((i & j) == 0);
+            const bool up = (((r * 32 + lane) & size) == 0) == low;
             x[r] = (x[r] > y) == up ? x[r] : y;
-        }
-    } else {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int o = r ^ (j / 32);
-            if (o > r) {
-                const bool down = (r * 32 & size) != 0;
-                const uint64_t a = x[r], b = x[o];
-                if ((a < b) != down) {
-                    x[r] = b;
-                    x[o] = a;
-                }
-            }
         }
     }
 }
 
 template <int R>
 __device__ __forceinline__ void sort_keys(uint64_t (&x)[R], int lane) {
-#pragma unroll
-    for (int size = 2; size <= 32 * R; size *= 2)
-#pragma unroll
-        for (int j = size / 2; j > 0; j /= 2) exchange<R>(x, size, j, lane);
+#pragma unroll 1
+    for (int size = 2; size <= 32 * R; size *= 2) exchanges<R>(x, size, size / 2, lane);
 }
 
 // The greatest 32 R of two descending lists, descending.
@@ -78,8 +80,7 @@ __device__ __forceinline__ void merge_keys(uint64_t (&x)[R], const uint64_t (&y)
         const uint64_t o = __shfl_sync(0xffffffffu, y[R - 1 - r], 31 - lane);
         x[r] = x[r] > o ? x[r] : o;
     }
-#pragma unroll
-    for (int j = 16 * R; j > 0; j /= 2) exchange<R>(x, 64 * R, j, lane);
+    exchanges<R>(x, 64 * R, 16 * R, lane);
 }
 
 // The same of two lists in shared memory, into the first.
@@ -103,7 +104,7 @@ struct Candidates {
     static constexpr int kBatch = 32 * R;
     uint64_t list[kBatch];
     uint64_t waiting[kBatch + 256];  // a unit of each lane goes in before the count is looked at again
-    uint32_t units[64];              // a batch adds up to 32, and 32 are taken at once
+    uint32_t units[32 + 32 * kVocabUnroll];  // a batch adds up to 32 kVocabUnroll; they are taken by 32
     int count, n_units;
 };
 
@@ -131,60 +132,68 @@ __device__ __noinline__ void take_waiting(Candidates<R>* q, int top_k, bool all)
     __syncwarp();
 }
 
-// Looks at the units that wait, one a lane at a time (their second read comes from L2), and returns the
-// bound for the tokens that follow all of them.
+// Looks at the units that wait (from the segment's first one, c0, on), one a lane (their second read comes from
+// L2): whole 32s of them or all.  Candidates are at least `floor`; returns the bound for the tokens that follow.
 template <bool kBf16, int R>
-__device__ __noinline__ float take_units(Candidates<R>* q, const char* row, int c0, int limit, int top_k, float bound,
-                                         int* status) {
+__device__ __noinline__ float take_units(Candidates<R>* q, const char* row, int c0, int limit, int top_k, float floor,
+                                         bool all, int* status) {
     constexpr int per = kBf16 ? 8 : 4;
-    const int lane = threadIdx.x & 31, n = q->n_units;
+    const int lane = threadIdx.x & 31;
+    int n = q->n_units;
     // these units are not in the order of the tokens: an equal of the list's last may come before it or after
     uint64_t last = q->list[top_k - 1];
-    float cut = last ? fmaxf(bound, key_logit(last)) : bound;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const uint32_t mine = i0 + lane < n ? q->units[i0 + lane] : 0;
-        uint32_t hits = mine & ((1u << kVocabUnroll) - 1);
-        const int place = c0 + (int)(mine >> kVocabUnroll);
-        while (__any_sync(0xffffffffu, hits != 0)) {
-            if (hits) {
-                const int c = place + 32 * (__ffs(hits) - 1), first = c * per;
-                hits &= hits - 1;
-                if (first < limit) {  // (a lane past the segment marks its -inf where there is no bound yet)
-                    const uint4 u = ld_stream(row + (int64_t)c * 16);
-                    uint32_t in = 0;
+    float cut = last ? fmaxf(floor, key_logit(last)) : floor;
+    while (n >= 32 || (all && n > 0)) {
+        const int take = n < 32 ? n : 32;
+        n -= take;
+        if (lane < take) {
+            const int c = c0 + (int)q->units[n + lane], first = c * per;
+            if (first < limit) {  // (a lane past the segment marks its -inf where there is no bound yet)
+                const uint4 u = ld_stream(row + (int64_t)c * 16);
+                uint32_t in = 0;
 #pragma unroll
-                    for (int e = 0; e < per; ++e) in |= element<kBf16>(u, e) >= cut ? 1u << e : 0u;
-                    if (limit - first < per) in &= (1u << (limit - first)) - 1;
-                    if (last && key_logit(last) == cut) {
-                        const int before = key_token(last) - first;  // tokens of the unit that come before the last
-                        uint32_t equal = 0;
+                for (int e = 0; e < per; ++e) in |= element<kBf16>(u, e) >= cut ? 1u << e : 0u;
+                if (limit - first < per) in &= (1u << (limit - first)) - 1;
+                if (last && key_logit(last) == cut) {
+                    const int before = key_token(last) - first;  // tokens of the unit that come before the last
+                    uint32_t equal = 0;
 #pragma unroll
-                        for (int e = 0; e < per; ++e) equal |= element<kBf16>(u, e) == cut ? 1u << e : 0u;
-                        if (before < per) in &= ~equal | (before > 0 ? (1u << before) - 1 : 0u);
-                    }
-                    if (in) {
-                        int at = atomicAdd(&q->count, __popc(in));
-                        do {
-                            const int e = __ffs(in) - 1;
-                            in &= in - 1;
-                            if (in_bounds(at < 32 * R + 256, status)) q->waiting[at] = key_of(element_of<kBf16>(u, e), first + e);
-                            ++at;
-                        } while (in);
-                    }
+                    for (int e = 0; e < per; ++e) equal |= element<kBf16>(u, e) == cut ? 1u << e : 0u;
+                    if (before < per) in &= ~equal | (before > 0 ? (1u << before) - 1 : 0u);
+                }
+                if (in) {
+                    int at = atomicAdd(&q->count, __popc(in));
+                    do {
+                        const int e = __ffs(in) - 1;
+                        in &= in - 1;
+                        if (in_bounds(at < 32 * R + 256, status)) q->waiting[at] = key_of(element_of<kBf16>(u, e), first + e);
+                        ++at;
+                    } while (in);
                 }
             }
-            __syncwarp();
-            if (q->count >= 32 * R) {
-                take_waiting<R>(q, top_k, false);
-                last = q->list[top_k - 1];
-                if (last) cut = fmaxf(cut, key_logit(last));
-            }
-            __syncwarp();
         }
+        __syncwarp();
+        if (q->count >= 32 * R) {
+            take_waiting<R>(q, top_k, false);
+            last = q->list[top_k - 1];
+            if (last) cut = fmaxf(cut, key_logit(last));
+        }
+        __syncwarp();
     }
-    if (lane == 0) q->n_units = 0;
+    if (lane == 0) q->n_units = n;
     __syncwarp();
-    return last ? fmaxf(bound, unordered((uint32_t)(last >> 32) + 1)) : bound;  // the next number above it
+    return last ? fmaxf(floor, unordered((uint32_t)(last >> 32) + 1)) : floor;  // the next number above it
+}
+
+// The lists of a block's warps merged into the first one's, by pairs (the whole block).
+template <int R>
+__device__ __forceinline__ void merge_block(Candidates<R>* cand) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll 1
+    for (int half = kWarps / 2; half > 0; half /= 2) {
+        if (warp < half) merge_lists<R>(cand[warp].list, cand[warp + half].list, lane);
+        __syncthreads();
+    }
 }
 
 // A logit that at least top_k of the warp's 32 G values reach (or -inf): the order bits from the top
@@ -219,8 +228,11 @@ struct LpArgs {
     float2* norm;
     int32_t* top_ids;
     float* top_logprobs;
-    float4* part;      // [pieces][2]: m, s, t of a piece's first and last row
-    uint64_t* lists;   // [pieces][2][32 R]
+    int blocks, span;  // few rows: blocks a row and units a warp (0: equal pieces)
+    float4* part;      // [slots]: m, s, t of a part: two a piece, for its first and its last row, or one a block
+    uint64_t* lists;   // [slots][32 R]
+    uint32_t* count;   // [slots]: parts that have arrived of a row, by its first piece or its index
+    int64_t slots;
     int* status;
 };
 
@@ -232,7 +244,7 @@ __device__ __forceinline__ RowStat stream_row(const LpArgs& a, const char* row, 
     const int limit = min(V, c1 * per);                  // tokens of the segment end here
     const int whole = min(c1, V / per);                  // units before a partial one
     LaneStat<true> st;
-    float bound = -INFINITY;
+    float floor = -INFINITY, bound = -INFINITY;
     for (int b = c0; b < c1; b += 32 * kVocabUnroll) {
         uint4 v[kVocabUnroll];
         const int c = b + lane;
@@ -251,31 +263,52 @@ __device__ __forceinline__ RowStat stream_row(const LpArgs& a, const char* row, 
                 float g[G];
 #pragma unroll
                 for (int i = 0; i < G; ++i) g[i] = units_max<kBf16, w>(v + i * w);
-                bound = reached_by<G>(g, a.top_k);
+                floor = bound = reached_by<G>(g, a.top_k);
             }
-            // a lane with candidates leaves its place and a bit for each unit that holds one
+            // units with candidates are queued; the longer part waits until the batch is in the sums
             if (__any_sync(0xffffffffu, bm >= bound)) {
                 uint32_t hits = 0;
 #pragma unroll
                 for (int k = 0; k < kVocabUnroll; ++k) hits |= units_max<kBf16, 1>(v + k) >= bound ? 1u << k : 0u;
-                if (hits) q->units[atomicAdd(&q->n_units, 1)] = (uint32_t)(c - c0) << kVocabUnroll | hits;
-                __syncwarp();
-                if (q->n_units >= 32) bound = take_units<kBf16, R>(q, row, c0, limit, a.top_k, bound, a.status);
+                if (hits)
+                    for (int at = atomicAdd(&q->n_units, __popc(hits)); hits; hits &= hits - 1, ++at)
+                        if (in_bounds(at < 32 + 32 * kVocabUnroll, a.status)) q->units[at] = (uint32_t)(c - c0 + 32 * (__ffs(hits) - 1));
                 __syncwarp();
             }
         }
         st.template add_units<kBf16>(v, bm, a.c);
+        if constexpr (R > 0) {
+            if (q->n_units >= 32) bound = take_units<kBf16, R>(q, row, c0, limit, a.top_k, floor, false, a.status);
+            __syncwarp();
+        }
     }
     if constexpr (R > 0) {
-        take_units<kBf16, R>(q, row, c0, limit, a.top_k, bound, a.status);
+        take_units<kBf16, R>(q, row, c0, limit, a.top_k, floor, true, a.status);
         take_waiting<R>(q, a.top_k, true);
     }
     return st.row(a.c);
 }
 
+// A row's target and the bits of its logit, asked for where the row begins (lane 0).
+struct Target {
+    int t;
+    uint32_t z;
+};
+
+template <bool kBf16>
+__device__ __forceinline__ Target ask_target(const LpArgs& a, int64_t r, const char* row) {
+    Target x{-1, 0u};
+    if (a.logprob && (threadIdx.x & 31) == 0 && in_bounds(r < a.rows.n_rows, a.status)) {
+        x.t = a.targets[r];
+        if (x.t >= 0 && x.t < a.rows.V)
+            x.z = kBf16 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[x.t] : reinterpret_cast<const uint32_t*>(row)[x.t];
+    }
+    return x;
+}
+
 // What a row's statistics and list say, written by a warp.
 template <bool kBf16, int R>
-__device__ __forceinline__ void write_row(const LpArgs& a, int64_t r, const char* row, const RowStat& st,
+__device__ __forceinline__ void write_row(const LpArgs& a, int64_t r, const Target& x, const RowStat& st,
                                           const uint64_t* list) {
     const int lane = threadIdx.x & 31;
     if (!in_bounds(r >= 0 && r < a.rows.n_rows, a.status)) return;
@@ -285,13 +318,10 @@ __device__ __forceinline__ void write_row(const LpArgs& a, int64_t r, const char
         if (a.entropy) a.entropy[r] = empty ? 0.f : ls - kLn2 * (st.t / st.s);
         if (a.norm) a.norm[r] = make_float2(st.m, st.s);
         if (a.logprob) {
-            const int t = a.targets[r];
-            float lp = 0.f;
-            if (t >= a.rows.V) {
+            float lp = x.t < 0 ? 0.f : (__uint_as_float(kBf16 ? x.z << 16 : x.z) - m) / a.T - ls;
+            if (x.t >= a.rows.V) {
                 report(a.status, ESTP_ERR_INVALID_ARG);
                 lp = NAN;
-            } else if (t >= 0) {
-                lp = (logit_at<kBf16>(row, t) - m) / a.T - ls;
             }
             a.logprob[r] = lp;
         }
@@ -308,156 +338,170 @@ __device__ __forceinline__ void write_row(const LpArgs& a, int64_t r, const char
     }
 }
 
-// The row that all of block b's pieces lie in, or -1: its warps then join their parts themselves.
-__device__ __forceinline__ int64_t row_of_block(const VocabRows& a, int64_t b) {
-    const int64_t lo = b * kWarps, hi = lo + kWarps < a.pieces ? lo + kWarps : a.pieces;
-    const int64_t r = piece_start(a, lo) / a.nvec;
-    return (piece_start(a, hi) - 1) / a.nvec == r ? r : -1;
+// A part of a row goes to its slot (a warp).
+template <int R>
+__device__ __forceinline__ void put_part(const LpArgs& a, int64_t slot, const RowStat& st, const uint64_t* list) {
+    const int lane = threadIdx.x & 31;
+    if (!in_bounds(slot >= 0 && slot < a.slots, a.status)) return;
+    if (lane == 0) a.part[slot] = make_float4(st.m, st.s, st.t, 0.f);
+    if constexpr (R > 0)
+        for (int i = lane; i < 32 * R; i += 32) a.lists[slot * (32 * R) + i] = list[i];
 }
 
+// A part has been written (by the whole warp): whether it is the last of the row's n.  The counter is zero
+// between launches.
+__device__ __forceinline__ bool arrive(const LpArgs& a, int64_t counter, int n) {
+    uint32_t last = 0;
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0 && in_bounds(counter >= 0 && counter < a.slots, a.status)) {
+        __threadfence();
+        last = atomicAdd(&a.count[counter], 1u) == (uint32_t)n - 1 ? 1u : 0u;
+        if (last) a.count[counter] = 0;
+        __threadfence();
+    }
+    return __shfl_sync(0xffffffffu, last, 0) != 0;
+}
+
+// The statistics of a row's n parts, part 0 in `slot0` and the others from `slot` on, `step` apart: joined in one
+// order whichever warp does it.
+__device__ __forceinline__ RowStat join_parts(const LpArgs& a, int64_t slot0, int64_t slot, int step, int n) {
+    RowStat st = no_stat();
+    for (int i = threadIdx.x & 31; i < n; i += 32) {
+        const float4 x = __ldcg(&a.part[i ? slot + (int64_t)(i - 1) * step : slot0]);
+        join(st, RowStat{x.x, x.y, x.z}, a.c);
+    }
+    __syncwarp();
+    join_lanes(st, a.c);
+    return st;
+}
+
+// The lists of parts i0, i0 + by, .. merged into `list` (keys all differ: any order gives the same).
+template <int R>
+__device__ __forceinline__ void merge_parts(const LpArgs& a, int64_t slot0, int64_t slot, int step, int n, int i0, int by,
+                                            uint64_t* list) {
+    const int lane = threadIdx.x & 31;
+    uint64_t x[R], y[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) x[k] = y[k] = 0;
+#pragma unroll 1
+    for (int i = i0; i < n + by; i += by) {  // the next part loads while this one is merged
+        uint64_t z[R];
+        const int64_t at = (i ? slot + (int64_t)(i - 1) * step : slot0) * (32 * R);
+#pragma unroll
+        for (int k = 0; k < R; ++k) z[k] = i < n ? __ldcg(&a.lists[at + k * 32 + lane]) : 0;
+        if (i > i0) merge_keys<R>(x, y, lane);
+#pragma unroll
+        for (int k = 0; k < R; ++k) y[k] = z[k];
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) list[k * 32 + lane] = x[k];
+    __syncwarp();
+}
+
+template <int R>
+__device__ __forceinline__ void clear_list(Candidates<R>* q) {
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+    for (int i = lane; i < 32 * R; i += 32) q->list[i] = 0;
+    if (lane == 0) q->count = q->n_units = 0;
+    __syncwarp();
+}
+
+// Many rows: a warp an equal piece of the flat run.
 template <bool kBf16, int R>
 __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(const LpArgs a) {
     constexpr int kLists = R ? R : 1;
     __shared__ Candidates<kLists> cand[R ? kWarps : 1];
-    __shared__ RowStat stats[kWarps];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join may be scheduled
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int warp = threadIdx.x >> 5;
     const int64_t w = (int64_t)blockIdx.x * kWarps + warp;
-    const bool one_row = row_of_block(a.rows, blockIdx.x) >= 0;
+    if (w >= a.rows.pieces) return;
     Candidates<kLists>* q = R ? &cand[warp] : nullptr;
-    const int64_t start = w < a.rows.pieces ? piece_start(a.rows, w) : 0, end = w < a.rows.pieces ? piece_start(a.rows, w + 1) : 0;
-    RowStat st = no_stat();
-    if (R > 0 && start == end) {
-        for (int i = lane; i < 32 * R; i += 32) q->list[i] = 0;
-        __syncwarp();
-    }
+    const int64_t start = piece_start(a.rows, w), end = piece_start(a.rows, w + 1);
     for (int64_t u = start; u < end;) {
         const int64_t r = u / a.rows.nvec, u0 = r * a.rows.nvec;
         const int c0 = (int)(u - u0), c1 = (int)(min(end, u0 + a.rows.nvec) - u0);
         const char* row = a.rows.base + r * a.rows.ld_bytes;
+        const Target x = ask_target<kBf16>(a, r, row);
+        RowStat st;
         if constexpr (R > 0) {
-            __syncwarp();
-            for (int i = lane; i < 32 * R; i += 32) q->list[i] = 0;
-            if (lane == 0) q->count = q->n_units = 0;
-            __syncwarp();
-        }
-        if constexpr (R > 0) st = stream_row<kBf16, R>(a, row, c0, c1, q);
-        else st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);
-        join_lanes(st, a.c);
-        if (one_row) break;
-        if (c0 == 0 && c1 == a.rows.nvec) {
-            write_row<kBf16, R>(a, r, row, st, R ? q->list : nullptr);
+            clear_list<R>(q);
+            st = stream_row<kBf16, R>(a, row, c0, c1, q);
         } else {
-            const int64_t slot = w * 2 + (u == start ? 0 : 1);
-            if (lane == 0) a.part[slot] = make_float4(st.m, st.s, st.t, 0.f);
-            if constexpr (R > 0)
-                for (int i = lane; i < 32 * R; i += 32) a.lists[slot * (32 * R) + i] = q->list[i];
+            st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);
         }
+        join_lanes(st, a.c);
+        bool write = true;
+        if (c0 != 0 || c1 != a.rows.nvec) {
+            put_part<R>(a, w * 2 + (u == start ? 0 : 1), st, R ? q->list : nullptr);
+            // the row's pieces lo .. hi; only the first may begin in the row before it
+            const int64_t lo = piece_of(a.rows, u0), hi = piece_of(a.rows, u0 + a.rows.nvec - 1);
+            const int64_t slot0 = lo * 2 + (piece_start(a.rows, lo) < u0 ? 1 : 0);
+            const int n = (int)(hi - lo + 1);
+            write = arrive(a, lo, n);
+            if (write) {
+                st = join_parts(a, slot0, lo * 2 + 2, 2, n);
+                if constexpr (R > 0) merge_parts<R>(a, slot0, lo * 2 + 2, 2, n, 0, 1, q->list);
+            }
+        }
+        if (write) write_row<kBf16, R>(a, r, x, st, R ? q->list : nullptr);
         u = u0 + c1;
-    }
-    if (!one_row) return;
-    // pairs of warps, the lower half taking from the upper one
-    for (int half = kWarps / 2; half > 0; half /= 2) {
-        if (lane == 0) stats[warp] = st;
-        __syncthreads();
-        if (warp < half) {
-            join(st, stats[warp + half], a.c);
-            if constexpr (R > 0) merge_lists<R>(q->list, cand[warp + half].list, lane);
-        }
-        __syncthreads();
-    }
-    if (warp != 0) return;
-    const int64_t r = start / a.rows.nvec, lo = blockIdx.x * (int64_t)kWarps;
-    const int64_t next = piece_start(a.rows, lo + kWarps < a.rows.pieces ? lo + kWarps : a.rows.pieces);
-    if (start == r * a.rows.nvec && next == start + a.rows.nvec) {
-        write_row<kBf16, R>(a, r, a.rows.base + r * a.rows.ld_bytes, st, R ? q->list : nullptr);
-    } else {  // in the place of the block's first piece
-        if (lane == 0) a.part[w * 2] = make_float4(st.m, st.s, st.t, 0.f);
-        if constexpr (R > 0)
-            for (int i = lane; i < 32 * R; i += 32) a.lists[w * 2 * (32 * R) + i] = q->list[i];
     }
 }
 
-// Rows cut between pieces, `warps` warps a row (1 or all of the block's): each joins the parts of every
-// warps-th block of the forward in order, then pairs of warps join what they have.
+// Few rows: a.blocks blocks a row, whose warps join their parts themselves.
 template <bool kBf16, int R>
-__global__ void __launch_bounds__(kVocabThreads) logprobs_join_kernel(const LpArgs a, int warps) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the parts are complete
-    constexpr int kList = R ? 32 * R : 1;
-    __shared__ uint64_t lists[kWarps][kList];
+__global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_few_kernel(const LpArgs a) {
+    constexpr int kLists = R ? R : 1;
+    __shared__ Candidates<kLists> cand[R ? kWarps : 1];
     __shared__ RowStat stats[kWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % warps;
-    const int64_t r = ((int64_t)blockIdx.x * kWarps + warp) / warps;
-    int64_t lo = 0, hi = 0;
-    bool cut = false;
-    if (r < a.rows.n_rows) {
-        lo = piece_of(a.rows, r * a.rows.nvec);
-        hi = piece_of(a.rows, (r + 1) * a.rows.nvec - 1);
-        // one piece that held the whole row has written it, or one block
-        cut = lo < hi;
-        if (cut && lo / kWarps == hi / kWarps && row_of_block(a.rows, lo / kWarps) == r &&
-            piece_start(a.rows, lo / kWarps * kWarps) == r * a.rows.nvec &&
-            piece_start(a.rows, min((lo / kWarps + 1) * kWarps, a.rows.pieces)) == (r + 1) * a.rows.nvec)
-            cut = false;
-    }
+    __shared__ int last;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int r = blockIdx.x / a.blocks, b = blockIdx.x - r * a.blocks;
+    const char* row = a.rows.base + r * a.rows.ld_bytes;
+    Candidates<kLists>* q = R ? &cand[warp] : nullptr;
+    Target x{-1, 0u};
+    if (warp == 0) x = ask_target<kBf16>(a, r, row);
+    const int c0 = min(a.rows.nvec, (b * kWarps + warp) * a.span), c1 = min(a.rows.nvec, c0 + a.span);
     RowStat st = no_stat();
-    uint64_t x[R ? R : 1];
-#pragma unroll
-    for (int i = 0; i < (R ? R : 1); ++i) x[i] = 0;
-    auto take = [&](int64_t slot) {
-        const float4 p = a.part[slot];
-        if constexpr (R > 0) {
-            uint64_t y[R];
-#pragma unroll
-            for (int i = 0; i < R; ++i) y[i] = a.lists[slot * kList + i * 32 + lane];
-            merge_keys<R>(x, y, lane);
-        }
-        join(st, RowStat{p.x, p.y, p.z}, a.c);
-    };
-    if (cut) {
-        for (int64_t b = lo / kWarps + sub; b <= hi / kWarps; b += warps) {
-            if (row_of_block(a.rows, b) == r) {
-                take(b * kWarps * 2);
-            } else {
-                const int64_t last = min(hi, (b + 1) * kWarps - 1);
-                for (int64_t w = b * kWarps > lo ? b * kWarps : lo; w <= last; ++w)
-                    take(w * 2 + (piece_start(a.rows, w) / a.rows.nvec == r ? 0 : 1));
-            }
-        }
+    if constexpr (R > 0) {
+        clear_list<R>(q);
+        if (c0 < c1) st = stream_row<kBf16, R>(a, row, c0, c1, q);
+    } else {
+        if (c0 < c1) st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);
     }
-    if (R > 0) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) lists[warp][i * 32 + lane] = x[i];
-        __syncwarp();
+    join_lanes(st, a.c);
+    if (lane == 0) stats[warp] = st;
+    __syncthreads();
+    if constexpr (R > 0) merge_block<R>(cand);
+    const int64_t slot = (int64_t)r * a.blocks;
+    if (warp == 0) {
+        st = lane < kWarps ? stats[lane] : no_stat();
+        join_lanes(st, a.c);
+        bool l = false;
+        if (a.blocks > 1) {
+            put_part<R>(a, blockIdx.x, st, R ? q->list : nullptr);
+            l = arrive(a, r, a.blocks);
+        } else {
+            write_row<kBf16, R>(a, r, x, st, R ? q->list : nullptr);
+        }
+        if (lane == 0) last = l;
     }
-    for (int half = warps / 2; half > 0; half /= 2) {  // (warps is the same for the whole grid)
-        if (lane == 0) stats[warp] = st;
+    if (a.blocks == 1) return;
+    __syncthreads();
+    if (!last) return;
+    if constexpr (R > 0) {
+        merge_parts<R>(a, slot, slot + 1, 1, a.blocks, warp, kWarps, q->list);
         __syncthreads();
-        if (warp < half && cut) {
-            join(st, stats[warp + half], a.c);
-            if constexpr (R > 0) merge_lists<R>(lists[warp], lists[warp + half], lane);
-        }
-        __syncthreads();
+        merge_block<R>(cand);
     }
-    if (cut && sub == 0) write_row<kBf16, R>(a, r, a.rows.base + r * a.rows.ld_bytes, st, lists[warp]);
+    if (warp == 0) write_row<kBf16, R>(a, r, x, join_parts(a, slot, slot + 1, 1, a.blocks), R ? q->list : nullptr);
 }
 
 template <bool kBf16, int R>
 cudaError_t launch_forward(const LpArgs& a, cudaStream_t st) {
-    logprobs_kernel<kBf16, R><<<(unsigned)((a.rows.pieces + kWarps - 1) / kWarps), kVocabThreads, 0, st>>>(a);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    const int warps = a.rows.pieces > 4 * a.rows.n_rows ? kWarps : 1;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((a.rows.n_rows * warps + kWarps - 1) / kWarps));
-    cfg.blockDim = dim3(kVocabThreads);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, logprobs_join_kernel<kBf16, R>, a, warps);
+    if (a.blocks) logprobs_few_kernel<kBf16, R><<<(unsigned)(a.rows.n_rows * a.blocks), kVocabThreads, 0, st>>>(a);
+    else logprobs_kernel<kBf16, R><<<(unsigned)((a.rows.pieces + kWarps - 1) / kWarps), kVocabThreads, 0, st>>>(a);
+    return cudaGetLastError();
 }
 
 template <bool kBf16>
@@ -694,6 +738,21 @@ estp_status launch_token_logprobs(estp_ctx* ctx, const void* logits, estp_dtype 
                                   cudaStream_t st) {
     LpArgs a;
     a.rows = vocab_rows(ctx, logits, dtype, n_rows, V, ld, 32 * kVocabUnroll, kVocabBlocks);
+    const int64_t most = (int64_t)ctx->num_sms * kVocabBlocks;  // blocks at once
+    a.slots = 2 * most * kWarps;
+    a.blocks = a.span = 0;
+    if (n_rows <= most / 2) {
+        // Blocks a row: two for every place on the GPU between all rows, a batch a warp at least.  One row of 152064
+        // tokens with 20 alternatives takes NN us, by equal pieces and a second launch that joined them 19.
+        const int64_t batches = ((int64_t)a.rows.nvec + kWarps * 32 * kVocabUnroll - 1) / (kWarps * 32 * kVocabUnroll);
+        const int64_t want = 2 * most / n_rows;
+        a.blocks = (int)(batches < want ? batches : want);
+        a.span = (a.rows.nvec + a.blocks * kWarps - 1) / (a.blocks * kWarps);
+    } else if (top_k > 0 && a.rows.pieces > n_rows) {
+        // a list costs as much to begin as some thousand logits: pieces of whole rows while that idles few warps
+        const int64_t whole = a.rows.pieces / n_rows * n_rows;
+        if (4 * whole >= 3 * a.rows.pieces) a.rows.pieces = whole;
+    }
     a.targets = targets;
     a.T = T;
     a.c = (float)(1.4426950408889634 / (double)T);
@@ -705,6 +764,7 @@ estp_status launch_token_logprobs(estp_ctx* ctx, const void* logits, estp_dtype 
     a.top_logprobs = top_logprobs;
     a.part = ctx->vocab_part;
     a.lists = ctx->vocab_lists;
+    a.count = ctx->vocab_count;
     a.status = ctx->status;
     const cudaError_t e = dtype == ESTP_BF16 ? launch_forward<true>(a, st) : launch_forward<false>(a, st);
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "log probability launch");
