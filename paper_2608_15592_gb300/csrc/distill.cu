@@ -13,6 +13,8 @@
 // Bound: the gradient needs the row's sum before its first element, so a row is either read twice or
 // kept.  Here it is kept: a cluster of C CTAs takes a row, each a slice that fits its shared memory
 // beside those of the other CTAs of the SM, so logits are read once and the gradient is written once.
+#include <type_traits>
+
 #include "vocab.cuh"
 
 namespace estp {
@@ -105,10 +107,14 @@ __device__ __forceinline__ void take_entries(const DistillArgs& a, const Asked& 
     __syncwarp();
     e.w = a.weight ? q.w : 1.f;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < kPer; ++i) {  // (here and below, what lies past K costs a branch)
         const int j = i * 32 + lane;
-        e.id[i] = j < a.K ? q.id[j] : -1;
-        e.x[i] = j < a.K ? q.x[j] : -INFINITY;
+        e.id[i] = -1;
+        e.x[i] = -INFINITY;
+        if (i * 32 < a.K && j < a.K) {
+            e.id[i] = q.id[j];
+            e.x[i] = q.x[j];
+        }
     }
     __syncwarp();
 }
@@ -124,6 +130,8 @@ __device__ __forceinline__ void check_entries(const DistillArgs& a, int64_t r, E
     bool bad = false, again = false;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
+        old[i] = -1;
+        if (i * 32 >= a.K) continue;
         if (e.id[i] >= a.V) {
             bad = true;
             e.id[i] = -1;
@@ -133,6 +141,7 @@ __device__ __forceinline__ void check_entries(const DistillArgs& a, int64_t r, E
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
+        if (i * 32 >= a.K) continue;
         for (int tries = 1; tries < kSlots && old[i] != -1 && old[i] != e.id[i]; ++tries) {
             slot[i] = (slot[i] + 1) % kSlots;
             old[i] = atomicCAS(&table[slot[i]], -1, e.id[i]);
@@ -142,7 +151,7 @@ __device__ __forceinline__ void check_entries(const DistillArgs& a, int64_t r, E
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-        if (e.id[i] >= 0) table[slot[i]] = -1;
+        if (i * 32 < a.K && e.id[i] >= 0) table[slot[i]] = -1;
     e.repeated = __any_sync(0xffffffffu, again);
     if (e.repeated && a.tail) {  // a token has one probability: but for its first entry it is left out
         uint32_t out = 0;
@@ -167,7 +176,7 @@ __device__ __forceinline__ void check_entries(const DistillArgs& a, int64_t r, E
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         e.z[i] = kBf16 ? 0xFF80u : 0xFF800000u;
-        if (e.id[i] >= 0)
+        if (i * 32 < a.K && e.id[i] >= 0)
             e.z[i] = kBf16 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[e.id[i]] : reinterpret_cast<const uint32_t*>(row)[e.id[i]];
         if (e.id[i] < 0) e.x[i] = -INFINITY;
     }
@@ -226,15 +235,17 @@ __device__ __forceinline__ void put_entries(const DistillArgs& a, const Entries&
         const bool none = sum == 0.f;  // no entry, or only such of -inf
         const float l = none ? 0.f : logf(sum);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            q[i] = none ? 0.f : q[i] / sum;
-            lq[i] -= l;
-        }
+        for (int i = 0; i < kPer; ++i)
+            if (i * 32 < a.K) {
+                q[i] = none ? 0.f : q[i] / sum;
+                lq[i] -= l;
+            }
         Q = none ? 0.f : 1.f;
         some = !none;
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
+        if (i * 32 >= a.K) continue;
         const int j = i * 32 + lane;
         t.id[j] = e.id[i];
         t.q[j] = q[i];
@@ -307,11 +318,11 @@ __device__ __forceinline__ float named_grad(const DistillArgs& a, const Teacher&
 
 // Calls f(j) in every lane for each token j of a unit.
 template <class F>
-__device__ __forceinline__ void each_named(const Teacher& t, int K, int per, int unit, F f) {
+__device__ __forceinline__ void each_named(const int32_t* ids, int K, int per, int unit, F f) {
     const int lane = threadIdx.x & 31;
     for (int i0 = 0; i0 < K; i0 += 32) {
         const int i = i0 + lane;
-        const int id = i < K ? t.id[i] : -1;
+        const int id = i < K ? ids[i] : -1;
         uint32_t hit = __ballot_sync(0xffffffffu, id >= 0 && id / per == unit);
         while (hit) {
             const int j = i0 + __ffs(hit) - 1;
@@ -321,17 +332,18 @@ __device__ __forceinline__ void each_named(const Teacher& t, int K, int per, int
     }
 }
 
-// Named tokens among a warp's 32 units from `unit` on become -inf; `lanes` marks the units.
+// Named tokens among a warp's 32 units from `unit` on become -inf; `lanes` marks the units.  (A call, so that the loops
+// around it stay short: a row has K such units among thousands.)
 template <bool kBf16>
-__device__ __forceinline__ void mask_named(const Teacher& t, int K, uint32_t lanes, int unit, uint4& v) {
+__device__ __noinline__ uint4 mask_ids(const int32_t* ids, int K, uint32_t lanes, int unit, uint4 v) {
     constexpr int per = kBf16 ? 8 : 4;
     const int lane = threadIdx.x & 31;
     uint32_t* w = reinterpret_cast<uint32_t*>(&v);
     while (lanes) {
         const int l = __ffs(lanes) - 1;
         lanes &= lanes - 1;
-        each_named(t, K, per, unit + l, [&](int j) {
-            const int at = t.id[j] - (unit + l) * per;
+        each_named(ids, K, per, unit + l, [&](int j) {
+            const int at = ids[j] - (unit + l) * per;
 #pragma unroll
             for (int e = 0; e < per; ++e)
                 if (lane == l && e == at) {
@@ -341,6 +353,7 @@ __device__ __forceinline__ void mask_named(const Teacher& t, int K, uint32_t lan
                 }
         });
     }
+    return v;
 }
 
 template <bool kBf16, bool kFramed>
@@ -358,18 +371,29 @@ __device__ __forceinline__ void other_grad(const Factors& f, const uint4& v, flo
 }
 
 // ------------------------------------------------------------------ rows kept by a cluster
-// Eight warps hold the slice.  A thread copies its own units into shared memory (cp.async), reads them from
-// there twice and, once it has read a unit for the last time, copies the next row's into its place: so the next
-// row is on its way while this one is computed and written, and no barrier stands between a copy
-// and its use.  The ninth warp is a row ahead on the teacher's side (tokens, their logits, q), forms the loss behind
-// the barrier, and puts the named tokens' gradients over what the others wrote there one row later.
-// One cluster barrier a row: before it each warp stores its statistics into every CTA of the cluster,
-// after it every warp joins them for itself.  Up to three CTAs an SM.
-constexpr int kHold = 256;             // threads that hold the slice
-constexpr int kHoldWarps = kHold / 32;
-constexpr int kClusterThreads = kHold + 32;
+// A cluster of C CTAs takes a row, each a slice; up to three CTAs an SM, of different clusters, so that one
+// computes while another waits.  Eight warps work on the slice: a thread copies its own units into
+// shared memory (cp.async), reads them there for the statistics, and again for the gradient, after which it
+// copies the next row's into their place: the next row is on its way while this one is written, and no
+// barrier stands between a copy and its use.
+//
+// The ninth warp has the teacher's side of the next row ready, forms the loss, and one row later writes the named
+// tokens' gradients over what the workers wrote there.
+//
+// One cluster barrier a row: before it each worker warp stores its statistics into every CTA of the cluster, after
+// it every warp joins them for itself.
+//
+// One CTA an SM with the slices of two or three rows, the statistics a row ahead of the gradient and warps of their own for the
+// joins and the teacher hides the barrier, but its 16 or 24 workers then do the same thing at the same time: 2048
+// rows of 128256 tokens in 234 us and 1021 of 152064 with the tail in 185.
+constexpr int kWork = 256;
+constexpr int kWorkWarps = kWork / 32;
+constexpr int kRowThreads = kWork + 32;
+constexpr int kRowBlocks = 3;  // CTAs an SM at most
+constexpr int kGroup = 3;      // units a worker has in registers at once (8: 215 us, the loops outgrow the instruction cache)
+constexpr int kTeachers = 3;   // rows i - 1 .. i + 1
 constexpr int kMaxCluster = 8;
-constexpr int kSliceBytes = 200 * 1024;  // most of a CTA's dynamic shared memory
+constexpr int kSliceBytes = 200 * 1024;  // dynamic shared memory at most
 
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -388,215 +412,360 @@ __device__ __forceinline__ void copy_unit(uint4* to, const char* from) {
     asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from)
                  : "memory");
 }
-// A thread's units of a slice: tid, tid + kHold, .. below n; u0: the slice's first unit.
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All but the thread's last `left` groups of copies are there.
+__device__ __forceinline__ void copies_wait(int left) {
+    switch (left) {
+        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    }
+}
+
+// A CTA's slice of a row: n units, the row's u0-th on; a worker's are tid, tid + kWork, .. in groups of kGroup, the last
+// one of what is left.
 struct Slice {
     uint4* kept;
     const uint32_t* bits;  // with the tail: units that hold a named token
     int n, u0;
 };
 
-// N of the thread's units, from `at` on, into the statistics; `next`: the next row's first copied unit, or NULL.
-template <bool kBf16, int N, bool kRefill>
-__device__ __forceinline__ void hold_units(const DistillArgs& a, const Teacher& t, const Slice& s, int at, const char* next,
+// Calls f(at, N) for each of the groups; every worker has all of a group's units, and all of them are whole, but for
+// the last unit of the last group.
+template <class F, int N = kGroup>
+__device__ __forceinline__ void last_group(int left, int at, F& f) {
+    if constexpr (N > 1) {
+        if (left < N) {
+            last_group<F, N - 1>(left, at, f);
+            return;
+        }
+    }
+    f(at, std::integral_constant<int, N>(), true);
+}
+template <class F>
+__device__ __forceinline__ void each_group(int n, F f) {
+    const int units = (n + kWork - 1) / kWork;  // of a worker, the last one not of all
+    int u = 0;
+    for (; u + kGroup < units; u += kGroup) f(u * kWork, std::integral_constant<int, kGroup>(), false);
+    if (u < units) last_group(units - u, u * kWork, f);
+}
+__device__ __forceinline__ int groups_of(int n) { return ((n + kWork - 1) / kWork + kGroup - 1) / kGroup; }
+
+template <int N>
+__device__ __forceinline__ void copy_group(const Slice& s, int at, bool last, const char* from) {
+    const int c = at + (int)threadIdx.x;
+    const char* q = from + (int64_t)c * 16;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        if (k < N - 1 || !last || c + k * kWork < s.n) copy_unit(&s.kept[c + k * kWork], q + k * (kWork * 16));
+    copies_commit();
+}
+
+// N of the worker's units, from `at` on, into the statistics.
+template <bool kBf16, int N>
+__device__ __forceinline__ void hold_units(const DistillArgs& a, const Teacher& t, const Slice& s, int at, bool last,
                                            LaneStat<false>& st) {
     constexpr int per = kBf16 ? 8 : 4;
-    const int tid = threadIdx.x, warp = tid >> 5;
+    const int c = at + (int)threadIdx.x;
     uint4 v[N];
-    if (at + N * kHold <= min(s.n, a.V / per - s.u0)) {  // whole units all
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = s.kept[at + k * kHold + tid];
+    for (int k = 0; k < N - 1; ++k) v[k] = s.kept[c + k * kWork];
+    if (last) {
+        const int l = c + (N - 1) * kWork, valid = a.V - (s.u0 + l) * per;
+        v[N - 1] = l < s.n ? s.kept[l] : masked_unit<kBf16>();
+        if (valid < per) mask_unit<kBf16>(v[N - 1], valid);
     } else {
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const int c = at + k * kHold + tid, valid = a.V - (s.u0 + c) * per;
-            v[k] = c < s.n ? s.kept[c] : masked_unit<kBf16>();
-            if (valid < per) mask_unit<kBf16>(v[k], valid);
-        }
+        v[N - 1] = s.kept[c + (N - 1) * kWork];
     }
     if (a.tail) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const int w = at + k * kHold + warp * 32;  // the warp's units
+            const int w = (c & ~31) + k * kWork;  // the warp's units
             const uint32_t lanes = w < s.n ? s.bits[w >> 5] : 0;
-            if (lanes) mask_named<kBf16>(t, a.K, lanes, s.u0 + w, v[k]);
+            if (lanes) v[k] = mask_ids<kBf16>(t.id, a.K, lanes, s.u0 + w, v[k]);
         }
     }
     st.template add_units<kBf16>(v, units_max<kBf16, N>(v), a.c);
-    if (kRefill && next) {  // (every value has been used)
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (at + k * kHold + tid < s.n) copy_unit(&s.kept[at + k * kHold + tid], next + (int64_t)(at + k * kHold + tid) * 16);
-    }
 }
 
-template <bool kBf16, bool kFramed>
-__device__ __forceinline__ void kept_grad(const DistillArgs& a, const Factors& f, const Slice& s, char* out, const char* next) {
+// The gradient of N of them, and copies of the next row (`next`, if any) into their place.
+template <bool kBf16, bool kFramed, int N>
+__device__ __forceinline__ void kept_grad(const DistillArgs& a, const Factors& f, const Slice& s, int at, bool last, char* out,
+                                          const char* next) {
     constexpr int per = kBf16 ? 8 : 4;
-    const int tid = threadIdx.x, whole = min(s.n, a.V / per - s.u0);
-    int c = tid;
-    for (; c + 3 * kHold < whole; c += 4 * kHold) {
-        uint4 v[4];
+    const int c = at + (int)threadIdx.x;
+    char* p = out + (int64_t)c * 16;
+    uint4 v[N];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = s.kept[c + k * kHold];
-        char* p = out + (int64_t)c * 16;
+    for (int k = 0; k < N - 1; ++k) v[k] = s.kept[c + k * kWork];
+    v[N - 1] = last && c + (N - 1) * kWork >= s.n ? masked_unit<kBf16>() : s.kept[c + (N - 1) * kWork];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float x[8];
-            other_grad<kBf16, kFramed>(f, v[k], a.c, x);
-            store_whole<kBf16>(p + k * (kHold * 16), x);
-        }
-        if (next) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) copy_unit(&s.kept[c + k * kHold], next + (int64_t)(c + k * kHold) * 16);
-        }
-    }
-    for (; c < s.n; c += kHold) {
+    for (int k = 0; k < N; ++k) {
         float x[8];
-        other_grad<kBf16, kFramed>(f, s.kept[c], a.c, x);
-        store_unit<kBf16>(out, c, a.V - s.u0 * per, x);
-        if (next) copy_unit(&s.kept[c], next + (int64_t)c * 16);
+        other_grad<kBf16, kFramed>(f, v[k], a.c, x);
+        if (k < N - 1 || !last) store_whole<kBf16>(p + k * (kWork * 16), x);
+        else if (c + k * kWork < s.n) store_unit<kBf16>(out, c + k * kWork, a.V - s.u0 * per, x);
+    }
+    if (next) copy_group<N>(s, at, last, next);  // (every value has been used)
+}
+
+// The named tokens of a slice, over what an unnamed one would have there (a warp).
+template <bool kBf16>
+__device__ __forceinline__ void put_named(const DistillArgs& a, int64_t r, const Teacher& t, const Factors& f, int u0, int n) {
+    constexpr int per = kBf16 ? 8 : 4;
+    const int lane = threadIdx.x & 31;
+    if (f.zero) return;
+    char* out = a.out + r * a.out_bytes;
+    for (int j0 = 0; j0 < a.K; j0 += 32) {
+        const int j = j0 + lane, id = j < a.K ? t.id[j] : -1;
+        const unsigned u = (unsigned)(id / per - u0);
+        const bool mine = id >= 0 && u < (unsigned)n;
+        bool first = mine;
+        float x = 0.f;
+        if (mine && !a.tail) x = f.A * ex2(max_nan((t.z[j] - f.pivot) * a.c, kCut));
+        if (!t.repeated || a.tail) {
+            if (mine) x = named_grad(a, t, f, j, x);
+        } else {  // a repeated token counts each time: its first place has the sum
+            for (int k = 0; k < a.K; ++k)
+                if (mine && t.id[k] == id) {
+                    x = named_grad(a, t, f, k, x);
+                    first &= k >= j;
+                }
+        }
+        if (first && in_bounds(id < a.V && r < a.n_rows, a.status)) {
+            if (kBf16) reinterpret_cast<__nv_bfloat16*>(out)[id] = __float2bfloat16_rn(x);
+            else reinterpret_cast<float*>(out)[id] = x;
+        }
     }
 }
 
-template <bool kBf16, bool kGrad>
-__global__ void __launch_bounds__(kClusterThreads, 3) distill_cluster_kernel(const DistillArgs a, int slice, int C) {
+template <bool kBf16>
+__global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(const DistillArgs a, int slice, int C) {
     constexpr int per = kBf16 ? 8 : 4;
-    extern __shared__ uint4 room[];
-    __shared__ Teacher teachers[3];                         // of three rows: last, this and next
-    __shared__ float2 stats[2][kMaxCluster * kHoldWarps];  // m, s of each warp of the cluster, of two rows
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rank = blockIdx.x % C, n_clusters = gridDim.x / C, words = (slice + 31) / 32;
-    const int u0 = min(rank * slice, a.nvec), n = min(slice, a.nvec - u0);
-    uint32_t* bits = reinterpret_cast<uint32_t*>(room + slice);  // [3][words]
-    const bool holds = warp < kHoldWarps;
-
+    extern __shared__ uint4 room[];                 // [slice], then with the tail [kTeachers][words]
+    __shared__ Teacher teachers[kTeachers];
+    __shared__ float2 stats[2][kMaxCluster * kWorkWarps];  // m, s of each worker warp of the cluster, of two rows
     __shared__ int32_t table[kSlots];
     __shared__ Asked asked;
-    // the ninth warp: the teacher's side of a row, once its entries and their logits have come
-    auto put = [&](const Entries& e, int k) {
-        uint32_t* b = bits + k * words;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = blockIdx.x % C, words = (slice + 31) / 32;
+    const int u0 = min(rank * slice, a.nvec), n = min(slice, a.nvec - u0);
+    const int64_t r0 = blockIdx.x / C, step = gridDim.x / C;
+    const int rows = r0 < a.n_rows ? (int)((a.n_rows - r0 + step - 1) / step) : 0;  // of this cluster
+    uint32_t* bits = reinterpret_cast<uint32_t*>(room + slice);
+    const bool works = warp < kWorkWarps;
+    auto from = [&](int i) { return a.base + (r0 + i * step) * a.ld_bytes + (int64_t)u0 * 16; };
+    auto next_of = [](int k) { return k + 1 == kTeachers ? 0 : k + 1; };
+
+    Entries e;  // (ninth warp) of the next row to be put, with its logits; `asked` is of the one after it
+    auto put = [&](int i, int at) {
+        if (i >= rows) return;
+        uint32_t* b = bits + at * words;
         if (a.tail) {
-            for (int i = lane; i < words; i += 32) b[i] = 0;
+            for (int k = lane; k < words; k += 32) b[k] = 0;
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const unsigned u = (unsigned)(e.id[i] / per - u0);
-                if (e.id[i] >= 0 && u < (unsigned)n) atomicOr(&b[u >> 5], 1u << (u & 31));
+            for (int k = 0; k < kPer; ++k) {
+                const unsigned u = (unsigned)(e.id[k] / per - u0);
+                if (k * 32 < a.K && e.id[k] >= 0 && u < (unsigned)n) atomicOr(&b[u >> 5], 1u << (u & 31));
             }
         }
-        put_entries<kBf16>(a, e, teachers[k]);
+        put_entries<kBf16>(a, e, teachers[at]);
     };
-    // the named tokens of the slice, over what an unnamed one would have there
-    auto put_named = [&](int64_t r, const Teacher& t, const Factors& f) {
-        if (f.zero) return;
-        char* out = a.out + r * a.out_bytes;
-        for (int j0 = 0; j0 < a.K; j0 += 32) {
-            const int j = j0 + lane, id = j < a.K ? t.id[j] : -1;
-            const unsigned u = (unsigned)(id / per - u0);
-            const bool mine = id >= 0 && u < (unsigned)n;
-            float x = 0.f;
-            if (mine) x = a.tail ? 0.f : f.A * ex2(max_nan((t.z[j] - f.pivot) * a.c, kCut));
-            bool first = mine;
-            if (a.tail) {
-                if (mine) x = named_grad(a, t, f, j, 0.f);
-            } else if (!t.repeated) {
-                if (mine) x = named_grad(a, t, f, j, x);
-            } else {
-                // a repeated token counts each time: its first place has the sum
-                for (int k = 0; k < a.K; ++k)
-                    if (mine && t.id[k] == id) {
-                        x = named_grad(a, t, f, k, x);
-                        first &= k >= j;
-                    }
-            }
-            if (first && in_bounds(id < a.V, a.status)) {
-                if (kBf16) reinterpret_cast<__nv_bfloat16*>(out)[id] = __float2bfloat16_rn(x);
-                else reinterpret_cast<float*>(out)[id] = x;
-            }
-        }
+    auto fetch = [&](int i) {  // row i's entries, row i + 1's asked for
+        if (i >= rows) return;
+        take_entries(a, asked, e);
+        if (i + 1 < rows) ask_entries(a, r0 + (i + 1) * step, asked);
+        check_entries<kBf16>(a, r0 + i * step, e, table);
     };
-
-    int64_t r = blockIdx.x / C;
-    Entries e;  // of the next row, with its logits; `asked` is of the one after it
-    if (holds) {
-        if (r < a.n_rows) {
-            const char* from = a.base + r * a.ld_bytes + (int64_t)u0 * 16;
-            for (int c = tid; c < n; c += kHold) copy_unit(&room[c], from + (int64_t)c * 16);
-        }
-    } else if (r < a.n_rows) {
+    const int groups = groups_of(n);
+    if (works) {
+        const Slice s{room, bits, n, u0};
+        if (rows > 0) each_group(n, [&](int at, auto N, bool last) { copy_group<decltype(N)::value>(s, at, last, from(0)); });
+    } else {
         for (int i = lane; i < kSlots; i += 32) table[i] = -1;
         __syncwarp();
-        ask_entries(a, r, asked);
-        take_entries(a, asked, e);
-        ask_entries(a, r + n_clusters, asked);
-        check_entries<kBf16>(a, r, e, table);
-        put(e, 0);
-        if (r + n_clusters < a.n_rows) {
-            take_entries(a, asked, e);
-            ask_entries(a, r + 2 * (int64_t)n_clusters, asked);
-            check_entries<kBf16>(a, r + n_clusters, e, table);
-        }
+        if (rows > 0) ask_entries(a, r0, asked);
+        fetch(0);
+        put(0, 0);
+        fetch(1);
     }
     __syncthreads();
     Factors f{};
-    for (int i = 0; r < a.n_rows; r += n_clusters, ++i) {
-        const Teacher& t = teachers[i % 3];
-        const Slice s{room, bits + i % 3 * words, n, u0};
-        const int64_t after = r + n_clusters;
-        const char* next = after < a.n_rows ? a.base + after * a.ld_bytes + (int64_t)u0 * 16 : nullptr;
+    int before = 0;
+    for (int i = 0, k = 0; i < rows; ++i, k = next_of(k)) {
+        const Teacher& t = teachers[k];
+        const Slice s{room, bits + k * words, n, u0};
         float2* mine = stats[i & 1];
-        if (holds) {
-            copies_done();
+        if (works) {
             LaneStat<false> st;
-            int at = 0;
-            for (; at + 6 * kHold < n; at += 8 * kHold) hold_units<kBf16, 8, !kGrad>(a, t, s, at, next, st);
-            for (; at < n; at += 2 * kHold) hold_units<kBf16, 2, !kGrad>(a, t, s, at, next, st);
+            int left = groups;
+            each_group(n, [&](int at, auto N, bool last) {
+                copies_wait(--left);
+                hold_units<kBf16, decltype(N)::value>(a, t, s, at, last, st);
+            });
             RowStat x = st.row(a.c);
             join_lanes<false>(x, a.c);
-            if (lane < C) store_remote(&mine[rank * kHoldWarps + warp], lane, x.m, x.s);
-        } else if (next) {
-            put(e, (i + 1) % 3);
-            if (after + n_clusters < a.n_rows) {
-                take_entries(a, asked, e);
-                ask_entries(a, after + 2 * (int64_t)n_clusters, asked);
-                check_entries<kBf16>(a, after + n_clusters, e, table);
-            }
+            if (lane < C) store_remote(&mine[rank * kWorkWarps + warp], lane, x.m, x.s);
+        } else {
+            put(i + 1, next_of(k));
         }
         __syncwarp();
         cluster_sync();
         RowStat st = no_stat();
-        for (int k = lane; k < C * kHoldWarps; k += 32) {
-            if (k < 32) st = RowStat{mine[k].x, mine[k].y, 0.f};
-            else join(st, RowStat{mine[k].x, mine[k].y, 0.f}, a.c);
+        for (int w = lane; w < C * kWorkWarps; w += 32) {
+            if (w < 32) st = RowStat{mine[w].x, mine[w].y, 0.f};
+            else join(st, RowStat{mine[w].x, mine[w].y, 0.f}, a.c);
         }
+        __syncwarp();
         join_lanes<false>(st, a.c);
-        if (!holds && kGrad && i > 0) put_named(r - n_clusters, teachers[(i + 2) % 3], f);
-        f = row_factors(a, t, st);
-        if (!holds) {
+        if (!works) {
+            // (the workers' gradient of the row before is behind the barrier)
+            if (i > 0) put_named<kBf16>(a, r0 + (i - 1) * step, teachers[before], f, u0, n);
+            f = row_factors(a, t, st);
             if (rank == 0) {
                 const float loss = row_loss(a, t, st, f);
-                if (lane == 0) a.loss[r] = loss;
+                if (lane == 0) a.loss[r0 + i * step] = loss;
             }
-        } else if (kGrad) {
-            char* out = a.out + r * a.out_bytes + (int64_t)u0 * 16;
+            before = k;
+            fetch(i + 2);
+        } else {
+            f = row_factors(a, t, st);
+            char* out = a.out + (r0 + i * step) * a.out_bytes + (int64_t)u0 * 16;
+            const char* next = i + 1 < rows ? from(i + 1) : nullptr;
             if (f.zero) {
                 const float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                for (int c = tid; c < n; c += kHold) {
-                    store_unit<kBf16>(out, c, a.V - u0 * per, x);
-                    if (next) copy_unit(&room[c], next + (int64_t)c * 16);
-                }
+                for (int c = tid; c < n; c += kWork) store_unit<kBf16>(out, c, a.V - u0 * per, x);
+                if (next) each_group(n, [&](int at, auto N, bool last) { copy_group<decltype(N)::value>(s, at, last, next); });
             } else if (f.framed) {
-                kept_grad<kBf16, true>(a, f, s, out, next);
+                each_group(n, [&](int at, auto N, bool last) { kept_grad<kBf16, true, decltype(N)::value>(a, f, s, at, last, out, next); });
             } else {
-                kept_grad<kBf16, false>(a, f, s, out, next);
+                each_group(n, [&](int at, auto N, bool last) { kept_grad<kBf16, false, decltype(N)::value>(a, f, s, at, last, out, next); });
             }
         }
         __syncwarp();
     }
-    if (kGrad) {
-        __syncthreads();  // the last row's stores
-        const int rows = (int)((r - blockIdx.x / C) / n_clusters);
-        if (!holds && rows > 0) put_named(r - n_clusters, teachers[(rows - 1) % 3], f);
+    __syncthreads();  // the last row's stores
+    if (!works && rows > 0) put_named<kBf16>(a, r0 + (rows - 1) * step, teachers[before], f, u0, n);
+}
+
+// ------------------------------------------------------------------ the loss alone
+// A warp an equal piece of the flat run of units (vocab.cuh); of a row cut between warps each leaves its
+// statistics, and the one that leaves the last joins them in order and forms the loss.
+struct EvalArgs {
+    DistillArgs d;
+    VocabRows rows;
+    float4* part;      // [pieces][2]: m, s of a piece's first and last row
+    uint32_t* count;   // by a row's first piece; zero between launches
+};
+
+// Units [c0, c1) of a row; with the tail, named tokens do not count.
+template <bool kBf16>
+__device__ __forceinline__ RowStat eval_units(const DistillArgs& a, const char* row, int c0, int c1, const int32_t* ids,
+                                              uint32_t* bits) {
+    constexpr int per = kBf16 ? 8 : 4;
+    const int lane = threadIdx.x & 31, whole = min(c1, a.V / per);
+    LaneStat<false> st;
+    for (int chunk = c0; chunk < c1; chunk += 1024) {
+        const int stop = min(c1, chunk + 1024);
+        uint32_t word = 0, steps = 0;
+        if (a.tail) {  // the chunk's units that hold one, lane l's word those of its step l
+            bits[lane] = 0;
+            __syncwarp();
+            for (int j = lane; j < a.K; j += 32) {
+                const unsigned k = (unsigned)(ids[j] / per - chunk);
+                if (ids[j] >= 0 && k < 1024u) atomicOr(&bits[k >> 5], 1u << (k & 31));
+            }
+            __syncwarp();
+            word = bits[lane];
+            steps = __ballot_sync(0xffffffffu, word != 0);
+            __syncwarp();
+        }
+        for (int b = chunk; b < stop; b += 32 * kVocabUnroll) {
+            uint4 v[kVocabUnroll];
+            if (b + 32 * kVocabUnroll <= whole) {
+#pragma unroll
+                for (int k = 0; k < kVocabUnroll; ++k) v[k] = ld_stream(row + (int64_t)(b + 32 * k + lane) * 16);
+            } else {
+#pragma unroll
+                for (int k = 0; k < kVocabUnroll; ++k) v[k] = load_unit<kBf16>(row, b + 32 * k + lane, stop, a.V);
+            }
+            if (steps >> ((b - chunk) / 32) & ((1u << kVocabUnroll) - 1)) {
+#pragma unroll
+                for (int k = 0; k < kVocabUnroll; ++k) {
+                    const uint32_t lanes = __shfl_sync(0xffffffffu, word, (b - chunk) / 32 + k);
+                    if (lanes) v[k] = mask_ids<kBf16>(ids, a.K, lanes, b + 32 * k, v[k]);
+                }
+            }
+            st.template add_units<kBf16>(v, units_max<kBf16, kVocabUnroll>(v), a.c);
+        }
+    }
+    RowStat x = st.row(a.c);
+    join_lanes<false>(x, a.c);
+    return x;
+}
+
+template <bool kBf16>
+__global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kernel(const EvalArgs a) {
+    constexpr int kWarps = kVocabThreads / 32;
+    __shared__ Teacher teachers[kWarps];
+    __shared__ Asked asked[kWarps];
+    __shared__ int32_t tables[kWarps][kSlots];
+    __shared__ uint32_t bits[kWarps][32];
+    const DistillArgs& d = a.d;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t w = (int64_t)blockIdx.x * kWarps + warp;
+    if (w >= a.rows.pieces) return;
+    const int64_t start = piece_start(a.rows, w), end = piece_start(a.rows, w + 1);
+    for (int i = lane; i < kSlots; i += 32) tables[warp][i] = -1;
+    __syncwarp();
+    for (int64_t u = start; u < end;) {
+        const int64_t r = u / a.rows.nvec, u0 = r * a.rows.nvec;
+        const int c0 = (int)(u - u0), c1 = (int)(min(end, u0 + a.rows.nvec) - u0);
+        const char* row = d.base + r * d.ld_bytes;
+        Entries e;
+        ask_entries(d, r, asked[warp]);
+        if (d.tail) {
+            copies_done();
+            __syncwarp();
+        }
+        RowStat st = eval_units<kBf16>(d, row, c0, c1, asked[warp].id, bits[warp]);
+        bool write = true;
+        if (c0 != 0 || c1 != a.rows.nvec) {
+            const int64_t slot = w * 2 + (u == start ? 0 : 1);
+            const int64_t lo = piece_of(a.rows, u0), hi = piece_of(a.rows, u0 + a.rows.nvec - 1);
+            const int n = (int)(hi - lo + 1);
+            uint32_t last = 0;
+            if (lane == 0 && in_bounds(slot < 2 * a.rows.pieces, d.status)) {
+                a.part[slot] = make_float4(st.m, st.s, 0.f, 0.f);
+                __threadfence();
+                last = atomicAdd(&a.count[lo], 1u) == (uint32_t)n - 1 ? 1u : 0u;
+                if (last) a.count[lo] = 0;
+                __threadfence();
+            }
+            write = __shfl_sync(0xffffffffu, last, 0) != 0;
+            if (write) {
+                st = no_stat();
+                for (int i = lane; i < n; i += 32) {
+                    const float4 x = __ldcg(&a.part[i ? (lo + i) * 2 : lo * 2 + (piece_start(a.rows, lo) < u0 ? 1 : 0)]);
+                    join(st, RowStat{x.x, x.y, 0.f}, d.c);
+                }
+                __syncwarp();
+                join_lanes<false>(st, d.c);
+            }
+        }
+        if (write) {
+            Teacher& t = teachers[warp];
+            take_entries(d, asked[warp], e);
+            check_entries<kBf16>(d, r, e, tables[warp]);
+            put_entries<kBf16>(d, e, t);
+            const float loss = row_loss(d, t, st, row_factors(d, t, st));
+            if (lane == 0) d.loss[r] = loss;
+        }
+        copies_done();
+        __syncwarp();
+        u = u0 + c1;
     }
 }
 
@@ -651,7 +820,7 @@ __global__ void __launch_bounds__(kLongThreads) distill_long_kernel(const Distil
                     for (int k = 0; k < kVocabUnroll; ++k) {
                         const int c = b + 32 * k;
                         const uint32_t lanes = c < stop ? bits[(c - span) >> 5] : 0;
-                        if (lanes) mask_named<kBf16>(t, a.K, lanes, c, v[k]);
+                        if (lanes) v[k] = mask_ids<kBf16>(t.id, a.K, lanes, c, v[k]);
                     }
                 }
                 st.template add_units<kBf16>(v, units_max<kBf16, kVocabUnroll>(v), a.c);
@@ -670,7 +839,6 @@ __global__ void __launch_bounds__(kLongThreads) distill_long_kernel(const Distil
             const float loss = row_loss(a, t, all, f);
             if (lane == 0) a.loss[r] = loss;
         }
-        if (!a.out) continue;
         char* out = a.out + r * a.out_bytes;
         for (int span = 0; span < a.nvec; span += kSpanUnits) {
             const int stop = min(a.nvec, span + kSpanUnits);
@@ -682,7 +850,7 @@ __global__ void __launch_bounds__(kLongThreads) distill_long_kernel(const Distil
                     const uint32_t lanes = bits[(c - span) >> 5];
                     for (uint32_t left = lanes; left; left &= left - 1) {
                         const int l = __ffs(left) - 1;
-                        each_named(t, a.K, per, c + l, [&](int j) {
+                        each_named(t.id, a.K, per, c + l, [&](int j) {
 #pragma unroll
                             for (int e = 0; e < per; ++e)
                                 if (lane == l && (c + l) * per + e == t.id[j]) x[e] = named_grad(a, t, f, j, x[e]);
@@ -698,40 +866,50 @@ __global__ void __launch_bounds__(kLongThreads) distill_long_kernel(const Distil
 }
 
 // ------------------------------------------------------------------ launch
-using ClusterKernel = void (*)(DistillArgs, int, int);
-template <bool kBf16>
-ClusterKernel cluster_kernel(bool grad) {
-    return grad ? distill_cluster_kernel<kBf16, true> : distill_cluster_kernel<kBf16, false>;
-}
+using RowsKernel = void (*)(DistillArgs, int, int);
 
-constexpr size_t kSharedStatic = sizeof(Teacher) * 3 + sizeof(int32_t) * kSlots + sizeof(Asked) + sizeof(float2) * 2 * kMaxCluster * kHoldWarps;
+size_t rows_bytes(int nvec, int C) {
+    const size_t slice = (size_t)((nvec + C - 1) / C);
+    return slice * 16 + kTeachers * ((slice + 31) / 32) * 4;
+}
 
 // CTAs an SM with `bytes` of dynamic shared memory each (1 KB of the SM's goes to every CTA).
 int ctas_per_sm(size_t bytes) {
-    const size_t n = (size_t)(228 * 1024) / (bytes + kSharedStatic + 1024);
-    return n > 3 ? 3 : (int)n;
+    constexpr size_t kStatic = sizeof(Teacher) * kTeachers + sizeof(float2) * 2 * kMaxCluster * kWorkWarps +
+                               sizeof(int32_t) * kSlots + sizeof(Asked);
+    const size_t n = (size_t)(228 * 1024) / (bytes + kStatic + 1024);
+    return n > kRowBlocks ? kRowBlocks : (int)n;
 }
 
-// Clusters of C that the GPU holds at once, asked once for each kernel, C and number of CTAs an SM.
-int clusters_at_once(estp_ctx* ctx, ClusterKernel kernel, int which, int C, size_t bytes, int per_sm) {
-    int& known = ctx->distill_clusters[which][per_sm - 1][C - 1];
-    if (known) return known;
+// Launch of `clusters` clusters of C CTAs.
+struct ClusterLaunch {
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)C;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(C * ctx->num_sms));
-    cfg.blockDim = dim3(kClusterThreads);
-    cfg.dynamicSmemBytes = bytes;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-        cudaGetLastError();
-        n = 0;
+    ClusterLaunch(int C, int clusters, size_t bytes, cudaStream_t st) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)C;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.gridDim = dim3((unsigned)(C * clusters));
+        cfg.blockDim = dim3(kRowThreads);
+        cfg.dynamicSmemBytes = bytes;
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
     }
-    known = n > 0 ? n : -1;  // -1: no such cluster here
+};
+
+// Clusters of C that the GPU holds at once, asked once for each type, C and number of CTAs an SM.
+int clusters_at_once(estp_ctx* ctx, RowsKernel kernel, int which, int C, size_t bytes, int per_sm) {
+    int& known = ctx->distill_clusters[which][per_sm - 1][C - 1];
+    if (known == 0) {
+        ClusterLaunch l(C, ctx->num_sms, bytes, nullptr);
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg) != cudaSuccess) {
+            cudaGetLastError();
+            n = 0;
+        }
+        known = n > 0 ? n : -1;  // -1: no such cluster here
+    }
     return known;
 }
 
@@ -759,57 +937,57 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
     a.out = static_cast<char*>(out);
     a.out_bytes = ld_out * esize(dtype);
     a.status = ctx->status;
+    cudaError_t e;
 
-    // The cluster size by what a wave of rows takes: a unit's share of the memory's rate (0.36 ns of an SM's
-    // for the read, as much for the write) on the CTAs that share an SM, and 2 us a row of barrier, joins and latency.
-    const int which = (bf16 ? 2 : 0) + (out ? 1 : 0);
-    const ClusterKernel kernel = bf16 ? cluster_kernel<true>(out != nullptr) : cluster_kernel<false>(out != nullptr);
-    if (!(ctx->distill_set >> which & 1)) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
+    if (!out) {
+        EvalArgs v;
+        v.d = a;
+        v.rows = vocab_rows(ctx, logits, dtype, n_rows, V, ld, 32 * kVocabUnroll, kVocabBlocks);
+        v.part = ctx->vocab_part;
+        v.count = ctx->vocab_count;
+        constexpr int kWarps = kVocabThreads / 32;
+        const unsigned blocks = (unsigned)((v.rows.pieces + kWarps - 1) / kWarps);
+        if (bf16) distill_eval_kernel<true><<<blocks, kVocabThreads, 0, st>>>(v);
+        else distill_eval_kernel<false><<<blocks, kVocabThreads, 0, st>>>(v);
+        e = cudaGetLastError();
+        return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
+    }
+
+    // The cluster size by what a wave of rows takes: a unit's share of an SM's part of the memory's rate (0.72 ns for
+    // its read and its write) on the CTAs that share an SM, of which one by itself reaches some 0.4, and 2 us a row.
+    const RowsKernel kernel = bf16 ? distill_rows_kernel<true> : distill_rows_kernel<false>;
+    if (!(ctx->distill_set >> bf16 & 1)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
         if (e != cudaSuccess) return cuda_fail(e, "distillation kernel's shared memory");
-        ctx->distill_set |= 1u << which;
+        ctx->distill_set |= 1u << bf16;
     }
     int C = 0, clusters = 0;
     double best = 0.;
     for (int c = 1; c <= kMaxCluster; ++c) {
-        const int slice = (a.nvec + c - 1) / c;
-        const size_t bytes = (size_t)slice * 16 + 3 * (size_t)((slice + 31) / 32) * 4;
-        if (bytes > kSliceBytes) continue;
-        const int per_sm = ctas_per_sm(bytes);
-        const int at_once = clusters_at_once(ctx, kernel, which, c, bytes, per_sm);
+        const size_t bytes = rows_bytes(a.nvec, c);
+        if (bytes > (size_t)kSliceBytes) continue;
+        const int per_sm = ctas_per_sm(bytes), at_once = clusters_at_once(ctx, kernel, bf16, c, bytes, per_sm);
         if (at_once < 1) continue;
-        const int64_t waves = (n_rows + at_once - 1) / at_once;
         const int64_t share = (n_rows * c + ctx->num_sms - 1) / ctx->num_sms;  // CTAs an SM really has
-        // (a CTA by itself reaches some 0.4 of the rate)
-        const double sharing = share < per_sm ? (share < 3 ? 2.5 : (double)share) : per_sm < 3 ? 2.5 : (double)per_sm;
-        const double cost = (double)waves * ((out ? 0.72 : 0.36) * slice * sharing + 2000.);
+        const double together = share < per_sm ? (double)share : (double)per_sm;
+        const double cost = (double)((n_rows + at_once - 1) / at_once) *
+                            (0.72 * ((a.nvec + c - 1) / c) * (together < 2.5 ? 2.5 : together) + 2000.);
         if (C == 0 || cost < best) {
             best = cost;
             C = c;
             clusters = n_rows < at_once ? (int)n_rows : at_once;
         }
     }
-    if (C == 0) {
+    if (C == 0) {  // longer than the largest cluster keeps
         const int64_t most = (int64_t)ctx->num_sms * 2;
         const unsigned blocks = (unsigned)(n_rows < most ? n_rows : most);
         if (bf16) distill_long_kernel<true><<<blocks, kLongThreads, 0, st>>>(a);
         else distill_long_kernel<false><<<blocks, kLongThreads, 0, st>>>(a);
-        const cudaError_t e = cudaGetLastError();
-        return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
+        e = cudaGetLastError();
+    } else {
+        ClusterLaunch l(C, clusters, rows_bytes(a.nvec, C), st);
+        e = cudaLaunchKernelEx(&l.cfg, kernel, a, (a.nvec + C - 1) / C, C);
     }
-    const int slice = (a.nvec + C - 1) / C;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)C;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(C * clusters));
-    cfg.blockDim = dim3(kClusterThreads);
-    cfg.dynamicSmemBytes = (size_t)slice * 16 + 3 * (size_t)((slice + 31) / 32) * 4;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, slice, C);
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
 }
 

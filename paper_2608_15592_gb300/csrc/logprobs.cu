@@ -148,7 +148,7 @@ __device__ __noinline__ float take_units(Candidates<R>* q, const char* row, int 
         n -= take;
         if (lane < take) {
             const int c = c0 + (int)q->units[n + lane], first = c * per;
-            if (first < limit) {  // (a lane past the segment marks its -inf where there is no bound yet)
+            if (first < limit) {
                 const uint4 u = ld_stream(row + (int64_t)c * 16);
                 uint32_t in = 0;
 #pragma unroll
@@ -195,6 +195,10 @@ __device__ __forceinline__ void merge_block(Candidates<R>* cand) {
         __syncthreads();
     }
 }
+
+// Masked tokens (-inf) do not become candidates: a list that is short of top_k keys has every token that is not masked,
+// and write_row fills it up.
+constexpr float kLowest = -3.4028234663852886e38f;
 
 // A logit that at least top_k of the warp's 32 G values reach (or -inf): the order bits from the top
 // down, as far as 16 of them go.
@@ -263,7 +267,7 @@ __device__ __forceinline__ RowStat stream_row(const LpArgs& a, const char* row, 
                 float g[G];
 #pragma unroll
                 for (int i = 0; i < G; ++i) g[i] = units_max<kBf16, w>(v + i * w);
-                floor = bound = reached_by<G>(g, a.top_k);
+                floor = bound = fmaxf(reached_by<G>(g, a.top_k), kLowest);
             }
             // units with candidates are queued; the longer part waits until the batch is in the sums
             if (__any_sync(0xffffffffu, bm >= bound)) {
@@ -332,9 +336,28 @@ __device__ __forceinline__ void write_row(const LpArgs& a, int64_t r, const Targ
         for (int i = lane; i < 32 * R; i += 32)
             if (i < a.top_k) {
                 const uint64_t k = list[i];
+                if (k == 0 && !none) continue;
                 a.top_ids[r * a.top_k + i] = none ? -1 : key_token(k);
                 if (a.top_logprobs) a.top_logprobs[r * a.top_k + i] = none ? NAN : (key_logit(k) - m) / a.T - ls;
             }
+        if (list[a.top_k - 1] == 0 && !none) {
+            // short of tokens: the masked ones of lowest index follow, which are among the first top_k
+            int n = 0;
+            while (n < a.top_k && list[n] != 0) ++n;
+            const int have = n;
+            for (int v0 = 0; v0 < a.top_k && n < a.top_k; v0 += 32) {
+                const int v = v0 + lane;
+                bool masked = v < a.top_k;
+                for (int i = 0; i < have; ++i) masked &= key_token(list[i]) != v;
+                const uint32_t all = __ballot_sync(0xffffffffu, masked);
+                const int at = n + __popc(all & ((1u << lane) - 1));
+                if (masked && at < a.top_k) {
+                    a.top_ids[r * a.top_k + at] = v;
+                    if (a.top_logprobs) a.top_logprobs[r * a.top_k + at] = -INFINITY;
+                }
+                n += __popc(all);
+            }
+        }
     }
 }
 

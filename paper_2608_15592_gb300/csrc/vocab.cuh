@@ -109,9 +109,9 @@ __device__ __forceinline__ float units_max(const uint4* v) {
             x[k] = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
         }
 #pragma unroll
-        for (int w = N / 2; w > 0; w /= 2)
+        for (int w = 1; w < N; w *= 2)
 #pragma unroll
-            for (int k = 0; k < w; ++k) x[k] = __hmax2(x[k], x[k + w]);
+            for (int k = 0; k + w < N; k += 2 * w) x[k] = __hmax2(x[k], x[k + w]);
         return fmaxf(__low2float(x[0]), __high2float(x[0]));
     }
     float x = -INFINITY;
