@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kern
     for (int i = lane; i < kSlots; i += 32) tables[warp][i] = -1;
     __syncwarp();
     for (int64_t u = start; u < end;) {
-        const int64_t r = u / a.rows.nvec, u0 = r * a.rows.nvec;
+        const int64_t r = quotient(u, a.rows.nvec), u0 = r * a.rows.nvec;
         const int c0 = (int)(u - u0), c1 = (int)(min(end, u0 + a.rows.nvec) - u0);
         const char* row = d.base + r * d.ld_bytes;
         Entries e;

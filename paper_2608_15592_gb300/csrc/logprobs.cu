@@ -293,21 +293,23 @@ __device__ __forceinline__ RowStat stream_row(const LpArgs& a, const char* row, 
     return st.row(a.c);
 }
 
-// A row's target and the bits of its logit, asked for where the row begins (lane 0).
+// A row's target and the bits of its logit (lane 0): the one asked for where the row begins, the other, which needs it,
+// behind the stream.
 struct Target {
     int t;
     uint32_t z;
 };
 
-template <bool kBf16>
-__device__ __forceinline__ Target ask_target(const LpArgs& a, int64_t r, const char* row) {
+__device__ __forceinline__ Target ask_target(const LpArgs& a, int64_t r) {
     Target x{-1, 0u};
-    if (a.logprob && (threadIdx.x & 31) == 0 && in_bounds(r < a.rows.n_rows, a.status)) {
-        x.t = a.targets[r];
-        if (x.t >= 0 && x.t < a.rows.V)
-            x.z = kBf16 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[x.t] : reinterpret_cast<const uint32_t*>(row)[x.t];
-    }
+    if (a.logprob && (threadIdx.x & 31) == 0 && in_bounds(r < a.rows.n_rows, a.status)) x.t = a.targets[r];
     return x;
+}
+
+template <bool kBf16>
+__device__ __forceinline__ void ask_logit(const LpArgs& a, const char* row, Target& x) {
+    if (x.t >= 0 && x.t < a.rows.V)
+        x.z = kBf16 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[x.t] : reinterpret_cast<const uint32_t*>(row)[x.t];
 }
 
 // What a row's statistics and list say, written by a warp.
@@ -441,10 +443,10 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(c
     Candidates<kLists>* q = R ? &cand[warp] : nullptr;
     const int64_t start = piece_start(a.rows, w), end = piece_start(a.rows, w + 1);
     for (int64_t u = start; u < end;) {
-        const int64_t r = u / a.rows.nvec, u0 = r * a.rows.nvec;
+        const int64_t r = quotient(u, a.rows.nvec), u0 = r * a.rows.nvec;
         const int c0 = (int)(u - u0), c1 = (int)(min(end, u0 + a.rows.nvec) - u0);
         const char* row = a.rows.base + r * a.rows.ld_bytes;
-        const Target x = ask_target<kBf16>(a, r, row);
+        Target x = ask_target(a, r);
         RowStat st;
         if constexpr (R > 0) {
             clear_list<R>(q);
@@ -452,6 +454,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(c
         } else {
             st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);
         }
+        ask_logit<kBf16>(a, row, x);
         join_lanes(st, a.c);
         bool write = true;
         if (c0 != 0 || c1 != a.rows.nvec) {
@@ -483,7 +486,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_few_kern
     const char* row = a.rows.base + r * a.rows.ld_bytes;
     Candidates<kLists>* q = R ? &cand[warp] : nullptr;
     Target x{-1, 0u};
-    if (warp == 0) x = ask_target<kBf16>(a, r, row);
+    if (warp == 0) x = ask_target(a, r);
     const int c0 = min(a.rows.nvec, (b * kWarps + warp) * a.span), c1 = min(a.rows.nvec, c0 + a.span);
     RowStat st = no_stat();
     if constexpr (R > 0) {
@@ -492,6 +495,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_few_kern
     } else {
         if (c0 < c1) st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);
     }
+    ask_logit<kBf16>(a, row, x);
     join_lanes(st, a.c);
     if (lane == 0) stats[warp] = st;
     __syncthreads();
@@ -661,7 +665,7 @@ __global__ void __launch_bounds__(kVocabThreads, kGradBlocks) logprobs_grad_kern
     const int64_t start = piece_start(a.rows, w), end = piece_start(a.rows, w + 1);
     const float inv_T = 1.f / a.T;
     for (int64_t u = start; u < end;) {
-        const int64_t r = u / a.rows.nvec, u0 = r * a.rows.nvec;
+        const int64_t r = quotient(u, a.rows.nvec), u0 = r * a.rows.nvec;
         const int c0 = (int)(u - u0), c1 = (int)(min(end, u0 + a.rows.nvec) - u0);
         const char* row = a.rows.base + r * a.rows.ld_bytes;
         char* out = a.out + r * a.out_bytes;
@@ -772,9 +776,10 @@ estp_status launch_token_logprobs(estp_ctx* ctx, const void* logits, estp_dtype 
         a.blocks = (int)(batches < want ? batches : want);
         a.span = (a.rows.nvec + a.blocks * kWarps - 1) / (a.blocks * kWarps);
     } else if (top_k > 0 && a.rows.pieces > n_rows) {
-        // a list costs as much to begin as some thousand logits: pieces of whole rows while that idles few warps
-        const int64_t whole = a.rows.pieces / n_rows * n_rows;
-        if (4 * whole >= 3 * a.rows.pieces) a.rows.pieces = whole;
+        // a list costs as much to begin as some thousand logits: pieces of whole rows while that idles few warps (fewer
+        // than 16 a row here, and a row has at most 2^24 units)
+        const int64_t per_row = a.rows.pieces / n_rows;
+        if (4 * per_row * n_rows >= 3 * a.rows.pieces) cut_rows(a.rows, per_row * n_rows, (int)per_row);
     }
     a.targets = targets;
     a.T = T;

@@ -30,23 +30,49 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 
 // ------------------------------------------------------------------ the flat cut
 // The rows as one run of 16-byte units, cut into equal pieces, a warp each: every warp streams the
-// same number of bytes whatever V and n_rows are.
+// same number of bytes whatever V and n_rows are.  (The first `more` pieces have a unit more.)  Or each row into
+// `per_row` pieces.
 struct VocabRows {
     const char* base;
     int64_t ld_bytes;
     int64_t n_rows;
     int64_t units;   // n_rows * nvec
     int64_t pieces;
+    int64_t q, more;
     int32_t V;
     int32_t nvec;    // units of a row (the last one may be partial)
+    int32_t per_row; // 0: equal pieces of all rows
 };
 
-__device__ __forceinline__ int64_t piece_start(const VocabRows& a, int64_t w) { return a.units * w / a.pieces; }
+// Quotients of what nearly always fits 32 bits: a 64-bit division takes some hundred instructions, and
+// a warp makes several before its first load.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return (((uint64_t)a | (uint64_t)b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+__device__ __forceinline__ int64_t piece_start(const VocabRows& a, int64_t w) {
+    if (a.per_row) {
+        const uint32_t r = (uint32_t)w / (uint32_t)a.per_row, i = (uint32_t)w - r * (uint32_t)a.per_row;
+        return (int64_t)r * a.nvec + (uint32_t)a.nvec * i / (uint32_t)a.per_row;  // (both below 2^16 and 2^24: see vocab_rows)
+    }
+    return w * a.q + (w < a.more ? w : a.more);
+}
 
 // The last piece that starts at or before unit u.
 __device__ __forceinline__ int64_t piece_of(const VocabRows& a, int64_t u) {
-    const int64_t w = ((u + 1) * a.pieces - 1) / a.units;
-    return w < a.pieces - 1 ? w : a.pieces - 1;
+    if (a.per_row) {
+        const int64_t r = quotient(u, a.nvec);
+        return r * a.per_row + ((uint32_t)(u - r * a.nvec + 1) * (uint32_t)a.per_row - 1) / (uint32_t)a.nvec;
+    }
+    const int64_t b = a.more * (a.q + 1);
+    return u < b ? quotient(u, a.q + 1) : a.more + quotient(u - b, a.q);
+}
+
+inline void cut_rows(VocabRows& a, int64_t pieces, int per_row) {
+    a.pieces = pieces;
+    a.per_row = per_row;
+    a.q = a.units / pieces;
+    a.more = a.units % pieces;
 }
 
 inline VocabRows vocab_rows(const estp_ctx* ctx, const void* logits, estp_dtype dtype, int64_t n_rows, int64_t V,
@@ -61,7 +87,7 @@ inline VocabRows vocab_rows(const estp_ctx* ctx, const void* logits, estp_dtype 
     a.units = n_rows * a.nvec;
     const int64_t most = (int64_t)ctx->num_sms * blocks * (kVocabThreads / 32);
     const int64_t want = (a.units + min_units - 1) / min_units;
-    a.pieces = want < most ? want : most;
+    cut_rows(a, want < most ? want : most, 0);
     return a;
 }
 
