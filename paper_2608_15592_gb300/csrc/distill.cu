@@ -769,6 +769,50 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kern
     }
 }
 
+// ------------------------------------------------------------------ many short rows
+// A warp a row: both passes read it from memory, the second from the caches.  Where a row is a few KB, a cluster's
+// barriers and its ninth warp take longer than the row: 8192 bf16 rows of 1000 tokens take 81 us by clusters and 30 so; of
+// 2000 fp32 rows of 4000 (16 KB), 30 and 41.
+constexpr int kShortUnits = 256;
+
+template <bool kBf16>
+__global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_short_kernel(const DistillArgs a) {
+    constexpr int kWarps = kVocabThreads / 32;
+    __shared__ Teacher teachers[kWarps];
+    __shared__ Asked asked[kWarps];
+    __shared__ int32_t tables[kWarps][kSlots];
+    __shared__ uint32_t bits[kWarps][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t step = (int64_t)gridDim.x * kWarps;
+    int64_t r = (int64_t)blockIdx.x * kWarps + warp;
+    Teacher& t = teachers[warp];
+    for (int i = lane; i < kSlots; i += 32) tables[warp][i] = -1;
+    __syncwarp();
+    ask_entries(a, r, asked[warp]);
+    for (; r < a.n_rows; r += step) {
+        const char* row = a.base + r * a.ld_bytes;
+        Entries e;
+        take_entries(a, asked[warp], e);
+        check_entries<kBf16>(a, r, e, tables[warp]);
+        const RowStat st = eval_units<kBf16>(a, row, 0, a.nvec, asked[warp].id, bits[warp]);
+        __syncwarp();
+        ask_entries(a, r + step, asked[warp]);
+        put_entries<kBf16>(a, e, t);
+        const Factors f = row_factors(a, t, st);
+        const float loss = row_loss(a, t, st, f);
+        if (lane == 0) a.loss[r] = loss;
+        char* out = a.out + r * a.out_bytes;
+        for (int c = lane; c < a.nvec; c += 32) {
+            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (!f.zero) other_grad<kBf16, false>(f, load_unit<kBf16>(row, c, a.nvec, a.V), a.c, x);
+            store_unit<kBf16>(out, c, a.V, x);
+        }
+        __syncwarp();  // the named tokens go over these
+        put_named<kBf16>(a, r, t, f, 0, a.nvec);
+        __syncwarp();
+    }
+}
+
 // ------------------------------------------------------------------ longer rows
 // A block takes a row in two passes; named units are marked for a span of it at a time.
 constexpr int kLongThreads = 512;
@@ -949,6 +993,16 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
         const unsigned blocks = (unsigned)((v.rows.pieces + kWarps - 1) / kWarps);
         if (bf16) distill_eval_kernel<true><<<blocks, kVocabThreads, 0, st>>>(v);
         else distill_eval_kernel<false><<<blocks, kVocabThreads, 0, st>>>(v);
+        e = cudaGetLastError();
+        return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
+    }
+
+    if (a.nvec <= kShortUnits && n_rows >= (int64_t)ctx->num_sms * 4) {  // (fewer rows leave warps without one)
+        constexpr int kWarps = kVocabThreads / 32;
+        const int64_t want = (n_rows + kWarps - 1) / kWarps, most = (int64_t)ctx->num_sms * kVocabBlocks;
+        const unsigned blocks = (unsigned)(want < most ? want : most);
+        if (bf16) distill_short_kernel<true><<<blocks, kVocabThreads, 0, st>>>(a);
+        else distill_short_kernel<false><<<blocks, kVocabThreads, 0, st>>>(a);
         e = cudaGetLastError();
         return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
     }

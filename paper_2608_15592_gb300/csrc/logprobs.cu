@@ -557,7 +557,7 @@ struct LpGradArgs {
     int* status;
 };
 
-constexpr int kGradUnroll = 4, kGradBlocks = 4;
+constexpr int kGradUnroll = 4, kGradBlocks = 3;
 
 // The tokens of a row that have a term of their own.
 struct Named {

@@ -63,11 +63,26 @@ def test_kinds(cuda_lib, dtype, tail, kind, T):
     _check(cuda_lib.Context(0), R.logits(kind, 14, 1003, dtype), T, 16, tail, weight=False)
 
 
-@pytest.mark.parametrize("V", [300007, 500001])
-def test_long_rows(cuda_lib, V):
-    """The longest that a cluster keeps, and one of more units than a block marks at a time."""
+@pytest.mark.parametrize("V,dtype", [(300007, F32), (500001, F32), (900001, BF)], ids=str)
+def test_long_rows(cuda_lib, V, dtype):
+    """The longest that a cluster keeps, and some of more units than a block marks at a time."""
     for tail in (False, True):
-        _check(cuda_lib.Context(0), R.logits("normal", 2, V, F32, seed=4), 1.0, 24, tail)
+        _check(cuda_lib.Context(0), R.logits("normal", 2, V, dtype, seed=4), 1.0, 24, tail)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tail", [False, True], ids=["renormalised", "tail"])
+@pytest.mark.parametrize("rows,V,K", [(700, 1, 1), (1300, 33, 8), (4000, 40, 33), (650, 1001, 128), (611, 4095, 20)])
+def test_many_short_rows(cuda_lib, dtype, tail, rows, V, K):
+    """A warp a row; some warps take several."""
+    _check(cuda_lib.Context(0), R.logits("normal", rows, V, dtype, seed=rows), 0.8, K, tail, repeat=not tail and K > 2)
+
+
+@pytest.mark.parametrize("rows,V", [(700, 60), (5, 5000)])
+def test_kinds_of_rows_by_either_way(cuda_lib, rows, V):
+    for kind in ("masked", "lowest", "sharp", "ties"):
+        for tail in (False, True):
+            _check(cuda_lib.Context(0), R.logits(kind, rows, V, BF), 1.3, 12, tail)
 
 
 def test_repeated_tokens(cuda_lib):

@@ -56,6 +56,27 @@ def test_shapes(cuda_lib, dtype, rows, V, k):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["normal", "ties", "masked", "equal"])
+@pytest.mark.parametrize("rows,V,k", [(228, 4099, 9), (229, 4099, 9), (250, 30011, 70), (500, 9001, 20), (2500, 1500, 30), (4000, 77, 5)])
+def test_rows_cut_in_every_way(cuda_lib, dtype, kind, rows, V, k):
+    """Blocks a row, pieces of whole rows, equal pieces that begin and end inside rows, several rows a piece."""
+    z = R.logits(kind, rows, V, dtype, seed=V + rows)
+    _check(cuda_lib, cuda_lib.Context(0), z, 1.0, k, _targets(rows, V, 3))
+
+
+@pytest.mark.parametrize("T", [1e-6, 1e-3, 1e4, 1e30])
+def test_extreme_temperatures(cuda_lib, T):
+    for kind in ("normal", "masked"):
+        _check(cuda_lib, cuda_lib.Context(0), R.logits(kind, 9, 3001, F32), T, 8, _targets(9, 3001, 3))
+
+
+def test_a_long_row(cuda_lib):
+    """Two million logits: many blocks a row."""
+    for rows in (1, 3):
+        _check(cuda_lib, cuda_lib.Context(0), R.logits("normal", rows, (1 << 21) + 3, BF), 1.0, 20, _targets(rows, 1 << 21, 3))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("rows,V,k,T", [(13, 300, 20, 0.5), (6, 5003, 100, 1.0), (2, 40001, 40, 3.0)])
 def test_kinds(cuda_lib, dtype, kind, rows, V, k, T):

@@ -156,13 +156,15 @@ def distill(z, T, ids, x, tail):
             other = ~named
             if bool((lp[r][other] > -math.inf).any()):
                 top = lp[r][other].amax()
-                lt = top + torch.logsumexp(lp[r][other] - top, 0)
+                near = lp[r][other] - top  # (beside the type's lowest value the sum's logarithm would be lost)
+                lt = top + torch.logsumexp(near, 0)
+                within = torch.softmax(near, 0)
                 loss[r] += rest * (math.log(rest) - lt)
                 size[r] += rest * (abs(math.log(rest)) + lt.abs() + 1) + 4 * 2.0 ** -24 / SUM(V) * (lt.abs() + 20)
-                share = rest * torch.exp(lp[r][other] - lt)
+                share = rest * within
                 grad_[r][other] -= share
                 # the rest is 1 less a sum: off by a few steps of 1
-                gsize[r][other] += share + torch.exp(lp[r][other] - lt) * 4 * 2.0 ** -24 / SUM(V)
+                gsize[r][other] += share + within * 4 * 2.0 ** -24 / SUM(V)
             else:
                 loss[r] = math.inf
     return loss, grad_ / T, size, gsize * far / T
