@@ -22,6 +22,27 @@ namespace {
 
 constexpr int kK = kMaxAlternatives;
 
+// Sums of two floats (some 48 bits): a + b and a b exactly, and a + b of such.
+struct Two {
+    float hi, lo;
+};
+__device__ __forceinline__ Two two_sum(float a, float b) {
+    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+    return Two{s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ Two two_prod(float a, float b) {
+    const float p = __fmul_rn(a, b);
+    return Two{p, __fmaf_rn(a, b, -p)};
+}
+__device__ __forceinline__ Two plus(Two a, Two b) {
+    const Two s = two_sum(a.hi, b.hi);
+    return Two{s.hi, s.lo + (a.lo + b.lo)};
+}
+__device__ __forceinline__ Two times(Two a, Two b) {
+    const Two p = two_prod(a.hi, b.hi);
+    return Two{p.hi, p.lo + (a.hi * b.lo + a.lo * b.hi)};
+}
+
 struct DistillArgs {
     const char* base;
     int64_t ld_bytes;
@@ -31,6 +52,7 @@ struct DistillArgs {
     const float* teacher;
     int K, tail;
     float T, c;
+    Two inv_T;  // 1 / T
     const float* weight;
     float* loss;
     char* out;
@@ -43,7 +65,8 @@ struct Teacher {
     int32_t id[kK];            // -1: none
     float lq[kK], q[kK], z[kK];  // ln q, q, the student's logit
     RowStat in;                // with the tail: statistics of the named tokens
-    float Q, rest, g;          // g = row weight / T
+    float Q, rest, g;          // the sum of the q, 1 less it, row weight / T
+    float Q_lo, rest_lo;       // what the first two were rounded by
     int some, repeated;        // has entries; has a token twice
 };
 
@@ -197,10 +220,10 @@ __device__ __forceinline__ void put_entries(const DistillArgs& a, const Entries&
         top = fmaxf(top, e.x[i]);
     }
     some = __any_sync(0xffffffffu, some);
-    float Q, rest = 0.f, q[kPer], lq[kPer];
+    float q[kPer], lq[kPer];
+    Two Q{0.f, 0.f}, rest{0.f, 0.f};
     if (a.tail) {
-        // 1 - sum q in 64 bits: each q is a rounded exponential, but their sum adds no error
-        double sum = 0.;
+        // the q are rounded exponentials, but their sum and 1 less it add no error
         RowStat in = no_stat();
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -208,15 +231,20 @@ __device__ __forceinline__ void put_entries(const DistillArgs& a, const Entries&
             q[i] = 0.f;
             if (i * 32 < a.K) {
                 q[i] = expf(e.x[i]);
-                sum += (double)q[i];
+                Q = plus(Q, Two{q[i], 0.f});
                 const bool bad = isnan(z[i]) || z[i] == INFINITY;
                 if (e.id[i] >= 0) join(in, RowStat{z[i], bad ? NAN : z[i] == -INFINITY ? 0.f : 1.f, 0.f}, a.c);
             }
         }
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-        Q = (float)sum;
-        rest = !some || sum > 1. ? 0.f : (float)(1. - sum);
+        for (int off = 16; off > 0; off >>= 1)
+            Q = plus(Q, Two{__shfl_xor_sync(0xffffffffu, Q.hi, off), __shfl_xor_sync(0xffffffffu, Q.lo, off)});
+        Q = two_sum(Q.hi, Q.lo);
+        if (some) {
+            rest = two_sum(1.f, -Q.hi);
+            rest = two_sum(rest.hi, rest.lo - Q.lo);
+            if (rest.hi < 0.f) rest = Two{0.f, 0.f};
+        }
         join_lanes<false>(in, a.c);
         t.in = in;
     } else {
@@ -240,7 +268,7 @@ __device__ __forceinline__ void put_entries(const DistillArgs& a, const Entries&
                 q[i] = none ? 0.f : q[i] / sum;
                 lq[i] -= l;
             }
-        Q = none ? 0.f : 1.f;
+        Q.hi = none ? 0.f : 1.f;
         some = !none;
     }
 #pragma unroll
@@ -253,8 +281,10 @@ __device__ __forceinline__ void put_entries(const DistillArgs& a, const Entries&
         t.z[j] = z[i];
     }
     if (lane == 0) {
-        t.Q = Q;
-        t.rest = rest;
+        t.Q = Q.hi;
+        t.rest = rest.hi;
+        t.Q_lo = Q.lo;
+        t.rest_lo = rest.lo;
         t.some = some;
         t.repeated = e.repeated;
         t.g = e.w / a.T;
@@ -281,9 +311,10 @@ __device__ __forceinline__ Factors row_factors(const DistillArgs& a, const Teach
         if (no_other && f.rest <= 0x1p-20f) f.rest = 0.f;
         // the exponentials of these elements are taken against the maximum that their own sum belongs to
         f.pivot = pivot(st.m);
-        f.A = no_other || f.empty
-                  ? 0.f
-                  : t.g * ((t.Q + f.rest) * ex2(max_nan((f.pivot - f.m) * a.c, kCut)) / all.s - f.rest / st.s);
+        // (Q + q_r) / s - q_r / s_other over one denominator, where s = s_other + s_named: the terms that cancel are gone
+        const float other = st.s * ex2(max_nan((f.pivot - f.m) * a.c, kCut));
+        const float named = t.in.s * ex2(max_nan((t.in.m - f.m) * a.c, kCut));
+        f.A = no_other || f.empty ? 0.f : t.g * ((t.Q * other - f.rest * named) / (all.s * st.s));
     }
     f.M = f.pivot * a.c;
     f.framed = near_frame(f.M);
@@ -291,21 +322,82 @@ __device__ __forceinline__ Factors row_factors(const DistillArgs& a, const Teach
     return f;
 }
 
-// One warp.
+// ln x for x > 0 to about 1e-9: x = 2^k m with m in [3/4, 3/2), ln m = 2 artanh s with s = (m - 1) / (m + 1), |s| <= 1/5.
+// s is carried in two floats, and so are k ln 2 (its first 12 bits times k are exact) and the sum; the series
+// behind 2 s is below 0.006 and needs one.
+__device__ __forceinline__ Two two_log(Two x) {
+    const int b = __float_as_int(x.hi), k = (b - 0x3F400000) >> 23;
+    const float m = __int_as_float(b - (k << 23)), ml = x.lo * __int_as_float((127 - k) << 23);
+    const float n = m - 1.f;  // exact
+    Two d = two_sum(m, 1.f);
+    d.lo += ml;
+    const float s = n / d.hi, sl = (__fmaf_rn(-s, d.hi, n) + (ml - s * d.lo)) / d.hi, w = s * s;
+    float p = 1.f / 13.f;
+    p = fmaf(p, w, 1.f / 11.f);
+    p = fmaf(p, w, 1.f / 9.f);
+    p = fmaf(p, w, 1.f / 7.f);
+    p = fmaf(p, w, 1.f / 5.f);
+    p = fmaf(p, w, 1.f / 3.f);
+    constexpr float kHi = 2839.f / 4096.f, kLo = (float)(0.69314718055994531 - 2839. / 4096.);
+    return plus(Two{(float)k * kHi, (float)k * kLo}, Two{2.f * s, 2.f * (sl + s * w * p)});
+}
+
+// One warp.  From the fp32 sums on in two floats: where student and teacher agree, or both leave nearly everything to the
+// other tokens (a high temperature), the loss is a small difference of terms whose logarithms are off by 1e-6 in one
+// float, and with them a loss of 1e-3 has three digits left.  (64-bit arithmetic does as well and takes 10 % of the
+// whole call, as there are 2 such operations a clock on an SM.)
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const Teacher& t, const RowStat& st, const Factors& f) {
     const int lane = threadIdx.x & 31;
     if (!t.some) return 0.f;
-    const float ls = f.empty ? -INFINITY : logf(f.s);
-    float loss = 0.f;
+    Two sum{0.f, 0.f};
+    float plain = 0.f;
+    bool any = f.rest != 0.f;
     for (int j = lane; j < a.K; j += 32) {
-        const float q = t.q[j];
-        // q first: beside a logit of the type's lowest value ln p may exceed fp32 where the loss does not
-        if (t.id[j] >= 0 && q != 0.f) loss += f.empty ? INFINITY : q * (t.lq[j] + ls) + q * (f.m - t.z[j]) / a.T;
+        const float q = t.q[j], z = t.z[j];
+        if (t.id[j] >= 0 && q != 0.f) {
+            any = true;
+            plain += q * t.lq[j] + q * (f.m - z) / a.T;
+            const Two y = times(two_sum(z, -f.m), a.inv_T);
+            sum = plus(sum, times(Two{q, 0.f}, plus(Two{t.lq[j], 0.f}, Two{-y.hi, -y.lo})));
+        }
     }
-    loss = warp_sum(loss);
-    if (f.rest != 0.f)
-        loss += f.rest * (logf(f.rest) - (st.s == 0.f ? -INFINITY : (f.pivot - f.m) / a.T + (logf(st.s) - ls)));
-    return loss;
+    any = __any_sync(0xffffffffu, any);
+    plain = warp_sum(plain);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+        sum = plus(sum, Two{__shfl_xor_sync(0xffffffffu, sum.hi, off), __shfl_xor_sync(0xffffffffu, sum.lo, off)});
+    if (f.empty) return any ? INFINITY : 0.f;
+    if (f.rest != 0.f && st.s == 0.f) return INFINITY;
+    // infinite, NaN, or near a float's end (tokens at the type's lowest value): in one float
+    if (!(fabsf(plain) < 1e4f) || isnan(f.s) || (f.rest != 0.f && !(f.pivot - f.m > -1e30f))) {
+        plain += t.Q * logf(f.s);
+        if (f.rest != 0.f) plain += f.rest * (logf(f.rest) - logf(st.s) + logf(f.s)) + f.rest * (f.m - f.pivot) / a.T;
+        return plain;
+    }
+    // ln of the sum, of what the teacher leaves to the others, and of what the student does: 1 - sum p_id while that is at
+    // least a half, else by their own sum
+    Two left{1.f, 0.f};
+    bool direct = false;
+    if (a.tail) {
+        const float num = t.in.s * ex2(max_nan((t.in.m - f.m) * a.c, kCut)), named = num / f.s;
+        direct = !(named <= 0.5f);
+        left = two_sum(1.f, -named);
+        left.lo -= __fmaf_rn(-named, f.s, num) / f.s;
+        if (direct) left = Two{st.s, 0.f};
+    }
+    const Two rest{t.rest, t.rest_lo};
+    const Two l = two_log(lane == 0 ? Two{f.s, 0.f} : lane == 1 ? rest : left);
+    const Two ls{__shfl_sync(0xffffffffu, l.hi, 0), __shfl_sync(0xffffffffu, l.lo, 0)};
+    sum = plus(sum, times(Two{t.Q, t.Q_lo}, ls));
+    if (f.rest != 0.f) {
+        const Two lrest{__shfl_sync(0xffffffffu, l.hi, 1), __shfl_sync(0xffffffffu, l.lo, 1)};
+        Two lp{__shfl_sync(0xffffffffu, l.hi, 2), __shfl_sync(0xffffffffu, l.lo, 2)};
+        if (direct) {
+            lp = plus(plus(times(two_sum(f.pivot, -f.m), a.inv_T), lp), Two{-ls.hi, -ls.lo});
+        }
+        sum = plus(sum, times(rest, plus(lrest, Two{-lp.hi, -lp.lo})));
+    }
+    return sum.hi + sum.lo;
 }
 
 // The gradient at a named token, given what it would be were it not one.
@@ -976,6 +1068,8 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
     a.tail = tail;
     a.T = T;
     a.c = (float)(1.4426950408889634 / (double)T);
+    const double inv_T = 1. / (double)T;
+    a.inv_T = Two{(float)inv_T, (float)(inv_T - (double)(float)inv_T)};
     a.weight = weight;
     a.loss = loss;
     a.out = static_cast<char*>(out);

@@ -148,6 +148,28 @@ def test_a_tail_that_is_far_below(cuda_lib):
     assert bool((grad[0, 12:] < 0).all())
 
 
+@pytest.mark.parametrize("V,K,T", [(4001, 8, 3.0), (32000, 20, 2.0), (300, 4, 1.0), (9000, 1, 2.0)])
+def test_a_small_loss_keeps_its_digits(cuda_lib, V, K, T):
+    """A student near its teacher, most of whose mass lies in the rest: the loss is far below its terms.  What is off: the
+    named tokens' share of the sums (SUM(V) and two roundings of an exponent of some 20, 2^-19, relative), q by two steps,
+    and the result's rounding; the logarithms' errors would be 2^-20 of 1."""
+    ctx, rows = cuda_lib.Context(0), 6
+    z = R.logits("normal", rows, V, F32, seed=V) / 3
+    g = torch.Generator().manual_seed(K)
+    teacher = z.double() + 0.02 * torch.randn(rows, V, generator=g, dtype=torch.float64)
+    lt = torch.log_softmax(teacher / T, 1)
+    ids = torch.topk(lt, K, dim=1).indices
+    x = lt.gather(1, ids).float()
+    loss, grad = ctx.distill_loss(R.padded(z), ids.int().cuda(), x.cuda(), temperature=T, tail=True)
+    ctx.sync_status()
+    want, gwant, _, gsize = R.distill(z, T, ids.int(), x, True)
+    named = R.softmax(z, T)[1].gather(1, ids).sum(1) + x.double().exp().sum(1)
+    allowed = (R.SUM(V) + 2.0 ** -19) * named + 2.0 ** -22 * want
+    assert float(named.max()) < 1.5 and float((want / named).max()) < 0.05  # the case that is meant
+    R.close(loss, want, allowed, "loss")
+    R.close(grad, gwant, (2 * R.SUM(V) + 2.0 ** -21) * gsize, "gradient")
+
+
 def test_gradient_agrees_with_differences(cuda_lib):
     ctx, rows, V, K = cuda_lib.Context(0), 3, 41, 5
     z = R.logits("normal", rows, V, F32, seed=2)
