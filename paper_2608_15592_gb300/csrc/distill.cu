@@ -863,9 +863,27 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kern
 
 // ------------------------------------------------------------------ many short rows
 // A warp a row: both passes read it from memory, the second from the caches.  Where a row is a few KB, a cluster's
-// barriers and its ninth warp take longer than the row: 8192 bf16 rows of 1000 tokens take 81 us by clusters and 30 so; of
-// 2000 fp32 rows of 4000 (16 KB), 30 and 41.
-constexpr int kShortUnits = 256;
+// barriers and its ninth warp take longer than the row.  By clusters and so, us: 8192 bf16 rows of 1000 tokens 91 and
+// 32, of 2500 95 and 46, 7880 of 4707 (589 units) 103 and 73, 8192 of 8000 109 and 114; 1000 of 4707 25 and 28.
+constexpr int kShortUnits = 256;    // at most, with a row for every sixth warp
+constexpr int kManyShortUnits = 640;  // at most, with one for every warp
+
+template <bool kBf16, bool kFramed>
+__device__ __forceinline__ void short_grad(const DistillArgs& a, const Factors& f, const char* row, char* out) {
+    constexpr int N = 4;
+    const int lane = threadIdx.x & 31;
+    for (int b = lane; b < a.nvec; b += 32 * N) {
+        uint4 v[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = load_unit<kBf16>(row, b + 32 * k, a.nvec, a.V);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float x[8];
+            other_grad<kBf16, kFramed>(f, v[k], a.c, x);
+            if (b + 32 * k < a.nvec) store_unit<kBf16>(out, b + 32 * k, a.V, x);
+        }
+    }
+}
 
 template <bool kBf16>
 __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_short_kernel(const DistillArgs a) {
@@ -894,10 +912,13 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_short_ker
         const float loss = row_loss(a, t, st, f);
         if (lane == 0) a.loss[r] = loss;
         char* out = a.out + r * a.out_bytes;
-        for (int c = lane; c < a.nvec; c += 32) {
-            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (!f.zero) other_grad<kBf16, false>(f, load_unit<kBf16>(row, c, a.nvec, a.V), a.c, x);
-            store_unit<kBf16>(out, c, a.V, x);
+        if (f.zero) {
+            const float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            for (int c = lane; c < a.nvec; c += 32) store_unit<kBf16>(out, c, a.V, x);
+        } else if (f.framed) {
+            short_grad<kBf16, true>(a, f, row, out);
+        } else {
+            short_grad<kBf16, false>(a, f, row, out);
         }
         __syncwarp();  // the named tokens go over these
         put_named<kBf16>(a, r, t, f, 0, a.nvec);
@@ -1076,6 +1097,7 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
     a.out_bytes = ld_out * esize(dtype);
     a.status = ctx->status;
     cudaError_t e;
+    constexpr int kWarps = kVocabThreads / 32;
 
     if (!out) {
         EvalArgs v;
@@ -1083,7 +1105,6 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
         v.rows = vocab_rows(ctx, logits, dtype, n_rows, V, ld, 32 * kVocabUnroll, kVocabBlocks);
         v.part = ctx->vocab_part;
         v.count = ctx->vocab_count;
-        constexpr int kWarps = kVocabThreads / 32;
         const unsigned blocks = (unsigned)((v.rows.pieces + kWarps - 1) / kWarps);
         if (bf16) distill_eval_kernel<true><<<blocks, kVocabThreads, 0, st>>>(v);
         else distill_eval_kernel<false><<<blocks, kVocabThreads, 0, st>>>(v);
@@ -1091,8 +1112,8 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
         return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
     }
 
-    if (a.nvec <= kShortUnits && n_rows >= (int64_t)ctx->num_sms * 4) {  // (fewer rows leave warps without one)
-        constexpr int kWarps = kVocabThreads / 32;
+    const int64_t at_once = (int64_t)ctx->num_sms * kVocabBlocks * kWarps;
+    if (a.nvec <= kManyShortUnits && n_rows * 6 >= at_once && (a.nvec <= kShortUnits || n_rows >= at_once)) {
         const int64_t want = (n_rows + kWarps - 1) / kWarps, most = (int64_t)ctx->num_sms * kVocabBlocks;
         const unsigned blocks = (unsigned)(want < most ? want : most);
         if (bf16) distill_short_kernel<true><<<blocks, kVocabThreads, 0, st>>>(a);
@@ -1114,16 +1135,16 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
     for (int c = 1; c <= kMaxCluster; ++c) {
         const size_t bytes = rows_bytes(a.nvec, c);
         if (bytes > (size_t)kSliceBytes) continue;
-        const int per_sm = ctas_per_sm(bytes), at_once = clusters_at_once(ctx, kernel, bf16, c, bytes, per_sm);
-        if (at_once < 1) continue;
+        const int per_sm = ctas_per_sm(bytes), fit = clusters_at_once(ctx, kernel, bf16, c, bytes, per_sm);
+        if (fit < 1) continue;
         const int64_t share = (n_rows * c + ctx->num_sms - 1) / ctx->num_sms;  // CTAs an SM really has
         const double together = share < per_sm ? (double)share : (double)per_sm;
-        const double cost = (double)((n_rows + at_once - 1) / at_once) *
+        const double cost = (double)((n_rows + fit - 1) / fit) *
                             (0.72 * ((a.nvec + c - 1) / c) * (together < 2.5 ? 2.5 : together) + 2000.);
         if (C == 0 || cost < best) {
             best = cost;
             C = c;
-            clusters = n_rows < at_once ? (int)n_rows : at_once;
+            clusters = n_rows < fit ? (int)n_rows : fit;
         }
     }
     if (C == 0) {  // longer than the largest cluster keeps

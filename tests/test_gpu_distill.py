@@ -72,7 +72,7 @@ def test_long_rows(cuda_lib, V, dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("tail", [False, True], ids=["renormalised", "tail"])
-@pytest.mark.parametrize("rows,V,K", [(700, 1, 1), (1300, 33, 8), (4000, 40, 33), (650, 1001, 128), (611, 4095, 20)])
+@pytest.mark.parametrize("rows,V,K", [(700, 1, 1), (1300, 33, 8), (4000, 40, 33), (650, 1001, 128), (611, 4095, 20), (3700, 1200, 9)])
 def test_many_short_rows(cuda_lib, dtype, tail, rows, V, K):
     """A warp a row; some warps take several."""
     _check(cuda_lib.Context(0), R.logits("normal", rows, V, dtype, seed=rows), 0.8, K, tail, repeat=not tail and K > 2)
