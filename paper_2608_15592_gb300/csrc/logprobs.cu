@@ -4,8 +4,15 @@
 // logprobs_kernel streams the logits once: a warp takes one of the equal pieces of the flat run of
 // 16-byte units (vocab.cuh), keeps (m, s, t) per lane and, where alternatives are asked for, the
 // list of the 32 R greatest logits it has met.  A row that lies within a piece is finished by its warp; of a
-// row cut between warps each writes its part (a block that lies in one row one part), and whoever writes a
-// row's last part joins all of them, in an order that does not depend on who that is.
+// row cut between warps each writes its part, and the warp that writes a row's last part joins all of them, in an
+// order that does not depend on which it is.  Where rows are few, logprobs_few_kernel gives each a number of blocks,
+// whose warps join their parts in shared memory first.
+//
+// Bound: the read of the logits.  42 instructions and 8 exponentials for 256 bf16 logits leave the issue slots half idle
+// at the memory's rate: 4096 rows of 128256 tokens in 162 us (6.5 TB/s), 2048 of 152064 in 103; some 14 us of a call are
+// its launch, the first loads and the last row's join, which is what 1024 rows (60 us for 46 us of bytes) and less pay.
+// Alternatives add what their candidates take: 1537 rows of 152064 in 132 us with 64, 48 % of the instructions for
+// the lists (sorting 64 at a time is half of that).
 //
 // The list.  A candidate is a 64-bit key: the logit's bits in the order of the numbers above the token's
 // index, inverted; so keys are unique, a greater key is a greater logit or the same one at a lower
@@ -625,7 +632,7 @@ __device__ __forceinline__ void grad_chunk(const char* row, char* out, int chunk
         uint4 v[kGradUnroll];
         const int64_t at = (int64_t)(b + lane) * 16;
 #pragma unroll
-        for (int k = 0; k < kGradUnroll; ++k) v[k] = ld_stream(row + at + k * 512);
+        for (int k = 0; k < kGradUnroll; ++k) v[k] = ld_once(row + at + k * 512);
 #pragma unroll
         for (int k = 0; k < kGradUnroll; ++k) {
             float x[8];
@@ -654,6 +661,10 @@ __device__ __forceinline__ void grad_chunk(const char* row, char* out, int chunk
 
 // A warp a piece, as in the forward pass; a lane reads a unit before it writes it, so the gradient may
 // take the logits' place.
+//
+// Bound: the read and the write.  4096 rows of 128256 tokens in 339 us (6.2 TB/s of both); a kernel that only reads
+// and writes takes 323 to 343 with as many warps and loads.  Three blocks an SM of four loads a lane: 335, four blocks 341, two
+// of eight loads 333 but 26 instead of 23 for 501 fp32 rows of 32001.
 template <bool kBf16>
 __global__ void __launch_bounds__(kVocabThreads, kGradBlocks) logprobs_grad_kernel(const LpGradArgs a) {
     constexpr int per = kBf16 ? 8 : 4;
@@ -770,7 +781,7 @@ estp_status launch_token_logprobs(estp_ctx* ctx, const void* logits, estp_dtype 
     a.blocks = a.span = 0;
     if (n_rows <= most / 2) {
         // Blocks a row: two for every place on the GPU between all rows, a batch a warp at least.  One row of 152064
-        // tokens with 20 alternatives takes NN us, by equal pieces and a second launch that joined them 19.
+        // tokens with 20 alternatives takes 11.5 us, by equal pieces and a second launch that joined them 19.
         const int64_t batches = ((int64_t)a.rows.nvec + kWarps * 32 * kVocabUnroll - 1) / (kWarps * 32 * kVocabUnroll);
         const int64_t want = 2 * most / n_rows;
         a.blocks = (int)(batches < want ? batches : want);

@@ -15,8 +15,8 @@
 namespace estp {
 
 constexpr int kVocabThreads = 256;
-constexpr int kVocabBlocks = 3;       // resident blocks an SM the registers of the streams are sized for
-constexpr int kVocabUnroll = 8;       // 16-byte loads a lane has in flight
+constexpr int kVocabBlocks = 3;       // resident blocks an SM the registers of the streams are sized for: 80 a thread
+constexpr int kVocabUnroll = 8;       // 16-byte loads a lane has in flight: 96 KB an SM, twice what its share of the memory's rate needs
 constexpr int kMaxAlternatives = 128;  // entries of a row's list
 constexpr int64_t kMaxVocab = 1 << 26;  // the index of a row's 16-byte unit in 24 bits
 constexpr float kMinTemperature = 1e-6f;  // log2(e) / T stays far from overflow
@@ -262,12 +262,23 @@ __device__ __forceinline__ uint4 masked_unit() {
     return make_uint4(w, w, w, w);
 }
 
+// A 16-byte load past L1 of memory that the kernel may write as well (ld_stream's must not be: a gradient may take
+// its logits' place).
+__device__ __forceinline__ uint4 ld_once(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.L2::256B.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p)
+                 : "memory");
+    return v;
+}
+
 // Unit c of a row whose units end at c1; past it, and past V, -inf.
 template <bool kBf16>
 __device__ __forceinline__ uint4 load_unit(const char* row, int c, int c1, int V) {
     constexpr int per = kBf16 ? 8 : 4;
     if (c >= c1) return masked_unit<kBf16>();
-    uint4 v = ld_stream(row + (int64_t)c * 16);
+    uint4 v = ld_once(row + (int64_t)c * 16);
     if (V - c * per < per) mask_unit<kBf16>(v, V - c * per);
     return v;
 }
