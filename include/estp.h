@@ -472,7 +472,9 @@ estp_status estp_cache_evict(estp_ctx* ctx, const estp_kv_cache* cache, const in
  * token, p = 0), or the type's lowest value.  A row of -inf alone has ln p = -inf, entropy 0 and
  * gradients of 0.  A row that holds NaN or +inf gives NaN.  Sums are held in fp32.
  * Their scratch has a fixed size and comes with the context: they allocate nothing, a first call may
- * be captured in a graph.
+ * be captured in a graph.  estp_token_logprobs and the loss without its gradient use it, so such calls
+ * (and graphs of them) on one context that overlap on the GPU race on it: order them, as those of
+ * estp_token_entropy, or take a context for each stream.
  *
  * Log probabilities of given tokens, with entropy and the greatest alternatives:
  *   targets          : int32 [n_rows], a token of each row; negative: none (its log probability is
