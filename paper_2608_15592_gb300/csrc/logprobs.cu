@@ -11,8 +11,10 @@
 // Bound: the read of the logits.  42 instructions and 8 exponentials for 256 bf16 logits leave the issue slots half idle
 // at the memory's rate: 4096 rows of 128256 tokens in 162 us (6.5 TB/s), 2048 of 152064 in 103; some 14 us of a call are
 // its launch, the first loads and the last row's join, which is what 1024 rows (60 us for 46 us of bytes) and less pay.
-// Alternatives add what their candidates take: 1537 rows of 152064 in 132 us with 64, 48 % of the instructions for
-// the lists (sorting 64 at a time is half of that).
+// Alternatives add what their candidates take: 1537 rows of 152064 in 125 us with 64, 44 % of the instructions for
+// the lists, in chains that five warps a scheduler issue at 2.1 a clock.  Measured beside it: bounds not shared between the
+// warps of a row 133; candidates kept in no order and thinned out by the bits of their keys 127; the next batch copied into shared
+// memory meanwhile 140 and four blocks an SM with four loads 142 (both take more instructions).
 //
 // The list.  A candidate is a 64-bit key: the logit's bits in the order of the numbers above the token's
 // index, inverted; so keys are unique, a greater key is a greater logit or the same one at a lower
@@ -21,7 +23,8 @@
 // passes goes to a buffer in shared memory, which is sorted and merged into the list when
 // it holds 32 R candidates.  The bound starts as a logit that at least top_k of the first batch's
 // partial maxima reach, and after each merge is the next number above the list's entry top_k (later
-// tokens have higher indices: equals lose).  Of n logits about top_k ln(n / top_k) pass.
+// tokens have higher indices: equals lose), or what the warps on the same row have all reached in part (post).  Of n logits
+// about top_k ln(n / top_k) pass.
 #include "vocab.cuh"
 
 namespace estp {
@@ -113,7 +116,30 @@ struct Candidates {
     uint64_t waiting[kBatch + 256];  // a unit of each lane goes in before the count is looked at again
     uint32_t units[32 + 32 * kVocabUnroll];  // a batch adds up to 32 kVocabUnroll; they are taken by 32
     int count, n_units;
+    int first_mate, mates, each;  // warps that stream this row too, itself among them, from this one; 1: none
+    uint32_t row;                 // (+ 1)
+    volatile uint64_t posted;     // a row (+ 1) above the ordered bits of a logit that `each` of the warp's tokens reach
 };
+
+// What the warps of a block that stream the same row tell each other.  A logit that `each` tokens of each of the `mates`
+// reach is reached by mates x each >= top_k tokens of the row: smaller ones cannot be alternatives, whatever the
+// warps still meet.  What is posted is read as it comes, which changes how much is looked at and not what is found.
+template <int R>
+__device__ __forceinline__ void post(Candidates<R>* q, uint32_t bits) {
+    const uint64_t x = (uint64_t)q->row << 32 | bits;  // (a warp's rows ascend)
+    if ((threadIdx.x & 31) == 0 && x > q->posted) q->posted = x;
+}
+template <int R>
+__device__ __forceinline__ float shared_bound(const Candidates<R>* q) {
+    const int lane = threadIdx.x & 31;
+    uint32_t bits = 0xFFFFFFFFu;
+    if (lane < q->mates) {
+        const uint64_t x = (q + q->first_mate + lane)->posted;
+        bits = (uint32_t)(x >> 32) == q->row ? (uint32_t)x : 0u;
+    }
+    bits = __reduce_min_sync(0xffffffffu, bits);
+    return bits > 0x007FFFFFu ? unordered(bits) : -INFINITY;
+}
 
 // Merges waiting candidates into the list, whole batches or (all) every one.
 template <int R>
@@ -183,7 +209,11 @@ __device__ __noinline__ float take_units(Candidates<R>* q, const char* row, int 
         if (q->count >= 32 * R) {
             take_waiting<R>(q, top_k, false);
             last = q->list[top_k - 1];
-            if (last) cut = fmaxf(cut, key_logit(last));
+            if (q->mates > 1) {
+                if (const uint64_t x = q->list[q->each - 1]) post<R>(q, (uint32_t)(x >> 32));
+                floor = fmaxf(floor, shared_bound<R>(q));
+            }
+            cut = fmaxf(floor, last ? key_logit(last) : floor);
         }
         __syncwarp();
     }
@@ -207,24 +237,37 @@ __device__ __forceinline__ void merge_block(Candidates<R>* cand) {
 // and write_row fills it up.
 constexpr float kLowest = -3.4028234663852886e38f;
 
-// A logit that at least top_k of the warp's 32 G values reach (or -inf): the order bits from the top
-// down, as far as 16 of them go.
+// A logit that at least top_k of the warp's 32 G values reach and hardly more (or -inf): the order bits from the first one
+// down in which the values differ, as far as 16 of them go.  `shared`: the ordered bits of the greatest logit met on the
+// way that `each` <= top_k of them reach.
 template <int G>
-__device__ __forceinline__ float reached_by(const float (&x)[G], int top_k) {
-    uint32_t o[G];
+__device__ __forceinline__ float reached_by(const float (&x)[G], int top_k, int each, uint32_t& shared) {
+    uint32_t o[G], lo = 0xFFFFFFFFu, hi = 0;
 #pragma unroll
-    for (int g = 0; g < G; ++g) o[g] = ordered(x[g]);
-    uint32_t t = 0;
-    for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t cand = t | 1u << bit;
+    for (int g = 0; g < G; ++g) {
+        o[g] = ordered(x[g]);
+        lo = min(lo, o[g]);
+        hi = max(hi, o[g]);
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    shared = 0;
+    int bit = 31 - __clz(lo ^ hi);  // -1: all alike
+    uint32_t t = bit < 0 ? hi : hi & ~((2u << bit) - 1);
+#pragma unroll 1
+    for (; bit >= 16; --bit) {
+        const uint32_t next = t | 1u << bit;
         int n = 0;
 #pragma unroll
-        for (int g = 0; g < G; ++g) n += __popc(__ballot_sync(0xffffffffu, o[g] >= cand));
+        for (int g = 0; g < G; ++g) n += __popc(__ballot_sync(0xffffffffu, o[g] >= next));
         if (n >= top_k) {
-            t = cand;
-            if (n == top_k) break;
+            t = next;
+            if (n <= top_k + top_k / 8) break;
+        } else if (n >= each) {
+            shared = max(shared, next);
         }
     }
+    shared = max(shared, t);
     return t <= 0x007FFFFFu ? -INFINITY : unordered(t);  // at or below the order of -inf
 }
 
@@ -267,20 +310,24 @@ __device__ __forceinline__ RowStat stream_row(const LpArgs& a, const char* row, 
 #pragma unroll
             for (int k = 0; k < kVocabUnroll; ++k) v[k] = load_unit<kBf16>(row, c + 32 * k, c1, V);
         }
-        const float bm = units_max<kBf16, kVocabUnroll>(v);
+        const UnitMaxima<kBf16, kVocabUnroll> um(v);
+        const float bm = um.all();
         if constexpr (R > 0) {
             if (b == c0) {
-                constexpr int G = 2 * R, w = kVocabUnroll / G;
+                constexpr int G = 2 * R, w = kVocabUnroll / G;  // 64 R maxima
                 float g[G];
 #pragma unroll
                 for (int i = 0; i < G; ++i) g[i] = units_max<kBf16, w>(v + i * w);
-                floor = bound = fmaxf(reached_by<G>(g, a.top_k), kLowest);
+                uint32_t shared;
+                floor = bound = fmaxf(reached_by<G>(g, a.top_k, q->each, shared), kLowest);
+                if (q->mates > 1) post<R>(q, shared);
+            } else if (q->mates > 1) {
+                floor = fmaxf(floor, shared_bound<R>(q));
+                bound = fmaxf(bound, floor);
             }
             // units with candidates are queued; the longer part waits until the batch is in the sums
             if (__any_sync(0xffffffffu, bm >= bound)) {
-                uint32_t hits = 0;
-#pragma unroll
-                for (int k = 0; k < kVocabUnroll; ++k) hits |= units_max<kBf16, 1>(v + k) >= bound ? 1u << k : 0u;
+                uint32_t hits = um.reached(bound);
                 if (hits)
                     for (int at = atomicAdd(&q->n_units, __popc(hits)); hits; hits &= hits - 1, ++at)
                         if (in_bounds(at < 32 + 32 * kVocabUnroll, a.status)) q->units[at] = (uint32_t)(c - c0 + 32 * (__ffs(hits) - 1));
@@ -431,11 +478,17 @@ __device__ __forceinline__ void merge_parts(const LpArgs& a, int64_t slot0, int6
 }
 
 template <int R>
-__device__ __forceinline__ void clear_list(Candidates<R>* q) {
+__device__ __forceinline__ void clear_list(Candidates<R>* q, uint32_t row, int first_mate, int mates, int top_k) {
     const int lane = threadIdx.x & 31;
     __syncwarp();
     for (int i = lane; i < 32 * R; i += 32) q->list[i] = 0;
-    if (lane == 0) q->count = q->n_units = 0;
+    if (lane == 0) {
+        q->count = q->n_units = 0;
+        q->row = row;
+        q->first_mate = first_mate;
+        q->mates = mates;
+        q->each = (top_k + mates - 1) / mates;
+    }
     __syncwarp();
 }
 
@@ -445,7 +498,11 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(c
     constexpr int kLists = R ? R : 1;
     __shared__ Candidates<kLists> cand[R ? kWarps : 1];
     const int warp = threadIdx.x >> 5;
-    const int64_t w = (int64_t)blockIdx.x * kWarps + warp;
+    const int64_t first = (int64_t)blockIdx.x * kWarps, w = first + warp;
+    if constexpr (R > 0) {
+        if (threadIdx.x < kWarps) cand[threadIdx.x].posted = 0;
+        __syncthreads();
+    }
     if (w >= a.rows.pieces) return;
     Candidates<kLists>* q = R ? &cand[warp] : nullptr;
     const int64_t start = piece_start(a.rows, w), end = piece_start(a.rows, w + 1);
@@ -456,7 +513,13 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(c
         Target x = ask_target(a, r);
         RowStat st;
         if constexpr (R > 0) {
-            clear_list<R>(q);
+            int mate = warp, mates = 1;
+            if (c0 != 0 || c1 != a.rows.nvec) {
+                const int64_t lo = piece_of(a.rows, u0) - first, hi = piece_of(a.rows, u0 + a.rows.nvec - 1) - first;
+                mate = lo > 0 ? (int)lo : 0;
+                mates = (int)(hi < kWarps - 1 ? hi : kWarps - 1) - mate + 1;
+            }
+            clear_list<R>(q, (uint32_t)r + 1, mate - warp, mates, a.top_k);
             st = stream_row<kBf16, R>(a, row, c0, c1, q);
         } else {
             st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);
@@ -497,7 +560,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_few_kern
     const int c0 = min(a.rows.nvec, (b * kWarps + warp) * a.span), c1 = min(a.rows.nvec, c0 + a.span);
     RowStat st = no_stat();
     if constexpr (R > 0) {
-        clear_list<R>(q);
+        clear_list<R>(q, 1, 0, 1, a.top_k);
         if (c0 < c1) st = stream_row<kBf16, R>(a, row, c0, c1, q);
     } else {
         if (c0 < c1) st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);

@@ -147,6 +147,45 @@ __device__ __forceinline__ float units_max(const uint4* v) {
     return x;
 }
 
+// The maxima of N units of a lane, of which bf16 ones stay a pair each.
+template <bool kBf16, int N>
+struct UnitMaxima {
+    __nv_bfloat162 x[kBf16 ? N : 1];
+    float y[kBf16 ? 1 : N];
+    __device__ __forceinline__ explicit UnitMaxima(const uint4 (&v)[N]) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v[k]);
+            if constexpr (kBf16) x[k] = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+            else y[k] = units_max<false, 1>(&v[k]);
+        }
+    }
+    __device__ __forceinline__ float all() const {
+        if constexpr (kBf16) {
+            __nv_bfloat162 m = x[0];
+#pragma unroll
+            for (int k = 1; k < N; ++k) m = __hmax2(m, x[k]);
+            return fmaxf(__low2float(m), __high2float(m));
+        } else {
+            float m = y[0];
+#pragma unroll
+            for (int k = 1; k < N; ++k) m = fmaxf(m, y[k]);
+            return m;
+        }
+    }
+    // The units that hold a logit of at least `bound`, a bit each (a bf16 logit reaches what rounds up to it).
+    __device__ __forceinline__ uint32_t reached(float bound) const {
+        uint32_t hits = 0;
+        const __nv_bfloat162 b = __bfloat162bfloat162(__float2bfloat16_ru(bound));
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            if constexpr (kBf16) hits |= __hge2_mask(x[k], b) != 0u ? 1u << k : 0u;
+            else hits |= y[k] >= bound ? 1u << k : 0u;
+        }
+        return hits;
+    }
+};
+
 // Two consecutive elements of a unit, as fp32.
 template <bool kBf16>
 __device__ __forceinline__ float2 pair(const uint4& v, int i) {
