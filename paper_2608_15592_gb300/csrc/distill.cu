@@ -149,7 +149,7 @@ __device__ __forceinline__ void take_entries(const DistillArgs& a, const Asked& 
 
 // Tokens outside of the vocabulary are left out; repeated ones are found by a table of kSlots places with linear
 // probing, empty (-1) before and after.  Then the logits are asked for.
-constexpr int kSlots = 512;
+constexpr int kSlots = 256;
 template <bool kBf16>
 __device__ __forceinline__ void check_entries(const DistillArgs& a, int64_t r, Entries& e, int32_t* table) {
     const int lane = threadIdx.x & 31;
@@ -164,7 +164,7 @@ __device__ __forceinline__ void check_entries(const DistillArgs& a, int64_t r, E
             bad = true;
             e.id[i] = -1;
         }
-        slot[i] = (uint32_t)e.id[i] * 2654435761u >> 23;
+        slot[i] = (uint32_t)e.id[i] * 2654435761u >> 24;
         old[i] = e.id[i] >= 0 ? atomicCAS(&table[slot[i]], -1, e.id[i]) : -1;
     }
 #pragma unroll
@@ -520,11 +520,44 @@ __device__ __forceinline__ void copies_wait(int left) {
     }
 }
 
+// Elements of a unit whose bits are set in `marks` become -inf.
+template <bool kBf16>
+__device__ __forceinline__ uint4 mask_marked(uint4 v, uint32_t marks) {
+    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+    for (int e = 0; e < (kBf16 ? 8 : 4); ++e)
+        if (marks >> e & 1) {
+            if (!kBf16) w[e] = 0xFF800000u;
+            else if (e & 1) w[e >> 1] = (w[e >> 1] & 0x0000FFFFu) | 0xFF800000u;
+            else w[e >> 1] = (w[e >> 1] & 0xFFFF0000u) | 0x0000FF80u;
+        }
+    return v;
+}
+
+// The three forms of the kernel: the code of a row's loops should be short, as 27 warps in three places of it share an SM's
+// instruction caches.  (One kernel for all: 2048 rows of 128256 tokens 183 us, by forms 179; 8192 of 32000 202 and 183.)
+// With the tail, named tokens are not in the sums.  Making marks for them takes the ninth warp longer than it takes
+// the workers to look a few tokens through: by tokens and by marks, us, 1021 rows of 152064 with 32 named 130 and
+// 134, 2048 of 128256 with 64 209 and 208, 8192 of 32000 with 64 263 and 236.
+constexpr int kTailFew = 1, kTailMarks = 2;
+constexpr int kFewNamed = 32;
+
+// Named tokens of a warp's 32 units become -inf: `units` marks the units that hold some, whose bytes of marks, a bit each,
+// stand in their order from `first` on.
+template <bool kBf16>
+__device__ __noinline__ uint4 mask_named(uint4 v, uint32_t units, const uint8_t* first) {
+    const int lane = threadIdx.x & 31;
+    if (units >> lane & 1) v = mask_marked<kBf16>(v, first[__popc(units & ((1u << lane) - 1))]);
+    return v;
+}
+
 // A CTA's slice of a row: n units, the row's u0-th on; a worker's are tid, tid + kWork, .. in groups of kGroup, the last
 // one of what is left.
 struct Slice {
     uint4* kept;
-    const uint32_t* bits;  // with the tail: units that hold a named token
+    const uint32_t* bits;   // with the tail: units that hold a named token, and behind them the place of each 32's first one
+    int words;              // among
+    const uint8_t* marks;
     int n, u0;
 };
 
@@ -560,7 +593,7 @@ __device__ __forceinline__ void copy_group(const Slice& s, int at, bool last, co
 }
 
 // N of the worker's units, from `at` on, into the statistics.
-template <bool kBf16, int N>
+template <bool kBf16, int kTail, int N>
 __device__ __forceinline__ void hold_units(const DistillArgs& a, const Teacher& t, const Slice& s, int at, bool last,
                                            LaneStat<false>& st) {
     constexpr int per = kBf16 ? 8 : 4;
@@ -575,12 +608,14 @@ __device__ __forceinline__ void hold_units(const DistillArgs& a, const Teacher& 
     } else {
         v[N - 1] = s.kept[c + (N - 1) * kWork];
     }
-    if (a.tail) {
+    if constexpr (kTail != 0) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const int w = (c & ~31) + k * kWork;  // the warp's units
-            const uint32_t lanes = w < s.n ? s.bits[w >> 5] : 0;
-            if (lanes) v[k] = mask_ids<kBf16>(t.id, a.K, lanes, s.u0 + w, v[k]);
+            const uint32_t units = w < s.n ? s.bits[w >> 5] : 0;
+            if (units)
+                v[k] = kTail == kTailMarks ? mask_named<kBf16>(v[k], units, s.marks + s.bits[s.words + (w >> 5)])
+                                           : mask_ids<kBf16>(t.id, a.K, units, s.u0 + w, v[k]);
         }
     }
     st.template add_units<kBf16>(v, units_max<kBf16, N>(v), a.c);
@@ -637,14 +672,17 @@ __device__ __forceinline__ void put_named(const DistillArgs& a, int64_t r, const
     }
 }
 
-template <bool kBf16>
-__global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(const DistillArgs a, int slice, int C) {
+template <bool kBf16, int kTail>
+__global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(const DistillArgs args, int slice, int C) {
     constexpr int per = kBf16 ? 8 : 4;
-    extern __shared__ uint4 room[];                 // [slice], then with the tail [kTeachers][words]
+    DistillArgs a = args;
+    a.tail = kTail != 0;  // (known to the compiler)
+    extern __shared__ uint4 room[];                 // [slice], then with the tail [2][2][words]
     __shared__ Teacher teachers[kTeachers];
     __shared__ float2 stats[2][kMaxCluster * kWorkWarps];  // m, s of each worker warp of the cluster, of two rows
     __shared__ int32_t table[kSlots];
     __shared__ Asked asked;
+    __shared__ uint32_t marks[2][kK / 4], places;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = blockIdx.x % C, words = (slice + 31) / 32;
     const int u0 = min(rank * slice, a.nvec), n = min(slice, a.nvec - u0);
@@ -658,16 +696,6 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(c
     Entries e;  // (ninth warp) of the next row to be put, with its logits; `asked` is of the one after it
     auto put = [&](int i, int at) {
         if (i >= rows) return;
-        uint32_t* b = bits + at * words;
-        if (a.tail) {
-            for (int k = lane; k < words; k += 32) b[k] = 0;
-            __syncwarp();
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) {
-                const unsigned u = (unsigned)(e.id[k] / per - u0);
-                if (k * 32 < a.K && e.id[k] >= 0 && u < (unsigned)n) atomicOr(&b[u >> 5], 1u << (u & 31));
-            }
-        }
         put_entries<kBf16>(a, e, teachers[at]);
     };
     auto fetch = [&](int i) {  // row i's entries, row i + 1's asked for
@@ -675,10 +703,38 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(c
         take_entries(a, asked, e);
         if (i + 1 < rows) ask_entries(a, r0 + (i + 1) * step, asked);
         check_entries<kBf16>(a, r0 + i * step, e, table);
+        // (the workers have looked at row i - 2, whose place this is)
+        if (a.tail) {
+            uint32_t *b = bits + (i & 1) * 2 * words, *place = b + words;
+            for (int k = lane; k < words; k += 32) b[k] = 0;
+            marks[i & 1][lane] = 0;
+            if (lane == 0) places = 0;
+            __syncwarp();
+            unsigned u[kPer];
+            uint32_t old[kPer];
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                u[k] = (unsigned)(e.id[k] / per - u0);
+                if (k * 32 >= a.K || e.id[k] < 0 || u[k] >= (unsigned)n) u[k] = ~0u;
+                old[k] = u[k] != ~0u ? atomicOr(&b[u[k] >> 5], 1u << (u[k] & 31)) : 1u;
+            }
+            if (kTail != kTailMarks) return;
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)  // who was the first of 32 units gives them their places
+                if (old[k] == 0) place[u[k] >> 5] = atomicAdd(&places, __popc(b[u[k] >> 5]));
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (u[k] != ~0u) {
+                    const uint32_t m = place[u[k] >> 5] + __popc(b[u[k] >> 5] & ((1u << (u[k] & 31)) - 1));
+                    atomicOr(&marks[i & 1][m >> 2], 1u << ((m & 3) * 8 + e.id[k] % per));
+                }
+        }
     };
     const int groups = groups_of(n);
     if (works) {
-        const Slice s{room, bits, n, u0};
+        const Slice s{room, nullptr, 0, nullptr, n, u0};
         if (rows > 0) each_group(n, [&](int at, auto N, bool last) { copy_group<decltype(N)::value>(s, at, last, from(0)); });
     } else {
         for (int i = lane; i < kSlots; i += 32) table[i] = -1;
@@ -694,14 +750,14 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(c
     int before = 0;
     for (int i = 0, k = 0; i < rows; ++i, k = next_of(k)) {
         const Teacher& t = teachers[k];
-        const Slice s{room, bits + k * words, n, u0};
+        const Slice s{room, bits + (i & 1) * 2 * words, words, reinterpret_cast<const uint8_t*>(marks[i & 1]), n, u0};
         float2* mine = stats[i & 1];
         if (works) {
             LaneStat<false> st;
             int left = groups;
             each_group(n, [&](int at, auto N, bool last) {
                 copies_wait(--left);
-                hold_units<kBf16, decltype(N)::value>(a, t, s, at, last, st);
+                hold_units<kBf16, kTail, decltype(N)::value>(a, t, s, at, last, st);
             });
             RowStat x = st.row(a.c);
             join_lanes<false>(x, a.c);
@@ -758,20 +814,6 @@ struct EvalArgs {
     float4* part;      // [pieces][2]: m, s of a piece's first and last row
     uint32_t* count;   // by a row's first piece; zero between launches
 };
-
-// Elements of a unit whose bits are set in `marks` become -inf.
-template <bool kBf16>
-__device__ __noinline__ uint4 mask_marked(uint4 v, uint32_t marks) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-#pragma unroll
-    for (int e = 0; e < (kBf16 ? 8 : 4); ++e)
-        if (marks >> e & 1) {
-            if (!kBf16) w[e] = 0xFF800000u;
-            else if (e & 1) w[e >> 1] = (w[e >> 1] & 0x0000FFFFu) | 0xFF800000u;
-            else w[e >> 1] = (w[e >> 1] & 0xFFFF0000u) | 0x0000FF80u;
-        }
-    return v;
-}
 
 // A byte for each unit of a chunk, a bit for each named token in it (a warp's own).
 constexpr int kChunkUnits = 1024;
@@ -1056,15 +1098,15 @@ __global__ void __launch_bounds__(kLongThreads) distill_long_kernel(const Distil
 // ------------------------------------------------------------------ launch
 using RowsKernel = void (*)(DistillArgs, int, int);
 
-size_t rows_bytes(int nvec, int C) {
+size_t rows_bytes(int nvec, int C, bool tail) {
     const size_t slice = (size_t)((nvec + C - 1) / C);
-    return slice * 16 + kTeachers * ((slice + 31) / 32) * 4;
+    return slice * 16 + (tail ? 4 * ((slice + 31) / 32) * sizeof(uint32_t) : 0);
 }
 
 // CTAs an SM with `bytes` of dynamic shared memory each (1 KB of the SM's goes to every CTA).
 int ctas_per_sm(size_t bytes) {
     constexpr size_t kStatic = sizeof(Teacher) * kTeachers + sizeof(float2) * 2 * kMaxCluster * kWorkWarps +
-                               sizeof(int32_t) * kSlots + sizeof(Asked);
+                               sizeof(int32_t) * kSlots + sizeof(Asked) + sizeof(uint32_t) * 2 * (kK / 4);
     const size_t n = (size_t)(228 * 1024) / (bytes + kStatic + 1024);
     return n > kRowBlocks ? kRowBlocks : (int)n;
 }
@@ -1155,18 +1197,22 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
 
     // The cluster size by what a wave of rows takes: a unit's share of an SM's part of the memory's rate (0.72 ns for
     // its read and its write) on the CTAs that share an SM, of which one by itself reaches some 0.4, and 2 us a row.
-    const RowsKernel kernel = bf16 ? distill_rows_kernel<true> : distill_rows_kernel<false>;
-    if (!(ctx->distill_set >> bf16 & 1)) {
+    const int kind = !tail ? 0 : K <= kFewNamed ? kTailFew : kTailMarks, which = 2 * kind + bf16;
+    constexpr RowsKernel kernels[] = {distill_rows_kernel<false, 0>, distill_rows_kernel<true, 0>,
+                                      distill_rows_kernel<false, kTailFew>, distill_rows_kernel<true, kTailFew>,
+                                      distill_rows_kernel<false, kTailMarks>, distill_rows_kernel<true, kTailMarks>};
+    const RowsKernel kernel = kernels[which];
+    if (!(ctx->distill_set >> which & 1)) {
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
         if (e != cudaSuccess) return cuda_fail(e, "distillation kernel's shared memory");
-        ctx->distill_set |= 1u << bf16;
+        ctx->distill_set |= 1u << which;
     }
     int C = 0, clusters = 0;
     double best = 0.;
     for (int c = 1; c <= kMaxCluster; ++c) {
-        const size_t bytes = rows_bytes(a.nvec, c);
+        const size_t bytes = rows_bytes(a.nvec, c, tail);
         if (bytes > (size_t)kSliceBytes) continue;
-        const int per_sm = ctas_per_sm(bytes), fit = clusters_at_once(ctx, kernel, bf16, c, bytes, per_sm);
+        const int per_sm = ctas_per_sm(bytes), fit = clusters_at_once(ctx, kernel, which, c, bytes, per_sm);
         if (fit < 1) continue;
         const int64_t share = (n_rows * c + ctx->num_sms - 1) / ctx->num_sms;  // CTAs an SM really has
         const double together = share < per_sm ? (double)share : (double)per_sm;
@@ -1185,7 +1231,7 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
         else distill_long_kernel<false><<<blocks, kLongThreads, 0, st>>>(a);
         e = cudaGetLastError();
     } else {
-        ClusterLaunch l(C, clusters, rows_bytes(a.nvec, C), st);
+        ClusterLaunch l(C, clusters, rows_bytes(a.nvec, C, tail), st);
         e = cudaLaunchKernelEx(&l.cfg, kernel, a, (a.nvec + C - 1) / C, C);
     }
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
