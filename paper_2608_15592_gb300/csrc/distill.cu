@@ -16,7 +16,7 @@
 // caches (distill_short_kernel); the loss alone is one read (distill_eval_kernel).
 //
 // 2048 rows of 128256 bf16 tokens take 179 us (155 at the copy's rate; a block a row with both passes from memory: 419), 1021
-// of 152064 with the tail 133 (92).  Two exponentials a logit and some 110 instructions for 256 of them are issued at
+// of 152064 with the tail 131 (92).  Two exponentials a logit and some 110 instructions for 256 of them are issued at
 // 2.2 a clock of 4: what is left is their latency where warps wait for the row's barrier.
 #include <type_traits>
 
@@ -870,14 +870,15 @@ __device__ __forceinline__ RowStat eval_units(const DistillArgs& a, const char* 
     return x;
 }
 
-template <bool kBf16>
+template <bool kBf16, bool kTail>
 __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kernel(const EvalArgs a) {
     constexpr int kWarps = kVocabThreads / 32;
     __shared__ Teacher teachers[kWarps];
     __shared__ Asked asked[kWarps];
     __shared__ int32_t tables[kWarps][kSlots];
     __shared__ Marks marks[kWarps];
-    const DistillArgs& d = a.d;
+    DistillArgs d = a.d;
+    d.tail = kTail;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t w = (int64_t)blockIdx.x * kWarps + warp;
     if (w >= a.rows.pieces) return;
@@ -935,8 +936,8 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kern
 
 // ------------------------------------------------------------------ many short rows
 // A warp a row: both passes read it from memory, the second from the caches.  Where a row is a few KB, a cluster's
-// barriers and its ninth warp take longer than the row.  By clusters and so, us: 8192 bf16 rows of 1000 tokens 91 and
-// 32, of 2500 95 and 46, 7880 of 4707 (589 units) 103 and 73, 8192 of 8000 109 and 114; 1000 of 4707 25 and 28.
+// barriers and its ninth warp take longer than the row.  By clusters and so, us: 8192 bf16 rows of 1000 tokens 85 and
+// 28, of 2500 88 and 41, 7880 of 4707 (589 units) 100 and 66, 8192 of 8000 105 and 105; 1000 of 4707 25 and 28.
 constexpr int kShortUnits = 256;    // at most, with a row for every sixth warp
 constexpr int kManyShortUnits = 640;  // at most, with one for every warp
 
@@ -957,8 +958,10 @@ __device__ __forceinline__ void short_grad(const DistillArgs& a, const Factors& 
     }
 }
 
-template <bool kBf16>
-__global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_short_kernel(const DistillArgs a) {
+template <bool kBf16, bool kTail>
+__global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_short_kernel(const DistillArgs args) {
+    DistillArgs a = args;
+    a.tail = kTail;
     constexpr int kWarps = kVocabThreads / 32;
     __shared__ Teacher teachers[kWarps];
     __shared__ Asked asked[kWarps];
@@ -1179,8 +1182,10 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
         v.part = ctx->vocab_part;
         v.count = ctx->vocab_count;
         const unsigned blocks = (unsigned)((v.rows.pieces + kWarps - 1) / kWarps);
-        if (bf16) distill_eval_kernel<true><<<blocks, kVocabThreads, 0, st>>>(v);
-        else distill_eval_kernel<false><<<blocks, kVocabThreads, 0, st>>>(v);
+        if (bf16 && tail) distill_eval_kernel<true, true><<<blocks, kVocabThreads, 0, st>>>(v);
+        else if (bf16) distill_eval_kernel<true, false><<<blocks, kVocabThreads, 0, st>>>(v);
+        else if (tail) distill_eval_kernel<false, true><<<blocks, kVocabThreads, 0, st>>>(v);
+        else distill_eval_kernel<false, false><<<blocks, kVocabThreads, 0, st>>>(v);
         e = cudaGetLastError();
         return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
     }
@@ -1189,8 +1194,10 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
     if (a.nvec <= kManyShortUnits && n_rows * 6 >= at_once && (a.nvec <= kShortUnits || n_rows >= at_once)) {
         const int64_t want = (n_rows + kWarps - 1) / kWarps, most = (int64_t)ctx->num_sms * kVocabBlocks;
         const unsigned blocks = (unsigned)(want < most ? want : most);
-        if (bf16) distill_short_kernel<true><<<blocks, kVocabThreads, 0, st>>>(a);
-        else distill_short_kernel<false><<<blocks, kVocabThreads, 0, st>>>(a);
+        if (bf16 && tail) distill_short_kernel<true, true><<<blocks, kVocabThreads, 0, st>>>(a);
+        else if (bf16) distill_short_kernel<true, false><<<blocks, kVocabThreads, 0, st>>>(a);
+        else if (tail) distill_short_kernel<false, true><<<blocks, kVocabThreads, 0, st>>>(a);
+        else distill_short_kernel<false, false><<<blocks, kVocabThreads, 0, st>>>(a);
         e = cudaGetLastError();
         return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "distillation launch");
     }
