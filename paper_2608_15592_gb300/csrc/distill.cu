@@ -361,9 +361,13 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const Teacher& t
         const float q = t.q[j], z = t.z[j];
         if (t.id[j] >= 0 && q != 0.f) {
             any = true;
-            plain += q * t.lq[j] + q * (f.m - z) / a.T;
+            // (halves: the distance of two finite logits may overflow)
+            const float term = q * t.lq[j] + q * (0.5f * f.m - 0.5f * z) / a.T * 2.f;
+            plain += term;
+            // q may be next to nothing where (z - m) / T is beyond a float's end, or so near it that a product of two
+            // floats is infinity and its error -infinity: such a term in one float
             const Two y = times(two_sum(z, -f.m), a.inv_T);
-            sum = plus(sum, times(Two{q, 0.f}, plus(Two{t.lq[j], 0.f}, Two{-y.hi, -y.lo})));
+            sum = plus(sum, fabsf(y.hi) < 1e30f ? times(Two{q, 0.f}, plus(Two{t.lq[j], 0.f}, Two{-y.hi, -y.lo})) : Two{term, 0.f});
         }
     }
     any = __any_sync(0xffffffffu, any);
@@ -376,7 +380,8 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const Teacher& t
     // infinite, NaN, or near a float's end (tokens at the type's lowest value): in one float
     if (!(fabsf(plain) < 1e4f) || isnan(f.s) || (f.rest != 0.f && !(f.pivot - f.m > -1e30f))) {
         plain += t.Q * logf(f.s);
-        if (f.rest != 0.f) plain += f.rest * (logf(f.rest) - logf(st.s) + logf(f.s)) + f.rest * (f.m - f.pivot) / a.T;
+        if (f.rest != 0.f)
+            plain += f.rest * (logf(f.rest) - logf(st.s) + logf(f.s)) + f.rest * (0.5f * f.m - 0.5f * f.pivot) / a.T * 2.f;
         return plain;
     }
     // ln of the sum, of what the teacher leaves to the others, and of what the student does: 1 - sum p_id while that is at
