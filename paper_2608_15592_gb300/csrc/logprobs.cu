@@ -367,6 +367,9 @@ __device__ __forceinline__ void ask_logit(const LpArgs& a, const char* row, Targ
         x.z = kBf16 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[x.t] : reinterpret_cast<const uint32_t*>(row)[x.t];
 }
 
+// (z - m) / T by halves: the distance of two finite logits may overflow where its quotient does not.
+__device__ __forceinline__ float below(float z, float m, float T) { return (0.5f * z - 0.5f * m) / T * 2.f; }
+
 // What a row's statistics and list say, written by a warp.
 template <bool kBf16, int R>
 __device__ __forceinline__ void write_row(const LpArgs& a, int64_t r, const Target& x, const RowStat& st,
@@ -379,7 +382,7 @@ __device__ __forceinline__ void write_row(const LpArgs& a, int64_t r, const Targ
         if (a.entropy) a.entropy[r] = empty ? 0.f : ls - kLn2 * (st.t / st.s);
         if (a.norm) a.norm[r] = make_float2(st.m, st.s);
         if (a.logprob) {
-            float lp = x.t < 0 ? 0.f : (__uint_as_float(kBf16 ? x.z << 16 : x.z) - m) / a.T - ls;
+            float lp = x.t < 0 ? 0.f : below(__uint_as_float(kBf16 ? x.z << 16 : x.z), m, a.T) - ls;
             if (x.t >= a.rows.V) {
                 report(a.status, ESTP_ERR_INVALID_ARG);
                 lp = NAN;
@@ -395,7 +398,7 @@ __device__ __forceinline__ void write_row(const LpArgs& a, int64_t r, const Targ
                 const uint64_t k = list[i];
                 if (k == 0 && !none) continue;
                 a.top_ids[r * a.top_k + i] = none ? -1 : key_token(k);
-                if (a.top_logprobs) a.top_logprobs[r * a.top_k + i] = none ? NAN : (key_logit(k) - m) / a.T - ls;
+                if (a.top_logprobs) a.top_logprobs[r * a.top_k + i] = none ? NAN : below(key_logit(k), m, a.T) - ls;
             }
         if (list[a.top_k - 1] == 0 && !none) {
             // short of tokens: the masked ones of lowest index follow, which are among the first top_k
