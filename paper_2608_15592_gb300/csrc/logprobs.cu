@@ -754,6 +754,7 @@ __global__ void __launch_bounds__(kVocabThreads, kGradBlocks) logprobs_grad_kern
         const bool empty = norm.y == 0.f;
         // named tokens and the sum of their gradients
         float pull = 0.f;
+        bool asked = false;  // something of the row at all
         int n_named = 0;
         __syncwarp();
         if (a.g_top) {
@@ -769,7 +770,9 @@ __global__ void __launch_bounds__(kVocabThreads, kGradBlocks) logprobs_grad_kern
                 q.id[i] = id;
                 q.g[i] = g * inv_T;
                 pull += g;
+                asked |= g != 0.f;
             }
+            asked = __any_sync(0xffffffffu, asked);
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) pull += __shfl_xor_sync(0xffffffffu, pull, off);
         }
@@ -787,11 +790,14 @@ __global__ void __launch_bounds__(kVocabThreads, kGradBlocks) logprobs_grad_kern
             }
             ++n_named;
             pull += g;
+            asked |= g != 0.f;
         }
         __syncwarp();
         const float gH = a.g_entropy && !empty ? a.g_entropy[r] : 0.f, gl = a.g_lse ? a.g_lse[r] : 0.f;
-        // nothing for the row as a whole: zeros, whatever its logits hold
-        const bool flat = empty || (gl - pull == 0.f && gH == 0.f);
+        // nothing for the row as a whole: zeros but for named tokens, and where nothing is asked whatever its logits hold
+        // (in a row of NaN what cancels is NaN)
+        asked |= gl != 0.f;
+        const bool flat = empty || (gl - pull == 0.f && gH == 0.f && !(asked && isnan(norm.y)));
         RowGrad g{pivot(norm.x), 0.f, 0.f, 0.f, false};
         g.M = g.m * a.c;
         g.framed = near_frame(g.M);
