@@ -46,6 +46,18 @@ estp_status set_device(estp_ctx* ctx) {
     return e == cudaSuccess ? ESTP_OK : cuda_fail(e, "cudaSetDevice");
 }
 
+// A memset of the legacy default stream is ordered before no call on a non-blocking stream, and waits behind whatever
+// that stream holds: so a stream of its own.
+cudaError_t zero_now(void* p, size_t bytes) {
+    cudaStream_t s = nullptr;
+    cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+    if (e != cudaSuccess) return e;
+    e = cudaMemsetAsync(p, 0, bytes, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    const cudaError_t d = cudaStreamDestroy(s);
+    return e == cudaSuccess ? d : e;
+}
+
 // Grows the workspace to at least `bytes`.  cudaFree waits for the device, so work
 // already enqueued on the old buffer finishes before it is released.
 estp_status ws_reserve(estp_ctx* ctx, size_t bytes) {
@@ -118,7 +130,7 @@ estp_status estp_create(estp_ctx** out, int device) {
     if (e != cudaSuccess) { delete ctx; return cuda_fail(e, "cudaDeviceGetAttribute"); }
     // the status word and, on the next 128-byte line, the cache kernels' arrival counter and timeout mark
     e = cudaMalloc(&ctx->status, 256);
-    if (e == cudaSuccess) e = cudaMemset(ctx->status, 0, 256);
+    if (e == cudaSuccess) e = zero_now(ctx->status, 256);
     if (e != cudaSuccess) { cudaFree(ctx->status); delete ctx; return cuda_fail(e, "status word"); }
     // the log probability kernels' parts and lists: a bound of what any call needs (7.7 MB), so that no
     // call allocates and a captured one keeps its buffers whatever comes after it
@@ -126,7 +138,7 @@ estp_status estp_create(estp_ctx** out, int device) {
     e = cudaMalloc(&ctx->vocab_part, slots * (sizeof(float4) + kMaxAlternatives * sizeof(uint64_t) + sizeof(uint32_t)));
     ctx->vocab_lists = reinterpret_cast<uint64_t*>(ctx->vocab_part + slots);
     ctx->vocab_count = reinterpret_cast<uint32_t*>(ctx->vocab_lists + slots * kMaxAlternatives);
-    if (e == cudaSuccess) e = cudaMemset(ctx->vocab_count, 0, slots * sizeof(uint32_t));
+    if (e == cudaSuccess) e = zero_now(ctx->vocab_count, slots * sizeof(uint32_t));
     if (e != cudaSuccess) {
         cudaFree(ctx->vocab_part);
         cudaFree(ctx->status);

@@ -58,6 +58,7 @@ estp_status fail(estp_status st, const char* fmt, ...);
 estp_status cuda_fail(cudaError_t e, const char* what);
 estp_status ws_reserve(estp_ctx* ctx, size_t bytes);
 estp_status set_device(estp_ctx* ctx);
+cudaError_t zero_now(void* p, size_t bytes);  // zeros that any stream's work finds once this has returned
 
 // Raises a kernel's dynamic shared memory limit, once a context (`bit` is the kernel's own).
 template <class Kernel>
