@@ -413,7 +413,7 @@ estp_status launch_pool(estp_ctx* ctx, const void* hidden, estp_dtype dtype, int
         ctx->pool_done = nullptr;
         ctx->pool_done_cap = 0;
         e = cudaMalloc(&ctx->pool_done, sizeof(uint32_t) * (size_t)B);
-        if (e == cudaSuccess) e = cudaMemset(ctx->pool_done, 0, sizeof(uint32_t) * (size_t)B);
+        if (e == cudaSuccess) e = zero_now(ctx->pool_done, sizeof(uint32_t) * (size_t)B);
         if (e != cudaSuccess) {
             cudaGetLastError();
             return fail(ESTP_ERR_WORKSPACE, "pool counters: %s", cudaGetErrorString(e));
