@@ -906,15 +906,11 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kern
             const int64_t slot = w * 2 + (u == start ? 0 : 1);
             const int64_t lo = piece_of(a.rows, u0), hi = piece_of(a.rows, u0 + a.rows.nvec - 1);
             const int n = (int)(hi - lo + 1);
-            uint32_t last = 0;
-            if (lane == 0 && in_bounds(slot < 2 * a.rows.pieces, d.status)) {
-                a.part[slot] = make_float4(st.m, st.s, 0.f, 0.f);
-                __threadfence();
-                last = atomicAdd(&a.count[lo], 1u) == (uint32_t)n - 1 ? 1u : 0u;
-                if (last) a.count[lo] = 0;
-                __threadfence();
+            write = false;
+            if (in_bounds(lo >= 0 && slot < 2 * a.rows.pieces, d.status)) {
+                if (lane == 0) a.part[slot] = make_float4(st.m, st.s, 0.f, 0.f);
+                write = arrive(a.count + lo, n);
             }
-            write = __shfl_sync(0xffffffffu, last, 0) != 0;
             if (write) {
                 st = no_stat();
                 for (int i = lane; i < n; i += 32) {

@@ -431,20 +431,6 @@ __device__ __forceinline__ void put_part(const LpArgs& a, int64_t slot, const Ro
         for (int i = lane; i < 32 * R; i += 32) a.lists[slot * (32 * R) + i] = list[i];
 }
 
-// A part has been written (by the whole warp): whether it is the last of the row's n.  The counter is zero
-// between launches.
-__device__ __forceinline__ bool arrive(const LpArgs& a, int64_t counter, int n) {
-    uint32_t last = 0;
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0 && in_bounds(counter >= 0 && counter < a.slots, a.status)) {
-        __threadfence();
-        last = atomicAdd(&a.count[counter], 1u) == (uint32_t)n - 1 ? 1u : 0u;
-        if (last) a.count[counter] = 0;
-        __threadfence();
-    }
-    return __shfl_sync(0xffffffffu, last, 0) != 0;
-}
-
 // The statistics of a row's n parts, part 0 in `slot0` and the others from `slot` on, `step` apart: joined in one
 // order whichever warp does it.
 __device__ __forceinline__ RowStat join_parts(const LpArgs& a, int64_t slot0, int64_t slot, int step, int n) {
@@ -538,7 +524,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(c
             const int64_t lo = piece_of(a.rows, u0), hi = piece_of(a.rows, u0 + a.rows.nvec - 1);
             const int64_t slot0 = lo * 2 + (piece_start(a.rows, lo) < u0 ? 1 : 0);
             const int n = (int)(hi - lo + 1);
-            write = arrive(a, lo, n);
+            write = in_bounds(lo >= 0 && lo < a.slots, a.status) && arrive(a.count + lo, n);
             if (write) {
                 st = join_parts(a, slot0, lo * 2 + 2, 2, n);
                 if constexpr (R > 0) merge_parts<R>(a, slot0, lo * 2 + 2, 2, n, 0, 1, q->list);
@@ -582,7 +568,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_few_kern
         bool l = false;
         if (a.blocks > 1) {
             put_part<R>(a, blockIdx.x, st, R ? q->list : nullptr);
-            l = arrive(a, r, a.blocks);
+            l = in_bounds(r < a.slots, a.status) && arrive(a.count + r, a.blocks);
         } else {
             write_row<kBf16, R>(a, r, x, st, R ? q->list : nullptr);
         }

@@ -282,6 +282,23 @@ struct LaneStat {
     }
 };
 
+// A part of a row has been written (by the whole warp): whether it is the last of the row's n, by a counter that is zero
+// between launches.  The shuffle that tells the lanes orders no memory: what lets them read the other warps' parts is the
+// barrier behind it, after lane 0's fence.
+__device__ __forceinline__ bool arrive(uint32_t* count, int n) {
+    uint32_t last = 0;
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) {
+        __threadfence();
+        last = atomicAdd(count, 1u) == (uint32_t)n - 1 ? 1u : 0u;
+        if (last) *count = 0;
+        __threadfence();
+    }
+    last = __shfl_sync(0xffffffffu, last, 0);
+    __syncwarp();
+    return last != 0;
+}
+
 // A unit whose elements from `valid` on are -inf: they count nowhere.
 template <bool kBf16>
 __device__ __forceinline__ void mask_unit(uint4& v, int valid) {
