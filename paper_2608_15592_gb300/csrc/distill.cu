@@ -20,6 +20,7 @@
 // 2.2 a clock of 4: what is left is their latency where warps wait for the row's barrier.
 #include <type_traits>
 
+#include "split_rules.cuh"
 #include "vocab.cuh"
 
 namespace estp {
@@ -1107,12 +1108,20 @@ size_t rows_bytes(int nvec, int C, bool tail) {
     return slice * 16 + (tail ? 4 * ((slice + 31) / 32) * sizeof(uint32_t) : 0);
 }
 
-// CTAs an SM with `bytes` of dynamic shared memory each (1 KB of the SM's goes to every CTA).
-int ctas_per_sm(size_t bytes) {
-    constexpr size_t kStatic = sizeof(Teacher) * kTeachers + sizeof(float2) * 2 * kMaxCluster * kWorkWarps +
-                               sizeof(int32_t) * kSlots + sizeof(Asked) + sizeof(uint32_t) * 2 * (kK / 4);
-    const size_t n = (size_t)(228 * 1024) / (bytes + kStatic + 1024);
-    return n > kRowBlocks ? kRowBlocks : (int)n;
+// Raises a kernel's shared memory limit and finds what CTAs that share an SM leave each other; once a context.
+cudaError_t set_rows(estp_ctx* ctx, RowsKernel kernel, int which) {
+    if (ctx->distill_set >> which & 1) return cudaSuccess;
+    cudaFuncAttributes has;
+    int sm = 0, system = 0;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&has, kernel);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sm, cudaDevAttrMaxSharedMemoryPerMultiprocessor, ctx->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&system, cudaDevAttrReservedSharedMemoryPerBlock, ctx->device);
+    if (e != cudaSuccess) return e;
+    for (int n = 1; n <= kRowBlocks; ++n)
+        ctx->distill_room[which][n - 1] = cta_room(sm, (int)has.sharedSizeBytes + system, n, kSliceBytes);
+    ctx->distill_set |= 1u << which;
+    return cudaSuccess;
 }
 
 // Launch of `clusters` clusters of C CTAs.
@@ -1132,19 +1141,19 @@ struct ClusterLaunch {
     }
 };
 
-// Clusters of C that the GPU holds at once, asked once for each type, C and number of CTAs an SM.
-int clusters_at_once(estp_ctx* ctx, RowsKernel kernel, int which, int C, size_t bytes, int per_sm) {
+// Clusters of C that the GPU holds at once, asked once for each kernel, C and number of CTAs an SM: for the most shared
+// memory of so many CTAs, so that the answer does not depend on the call that asked.
+cudaError_t clusters_at_once(estp_ctx* ctx, RowsKernel kernel, int which, int C, int per_sm, int* fit) {
     int& known = ctx->distill_clusters[which][per_sm - 1][C - 1];
     if (known == 0) {
-        ClusterLaunch l(C, ctx->num_sms, bytes, nullptr);
+        ClusterLaunch l(C, ctx->num_sms, (size_t)ctx->distill_room[which][per_sm - 1], nullptr);
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg) != cudaSuccess) {
-            cudaGetLastError();
-            n = 0;
-        }
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg);
+        if (e != cudaSuccess) return e;
         known = n > 0 ? n : -1;  // -1: no such cluster here
     }
-    return known;
+    *fit = known;
+    return cudaSuccess;
 }
 
 }  // namespace
@@ -1210,17 +1219,16 @@ estp_status launch_distill_loss(estp_ctx* ctx, const void* logits, estp_dtype dt
                                       distill_rows_kernel<false, kTailFew>, distill_rows_kernel<true, kTailFew>,
                                       distill_rows_kernel<false, kTailMarks>, distill_rows_kernel<true, kTailMarks>};
     const RowsKernel kernel = kernels[which];
-    if (!(ctx->distill_set >> which & 1)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
-        if (e != cudaSuccess) return cuda_fail(e, "distillation kernel's shared memory");
-        ctx->distill_set |= 1u << which;
-    }
+    e = set_rows(ctx, kernel, which);
+    if (e != cudaSuccess) return cuda_fail(e, "distillation kernel's shared memory");
     int C = 0, clusters = 0;
     double best = 0.;
     for (int c = 1; c <= kMaxCluster; ++c) {
-        const size_t bytes = rows_bytes(a.nvec, c, tail);
-        if (bytes > (size_t)kSliceBytes) continue;
-        const int per_sm = ctas_per_sm(bytes), fit = clusters_at_once(ctx, kernel, which, c, bytes, per_sm);
+        const int per_sm = ctas_of((int64_t)rows_bytes(a.nvec, c, tail), ctx->distill_room[which], kRowBlocks);
+        if (per_sm < 1) continue;
+        int fit = 0;
+        e = clusters_at_once(ctx, kernel, which, c, per_sm, &fit);
+        if (e != cudaSuccess) return cuda_fail(e, "distillation clusters");
         if (fit < 1) continue;
         const int64_t share = (n_rows * c + ctx->num_sms - 1) / ctx->num_sms;  // CTAs an SM really has
         const double together = share < per_sm ? (double)share : (double)per_sm;

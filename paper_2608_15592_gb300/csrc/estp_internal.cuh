@@ -34,8 +34,9 @@ struct estp_ctx {
     float4* vocab_part = nullptr;    // parts of rows cut between warps, two a piece (log probabilities)
     uint64_t* vocab_lists = nullptr; // and their lists of alternatives; a fixed size, from estp_create on
     uint32_t* vocab_count = nullptr; // arrival counters of rows (zero between launches)
+    int distill_room[6][3] = {};         // by kernel: dynamic shared memory of each of 1 to 3 CTAs an SM
     int distill_clusters[6][3][8] = {};  // clusters the GPU holds at once, by kernel, CTAs an SM and cluster size (0: not asked)
-    uint32_t distill_set = 0;            // distillation kernels whose shared memory limit is set, a bit each
+    uint32_t distill_set = 0;            // distillation kernels whose shared memory limit and room are set, a bit each
     uint32_t smem_set = 0;      // cache kernels whose shared memory limit is set on the device, a bit each
     // limit of the attention kernels' abortable waits (estp_set_wait_limit)
     long long wait_cycles = kWaitCycles;

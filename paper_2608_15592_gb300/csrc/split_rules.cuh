@@ -192,4 +192,19 @@ inline int wide_ranks(int64_t tiles, int64_t n_k, int num_sms) {
     return S;
 }
 
+// --------------------------------------------------------------- rows kept by clusters (distillation)
+// The most dynamic shared memory that each of n CTAs of an SM can have beside its `fixed` bytes (its static ones and what
+// the system takes of each CTA), which are handed out in units of 128; `most`: a CTA's limit.
+inline int cta_room(int sm_bytes, int fixed, int n, int most) {
+    const int room = sm_bytes / n / 128 * 128 - fixed;
+    return room < most ? room : most;
+}
+
+// CTAs an SM of that many bytes, given the room of 1 .. `blocks`; 0: not even one.
+inline int ctas_of(int64_t bytes, const int* room, int blocks) {
+    int n = blocks;
+    while (n > 0 && bytes > room[n - 1]) --n;
+    return n;
+}
+
 }  // namespace estp
