@@ -66,6 +66,15 @@ struct DistillArgs {
     int* status;
 };
 
+// Units [u0, u1) of row r are the logits' and the gradient's; with `whole` none of them is the row's partial last one.
+__device__ __forceinline__ bool units_there(const DistillArgs& a, int64_t r, int u0, int u1, int per, bool whole) {
+    return in_bounds(r >= 0 && r < a.n_rows && u0 >= 0 && u0 < u1 && (whole ? u1 <= a.V / per : u1 <= a.nvec), a.status);
+}
+
+__device__ __forceinline__ void put_loss(const DistillArgs& a, int64_t r, float loss) {
+    if ((threadIdx.x & 31) == 0 && in_bounds(r >= 0 && r < a.n_rows, a.status)) a.loss[r] = loss;
+}
+
 // The teacher's side of a row, which its logits have no part in but for those of the named tokens.
 struct Teacher {
     int32_t id[kK];            // -1: none
@@ -205,7 +214,7 @@ __device__ __forceinline__ void check_entries(const DistillArgs& a, int64_t r, E
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         e.z[i] = kBf16 ? 0xFF80u : 0xFF800000u;
-        if (i * 32 < a.K && e.id[i] >= 0)
+        if (i * 32 < a.K && e.id[i] >= 0 && in_bounds(r < a.n_rows && e.id[i] < a.V, a.status))
             e.z[i] = kBf16 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[e.id[i]] : reinterpret_cast<const uint32_t*>(row)[e.id[i]];
         if (e.id[i] < 0) e.x[i] = -INFINITY;
     }
@@ -588,13 +597,18 @@ __device__ __forceinline__ void each_group(int n, F f) {
 }
 __device__ __forceinline__ int groups_of(int n) { return ((n + kWork - 1) / kWork + kGroup - 1) / kGroup; }
 
+// Copies N of the worker's units of row r, whose slice is at `from`.
 template <int N>
-__device__ __forceinline__ void copy_group(const Slice& s, int at, bool last, const char* from) {
+__device__ __forceinline__ void copy_group(const DistillArgs& a, int64_t r, const Slice& s, int at, bool last, const char* from) {
     const int c = at + (int)threadIdx.x;
     const char* q = from + (int64_t)c * 16;
 #pragma unroll
     for (int k = 0; k < N; ++k)
-        if (k < N - 1 || !last || c + k * kWork < s.n) copy_unit(&s.kept[c + k * kWork], q + k * (kWork * 16));
+        if (k < N - 1 || !last || c + k * kWork < s.n) {
+            const int u = c + k * kWork;
+            if (units_there(a, r, s.u0 + u, s.u0 + u + 1, 1, false) && in_bounds(u < s.n, a.status))
+                copy_unit(&s.kept[u], q + k * (kWork * 16));
+        }
     copies_commit();
 }
 
@@ -627,10 +641,10 @@ __device__ __forceinline__ void hold_units(const DistillArgs& a, const Teacher& 
     st.template add_units<kBf16>(v, units_max<kBf16, N>(v), a.c);
 }
 
-// The gradient of N of them, and copies of the next row (`next`, if any) into their place.
+// The gradient of N of them, of row r, and copies of row r + step (`next`, if any) into their place.
 template <bool kBf16, bool kFramed, int N>
-__device__ __forceinline__ void kept_grad(const DistillArgs& a, const Factors& f, const Slice& s, int at, bool last, char* out,
-                                          const char* next) {
+__device__ __forceinline__ void kept_grad(const DistillArgs& a, int64_t r, int64_t step, const Factors& f, const Slice& s, int at,
+                                          bool last, char* out, const char* next) {
     constexpr int per = kBf16 ? 8 : 4;
     const int c = at + (int)threadIdx.x;
     char* p = out + (int64_t)c * 16;
@@ -642,10 +656,15 @@ __device__ __forceinline__ void kept_grad(const DistillArgs& a, const Factors& f
     for (int k = 0; k < N; ++k) {
         float x[8];
         other_grad<kBf16, kFramed>(f, v[k], a.c, x);
-        if (k < N - 1 || !last) store_whole<kBf16>(p + k * (kWork * 16), x);
-        else if (c + k * kWork < s.n) store_unit<kBf16>(out, c + k * kWork, a.V - s.u0 * per, x);
+        const int u = c + k * kWork;
+        if (k < N - 1 || !last) {
+            if (units_there(a, r, s.u0 + u, s.u0 + u + 1, per, true) && in_bounds(u < s.n, a.status))
+                store_whole<kBf16>(p + k * (kWork * 16), x);
+        } else if (u < s.n && units_there(a, r, s.u0 + u, s.u0 + u + 1, per, false)) {
+            store_unit<kBf16>(out, u, a.V - s.u0 * per, x);
+        }
     }
-    if (next) copy_group<N>(s, at, last, next);  // (every value has been used)
+    if (next) copy_group<N>(a, r + step, s, at, last, next);  // (every value has been used)
 }
 
 // The named tokens of a slice, over what an unnamed one would have there (a warp).
@@ -741,7 +760,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(c
     const int groups = groups_of(n);
     if (works) {
         const Slice s{room, nullptr, 0, nullptr, n, u0};
-        if (rows > 0) each_group(n, [&](int at, auto N, bool last) { copy_group<decltype(N)::value>(s, at, last, from(0)); });
+        if (rows > 0) each_group(n, [&](int at, auto N, bool last) { copy_group<decltype(N)::value>(a, r0, s, at, last, from(0)); });
     } else {
         for (int i = lane; i < kSlots; i += 32) table[i] = -1;
         __syncwarp();
@@ -767,7 +786,8 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(c
             });
             RowStat x = st.row(a.c);
             join_lanes<false>(x, a.c);
-            if (lane < C) store_remote(&mine[rank * kWorkWarps + warp], lane, x.m, x.s);
+            if (lane < C && in_bounds(C <= kMaxCluster && rank * kWorkWarps + warp < C * kWorkWarps, a.status))
+                store_remote(&mine[rank * kWorkWarps + warp], lane, x.m, x.s);
         } else {
             put(i + 1, next_of(k));
         }
@@ -784,24 +804,23 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(c
             // (the workers' gradient of the row before is behind the barrier)
             if (i > 0) put_named<kBf16>(a, r0 + (i - 1) * step, teachers[before], f, u0, n);
             f = row_factors(a, t, st);
-            if (rank == 0) {
-                const float loss = row_loss(a, t, st, f);
-                if (lane == 0) a.loss[r0 + i * step] = loss;
-            }
+            if (rank == 0) put_loss(a, r0 + i * step, row_loss(a, t, st, f));
             before = k;
             fetch(i + 2);
         } else {
             f = row_factors(a, t, st);
-            char* out = a.out + (r0 + i * step) * a.out_bytes + (int64_t)u0 * 16;
+            const int64_t r = r0 + i * step;
+            char* out = a.out + r * a.out_bytes + (int64_t)u0 * 16;
             const char* next = i + 1 < rows ? from(i + 1) : nullptr;
             if (f.zero) {
                 const float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                for (int c = tid; c < n; c += kWork) store_unit<kBf16>(out, c, a.V - u0 * per, x);
-                if (next) each_group(n, [&](int at, auto N, bool last) { copy_group<decltype(N)::value>(s, at, last, next); });
+                for (int c = tid; c < n; c += kWork)
+                    if (units_there(a, r, u0 + c, u0 + c + 1, per, false)) store_unit<kBf16>(out, c, a.V - u0 * per, x);
+                if (next) each_group(n, [&](int at, auto N, bool last) { copy_group<decltype(N)::value>(a, r + step, s, at, last, next); });
             } else if (f.framed) {
-                each_group(n, [&](int at, auto N, bool last) { kept_grad<kBf16, true, decltype(N)::value>(a, f, s, at, last, out, next); });
+                each_group(n, [&](int at, auto N, bool last) { kept_grad<kBf16, true, decltype(N)::value>(a, r, step, f, s, at, last, out, next); });
             } else {
-                each_group(n, [&](int at, auto N, bool last) { kept_grad<kBf16, false, decltype(N)::value>(a, f, s, at, last, out, next); });
+                each_group(n, [&](int at, auto N, bool last) { kept_grad<kBf16, false, decltype(N)::value>(a, r, step, f, s, at, last, out, next); });
             }
         }
         __syncwarp();
@@ -895,6 +914,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kern
         const int64_t r = quotient(u, a.rows.nvec), u0 = r * a.rows.nvec;
         const int c0 = (int)(u - u0), c1 = (int)(min(end, u0 + a.rows.nvec) - u0);
         const char* row = d.base + r * d.ld_bytes;
+        if (!units_there(d, r, c0, c1, 1, false)) return;
         Entries e;
         ask_entries(d, r, asked[warp]);
         if (d.tail) {
@@ -915,7 +935,9 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kern
             if (write) {
                 st = no_stat();
                 for (int i = lane; i < n; i += 32) {
-                    const float4 x = __ldcg(&a.part[i ? (lo + i) * 2 : lo * 2 + (piece_start(a.rows, lo) < u0 ? 1 : 0)]);
+                    const int64_t at = i ? (lo + i) * 2 : lo * 2 + (piece_start(a.rows, lo) < u0 ? 1 : 0);
+                    if (!in_bounds(at < 2 * a.rows.pieces, d.status)) break;
+                    const float4 x = __ldcg(&a.part[at]);
                     join(st, RowStat{x.x, x.y, 0.f}, d.c);
                 }
                 __syncwarp();
@@ -927,8 +949,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kern
             take_entries(d, asked[warp], e);
             check_entries<kBf16>(d, r, e, tables[warp]);
             put_entries<kBf16>(d, e, t);
-            const float loss = row_loss(d, t, st, row_factors(d, t, st));
-            if (lane == 0) d.loss[r] = loss;
+            put_loss(d, r, row_loss(d, t, st, row_factors(d, t, st)));
         }
         copies_done();
         __syncwarp();
@@ -944,7 +965,7 @@ constexpr int kShortUnits = 256;    // at most, with a row for every sixth warp
 constexpr int kManyShortUnits = 640;  // at most, with one for every warp
 
 template <bool kBf16, bool kFramed>
-__device__ __forceinline__ void short_grad(const DistillArgs& a, const Factors& f, const char* row, char* out) {
+__device__ __forceinline__ void short_grad(const DistillArgs& a, int64_t r, const Factors& f, const char* row, char* out) {
     constexpr int N = 4;
     const int lane = threadIdx.x & 31;
     for (int b = lane; b < a.nvec; b += 32 * N) {
@@ -955,7 +976,7 @@ __device__ __forceinline__ void short_grad(const DistillArgs& a, const Factors& 
         for (int k = 0; k < N; ++k) {
             float x[8];
             other_grad<kBf16, kFramed>(f, v[k], a.c, x);
-            if (b + 32 * k < a.nvec) store_unit<kBf16>(out, b + 32 * k, a.V, x);
+            if (b + 32 * k < a.nvec && units_there(a, r, b + 32 * k, b + 32 * k + 1, 1, false)) store_unit<kBf16>(out, b + 32 * k, a.V, x);
         }
     }
 }
@@ -978,6 +999,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_short_ker
     ask_entries(a, r, asked[warp]);
     for (; r < a.n_rows; r += step) {
         const char* row = a.base + r * a.ld_bytes;
+        if (!units_there(a, r, 0, a.nvec, 1, false)) return;
         Entries e;
         take_entries(a, asked[warp], e);
         check_entries<kBf16>(a, r, e, tables[warp]);
@@ -987,16 +1009,15 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_short_ker
         if (r + step < a.n_rows) fetch_units(row + step * a.ld_bytes, 0, a.nvec, a.nvec);
         put_entries<kBf16>(a, e, t);
         const Factors f = row_factors(a, t, st);
-        const float loss = row_loss(a, t, st, f);
-        if (lane == 0) a.loss[r] = loss;
+        put_loss(a, r, row_loss(a, t, st, f));
         char* out = a.out + r * a.out_bytes;
         if (f.zero) {
             const float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             for (int c = lane; c < a.nvec; c += 32) store_unit<kBf16>(out, c, a.V, x);
         } else if (f.framed) {
-            short_grad<kBf16, true>(a, f, row, out);
+            short_grad<kBf16, true>(a, r, f, row, out);
         } else {
-            short_grad<kBf16, false>(a, f, row, out);
+            short_grad<kBf16, false>(a, r, f, row, out);
         }
         __syncwarp();  // the named tokens go over these
         put_named<kBf16>(a, r, t, f, 0, a.nvec);
@@ -1048,8 +1069,9 @@ __global__ void __launch_bounds__(kLongThreads) distill_long_kernel(const Distil
             mark(span, true);
             for (int b = span + warp * kStep; b < stop; b += kLongWarps * kStep) {
                 uint4 v[kVocabUnroll];
+                const bool there = units_there(a, r, b, stop, per, false);
 #pragma unroll
-                for (int k = 0; k < kVocabUnroll; ++k) v[k] = load_unit<kBf16>(row, b + 32 * k + lane, stop, a.V);
+                for (int k = 0; k < kVocabUnroll; ++k) v[k] = load_unit<kBf16>(row, b + 32 * k + lane, there ? stop : b, a.V);
                 if (a.tail) {
 #pragma unroll
                     for (int k = 0; k < kVocabUnroll; ++k) {
@@ -1070,10 +1092,7 @@ __global__ void __launch_bounds__(kLongThreads) distill_long_kernel(const Distil
         RowStat all = lane < kLongWarps ? part[lane] : no_stat();
         join_lanes(all, a.c);
         const Factors f = row_factors(a, t, all);
-        if (warp == 0) {
-            const float loss = row_loss(a, t, all, f);
-            if (lane == 0) a.loss[r] = loss;
-        }
+        if (warp == 0) put_loss(a, r, row_loss(a, t, all, f));
         char* out = a.out + r * a.out_bytes;
         for (int span = 0; span < a.nvec; span += kSpanUnits) {
             const int stop = min(a.nvec, span + kSpanUnits);
@@ -1092,7 +1111,7 @@ __global__ void __launch_bounds__(kLongThreads) distill_long_kernel(const Distil
                         });
                     }
                 }
-                if (c + lane < stop) store_unit<kBf16>(out, c + lane, a.V, x);
+                if (c + lane < stop && units_there(a, r, c + lane, c + lane + 1, per, false)) store_unit<kBf16>(out, c + lane, a.V, x);
             }
             __syncthreads();
             mark(span, false);

@@ -436,7 +436,9 @@ __device__ __forceinline__ void put_part(const LpArgs& a, int64_t slot, const Ro
 __device__ __forceinline__ RowStat join_parts(const LpArgs& a, int64_t slot0, int64_t slot, int step, int n) {
     RowStat st = no_stat();
     for (int i = threadIdx.x & 31; i < n; i += 32) {
-        const float4 x = __ldcg(&a.part[i ? slot + (int64_t)(i - 1) * step : slot0]);
+        const int64_t at = i ? slot + (int64_t)(i - 1) * step : slot0;
+        if (!in_bounds(at >= 0 && at < a.slots, a.status)) break;
+        const float4 x = __ldcg(&a.part[at]);
         join(st, RowStat{x.x, x.y, x.z}, a.c);
     }
     __syncwarp();
@@ -457,7 +459,7 @@ __device__ __forceinline__ void merge_parts(const LpArgs& a, int64_t slot0, int6
         uint64_t z[R];
         const int64_t at = (i ? slot + (int64_t)(i - 1) * step : slot0) * (32 * R);
 #pragma unroll
-        for (int k = 0; k < R; ++k) z[k] = i < n ? __ldcg(&a.lists[at + k * 32 + lane]) : 0;
+        for (int k = 0; k < R; ++k) z[k] = i < n && in_bounds(at >= 0 && at < a.slots * (32 * R), a.status) ? __ldcg(&a.lists[at + k * 32 + lane]) : 0;
         if (i > i0) merge_keys<R>(x, y, lane);
 #pragma unroll
         for (int k = 0; k < R; ++k) y[k] = z[k];
@@ -500,6 +502,7 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_kernel(c
         const int64_t r = quotient(u, a.rows.nvec), u0 = r * a.rows.nvec;
         const int c0 = (int)(u - u0), c1 = (int)(min(end, u0 + a.rows.nvec) - u0);
         const char* row = a.rows.base + r * a.rows.ld_bytes;
+        if (!in_bounds(r < a.rows.n_rows && c0 < c1 && c1 <= a.rows.nvec, a.status)) return;
         Target x = ask_target(a, r);
         RowStat st;
         if constexpr (R > 0) {
@@ -550,11 +553,12 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) logprobs_few_kern
     if (warp == 0) x = ask_target(a, r);
     const int c0 = min(a.rows.nvec, (b * kWarps + warp) * a.span), c1 = min(a.rows.nvec, c0 + a.span);
     RowStat st = no_stat();
+    const bool some = c0 < c1 && in_bounds(r < a.rows.n_rows && c1 <= a.rows.nvec, a.status);
     if constexpr (R > 0) {
         clear_list<R>(q, 1, 0, 1, a.top_k);
-        if (c0 < c1) st = stream_row<kBf16, R>(a, row, c0, c1, q);
+        if (some) st = stream_row<kBf16, R>(a, row, c0, c1, q);
     } else {
-        if (c0 < c1) st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);
+        if (some) st = stream_row<kBf16, 0>(a, row, c0, c1, nullptr);
     }
     ask_logit<kBf16>(a, row, x);
     join_lanes(st, a.c);
