@@ -644,7 +644,8 @@ class Context:
     def token_logprobs(self, logits, targets=None, top_k: int = 0, temperature: float = 1.0, V: int | None = None,
                        stream=None) -> TokenLogprobs:
         """estp_token_logprobs on logits [rows, >= V]: ln p of `targets` (int32 [rows], negative: none),
-        the entropy, what the gradient needs, and the top_k greatest alternatives."""
+        the entropy, what the gradient needs, and the top_k greatest alternatives.  Uses the context's scratch: calls on
+        several streams that may overlap are ordered by the caller or take a context each."""
         import torch
         rows, V, ld = self._logits(logits, V)
         f32, dev = torch.float32, logits.device
@@ -701,7 +702,7 @@ class Context:
         tokens (teacher_ids int32, teacher_logits fp32 [rows, K]): the loss [rows] and, with grads, its
         gradient [rows, V] times row_weight [rows].  tail: teacher_logits are log probabilities
         at this temperature and the rest of the vocabulary is one bucket.  out: where the
-        gradient goes, logits itself allowed."""
+        gradient goes, logits itself allowed.  The loss alone uses the context's scratch, as token_logprobs does."""
         import torch
         rows, V, ld = self._logits(logits, V)
         K = teacher_ids.shape[-1]

@@ -15,8 +15,8 @@
 // those of the other CTAs of the SM.  Rows too long for that are read twice (distill_long_kernel), very short ones from the
 // caches (distill_short_kernel); the loss alone is one read (distill_eval_kernel).
 //
-// 2048 rows of 128256 bf16 tokens take 179 us (155 at the copy's rate; a block a row with both passes from memory: 419), 1021
-// of 152064 with the tail 131 (92).  Two exponentials a logit and some 110 instructions for 256 of them are issued at
+// 2048 rows of 128256 bf16 tokens take 177 us (155 at the copy's rate; a block a row with both passes from memory: 419), 1021
+// of 152064 with the tail 128 (92).  Two exponentials a logit and some 110 instructions for 256 of them are issued at
 // 2.2 a clock of 4: what is left is their latency where warps wait for the row's barrier.
 #include <type_traits>
 
@@ -359,8 +359,8 @@ __device__ __forceinline__ Two two_log(Two x) {
 
 // One warp.  From the fp32 sums on in two floats: where student and teacher agree, or both leave nearly everything to the
 // other tokens (a high temperature), the loss is a small difference of terms whose logarithms are off by 1e-6 in one
-// float, and with them a loss of 1e-3 has three digits left.  (64-bit arithmetic does as well and takes 10 % of the
-// whole call, as there are 2 such operations a clock on an SM.)
+// float, and with them a loss of 1e-3 has three digits left.  (64-bit arithmetic does as well, but there are 2 such
+// operations a clock on an SM: 2048 rows of 128256 took 210 us with it and 183 in two floats, one step apart.)
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const Teacher& t, const RowStat& st, const Factors& f) {
     const int lane = threadIdx.x & 31;
     if (!t.some) return 0.f;
@@ -832,7 +832,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) distill_rows_kernel(c
 // ------------------------------------------------------------------ the loss alone
 // A warp an equal piece of the flat run of units (vocab.cuh); of a row cut between warps each leaves its
 // statistics, and the one that leaves the last joins them in order and forms the loss.  1024 rows of 152064 tokens with 100
-// teacher logits in 64 us, which is what their log probabilities take (clusters as below: 75 to 105).
+// teacher logits in 63 to 66 us, 46 of bytes (clusters as above: 75 to 105).
 struct EvalArgs {
     DistillArgs d;
     VocabRows rows;
@@ -960,7 +960,9 @@ __global__ void __launch_bounds__(kVocabThreads, kVocabBlocks) distill_eval_kern
 // ------------------------------------------------------------------ many short rows
 // A warp a row: both passes read it from memory, the second from the caches.  Where a row is a few KB, a cluster's
 // barriers and its ninth warp take longer than the row.  By clusters and so, us: 8192 bf16 rows of 1000 tokens 85 and
-// 28, of 2500 88 and 41, 7880 of 4707 (589 units) 100 and 66, 8192 of 8000 105 and 105; 1000 of 4707 25 and 28.
+// 28, of 2500 88 and 41, 7880 of 4707 (589 units) 100 and 66, 8192 of 8000 105 and 105; 1000 of 4707 25 and 28.  (Calls back
+// to back, without the host: 8192 of 1000 22, 30000 of 4000 190, for 5 and 72 of bytes: in a warp the teacher's side, the
+// stream, the loss and the write stand one after another.)
 constexpr int kShortUnits = 256;    // at most, with a row for every sixth warp
 constexpr int kManyShortUnits = 640;  // at most, with one for every warp
 

@@ -9,12 +9,14 @@
 // whose warps join their parts in shared memory first.
 //
 // Bound: the read of the logits.  42 instructions and 8 exponentials for 256 bf16 logits leave the issue slots half idle
-// at the memory's rate: 4096 rows of 128256 tokens in 162 us (6.5 TB/s), 2048 of 152064 in 103; some 14 us of a call are
+// at the memory's rate: 4096 rows of 128256 tokens in 159 us (6.6 TB/s), 2048 of 152064 in 103; some 14 us of a call are
 // its launch, the first loads and the last row's join, which is what 1024 rows (60 us for 46 us of bytes) and less pay.
-// Alternatives add what their candidates take: 1537 rows of 152064 in 125 us with 64, 44 % of the instructions for
+// A batch that holds a mask is summed twice (vocab.cuh): with half of all tokens masked the 4096 rows take 217.
+// Alternatives add what their candidates take: 1537 rows of 152064 in 123 us with 64, 44 % of the instructions for
 // the lists, in chains that five warps a scheduler issue at 2.1 a clock.  Measured beside it: bounds not shared between the
 // warps of a row 133; candidates kept in no order and thinned out by the bits of their keys 127; the next batch copied into shared
-// memory meanwhile 140 and four blocks an SM with four loads 142 (both take more instructions).
+// memory meanwhile 140 and four blocks an SM with four loads 142 (both take more instructions).  20 alternatives take 104, 128
+// take 156: the kernel for more than 64 spills.
 //
 // The list.  A candidate is a 64-bit key: the logit's bits in the order of the numbers above the token's
 // index, inverted; so keys are unique, a greater key is a greater logit or the same one at a lower
@@ -720,7 +722,7 @@ __device__ __forceinline__ void grad_chunk(const char* row, char* out, int chunk
 // A warp a piece, as in the forward pass; a lane reads a unit before it writes it, so the gradient may
 // take the logits' place.
 //
-// Bound: the read and the write.  4096 rows of 128256 tokens in 339 us (6.2 TB/s of both); a kernel that only reads
+// Bound: the read and the write.  4096 rows of 128256 tokens in 331 to 341 us (6.2 TB/s of both and more); a kernel that only reads
 // and writes takes 323 to 343 with as many warps and loads.  Three blocks an SM of four loads a lane: 335, four blocks 341, two
 // of eight loads 333 but 26 instead of 23 for 501 fp32 rows of 32001.
 template <bool kBf16>
